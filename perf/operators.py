@@ -252,7 +252,7 @@ def _plain_product(s):
     if s["bias"] is not None:
         y = y + s["bias"][:, None]
     if s["case"]["relu"]:
-        y = torch.where(y > 0, y, 0.0)
+        y = torch.where(y < 0, 0.0, y)
     return _rows(y, s["offsets"], s["x"].shape[0]).to(DTYPES[s["case"]["out"]])
 
 
@@ -271,9 +271,12 @@ def _plain_product_dw(s):
 
 
 def _plain_logprobs(logits, targets, allowed, temperature, top):
-    z = logits.float() * (1.0 / temperature)
+    # a logit at or below -1e30 is a mask's: the lowest value of its type stands for minus infinity
+    raw = logits.float()
+    raw = torch.where(raw <= -1e30, -math.inf, raw)
     if allowed is not None:
-        z = torch.where(allowed, z, -math.inf)
+        raw = torch.where(allowed, raw, -math.inf)
+    z = raw * (1.0 / temperature)
     m = z.amax(1, keepdim=True)
     m = torch.where(m == -math.inf, 0.0, m)
     e = torch.exp(z - m)
@@ -287,7 +290,6 @@ def _plain_logprobs(logits, targets, allowed, temperature, top):
     out = {"logp": torch.where(targets < 0, 0.0, logp[:, 0]), "entropy": entropy[:, 0], "lse": lse[:, 0]}
     if top:
         # a stable sort: equal logits keep their order, so the lowest index comes first
-        raw = logits.float() if allowed is None else torch.where(allowed, logits.float(), -math.inf)
         order = torch.sort(raw, dim=1, descending=True, stable=True).indices[:, :top]
         if order.shape[1] < top:
             order = torch.nn.functional.pad(order, (0, top - order.shape[1]), value=-1)
