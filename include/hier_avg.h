@@ -267,6 +267,127 @@ int hier_avg_profile_every(hier_avg* h, int every);
 int hier_avg_profile_read(hier_avg* h, int kind, double* total_ms, int64_t* launches,
                           double* bytes, double* flops);
 
+/* ---------------------------------------------------------------------------
+ * Operators for models whose groups of rows have weights of their own (experts, or
+ * learners with batches of different sizes), for their loss over many classes, and
+ * for steps other than plain SGD.  Stateless but for the AdamW plan.  They run on the
+ * current device, asynchronously on `stream`, and allocate nothing.  All sums are held
+ * in fp32.
+ * ------------------------------------------------------------------------- */
+#define HA_TYPE_FP32 0
+#define HA_TYPE_BF16 1
+#define HA_TYPE_FP16 2
+
+/* Grouped products.  Rows [offsets[g], offsets[g+1]) of x (and dy) belong to group g,
+ * which has the weights W_g [outer, inner]; offsets_dev [groups + 1] int32 stays on the
+ * device and is not read by the host.  Groups may be empty and of any size; offsets are
+ * clamped to [0, rows], and one that goes back leaves its group empty.
+ *   hier_avg_grouped_product     y[t]  = act(W_g x[t] + b_g)
+ *   hier_avg_grouped_product_dx  dx[t] = W_g^T dy[t], zero where h[t] <= 0 (h_dev != NULL)
+ *   hier_avg_grouped_product_dw  dW_g  = sum over the group's t of dy[t] x[t]^T, and with
+ *                                db_dev db_g = sum of dy[t]; zero for an empty group
+ * Rows of y and dx that belong to no group are set to zero.
+ *   type          HA_TYPE_BF16 or HA_TYPE_FP16, of x, w, dy and h; products are exact and
+ *                 summed in fp32
+ *   y_type, ...   the inputs' type (rounded once) or HA_TYPE_FP32
+ *   *_ld          elements between rows; w_gs, dw_gs: between groups; unit stride inside
+ *                 rows.  bias_dev [groups, outer] and db_dev fp32, rows bias_ld / db_ld apart
+ *   relu          1: act(v) = max(v, 0), 0: act(v) = v
+ *   workspace_dev 16-byte aligned, of the bytes that hier_avg_grouped_product_workspace says
+ *                 (0 for operands whose address and strides are multiples of 16 bytes;
+ *                 others are first copied there)
+ * Errors: HA_EINVAL for sizes, types, strides or pointers out of range, HA_ENOMEM for a
+ * workspace that is too small, HA_EUNSUPPORTED for more than 1024 groups or 2^31 tiles,
+ * HA_ECUDA.  rows = 0 is valid (dW is then zero). */
+#define HA_GROUPED_FORWARD 0
+#define HA_GROUPED_DX 1
+#define HA_GROUPED_DW 2
+/* a: x (forward) or dy; b: w (forward, dx) or x (dw; b_gs is not read). */
+int hier_avg_grouped_product_workspace(int op, const void* a_dev, int64_t a_ld, const void* b_dev,
+                                       int64_t b_ld, int64_t b_gs, int groups, int64_t rows,
+                                       int inner, int outer, int64_t* bytes);
+int hier_avg_grouped_product(const void* x_dev, int64_t x_ld, const void* w_dev, int64_t w_ld,
+                             int64_t w_gs, int type, const int32_t* offsets_dev, int groups,
+                             int64_t rows, int inner, int outer, const float* bias_dev,
+                             int64_t bias_ld, int relu, void* y_dev, int64_t y_ld, int y_type,
+                             void* workspace_dev, int64_t workspace_bytes, void* stream);
+int hier_avg_grouped_product_dx(const void* dy_dev, int64_t dy_ld, const void* w_dev, int64_t w_ld,
+                                int64_t w_gs, int type, const int32_t* offsets_dev, int groups,
+                                int64_t rows, int inner, int outer, const void* h_dev,
+                                int64_t h_ld, void* dx_dev, int64_t dx_ld, int dx_type,
+                                void* workspace_dev, int64_t workspace_bytes, void* stream);
+int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, const void* x_dev, int64_t x_ld,
+                                int type, const int32_t* offsets_dev, int groups, int64_t rows,
+                                int inner, int outer, void* dw_dev, int64_t dw_ld, int64_t dw_gs,
+                                int dw_type, float* db_dev, int64_t db_ld, void* workspace_dev,
+                                int64_t workspace_bytes, void* stream);
+
+/* Log probabilities of given classes.  With z_j = logits_j / temperature over the allowed
+ * classes of a row:
+ *   lse = log sum_j e^{z_j},  logp = z_target - lse,  entropy = -sum_j p_j log p_j,
+ * and the `top` likeliest classes with their log probabilities, equal logits in the order
+ * of their index.
+ *   logits_dev  [rows, classes], rows ld apart, any HA_TYPE_*
+ *   targets_dev [rows], int32 or int64 (target_bytes 4 or 8); below 0: logp is 0 and has no
+ *               gradient; a target >= classes gives NaN
+ *   allowed_dev NULL, or one byte a class, not 0 where it is allowed: [rows, classes] with
+ *               rows allowed_ld apart, or [classes] for all rows with allowed_ld = 0
+ *   top         0 .. 32; top_logp_dev, top_index_dev [rows, top]
+ * A logit at or below -1e30 counts as not allowed.  A row without an allowed class has
+ * lse = logp = -inf and entropy 0; alternatives that do not exist have index -1 and
+ * -inf.  A row with NaN or +inf among its allowed logits gives NaN (indices -1).
+ * Errors: HA_EINVAL; HA_EUNSUPPORTED for top > 32 or more than 2^31 blocks; HA_ECUDA. */
+int hier_avg_token_logprobs(const void* logits_dev, int type, int64_t rows, int64_t classes,
+                            int64_t ld, const void* targets_dev, int target_bytes,
+                            const uint8_t* allowed_dev, int64_t allowed_ld, float temperature,
+                            int top, float* logp_dev, float* entropy_dev, float* lse_dev,
+                            float* top_logp_dev, int32_t* top_index_dev, void* stream);
+/* The gradient with respect to the logits, from the forward's lse and entropy and the
+ * gradients dlogp_dev and dentropy_dev [rows] (dentropy_dev NULL: zero, and entropy_dev is
+ * not read).  dlogits_dev has the logits' type and may be logits_dev itself (with the same
+ * ld).  Zero where a class is not allowed. */
+int hier_avg_token_logprobs_backward(const void* logits_dev, int type, int64_t rows,
+                                     int64_t classes, int64_t ld, const void* targets_dev,
+                                     int target_bytes, const uint8_t* allowed_dev,
+                                     int64_t allowed_ld, float temperature, const float* lse_dev,
+                                     const float* entropy_dev, const float* dlogp_dev,
+                                     const float* dentropy_dev, void* dlogits_dev,
+                                     int64_t dlogits_ld, void* stream);
+
+/* AdamW over many tensors in one launch:
+ *   m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2
+ *   p <- p (1 - lr decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32, g being the gradient times *grad_scale_dev (NULL: 1).
+ * A plan is made once for a list of pieces (contiguous runs of fp32 parameters, in order of
+ * their tensor): piece i is p_dev[i][0 .. n[i]), its 16-bit copy (copy_dev or an entry of it
+ * may be NULL) and its gradient, which starts at element grad_offset[i] of tensor[i]'s
+ * gradient; decay[i] is its weight decay.  The state arrays hold the pieces one after the
+ * other, each from a multiple of 256 elements on (zeros between them).
+ *   bits = 32   m_dev, v_dev: fp32 [elements]
+ *   bits = 8    m_dev, v_dev: e4m3 [elements], m_scale_dev, root_scale_dev: fp32
+ *               [elements / 256]; m = code * scale, and v_dev holds sqrt(v) in the same way,
+ *               rounded up or down at random by `seed` and the element's place.  A block with
+ *               a NaN or an infinity becomes NaN as a whole.
+ * hier_avg_adamw_bind copies the plan to table_dev (16-byte aligned) and keeps the addresses.
+ * t counts steps from 1.  Errors: HA_EINVAL (eps must be > 0, betas in [0, 1)), HA_ENOMEM,
+ * HA_ESTATE for a step before bind, HA_ECUDA. */
+typedef struct hier_avg_adamw hier_avg_adamw;
+int hier_avg_adamw_create(int bits, int n_tensors, int64_t n_pieces, const int* tensor,
+                          float* const* p_dev, void* const* copy_dev, int copy_type,
+                          const int64_t* n, const int64_t* grad_offset, const float* decay,
+                          hier_avg_adamw** out);
+void hier_avg_adamw_destroy(hier_avg_adamw* plan);
+int hier_avg_adamw_sizes(const hier_avg_adamw* plan, int64_t* elements, int64_t* table_bytes);
+int hier_avg_adamw_bind(hier_avg_adamw* plan, void* table_dev, int64_t table_bytes, void* m_dev,
+                        void* v_dev, float* m_scale_dev, float* root_scale_dev, void* stream);
+int hier_avg_adamw_step(hier_avg_adamw* plan, const void* const* grads_dev, int grad_type,
+                        double lr, double beta1, double beta2, double eps, int64_t t,
+                        const float* grad_scale_dev, uint32_t seed, void* stream);
+
+/* Synchronise `stream` and report a bounded wait inside a grouped product that ran out on
+ * this device (HA_ETIMEOUT, once; the outputs are then invalid) or an asynchronous error. */
+int hier_avg_operator_check(void* stream);
+
 const char* hier_avg_strerror(int status);
 const char* hier_avg_last_error(const hier_avg* h);
 

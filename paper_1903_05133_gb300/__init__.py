@@ -12,4 +12,8 @@ def __getattr__(name):
                 "local_global_average_buffer"):
         from . import hier_avg
         return getattr(hier_avg, name)
+    if name in ("grouped_product", "grouped_product_dx", "grouped_product_dw", "token_logprobs",
+                "token_logprobs_backward", "TokenLogprobs", "AdamW", "operator_check"):
+        from . import operators
+        return getattr(operators, name)
     raise AttributeError(name)

@@ -47,6 +47,36 @@ SIGNATURES = {
     "hier_avg_set_batch": (c_int, [c_void_p, c_int]),
     "hier_avg_profile_every": (c_int, [c_void_p, c_int]),
     "hier_avg_profile_read": (c_int, [c_void_p, c_int, P_double, P_int64, P_double, P_double]),
+    "hier_avg_grouped_product_workspace": (c_int, [c_int, c_void_p, c_int64, c_void_p, c_int64,
+                                                   c_int64, c_int, c_int64, c_int, c_int, P_int64]),
+    "hier_avg_grouped_product": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int64, c_int,
+                                         c_void_p, c_int, c_int64, c_int, c_int, c_void_p, c_int64,
+                                         c_int, c_void_p, c_int64, c_int, c_void_p, c_int64,
+                                         c_void_p]),
+    "hier_avg_grouped_product_dx": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int64, c_int,
+                                            c_void_p, c_int, c_int64, c_int, c_int, c_void_p,
+                                            c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64,
+                                            c_void_p]),
+    "hier_avg_grouped_product_dw": (c_int, [c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p,
+                                            c_int, c_int64, c_int, c_int, c_void_p, c_int64,
+                                            c_int64, c_int, c_void_p, c_int64, c_void_p, c_int64,
+                                            c_void_p]),
+    "hier_avg_token_logprobs": (c_int, [c_void_p, c_int, c_int64, c_int64, c_int64, c_void_p, c_int,
+                                        c_void_p, c_int64, c_float, c_int, c_void_p, c_void_p,
+                                        c_void_p, c_void_p, c_void_p, c_void_p]),
+    "hier_avg_token_logprobs_backward": (c_int, [c_void_p, c_int, c_int64, c_int64, c_int64,
+                                                 c_void_p, c_int, c_void_p, c_int64, c_float,
+                                                 c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                                 c_int64, c_void_p]),
+    "hier_avg_adamw_create": (c_int, [c_int, c_int, c_int64, c_void_p, c_void_p, c_void_p, c_int,
+                                      c_void_p, c_void_p, c_void_p, ctypes.POINTER(c_void_p)]),
+    "hier_avg_adamw_destroy": (None, [c_void_p]),
+    "hier_avg_adamw_sizes": (c_int, [c_void_p, P_int64, P_int64]),
+    "hier_avg_adamw_bind": (c_int, [c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_void_p,
+                                    c_void_p, c_void_p]),
+    "hier_avg_adamw_step": (c_int, [c_void_p, c_void_p, c_int, c_double, c_double, c_double,
+                                    c_double, c_int64, c_void_p, ctypes.c_uint32, c_void_p]),
+    "hier_avg_operator_check": (c_int, [c_void_p]),
     "hier_avg_strerror": (c_char_p, [c_int]),
     "hier_avg_last_error": (c_char_p, [c_void_p]),
 }

@@ -27,23 +27,8 @@ constexpr int64_t kTargetCtas = 152;   // persistent kernels: one CTA per SM of 
 constexpr int64_t kPieceChunks = 48;   // chunks per piece of a split tile (forward, backward)
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                                  const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  if (!fn) {
-    cudaDriverEntryPointQueryResult q;
-    void* p = nullptr;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
-                                         &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(p);
-  }
-  return fn;
-}
+using ha::EncodeTiledFn;
+using ha::encode_fn;
 
 struct ProfRec {
   int kind;
