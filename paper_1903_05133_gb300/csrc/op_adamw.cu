@@ -24,7 +24,7 @@ namespace ha {
 namespace {
 
 constexpr int kBlock = 256;         // elements that share a scale: one warp, 8 a lane
-constexpr int kChunk = 4096;        // elements of one CTA
+constexpr int kChunk = 2048;        // elements of one CTA: a block for each warp
 constexpr int kThreads = 256;
 constexpr float kTop = 448.0f;      // largest e4m3 value
 constexpr float kTiny = 1e-30f;     // a block whose largest magnitude is below is stored as 0
@@ -55,10 +55,26 @@ struct StepArgs {
   uint32_t seed;
 };
 
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ float rcp_fast(float x) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
+}
+
+// sqrt(x), rounded to nearest: the residual of x * (1 / sqrt(x)) corrects its last bit
+// (Markstein 1990).  From 2^-102 on all fp32 numbers give __fsqrt_rn's result (compared one by
+// one); below, where the residual underflows, some are off in the last bit, and below the
+// smallest normal number the result is too small (0 stays 0).
+__device__ __forceinline__ float sqrt_near(float x) {
+  float y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(max_nan(x, 1.17549435e-38f)));
+  const float s = __fmul_rn(x, y);
+  return __fmaf_rn(__fmaf_rn(-s, s, x), 0.5f * y, s);
 }
 
 // 20 random bits for place j: a multiplicative hash with the fractions of the golden
@@ -66,16 +82,19 @@ __device__ __forceinline__ float rcp_fast(float x) {
 __device__ __forceinline__ uint32_t random20(uint32_t j, uint32_t seed) {
   uint32_t x = (j + seed * 0xBB67AE85u) * 0x9E3779B9u;
   x = (x ^ (x >> 15)) * 0x6A09E667u;
-  return (x ^ (x >> 13)) >> 12;
+  return (x >> 12) ^ (x >> 25);        // (x ^ x >> 13) >> 12
 }
 
-// a >= 0 rounded to a value of e4m3's grid, up or down by the 20 random bits.  Above
-// 2^-6 the grid keeps 3 mantissa bits of fp32's 23; below it is even with step 2^-9,
-// which is the same truncation after adding 2^-6.
+// a >= 0 rounded to a value of e4m3's grid, up or down by the 20 random bits.  From 2^-6 on
+// the grid keeps 3 mantissa bits of fp32's 23; below it is even with step 2^-9, which is the
+// same truncation after adding 2^-6.  What is not 0 stays so.
+__device__ __forceinline__ float round_random_normal(float a, uint32_t r) {
+  return __uint_as_float((__float_as_uint(a) + r) & 0xFFF00000u);
+}
 __device__ __forceinline__ float round_random(float a, uint32_t r) {
   const float low = a < 0.015625f ? 0.015625f : 0.0f;
-  const float t = __uint_as_float((__float_as_uint(a + low) + r) & 0xFFF00000u) - low;
-  return fmaxf(t, 0.001953125f);
+  const float t = round_random_normal(a + low, r) - low;
+  return a == 0.0f ? 0.0f : fmaxf(t, 0.001953125f);
 }
 
 __device__ __forceinline__ uint32_t to_e4m3x4(const float* x) {
@@ -113,14 +132,11 @@ __device__ __forceinline__ void load_grad4(const G* g, float* x) {
 __device__ __forceinline__ float warp_abs_max(float a) {
   return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(a) & 0x7FFFFFFFu));
 }
-__device__ __forceinline__ float abs_max(float a, float b) {
-  return __uint_as_float(max(__float_as_uint(a) & 0x7FFFFFFFu, __float_as_uint(b) & 0x7FFFFFFFu));
-}
 
-// One CTA a chunk, one warp a block of 256 elements at a time, each lane two groups of
-// four consecutive elements, so that every load and store of a warp is contiguous.
+// One CTA a chunk, one warp a block of 256 elements, each lane two groups of four
+// consecutive elements, so that every load and store of a warp is contiguous.
 template <int BITS, typename G, int NG>
-__global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Grads<NG> grads,
+__global__ void __launch_bounds__(kThreads, 5) k_adamw(const __grid_constant__ Grads<NG> grads,
                                                     const __grid_constant__ StepArgs a) {
   const Chunk c = a.chunks[blockIdx.x];
   const G* g = static_cast<const G*>(grads.p[c.tensor - a.first_tensor]) + c.grad;
@@ -130,7 +146,8 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Grad
   const bool wide = ((reinterpret_cast<uintptr_t>(c.p) & 15) |
                      (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(G) - 1)) |
                      (reinterpret_cast<uintptr_t>(c.copy) & 7)) == 0;
-  for (int b0 = (threadIdx.x >> 5) * kBlock; b0 < c.n; b0 += kThreads / 32 * kBlock) {
+  const int b0 = (threadIdx.x >> 5) * kBlock;
+  if (b0 < c.n) {
     float p[8], gr[8], m[8], v[8];
     const bool full = wide && b0 + kBlock <= c.n;
     const int64_t s0 = c.state + b0;
@@ -177,53 +194,17 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Grad
       const float gi = __fmul_rn(gr[i], gs);
       m[i] = __fadd_rn(__fmul_rn(a.b1, m[i]), __fmul_rn(a.omb1, gi));
       v[i] = __fadd_rn(__fmul_rn(a.b2, v[i]), __fmul_rn(__fmul_rn(a.omb2, gi), gi));
-      root[i] = __fsqrt_rn(v[i]);
+      root[i] = sqrt_near(v[i]);
       p[i] = p[i] * keep - a.step * (m[i] * rcp_fast(root[i] * a.inv_c2 + a.eps));
       if constexpr (BITS == 8) {
-        m_top = abs_max(m_top, m[i]);
-        r_top = abs_max(r_top, root[i]);
-      }
-    }
-    uint32_t m8[2], r8[2];
-    if constexpr (BITS == 8) {
-      m_top = warp_abs_max(m_top);
-      r_top = warp_abs_max(r_top);
-      if (m_top < kTiny) m_top = 0.0f;
-      if (r_top < kTiny) r_top = 0.0f;
-      const float mi = m_top == 0.0f ? 0.0f : __fmul_rn(__frcp_rn(m_top), kTop);
-      const float ri = r_top == 0.0f ? 0.0f : __fmul_rn(__frcp_rn(r_top), kTop);
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        float x[4], y[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t j = static_cast<uint32_t>(s0) + q * 128 + lane * 4 + i;
-          x[i] = __fmul_rn(m[4 * q + i], mi);
-          const float w = __fmul_rn(root[4 * q + i], ri);
-          y[i] = w == 0.0f ? 0.0f : round_random(w, random20(j, a.seed));
-        }
-        m8[q] = to_e4m3x4(x);
-        r8[q] = to_e4m3x4(y);
-      }
-      if (lane == 0) {
-        a.m_scale[s0 / kBlock] = m_top * (1.0f / kTop);
-        a.v_scale[s0 / kBlock] = r_top * (1.0f / kTop);
+        m_top = max_nan(m_top, fabsf(m[i]));
+        r_top = max_nan(r_top, root[i]);
       }
     }
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       const int e = b0 + q * 128 + lane * 4;
-      const int64_t s = s0 + q * 128 + lane * 4;
       const float* x = p + 4 * q;
-      if constexpr (BITS == 32) {
-        __stcs(reinterpret_cast<float4*>(static_cast<float*>(a.m) + s),
-               make_float4(m[4 * q], m[4 * q + 1], m[4 * q + 2], m[4 * q + 3]));
-        __stcs(reinterpret_cast<float4*>(static_cast<float*>(a.v) + s),
-               make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
-      } else {
-        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.m) + s), m8[q]);
-        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v) + s), r8[q]);
-      }
       if (full) {
         __stcs(reinterpret_cast<float4*>(c.p + e), make_float4(x[0], x[1], x[2], x[3]));
         if (c.copy) {
@@ -246,6 +227,54 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Grad
                 static_cast<__half*>(c.copy)[e + i] = __float2half_rn(x[i]);
             }
           }
+      }
+    }
+    uint32_t m8[2], r8[2];
+    if constexpr (BITS == 8) {
+      m_top = warp_abs_max(m_top);
+      r_top = warp_abs_max(r_top);
+      if (m_top < kTiny) m_top = 0.0f;
+      if (r_top < kTiny) r_top = 0.0f;
+      const float mi = m_top == 0.0f ? 0.0f : __fmul_rn(__frcp_rn(m_top), kTop);
+      const float ri = r_top == 0.0f ? 0.0f : __fmul_rn(__frcp_rn(r_top), kTop);
+      float least = INFINITY;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        m[i] = __fmul_rn(m[i], mi);
+        root[i] = __fmul_rn(root[i], ri);
+        least = fminf(least, root[i]);
+      }
+      const uint32_t j = static_cast<uint32_t>(s0) + lane * 4;
+      if (__all_sync(~0u, least >= 0.015625f)) {       // nearly always: no value below 2^-6
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          root[i] = round_random_normal(root[i], random20(j + (i >> 2) * 128 + (i & 3), a.seed));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          root[i] = round_random(root[i], random20(j + (i >> 2) * 128 + (i & 3), a.seed));
+      }
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        m8[q] = to_e4m3x4(m + 4 * q);
+        r8[q] = to_e4m3x4(root + 4 * q);
+      }
+      if (lane == 0) {
+        a.m_scale[s0 / kBlock] = m_top * (1.0f / kTop);
+        a.v_scale[s0 / kBlock] = r_top * (1.0f / kTop);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int64_t s = s0 + q * 128 + lane * 4;
+      if constexpr (BITS == 32) {
+        __stcs(reinterpret_cast<float4*>(static_cast<float*>(a.m) + s),
+               make_float4(m[4 * q], m[4 * q + 1], m[4 * q + 2], m[4 * q + 3]));
+        __stcs(reinterpret_cast<float4*>(static_cast<float*>(a.v) + s),
+               make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
+      } else {
+        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.m) + s), m8[q]);
+        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v) + s), r8[q]);
       }
     }
   }
@@ -287,8 +316,9 @@ cudaError_t launch_range(const hier_avg_adamw* h, const void* const* grads, int 
 template <int BITS, typename G>
 cudaError_t launch_all(const hier_avg_adamw* h, const void* const* grads, const StepArgs& a,
                        cudaStream_t s) {
-  constexpr int kFew = 64, kMany = 3968;
+  constexpr int kFew = 64, kSome = 512, kMany = 3968;
   if (h->n_tensors <= kFew) return launch_range<BITS, G, kFew>(h, grads, 0, h->n_tensors, a, s);
+  if (h->n_tensors <= kSome) return launch_range<BITS, G, kSome>(h, grads, 0, h->n_tensors, a, s);
   for (int t = 0; t < h->n_tensors; t += kMany) {
     const int end = t + kMany < h->n_tensors ? t + kMany : h->n_tensors;
     const cudaError_t e = launch_range<BITS, G, kMany>(h, grads, t, end, a, s);

@@ -16,7 +16,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kThreads = 512;
+constexpr int kMaxWarps = 16;
 constexpr int kUnroll = 4;            // 16-byte loads in flight a thread
 constexpr int kCap = 2048;            // candidates kept before they are cut to the best
 constexpr int kMaxTop = 32;
@@ -36,30 +36,42 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 struct Stat {
   float m, S, A;      // m: largest logit as given (before the temperature)
 };
-// Where m starts.  A logit at or below it adds nothing, so a mask written with the lowest
-// finite value of bf16 or fp32 works as one of minus infinity does, and m stays finite.
-constexpr float kNone = -1e30f;
 
-// The sums of `b` added to those of `a`; c = log2(e) / temperature.
-__device__ __forceinline__ Stat join(Stat a, Stat b, float c) {
-  Stat r;
-  r.m = fmaxf(a.m, b.m);
-  const float da = max_nan((a.m - r.m) * c, -200.0f), db = max_nan((b.m - r.m) * c, -200.0f);
-  const float ea = exp2_fast(da), eb = exp2_fast(db);
-  r.S = a.S * ea + b.S * eb;
-  r.A = (a.A + a.S * da) * ea + (b.A + b.S * db) * eb;
+// Logits at or below this count as not allowed, so a mask written with the lowest finite value
+// of bf16 or fp32 works as one of minus infinity does.  They are raised to it on loading, which
+// keeps every difference finite, and a row whose largest logit it is has no class.  (bf16: the
+// largest value of the type that is not above -1e30.)
+template <typename T> constexpr float kNone = -1e30f;
+template <> constexpr float kNone<__nv_bfloat16> = -1.0002555517425873e30f;
+
+// Order of floats (no NaN) as unsigned integers, and back.
+__device__ __forceinline__ uint32_t ordered(float v) {
+  const uint32_t u = __float_as_uint(v);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float from_ordered(uint32_t o) {
+  return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+}
+
+// The warp's sums, the same in every lane; c = log2(e) / temperature.
+__device__ __forceinline__ Stat warp_join(Stat s, float c) {
+  const float m = from_ordered(__reduce_max_sync(~0u, ordered(s.m)));
+  const float d = max_nan((s.m - m) * c, -200.0f), e = exp2_fast(d);
+  Stat r = {m, s.S * e, (s.A + s.S * d) * e};
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    r.S += __shfl_xor_sync(~0u, r.S, o);
+    r.A += __shfl_xor_sync(~0u, r.A, o);
+  }
   return r;
 }
 
 // Keys order by value, equal values by lower index.
 __device__ __forceinline__ uint64_t key_of(float v, uint32_t index) {
-  const uint32_t u = __float_as_uint(v);
-  const uint32_t o = u & 0x80000000u ? ~u : u | 0x80000000u;
-  return (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~index);
+  return (static_cast<uint64_t>(ordered(v)) << 32) | static_cast<uint32_t>(~index);
 }
 __device__ __forceinline__ float key_value(uint64_t k) {
-  const uint32_t o = static_cast<uint32_t>(k >> 32);
-  return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+  return from_ordered(static_cast<uint32_t>(k >> 32));
 }
 __device__ __forceinline__ uint32_t key_index(uint64_t k) { return ~static_cast<uint32_t>(k); }
 // 0 orders below the key of every value, minus infinity's among them.
@@ -78,16 +90,19 @@ struct FwdArgs {
 
 struct TopState {
   uint64_t keys[kCap];
+  uint64_t best[kMaxTop];
+  uint64_t bar;                    // keys below it are not among the best
+  uint32_t warp_low[kMaxWarps];
   int count;
-  uint64_t bar;       // keys below it are not among the best
 };
 
-// Descending bitonic sort of s.keys[0, n), n a power of two, by the whole CTA.
-__device__ void sort_keys(uint64_t* keys, int n) {
+// Descending bitonic sort of keys[0, n), n a power of two, by the whole CTA.
+template <int THREADS>
+__device__ __noinline__ void sort_keys(uint64_t* keys, int n) {
   for (int k = 2; k <= n; k <<= 1)
     for (int j = k >> 1; j > 0; j >>= 1) {
       __syncthreads();
-      for (int i = threadIdx.x; i < n / 2; i += kThreads) {
+      for (int i = threadIdx.x; i < n / 2; i += THREADS) {
         const int x = ((i & ~(j - 1)) << 1) | (i & (j - 1)), y = x | j;
         const uint64_t a = keys[x], b = keys[y];
         const bool down = (x & k) == 0;
@@ -100,18 +115,34 @@ __device__ void sort_keys(uint64_t* keys, int n) {
   __syncthreads();
 }
 
-// Sorts the candidates and keeps the best `top`; the bar rises to the last of them.
-__device__ void cut(TopState& s, int top) {
+// Keeps the best `top` candidates, in order; the bar rises to the last of them.  Few
+// candidates (the common case) are ranked by counting the larger ones, by all threads at
+// once: `per` neighbours share a candidate.
+template <int THREADS>
+__device__ __noinline__ void cut(TopState& s, int top) {
   __syncthreads();
-  const int count = min(s.count, kCap);
-  int n = 64;
-  while (n < count) n <<= 1;
-  for (int i = count + threadIdx.x; i < n; i += kThreads) s.keys[i] = 0;
-  sort_keys(s.keys, n);
-  if (threadIdx.x == 0) {
-    s.count = min(count, top);
-    if (count >= top) s.bar = s.keys[top - 1];
+  const int count = min(s.count, kCap), tid = threadIdx.x;
+  if (count <= THREADS) {
+    int per = 32;
+    while (per > 1 && count * per > THREADS) per >>= 1;
+    const int c = tid / per, part = tid % per;
+    const uint64_t k = c < count ? s.keys[c] : ~0ull;
+    int rank = 0;
+#pragma unroll 4
+    for (int i = part; i < count; i += per) rank += s.keys[i] > k;
+    for (int o = per >> 1; o > 0; o >>= 1) rank += __shfl_xor_sync(~0u, rank, o);
+    if (c < count && part == 0 && rank < top) s.best[rank] = k;
+    __syncthreads();
+    if (tid < min(count, top)) s.keys[tid] = s.best[tid];
+  } else {
+    int n = 2 * THREADS;
+    while (n < count) n <<= 1;
+    for (int i = count + tid; i < n; i += THREADS) s.keys[i] = 0;
+    sort_keys<THREADS>(s.keys, n);
   }
+  if (tid == 0) s.count = min(count, top);
+  __syncthreads();
+  if (tid == 0 && count >= top) s.bar = s.keys[top - 1];
   __syncthreads();
 }
 
@@ -137,6 +168,8 @@ __device__ __forceinline__ void cluster_barrier() {
 }
 
 template <typename T> constexpr int kVec = 16 / sizeof(T);
+template <typename T> constexpr bool kIsBf16 = false;
+template <> constexpr bool kIsBf16<__nv_bfloat16> = true;
 
 template <typename T>
 __device__ __forceinline__ void unpack(uint4 w, float* v) {
@@ -149,45 +182,118 @@ __device__ __forceinline__ void unpack(uint4 w, float* v) {
   }
 }
 
-// Entries that are not allowed become minus infinity.
-template <int N>
-__device__ __forceinline__ void apply_mask(float* v, const uint8_t* a) {
-  uint32_t w[2];
-  if ((reinterpret_cast<uintptr_t>(a) & (N - 1)) == 0) {
-    if constexpr (N == 8) {
-      const uint2 x = *reinterpret_cast<const uint2*>(a);
-      w[0] = x.x; w[1] = x.y;
+// Raises a vector's entries to kNone where they are below it or not allowed; returns the
+// largest (not a NaN).  16-bit entries stay packed, two to an instruction.
+template <typename T>
+__device__ __forceinline__ float clean(uint4& w, const uint8_t* ok) {
+  constexpr int N = kVec<T>;
+  uint32_t* x = &w.x;
+  if (ok) {
+    uint32_t m[2];
+    if ((reinterpret_cast<uintptr_t>(ok) & (N - 1)) == 0) {
+      m[0] = *reinterpret_cast<const uint32_t*>(ok);
+      if constexpr (N == 8) m[1] = *reinterpret_cast<const uint32_t*>(ok + 4);
     } else {
-      w[0] = *reinterpret_cast<const uint32_t*>(a);
+#pragma unroll
+      for (int h = 0; h < N / 4; ++h)
+        m[h] = ok[4 * h] | (ok[4 * h + 1] << 8) | (ok[4 * h + 2] << 16) | (ok[4 * h + 3] << 24);
     }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool out = ((m[i >> 2] >> (8 * (i & 3))) & 0xFFu) == 0;
+      if constexpr (N == 4) {
+        if (out) x[i] = 0xFF800000u;                       // minus infinity
+      } else {
+        constexpr uint32_t inf = sizeof(T) == 2 && kIsBf16<T> ? 0xFF80u : 0xFC00u;
+        if (out) x[i >> 1] = i & 1 ? (x[i >> 1] & 0xFFFFu) | (inf << 16) : (x[i >> 1] & 0xFFFF0000u) | inf;
+      }
+    }
+  }
+  float top;
+  if constexpr (kIsBf16<T>) {
+    const __nv_bfloat162 low = __float2bfloat162_rn(kNone<T>);
+    __nv_bfloat162 h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      h[i] = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&x[i]), low);
+      x[i] = *reinterpret_cast<const uint32_t*>(&h[i]);
+    }
+    const __nv_bfloat162 t = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    top = fmaxf(__low2float(t), __high2float(t));
+  } else if constexpr (sizeof(T) == 2) {
+    __half2 h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = *reinterpret_cast<const __half2*>(&x[i]);
+    const __half2 t = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    top = fmaxf(__low2float(t), __high2float(t));
   } else {
 #pragma unroll
-    for (int h = 0; h < N / 4; ++h)
-      w[h] = a[4 * h] | (a[4 * h + 1] << 8) | (a[4 * h + 2] << 16) | (a[4 * h + 3] << 24);
+    for (int i = 0; i < 4; ++i) x[i] = __float_as_uint(max_nan(__uint_as_float(x[i]), kNone<T>));
+    top = fmaxf(fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])),
+                fmaxf(__uint_as_float(x[2]), __uint_as_float(x[3])));
   }
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (((w[i >> 2] >> (8 * (i & 3))) & 0xFFu) == 0) v[i] = -INFINITY;
+  return top;
 }
 
-template <int N>
-__device__ __forceinline__ void add_stat(Stat& s, const float* v, float c) {
-  float top = v[0];
-#pragma unroll
-  for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
+// Two floats an instruction.
+struct Pair { uint64_t w; };
+__device__ __forceinline__ Pair pair(float a, float b) {
+  Pair p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p.w) : "f"(a), "f"(b));
+  return p;
+}
+__device__ __forceinline__ void halves(Pair p, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.w));
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  Pair p;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(p.w) : "l"(a.w), "l"(b.w));
+  return p;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+  Pair p;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(p.w) : "l"(a.w), "l"(b.w));
+  return p;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair p;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(p.w) : "l"(a.w), "l"(b.w), "l"(c.w));
+  return p;
+}
+
+// A thread's sums, over even and odd entries apart.
+struct Sums {
+  float m;
+  Pair S, A;
+};
+// A new largest value: the sums are rescaled to it.
+__device__ __forceinline__ void raise(Sums& s, float top, float c) {
   if (top > s.m) {
     const float d = max_nan((s.m - top) * c, -200.0f), e = exp2_fast(d);
-    s.A = (s.A + s.S * d) * e;
-    s.S *= e;
+    s.A = mul2(fma2(s.S, pair(d, d), s.A), pair(e, e));
+    s.S = mul2(s.S, pair(e, e));
     s.m = top;
   }
+}
+__device__ __forceinline__ void add_pair(Sums& s, float a, float b, float c) {
+  const Pair d = mul2(add2(pair(a, b), pair(-s.m, -s.m)), pair(c, c));
+  float x, y;
+  halves(d, x, y);
+  const Pair e = pair(exp2_fast(x), exp2_fast(y));
+  s.S = add2(s.S, e);
+  s.A = fma2(e, d, s.A);
+}
+template <typename T>
+__device__ __forceinline__ void add_vec(Sums& s, const uint4& w, float c) {
+  float v[kVec<T>];
+  unpack<T>(w, v);
+  if constexpr (sizeof(T) == 2 && !kIsBf16<T>) {
+    // minus infinity in fp16 has not been raised yet
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    // minus infinity gives 2^-200 = 0; NaN stays
-    const float d = max_nan((v[i] - s.m) * c, -200.0f), e = exp2_fast(d);
-    s.S += e;
-    s.A = fmaf(e, d, s.A);
+    for (int i = 0; i < kVec<T>; ++i) v[i] = max_nan(v[i], kNone<T>);
   }
+#pragma unroll
+  for (int i = 0; i < kVec<T>; i += 2) add_pair(s, v[i], v[i + 1], c);
 }
 
 __device__ __forceinline__ int64_t target_of(const void* targets, bool wide, int64_t row) {
@@ -195,11 +301,11 @@ __device__ __forceinline__ int64_t target_of(const void* targets, bool wide, int
 }
 
 // One cluster a row; its CTAs take equal shares of the row's 16-byte vectors.
-template <typename T, bool TOP, bool MASK>
-__global__ void __launch_bounds__(kThreads, TOP ? 2 : 3) k_logprobs(const FwdArgs a) {
-  constexpr int V = kVec<T>;
-  __shared__ Stat warp_stat[kThreads / 32];
-  __shared__ Stat cta_stat;
+template <typename T, bool TOP, bool MASK, int THREADS>
+__global__ void __launch_bounds__(THREADS, (TOP ? 1024 : 1536) / THREADS) k_logprobs(const __grid_constant__ FwdArgs a) {
+  constexpr int V = kVec<T>, kWarps = THREADS / 32;
+  __shared__ Stat warp_stat[kWarps];
+  __shared__ Stat cta_stat, row_stat;
   extern __shared__ __align__(16) unsigned char dyn[];
   TopState& ts = *reinterpret_cast<TopState*>(dyn);
 
@@ -209,18 +315,22 @@ __global__ void __launch_bounds__(kThreads, TOP ? 2 : 3) k_logprobs(const FwdArg
   const int64_t row = blockIdx.x / parts;
   const T* z = static_cast<const T*>(a.logits) + row * a.ld;
   const uint8_t* ok = MASK ? a.allowed + row * a.allowed_ld : nullptr;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31;
   const float c = a.inv_t * kLog2e;
+  const int classes = static_cast<int>(a.classes);
 
   // The vectors start at the row's first 16-byte boundary; the entries before and after
   // them are taken one by one, by the first and the last CTA.
   const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
-  const int64_t head = min(a.classes, static_cast<int64_t>(shift ? V - shift : 0));
-  const int64_t vecs = (a.classes - head) / V;
-  const int64_t v0 = vecs * rank / parts, v1 = vecs * (rank + 1) / parts;
-  const int64_t tail = head + vecs * V;
+  const int head = min(classes, shift ? V - shift : 0);
+  const int vecs = (classes - head) / V;
+  const int v0 = static_cast<int>(static_cast<int64_t>(vecs) * rank / parts);
+  const int v1 = static_cast<int>(static_cast<int64_t>(vecs) * (rank + 1) / parts);
+  const int tail = head + vecs * V;
+  const T* zv = z + head;
+  const uint8_t* okv = MASK ? ok + head : nullptr;
 
-  Stat s = {kNone, 0.0f, 0.0f};
+  Sums sums = {kNone<T>, pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
   if (TOP) {
     if (tid == 0) {
       ts.count = 0;
@@ -229,144 +339,168 @@ __global__ void __launch_bounds__(kThreads, TOP ? 2 : 3) k_logprobs(const FwdArg
     __syncthreads();
   }
 
-  const int64_t rounds = (v1 - v0 + kThreads * kUnroll - 1) / (kThreads * kUnroll);
-  for (int64_t r = 0; r <= rounds; ++r) {
-    // round 0 .. rounds-1: vectors; the last: the single entries at the row's ends
-    float v[kUnroll][V];
-    int64_t at[kUnroll];
-    if (r < rounds) {
-      uint4 w[kUnroll];
+  // What is left over of the row: at most 2 (V - 1) entries.
+  int one = -1;
+  float one_z = kNone<T>;
+  if (rank == 0 && tid < head) one = tid;
+  if (rank == parts - 1 && tid >= 32 && tail + tid - 32 < classes) one = tail + tid - 32;
+  if (one >= 0 && (!MASK || ok[one])) {
+    one_z = max_nan(Elem<T>::up(z[one]), kNone<T>);
+    sums.m = one_z;
+    sums.S = pair(1.0f, 0.0f);
+  }
+
+  for (int r = v0; r < v1; r += THREADS * kUnroll) {
+    uint4 w[kUnroll];
+    float top[kUnroll];
+    const bool whole = r + THREADS * kUnroll <= v1;     // without checks
+    if (whole) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const int64_t i = v0 + (r * kUnroll + u) * kThreads + tid;
-        at[u] = i < v1 ? head + i * V : -1;
-        if (i < v1) w[u] = __ldcs(reinterpret_cast<const uint4*>(z + at[u]));
-      }
+      for (int u = 0; u < kUnroll; ++u) w[u] = __ldcs(reinterpret_cast<const uint4*>(zv) + r + u * THREADS + tid);
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        if (at[u] < 0) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) v[u][i] = -INFINITY;
-          continue;
-        }
-        unpack<T>(w[u], v[u]);
-        if (MASK) apply_mask<V>(v[u], ok + at[u]);
-        add_stat<V>(s, v[u], c);
-      }
+      for (int u = 0; u < kUnroll; ++u)
+        top[u] = clean<T>(w[u], MASK ? okv + (r + u * THREADS + tid) * V : nullptr);
     } else {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
-        at[u] = -1;
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[u][i] = -INFINITY;
+        const int i = r + u * THREADS + tid;
+        top[u] = kNone<T>;
+        if (i < v1) w[u] = __ldcs(reinterpret_cast<const uint4*>(zv) + i);
       }
-      int64_t i = -1;
-      if (rank == 0 && tid < head) i = tid;
-      if (rank == parts - 1 && tid >= 32 && tail + tid - 32 < a.classes) i = tail + tid - 32;
-      if (i >= 0 && (!MASK || ok[i])) {
-        at[0] = i;
-        v[0][0] = Elem<T>::up(z[i]);
-        add_stat<1>(s, v[0], c);
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const int i = r + u * THREADS + tid;
+        if (i < v1) top[u] = clean<T>(w[u], MASK ? okv + i * V : nullptr);
       }
     }
-    if (TOP) {
-      float most = -INFINITY;
+    raise(sums, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), c);
+    static_assert(kUnroll == 4, "");
+    if (whole) {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) add_vec<T>(sums, w[u], c);
+    } else {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u)
+        if (r + u * THREADS + tid < v1) add_vec<T>(sums, w[u], c);
+    }
+  }
+
+  if (TOP) {
+    // A bound from below for the best: every warp has `share` threads whose largest entry
+    // reaches the warp's bound, all warps together at least `top` entries.
+    const int share = (a.top + kWarps - 1) / kWarps, warp = tid >> 5;
+    const uint32_t most = ordered(sums.m);
+    uint32_t left = most, low = 0;
+    for (int i = 0; i < share; ++i) {
+      low = __reduce_max_sync(~0u, left);
+      // the threads that hold it are many only for equal values; one of them leaves
+      if (lane == __ffs(__ballot_sync(~0u, left == low)) - 1) left = 0;
+    }
+    if (lane == 0) ts.warp_low[warp] = low;
+    __syncthreads();
+    low = __reduce_min_sync(~0u, ts.warp_low[lane % kWarps]);
+    // Entries over the bar become candidates.  They are among the vectors of the threads whose
+    // largest entry is over it; the lanes of a warp read such threads' vectors again together,
+    // `per` lanes a thread.  What finds no room waits until the candidates have been cut to
+    // the best and the bar raised.
+    uint32_t hot = __ballot_sync(~0u, sums.m > kNone<T> && most >= low);
+    bool one_done = !(one_z > kNone<T>);
+    int per = 1;
+    while (per < 32 && v0 + per * THREADS < v1) per *= 2;
+    const int skip = lane / per;
+    int j0 = 0;                                       // first of the threads' vectors
+    uint32_t done = 0;                                // entries of this lane's vector
+    while (true) {
+      uint64_t bar = static_cast<uint64_t>(low) << 32;
+      if (ts.bar > bar) bar = ts.bar;
+      const float bar_value = key_value(bar);
+      auto offer = [&](float x, int index) {          // false: no room
+        const uint64_t k = key_of(x, static_cast<uint32_t>(index));
+        if (!(x > kNone<T>) || k < bar) return true;
+        const int place = atomicAdd(&ts.count, 1);
+        if (place < kCap) ts.keys[place] = k;
+        return place < kCap;
+      };
+      if (!one_done) one_done = offer(one_z, one);
+      bool waiting = !one_done;
+      while (hot && !__any_sync(~0u, waiting)) {
+        uint32_t rest = hot;
+        for (int x = 0; x < skip; ++x) rest &= rest - 1;
+        const int i = v0 + (j0 + lane % per) * THREADS + warp * 32 + __ffs(rest) - 1;
+        if (rest && i < v1) {
+          uint4 x = *(reinterpret_cast<const uint4*>(zv) + i);
+          if (!(clean<T>(x, MASK ? okv + i * V : nullptr) < bar_value)) {
+            float v[V];
+            unpack<T>(x, v);
 #pragma unroll
-        for (int i = 0; i < V; ++i) most = fmaxf(most, v[u][i]);
-      if (r == 0 && rounds > 0) {
-        // The best `top` of the threads' largest entries bound the best of all from below.
-        uint64_t k = 0;
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-          for (int i = V - 1; i >= 0; --i)
-            if (v[u][i] == most && most > kNone) {
-              const uint64_t n = key_of(most, static_cast<uint32_t>(at[u] + i));
-              k = n > k ? n : k;
-            }
-        if (k) ts.keys[atomicAdd(&ts.count, 1)] = k;
-        cut(ts, a.top);
-        if (tid == 0) ts.count = 0;
-        __syncthreads();
-      }
-      // Entries over the bar become candidates.  What does not fit waits until the
-      // candidates have been cut to the best and the bar raised.
-      bool waiting = true;
-      uint32_t done[kUnroll] = {};
-      while (true) {
-        const uint64_t bar = ts.bar;
-        const float low = key_value(bar);
-        if (waiting) {
-          waiting = false;
-          if (!(most < low) || bar == 0) {
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-              for (int i = 0; i < V; ++i) {
-                if (!(v[u][i] > kNone) || (done[u] >> i & 1)) continue;
-                const uint64_t k = key_of(v[u][i], static_cast<uint32_t>(at[u] + i));
-                if (k >= bar) {
-                  const int place = atomicAdd(&ts.count, 1);
-                  if (place < kCap) {
-                    ts.keys[place] = k;
-                    done[u] |= 1u << i;
-                  } else {
-                    waiting = true;
-                  }
-                }
+            for (int e = 0; e < V; ++e)
+              if (!(done >> e & 1u)) {
+                if (offer(v[e], head + i * V + e)) done |= 1u << e;
+                else waiting = true;
               }
           }
         }
-        if (!__syncthreads_or(waiting)) break;
-        cut(ts, a.top);
+        if (__any_sync(~0u, waiting)) break;
+        done = 0;
+        j0 += per;
+        if (v0 + j0 * THREADS >= v1) {
+          j0 = 0;
+          for (int x = 0; x < 32 / per; ++x) hot &= hot - 1;
+        }
       }
+      if (!__syncthreads_or(waiting)) break;
+      cut<THREADS>(ts, a.top);
     }
   }
 
   // Threads, warps and CTAs of the row join their sums.
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const Stat b = {__shfl_xor_sync(~0u, s.m, o), __shfl_xor_sync(~0u, s.S, o), __shfl_xor_sync(~0u, s.A, o)};
-    s = join(s, b, c);
+  Stat s = {sums.m, 0.0f, 0.0f};
+  {
+    float x, y;
+    halves(sums.S, x, y);
+    s.S = x + y;
+    halves(sums.A, x, y);
+    s.A = x + y;
   }
-  if ((tid & 31) == 0) warp_stat[tid >> 5] = s;
-  if (TOP) cut(ts, a.top);
+  s = warp_join(s, c);
+  if (lane == 0) warp_stat[tid >> 5] = s;
+  if (TOP) cut<THREADS>(ts, a.top);
   __syncthreads();
   if (tid < 32) {
-    s = tid < kThreads / 32 ? warp_stat[tid] : Stat{kNone, 0.0f, 0.0f};
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const Stat b = {__shfl_xor_sync(~0u, s.m, o), __shfl_xor_sync(~0u, s.S, o), __shfl_xor_sync(~0u, s.A, o)};
-      s = join(s, b, c);
-    }
+    s = warp_join(tid < kWarps ? warp_stat[tid] : Stat{kNone<T>, 0.0f, 0.0f}, c);
     if (tid == 0) cta_stat = s;
   }
   if (parts > 1) {
     cluster_barrier();
     if (rank == 0) {
-      s = cta_stat;
-      for (uint32_t q = 1; q < parts; ++q)
-        s = join(s, {from_cta(&cta_stat.m, q), from_cta(&cta_stat.S, q), from_cta(&cta_stat.A, q)}, c);
+      if (tid < 32) {
+        // one lane a CTA (at most kMaxCluster), so that their loads are in flight together
+        s = {kNone<T>, 0.0f, 0.0f};
+        if (tid < static_cast<int>(parts))
+          s = {from_cta(&cta_stat.m, tid), from_cta(&cta_stat.S, tid), from_cta(&cta_stat.A, tid)};
+        s = warp_join(s, c);
+        if (tid == 0) row_stat = s;
+      }
       if (TOP) {
         // the other CTAs' best after this one's
-        for (int i = tid; i < static_cast<int>(parts - 1) * kMaxTop; i += kThreads) {
+        for (int i = tid; i < static_cast<int>(parts - 1) * kMaxTop; i += THREADS) {
           const int q = 1 + i / kMaxTop, k = i % kMaxTop;
-          if (k < from_cta(&ts.count, q)) ts.keys[atomicAdd(&ts.count, 1)] = from_cta(&ts.keys[k], q);
+          const uint64_t key = from_cta(&ts.keys[k], q);
+          if (k < from_cta(&ts.count, q)) ts.keys[atomicAdd(&ts.count, 1)] = key;
         }
-        cut(ts, a.top);
+        cut<THREADS>(ts, a.top);
       }
     }
     cluster_barrier();
     if (rank != 0) return;
+    s = row_stat;
   } else {
     __syncthreads();
     s = cta_stat;
   }
 
   const float log_s = log2f(s.S);
-  const bool none = s.S == 0.0f;
+  const bool none = !(s.m > kNone<T>) && s.S == s.S;       // NaN stays
   const float lse = none ? -INFINITY : fmaf(s.m, a.inv_t, log_s * kLn2);
   if (tid == 0) {
     const int64_t t = target_of(a.targets, a.wide_targets, row);
@@ -375,7 +509,7 @@ __global__ void __launch_bounds__(kThreads, TOP ? 2 : 3) k_logprobs(const FwdArg
       lp = NAN;
     } else if (t >= 0) {
       float zt = Elem<T>::up(z[t]);
-      if (zt <= kNone || (MASK && !ok[t])) zt = -INFINITY;
+      if (zt <= kNone<T> || (MASK && !ok[t])) zt = -INFINITY;
       lp = none ? -INFINITY : ((zt - s.m) * c - log_s) * kLn2;
     }
     a.logp[row] = lp;
@@ -405,19 +539,22 @@ struct BwdArgs {
 
 // d_j = (g (1[j = t] - p_j) - h p_j (log p_j + H)) / temperature, with p_j = e^(z_j - lse)
 // read back from the forward's lse and entropy H; g and h are the gradients of logp and of
-// the entropy.  p (log p + H) is taken as 0 where p is.
-template <typename T, bool ENT>
-__device__ __forceinline__ float grad_of(float z, float inv_t, float lse, float g, float h, float ent2) {
-  const float d = max_nan(fmaf(z, inv_t, -lse) * kLog2e, -200.0f), p = exp2_fast(d);
-  return ENT ? -p * fmaf(h, d + ent2, g) : -p * g;
+// the entropy.  With d = log2 p_j this is -p (h' d + k) plus g at the target.
+template <bool ENT>
+__device__ __forceinline__ float grad_of(float z, float inv_t, float lse, float h, float k) {
+  const float d = fmaf(z, inv_t, -lse) * kLog2e;
+  if constexpr (!ENT) return -exp2_fast(d) * k;
+  const float f = max_nan(d, -200.0f);                   // minus infinity times 0
+  return -exp2_fast(f) * fmaf(h, f, k);
 }
 
 constexpr int kBwdThreads = 256;
 constexpr int kBwdUnroll = 4;
 
-// grid.x: pieces of kBwdThreads * kBwdUnroll vectors of a row; grid.y: rows (strided).
+// A CTA takes kBwdThreads * kBwdUnroll vectors of a row.
 template <typename T, bool ENT, bool MASK>
-__global__ void __launch_bounds__(kBwdThreads) k_logprobs_backward(const BwdArgs a, int pieces) {
+__global__ void __launch_bounds__(kBwdThreads) k_logprobs_backward(const __grid_constant__ BwdArgs a,
+                                                                  int pieces) {
   constexpr int V = kVec<T>;
   const int64_t row = blockIdx.x / pieces;
   const int piece = static_cast<int>(blockIdx.x % pieces);
@@ -425,40 +562,53 @@ __global__ void __launch_bounds__(kBwdThreads) k_logprobs_backward(const BwdArgs
   T* out = static_cast<T*>(a.out) + row * a.out_ld;
   const uint8_t* ok = MASK ? a.allowed + row * a.allowed_ld : nullptr;
   const int tid = threadIdx.x;
-  const int64_t t = target_of(a.targets, a.wide_targets, row);
-  const float lse = a.lse[row];
-  const bool none = lse == -INFINITY;            // nothing allowed: no gradient
-  const float g0 = t < 0 || none ? 0.0f : a.dlogp[row];
-  const float g = g0 * a.inv_t;
-  // d is in units of log 2
-  const float h = ENT && !none ? a.dentropy[row] * a.inv_t * kLn2 : 0.0f;
-  const float ent2 = ENT && !none ? a.entropy[row] * kLog2e : 0.0f;
-
+  const int classes = static_cast<int>(a.classes);
   const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
-  const int64_t head = min(a.classes, static_cast<int64_t>(shift ? V - shift : 0));
-  const int64_t vecs = (a.classes - head) / V;
-  const int64_t tail = head + vecs * V;
-  const bool wide_out = ((reinterpret_cast<uintptr_t>(out + head)) & 15) == 0;
-
-  const int64_t base = static_cast<int64_t>(piece) * kBwdThreads * kBwdUnroll;
+  const int head = min(classes, shift ? V - shift : 0);
+  const int vecs = (classes - head) / V;
+  const int tail = head + vecs * V;
+  const int base = piece * kBwdThreads * kBwdUnroll + tid;
   uint4 w[kBwdUnroll];
 #pragma unroll
   for (int u = 0; u < kBwdUnroll; ++u) {
-    const int64_t i = base + u * kBwdThreads + tid;
-    if (i < vecs) w[u] = __ldcs(reinterpret_cast<const uint4*>(z + head + i * V));
+    const int i = base + u * kBwdThreads;
+    if (i < vecs) w[u] = __ldcs(reinterpret_cast<const uint4*>(z + head) + i);
   }
+
+  const int64_t t64 = target_of(a.targets, a.wide_targets, row);
+  const int t = t64 < 0 || t64 >= a.classes ? -1 : static_cast<int>(t64);
+  const float lse0 = a.lse[row];
+  const bool none = lse0 == -INFINITY;           // nothing allowed: no gradient
+  const float lse = none ? INFINITY : lse0;      // every p is then 0
+  const float g = t64 < 0 || none ? 0.0f : a.dlogp[row] * a.inv_t;
+  const float h0 = ENT && !none ? a.dentropy[row] * a.inv_t : 0.0f;
+  const float h = h0 * kLn2;                     // d is in units of log 2
+  const float k = ENT && !none ? fmaf(h0, a.entropy[row], g) : g;
+  const bool wide_out = ((reinterpret_cast<uintptr_t>(out + head)) & 15) == 0;
+  const int t_vec = t >= head && t < tail ? (t - head) / V : -1;
+
 #pragma unroll
   for (int u = 0; u < kBwdUnroll; ++u) {
-    const int64_t i = base + u * kBwdThreads + tid;
+    const int i = base + u * kBwdThreads;
     if (i >= vecs) continue;
+    const int at = head + i * V;
     float v[V];
     unpack<T>(w[u], v);
-    const int64_t at = head + i * V;
-    if (MASK) apply_mask<V>(v, ok + at);
+    uint32_t off = 0;                            // entries that are not allowed
+    if (MASK) {
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const float x = none ? 0.0f : grad_of<T, ENT>(v[k], a.inv_t, lse, g, h, ent2);
-      v[k] = at + k == t && v[k] > kNone ? x + g : x;
+      for (int x = 0; x < V; ++x) off |= ok[at + x] ? 0u : 1u << x;
+    }
+    const float zt = i == t_vec ? Elem<T>::up(z[t]) : -INFINITY;
+#pragma unroll
+    for (int x = 0; x < V; ++x) {
+      v[x] = grad_of<ENT>(v[x], a.inv_t, lse, h, k);
+      if (MASK && (off >> x & 1u)) v[x] = 0.0f;
+    }
+    if (i == t_vec && zt > kNone<T> && !(MASK && !ok[t])) {
+#pragma unroll
+      for (int x = 0; x < V; ++x)
+        if (at + x == t) v[x] += g;
     }
     if (wide_out) {
       uint4 o;
@@ -469,35 +619,35 @@ __global__ void __launch_bounds__(kBwdThreads) k_logprobs_backward(const BwdArgs
       __stcs(reinterpret_cast<uint4*>(out + at), o);
     } else {
 #pragma unroll
-      for (int k = 0; k < V; ++k) out[at + k] = Elem<T>::down(v[k]);
+      for (int x = 0; x < V; ++x) out[at + x] = Elem<T>::down(v[x]);
     }
   }
   if (piece == 0) {
-    int64_t i = -1;
+    int i = -1;
     if (tid < head) i = tid;
-    if (tid >= 32 && tail + tid - 32 < a.classes) i = tail + tid - 32;
+    if (tid >= 32 && tail + tid - 32 < classes) i = tail + tid - 32;
     if (i >= 0) {
-      const float z1 = MASK && !ok[i] ? -INFINITY : Elem<T>::up(z[i]);
-      const float x = none ? 0.0f : grad_of<T, ENT>(z1, a.inv_t, lse, g, h, ent2);
-      out[i] = Elem<T>::down(i == t && z1 > kNone ? x + g : x);
+      const float z1 = Elem<T>::up(z[i]);
+      const bool in = !MASK || ok[i];
+      const float x = in ? grad_of<ENT>(z1, a.inv_t, lse, h, k) : 0.0f;
+      out[i] = Elem<T>::down(in && i == t && z1 > kNone<T> ? x + g : x);
     }
   }
 }
 
 // CTAs a row: enough that all rows fill the GPU twice (152 SMs), as long as each keeps
-// at least two rounds of loads.
+// half a round of loads.
 int cluster_size(int64_t rows, int64_t bytes) {
   int parts = 1;
-  while (parts < kMaxCluster && rows * parts < 304 && bytes / (2 * parts) >= kThreads * 16) parts *= 2;
+  while (parts < kMaxCluster && rows * parts < 304 && bytes / (2 * parts) >= 512 * kUnroll * 8) parts *= 2;
   return parts;
 }
 
-template <typename T, bool TOP, bool MASK>
-cudaError_t launch_forward(const FwdArgs& a, cudaStream_t s) {
-  const int parts = cluster_size(a.rows, a.classes * static_cast<int64_t>(sizeof(T)));
+template <typename T, bool TOP, bool MASK, int THREADS>
+cudaError_t launch_forward(const FwdArgs& a, int parts, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(a.rows * parts));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(THREADS);
   cfg.dynamicSmemBytes = TOP ? sizeof(TopState) : 0;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
@@ -506,15 +656,24 @@ cudaError_t launch_forward(const FwdArgs& a, cudaStream_t s) {
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_logprobs<T, TOP, MASK>, a);
+  cfg.numAttrs = parts > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, k_logprobs<T, TOP, MASK, THREADS>, a);
+}
+
+// Few CTAs take 512 threads each; where they fill the GPU, half the threads have half the
+// cost of a row's end and overlap it with other CTAs' loads (8192 rows of 32768 bf16: 127 us with
+// 512 threads, 108 us with 256).
+template <typename T, bool TOP, bool MASK>
+cudaError_t forward_rows(const FwdArgs& a, cudaStream_t s) {
+  const int parts = cluster_size(a.rows, a.classes * static_cast<int64_t>(sizeof(T)));
+  return parts * a.rows < 152 ? launch_forward<T, TOP, MASK, 512>(a, parts, s)
+                                   : launch_forward<T, TOP, MASK, 256>(a, parts, s);
 }
 
 template <typename T>
 cudaError_t forward_type(const FwdArgs& a, cudaStream_t s) {
-  if (a.top)
-    return a.allowed ? launch_forward<T, true, true>(a, s) : launch_forward<T, true, false>(a, s);
-  return a.allowed ? launch_forward<T, false, true>(a, s) : launch_forward<T, false, false>(a, s);
+  if (a.top) return a.allowed ? forward_rows<T, true, true>(a, s) : forward_rows<T, true, false>(a, s);
+  return a.allowed ? forward_rows<T, false, true>(a, s) : forward_rows<T, false, false>(a, s);
 }
 
 template <typename T, bool ENT, bool MASK>

@@ -9,7 +9,9 @@ is given.  A call on ``stream`` makes its results and workspace there.
 from __future__ import annotations
 
 import ctypes
+from array import array
 from contextlib import nullcontext
+from operator import attrgetter
 from typing import Dict, List, NamedTuple, Optional, Sequence
 
 import torch
@@ -19,14 +21,20 @@ from ._lib import c_int64, c_void_p, check
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 FORWARD, DX, DW = 0, 1, 2
+_SHAPE, _DTYPE, _CUDA = attrgetter("shape"), attrgetter("dtype"), attrgetter("is_cuda")
+_ADDRESS, _CONTIGUOUS = torch.Tensor.data_ptr, torch.Tensor.is_contiguous
 BLOCK = 256                     # elements that share a scale of the 8-bit AdamW states
 MAX_TOP = 32
 
 
-def _on(stream):
-    """The stream's handle and a context that allocates on it."""
+_NOWHERE = nullcontext()
+_RAW_STREAM = torch._C._cuda_getCurrentRawStream    # current_stream() makes an object: 5 us
+
+
+def _on(t, stream):
+    """The stream's handle (the current one of t's device) and a context that allocates on it."""
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream, nullcontext()
+        return _RAW_STREAM(t.get_device()), _NOWHERE
     return stream.cuda_stream, torch.cuda.stream(stream)
 
 
@@ -36,29 +44,33 @@ def _need(ok: bool, message: str) -> None:
 
 
 def _rows_of(name: str, t: torch.Tensor, dtypes, rows: Optional[int] = None,
-             cols: Optional[int] = None) -> None:
-    """t is a CUDA matrix of one of the types whose rows have unit stride."""
-    _need(t.is_cuda and t.dim() == 2 and t.dtype in dtypes,
-          f"{name} must be a CUDA matrix of {' or '.join(str(d) for d in dtypes)}")
-    _need(rows is None or t.shape[0] == rows, f"{name} must have {rows} rows")
-    _need(cols is None or t.shape[1] == cols, f"{name} must have {cols} columns")
-    _need(t.shape[1] >= 1 and (t.stride(1) == 1 or t.shape[1] == 1),
-          f"{name} must have columns of unit stride")
-    _need(t.shape[0] <= 1 or t.stride(0) >= t.shape[1], f"{name}'s rows must not overlap")
+             cols: Optional[int] = None) -> int:
+    """Elements between the rows of t, a CUDA matrix of one of the types whose rows have unit
+    stride (the width where there is one row and the stride says nothing)."""
+    if not (t.is_cuda and t.dim() == 2 and t.dtype in dtypes):
+        raise ValueError(f"{name} must be a CUDA matrix of {' or '.join(str(d) for d in dtypes)}")
+    (r, c), (ld, unit) = t.shape, t.stride()
+    if (rows is not None and r != rows) or (cols is not None and c != cols):
+        raise ValueError(f"{name} must be [{r if rows is None else rows}, {c if cols is None else cols}]")
+    if c < 1 or (unit != 1 and c != 1):
+        raise ValueError(f"{name} must have columns of unit stride")
+    if r <= 1:
+        return c
+    if ld < c:
+        raise ValueError(f"{name}'s rows must not overlap")
+    return ld
 
 
 def _ld(t: torch.Tensor) -> int:
-    """Elements between rows (the width where there is one row and the stride says nothing)."""
     return max(t.stride(-2), t.shape[-1]) if t.shape[-2] > 1 else t.shape[-1]
 
 
-def _result(out, shape, dtype, device, name="out"):
-    if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    _need(out.is_cuda and tuple(out.shape) == tuple(shape) and out.dtype == dtype and
-          (out.stride(-1) == 1 or shape[-1] == 1), f"{name} must be {dtype} {list(shape)} with unit column stride")
+def _given(out, shape, dtype):
+    if not (out.is_cuda and tuple(out.shape) == shape and out.dtype == dtype and
+            (out.stride(-1) == 1 or shape[-1] == 1)):
+        raise ValueError(f"out must be {dtype} {list(shape)} with unit column stride")
     _need(all(out.stride(i) >= out.shape[i + 1] * max(out.stride(i + 1), 1)
-              for i in range(out.dim() - 1) if out.shape[i] > 1), f"{name}'s rows must not overlap")
+              for i in range(out.dim() - 1) if out.shape[i] > 1), "out's rows must not overlap")
     return out
 
 
@@ -66,38 +78,47 @@ def _result(out, shape, dtype, device, name="out"):
 _HALF = (torch.bfloat16, torch.float16)
 
 
-def _grouped(rows_t, w, offsets, name):
-    _need(w.is_cuda and w.dim() == 3 and w.dtype == rows_t.dtype,
-          f"w must be a CUDA tensor [groups, outer, inner] of {name}'s type")
-    _need(min(w.shape) >= 1 and (w.stride(2) == 1 or w.shape[2] == 1), "w must have rows of unit stride")
-    _need((w.shape[1] == 1 or w.stride(1) >= w.shape[2]) and w.stride(0) >= 0, "w's rows must not overlap")
-    _offsets(offsets, w.shape[0])
+def _grouped(w, offsets, dtype, name):
+    """Groups, outer, inner, the row and the group stride of w."""
+    if not (w.is_cuda and w.dim() == 3 and w.dtype == dtype):
+        raise ValueError(f"w must be a CUDA tensor [groups, outer, inner] of {name}'s type")
+    (G, N, K), (gs, ld, unit) = w.shape, w.stride()
+    if min(G, N, K) < 1 or (unit != 1 and K != 1):
+        raise ValueError("w must have rows of unit stride")
+    if N == 1:
+        ld = K
+    _need(ld >= K, "w's rows must not overlap")
+    _offsets(offsets, G)
+    return G, N, K, ld, gs
 
 
 def _offsets(offsets, groups):
-    _need(offsets.is_cuda and offsets.dtype == torch.int32 and offsets.dim() == 1 and
-          offsets.is_contiguous(), "offsets must be a contiguous CUDA int32 vector")
-    _need(groups is None or offsets.shape[0] == groups + 1, "offsets must have one entry more than there are groups")
-    _need(offsets.shape[0] >= 2, "offsets must name at least one group")
+    if not (offsets.is_cuda and offsets.dtype == torch.int32 and offsets.dim() == 1 and
+            offsets.is_contiguous()):
+        raise ValueError("offsets must be a contiguous CUDA int32 vector")
+    n = offsets.shape[0]
+    _need(n >= 2 and (groups is None or n == groups + 1), "offsets must have one entry more than there are groups")
+    return n - 1
 
 
 def _out_type(out_dtype, out, dtype):
     d = out_dtype if out_dtype is not None else (out.dtype if out is not None else dtype)
-    _need(d in (dtype, torch.float32), f"the result is {dtype} or torch.float32")
+    if d is not dtype and d is not torch.float32:
+        raise ValueError(f"the result is {dtype} or torch.float32")
     return d
 
 
-def _aligned(t: torch.Tensor) -> bool:
-    return t.data_ptr() % 16 == 0 and all(
-        t.stride(i) % 8 == 0 and t.stride(i) > 0 for i in range(t.dim() - 1) if t.shape[i] > 1)
-
-
-def _workspace(lib, op, a, b, groups, rows, inner, outer, device):
+def _workspace(lib, op, a, a_ld, b, b_ld, b_gs, groups, rows, inner, outer):
+    """Device memory for operands that have to be copied first (None where there are none)."""
+    if not (a_ld & 7 or b_ld & 7 or (b_gs & 7 or b_gs <= 0) and groups > 1 and op != DW or
+            (a.data_ptr() | b.data_ptr()) & 15) or rows == 0:
+        return None, None, 0
     n = c_int64()
     check(lib.hier_avg_grouped_product_workspace(
-        op, a.data_ptr(), _ld(a), b.data_ptr(), _ld(b), b.stride(0) if b.dim() == 3 else 0, groups,
-        rows, inner, outer, ctypes.byref(n)), "grouped_product_workspace")
-    return (torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None), n.value
+        op, a.data_ptr(), a_ld, b.data_ptr(), b_ld, b_gs, groups, rows, inner, outer,
+        ctypes.byref(n)), "grouped_product_workspace")
+    ws = torch.empty(max(n.value, 16), dtype=torch.uint8, device=a.device)
+    return ws, ws.data_ptr(), n.value
 
 
 def grouped_product(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
@@ -110,22 +131,22 @@ def grouped_product(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
     groups; offsets [groups + 1] int32 on the device; bias [groups, outer] fp32.  The result is
     of x's type or fp32; rows of no group are zero."""
     lib = _lib.load()
-    _rows_of("x", x, _HALF)
-    _grouped(x, w, offsets, "x")
-    G, N, K = w.shape
-    _need(x.shape[1] == K, f"x must have {K} columns, as w")
-    if bias is not None:
-        _rows_of("bias", bias, (torch.float32,), G, N)
-    d = _out_type(out_dtype, out, x.dtype)
+    ld = _rows_of("x", x, _HALF)
+    kind = x.dtype
+    G, N, K, w_ld, gs = _grouped(w, offsets, kind, "x")
     T = x.shape[0]
-    s, where = _on(stream)
+    if x.shape[1] != K:
+        raise ValueError(f"x must have {K} columns, as w")
+    bias_ld = 0 if bias is None else _rows_of("bias", bias, (torch.float32,), G, N)
+    d = _out_type(out_dtype, out, kind)
+    s, where = _on(x, stream)
     with where:
-        y = _result(out, (T, N), d, x.device)
-        ws, n = (None, 0) if _aligned(x) and _aligned(w) else _workspace(lib, FORWARD, x, w, G, T, K, N, x.device)
+        y = torch.empty((T, N), dtype=d, device=x.device) if out is None else _given(out, (T, N), d)
+        ws, p, n = _workspace(lib, FORWARD, x, ld, w, w_ld, gs, G, T, K, N)
     check(lib.hier_avg_grouped_product(
-        x.data_ptr(), _ld(x), w.data_ptr(), _ld(w), w.stride(0), TYPES[x.dtype], offsets.data_ptr(), G,
-        T, K, N, bias.data_ptr() if bias is not None else None, _ld(bias) if bias is not None else 0,
-        int(relu), y.data_ptr(), _ld(y), TYPES[d], ws.data_ptr() if n else None, n, s), "grouped_product")
+        x.data_ptr(), ld, w.data_ptr(), w_ld, gs, TYPES[kind], offsets.data_ptr(), G, T, K, N,
+        None if bias is None else bias.data_ptr(), bias_ld, relu, y.data_ptr(),
+        N if out is None else _ld(y), TYPES[d], p, n, s), "grouped_product")
     return y
 
 
@@ -135,22 +156,22 @@ def grouped_product_dx(dy: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
     """dx[t] = w[g]^T dy[t] for the rows of group g; with h [rows, inner] (the activations that
     grouped_product read, after a ReLU) zero where h is not positive."""
     lib = _lib.load()
-    _rows_of("dy", dy, _HALF)
-    _grouped(dy, w, offsets, "dy")
-    G, N, K = w.shape
-    _need(dy.shape[1] == N, f"dy must have {N} columns, as w has rows")
+    ld = _rows_of("dy", dy, _HALF)
+    kind = dy.dtype
+    G, N, K, w_ld, gs = _grouped(w, offsets, kind, "dy")
     T = dy.shape[0]
-    if h is not None:
-        _rows_of("h", h, (dy.dtype,), T, K)
-    d = _out_type(out_dtype, out, dy.dtype)
-    s, where = _on(stream)
+    if dy.shape[1] != N:
+        raise ValueError(f"dy must have {N} columns, as w has rows")
+    h_ld = 0 if h is None else _rows_of("h", h, (kind,), T, K)
+    d = _out_type(out_dtype, out, kind)
+    s, where = _on(dy, stream)
     with where:
-        dx = _result(out, (T, K), d, dy.device)
-        ws, n = (None, 0) if _aligned(dy) and _aligned(w) else _workspace(lib, DX, dy, w, G, T, K, N, dy.device)
+        dx = torch.empty((T, K), dtype=d, device=dy.device) if out is None else _given(out, (T, K), d)
+        ws, p, n = _workspace(lib, DX, dy, ld, w, w_ld, gs, G, T, K, N)
     check(lib.hier_avg_grouped_product_dx(
-        dy.data_ptr(), _ld(dy), w.data_ptr(), _ld(w), w.stride(0), TYPES[dy.dtype], offsets.data_ptr(), G,
-        T, K, N, h.data_ptr() if h is not None else None, _ld(h) if h is not None else 0, dx.data_ptr(),
-        _ld(dx), TYPES[d], ws.data_ptr() if n else None, n, s), "grouped_product_dx")
+        dy.data_ptr(), ld, w.data_ptr(), w_ld, gs, TYPES[kind], offsets.data_ptr(), G, T, K, N,
+        None if h is None else h.data_ptr(), h_ld, dx.data_ptr(), K if out is None else _ld(dx),
+        TYPES[d], p, n, s), "grouped_product_dx")
     return dx
 
 
@@ -160,20 +181,21 @@ def grouped_product_dw(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor,
     """dw[g] = sum of dy[t] x[t]^T over group g's rows, [groups, outer, inner] in dy's type or fp32;
     with bias_grad the pair (dw, db), db[g] = sum of dy[t] in fp32.  Empty groups give zero."""
     lib = _lib.load()
-    _rows_of("dy", dy, _HALF)
-    _rows_of("x", x, (dy.dtype,), dy.shape[0])
-    _offsets(offsets, None)
-    T, N, K, G = dy.shape[0], dy.shape[1], x.shape[1], offsets.shape[0] - 1
-    d = _out_type(out_dtype, out, dy.dtype)
-    s, where = _on(stream)
+    ld = _rows_of("dy", dy, _HALF)
+    kind, (T, N) = dy.dtype, dy.shape
+    x_ld = _rows_of("x", x, (kind,), T)
+    G, K = _offsets(offsets, None), x.shape[1]
+    d = _out_type(out_dtype, out, kind)
+    s, where = _on(dy, stream)
     with where:
-        dw = _result(out, (G, N, K), d, dy.device)
-        db = torch.empty(G, N, dtype=torch.float32, device=dy.device) if bias_grad else None
-        ws, n = (None, 0) if T == 0 or (_aligned(dy) and _aligned(x)) else _workspace(lib, DW, dy, x, G, T, K, N, dy.device)
+        dw = torch.empty((G, N, K), dtype=d, device=dy.device) if out is None else _given(out, (G, N, K), d)
+        db = torch.empty((G, N), dtype=torch.float32, device=dy.device) if bias_grad else None
+        ws, p, n = _workspace(lib, DW, dy, ld, x, x_ld, 0, G, T, K, N)
+    dw_ld, dw_gs = (K, N * K) if out is None else (_ld(dw), dw.stride(0))
     check(lib.hier_avg_grouped_product_dw(
-        dy.data_ptr(), _ld(dy), x.data_ptr(), _ld(x), TYPES[dy.dtype], offsets.data_ptr(), G, T, K, N,
-        dw.data_ptr(), _ld(dw), dw.stride(0), TYPES[d], db.data_ptr() if bias_grad else None, N,
-        ws.data_ptr() if n else None, n, s), "grouped_product_dw")
+        dy.data_ptr(), ld, x.data_ptr(), x_ld, TYPES[kind], offsets.data_ptr(), G, T, K, N,
+        dw.data_ptr(), dw_ld, dw_gs, TYPES[d], db.data_ptr() if bias_grad else None, N, p, n, s),
+        "grouped_product_dw")
     return (dw, db) if bias_grad else dw
 
 
@@ -187,20 +209,21 @@ class TokenLogprobs(NamedTuple):
 
 
 def _logits(logits, targets, allowed, temperature):
-    _rows_of("logits", logits, tuple(TYPES))
+    """The logits' row stride, the mask's address and its row stride."""
+    ld = _rows_of("logits", logits, TYPES)
     T, V = logits.shape
-    _need(targets.is_cuda and targets.dtype in (torch.int32, torch.int64) and
-          tuple(targets.shape) == (T,) and targets.is_contiguous(),
-          "targets must be a contiguous CUDA int32 or int64 vector, one entry a row")
+    if not (targets.is_cuda and targets.dtype in (torch.int32, torch.int64) and
+            targets.dim() == 1 and targets.shape[0] == T and targets.is_contiguous()):
+        raise ValueError("targets must be a contiguous CUDA int32 or int64 vector, one entry a row")
     _need(0 < temperature < float("inf"), "temperature must be positive and finite")
     if allowed is None:
-        return None, 0
-    _need(allowed.is_cuda and allowed.dtype in (torch.bool, torch.uint8) and
-          tuple(allowed.shape) in ((V,), (T, V)) and (allowed.stride(-1) == 1 or V == 1),
-          "allowed must be a CUDA bool tensor [classes] or [rows, classes] with unit stride in rows")
+        return ld, None, 0
+    if not (allowed.is_cuda and allowed.dtype in (torch.bool, torch.uint8) and
+            tuple(allowed.shape) in ((V,), (T, V)) and (allowed.stride(-1) == 1 or V == 1)):
+        raise ValueError("allowed must be a CUDA bool tensor [classes] or [rows, classes] with unit stride in rows")
     if allowed.dim() == 1 or (T > 1 and allowed.stride(0) == 0):
-        return allowed.data_ptr(), 0
-    return allowed.data_ptr(), _ld(allowed)
+        return ld, allowed.data_ptr(), 0
+    return ld, allowed.data_ptr(), _ld(allowed)
 
 
 def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, top: int = 0, temperature: float = 1.0,
@@ -211,20 +234,25 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, top: int = 0, te
     logits [rows, classes] fp32, bf16 or fp16; targets int32 or int64, below 0 for no target (logp 0);
     allowed: a mask [classes] or [rows, classes], False where a class is left out."""
     lib = _lib.load()
-    mask, mask_ld = _logits(logits, targets, allowed, temperature)
-    _need(0 <= top <= MAX_TOP, f"top must be in [0, {MAX_TOP}]")
+    ld, mask, mask_ld = _logits(logits, targets, allowed, temperature)
+    if not 0 <= top <= MAX_TOP:
+        raise ValueError(f"top must be in [0, {MAX_TOP}]")
     T, V = logits.shape
-    s, where = _on(stream)
+    s, where = _on(logits, stream)
+    best = index = b = i = None
     with where:
-        r = torch.empty(3, T, dtype=torch.float32, device=logits.device)
-        best = torch.empty(T, top, dtype=torch.float32, device=logits.device) if top else None
-        index = torch.empty(T, top, dtype=torch.int32, device=logits.device) if top else None
-    p = r.data_ptr()
+        dev = logits.device
+        # three tensors and not three rows of one: a view costs more than an allocation
+        logp = torch.empty(T, dtype=torch.float32, device=dev)
+        entropy = torch.empty(T, dtype=torch.float32, device=dev)
+        lse = torch.empty(T, dtype=torch.float32, device=dev)
+        if top:
+            best = torch.empty((T, top), dtype=torch.float32, device=dev)
+            index = torch.empty((T, top), dtype=torch.int32, device=dev)
+            b, i = best.data_ptr(), index.data_ptr()
     check(lib.hier_avg_token_logprobs(
-        logits.data_ptr(), TYPES[logits.dtype], T, V, _ld(logits), targets.data_ptr(),
-        targets.element_size(), mask, mask_ld, temperature, top, p, p + 4 * T, p + 8 * T,
-        best.data_ptr() if top else None, index.data_ptr() if top else None, s), "token_logprobs")
-    logp, entropy, lse = r.unbind(0)
+        logits.data_ptr(), TYPES[logits.dtype], T, V, ld, targets.data_ptr(), targets.element_size(),
+        mask, mask_ld, temperature, top, logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(), b, i, s), "token_logprobs")
     return TokenLogprobs(logp, entropy, lse, best, index)
 
 
@@ -236,21 +264,23 @@ def token_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, lse: to
     """The gradient of sum(dlogp * logp + dentropy * entropy) with respect to the logits, in their
     type, from token_logprobs's lse and entropy; ``out`` may be ``logits`` itself."""
     lib = _lib.load()
-    mask, mask_ld = _logits(logits, targets, allowed, temperature)
+    ld, mask, mask_ld = _logits(logits, targets, allowed, temperature)
     T, V = logits.shape
     _need(dentropy is None or entropy is not None, "the entropy's gradient needs the entropy")
     for name, v in (("lse", lse), ("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy)):
-        _need(v is None or (v.is_cuda and v.dtype == torch.float32 and tuple(v.shape) == (T,) and
-                            v.is_contiguous()), f"{name} must be a contiguous CUDA fp32 vector, one entry a row")
-    s, where = _on(stream)
+        if v is not None and not (v.is_cuda and v.dtype == torch.float32 and v.dim() == 1 and
+                                  v.shape[0] == T and v.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous CUDA fp32 vector, one entry a row")
+    s, where = _on(logits, stream)
     with where:
-        d = _result(out, (T, V), logits.dtype, logits.device)
+        d = torch.empty((T, V), dtype=logits.dtype, device=logits.device) if out is None else \
+            _given(out, (T, V), logits.dtype)
     check(lib.hier_avg_token_logprobs_backward(
-        logits.data_ptr(), TYPES[logits.dtype], T, V, _ld(logits), targets.data_ptr(),
+        logits.data_ptr(), TYPES[logits.dtype], T, V, ld, targets.data_ptr(),
         targets.element_size(), mask, mask_ld, temperature, lse.data_ptr(),
-        entropy.data_ptr() if entropy is not None else None, dlogp.data_ptr(),
-        dentropy.data_ptr() if dentropy is not None else None, d.data_ptr(), _ld(d), s),
-        "token_logprobs_backward")
+        None if entropy is None else entropy.data_ptr(), dlogp.data_ptr(),
+        None if dentropy is None else dentropy.data_ptr(), d.data_ptr(),
+        V if out is None else _ld(d), s), "token_logprobs_backward")
     return d
 
 
@@ -309,7 +339,7 @@ class AdamW:
         self.params, self.copies, self.bits = params, copies, bits
         self.beta1, self.beta2, self.eps, self.t = beta1, beta2, eps, 0
         e, dev = elements.value, params[0].device
-        s, where = _on(stream)
+        s, where = _on(params[0], stream)
         with where:
             self._table = torch.empty(max(table.value, 16), dtype=torch.uint8, device=dev)
             self.m_scale = self.root_scale = self.v = self.root = None
@@ -326,27 +356,27 @@ class AdamW:
             self.h, self._table.data_ptr(), table.value, self.m.data_ptr(), second.data_ptr(),
             self.m_scale.data_ptr() if bits == 8 else None,
             self.root_scale.data_ptr() if bits == 8 else None, s), "adamw_bind")
-        self._grads = (c_void_p * len(params))()
+        self._shapes = [p.shape for p in params]
 
     def step(self, grads: Sequence[torch.Tensor], lr: float, grad_scale: Optional[torch.Tensor] = None,
              seed: Optional[int] = None, stream=None) -> None:
         """One step from contiguous gradients of the params' shapes, all fp32, bf16 or fp16, times
         grad_scale (one fp32 value on the device) where given.  seed: of the 8-bit states' rounding
         (the step's number when None); the same seed gives the same step."""
-        _need(len(grads) == len(self.params), "one gradient a tensor")
-        kind = grads[0].dtype
-        _need(kind in TYPES, "gradients must be fp32, bf16 or fp16")
-        a = self._grads
-        for i, (g, p) in enumerate(zip(grads, self.params)):
-            if not (g.is_cuda and g.dtype == kind and g.shape == p.shape and g.is_contiguous()):
-                raise ValueError(f"gradient {i} must be a contiguous CUDA {kind} tensor {list(p.shape)}")
-            a[i] = g.data_ptr()
+        # each check runs over all tensors at once: a call over hundreds of them is host work
+        kind = grads[0].dtype if grads else None
+        if not (list(map(_SHAPE, grads)) == self._shapes and kind in TYPES and
+                set(map(_DTYPE, grads)) == {kind} and all(map(_CONTIGUOUS, grads)) and
+                set(map(_CUDA, grads)) == {True}):
+            raise ValueError("grads must be one contiguous CUDA tensor for each of the params, of its "
+                             "shape, all of them fp32, bf16 or fp16")
+        a = array("Q", map(_ADDRESS, grads))
         if grad_scale is not None:
             _need(grad_scale.is_cuda and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1,
                   "grad_scale must be one CUDA fp32 value")
-        s = (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+        s = _RAW_STREAM(grads[0].get_device()) if stream is None else stream.cuda_stream
         check(self._lib.hier_avg_adamw_step(
-            self.h, a, TYPES[kind], lr, self.beta1, self.beta2, self.eps, self.t + 1,
+            self.h, a.buffer_info()[0], TYPES[kind], lr, self.beta1, self.beta2, self.eps, self.t + 1,
             grad_scale.data_ptr() if grad_scale is not None else None,
             (self.t + 1 if seed is None else seed) & 0xFFFFFFFF, s), "adamw_step")
         self.t += 1
