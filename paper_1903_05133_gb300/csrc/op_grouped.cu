@@ -22,11 +22,13 @@ namespace {
 __device__ int g_operator_error;
 
 constexpr int kFwd = 0, kDx = 1, kDw = 2;
-constexpr int kM = 128;                 // features of a tile
+constexpr int kM = 128;                 // features of a CTA's tile
 constexpr int kK = 64;                  // values summed over in a chunk: one 128-byte line
 constexpr int kMaxGroups = 1024;
 constexpr int kEpiWarps = 8;            // two groups of four: a group reads half the columns
 constexpr int kThreads = (kEpiWarps + 2) * 32;
+constexpr int kPairCols = 256;          // columns of a tile of two CTAs
+constexpr int kFewCols = 32;            // of a tile of one CTA, where groups have few rows
 // fp32 results: the tensor core's running sum is taken into fp32 registers after this many
 // chunks.  Its additions truncate; over a sum of 4096 random products that cost 4.4e-6 of the
 // result's norm, over 16384 1.9e-5, over 512 4.7e-7 (fp32 additions: 6.1e-7, 1.5e-6 and 1.6e-7).
@@ -44,7 +46,8 @@ struct Args {
   int m, n, k;                // features; dW: columns; summed length (forward, rows)
   int in_type, out_type;
   int relu;
-  int wide_out;               // 16-byte stores of the output are aligned
+  int wide_out;               // 16-byte accesses of the output are aligned
+  int wide_h;                 // and of h
 };
 
 struct Tile {
@@ -54,7 +57,8 @@ struct Tile {
 // Column tiles of a group of n rows: as few as fit, of equal size.
 __device__ __forceinline__ int col_tiles(int n, int NT) { return (n + NT - 1) / NT; }
 
-// Element types of a kind::f16 MMA: bits 7-9 and 10-12 of the instruction descriptor.
+// Instruction descriptor of a kind::f16 MMA with fp32 sums: element types at bits 7-9 and
+// 10-12, N >> 3 at bits 17-22, M >> 4 at bits 24-28.
 __device__ __forceinline__ uint32_t idesc_of(int type, int M, int N) {
   const uint32_t t = type == HA_TYPE_BF16 ? 1u : 0u;
   return (1u << 4) | (t << 7) | (t << 10) | (static_cast<uint32_t>(N >> 3) << 17) |
@@ -69,38 +73,59 @@ __device__ __forceinline__ uint16_t narrow(float x, int type) {
   const __half b = __float2half_rn(x);
   return *reinterpret_cast<const uint16_t*>(&b);
 }
-__device__ __forceinline__ bool positive16(uint16_t w, int type) {   // > 0, not NaN
+__device__ __forceinline__ uint32_t narrow_pair(float a, float b, int type) {
+  return type == HA_TYPE_BF16 ? narrow2<__nv_bfloat16>(a, b) : narrow2<__half>(a, b);
+}
+__device__ __forceinline__ bool positive16(uint32_t w, int type) {   // > 0, not NaN
   return w != 0 && w <= (type == HA_TYPE_BF16 ? 0x7F80u : 0x7C00u);
 }
 
-template <int NT> struct Shape {
-  static constexpr int kA = kM * kK * 2;                 // bytes of a chunk of the weights
-  static constexpr int kB = NT * kK * 2;
-  static constexpr int kStages = NT == 256 ? 4 : 6;
-  static constexpr int kBoxRows = NT == 256 ? 64 : 16;   // rows of a load of x or dy
-  static constexpr int kStage = 8192;                    // results on their way out, per warp group
-  static constexpr int kTmem = 2 * NT;
-  static constexpr int kSmem = kStages * (kA + kB) + 2 * kStage + 1024;
+struct Table {
+  int* off;         // rows of each group, inside [0, rows]
+  int* first;       // first tile of each group
 };
+constexpr int kTableBytes = 2 * (kMaxGroups + 1) * 4;
 
-struct Shared {
-  uint64_t full[8], empty[8], tfull[2], tempty[2];
-  uint32_t tmem;
-  int off[kMaxGroups + 1];      // rows of each group, inside [0, rows]
-  int first[kMaxGroups + 1];    // first tile of each group
-};
+// The list of tiles, by all threads; ends with a CTA barrier.
+template <int MODE, int M, int NT>
+__device__ __forceinline__ void make_table(const Table& s, const Args& a) {
+  const int tid = threadIdx.x, lane = tid & 31;
+  for (int g = tid; g <= a.groups; g += kThreads) s.off[g] = min(max(a.offsets[g], 0), a.rows);
+  __syncthreads();
+  if (tid < 32) {
+    const int mt = (a.m + M - 1) / M, nt = (a.n + NT - 1) / NT;
+    int run = 0;
+    for (int g0 = 0; g0 < a.groups; g0 += 32) {
+      const int g = g0 + lane;
+      // offsets that go back leave a group empty
+      const int n = g < a.groups ? max(0, s.off[g + 1] - s.off[g]) : 0;
+      const int tiles = MODE == kDw ? (g < a.groups ? mt * nt : 0) : mt * col_tiles(n, NT);
+      int x = tiles;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(~0u, x, o);
+        if (lane >= o) x += y;
+      }
+      if (g < a.groups) s.first[g] = run + x - tiles;
+      run += __shfl_sync(~0u, x, 31);
+    }
+    if (lane == 0) s.first[a.groups] = run;
+  }
+  __syncthreads();
+}
 
-template <int MODE, int NT>
-__device__ __forceinline__ Tile tile_at(const Shared& s, const Args& a, int i) {
+// STEP: the columns of a tile are a multiple of it (but for the group's end).
+template <int MODE, int M, int NT, int STEP>
+__device__ __forceinline__ Tile tile_at(const Table& s, const Args& a, int i) {
   int lo = 0, hi = a.groups;             // first[lo] <= i < first[hi]
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (s.first[mid] <= i) lo = mid; else hi = mid;
   }
-  const int mt = (a.m + kM - 1) / kM, at = i - s.first[lo];
+  const int mt = (a.m + M - 1) / M, at = i - s.first[lo];
   Tile t;
   t.g = lo;
-  t.m0 = at % mt * kM;
+  t.m0 = at % mt * M;
   const int ct = at / mt, n = max(0, s.off[lo + 1] - s.off[lo]);
   if (MODE == kDw) {
     t.c0 = ct * NT;
@@ -108,7 +133,7 @@ __device__ __forceinline__ Tile tile_at(const Shared& s, const Args& a, int i) {
     t.r0 = s.off[lo];
     t.k = n;
   } else {
-    const int parts = col_tiles(n, NT), size = ((n + parts - 1) / parts + 15) / 16 * 16;
+    const int parts = col_tiles(n, NT), size = ((n + parts - 1) / parts + STEP - 1) / STEP * STEP;
     t.c0 = s.off[lo] + ct * size;
     t.cols = min(size, n - ct * size);
     t.r0 = t.c0;
@@ -119,9 +144,8 @@ __device__ __forceinline__ Tile tile_at(const Shared& s, const Args& a, int i) {
 
 // The rows that no group covers are zero.
 __device__ void clear_rows(const Args& a, int64_t begin, int64_t end) {
-  const int64_t per = a.m;
   for (int64_t r = begin + blockIdx.x; r < end; r += gridDim.x)
-    for (int64_t c = threadIdx.x; c < per; c += kThreads) {
+    for (int64_t c = threadIdx.x; c < a.m; c += kThreads) {
       if (a.out_type == HA_TYPE_FP32)
         static_cast<float*>(a.out)[r * a.out_ld + c] = 0.0f;
       else
@@ -129,286 +153,586 @@ __device__ void clear_rows(const Args& a, int64_t begin, int64_t end) {
     }
 }
 
-template <int MODE, int NT>
-__global__ void __launch_bounds__(kThreads, 1)
-    k_grouped(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
-              const __grid_constant__ Args a) {
-  using S = Shape<NT>;
-  extern __shared__ unsigned char raw[];
-  __shared__ Shared sh;
-  unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
-  unsigned char* As = base;
-  unsigned char* Bs = base + S::kStages * S::kA;
-  unsigned char* Out = base + S::kStages * (S::kA + S::kB);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+// ---- results of the forward and of the rows' gradient
+// A warp group holds 128 features (one a thread) of up to 32 columns, which are rows of the
+// output.  They pass through shared memory, so that a row's features leave as whole 16-byte
+// vectors.  Two buffers of 8 KB (32 rows of 16-bit values, 16 of fp32 ones) take turns, so
+// that one barrier a buffer is enough.
+constexpr int kRowsStage = 16384;
+template <int MODE, typename OUT>
+__device__ __forceinline__ void emit_rows(const Args& a, const float* v, int row0, int rows, int m0,
+                                          int feature, float bias, unsigned char* stage, int bar,
+                                          uint32_t& turn) {
+  constexpr int R = 8192 / (kM * sizeof(OUT));            // rows of a buffer: 32 or 16
+  constexpr int P = 16 / sizeof(OUT), S = kM / P;         // features of a vector, vectors of a row
+  const int et = threadIdx.x & 127;
+#pragma unroll
+  for (int j = 0; j < 32; j += R) {
+    if (j >= rows) return;                                // the same for the whole warp group
+    unsigned char* buf = stage + (turn++ & 1) * 8192;
+    uint4 hv[R * S / 128];
+    if (MODE == kDx && a.h) {
+      // the mask's values are asked for before the barrier
+#pragma unroll
+      for (int x = 0; x < R * S / 128; ++x) {
+        const int i = et + x * 128, r = i / S, e = m0 + i % S * P;
+        hv[x] = make_uint4(0, 0, 0, 0);
+        if (j + r < rows && e < a.m) {
+          const uint16_t* h = static_cast<const uint16_t*>(a.h) + static_cast<int64_t>(row0 + j + r) * a.h_ld + e;
+          if (a.wide_h && e + P <= a.m) {
+            if (sizeof(OUT) == 2) {
+              hv[x] = *reinterpret_cast<const uint4*>(h);
+            } else {
+              const uint2 w = *reinterpret_cast<const uint2*>(h);
+              hv[x].x = w.x;
+              hv[x].y = w.y;
+            }
+          } else {
+            uint16_t* q = reinterpret_cast<uint16_t*>(&hv[x]);
+#pragma unroll
+            for (int y = 0; y < P; ++y)
+              if (e + y < a.m) q[y] = h[y];
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < R; ++x) {
+      float f = v[j + x] + bias;
+      if (MODE == kFwd && a.relu && f < 0.0f) f = 0.0f;
+      if constexpr (sizeof(OUT) == 4)
+        reinterpret_cast<float*>(buf)[x * kM + feature] = f;
+      else
+        reinterpret_cast<uint16_t*>(buf)[x * kM + feature] = narrow(f, a.out_type);
+    }
+    named_barrier_sync(bar, 128);
+#pragma unroll
+    for (int x = 0; x < R * S / 128; ++x) {
+      const int i = et + x * 128, r = i / S, e = m0 + i % S * P;
+      if (j + r >= rows || e >= a.m) continue;
+      uint4 w = *reinterpret_cast<const uint4*>(buf + i * 16);
+      if (MODE == kDx && a.h) {
+        uint32_t* p = &w.x;
+        const uint32_t* q = &hv[x].x;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          if constexpr (sizeof(OUT) == 4) {
+            if (!positive16((q[y >> 1] >> (16 * (y & 1))) & 0xFFFFu, a.in_type)) p[y] = 0;
+          } else {
+            if (!positive16(q[y] & 0xFFFFu, a.in_type)) p[y] &= 0xFFFF0000u;
+            if (!positive16(q[y] >> 16, a.in_type)) p[y] &= 0xFFFFu;
+          }
+        }
+      }
+      OUT* o = static_cast<OUT*>(a.out) + static_cast<int64_t>(row0 + j + r) * a.out_ld + e;
+      if (a.wide_out && e + P <= a.m) {
+        *reinterpret_cast<uint4*>(o) = w;
+      } else {
+        const OUT* p = reinterpret_cast<const OUT*>(&w);
+#pragma unroll
+        for (int y = 0; y < P; ++y)
+          if (e + y < a.m) o[y] = p[y];
+      }
+    }
+  }
+}
 
-  // ---- the list of tiles
-  for (int g = tid; g <= a.groups; g += kThreads) sh.off[g] = min(max(a.offsets[g], 0), a.rows);
-  if (warp == kEpiWarps) tmem_alloc(&sh.tmem, S::kTmem);
+// ---- results of the weights' gradient
+// A warp holds 32 features (rows of dW, one a lane) of 32 columns at a time.  Rows of 128
+// bytes are put together in shared memory (16-byte pieces swapped by the row, as the tensor
+// map's 128-byte swizzle expects) and leave as one bulk store, which also cuts off what is
+// outside dW.  Where dW's rows are not aligned for that, lanes store their values.
+constexpr int kWarpStage = 4096;
+__device__ __forceinline__ void emit_weights(const Args& a, const CUtensorMap* to, const float* v, int g,
+                                             int f0, int c, int end, unsigned char* stage) {
+  const int lane = threadIdx.x & 31;
+  if (a.wide_out) {
+    const bool wide = a.out_type == HA_TYPE_FP32;
+    const int half = wide ? 0 : (c >> 5) & 1;             // which 32 of a 16-bit row's 64 columns
+    if (half == 0) {
+      if (lane == 0) tma_store_wait_read_all();
+      __syncwarp();
+    }
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      if (!wide && p >= 4) break;
+      uint4 w;
+      if (wide)
+        w = make_uint4(__float_as_uint(v[4 * p]), __float_as_uint(v[4 * p + 1]), __float_as_uint(v[4 * p + 2]),
+                       __float_as_uint(v[4 * p + 3]));
+      else
+        w = make_uint4(narrow_pair(v[8 * (p & 3)], v[8 * (p & 3) + 1], a.out_type),
+                       narrow_pair(v[8 * (p & 3) + 2], v[8 * (p & 3) + 3], a.out_type),
+                       narrow_pair(v[8 * (p & 3) + 4], v[8 * (p & 3) + 5], a.out_type),
+                       narrow_pair(v[8 * (p & 3) + 6], v[8 * (p & 3) + 7], a.out_type));
+      *reinterpret_cast<uint4*>(stage + lane * 128 + (((half * 4 + p) ^ (lane & 7)) << 4)) = w;
+    }
+    const int c_box = c - half * 32;
+    if (wide || half == 1 || c + 32 >= end) {
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0 && f0 < a.m) {
+        tma_store_3d(to, stage, c_box, f0, g);
+        tma_store_commit();
+      }
+    }
+    return;
+  }
+  const int f = f0 + lane;
+  if (f >= a.m) return;
+  const int64_t at = g * a.out_gs + f * a.out_ld + c;
+#pragma unroll
+  for (int x = 0; x < 32; ++x)
+    if (c + x < end) {
+      if (a.out_type == HA_TYPE_FP32)
+        static_cast<float*>(a.out)[at + x] = v[x];
+      else
+        static_cast<uint16_t*>(a.out)[at + x] = narrow(v[x], a.out_type);
+    }
+}
+
+// A warp's wait for sums, by one lane: 32 lanes asking keep the barrier unit from the roles
+// that feed the tensor cores.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) {
+  int ok = 1;
+  if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity, &g_operator_error);
+  ok = __shfl_sync(~0u, ok, 0);
+  tc_fence_after();
+  return ok != 0;
+}
+
+// A place in a ring of stages and the parity of its round.
+template <int STAGES>
+struct Ring {
+  uint32_t st = 0, round = 0;
+  __device__ __forceinline__ void next() {
+    if (++st == STAGES) {
+      st = 0;
+      round ^= 1;
+    }
+  }
+  // Whether the next stage is ready, asked a chunk ahead: even a barrier whose phase is over
+  // takes 170 cycles to answer.
+  __device__ __forceinline__ bool peek(uint64_t* bars, uint32_t flip) const {
+    const bool wrap = st + 1 == STAGES;
+    return mbar_test(&bars[wrap ? 0 : st + 1], (wrap ? round ^ 1 : round) ^ flip);
+  }
+  __device__ __forceinline__ void skip(int n) {
+    const uint32_t at = st + static_cast<uint32_t>(n);
+    st = at % STAGES;
+    round ^= (at / STAGES) & 1;
+  }
+};
+
+// One tile's results: `half` of its NT columns, from the sums in TMEM, segment by segment.
+template <int MODE, int NT, bool FOLD, typename Wait, typename Free>
+__device__ __forceinline__ bool finish_tile(const Args& a, const CUtensorMap* to, const Tile& t, uint32_t tmem,
+                                            int cta_m0, unsigned char* stage, uint32_t& seg, uint32_t& turn,
+                                            Wait wait, Free release) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2, quad = warp & 3;
+  const int nk = (t.k + kK - 1) / kK;
+  const int segs = FOLD ? (nk + kFold - 1) / kFold : (nk > 0 ? 1 : 0);
+  constexpr int H = NT / 2;
+  const int cb = half * H, ce = min(H, t.cols - cb);      // this warp group's columns
+  const int f = cta_m0 + quad * 32 + lane;                // this thread's feature
+  const float bias = MODE == kFwd && a.bias && f < a.m ? a.bias[t.g * a.bias_ld + f] : 0.0f;
+  constexpr int STEP = H < 32 ? H : 32;
+  auto emit = [&](const float* v, int j) {
+    if (MODE == kDw)
+      emit_weights(a, to, v, t.g, cta_m0 + quad * 32, t.c0 + cb + j, t.c0 + cb + ce, stage + warp * kWarpStage);
+    else if (FOLD)
+      emit_rows<MODE, float>(a, v, t.c0 + cb + j, min(STEP, ce - j), cta_m0, quad * 32 + lane, bias,
+                             stage + half * kRowsStage, 1 + half, turn);
+    else
+      emit_rows<MODE, uint16_t>(a, v, t.c0 + cb + j, min(STEP, ce - j), cta_m0, quad * 32 + lane, bias,
+                                stage + half * kRowsStage, 1 + half, turn);
+  };
+  auto read = [&](float* v, int buf, int j) {
+    const uint32_t at = tmem + (static_cast<uint32_t>(quad * 32) << 16) + buf * NT + cb + j;
+    if (STEP == 32) tmem_ld32(at, v);
+    else tmem_ld16(at, v);
+    tmem_ld_wait();
+  };
+  if (!FOLD) {
+    if (segs && !wait(seg)) return false;
+#pragma unroll 1
+    for (int j = 0; j < H; j += STEP) {
+      if (j >= ce) break;
+      float v[32];
+#pragma unroll
+      for (int x = 0; x < 32; ++x) v[x] = 0.0f;
+      if (segs) read(v, seg & 1, j);
+      emit(v, j);
+    }
+    if (segs) release(seg++);
+    return true;
+  }
+  float acc[H < 32 ? 32 : H];
+#pragma unroll
+  for (int j = 0; j < (H < 32 ? 32 : H); ++j) acc[j] = 0.0f;
+  for (int s = 0; s < segs; ++s) {
+    if (!wait(seg)) return false;
+#pragma unroll
+    for (int j = 0; j < H; j += STEP)
+      if (j < ce) {
+        float v[32];
+        read(v, seg & 1, j);
+#pragma unroll
+        for (int x = 0; x < STEP; ++x) acc[j + x] += v[x];
+      }
+    release(seg++);
+  }
+#pragma unroll
+  for (int j = 0; j < H; j += STEP)
+    if (j < ce) emit(acc + j, j);
+  return true;
+}
+
+// ---- groups of few rows: one CTA a tile of 128 features and up to 32 rows
+// The weights' bytes are what counts, so the stages are many and small: a chunk of weights
+// is 16 KB, and 9 of them are in flight.
+struct Few {
+  static constexpr int kA = kM * kK * 2, kB = kFewCols * kK * 2, kStages = 9;
+  static constexpr int kSmem = kStages * (kA + kB) + 2 * kRowsStage + 1024;
+};
+
+template <int MODE, bool FOLD>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_grouped_few(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
+                  const __grid_constant__ Args a) {
+  extern __shared__ unsigned char raw[];
+  __shared__ uint64_t full[Few::kStages], empty[Few::kStages], tfull[2], tempty[2];
+  __shared__ uint32_t tmem_at;
+  __shared__ int table[2 * (kMaxGroups + 1)];
+  const Table tab = {table, table + kMaxGroups + 1};
+  unsigned char* As = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+  unsigned char* Bs = As + Few::kStages * Few::kA;
+  unsigned char* Out = Bs + Few::kStages * Few::kB;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (warp == kEpiWarps) {
+    tmem_alloc(&tmem_at, 2 * kFewCols);
+    tmem_relinquish();
+  }
   if (tid == 0) {
-    for (int i = 0; i < S::kStages; ++i) {
-      mbar_init(&sh.full[i], 1);
-      mbar_init(&sh.empty[i], 1);
+    for (int i = 0; i < Few::kStages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.tfull[i], 1);
-      mbar_init(&sh.tempty[i], kEpiWarps);
+      mbar_init(&tfull[i], 1);
+      mbar_init(&tempty[i], kEpiWarps);
     }
     fence_barrier_init();
   }
-  __syncthreads();
-  if (warp == 0) {
-    const int mt = (a.m + kM - 1) / kM, nt = (a.n + NT - 1) / NT;
-    int run = 0;
-    for (int g0 = 0; g0 < a.groups; g0 += 32) {
-      const int g = g0 + lane;
-      // offsets that go back leave a group empty
-      const int n = g < a.groups ? max(0, sh.off[g + 1] - sh.off[g]) : 0;
-      const int tiles = MODE == kDw ? (g < a.groups ? mt * nt : 0) : mt * col_tiles(n, NT);
-      int x = tiles;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(~0u, x, o);
-        if (lane >= o) x += y;
-      }
-      if (g < a.groups) sh.first[g] = run + x - tiles;
-      run += __shfl_sync(~0u, x, 31);
-    }
-    if (lane == 0) sh.first[a.groups] = run;
-  }
   tc_fence_before();
-  __syncthreads();
+  make_table<MODE, kM, kFewCols>(tab, a);
   tc_fence_after();
-  const uint32_t tmem = sh.tmem;
-  const int tiles = sh.first[a.groups];
-  if (MODE != kDw) {
-    clear_rows(a, 0, sh.off[0]);
-    clear_rows(a, sh.off[a.groups], a.rows);
-  }
+  const uint32_t tmem = tmem_at;
+  const int tiles = tab.first[a.groups];
+  clear_rows(a, 0, tab.off[0]);
+  clear_rows(a, tab.off[a.groups], a.rows);
 
   if (warp == kEpiWarps) {
     // ---- loads
-    if (lane == 0) {
-      uint32_t it = 0;
-      bool ok = true;
+    if (elect_one()) {
+      Ring<Few::kStages> at;
+      bool ok = true, peek = false;
+      const uint64_t stream = l2_stream_policy(true), keep = l2_stream_policy(false);
       for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
-        const Tile t = tile_at<MODE, NT>(sh, a, i);
-        const int nk = (t.k + kK - 1) / kK;
-        const int boxes = MODE == kDw ? (t.cols + 63) / 64 : (t.cols + S::kBoxRows - 1) / S::kBoxRows;
-        const uint32_t bytes = S::kA + boxes * (MODE == kDw ? 64 : S::kBoxRows) * 128;
-        for (int c = 0; c < nk; ++c, ++it) {
-          const int st = it % S::kStages;
-          if (!mbar_wait(&sh.empty[st], ((it / S::kStages) & 1) ^ 1, &g_operator_error)) { ok = false; break; }
-          uint64_t* bar = &sh.full[st];
-          mbar_arrive_expect_tx(bar, bytes);
-          unsigned char* A = As + st * S::kA;
-          unsigned char* B = Bs + st * S::kB;
+        const Tile t = tile_at<MODE, kM, kFewCols, 16>(tab, a, i);
+        const int nk = (t.k + kK - 1) / kK, boxes = (t.cols + 15) / 16;
+        for (int c = 0; c < nk; ++c, at.next()) {
+          const int st = at.st;
+          if (!peek && !mbar_wait_hot(&empty[st], at.round ^ 1, &g_operator_error)) { ok = false; break; }
+          peek = at.peek(empty, 1);
+          uint64_t* bar = &full[st];
+          mbar_arrive_expect_tx(bar, Few::kA + boxes * 2048);
+          unsigned char* A = As + st * Few::kA;
           if (MODE == kFwd) {
-            tma_load_3d(A, &ta, bar, c * kK, t.m0, t.g);
-          } else if (MODE == kDx) {
-            tma_load_3d(A, &ta, bar, t.m0, c * kK, t.g);
-            tma_load_3d(A + 8192, &ta, bar, t.m0 + 64, c * kK, t.g);
+            tma_load_3d_hint(A, &ta, bar, c * kK, t.m0, t.g, stream);
           } else {
-            tma_load_2d(A, &ta, bar, t.m0, t.r0 + c * kK);
-            tma_load_2d(A + 8192, &ta, bar, t.m0 + 64, t.r0 + c * kK);
+            tma_load_3d_hint(A, &ta, bar, t.m0, c * kK, t.g, stream);
+            tma_load_3d_hint(A + 8192, &ta, bar, t.m0 + 64, c * kK, t.g, stream);
+          }
+          for (int b = 0; b < boxes; ++b)
+            tma_load_3d_hint(Bs + st * Few::kB + b * 2048, &tb, bar, c * kK, t.r0 + b * 16, 0, keep);
+        }
+      }
+    }
+  } else if (warp == kEpiWarps + 1) {
+    // ---- matrix products, by one lane
+    if (elect_one()) {
+      Ring<Few::kStages> at;
+      uint32_t seg = 0;
+      bool ok = true, peek = false;
+      constexpr int fold = FOLD ? kFold : 1 << 30;
+      for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+        const Tile t = tile_at<MODE, kM, kFewCols, 16>(tab, a, i);
+        const int nk = (t.k + kK - 1) / kK;
+        const uint32_t idesc = idesc_of(a.in_type, kM, (t.cols + 15) / 16 * 16) | (MODE == kFwd ? 0u : 1u << 15);
+        for (int c = 0; c < nk; ++c, at.next()) {
+          const int buf = seg & 1;
+          ok = (c % fold != 0 || mbar_wait_hot(&tempty[buf], ((seg >> 1) & 1) ^ 1, &g_operator_error)) &&
+               (peek || mbar_wait_hot(&full[at.st], at.round, &g_operator_error));
+          if (!ok) break;
+          peek = at.peek(full, 0);
+          tc_fence_after();
+          const int steps = (min(t.k - c * kK, kK) + 15) / 16;
+          const uint32_t as = smem_u32(As + at.st * Few::kA), bs = smem_u32(Bs + at.st * Few::kB);
+          for (int k = 0; k < steps; ++k) {
+            const uint64_t da = MODE == kFwd ? umma_desc_sw128(as + k * 32) : umma_desc_sw128_mn(as + k * 2048, 8192);
+            tc_mma_bf16(tmem + buf * kFewCols, da, umma_desc_sw128(bs + k * 32), idesc, (c % fold) || k ? 1u : 0u);
+          }
+          tc_commit(&empty[at.st]);
+          if (c % fold == fold - 1 || c == nk - 1) {
+            tc_commit(&tfull[buf]);
+            ++seg;
+          }
+        }
+      }
+    }
+  } else {
+    // ---- results
+    uint32_t seg = 0, turn = 0;
+    bool ok = true;
+    for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+      const Tile t = tile_at<MODE, kM, kFewCols, 16>(tab, a, i);
+      ok = finish_tile<MODE, kFewCols, FOLD>(
+          a, nullptr, t, tmem, t.m0, Out, seg, turn,
+          [&](uint32_t s) {
+            return warp_wait(&tfull[s & 1], (s >> 1) & 1);
+          },
+          [&](uint32_t s) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&tempty[s & 1]);
+          });
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kEpiWarps) tmem_dealloc(tmem, 2 * kFewCols);
+}
+
+// ---- everything else: two CTAs of a cluster a tile of 256 features and up to 256 columns
+// The pair's MMA (cta_group::2) is issued by its first CTA.  Each CTA loads its own 128
+// features and half of the columns; the tensor cores read both halves of the columns, so a
+// CTA's shared memory takes in and hands out a third less per product than with a tile of
+// 128 x 256 of its own, where it would be the bound.  Each CTA has its features' sums in its
+// own TMEM, in two buffers, and writes its own results.
+struct Pair {
+  static constexpr int kA = kM * kK * 2, kB = kPairCols / 2 * kK * 2, kStages = 5;
+  static constexpr int kOut = 2 * kRowsStage;             // = kEpiWarps * kWarpStage
+  static constexpr int kSmem = kStages * (kA + kB) + kOut + 1024;
+};
+static_assert(2 * kRowsStage == kEpiWarps * kWarpStage, "one buffer serves both kinds of results");
+
+template <int MODE, bool FOLD>
+__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
+    k_grouped_pair(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
+                   const __grid_constant__ CUtensorMap to, const __grid_constant__ Args a) {
+  extern __shared__ unsigned char raw[];
+  // full: the first CTA's, on which both CTAs' loads are counted.  tempty: the first CTA's too.
+  // tail: the second CTA's load of a chunk that has to be cut, or (in the first CTA) that the
+  // second has cut it.
+  __shared__ uint64_t full[Pair::kStages], empty[Pair::kStages], tfull[2], tempty[2], tail[Pair::kStages];
+  __shared__ uint32_t tmem_at;
+  __shared__ int table[2 * (kMaxGroups + 1)];
+  const Table tab = {table, table + kMaxGroups + 1};
+  unsigned char* As = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+  unsigned char* Bs = As + Pair::kStages * Pair::kA;
+  unsigned char* Out = Bs + Pair::kStages * Pair::kB;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = cluster_rank();
+  if (warp == kEpiWarps) {
+    tmem_alloc_pair(&tmem_at, 2 * kPairCols);
+    tmem_relinquish_pair();
+  }
+  if (tid == 0) {
+    for (int i = 0; i < Pair::kStages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+      mbar_init(&tail[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&tfull[i], 1);
+      mbar_init(&tempty[i], 2 * kEpiWarps);
+    }
+    fence_barrier_init();
+  }
+  tc_fence_before();
+  make_table<MODE, 2 * kM, kPairCols>(tab, a);
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem = tmem_at;
+  const int tiles = tab.first[a.groups], pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  if (MODE != kDw) {
+    clear_rows(a, 0, tab.off[0]);
+    clear_rows(a, tab.off[a.groups], a.rows);
+  }
+
+  if (warp == kEpiWarps) {
+    // ---- loads, by both CTAs
+    if (elect_one()) {
+      Ring<Pair::kStages> at;
+      bool ok = true, peek = false;
+      const uint32_t full0 = cluster_addr(full, 0);
+      for (int i = pair; i < tiles && ok; i += pairs) {
+        const Tile t = tile_at<MODE, 2 * kM, kPairCols, 32>(tab, a, i);
+        const int nk = (t.k + kK - 1) / kK, hcols = (t.cols + 31) / 32 * 16;   // columns of a CTA
+        const int m0 = t.m0 + rank * kM, h0 = rank * hcols;
+        const int boxes = (hcols + 63) / 64;
+        const uint32_t bytes = Pair::kA + boxes * 8192;
+        for (int c = 0; c < nk; ++c, at.next()) {
+          const int st = at.st;
+          if (!peek && !mbar_wait_hot(&empty[st], at.round ^ 1, &g_operator_error)) { ok = false; break; }
+          peek = at.peek(empty, 1);
+          const bool cut = MODE == kDw && t.k - c * kK < kK;
+          uint32_t bar = full0 + st * 8;
+          if (rank == 0) {
+            mbar_arrive_expect_tx(&full[st], cut ? bytes : 2 * bytes);
+          } else if (cut) {
+            bar = smem_u32(&tail[st]);
+            mbar_arrive_expect_tx(&tail[st], bytes);
+          }
+          unsigned char* A = As + st * Pair::kA;
+          unsigned char* B = Bs + st * Pair::kB;
+          if (MODE == kFwd) {
+            tma_load_3d_pair(A, &ta, bar, c * kK, m0, t.g);
+          } else if (MODE == kDx) {
+            tma_load_3d_pair(A, &ta, bar, m0, c * kK, t.g);
+            tma_load_3d_pair(A + 8192, &ta, bar, m0 + 64, c * kK, t.g);
+          } else {
+            tma_load_3d_pair(A, &ta, bar, m0, t.r0 + c * kK, 0);
+            tma_load_3d_pair(A + 8192, &ta, bar, m0 + 64, t.r0 + c * kK, 0);
           }
           for (int b = 0; b < boxes; ++b) {
             if (MODE == kDw)
-              tma_load_2d(B + b * 8192, &tb, bar, t.c0 + b * 64, t.r0 + c * kK);
+              tma_load_3d_pair(B + b * 8192, &tb, bar, t.c0 + h0 + b * 64, t.r0 + c * kK, 0);
             else
-              tma_load_2d(B + b * S::kBoxRows * 128, &tb, bar, c * kK, t.r0 + b * S::kBoxRows);
+              tma_load_3d_pair(B + b * 8192, &tb, bar, c * kK, t.r0 + h0 + b * 64, 0);
           }
         }
       }
     }
   } else if (warp == kEpiWarps + 1) {
-    // ---- matrix products
-    uint32_t it = 0, seg = 0;
-    bool ok = true;
-    const int fold = a.out_type == HA_TYPE_FP32 ? kFold : 0x7FFFFFFF;
-    for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
-      const Tile t = tile_at<MODE, NT>(sh, a, i);
-      const int nk = (t.k + kK - 1) / kK;
-      const int N = (t.cols + 15) / 16 * 16;
-      uint32_t idesc = idesc_of(a.in_type, kM, N);
-      if (MODE != kFwd) idesc |= 1u << 15;
-      if (MODE == kDw) idesc |= 1u << 16;
-      for (int c = 0; c < nk && ok; ++c, ++it) {
-        const int buf = seg & 1;
-        if (c % fold == 0) {
-          ok = mbar_wait(&sh.tempty[buf], ((seg >> 1) & 1) ^ 1, &g_operator_error);
+    // ---- matrix products, by the first CTA; the second cuts its own half of a group's end
+    const bool one = elect_one();
+    Ring<Pair::kStages> at;
+    uint32_t seg = 0, tails = 0;                       // tails: parity of each stage's `tail`
+    bool ok = true, peek = false;
+    constexpr int fold = FOLD ? kFold : 1 << 30;
+    for (int i = pair; i < tiles && ok; i += pairs) {
+      const Tile t = tile_at<MODE, 2 * kM, kPairCols, 32>(tab, a, i);
+      const int nk = (t.k + kK - 1) / kK, N = (t.cols + 31) / 32 * 32;
+      const uint32_t idesc = idesc_of(a.in_type, 2 * kM, N) | (MODE == kFwd ? 0u : 1u << 15) |
+                             (MODE == kDw ? 1u << 16 : 0u);
+      // The rows after a group's last are another group's: cleared up to the step's end.
+      auto cut_rows = [&](int st, int left) {
+        unsigned char* A = As + st * Pair::kA;
+        unsigned char* B = Bs + st * Pair::kB;
+        const int blocks = 2 + (N / 2 + 63) / 64, r1 = (left + 15) / 16 * 16, n = r1 - left;
+        for (int x = lane; x < blocks * n * 8; x += 32) {
+          const int line = x >> 3, b = line / n, r = left + line % n;
+          unsigned char* p = (b < 2 ? A + b * 8192 : B + (b - 2) * 8192) + r * 128 + (x & 7) * 16;
+          *reinterpret_cast<uint4*>(p) = make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async();
+        __syncwarp();
+      };
+      if (rank != 0) {
+        const int left = t.k % kK;
+        at.skip(nk - (left != 0));
+        if (left && MODE != kDw) at.next();
+        if (MODE == kDw && left) {
+          const int st = at.st;
+          at.next();
+          ok = mbar_wait_hot(&tail[st], tails >> st & 1, &g_operator_error);
+          tails ^= 1u << st;
           if (!ok) break;
-          tc_fence_after();
-        }
-        const int st = it % S::kStages;
-        ok = mbar_wait(&sh.full[st], (it / S::kStages) & 1, &g_operator_error);
-        if (!ok) break;
-        tc_fence_after();
-        const int left = t.k - c * kK, steps = left >= kK ? kK / 16 : (left + 15) / 16;
-        unsigned char* A = As + st * S::kA;
-        unsigned char* B = Bs + st * S::kB;
-        if (MODE == kDw && left < kK && (left & 15)) {
-          // The rows after the group's last are another group's: cleared up to the step's end.
-          const int blocks = 2 + (t.cols + 63) / 64;
-          const int r0 = left, r1 = steps * 16;
-          for (int x = lane; x < blocks * (r1 - r0) * 8; x += 32) {
-            const int line = x >> 3, b = line / (r1 - r0), r = r0 + line % (r1 - r0);
-            unsigned char* p = (b < 2 ? A + b * 8192 : B + (b - 2) * 8192) + r * 128 + (x & 7) * 16;
-            *reinterpret_cast<uint4*>(p) = make_uint4(0, 0, 0, 0);
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-        }
-        if (lane == 0) {
-          const uint32_t as = smem_u32(A), bs = smem_u32(B);
-          for (int k = 0; k < steps; ++k) {
-            const uint64_t da = MODE == kFwd ? umma_desc_sw128(as + k * 32) : umma_desc_sw128_mn(as + k * 2048, 8192);
-            const uint64_t db = MODE == kDw ? umma_desc_sw128_mn(bs + k * 2048, 8192) : umma_desc_sw128(bs + k * 32);
-            tc_mma_bf16(tmem + buf * NT, da, db, idesc, (c % fold) || k ? 1u : 0u);
-          }
-          tc_commit(&sh.empty[st]);
-          if (c % fold == fold - 1 || c == nk - 1) tc_commit(&sh.tfull[buf]);
-        }
-        __syncwarp();
-        if (c % fold == fold - 1 || c == nk - 1) ++seg;
-      }
-    }
-  } else {
-    // ---- results
-    uint32_t seg = 0;
-    bool ok = true;
-    const int half = warp >> 2, quad = warp & 3;       // columns' half; TMEM lanes 32 quad ..
-    const int et = tid & 127;                          // thread of the warp group
-    const int esize = a.out_type == HA_TYPE_FP32 ? 4 : 2;
-    unsigned char* stage = Out + half * S::kStage;
-    const int tc = a.out_type == HA_TYPE_FP32 ? 16 : 32;   // columns of a stage
-    for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
-      const Tile t = tile_at<MODE, NT>(sh, a, i);
-      const int nk = (t.k + kK - 1) / kK;
-      const int segs = a.out_type == HA_TYPE_FP32 ? (nk + kFold - 1) / kFold : (nk > 0 ? 1 : 0);
-      const int cb = half * (NT / 2), ce = min(NT / 2, t.cols - cb);   // this group's columns
-      float acc[NT / 2];
-#pragma unroll
-      for (int j = 0; j < NT / 2; ++j) acc[j] = 0.0f;
-      for (int s = 0; s < segs && ok; ++s, ++seg) {
-        const int buf = seg & 1;
-        ok = mbar_wait(&sh.tfull[buf], (seg >> 1) & 1, &g_operator_error);
-        if (!ok) break;
-        tc_fence_after();
-#pragma unroll
-        for (int j = 0; j < NT / 2; j += 32) {
-          if (j < ce) {
-            float v[32];
-            tmem_ld32(tmem + (static_cast<uint32_t>(quad * 32) << 16) + buf * NT + cb + j, v);
-            tmem_ld_wait();
-#pragma unroll
-            for (int x = 0; x < 32; ++x) acc[j + x] += v[x];
-          }
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.tempty[buf]);
-      }
-      if (!ok) break;
-      const int f = t.m0 + quad * 32 + lane;            // this thread's feature
-      if (MODE == kDw) {
-        if (f < a.m) {
-          const int64_t at = t.g * a.out_gs + f * a.out_ld + t.c0 + cb;
-#pragma unroll
-          for (int j = 0; j < NT / 2; j += 16) {
-            if (j >= ce) continue;
-            if (a.wide_out && j + 16 <= ce) {
-              if (a.out_type == HA_TYPE_FP32) {
-                float4* o = reinterpret_cast<float4*>(static_cast<float*>(a.out) + at + j);
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-                  o[x] = make_float4(acc[j + 4 * x], acc[j + 4 * x + 1], acc[j + 4 * x + 2], acc[j + 4 * x + 3]);
-              } else {
-                uint32_t w[8];
-#pragma unroll
-                for (int x = 0; x < 8; ++x)
-                  w[x] = narrow(acc[j + 2 * x], a.out_type) | (static_cast<uint32_t>(narrow(acc[j + 2 * x + 1], a.out_type)) << 16);
-                uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at + j);
-                o[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                o[1] = make_uint4(w[4], w[5], w[6], w[7]);
-              }
-            } else {
-#pragma unroll
-              for (int x = 0; x < 16; ++x)
-                if (j + x < ce) {
-                  if (a.out_type == HA_TYPE_FP32)
-                    static_cast<float*>(a.out)[at + j + x] = acc[j + x];
-                  else
-                    static_cast<uint16_t*>(a.out)[at + j + x] = narrow(acc[j + x], a.out_type);
-                }
-            }
-          }
+          cut_rows(st, left);
+          if (one) mbar_arrive_release_cluster(cluster_addr(&tail[st], 0));
         }
         continue;
       }
-      const float bias = MODE == kFwd && a.bias && f < a.m ? a.bias[t.g * a.bias_ld + f] : 0.0f;
-      // Through shared memory, so that a row's features leave as whole 16-byte vectors.
-#pragma unroll
-      for (int j0 = 0; j0 < NT / 2; j0 += 16) {
-        if (j0 % tc) continue;
-        const bool any = j0 < ce;
-        if (!any) continue;                            // the same for the whole warp group
-        named_barrier_sync(1 + half, 128);
-#pragma unroll
-        for (int x = 0; x < 32; ++x) {
-          if (x < tc && j0 + x < NT / 2) {
-            float v = acc[(j0 + x) % (NT / 2)] + bias;
-            if (MODE == kFwd && a.relu && v < 0.0f) v = 0.0f;
-            if (a.out_type == HA_TYPE_FP32)
-              reinterpret_cast<float*>(stage)[x * kM + quad * 32 + lane] = v;
-            else
-              reinterpret_cast<uint16_t*>(stage)[x * kM + quad * 32 + lane] = narrow(v, a.out_type);
-          }
+      // One lane waits and issues (a wait of all lanes takes the barrier unit 32 times as
+      // long); the others join it where a group's end has to be cut.
+      const bool cut = MODE == kDw && t.k % kK != 0;
+      auto issue = [&](int c, int steps) {
+        const int st = at.st;
+        const uint32_t as = smem_u32(As + st * Pair::kA), bs = smem_u32(Bs + st * Pair::kB);
+        const uint32_t d = tmem + (seg & 1) * kPairCols;
+#pragma unroll 4
+        for (int k = 0; k < steps; ++k) {
+          const uint64_t da = MODE == kFwd ? umma_desc_sw128(as + k * 32) : umma_desc_sw128_mn(as + k * 2048, 8192);
+          const uint64_t db = MODE == kDw ? umma_desc_sw128_mn(bs + k * 2048, 8192) : umma_desc_sw128(bs + k * 32);
+          tc_mma_pair(d, da, db, idesc, (c % fold) || k ? 1u : 0u);
         }
-        named_barrier_sync(1 + half, 128);
-        const int per = 16 / esize, segsr = kM / per;   // elements of a vector, vectors of a row
-        for (int x = et; x < tc * segsr; x += 128) {
-          const int r = x / segsr, e = x % segsr * per;
-          if (j0 + r >= ce || t.m0 + e >= a.m) continue;
-          const int64_t row = t.c0 + cb + j0 + r;
-          const int nf = min(per, a.m - t.m0 - e);
-          uint4 w = *reinterpret_cast<const uint4*>(stage + (r * kM + e) * esize);
-          if (MODE == kDx && a.h) {
-            const uint16_t* h = static_cast<const uint16_t*>(a.h) + row * a.h_ld + t.m0 + e;
-            uint16_t hv[8];
-            for (int y = 0; y < nf; ++y) hv[y] = h[y];
-            if (esize == 4) {
-              float* p = reinterpret_cast<float*>(&w);
-#pragma unroll
-              for (int y = 0; y < 4; ++y)
-                if (y < nf && !positive16(hv[y], a.in_type)) p[y] = 0.0f;
-            } else {
-              uint16_t* p = reinterpret_cast<uint16_t*>(&w);
-#pragma unroll
-              for (int y = 0; y < 8; ++y)
-                if (y < nf && !positive16(hv[y], a.in_type)) p[y] = 0;
-            }
-          }
-          unsigned char* o = static_cast<unsigned char*>(a.out) + (row * a.out_ld + t.m0 + e) * esize;
-          if (a.wide_out && nf == per) {
-            *reinterpret_cast<uint4*>(o) = w;
-          } else if (esize == 4) {
-            const float* p = reinterpret_cast<const float*>(&w);
-            for (int y = 0; y < nf; ++y) reinterpret_cast<float*>(o)[y] = p[y];
-          } else {
-            const uint16_t* p = reinterpret_cast<const uint16_t*>(&w);
-            for (int y = 0; y < nf; ++y) reinterpret_cast<uint16_t*>(o)[y] = p[y];
-          }
+        tc_commit_pair(&empty[st]);
+        if (c % fold == fold - 1 || c == nk - 1) tc_commit_pair(&tfull[seg & 1]);
+      };
+      auto ready = [&](int c) {
+        if (c % fold == 0 && !mbar_wait_hot(&tempty[seg & 1], ((seg >> 1) & 1) ^ 1, &g_operator_error)) return false;
+        if (!peek && !mbar_wait_hot(&full[at.st], at.round, &g_operator_error)) return false;
+        peek = at.peek(full, 0);
+        tc_fence_after();
+        return true;
+      };
+      const int whole = nk - (cut ? 1 : 0);
+      const Ring<Pair::kStages> at0 = at;
+      const uint32_t seg0 = seg;
+      if (one) {
+        for (int c = 0; c < whole; ++c, at.next()) {
+          ok = ready(c);
+          if (!ok) break;
+          issue(c, (min(t.k - c * kK, kK) + 15) / 16);
+          if (c % fold == fold - 1 || c == nk - 1) ++seg;
         }
       }
+      ok = __all_sync(~0u, ok);
+      peek = __any_sync(~0u, one && peek);
+      at = at0;
+      at.skip(whole);
+      seg = seg0 + (cut ? whole / fold : (nk + fold - 1) / fold);
+      if (cut && ok) {
+        const int st = at.st, left = t.k % kK;
+        ok = ready(whole);
+        if (ok) {
+          cut_rows(st, left);
+          ok = mbar_wait_cluster(&tail[st], tails >> st & 1, &g_operator_error);
+          tails ^= 1u << st;
+          tc_fence_after();
+          if (one && ok) issue(whole, (left + 15) / 16);
+          __syncwarp();
+        }
+        at.next();
+        ++seg;
+      }
+      ok = __all_sync(~0u, ok);
     }
+  } else {
+    // ---- results, by both CTAs
+    uint32_t seg = 0, turn = 0;
+    bool ok = true;
+    for (int i = pair; i < tiles && ok; i += pairs) {
+      const Tile t = tile_at<MODE, 2 * kM, kPairCols, 32>(tab, a, i);
+      ok = finish_tile<MODE, kPairCols, FOLD>(
+          a, &to, t, tmem, t.m0 + rank * kM, Out, seg, turn,
+          [&](uint32_t s) {
+            return warp_wait(&tfull[s & 1], (s >> 1) & 1);
+          },
+          [&](uint32_t s) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(cluster_addr(&tempty[s & 1], 0));
+          });
+    }
+    if (MODE == kDw && lane == 0) tma_store_wait_all();
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == kEpiWarps) {
-    tmem_dealloc(tmem, S::kTmem);
-    tmem_relinquish();
-  }
+  cluster_sync_all();
+  if (warp == kEpiWarps) tmem_dealloc_pair(tmem, 2 * kPairCols);
 }
 
 // db_g[f] = sum of dy[t][f] over the group's rows: a CTA has 32 features, its warps take
@@ -443,15 +767,18 @@ __global__ void __launch_bounds__(256) k_pack(const uint16_t* src, int64_t rows,
 }
 
 constexpr int kSms = 152;
+// Groups of at most this many rows on average take the tiles for few rows.
+constexpr int kFewRows = 32;
 int64_t round8(int64_t x) { return (x + 7) / 8 * 8; }
 int64_t round256(int64_t x) { return (x + 255) / 256 * 256; }
 
-// One operand as the tensor maps need it: address and strides multiples of 16 bytes.
+// One operand as the tensor maps need it: address, strides and width multiples of 16 bytes (the
+// edge of a map is only sure to cut whole 16-byte pieces).
 struct Operand {
   const void* p;
   int64_t groups, rows, cols, ld, gs;   // gs: between groups (groups > 1)
   bool fits() const {
-    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0 &&
+    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0 && cols % 8 == 0 &&
            (groups == 1 || (gs > 0 && gs % 8 == 0));   // one matrix for all groups is copied
   }
   int64_t packed_bytes() const { return fits() ? 0 : round256(groups * rows * round8(cols) * 2); }
@@ -470,27 +797,61 @@ cudaError_t pack(Operand& o, unsigned char*& ws, cudaStream_t s) {
   return cudaGetLastError();
 }
 
-bool make_map(CUtensorMap* m, const Operand& o, int type, bool grouped, uint32_t b0, uint32_t b1) {
+// Three dimensions always; box {b0, b1, 1}.
+bool make_map(CUtensorMap* m, const Operand& o, int type, uint32_t b0, uint32_t b1) {
   const EncodeTiledFn enc = encode_fn();
   if (!enc) return false;
+  const int es = type_size(type);
   const cuuint64_t dims[3] = {static_cast<cuuint64_t>(o.cols), static_cast<cuuint64_t>(o.rows),
                               static_cast<cuuint64_t>(o.groups)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(o.ld * 2),
-                                 static_cast<cuuint64_t>((o.groups == 1 ? o.rows * o.ld : o.gs) * 2)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(o.ld * es),
+                                 static_cast<cuuint64_t>((o.groups == 1 ? o.rows * o.ld : o.gs) * es)};
   const cuuint32_t box[3] = {b0, b1, 1}, one[3] = {1, 1, 1};
-  return enc(m, type == HA_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-             grouped ? 3 : 2, const_cast<void*>(o.p), dims, strides, box, one,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const CUtensorMapDataType dt = type == HA_TYPE_FP32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                 : type == HA_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                        : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  return enc(m, dt, 3, const_cast<void*>(o.p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int MODE, int NT>
-int launch(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int64_t max_tiles, cudaStream_t s) {
-  const int smem = Shape<NT>::kSmem;
-  if (cudaFuncSetAttribute(k_grouped<MODE, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+template <int MODE, bool FOLD>
+int launch_few(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int64_t most, cudaStream_t s) {
+  if (cudaFuncSetAttribute(k_grouped_few<MODE, FOLD>, cudaFuncAttributeMaxDynamicSharedMemorySize, Few::kSmem) !=
+      cudaSuccess)
     return HA_ECUDA;
-  const int64_t grid = std::min<int64_t>(kSms, std::max<int64_t>(max_tiles, 1));
-  k_grouped<MODE, NT><<<static_cast<unsigned>(grid), kThreads, smem, s>>>(ta, tb, a);
+  k_grouped_few<MODE, FOLD><<<static_cast<unsigned>(std::min<int64_t>(kSms, std::max<int64_t>(most, 1))), kThreads,
+                             Few::kSmem, s>>>(ta, tb, a);
+  return cudaGetLastError() == cudaSuccess ? HA_OK : HA_ECUDA;
+}
+
+template <int MODE, bool FOLD>
+int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to, const Args& a, int64_t most,
+                cudaStream_t s) {
+  if (cudaFuncSetAttribute(k_grouped_pair<MODE, FOLD>, cudaFuncAttributeMaxDynamicSharedMemorySize, Pair::kSmem) !=
+      cudaSuccess)
+    return HA_ECUDA;
+  // As many pairs as the GPU holds at once (its clusters of two leave some SMs out): the tiles
+  // are dealt out in advance, so a pair that started late would finish late.
+  static int held = 0;
+  if (held == 0) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kSms);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Pair::kSmem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, k_grouped_pair<MODE, FOLD>, &cfg) != cudaSuccess || n < 1) return HA_ECUDA;
+    held = n;
+  }
+  const int64_t pairs = std::min<int64_t>(held, std::max<int64_t>(most, 1));
+  k_grouped_pair<MODE, FOLD><<<static_cast<unsigned>(2 * pairs), kThreads, Pair::kSmem, s>>>(ta, tb, to, a);
   return cudaGetLastError() == cudaSuccess ? HA_OK : HA_ECUDA;
 }
 
@@ -511,15 +872,17 @@ int rows_product(Operand x, Operand w, Args a, void* ws, int64_t ws_bytes, cudaS
   unsigned char* p = static_cast<unsigned char*>(ws);
   if (pack(x, p, s) != cudaSuccess || pack(w, p, s) != cudaSuccess) return HA_ECUDA;
   a.wide_out = (reinterpret_cast<uintptr_t>(a.out) & 15) == 0 && a.out_ld * type_size(a.out_type) % 16 == 0;
-  // Few rows a group: narrow tiles, whose smaller chunks leave room for more in flight.
-  const bool few = a.rows <= 64 * static_cast<int64_t>(a.groups);
+  a.wide_h = a.h && (reinterpret_cast<uintptr_t>(a.h) & 15) == 0 && a.h_ld % 8 == 0;
+  const bool few = a.rows <= kFewRows * static_cast<int64_t>(a.groups), fold = a.out_type == HA_TYPE_FP32;
   CUtensorMap ta, tb;
-  if (!make_map(&ta, w, a.in_type, true, 64, MODE == kFwd ? 128 : 64) ||
-      !make_map(&tb, x, a.in_type, false, 64, few ? Shape<64>::kBoxRows : Shape<256>::kBoxRows))
+  if (!make_map(&ta, w, a.in_type, 64, MODE == kFwd ? 128 : 64) || !make_map(&tb, x, a.in_type, 64, few ? 16 : 64))
     return HA_ECUDA;
-  const int64_t mt = (a.m + kM - 1) / kM;
-  const int64_t most = mt * std::min<int64_t>(a.rows, a.groups + a.rows / (few ? 64 : 256));
-  return few ? launch<MODE, 64>(ta, tb, a, most, s) : launch<MODE, 256>(ta, tb, a, most, s);
+  if (few) {
+    const int64_t most = (a.m + kM - 1) / kM * std::min<int64_t>(a.rows, a.groups + a.rows / kFewCols);
+    return fold ? launch_few<MODE, true>(ta, tb, a, most, s) : launch_few<MODE, false>(ta, tb, a, most, s);
+  }
+  const int64_t most = (a.m + 2 * kM - 1) / (2 * kM) * std::min<int64_t>(a.rows, a.groups + a.rows / kPairCols);
+  return fold ? launch_pair<MODE, true>(ta, tb, ta, a, most, s) : launch_pair<MODE, false>(ta, tb, ta, a, most, s);
 }
 
 }  // namespace
@@ -620,9 +983,8 @@ extern "C" int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, co
   Operand dy = {dy_dev, 1, rows, outer, dy_ld, 0}, x = {x_dev, 1, rows, inner, x_ld, 0};
   if (rows == 0) {
     // The maps below need an address and a row; nothing is read, since every group is empty.
-    dy = {dw_dev, 1, 1, outer, round8(outer), 0};
-    x = {dw_dev, 1, 1, inner, round8(inner), 0};
-    dy.p = x.p = reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(dw_dev) & ~uintptr_t(15));
+    const void* p16 = reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(dw_dev) & ~uintptr_t(15));
+    dy = x = {p16, 1, 1, 8, 8, 0};
   }
   if (dy.packed_bytes() + x.packed_bytes() > workspace_bytes) return HA_ENOMEM;
   if (workspace_bytes > 0 && (!workspace_dev || (reinterpret_cast<uintptr_t>(workspace_dev) & 15)))
@@ -651,13 +1013,19 @@ extern "C" int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, co
   a.in_type = type;
   a.out_type = dw_type;
   const int es = type_size(dw_type);
-  a.wide_out = (reinterpret_cast<uintptr_t>(dw_dev) & 15) == 0 && dw_ld * es % 16 == 0 &&
+  a.wide_out = (reinterpret_cast<uintptr_t>(dw_dev) & 15) == 0 && dw_ld * es % 16 == 0 && inner * es % 16 == 0 &&
                (groups == 1 || dw_gs * es % 16 == 0);
-  CUtensorMap ta, tb;
-  if (!make_map(&ta, dy, type, false, 64, 64) || !make_map(&tb, x, type, false, 64, 64)) return HA_ECUDA;
-  const int64_t most = groups * static_cast<int64_t>((outer + kM - 1) / kM) * ((inner + 255) / 256);
+  CUtensorMap ta, tb, to;
+  if (!make_map(&ta, dy, type, 64, 64) || !make_map(&tb, x, type, 64, 64)) return HA_ECUDA;
+  to = ta;
+  if (a.wide_out &&
+      !make_map(&to, {dw_dev, groups, outer, inner, dw_ld, dw_gs}, dw_type, dw_type == HA_TYPE_FP32 ? 32 : 64, 32))
+    return HA_ECUDA;
+  const int64_t most = groups * static_cast<int64_t>((outer + 2 * kM - 1) / (2 * kM)) *
+                       ((inner + kPairCols - 1) / kPairCols);
   if (most > 0x7FFFFFFF) return HA_EUNSUPPORTED;
-  return launch<kDw, 256>(ta, tb, a, most, s);
+  return dw_type == HA_TYPE_FP32 ? launch_pair<kDw, true>(ta, tb, to, a, most, s)
+                                 : launch_pair<kDw, false>(ta, tb, to, a, most, s);
 }
 
 extern "C" int hier_avg_operator_check(void* stream) {

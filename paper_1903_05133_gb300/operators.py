@@ -110,7 +110,7 @@ def _out_type(out_dtype, out, dtype):
 
 def _workspace(lib, op, a, a_ld, b, b_ld, b_gs, groups, rows, inner, outer):
     """Device memory for operands that have to be copied first (None where there are none)."""
-    if not (a_ld & 7 or b_ld & 7 or (b_gs & 7 or b_gs <= 0) and groups > 1 and op != DW or
+    if not ((a_ld | b_ld | inner | outer) & 7 or (b_gs & 7 or b_gs <= 0) and groups > 1 and op != DW or
             (a.data_ptr() | b.data_ptr()) & 15) or rows == 0:
         return None, None, 0
     n = c_int64()

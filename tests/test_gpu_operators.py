@@ -150,6 +150,15 @@ def test_product_strides(K, N):
         assert (out[1, :, :K] == 0).all() and out[:, :, K:].isnan().all()
         big[1:T + 1, shift:shift + N] = float("nan")
         assert big.isnan().all()                          # nothing outside the window changed
+    # aligned rows whose width is not: what lies between them is not read
+    wide = -(-max(K, N) // 8) * 8 + 8
+    X = torch.full((T, wide), float("nan"), dtype=BF, device="cuda")[:, :K].copy_(randn(g, T, K, dtype=BF))
+    W = torch.full((3, N, wide), float("nan"), dtype=BF, device="cuda")[:, :, :K].copy_(randn(g, 3, N, K, dtype=BF))
+    D = torch.full((T, wide), float("nan"), dtype=BF, device="cuda")[:, :N].copy_(randn(g, T, N, dtype=BF))
+    for got, ref, n in ((ops.grouped_product(X, W, off), ref_rows(X, W, sizes, True), K),
+                        (ops.grouped_product_dx(D, W, off), ref_rows(D, W, sizes, False), N),
+                        (ops.grouped_product_dw(D, X, off)[2], (D[30:].double().T @ X[30:].double(), D[30:].double().abs().T @ X[30:].double().abs()), 71)):
+        assert_within(got, ref[0], product_bound(ref[0], ref[1], n, BF))
     one = randn(g, N, K, dtype=BF)
     x = randn(g, T, K, dtype=BF)
     shared = ops.grouped_product(x, one.expand(3, N, K), off)
