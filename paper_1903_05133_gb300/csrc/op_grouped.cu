@@ -311,12 +311,8 @@ struct Ring {
       round ^= 1;
     }
   }
-  // Whether the next stage is ready, asked a chunk ahead: even a barrier whose phase is over
-  // takes 170 cycles to answer.
-  __device__ __forceinline__ bool peek(uint64_t* bars, uint32_t flip) const {
-    const bool wrap = st + 1 == STAGES;
-    return mbar_test(&bars[wrap ? 0 : st + 1], (wrap ? round ^ 1 : round) ^ flip);
-  }
+  __device__ __forceinline__ uint32_t next_st() const { return st + 1 == STAGES ? 0 : st + 1; }
+  __device__ __forceinline__ uint32_t next_round() const { return st + 1 == STAGES ? round ^ 1 : round; }
   __device__ __forceinline__ void skip(int n) {
     const uint32_t at = st + static_cast<uint32_t>(n);
     st = at % STAGES;
@@ -436,15 +432,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---- loads
     if (elect_one()) {
       Ring<Few::kStages> at;
-      bool ok = true, peek = false;
+      bool ok = true;
       const uint64_t stream = l2_stream_policy(true), keep = l2_stream_policy(false);
       for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
         const Tile t = tile_at<MODE, kM, kFewCols, 16>(tab, a, i);
         const int nk = (t.k + kK - 1) / kK, boxes = (t.cols + 15) / 16;
         for (int c = 0; c < nk; ++c, at.next()) {
           const int st = at.st;
-          if (!peek && !mbar_wait_hot(&empty[st], at.round ^ 1, &g_operator_error)) { ok = false; break; }
-          peek = at.peek(empty, 1);
+          if (!mbar_wait_hot(&empty[st], at.round ^ 1, &g_operator_error)) { ok = false; break; }
           uint64_t* bar = &full[st];
           mbar_arrive_expect_tx(bar, Few::kA + boxes * 2048);
           unsigned char* A = As + st * Few::kA;
@@ -475,15 +470,21 @@ __global__ void __launch_bounds__(kThreads, 1)
           ok = (c % fold != 0 || mbar_wait_hot(&tempty[buf], ((seg >> 1) & 1) ^ 1, &g_operator_error)) &&
                (peek || mbar_wait_hot(&full[at.st], at.round, &g_operator_error));
           if (!ok) break;
-          peek = at.peek(full, 0);
           tc_fence_after();
           const int steps = (min(t.k - c * kK, kK) + 15) / 16;
           const uint32_t as = smem_u32(As + at.st * Few::kA), bs = smem_u32(Bs + at.st * Few::kB);
-          for (int k = 0; k < steps; ++k) {
-            const uint64_t da = MODE == kFwd ? umma_desc_sw128(as + k * 32) : umma_desc_sw128_mn(as + k * 2048, 8192);
-            tc_mma_bf16(tmem + buf * kFewCols, da, umma_desc_sw128(bs + k * 32), idesc, (c % fold) || k ? 1u : 0u);
+          const uint64_t da = MODE == kFwd ? umma_desc_sw128(as) : umma_desc_sw128_mn(as, 8192);
+          const uint64_t db = umma_desc_sw128(bs);
+          constexpr int SA = MODE == kFwd ? 2 : 128;           // 16 values further, in 16 bytes
+          if (steps == 4) {
+            peek = tc_chunk<SA, 2>(tmem + buf * kFewCols, da, db, idesc, c % fold != 0, &empty[at.st],
+                                   &full[at.next_st()], at.next_round());
+          } else {
+            for (int k = 0; k < steps; ++k)
+              tc_mma_bf16(tmem + buf * kFewCols, da + k * SA, db + k * 2, idesc, (c % fold) || k ? 1u : 0u);
+            tc_commit(&empty[at.st]);
+            peek = false;
           }
-          tc_commit(&empty[at.st]);
           if (c % fold == fold - 1 || c == nk - 1) {
             tc_commit(&tfull[buf]);
             ++seg;
@@ -575,7 +576,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     // ---- loads, by both CTAs
     if (elect_one()) {
       Ring<Pair::kStages> at;
-      bool ok = true, peek = false;
+      bool ok = true;
       const uint32_t full0 = cluster_addr(full, 0);
       for (int i = pair; i < tiles && ok; i += pairs) {
         const Tile t = tile_at<MODE, 2 * kM, kPairCols, 32>(tab, a, i);
@@ -585,8 +586,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
         const uint32_t bytes = Pair::kA + boxes * 8192;
         for (int c = 0; c < nk; ++c, at.next()) {
           const int st = at.st;
-          if (!peek && !mbar_wait_hot(&empty[st], at.round ^ 1, &g_operator_error)) { ok = false; break; }
-          peek = at.peek(empty, 1);
+          if (!mbar_wait_hot(&empty[st], at.round ^ 1, &g_operator_error)) { ok = false; break; }
           const bool cut = MODE == kDw && t.k - c * kK < kK;
           uint32_t bar = full0 + st * 8;
           if (rank == 0) {
@@ -662,19 +662,22 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
         const int st = at.st;
         const uint32_t as = smem_u32(As + st * Pair::kA), bs = smem_u32(Bs + st * Pair::kB);
         const uint32_t d = tmem + (seg & 1) * kPairCols;
-#pragma unroll 4
-        for (int k = 0; k < steps; ++k) {
-          const uint64_t da = MODE == kFwd ? umma_desc_sw128(as + k * 32) : umma_desc_sw128_mn(as + k * 2048, 8192);
-          const uint64_t db = MODE == kDw ? umma_desc_sw128_mn(bs + k * 2048, 8192) : umma_desc_sw128(bs + k * 32);
-          tc_mma_pair(d, da, db, idesc, (c % fold) || k ? 1u : 0u);
+        const uint64_t da = MODE == kFwd ? umma_desc_sw128(as) : umma_desc_sw128_mn(as, 8192);
+        const uint64_t db = MODE == kDw ? umma_desc_sw128_mn(bs, 8192) : umma_desc_sw128(bs);
+        constexpr int SA = MODE == kFwd ? 2 : 128, SB = MODE == kDw ? 128 : 2;   // 16 values further
+        if (steps == 4) {
+          peek = tc_chunk_pair<SA, SB>(d, da, db, idesc, c % fold != 0, &empty[st], &full[at.next_st()],
+                                       at.next_round());
+        } else {
+          for (int k = 0; k < steps; ++k) tc_mma_pair(d, da + k * SA, db + k * SB, idesc, (c % fold) || k ? 1u : 0u);
+          tc_commit_pair(&empty[st]);
+          peek = false;
         }
-        tc_commit_pair(&empty[st]);
         if (c % fold == fold - 1 || c == nk - 1) tc_commit_pair(&tfull[seg & 1]);
       };
       auto ready = [&](int c) {
         if (c % fold == 0 && !mbar_wait_hot(&tempty[seg & 1], ((seg >> 1) & 1) ^ 1, &g_operator_error)) return false;
         if (!peek && !mbar_wait_hot(&full[at.st], at.round, &g_operator_error)) return false;
-        peek = at.peek(full, 0);
         tc_fence_after();
         return true;
       };
@@ -690,7 +693,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
         }
       }
       ok = __all_sync(~0u, ok);
-      peek = __any_sync(~0u, one && peek);
+      peek = __any_sync(~0u, one && peek);             // of the first CTA's issuing lane
       at = at0;
       at.skip(whole);
       seg = seg0 + (cut ? whole / fold : (nk + fold - 1) / fold);

@@ -197,6 +197,58 @@ __device__ __forceinline__ void tc_commit_pair(uint64_t* bar) {
 }
 __device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
 
+// ------------------------------------------------ one chunk of 64 summed values
+// Four MMAs (descriptors SA and SB further on each), their commit to `done`, and whether the
+// phase of `next` is over: asked before the MMAs and read after them, since a barrier takes 170
+// cycles to answer even when it is.
+template <int SA, int SB>
+__device__ __forceinline__ bool tc_chunk(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate,
+                                   uint64_t* done, uint64_t* next, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p, q, t;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 q, [%7], %8;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "setp.eq.b32 t, 0, 0;\n\t"
+      "add.s64 a1, %2, %9;\n\tadd.s64 a2, a1, %9;\n\tadd.s64 a3, a2, %9;\n\t"
+      "add.s64 b1, %3, %10;\n\tadd.s64 b2, b1, %10;\n\tadd.s64 b3, b2, %10;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%1], %2, %3, %4, p;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%1], a1, b1, %4, t;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%1], a2, b2, %4, t;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%1], a3, b3, %4, t;\n\t"
+      "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%6];\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(ok)
+      : "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(smem_u32(done)), "r"(smem_u32(next)), "r"(parity),
+        "n"(SA), "n"(SB)
+      : "memory");
+  return ok != 0;
+}
+// The same for a pair of CTAs.
+template <int SA, int SB>
+__device__ __forceinline__ bool tc_chunk_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate,
+                                   uint64_t* done, uint64_t* next, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p, q, t;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 q, [%7], %8;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "setp.eq.b32 t, 0, 0;\n\t"
+      "add.s64 a1, %2, %9;\n\tadd.s64 a2, a1, %9;\n\tadd.s64 a3, a2, %9;\n\t"
+      "add.s64 b1, %3, %10;\n\tadd.s64 b2, b1, %10;\n\tadd.s64 b3, b2, %10;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%1], %2, %3, %4, p;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%1], a1, b1, %4, t;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%1], a2, b2, %4, t;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%1], a3, b3, %4, t;\n\t"
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%6], %11;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(ok)
+      : "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(smem_u32(done)), "r"(smem_u32(next)), "r"(parity),
+        "n"(SA), "n"(SB), "h"(static_cast<uint16_t>(3))
+      : "memory");
+  return ok != 0;
+}
+
 // ------------------------------------------------ cross-CTA flags (global)
 // Add to a global counter with release order (prior writes of this thread, and
 // those it has observed, are visible before the new value); nothing is returned.
