@@ -26,7 +26,8 @@ constexpr int kM = 128;                 // features of a CTA's tile
 constexpr int kK = 64;                  // values summed over in a chunk: one 128-byte line
 constexpr int kMaxGroups = 1024;
 constexpr int kEpiWarps = 8;            // two groups of four: a group reads half the columns
-constexpr int kThreads = (kEpiWarps + 2) * 32;
+constexpr int kThreads = (kEpiWarps + 2) * 32;          // results, loads, products
+constexpr int kDwThreads = kThreads + 32;               // and the ends of groups
 constexpr int kPairCols = 256;          // columns of a tile of two CTAs
 constexpr int kFewCols = 32;            // of a tile of one CTA, where groups have few rows
 // fp32 results: the tensor core's running sum is taken into fp32 registers after this many
@@ -39,9 +40,10 @@ struct Args {
   const int* offsets;
   void* out;
   const float* bias;          // forward, or nullptr
+  float* db;                  // weights' gradient: the bias's, or nullptr
   const void* h;              // gradient of rows: the mask's activations, or nullptr
   int64_t out_ld, out_gs;     // in elements; out_gs: between groups of dW
-  int64_t bias_ld, h_ld;
+  int64_t bias_ld, h_ld;      // bias_ld: db's too
   int groups, rows;
   int m, n, k;                // features; dW: columns; summed length (forward, rows)
   int in_type, out_type;
@@ -52,6 +54,7 @@ struct Args {
 
 struct Tile {
   int g, m0, c0, cols, r0, k;   // group, first feature, first column, columns, first row, length
+  bool bias;                    // the sums of dy instead of a part of dW
 };
 
 // Column tiles of a group of n rows: as few as fit, of equal size.
@@ -87,13 +90,13 @@ struct Table {
 constexpr int kTableBytes = 2 * (kMaxGroups + 1) * 4;
 
 // The list of tiles, by all threads; ends with a CTA barrier.
-template <int MODE, int M, int NT>
+template <int MODE, int M, int NT, int THREADS>
 __device__ __forceinline__ void make_table(const Table& s, const Args& a) {
   const int tid = threadIdx.x, lane = tid & 31;
-  for (int g = tid; g <= a.groups; g += kThreads) s.off[g] = min(max(a.offsets[g], 0), a.rows);
+  for (int g = tid; g <= a.groups; g += THREADS) s.off[g] = min(max(a.offsets[g], 0), a.rows);
   __syncthreads();
   if (tid < 32) {
-    const int mt = (a.m + M - 1) / M, nt = (a.n + NT - 1) / NT;
+    const int mt = (a.m + M - 1) / M, nt = (a.n + NT - 1) / NT + (MODE == kDw && a.db ? 1 : 0);
     int run = 0;
     for (int g0 = 0; g0 < a.groups; g0 += 32) {
       const int g = g0 + lane;
@@ -114,33 +117,42 @@ __device__ __forceinline__ void make_table(const Table& s, const Args& a) {
   __syncthreads();
 }
 
-// STEP: the columns of a tile are a multiple of it (but for the group's end).
+// The tiles of a CTA (or pair), in rising order.  STEP: the columns of a tile are a multiple of
+// it (but for the group's end).
 template <int MODE, int M, int NT, int STEP>
-__device__ __forceinline__ Tile tile_at(const Table& s, const Args& a, int i) {
-  int lo = 0, hi = a.groups;             // first[lo] <= i < first[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (s.first[mid] <= i) lo = mid; else hi = mid;
+struct Tiles {
+  const Table& s;
+  const Args& a;
+  const int mt;
+  int g = 0;
+  __device__ __forceinline__ Tiles(const Table& s, const Args& a) : s(s), a(a), mt((a.m + M - 1) / M) {}
+  __device__ __forceinline__ Tile at(int i) {
+    if (MODE == kDw)
+      g = i / s.first[1];                  // as many tiles in every group
+    else
+      while (s.first[g + 1] <= i) ++g;
+    const int x = i - s.first[g];
+    Tile t;
+    t.g = g;
+    const int ct = x / mt, low = s.off[g], n = max(0, s.off[g + 1] - low);
+    t.m0 = (x - ct * mt) * M;
+    t.bias = false;
+    if (MODE == kDw) {
+      t.c0 = ct * NT;
+      t.bias = t.c0 >= a.n;
+      t.cols = t.bias ? 32 : min(NT, a.n - t.c0);
+      t.r0 = low;
+      t.k = n;
+    } else {
+      const int parts = col_tiles(n, NT), size = ((n + parts - 1) / parts + STEP - 1) / STEP * STEP;
+      t.c0 = low + ct * size;
+      t.cols = min(size, n - ct * size);
+      t.r0 = t.c0;
+      t.k = a.k;
+    }
+    return t;
   }
-  const int mt = (a.m + M - 1) / M, at = i - s.first[lo];
-  Tile t;
-  t.g = lo;
-  t.m0 = at % mt * M;
-  const int ct = at / mt, n = max(0, s.off[lo + 1] - s.off[lo]);
-  if (MODE == kDw) {
-    t.c0 = ct * NT;
-    t.cols = min(NT, a.n - t.c0);
-    t.r0 = s.off[lo];
-    t.k = n;
-  } else {
-    const int parts = col_tiles(n, NT), size = ((n + parts - 1) / parts + STEP - 1) / STEP * STEP;
-    t.c0 = s.off[lo] + ct * size;
-    t.cols = min(size, n - ct * size);
-    t.r0 = t.c0;
-    t.k = a.k;
-  }
-  return t;
-}
+};
 
 // The rows that no group covers are zero.
 __device__ void clear_rows(const Args& a, int64_t begin, int64_t end) {
@@ -327,7 +339,7 @@ __device__ __forceinline__ bool finish_tile(const Args& a, const CUtensorMap* to
                                             Wait wait, Free release) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2, quad = warp & 3;
   const int nk = (t.k + kK - 1) / kK;
-  const int segs = FOLD ? (nk + kFold - 1) / kFold : (nk > 0 ? 1 : 0);
+  const int segs = FOLD || t.bias ? (nk + kFold - 1) / kFold : (nk > 0 ? 1 : 0);
   constexpr int H = NT / 2;
   const int cb = half * H, ce = min(H, t.cols - cb);      // this warp group's columns
   const int f = cta_m0 + quad * 32 + lane;                // this thread's feature
@@ -349,6 +361,22 @@ __device__ __forceinline__ bool finish_tile(const Args& a, const CUtensorMap* to
     else tmem_ld16(at, v);
     tmem_ld_wait();
   };
+  if (MODE == kDw && t.bias) {
+    // every column has the sums of dy
+    float sum = 0.0f;
+    for (int s = 0; s < segs; ++s) {
+      if (!wait(seg)) return false;
+      if (half == 0) {
+        float v[16];
+        tmem_ld16(tmem + (static_cast<uint32_t>(quad * 32) << 16) + (seg & 1) * NT, v);
+        tmem_ld_wait();
+        sum += v[0];
+      }
+      release(seg++);
+    }
+    if (half == 0 && f < a.m) a.db[t.g * a.bias_ld + f] = sum;
+    return true;
+  }
   if (!FOLD) {
     if (segs && !wait(seg)) return false;
 #pragma unroll 1
@@ -421,7 +449,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_barrier_init();
   }
   tc_fence_before();
-  make_table<MODE, kM, kFewCols>(tab, a);
+  make_table<MODE, kM, kFewCols, kThreads>(tab, a);
+  Tiles<MODE, kM, kFewCols, 16> list(tab, a);
   tc_fence_after();
   const uint32_t tmem = tmem_at;
   const int tiles = tab.first[a.groups];
@@ -435,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool ok = true;
       const uint64_t stream = l2_stream_policy(true), keep = l2_stream_policy(false);
       for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
-        const Tile t = tile_at<MODE, kM, kFewCols, 16>(tab, a, i);
+        const Tile t = list.at(i);
         const int nk = (t.k + kK - 1) / kK, boxes = (t.cols + 15) / 16;
         for (int c = 0; c < nk; ++c, at.next()) {
           const int st = at.st;
@@ -462,7 +491,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool ok = true, peek = false;
       constexpr int fold = FOLD ? kFold : 1 << 30;
       for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
-        const Tile t = tile_at<MODE, kM, kFewCols, 16>(tab, a, i);
+        const Tile t = list.at(i);
         const int nk = (t.k + kK - 1) / kK;
         const uint32_t idesc = idesc_of(a.in_type, kM, (t.cols + 15) / 16 * 16) | (MODE == kFwd ? 0u : 1u << 15);
         for (int c = 0; c < nk; ++c, at.next()) {
@@ -497,7 +526,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t seg = 0, turn = 0;
     bool ok = true;
     for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
-      const Tile t = tile_at<MODE, kM, kFewCols, 16>(tab, a, i);
+      const Tile t = list.at(i);
       ok = finish_tile<MODE, kFewCols, FOLD>(
           a, nullptr, t, tmem, t.m0, Out, seg, turn,
           [&](uint32_t s) {
@@ -524,18 +553,18 @@ __global__ void __launch_bounds__(kThreads, 1)
 struct Pair {
   static constexpr int kA = kM * kK * 2, kB = kPairCols / 2 * kK * 2, kStages = 5;
   static constexpr int kOut = 2 * kRowsStage;             // = kEpiWarps * kWarpStage
-  static constexpr int kSmem = kStages * (kA + kB) + kOut + 1024;
+  static constexpr int kOnes = 8192;                      // dW: a column block of ones, for the bias
+  static constexpr int kSmem = kStages * (kA + kB) + kOut + kOnes + 1024;
 };
 static_assert(2 * kRowsStage == kEpiWarps * kWarpStage, "one buffer serves both kinds of results");
 
 template <int MODE, bool FOLD>
-__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
+__global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __cluster_dims__(2, 1, 1)
     k_grouped_pair(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
                    const __grid_constant__ CUtensorMap to, const __grid_constant__ Args a) {
   extern __shared__ unsigned char raw[];
-  // full: the first CTA's, on which both CTAs' loads are counted.  tempty: the first CTA's too.
-  // tail: the second CTA's load of a chunk that has to be cut, or (in the first CTA) that the
-  // second has cut it.
+  // full: the first CTA's, on which both CTAs' loads and two arrivals are counted.  tempty: the
+  // first CTA's too.  tail: this CTA's load of a chunk in which a group ends.
   __shared__ uint64_t full[Pair::kStages], empty[Pair::kStages], tfull[2], tempty[2], tail[Pair::kStages];
   __shared__ uint32_t tmem_at;
   __shared__ int table[2 * (kMaxGroups + 1)];
@@ -543,6 +572,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
   unsigned char* As = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   unsigned char* Bs = As + Pair::kStages * Pair::kA;
   unsigned char* Out = Bs + Pair::kStages * Pair::kB;
+  unsigned char* Ones = Out + Pair::kOut;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_rank();
   if (warp == kEpiWarps) {
@@ -551,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
   }
   if (tid == 0) {
     for (int i = 0; i < Pair::kStages; ++i) {
-      mbar_init(&full[i], 1);
+      mbar_init(&full[i], 2);
       mbar_init(&empty[i], 1);
       mbar_init(&tail[i], 1);
     }
@@ -561,8 +591,14 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     }
     fence_barrier_init();
   }
+  if (MODE == kDw && a.db) {
+    const uint32_t one = a.in_type == HA_TYPE_BF16 ? 0x3F803F80u : 0x3C003C00u;
+    for (int i = tid; i < Pair::kOnes / 4; i += kDwThreads) reinterpret_cast<uint32_t*>(Ones)[i] = one;
+    fence_proxy_async();
+  }
   tc_fence_before();
-  make_table<MODE, 2 * kM, kPairCols>(tab, a);
+  make_table<MODE, 2 * kM, kPairCols, MODE == kDw ? kDwThreads : kThreads>(tab, a);
+  Tiles<MODE, 2 * kM, kPairCols, 32> list(tab, a);
   cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = tmem_at;
@@ -576,149 +612,111 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     // ---- loads, by both CTAs
     if (elect_one()) {
       Ring<Pair::kStages> at;
-      bool ok = true;
+      bool ok = true, peek = false;
       const uint32_t full0 = cluster_addr(full, 0);
       for (int i = pair; i < tiles && ok; i += pairs) {
-        const Tile t = tile_at<MODE, 2 * kM, kPairCols, 32>(tab, a, i);
+        const Tile t = list.at(i);
         const int nk = (t.k + kK - 1) / kK, hcols = (t.cols + 31) / 32 * 16;   // columns of a CTA
-        const int m0 = t.m0 + rank * kM, h0 = rank * hcols;
-        const int boxes = (hcols + 63) / 64;
+        const int m0 = t.m0 + rank * kM, h0 = rank * hcols, boxes = t.bias ? 0 : (hcols + 63) / 64;
         const uint32_t bytes = Pair::kA + boxes * 8192;
         for (int c = 0; c < nk; ++c, at.next()) {
-          const int st = at.st;
-          if (!mbar_wait_hot(&empty[st], at.round ^ 1, &g_operator_error)) { ok = false; break; }
-          const bool cut = MODE == kDw && t.k - c * kK < kK;
-          uint32_t bar = full0 + st * 8;
-          if (rank == 0) {
-            mbar_arrive_expect_tx(&full[st], cut ? bytes : 2 * bytes);
-          } else if (cut) {
-            bar = smem_u32(&tail[st]);
-            mbar_arrive_expect_tx(&tail[st], bytes);
-          }
+          const int st = at.st, k = c * kK;
+          if (!peek && !mbar_wait_hot(&empty[st], at.round ^ 1, &g_operator_error)) { ok = false; break; }
+          // A chunk in which the group ends is first seen by the warp that clears what follows.
+          const bool cut = MODE == kDw && t.k - k < kK;
+          const uint32_t bar = cut ? smem_u32(&tail[st]) : full0 + st * 8;
+          uint64_t* arm = cut ? &tail[st] : &full[st];
+          const uint32_t armed = cut ? bytes : rank == 0 ? 2 * bytes : 0;
+          if (!cut && rank == 0) mbar_arrive(&full[st]);
           unsigned char* A = As + st * Pair::kA;
           unsigned char* B = Bs + st * Pair::kB;
-          if (MODE == kFwd) {
-            tma_load_3d_pair(A, &ta, bar, c * kK, m0, t.g);
-          } else if (MODE == kDx) {
-            tma_load_3d_pair(A, &ta, bar, m0, c * kK, t.g);
-            tma_load_3d_pair(A + 8192, &ta, bar, m0 + 64, c * kK, t.g);
-          } else {
-            tma_load_3d_pair(A, &ta, bar, m0, t.r0 + c * kK, 0);
-            tma_load_3d_pair(A + 8192, &ta, bar, m0 + 64, t.r0 + c * kK, 0);
-          }
-          for (int b = 0; b < boxes; ++b) {
-            if (MODE == kDw)
-              tma_load_3d_pair(B + b * 8192, &tb, bar, t.c0 + h0 + b * 64, t.r0 + c * kK, 0);
-            else
-              tma_load_3d_pair(B + b * 8192, &tb, bar, c * kK, t.r0 + h0 + b * 64, 0);
-          }
+          uint64_t* next = &empty[at.next_st()];
+          const uint32_t parity = at.next_round() ^ 1;
+          if (MODE == kFwd)
+            peek = tma_chunk_pair<false, false>(A, &ta, k, m0, t.g, B, &tb, k, t.r0 + h0, boxes, bar, arm, armed, next, parity);
+          else if (MODE == kDx)
+            peek = tma_chunk_pair<true, false>(A, &ta, m0, k, t.g, B, &tb, k, t.r0 + h0, boxes, bar, arm, armed, next, parity);
+          else
+            peek = tma_chunk_pair<true, true>(A, &ta, m0, t.r0 + k, 0, B, &tb, t.c0 + h0, t.r0 + k, boxes, bar, arm, armed,
+                                              next, parity);
         }
       }
     }
   } else if (warp == kEpiWarps + 1) {
-    // ---- matrix products, by the first CTA; the second cuts its own half of a group's end
-    const bool one = elect_one();
-    Ring<Pair::kStages> at;
-    uint32_t seg = 0, tails = 0;                       // tails: parity of each stage's `tail`
-    bool ok = true, peek = false;
-    constexpr int fold = FOLD ? kFold : 1 << 30;
-    for (int i = pair; i < tiles && ok; i += pairs) {
-      const Tile t = tile_at<MODE, 2 * kM, kPairCols, 32>(tab, a, i);
-      const int nk = (t.k + kK - 1) / kK, N = (t.cols + 31) / 32 * 32;
-      const uint32_t idesc = idesc_of(a.in_type, 2 * kM, N) | (MODE == kFwd ? 0u : 1u << 15) |
-                             (MODE == kDw ? 1u << 16 : 0u);
-      // The rows after a group's last are another group's: cleared up to the step's end.
-      auto cut_rows = [&](int st, int left) {
-        unsigned char* A = As + st * Pair::kA;
-        unsigned char* B = Bs + st * Pair::kB;
-        const int blocks = 2 + (N / 2 + 63) / 64, r1 = (left + 15) / 16 * 16, n = r1 - left;
-        for (int x = lane; x < blocks * n * 8; x += 32) {
-          const int line = x >> 3, b = line / n, r = left + line % n;
-          unsigned char* p = (b < 2 ? A + b * 8192 : B + (b - 2) * 8192) + r * 128 + (x & 7) * 16;
-          *reinterpret_cast<uint4*>(p) = make_uint4(0, 0, 0, 0);
-        }
-        fence_proxy_async();
-        __syncwarp();
-      };
-      if (rank != 0) {
-        const int left = t.k % kK;
-        at.skip(nk - (left != 0));
-        if (left && MODE != kDw) at.next();
-        if (MODE == kDw && left) {
-          const int st = at.st;
-          at.next();
-          ok = mbar_wait_hot(&tail[st], tails >> st & 1, &g_operator_error);
-          tails ^= 1u << st;
+    // ---- matrix products, by one lane of the first CTA (a wait of all lanes takes the barrier
+    // unit 32 times as long)
+    if (rank == 0 && elect_one()) {
+      Ring<Pair::kStages> at;
+      uint32_t seg = 0;
+      bool ok = true, peek = false;
+      for (int i = pair; i < tiles && ok; i += pairs) {
+        const Tile t = list.at(i);
+        const int nk = (t.k + kK - 1) / kK, N = (t.cols + 31) / 32 * 32;
+        const int fold = FOLD || t.bias ? kFold : 1 << 30;
+        const uint32_t idesc = idesc_of(a.in_type, 2 * kM, N) | (MODE == kFwd ? 0u : 1u << 15) |
+                               (MODE == kDw ? 1u << 16 : 0u);
+        int part = 0;                                       // chunks since the last fold
+        for (int c = 0; c < nk; ++c, at.next()) {
+          const int st = at.st, buf = seg & 1;
+          const bool cut = MODE == kDw && t.k - c * kK < kK;     // the other CTA has written there
+          ok = (part != 0 || mbar_wait_hot(&tempty[buf], ((seg >> 1) & 1) ^ 1, &g_operator_error)) &&
+               (cut ? mbar_wait_cluster(&full[st], at.round, &g_operator_error)
+                    : peek || mbar_wait_hot(&full[st], at.round, &g_operator_error));
           if (!ok) break;
-          cut_rows(st, left);
-          if (one) mbar_arrive_release_cluster(cluster_addr(&tail[st], 0));
-        }
-        continue;
-      }
-      // One lane waits and issues (a wait of all lanes takes the barrier unit 32 times as
-      // long); the others join it where a group's end has to be cut.
-      const bool cut = MODE == kDw && t.k % kK != 0;
-      auto issue = [&](int c, int steps) {
-        const int st = at.st;
-        const uint32_t as = smem_u32(As + st * Pair::kA), bs = smem_u32(Bs + st * Pair::kB);
-        const uint32_t d = tmem + (seg & 1) * kPairCols;
-        const uint64_t da = MODE == kFwd ? umma_desc_sw128(as) : umma_desc_sw128_mn(as, 8192);
-        const uint64_t db = MODE == kDw ? umma_desc_sw128_mn(bs, 8192) : umma_desc_sw128(bs);
-        constexpr int SA = MODE == kFwd ? 2 : 128, SB = MODE == kDw ? 128 : 2;   // 16 values further
-        if (steps == 4) {
-          peek = tc_chunk_pair<SA, SB>(d, da, db, idesc, c % fold != 0, &empty[st], &full[at.next_st()],
-                                       at.next_round());
-        } else {
-          for (int k = 0; k < steps; ++k) tc_mma_pair(d, da + k * SA, db + k * SB, idesc, (c % fold) || k ? 1u : 0u);
-          tc_commit_pair(&empty[st]);
-          peek = false;
-        }
-        if (c % fold == fold - 1 || c == nk - 1) tc_commit_pair(&tfull[seg & 1]);
-      };
-      auto ready = [&](int c) {
-        if (c % fold == 0 && !mbar_wait_hot(&tempty[seg & 1], ((seg >> 1) & 1) ^ 1, &g_operator_error)) return false;
-        if (!peek && !mbar_wait_hot(&full[at.st], at.round, &g_operator_error)) return false;
-        tc_fence_after();
-        return true;
-      };
-      const int whole = nk - (cut ? 1 : 0);
-      const Ring<Pair::kStages> at0 = at;
-      const uint32_t seg0 = seg;
-      if (one) {
-        for (int c = 0; c < whole; ++c, at.next()) {
-          ok = ready(c);
-          if (!ok) break;
-          issue(c, (min(t.k - c * kK, kK) + 15) / 16);
-          if (c % fold == fold - 1 || c == nk - 1) ++seg;
-        }
-      }
-      ok = __all_sync(~0u, ok);
-      peek = __any_sync(~0u, one && peek);             // of the first CTA's issuing lane
-      at = at0;
-      at.skip(whole);
-      seg = seg0 + (cut ? whole / fold : (nk + fold - 1) / fold);
-      if (cut && ok) {
-        const int st = at.st, left = t.k % kK;
-        ok = ready(whole);
-        if (ok) {
-          cut_rows(st, left);
-          ok = mbar_wait_cluster(&tail[st], tails >> st & 1, &g_operator_error);
-          tails ^= 1u << st;
           tc_fence_after();
-          if (one && ok) issue(whole, (left + 15) / 16);
-          __syncwarp();
+          const int steps = (min(t.k - c * kK, kK) + 15) / 16;
+          const uint32_t as = smem_u32(As + st * Pair::kA), bs = smem_u32(t.bias ? Ones : Bs + st * Pair::kB);
+          const uint32_t d = tmem + buf * kPairCols;
+          const uint64_t da = MODE == kFwd ? umma_desc_sw128(as) : umma_desc_sw128_mn(as, 8192);
+          const uint64_t db = MODE == kDw ? umma_desc_sw128_mn(bs, 8192) : umma_desc_sw128(bs);
+          constexpr int SA = MODE == kFwd ? 2 : 128, SB = MODE == kDw ? 128 : 2;   // 16 values further
+          if (steps == 4) {
+            peek = tc_chunk_pair<SA, SB>(d, da, db, idesc, part != 0, &empty[st], &full[at.next_st()], at.next_round());
+          } else {
+            for (int k = 0; k < steps; ++k) tc_mma_pair(d, da + k * SA, db + k * SB, idesc, part || k ? 1u : 0u);
+            tc_commit_pair(&empty[st]);
+            peek = false;
+          }
+          if (++part == fold || c == nk - 1) {
+            tc_commit_pair(&tfull[buf]);
+            ++seg;
+            part = 0;
+          }
         }
-        at.next();
-        ++seg;
       }
-      ok = __all_sync(~0u, ok);
+    }
+  } else if (MODE == kDw && warp == kEpiWarps + 2) {
+    // ---- the ends of groups, in both CTAs: the rows after a group's last are another group's,
+    // and are cleared up to the products' next step of 16
+    Ring<Pair::kStages> at;
+    uint32_t parity = 0;                                    // of each stage's `tail`
+    for (int i = pair; i < tiles; i += pairs) {
+      const Tile t = list.at(i);
+      const int left = t.k % kK;
+      at.skip(t.k / kK);
+      if (!left) continue;
+      const int st = at.st;
+      at.next();
+      const bool ok = mbar_wait(&tail[st], parity >> st & 1, &g_operator_error);
+      parity ^= 1u << st;
+      if (!__all_sync(~0u, ok)) break;
+      const int blocks = 2 + (t.bias ? 0 : ((t.cols + 31) / 32 * 16 + 63) / 64);
+      const int n = (left + 15) / 16 * 16 - left;
+      for (int x = lane; x < blocks * n * 8; x += 32) {
+        const int line = x >> 3, b = line / n, row = left + line % n;
+        unsigned char* p = (b < 2 ? As + st * Pair::kA + b * 8192 : Bs + st * Pair::kB + (b - 2) * 8192);
+        *reinterpret_cast<uint4*>(p + row * 128 + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_release_cluster(cluster_addr(&full[st], 0));
     }
   } else {
     // ---- results, by both CTAs
     uint32_t seg = 0, turn = 0;
     bool ok = true;
     for (int i = pair; i < tiles && ok; i += pairs) {
-      const Tile t = tile_at<MODE, 2 * kM, kPairCols, 32>(tab, a, i);
+      const Tile t = list.at(i);
       ok = finish_tile<MODE, kPairCols, FOLD>(
           a, &to, t, tmem, t.m0 + rank * kM, Out, seg, turn,
           [&](uint32_t s) {
@@ -736,26 +734,6 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
   __syncthreads();
   cluster_sync_all();
   if (warp == kEpiWarps) tmem_dealloc_pair(tmem, 2 * kPairCols);
-}
-
-// db_g[f] = sum of dy[t][f] over the group's rows: a CTA has 32 features, its warps take
-// the rows in turn and join in a fixed order.
-template <typename T>
-__global__ void __launch_bounds__(512) k_bias_grad(const T* dy, int64_t ld, const int* offsets,
-                                                   int rows, int n, float* db, int64_t db_ld) {
-  __shared__ float part[16][33];
-  const int g = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int f = blockIdx.x * 32 + lane;
-  const int begin = min(max(offsets[g], 0), rows), end = min(max(offsets[g + 1], 0), rows);
-  float s = 0.0f;
-  if (f < n)
-    for (int t = begin + warp; t < end; t += 16) s += Elem<T>::up(dy[t * ld + f]);
-  part[warp][lane] = s;
-  __syncthreads();
-  if (warp == 0 && f < n) {
-    for (int w = 1; w < 16; ++w) s += part[w][lane];
-    db[g * db_ld + f] = s;
-  }
 }
 
 // Rows of 16-bit values to a pitch of whole 16-byte vectors, for operands that a tensor
@@ -836,11 +814,12 @@ int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap&
     return HA_ECUDA;
   // As many pairs as the GPU holds at once (its clusters of two leave some SMs out): the tiles
   // are dealt out in advance, so a pair that started late would finish late.
+  constexpr int threads = MODE == kDw ? kDwThreads : kThreads;
   static int held = 0;
   if (held == 0) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(kSms);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = Pair::kSmem;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -854,7 +833,7 @@ int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap&
     held = n;
   }
   const int64_t pairs = std::min<int64_t>(held, std::max<int64_t>(most, 1));
-  k_grouped_pair<MODE, FOLD><<<static_cast<unsigned>(2 * pairs), kThreads, Pair::kSmem, s>>>(ta, tb, to, a);
+  k_grouped_pair<MODE, FOLD><<<static_cast<unsigned>(2 * pairs), threads, Pair::kSmem, s>>>(ta, tb, to, a);
   return cudaGetLastError() == cudaSuccess ? HA_OK : HA_ECUDA;
 }
 
@@ -993,20 +972,12 @@ extern "C" int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, co
   if (workspace_bytes > 0 && (!workspace_dev || (reinterpret_cast<uintptr_t>(workspace_dev) & 15)))
     return HA_EINVAL;
   unsigned char* p = static_cast<unsigned char*>(workspace_dev);
-  if (db_dev) {
-    const dim3 grid((outer + 31) / 32, groups);
-    if (type == HA_TYPE_BF16)
-      k_bias_grad<__nv_bfloat16><<<grid, 512, 0, s>>>(static_cast<const __nv_bfloat16*>(dy_dev), dy_ld,
-                                                      offsets_dev, static_cast<int>(rows), outer, db_dev, db_ld);
-    else
-      k_bias_grad<__half><<<grid, 512, 0, s>>>(static_cast<const __half*>(dy_dev), dy_ld, offsets_dev,
-                                               static_cast<int>(rows), outer, db_dev, db_ld);
-    if (cudaGetLastError() != cudaSuccess) return HA_ECUDA;
-  }
   if (pack(dy, p, s) != cudaSuccess || pack(x, p, s) != cudaSuccess) return HA_ECUDA;
   Args a = {};
   a.offsets = offsets_dev;
   a.out = dw_dev;
+  a.db = db_dev;
+  a.bias_ld = db_ld;
   a.out_ld = dw_ld;
   a.out_gs = dw_gs;
   a.groups = groups;
@@ -1025,7 +996,7 @@ extern "C" int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, co
       !make_map(&to, {dw_dev, groups, outer, inner, dw_ld, dw_gs}, dw_type, dw_type == HA_TYPE_FP32 ? 32 : 64, 32))
     return HA_ECUDA;
   const int64_t most = groups * static_cast<int64_t>((outer + 2 * kM - 1) / (2 * kM)) *
-                       ((inner + kPairCols - 1) / kPairCols);
+                       ((inner + kPairCols - 1) / kPairCols + (db_dev ? 1 : 0));
   if (most > 0x7FFFFFFF) return HA_EUNSUPPORTED;
   return dw_type == HA_TYPE_FP32 ? launch_pair<kDw, true>(ta, tb, to, a, most, s)
                                  : launch_pair<kDw, false>(ta, tb, to, a, most, s);

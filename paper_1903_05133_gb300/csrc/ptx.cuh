@@ -157,15 +157,6 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity
     __nanosleep(32);
   }
 }
-// A load into this CTA's shared memory that completes on a barrier of either CTA of the pair.
-__device__ __forceinline__ void tma_load_3d_pair(void* smem_dst, const void* tmap, uint32_t bar, int c0,
-                                                 int c1, int c2) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
-      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(smem_dst)),
-      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
-      : "memory");
-}
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t* dst, uint32_t ncols) {
   asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst)),
                "r"(ncols)
@@ -246,6 +237,35 @@ __device__ __forceinline__ bool tc_chunk_pair(uint32_t d, uint64_t a, uint64_t b
       : "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(smem_u32(done)), "r"(smem_u32(next)), "r"(parity),
         "n"(SA), "n"(SB), "h"(static_cast<uint16_t>(3))
       : "memory");
+  return ok != 0;
+}
+
+// One chunk's loads for a pair: A (with TWO its second 8 KB block, 64 further in c0) and `blocks`
+// (0 to 2) blocks of B (the second 64 further in c0 or c1), completing on `bar`, after an arrival
+// on `arm` that expects `bytes` (0: none).  Returns whether the phase of `next` is over, asked first.
+template <bool TWO, bool B_COLS>
+__device__ __forceinline__ bool tma_chunk_pair(void* a, const void* ta, int a0, int a1, int a2, void* b,
+                                               const void* tb, int b0, int b1, int blocks, uint32_t bar,
+                                               uint64_t* arm, uint32_t bytes, uint64_t* next, uint32_t parity) {
+  uint32_t ok;
+#define HA_LOAD "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
+  asm volatile(
+      "{\n\t.reg .pred q, e, x, y, w;\n\t.reg .b32 z;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 q, [%15], %16;\n\t"
+      "setp.ne.b32 e, %14, 0;\n\tsetp.ne.b32 x, %17, 0;\n\tsetp.gt.s32 y, %11, 1;\n\tsetp.gt.s32 w, %11, 0;\n\tmov.b32 z, 0;\n\t"
+      "@e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%13], %14;\n\t" HA_LOAD
+      "[%1], [%2, {%3, %4, %5}], [%12];\n\t@x " HA_LOAD
+      "[%18], [%2, {%19, %4, %5}], [%12];\n\t@w " HA_LOAD
+      "[%6], [%7, {%8, %9, z}], [%12];\n\t@y " HA_LOAD
+      "[%10], [%7, {%20, %21, z}], [%12];\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(a)), "l"(reinterpret_cast<uint64_t>(ta)), "r"(a0), "r"(a1), "r"(a2), "r"(smem_u32(b)),
+        "l"(reinterpret_cast<uint64_t>(tb)), "r"(b0), "r"(b1), "r"(smem_u32(b) + 8192), "r"(blocks),
+        "r"(bar), "r"(smem_u32(arm)), "r"(bytes), "r"(smem_u32(next)), "r"(parity), "n"(TWO ? 1 : 0),
+        "r"(smem_u32(a) + 8192), "r"(a0 + 64), "r"(B_COLS ? b0 + 64 : b0), "r"(B_COLS ? b1 : b1 + 64)
+      : "memory");
+#undef HA_LOAD
   return ok != 0;
 }
 
