@@ -27,7 +27,6 @@ constexpr int kK = 64;                  // values summed over in a chunk: one 12
 constexpr int kMaxGroups = 1024;
 constexpr int kEpiWarps = 8;            // two groups of four: a group reads half the columns
 constexpr int kThreads = (kEpiWarps + 2) * 32;          // results, loads, products
-constexpr int kDwThreads = kThreads + 32;               // and the ends of groups
 constexpr int kPairCols = 256;          // columns of a tile of two CTAs
 constexpr int kFewCols = 32;            // of a tile of one CTA, where groups have few rows
 // fp32 results: the tensor core's running sum is taken into fp32 registers after this many
@@ -90,10 +89,10 @@ struct Table {
 constexpr int kTableBytes = 2 * (kMaxGroups + 1) * 4;
 
 // The list of tiles, by all threads; ends with a CTA barrier.
-template <int MODE, int M, int NT, int THREADS>
+template <int MODE, int M, int NT>
 __device__ __forceinline__ void make_table(const Table& s, const Args& a) {
   const int tid = threadIdx.x, lane = tid & 31;
-  for (int g = tid; g <= a.groups; g += THREADS) s.off[g] = min(max(a.offsets[g], 0), a.rows);
+  for (int g = tid; g <= a.groups; g += kThreads) s.off[g] = min(max(a.offsets[g], 0), a.rows);
   __syncthreads();
   if (tid < 32) {
     const int mt = (a.m + M - 1) / M, nt = (a.n + NT - 1) / NT + (MODE == kDw && a.db ? 1 : 0);
@@ -250,42 +249,41 @@ __device__ __forceinline__ void emit_rows(const Args& a, const float* v, int row
 }
 
 // ---- results of the weights' gradient
-// A warp holds 32 features (rows of dW, one a lane) of 32 columns at a time.  Rows of 128
+// A warp holds 32 features (rows of dW, one a lane) of 32 columns at a time.  Rows of 64
 // bytes are put together in shared memory (16-byte pieces swapped by the row, as the tensor
-// map's 128-byte swizzle expects) and leave as one bulk store, which also cuts off what is
-// outside dW.  Where dW's rows are not aligned for that, lanes store their values.
-constexpr int kWarpStage = 4096;
+// map's 64-byte swizzle expects) and leave as one bulk store, which also cuts off what is
+// outside dW.  Three buffers take turns: with one the stores held up the next tile's (32 groups
+// of 512 rows, 4096 x 4096: 384 us with one of 4 KB).  Where dW's rows are not aligned for
+// that, lanes store their values.
+constexpr int kWarpStage = 3 * 2048;
 __device__ __forceinline__ void emit_weights(const Args& a, const CUtensorMap* to, const float* v, int g,
-                                             int f0, int c, int end, unsigned char* stage) {
+                                             int f0, int c, int end, unsigned char* stage, uint32_t& turn) {
   const int lane = threadIdx.x & 31;
   if (a.wide_out) {
     const bool wide = a.out_type == HA_TYPE_FP32;
-    const int half = wide ? 0 : (c >> 5) & 1;             // which 32 of a 16-bit row's 64 columns
-    if (half == 0) {
-      if (lane == 0) tma_store_wait_read_all();
-      __syncwarp();
-    }
 #pragma unroll
-    for (int p = 0; p < 8; ++p) {
-      if (!wide && p >= 4) break;
-      uint4 w;
-      if (wide)
-        w = make_uint4(__float_as_uint(v[4 * p]), __float_as_uint(v[4 * p + 1]), __float_as_uint(v[4 * p + 2]),
-                       __float_as_uint(v[4 * p + 3]));
-      else
-        w = make_uint4(narrow_pair(v[8 * (p & 3)], v[8 * (p & 3) + 1], a.out_type),
-                       narrow_pair(v[8 * (p & 3) + 2], v[8 * (p & 3) + 3], a.out_type),
-                       narrow_pair(v[8 * (p & 3) + 4], v[8 * (p & 3) + 5], a.out_type),
-                       narrow_pair(v[8 * (p & 3) + 6], v[8 * (p & 3) + 7], a.out_type));
-      *reinterpret_cast<uint4*>(stage + lane * 128 + (((half * 4 + p) ^ (lane & 7)) << 4)) = w;
-    }
-    const int c_box = c - half * 32;
-    if (wide || half == 1 || c + 32 >= end) {
+    for (int h = 0; h < 2; ++h) {                         // fp32: 16 columns a buffer
+      if (h == 1 && !wide) break;
+      unsigned char* buf = stage + turn * 2048;
+      turn = turn == 2 ? 0 : turn + 1;
+      if (lane == 0) tma_store_wait_read_2();
+      __syncwarp();
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        uint4 w;
+        if (wide)
+          w = make_uint4(__float_as_uint(v[16 * h + 4 * p]), __float_as_uint(v[16 * h + 4 * p + 1]),
+                         __float_as_uint(v[16 * h + 4 * p + 2]), __float_as_uint(v[16 * h + 4 * p + 3]));
+        else
+          w = make_uint4(narrow_pair(v[8 * p], v[8 * p + 1], a.out_type), narrow_pair(v[8 * p + 2], v[8 * p + 3], a.out_type),
+                         narrow_pair(v[8 * p + 4], v[8 * p + 5], a.out_type), narrow_pair(v[8 * p + 6], v[8 * p + 7], a.out_type));
+        *reinterpret_cast<uint4*>(buf + lane * 64 + ((p ^ ((lane >> 1) & 3)) << 4)) = w;
+      }
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0 && f0 < a.m) {
-        tma_store_3d(to, stage, c_box, f0, g);
-        tma_store_commit();
+      if (lane == 0) {
+        if (f0 < a.m && c + 16 * h < end) tma_store_3d(to, buf, c + 16 * h, f0, g);
+        tma_store_commit();                               // an empty group too: the count is of buffers
       }
     }
     return;
@@ -325,11 +323,6 @@ struct Ring {
   }
   __device__ __forceinline__ uint32_t next_st() const { return st + 1 == STAGES ? 0 : st + 1; }
   __device__ __forceinline__ uint32_t next_round() const { return st + 1 == STAGES ? round ^ 1 : round; }
-  __device__ __forceinline__ void skip(int n) {
-    const uint32_t at = st + static_cast<uint32_t>(n);
-    st = at % STAGES;
-    round ^= (at / STAGES) & 1;
-  }
 };
 
 // One tile's results: `half` of its NT columns, from the sums in TMEM, segment by segment.
@@ -347,7 +340,7 @@ __device__ __forceinline__ bool finish_tile(const Args& a, const CUtensorMap* to
   constexpr int STEP = H < 32 ? H : 32;
   auto emit = [&](const float* v, int j) {
     if (MODE == kDw)
-      emit_weights(a, to, v, t.g, cta_m0 + quad * 32, t.c0 + cb + j, t.c0 + cb + ce, stage + warp * kWarpStage);
+      emit_weights(a, to, v, t.g, cta_m0 + quad * 32, t.c0 + cb + j, t.c0 + cb + ce, stage + warp * kWarpStage, turn);
     else if (FOLD)
       emit_rows<MODE, float>(a, v, t.c0 + cb + j, min(STEP, ce - j), cta_m0, quad * 32 + lane, bias,
                              stage + half * kRowsStage, 1 + half, turn);
@@ -449,7 +442,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_barrier_init();
   }
   tc_fence_before();
-  make_table<MODE, kM, kFewCols, kThreads>(tab, a);
+  make_table<MODE, kM, kFewCols>(tab, a);
   Tiles<MODE, kM, kFewCols, 16> list(tab, a);
   tc_fence_after();
   const uint32_t tmem = tmem_at;
@@ -552,20 +545,20 @@ __global__ void __launch_bounds__(kThreads, 1)
 // own TMEM, in two buffers, and writes its own results.
 struct Pair {
   static constexpr int kA = kM * kK * 2, kB = kPairCols / 2 * kK * 2, kStages = 5;
-  static constexpr int kOut = 2 * kRowsStage;             // = kEpiWarps * kWarpStage
+  static constexpr int kOut = kEpiWarps * kWarpStage;
   static constexpr int kOnes = 8192;                      // dW: a column block of ones, for the bias
   static constexpr int kSmem = kStages * (kA + kB) + kOut + kOnes + 1024;
 };
-static_assert(2 * kRowsStage == kEpiWarps * kWarpStage, "one buffer serves both kinds of results");
+static_assert(2 * kRowsStage <= kEpiWarps * kWarpStage, "one buffer serves both kinds of results");
 
 template <int MODE, bool FOLD>
-__global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __cluster_dims__(2, 1, 1)
+__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     k_grouped_pair(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
-                   const __grid_constant__ CUtensorMap to, const __grid_constant__ Args a) {
+                   const __grid_constant__ CUtensorMap to, const __grid_constant__ CUtensorMap ta_head,
+                   const __grid_constant__ CUtensorMap tb_head, const __grid_constant__ Args a) {
   extern __shared__ unsigned char raw[];
-  // full: the first CTA's, on which both CTAs' loads and two arrivals are counted.  tempty: the
-  // first CTA's too.  tail: this CTA's load of a chunk in which a group ends.
-  __shared__ uint64_t full[Pair::kStages], empty[Pair::kStages], tfull[2], tempty[2], tail[Pair::kStages];
+  // full: the first CTA's, on which both CTAs' loads are counted.  tempty: the first CTA's too.
+  __shared__ uint64_t full[Pair::kStages], empty[Pair::kStages], tfull[2], tempty[2];
   __shared__ uint32_t tmem_at;
   __shared__ int table[2 * (kMaxGroups + 1)];
   const Table tab = {table, table + kMaxGroups + 1};
@@ -581,9 +574,8 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
   }
   if (tid == 0) {
     for (int i = 0; i < Pair::kStages; ++i) {
-      mbar_init(&full[i], 2);
+      mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
-      mbar_init(&tail[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&tfull[i], 1);
@@ -593,11 +585,11 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
   }
   if (MODE == kDw && a.db) {
     const uint32_t one = a.in_type == HA_TYPE_BF16 ? 0x3F803F80u : 0x3C003C00u;
-    for (int i = tid; i < Pair::kOnes / 4; i += kDwThreads) reinterpret_cast<uint32_t*>(Ones)[i] = one;
+    for (int i = tid; i < Pair::kOnes / 4; i += kThreads) reinterpret_cast<uint32_t*>(Ones)[i] = one;
     fence_proxy_async();
   }
   tc_fence_before();
-  make_table<MODE, 2 * kM, kPairCols, MODE == kDw ? kDwThreads : kThreads>(tab, a);
+  make_table<MODE, 2 * kM, kPairCols>(tab, a);
   Tiles<MODE, 2 * kM, kPairCols, 32> list(tab, a);
   cluster_sync_all();
   tc_fence_after();
@@ -622,23 +614,26 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
         for (int c = 0; c < nk; ++c, at.next()) {
           const int st = at.st, k = c * kK;
           if (!peek && !mbar_wait_hot(&empty[st], at.round ^ 1, &g_operator_error)) { ok = false; break; }
-          // A chunk in which the group ends is first seen by the warp that clears what follows.
-          const bool cut = MODE == kDw && t.k - k < kK;
-          const uint32_t bar = cut ? smem_u32(&tail[st]) : full0 + st * 8;
-          uint64_t* arm = cut ? &tail[st] : &full[st];
-          const uint32_t armed = cut ? bytes : rank == 0 ? 2 * bytes : 0;
-          if (!cut && rank == 0) mbar_arrive(&full[st]);
+          const uint32_t bar = full0 + st * 8, armed = rank == 0 ? 2 * bytes : 0;
           unsigned char* A = As + st * Pair::kA;
           unsigned char* B = Bs + st * Pair::kB;
           uint64_t* next = &empty[at.next_st()];
           const uint32_t parity = at.next_round() ^ 1;
-          if (MODE == kFwd)
-            peek = tma_chunk_pair<false, false>(A, &ta, k, m0, t.g, B, &tb, k, t.r0 + h0, boxes, bar, arm, armed, next, parity);
-          else if (MODE == kDx)
-            peek = tma_chunk_pair<true, false>(A, &ta, m0, k, t.g, B, &tb, k, t.r0 + h0, boxes, bar, arm, armed, next, parity);
-          else
-            peek = tma_chunk_pair<true, true>(A, &ta, m0, t.r0 + k, 0, B, &tb, t.c0 + h0, t.r0 + k, boxes, bar, arm, armed,
-                                              next, parity);
+          if (MODE == kFwd) {
+            peek = tma_chunk_pair<false, false>(A, &ta, k, m0, t.g, B, &tb, k, t.r0 + h0, 0, boxes, bar, &full[st], armed,
+                                                next, parity);
+          } else if (MODE == kDx) {
+            peek = tma_chunk_pair<true, false>(A, &ta, m0, k, t.g, B, &tb, k, t.r0 + h0, 0, boxes, bar, &full[st], armed,
+                                               next, parity);
+          } else {
+            // A group's rows that fill no chunk come first, as the first ones of a window that
+            // starts with the group, loaded from a row before it on: zeros, then the rows.
+            const int odd = t.k % kK, row = odd ? t.r0 + odd - kK + k : t.r0 + k;
+            const bool first = c == 0 && odd != 0;
+            peek = tma_chunk_pair<true, true>(A, first ? &ta_head : &ta, m0, first ? odd - kK : row, first ? t.r0 : 0, B,
+                                              first ? &tb_head : &tb, t.c0 + h0, first ? odd - kK : row, first ? t.r0 : 0,
+                                              boxes, bar, &full[st], armed, next, parity);
+          }
         }
       }
     }
@@ -658,18 +653,18 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
         int part = 0;                                       // chunks since the last fold
         for (int c = 0; c < nk; ++c, at.next()) {
           const int st = at.st, buf = seg & 1;
-          const bool cut = MODE == kDw && t.k - c * kK < kK;     // the other CTA has written there
           ok = (part != 0 || mbar_wait_hot(&tempty[buf], ((seg >> 1) & 1) ^ 1, &g_operator_error)) &&
-               (cut ? mbar_wait_cluster(&full[st], at.round, &g_operator_error)
-                    : peek || mbar_wait_hot(&full[st], at.round, &g_operator_error));
+               (peek || mbar_wait_hot(&full[st], at.round, &g_operator_error));
           if (!ok) break;
           tc_fence_after();
-          const int steps = (min(t.k - c * kK, kK) + 15) / 16;
+          // the values of an incomplete chunk: the last ones (dW) or the first
+          const int odd = t.k % kK;
+          const int steps = odd && c == (MODE == kDw ? 0 : nk - 1) ? (odd + 15) / 16 : 4, skip = MODE == kDw ? 4 - steps : 0;
           const uint32_t as = smem_u32(As + st * Pair::kA), bs = smem_u32(t.bias ? Ones : Bs + st * Pair::kB);
           const uint32_t d = tmem + buf * kPairCols;
-          const uint64_t da = MODE == kFwd ? umma_desc_sw128(as) : umma_desc_sw128_mn(as, 8192);
-          const uint64_t db = MODE == kDw ? umma_desc_sw128_mn(bs, 8192) : umma_desc_sw128(bs);
           constexpr int SA = MODE == kFwd ? 2 : 128, SB = MODE == kDw ? 128 : 2;   // 16 values further
+          const uint64_t da = (MODE == kFwd ? umma_desc_sw128(as) : umma_desc_sw128_mn(as, 8192)) + skip * SA;
+          const uint64_t db = (MODE == kDw ? umma_desc_sw128_mn(bs, 8192) : umma_desc_sw128(bs)) + skip * SB;
           if (steps == 4) {
             peek = tc_chunk_pair<SA, SB>(d, da, db, idesc, part != 0, &empty[st], &full[at.next_st()], at.next_round());
           } else {
@@ -684,32 +679,6 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
           }
         }
       }
-    }
-  } else if (MODE == kDw && warp == kEpiWarps + 2) {
-    // ---- the ends of groups, in both CTAs: the rows after a group's last are another group's,
-    // and are cleared up to the products' next step of 16
-    Ring<Pair::kStages> at;
-    uint32_t parity = 0;                                    // of each stage's `tail`
-    for (int i = pair; i < tiles; i += pairs) {
-      const Tile t = list.at(i);
-      const int left = t.k % kK;
-      at.skip(t.k / kK);
-      if (!left) continue;
-      const int st = at.st;
-      at.next();
-      const bool ok = mbar_wait(&tail[st], parity >> st & 1, &g_operator_error);
-      parity ^= 1u << st;
-      if (!__all_sync(~0u, ok)) break;
-      const int blocks = 2 + (t.bias ? 0 : ((t.cols + 31) / 32 * 16 + 63) / 64);
-      const int n = (left + 15) / 16 * 16 - left;
-      for (int x = lane; x < blocks * n * 8; x += 32) {
-        const int line = x >> 3, b = line / n, row = left + line % n;
-        unsigned char* p = (b < 2 ? As + st * Pair::kA + b * 8192 : Bs + st * Pair::kB + (b - 2) * 8192);
-        *reinterpret_cast<uint4*>(p + row * 128 + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
-      }
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_release_cluster(cluster_addr(&full[st], 0));
     }
   } else {
     // ---- results, by both CTAs
@@ -779,7 +748,7 @@ cudaError_t pack(Operand& o, unsigned char*& ws, cudaStream_t s) {
 }
 
 // Three dimensions always; box {b0, b1, 1}.
-bool make_map(CUtensorMap* m, const Operand& o, int type, uint32_t b0, uint32_t b1) {
+bool make_map(CUtensorMap* m, const Operand& o, int type, uint32_t b0, uint32_t b1, bool half_swizzle = false) {
   const EncodeTiledFn enc = encode_fn();
   if (!enc) return false;
   const int es = type_size(type);
@@ -792,7 +761,7 @@ bool make_map(CUtensorMap* m, const Operand& o, int type, uint32_t b0, uint32_t 
                                  : type == HA_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                                         : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
   return enc(m, dt, 3, const_cast<void*>(o.p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             half_swizzle ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -807,19 +776,18 @@ int launch_few(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int6
 }
 
 template <int MODE, bool FOLD>
-int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to, const Args& a, int64_t most,
-                cudaStream_t s) {
+int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to, const CUtensorMap& ta_head,
+                const CUtensorMap& tb_head, const Args& a, int64_t most, cudaStream_t s) {
   if (cudaFuncSetAttribute(k_grouped_pair<MODE, FOLD>, cudaFuncAttributeMaxDynamicSharedMemorySize, Pair::kSmem) !=
       cudaSuccess)
     return HA_ECUDA;
   // As many pairs as the GPU holds at once (its clusters of two leave some SMs out): the tiles
   // are dealt out in advance, so a pair that started late would finish late.
-  constexpr int threads = MODE == kDw ? kDwThreads : kThreads;
   static int held = 0;
   if (held == 0) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(kSms);
-    cfg.blockDim = dim3(threads);
+    cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = Pair::kSmem;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -833,7 +801,7 @@ int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap&
     held = n;
   }
   const int64_t pairs = std::min<int64_t>(held, std::max<int64_t>(most, 1));
-  k_grouped_pair<MODE, FOLD><<<static_cast<unsigned>(2 * pairs), threads, Pair::kSmem, s>>>(ta, tb, to, a);
+  k_grouped_pair<MODE, FOLD><<<static_cast<unsigned>(2 * pairs), kThreads, Pair::kSmem, s>>>(ta, tb, to, ta_head, tb_head, a);
   return cudaGetLastError() == cudaSuccess ? HA_OK : HA_ECUDA;
 }
 
@@ -864,7 +832,8 @@ int rows_product(Operand x, Operand w, Args a, void* ws, int64_t ws_bytes, cudaS
     return fold ? launch_few<MODE, true>(ta, tb, a, most, s) : launch_few<MODE, false>(ta, tb, a, most, s);
   }
   const int64_t most = (a.m + 2 * kM - 1) / (2 * kM) * std::min<int64_t>(a.rows, a.groups + a.rows / kPairCols);
-  return fold ? launch_pair<MODE, true>(ta, tb, ta, a, most, s) : launch_pair<MODE, false>(ta, tb, ta, a, most, s);
+  return fold ? launch_pair<MODE, true>(ta, tb, ta, ta, ta, a, most, s)
+              : launch_pair<MODE, false>(ta, tb, ta, ta, ta, a, most, s);
 }
 
 }  // namespace
@@ -989,17 +958,22 @@ extern "C" int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, co
   const int es = type_size(dw_type);
   a.wide_out = (reinterpret_cast<uintptr_t>(dw_dev) & 15) == 0 && dw_ld * es % 16 == 0 && inner * es % 16 == 0 &&
                (groups == 1 || dw_gs * es % 16 == 0);
-  CUtensorMap ta, tb, to;
-  if (!make_map(&ta, dy, type, 64, 64) || !make_map(&tb, x, type, 64, 64)) return HA_ECUDA;
+  // Windows of 64 rows, one for each row that may begin a group.  (The last ones reach past the
+  // tensor; only rows of a group are asked for.)
+  auto windows = [](const Operand& o) { return Operand{o.p, o.rows, kK, o.cols, o.ld, o.ld}; };
+  CUtensorMap ta, tb, to, ta_head, tb_head;
+  if (!make_map(&ta, dy, type, 64, 64) || !make_map(&tb, x, type, 64, 64) ||
+      !make_map(&ta_head, windows(dy), type, 64, 64) || !make_map(&tb_head, windows(x), type, 64, 64))
+    return HA_ECUDA;
   to = ta;
-  if (a.wide_out &&
-      !make_map(&to, {dw_dev, groups, outer, inner, dw_ld, dw_gs}, dw_type, dw_type == HA_TYPE_FP32 ? 32 : 64, 32))
+  if (a.wide_out && !make_map(&to, {dw_dev, groups, outer, inner, dw_ld, dw_gs}, dw_type,
+                              dw_type == HA_TYPE_FP32 ? 16 : 32, 32, true))
     return HA_ECUDA;
   const int64_t most = groups * static_cast<int64_t>((outer + 2 * kM - 1) / (2 * kM)) *
                        ((inner + kPairCols - 1) / kPairCols + (db_dev ? 1 : 0));
   if (most > 0x7FFFFFFF) return HA_EUNSUPPORTED;
-  return dw_type == HA_TYPE_FP32 ? launch_pair<kDw, true>(ta, tb, to, a, most, s)
-                                 : launch_pair<kDw, false>(ta, tb, to, a, most, s);
+  return dw_type == HA_TYPE_FP32 ? launch_pair<kDw, true>(ta, tb, to, ta_head, tb_head, a, most, s)
+                                 : launch_pair<kDw, false>(ta, tb, to, ta_head, tb_head, a, most, s);
 }
 
 extern "C" int hier_avg_operator_check(void* stream) {

@@ -127,35 +127,10 @@ __device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank) {
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ra) : "r"(smem_u32(p)), "r"(rank));
   return ra;
 }
-// Arrive on a barrier of the cluster; _release: with this thread's writes before it visible
-// to the cluster (that takes a fence, which waits for the thread's stores).
+// Arrive on a barrier of the cluster.  (With .release.cluster it would be a fence that waits for
+// the thread's loads and stores in flight: nothing that these arrivals order passes through them.)
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t addr) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
-}
-// mbar_wait, acquiring what other CTAs of the cluster released.
-__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, int* err,
-                                                  long long limit = kWaitLimitCycles) {
-  long long t0 = 0;
-  while (true) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    if (ok) return true;
-    if (t0 == 0) t0 = clock64();
-    if (clock64() - t0 > limit) {
-      if (err) atomicOr(err, HA_DEVERR_TIMEOUT);
-      return false;
-    }
-    __nanosleep(32);
-  }
 }
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t* dst, uint32_t ncols) {
   asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst)),
@@ -245,25 +220,25 @@ __device__ __forceinline__ bool tc_chunk_pair(uint32_t d, uint64_t a, uint64_t b
 // on `arm` that expects `bytes` (0: none).  Returns whether the phase of `next` is over, asked first.
 template <bool TWO, bool B_COLS>
 __device__ __forceinline__ bool tma_chunk_pair(void* a, const void* ta, int a0, int a1, int a2, void* b,
-                                               const void* tb, int b0, int b1, int blocks, uint32_t bar,
+                                               const void* tb, int b0, int b1, int b2, int blocks, uint32_t bar,
                                                uint64_t* arm, uint32_t bytes, uint64_t* next, uint32_t parity) {
   uint32_t ok;
 #define HA_LOAD "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
   asm volatile(
-      "{\n\t.reg .pred q, e, x, y, w;\n\t.reg .b32 z;\n\t"
+      "{\n\t.reg .pred q, e, x, y, w;\n\t"
       "mbarrier.test_wait.parity.shared::cta.b64 q, [%15], %16;\n\t"
-      "setp.ne.b32 e, %14, 0;\n\tsetp.ne.b32 x, %17, 0;\n\tsetp.gt.s32 y, %11, 1;\n\tsetp.gt.s32 w, %11, 0;\n\tmov.b32 z, 0;\n\t"
+      "setp.ne.b32 e, %14, 0;\n\tsetp.ne.b32 x, %17, 0;\n\tsetp.gt.s32 y, %11, 1;\n\tsetp.gt.s32 w, %11, 0;\n\t"
       "@e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%13], %14;\n\t" HA_LOAD
       "[%1], [%2, {%3, %4, %5}], [%12];\n\t@x " HA_LOAD
       "[%18], [%2, {%19, %4, %5}], [%12];\n\t@w " HA_LOAD
-      "[%6], [%7, {%8, %9, z}], [%12];\n\t@y " HA_LOAD
-      "[%10], [%7, {%20, %21, z}], [%12];\n\t"
+      "[%6], [%7, {%8, %9, %22}], [%12];\n\t@y " HA_LOAD
+      "[%10], [%7, {%20, %21, %22}], [%12];\n\t"
       "selp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(ok)
       : "r"(smem_u32(a)), "l"(reinterpret_cast<uint64_t>(ta)), "r"(a0), "r"(a1), "r"(a2), "r"(smem_u32(b)),
         "l"(reinterpret_cast<uint64_t>(tb)), "r"(b0), "r"(b1), "r"(smem_u32(b) + 8192), "r"(blocks),
         "r"(bar), "r"(smem_u32(arm)), "r"(bytes), "r"(smem_u32(next)), "r"(parity), "n"(TWO ? 1 : 0),
-        "r"(smem_u32(a) + 8192), "r"(a0 + 64), "r"(B_COLS ? b0 + 64 : b0), "r"(B_COLS ? b1 : b1 + 64)
+        "r"(smem_u32(a) + 8192), "r"(a0 + 64), "r"(B_COLS ? b0 + 64 : b0), "r"(B_COLS ? b1 : b1 + 64), "r"(b2)
       : "memory");
 #undef HA_LOAD
   return ok != 0;
@@ -396,6 +371,9 @@ __device__ __forceinline__ void tma_store_wait_read_all() {
 // All but the most recent bulk group have finished reading their shared memory.
 __device__ __forceinline__ void tma_store_wait_read_1() {
   asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+}
+__device__ __forceinline__ void tma_store_wait_read_2() {
+  asm volatile("cp.async.bulk.wait_group.read 2;" ::: "memory");
 }
 __device__ __forceinline__ void tma_store_wait_all() {
   asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
