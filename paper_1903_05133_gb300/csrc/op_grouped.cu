@@ -133,8 +133,11 @@ struct Tiles {
     const int x = i - s.first[g];
     Tile t;
     t.g = g;
-    const int ct = x / mt, low = s.off[g], n = max(0, s.off[g + 1] - low);
-    t.m0 = (x - ct * mt) * M;
+    // dW: the columns of a strip of rows one after the other, so that whole rows are written at
+    // about the same time; else the features first, which share the rows they read.
+    const int per = MODE == kDw ? s.first[1] / mt : mt, q = x / per, rest = x - q * per;
+    const int ct = MODE == kDw ? rest : q, low = s.off[g], n = max(0, s.off[g + 1] - low);
+    t.m0 = (MODE == kDw ? q : rest) * M;
     t.bias = false;
     if (MODE == kDw) {
       t.c0 = ct * NT;
@@ -249,43 +252,47 @@ __device__ __forceinline__ void emit_rows(const Args& a, const float* v, int row
 }
 
 // ---- results of the weights' gradient
-// A warp holds 32 features (rows of dW, one a lane) of 32 columns at a time.  Rows of 64
-// bytes are put together in shared memory (16-byte pieces swapped by the row, as the tensor
-// map's 64-byte swizzle expects) and leave as one bulk store, which also cuts off what is
-// outside dW.  Three buffers take turns: with one the stores held up the next tile's (32 groups
-// of 512 rows, 4096 x 4096: 384 us with one of 4 KB).  Where dW's rows are not aligned for
-// that, lanes store their values.
-constexpr int kWarpStage = 3 * 2048;
-__device__ __forceinline__ void emit_weights(const Args& a, const CUtensorMap* to, const float* v, int g,
-                                             int f0, int c, int end, unsigned char* stage, uint32_t& turn) {
+// A warp holds 32 features (rows of dW, one a lane) of 32 columns at a time.  Rows of 128
+// bytes are put together in shared memory (16-byte pieces swapped by the row, against bank
+// conflicts), and eight lanes store a row.  (32 groups of 512 rows, 4096 x 4096, 16 bits: lanes
+// storing their own rows 500 us, bulk stores of boxes with 64-byte rows 409 us.)  Where dW's rows
+// are not aligned for that, lanes store their values.
+constexpr int kWarpStage = 4096;
+__device__ __forceinline__ void emit_weights(const Args& a, const float* v, int g, int f0, int c, int end,
+                                             unsigned char* stage) {
   const int lane = threadIdx.x & 31;
   if (a.wide_out) {
     const bool wide = a.out_type == HA_TYPE_FP32;
+    const int half = wide ? 0 : (c >> 5) & 1;             // which 32 of a 16-bit row's 64 columns
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {                         // fp32: 16 columns a buffer
-      if (h == 1 && !wide) break;
-      unsigned char* buf = stage + turn * 2048;
-      turn = turn == 2 ? 0 : turn + 1;
-      if (lane == 0) tma_store_wait_read_2();
-      __syncwarp();
+    for (int p = 0; p < 8; ++p) {
+      if (!wide && p >= 4) break;
+      uint4 w;
+      if (wide)
+        w = make_uint4(__float_as_uint(v[4 * p]), __float_as_uint(v[4 * p + 1]), __float_as_uint(v[4 * p + 2]),
+                       __float_as_uint(v[4 * p + 3]));
+      else
+        w = make_uint4(narrow_pair(v[8 * (p & 3)], v[8 * (p & 3) + 1], a.out_type),
+                       narrow_pair(v[8 * (p & 3) + 2], v[8 * (p & 3) + 3], a.out_type),
+                       narrow_pair(v[8 * (p & 3) + 4], v[8 * (p & 3) + 5], a.out_type),
+                       narrow_pair(v[8 * (p & 3) + 6], v[8 * (p & 3) + 7], a.out_type));
+      *reinterpret_cast<uint4*>(stage + lane * 128 + (((half * 4 + p) ^ (lane & 7)) << 4)) = w;
+    }
+    if (!wide && half == 0 && c + 32 < end) return;       // the row's other half comes next
+    __syncwarp();
+    const int es = wide ? 4 : 2, piece = lane & 7, col = c - half * 32 + piece * (16 / es);
+    if (col < end) {
+      unsigned char* o = static_cast<unsigned char*>(a.out) +
+                         (g * a.out_gs + static_cast<int64_t>(f0 + (lane >> 3)) * a.out_ld + col) * es;
 #pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        uint4 w;
-        if (wide)
-          w = make_uint4(__float_as_uint(v[16 * h + 4 * p]), __float_as_uint(v[16 * h + 4 * p + 1]),
-                         __float_as_uint(v[16 * h + 4 * p + 2]), __float_as_uint(v[16 * h + 4 * p + 3]));
-        else
-          w = make_uint4(narrow_pair(v[8 * p], v[8 * p + 1], a.out_type), narrow_pair(v[8 * p + 2], v[8 * p + 3], a.out_type),
-                         narrow_pair(v[8 * p + 4], v[8 * p + 5], a.out_type), narrow_pair(v[8 * p + 6], v[8 * p + 7], a.out_type));
-        *reinterpret_cast<uint4*>(buf + lane * 64 + ((p ^ ((lane >> 1) & 3)) << 4)) = w;
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        if (f0 < a.m && c + 16 * h < end) tma_store_3d(to, buf, c + 16 * h, f0, g);
-        tma_store_commit();                               // an empty group too: the count is of buffers
+      for (int i = 0; i < 8; ++i) {
+        const int row = i * 4 + (lane >> 3);
+        if (f0 + row < a.m)
+          *reinterpret_cast<uint4*>(o + i * 4 * a.out_ld * es) =
+              *reinterpret_cast<const uint4*>(stage + row * 128 + ((piece ^ (row & 7)) << 4));
       }
     }
+    __syncwarp();
     return;
   }
   const int f = f0 + lane;
@@ -327,7 +334,7 @@ struct Ring {
 
 // One tile's results: `half` of its NT columns, from the sums in TMEM, segment by segment.
 template <int MODE, int NT, bool FOLD, typename Wait, typename Free>
-__device__ __forceinline__ bool finish_tile(const Args& a, const CUtensorMap* to, const Tile& t, uint32_t tmem,
+__device__ __forceinline__ bool finish_tile(const Args& a, const Tile& t, uint32_t tmem,
                                             int cta_m0, unsigned char* stage, uint32_t& seg, uint32_t& turn,
                                             Wait wait, Free release) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2, quad = warp & 3;
@@ -340,7 +347,7 @@ __device__ __forceinline__ bool finish_tile(const Args& a, const CUtensorMap* to
   constexpr int STEP = H < 32 ? H : 32;
   auto emit = [&](const float* v, int j) {
     if (MODE == kDw)
-      emit_weights(a, to, v, t.g, cta_m0 + quad * 32, t.c0 + cb + j, t.c0 + cb + ce, stage + warp * kWarpStage, turn);
+      emit_weights(a, v, t.g, cta_m0 + quad * 32, t.c0 + cb + j, t.c0 + cb + ce, stage + warp * kWarpStage);
     else if (FOLD)
       emit_rows<MODE, float>(a, v, t.c0 + cb + j, min(STEP, ce - j), cta_m0, quad * 32 + lane, bias,
                              stage + half * kRowsStage, 1 + half, turn);
@@ -372,6 +379,23 @@ __device__ __forceinline__ bool finish_tile(const Args& a, const CUtensorMap* to
   }
   if (!FOLD) {
     if (segs && !wait(seg)) return false;
+    if (MODE == kDw && segs) {
+      // all of a half's reads are under way before the first is used
+#pragma unroll
+      for (int j0 = 0; j0 < H; j0 += 64) {
+        if (j0 >= ce) break;
+        float v[64];
+        const uint32_t at = tmem + (static_cast<uint32_t>(quad * 32) << 16) + (seg & 1) * NT + cb + j0;
+        tmem_ld32(at, v);
+        tmem_ld32(at + 32, v + 32);
+        tmem_ld_wait();
+        if (j0 + 64 >= min(H, ce)) release(seg++);
+        emit(v, j0);
+        if (j0 + 32 < ce) emit(v + 32, j0 + 32);
+      }
+      if (ce <= 0) release(seg++);
+      return true;
+    }
 #pragma unroll 1
     for (int j = 0; j < H; j += STEP) {
       if (j >= ce) break;
@@ -521,7 +545,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
       const Tile t = list.at(i);
       ok = finish_tile<MODE, kFewCols, FOLD>(
-          a, nullptr, t, tmem, t.m0, Out, seg, turn,
+          a, t, tmem, t.m0, Out, seg, turn,
           [&](uint32_t s) {
             return warp_wait(&tfull[s & 1], (s >> 1) & 1);
           },
@@ -545,17 +569,17 @@ __global__ void __launch_bounds__(kThreads, 1)
 // own TMEM, in two buffers, and writes its own results.
 struct Pair {
   static constexpr int kA = kM * kK * 2, kB = kPairCols / 2 * kK * 2, kStages = 5;
-  static constexpr int kOut = kEpiWarps * kWarpStage;
+  static constexpr int kOut = 2 * kRowsStage;             // = kEpiWarps * kWarpStage
   static constexpr int kOnes = 8192;                      // dW: a column block of ones, for the bias
   static constexpr int kSmem = kStages * (kA + kB) + kOut + kOnes + 1024;
 };
-static_assert(2 * kRowsStage <= kEpiWarps * kWarpStage, "one buffer serves both kinds of results");
+static_assert(2 * kRowsStage == kEpiWarps * kWarpStage, "one buffer serves both kinds of results");
 
 template <int MODE, bool FOLD>
 __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     k_grouped_pair(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
-                   const __grid_constant__ CUtensorMap to, const __grid_constant__ CUtensorMap ta_head,
-                   const __grid_constant__ CUtensorMap tb_head, const __grid_constant__ Args a) {
+                   const __grid_constant__ CUtensorMap ta_head, const __grid_constant__ CUtensorMap tb_head,
+                   const __grid_constant__ Args a) {
   extern __shared__ unsigned char raw[];
   // full: the first CTA's, on which both CTAs' loads are counted.  tempty: the first CTA's too.
   __shared__ uint64_t full[Pair::kStages], empty[Pair::kStages], tfull[2], tempty[2];
@@ -687,7 +711,7 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
     for (int i = pair; i < tiles && ok; i += pairs) {
       const Tile t = list.at(i);
       ok = finish_tile<MODE, kPairCols, FOLD>(
-          a, &to, t, tmem, t.m0 + rank * kM, Out, seg, turn,
+          a, t, tmem, t.m0 + rank * kM, Out, seg, turn,
           [&](uint32_t s) {
             return warp_wait(&tfull[s & 1], (s >> 1) & 1);
           },
@@ -697,7 +721,6 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
             if (lane == 0) mbar_arrive_cluster(cluster_addr(&tempty[s & 1], 0));
           });
     }
-    if (MODE == kDw && lane == 0) tma_store_wait_all();
   }
   tc_fence_before();
   __syncthreads();
@@ -748,7 +771,7 @@ cudaError_t pack(Operand& o, unsigned char*& ws, cudaStream_t s) {
 }
 
 // Three dimensions always; box {b0, b1, 1}.
-bool make_map(CUtensorMap* m, const Operand& o, int type, uint32_t b0, uint32_t b1, bool half_swizzle = false) {
+bool make_map(CUtensorMap* m, const Operand& o, int type, uint32_t b0, uint32_t b1) {
   const EncodeTiledFn enc = encode_fn();
   if (!enc) return false;
   const int es = type_size(type);
@@ -761,7 +784,7 @@ bool make_map(CUtensorMap* m, const Operand& o, int type, uint32_t b0, uint32_t 
                                  : type == HA_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                                         : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
   return enc(m, dt, 3, const_cast<void*>(o.p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             half_swizzle ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -776,8 +799,8 @@ int launch_few(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int6
 }
 
 template <int MODE, bool FOLD>
-int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to, const CUtensorMap& ta_head,
-                const CUtensorMap& tb_head, const Args& a, int64_t most, cudaStream_t s) {
+int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& ta_head, const CUtensorMap& tb_head,
+                const Args& a, int64_t most, cudaStream_t s) {
   if (cudaFuncSetAttribute(k_grouped_pair<MODE, FOLD>, cudaFuncAttributeMaxDynamicSharedMemorySize, Pair::kSmem) !=
       cudaSuccess)
     return HA_ECUDA;
@@ -801,7 +824,7 @@ int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap&
     held = n;
   }
   const int64_t pairs = std::min<int64_t>(held, std::max<int64_t>(most, 1));
-  k_grouped_pair<MODE, FOLD><<<static_cast<unsigned>(2 * pairs), kThreads, Pair::kSmem, s>>>(ta, tb, to, ta_head, tb_head, a);
+  k_grouped_pair<MODE, FOLD><<<static_cast<unsigned>(2 * pairs), kThreads, Pair::kSmem, s>>>(ta, tb, ta_head, tb_head, a);
   return cudaGetLastError() == cudaSuccess ? HA_OK : HA_ECUDA;
 }
 
@@ -832,8 +855,8 @@ int rows_product(Operand x, Operand w, Args a, void* ws, int64_t ws_bytes, cudaS
     return fold ? launch_few<MODE, true>(ta, tb, a, most, s) : launch_few<MODE, false>(ta, tb, a, most, s);
   }
   const int64_t most = (a.m + 2 * kM - 1) / (2 * kM) * std::min<int64_t>(a.rows, a.groups + a.rows / kPairCols);
-  return fold ? launch_pair<MODE, true>(ta, tb, ta, ta, ta, a, most, s)
-              : launch_pair<MODE, false>(ta, tb, ta, ta, ta, a, most, s);
+  return fold ? launch_pair<MODE, true>(ta, tb, ta, tb, a, most, s)
+              : launch_pair<MODE, false>(ta, tb, ta, tb, a, most, s);
 }
 
 }  // namespace
@@ -961,19 +984,15 @@ extern "C" int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, co
   // Windows of 64 rows, one for each row that may begin a group.  (The last ones reach past the
   // tensor; only rows of a group are asked for.)
   auto windows = [](const Operand& o) { return Operand{o.p, o.rows, kK, o.cols, o.ld, o.ld}; };
-  CUtensorMap ta, tb, to, ta_head, tb_head;
+  CUtensorMap ta, tb, ta_head, tb_head;
   if (!make_map(&ta, dy, type, 64, 64) || !make_map(&tb, x, type, 64, 64) ||
       !make_map(&ta_head, windows(dy), type, 64, 64) || !make_map(&tb_head, windows(x), type, 64, 64))
-    return HA_ECUDA;
-  to = ta;
-  if (a.wide_out && !make_map(&to, {dw_dev, groups, outer, inner, dw_ld, dw_gs}, dw_type,
-                              dw_type == HA_TYPE_FP32 ? 16 : 32, 32, true))
     return HA_ECUDA;
   const int64_t most = groups * static_cast<int64_t>((outer + 2 * kM - 1) / (2 * kM)) *
                        ((inner + kPairCols - 1) / kPairCols + (db_dev ? 1 : 0));
   if (most > 0x7FFFFFFF) return HA_EUNSUPPORTED;
-  return dw_type == HA_TYPE_FP32 ? launch_pair<kDw, true>(ta, tb, to, ta_head, tb_head, a, most, s)
-                                 : launch_pair<kDw, false>(ta, tb, to, ta_head, tb_head, a, most, s);
+  return dw_type == HA_TYPE_FP32 ? launch_pair<kDw, true>(ta, tb, ta_head, tb_head, a, most, s)
+                                 : launch_pair<kDw, false>(ta, tb, ta_head, tb_head, a, most, s);
 }
 
 extern "C" int hier_avg_operator_check(void* stream) {

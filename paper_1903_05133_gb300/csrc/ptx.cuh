@@ -372,9 +372,6 @@ __device__ __forceinline__ void tma_store_wait_read_all() {
 __device__ __forceinline__ void tma_store_wait_read_1() {
   asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
 }
-__device__ __forceinline__ void tma_store_wait_read_2() {
-  asm volatile("cp.async.bulk.wait_group.read 2;" ::: "memory");
-}
 __device__ __forceinline__ void tma_store_wait_all() {
   asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
