@@ -26,6 +26,7 @@ namespace {
 constexpr int kBlock = 256;         // elements that share a scale: one warp, 8 a lane
 constexpr int kChunk = 2048;        // elements of one CTA: a block for each warp
 constexpr int kThreads = 256;
+constexpr int kSms = 152;
 constexpr float kTop = 448.0f;      // largest e4m3 value
 constexpr float kTiny = 1e-30f;     // a block whose largest magnitude is below is stored as 0
 
@@ -117,12 +118,12 @@ template <typename G>
 __device__ __forceinline__ void load_grad4(const G* g, float* x);
 template <>
 __device__ __forceinline__ void load_grad4<float>(const float* g, float* x) {
-  const float4 f = __ldcs(reinterpret_cast<const float4*>(g));
+  const float4 f = *reinterpret_cast<const float4*>(g);
   x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
 }
 template <typename G>
 __device__ __forceinline__ void load_grad4(const G* g, float* x) {
-  const uint2 w = __ldcs(reinterpret_cast<const uint2*>(g));
+  const uint2 w = *reinterpret_cast<const uint2*>(g);
   widen2<G>(w.x, x[0], x[1]);
   widen2<G>(w.y, x[2], x[3]);
 }
@@ -133,58 +134,50 @@ __device__ __forceinline__ float warp_abs_max(float a) {
   return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(a) & 0x7FFFFFFFu));
 }
 
-// One CTA a chunk, one warp a block of 256 elements, each lane two groups of four
-// consecutive elements, so that every load and store of a warp is contiguous.
-template <int BITS, typename G, int NG>
-__global__ void __launch_bounds__(kThreads, 5) k_adamw(const __grid_constant__ Grads<NG> grads,
-                                                    const __grid_constant__ StepArgs a) {
-  const Chunk c = a.chunks[blockIdx.x];
-  const G* g = static_cast<const G*>(grads.p[c.tensor - a.first_tensor]) + c.grad;
-  const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
-  const float keep = 1.0f - a.lr * c.decay;
+// A warp's block of 256 elements, 8 a lane: two groups of four consecutive ones, so that every
+// load and store of a warp is contiguous.
+struct Block {
+  const Chunk& c;
+  int b0;              // first element of the block in the chunk
+  int64_t s0;          // and in the state arrays
+  bool full;           // whole, and aligned for wide accesses
+};
+
+template <typename G>
+__device__ __forceinline__ bool is_wide(const Chunk& c, const G* g) {
+  return ((reinterpret_cast<uintptr_t>(c.p) & 15) | (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(G) - 1)) |
+          (reinterpret_cast<uintptr_t>(c.copy) & 7)) == 0;
+}
+
+template <typename G>
+__device__ __forceinline__ void load_pg(const Block& b, const G* g, float* p, float* gr) {
   const int lane = threadIdx.x & 31;
-  const bool wide = ((reinterpret_cast<uintptr_t>(c.p) & 15) |
-                     (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(G) - 1)) |
-                     (reinterpret_cast<uintptr_t>(c.copy) & 7)) == 0;
-  const int b0 = (threadIdx.x >> 5) * kBlock;
-  if (b0 < c.n) {
-    float p[8], gr[8], m[8], v[8];
-    const bool full = wide && b0 + kBlock <= c.n;
-    const int64_t s0 = c.state + b0;
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int e = b0 + q * 128 + lane * 4;
-      if (full) {
-        const float4 f = __ldcs(reinterpret_cast<const float4*>(c.p + e));
-        p[4 * q] = f.x; p[4 * q + 1] = f.y; p[4 * q + 2] = f.z; p[4 * q + 3] = f.w;
-        load_grad4<G>(g + e, gr + 4 * q);
-      } else {
+  for (int q = 0; q < 2; ++q) {
+    const int e = b.b0 + q * 128 + lane * 4;
+    if (b.full) {
+      const float4 f = __ldcs(reinterpret_cast<const float4*>(b.c.p + e));
+      p[4 * q] = f.x; p[4 * q + 1] = f.y; p[4 * q + 2] = f.z; p[4 * q + 3] = f.w;
+      load_grad4<G>(g + e, gr + 4 * q);
+    } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[4 * q + i] = e + i < c.n ? c.p[e + i] : 0.0f;
-          gr[4 * q + i] = e + i < c.n ? Elem<G>::up(g[e + i]) : 0.0f;
-        }
-      }
-      const int64_t s = s0 + q * 128 + lane * 4;
-      if constexpr (BITS == 32) {
-        const float4 fm = __ldcs(reinterpret_cast<const float4*>(static_cast<float*>(a.m) + s));
-        const float4 fv = __ldcs(reinterpret_cast<const float4*>(static_cast<float*>(a.v) + s));
-        m[4 * q] = fm.x; m[4 * q + 1] = fm.y; m[4 * q + 2] = fm.z; m[4 * q + 3] = fm.w;
-        v[4 * q] = fv.x; v[4 * q + 1] = fv.y; v[4 * q + 2] = fv.z; v[4 * q + 3] = fv.w;
-      } else {
-        from_e4m3x4(__ldcs(reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(a.m) + s)), m + 4 * q);
-        from_e4m3x4(__ldcs(reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(a.v) + s)), v + 4 * q);
+      for (int i = 0; i < 4; ++i) {
+        p[4 * q + i] = e + i < b.c.n ? b.c.p[e + i] : 0.0f;
+        gr[4 * q + i] = e + i < b.c.n ? Elem<G>::up(g[e + i]) : 0.0f;
       }
     }
-    if constexpr (BITS == 8) {
-      const float ms = a.m_scale[s0 / kBlock], vs = a.v_scale[s0 / kBlock];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        m[i] = __fmul_rn(m[i], ms);
-        v[i] = __fmul_rn(v[i], vs);
-        v[i] = __fmul_rn(v[i], v[i]);
-      }
-    }
+  }
+}
+
+// The step of a block and the stores of everything it changes.
+template <int BITS>
+__device__ __forceinline__ void update(const StepArgs& a, const Block& b, float gs, float* p, const float* gr,
+                                       float* m, float* v) {
+  const int lane = threadIdx.x & 31, b0 = b.b0;
+  const int64_t s0 = b.s0;
+  const bool full = b.full;
+  const Chunk& c = b.c;
+  const float keep = 1.0f - a.lr * c.decay;
     float root[8];
     float m_top = 0.0f, r_top = 0.0f;
 #pragma unroll
@@ -277,6 +270,141 @@ __global__ void __launch_bounds__(kThreads, 5) k_adamw(const __grid_constant__ G
         __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v) + s), r8[q]);
       }
     }
+}
+
+// States of 32 bits: one CTA a chunk.  The stream of 30 bytes an element keeps the memory busy
+// by itself (71.4 M elements with a 16-bit copy: 304 us, 7.0 TB/s).
+template <typename G, int NG>
+__global__ void __launch_bounds__(kThreads, 5) k_adamw32(const __grid_constant__ Grads<NG> grads,
+                                                         const __grid_constant__ StepArgs a) {
+  const Chunk c = a.chunks[blockIdx.x];
+  const G* g = static_cast<const G*>(grads.p[c.tensor - a.first_tensor]) + c.grad;
+  const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
+  const int lane = threadIdx.x & 31, b0 = (threadIdx.x >> 5) * kBlock;
+  if (b0 >= c.n) return;
+  const Block b = {c, b0, c.state + b0, is_wide(c, g) && b0 + kBlock <= c.n};
+  float p[8], gr[8], m[8], v[8];
+  load_pg(b, g, p, gr);
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int64_t s = b.s0 + q * 128 + lane * 4;
+    const float4 fm = __ldcs(reinterpret_cast<const float4*>(static_cast<float*>(a.m) + s));
+    const float4 fv = __ldcs(reinterpret_cast<const float4*>(static_cast<float*>(a.v) + s));
+    m[4 * q] = fm.x; m[4 * q + 1] = fm.y; m[4 * q + 2] = fm.z; m[4 * q + 3] = fm.w;
+    v[4 * q] = fv.x; v[4 * q + 1] = fv.y; v[4 * q + 2] = fv.z; v[4 * q + 3] = fv.w;
+  }
+  update<32>(a, b, gs, p, gr, m, v);
+}
+
+// States of 8 bits: half the bytes and twice the arithmetic, so a warp's loads have to run
+// ahead of its arithmetic.  CTAs stay and take chunks in turn; each warp keeps the loads of its
+// next kAhead blocks under way into shared memory (asynchronous copies hold no registers), and
+// the chunks' descriptions three blocks ahead of those.  (One CTA a chunk, as above: 949 us for
+// 285 M elements with a 16-bit copy, the warps waiting for loads most of the time.)
+constexpr int kAhead = 3;
+constexpr int kRecs = 8;              // descriptions kept: 2 * kAhead and the current one
+template <typename G> constexpr int kSlot = 1024 + 256 * sizeof(G) + 512 + 16;
+template <typename G> constexpr int kWarpBytes = kAhead * kSlot<G> + kRecs * static_cast<int>(sizeof(Chunk));
+static_assert(sizeof(Chunk) == 48, "three copies of 16 bytes");
+
+template <int N>
+__device__ __forceinline__ void copy_async(void* to, const void* from) {
+  const uint32_t d = static_cast<uint32_t>(__cvta_generic_to_shared(to));
+  if constexpr (N == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(from) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(d), "l"(from), "n"(N) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+template <typename G, int NG>
+__global__ void __launch_bounds__(kThreads, 4) k_adamw8(const __grid_constant__ Grads<NG> grads,
+                                                        const __grid_constant__ StepArgs a, int chunks) {
+  extern __shared__ __align__(16) unsigned char dyn[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b0 = warp * kBlock;
+  unsigned char* slots = dyn + warp * kWarpBytes<G>;
+  Chunk* recs = reinterpret_cast<Chunk*>(slots + kAhead * kSlot<G>);
+  const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
+  auto chunk_at = [&](int k) { return static_cast<int64_t>(blockIdx.x) + static_cast<int64_t>(k) * gridDim.x; };
+  auto grad_of = [&](const Chunk& c) { return static_cast<const G*>(grads.p[c.tensor - a.first_tensor]) + c.grad; };
+  auto fetch_rec = [&](int k) {
+    if (chunk_at(k) < chunks && lane < 3)
+      copy_async<16>(reinterpret_cast<unsigned char*>(&recs[k % kRecs]) + lane * 16,
+                     reinterpret_cast<const unsigned char*>(&a.chunks[chunk_at(k)]) + lane * 16);
+  };
+  auto fetch = [&](int k) {
+    if (chunk_at(k) >= chunks) return;
+    const Chunk& c = recs[k % kRecs];
+    if (b0 >= c.n) return;
+    unsigned char* slot = slots + k % kAhead * kSlot<G>;
+    const G* g = grad_of(c);
+    const int64_t s0 = c.state + b0;
+    const bool full = is_wide(c, g) && b0 + kBlock <= c.n;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int e = q * 128 + lane * 4;
+      if (full) {
+        copy_async<16>(slot + e * 4, c.p + b0 + e);
+        copy_async<4 * sizeof(G)>(slot + 1024 + e * sizeof(G), g + b0 + e);
+      }
+      copy_async<4>(slot + 1024 + 256 * sizeof(G) + e, static_cast<const uint8_t*>(a.m) + s0 + e);
+      copy_async<4>(slot + 1024 + 256 * sizeof(G) + 256 + e, static_cast<const uint8_t*>(a.v) + s0 + e);
+    }
+    if (lane < 2)
+      copy_async<4>(slot + 1024 + 256 * sizeof(G) + 512 + lane * 4, (lane ? a.v_scale : a.m_scale) + s0 / kBlock);
+  };
+  for (int k = 0; k < 2 * kAhead; ++k) fetch_rec(k);
+  copy_commit();
+  copy_wait<0>();
+  __syncwarp();
+  for (int k = 0; k < kAhead; ++k) {
+    fetch(k);
+    copy_commit();
+  }
+  for (int k = 0; chunk_at(k) < chunks; ++k) {
+    copy_wait<kAhead - 1>();
+    __syncwarp();
+    const Chunk c = recs[k % kRecs];
+    const G* g = grad_of(c);
+    const Block b = {c, b0, c.state + b0, is_wide(c, g) && b0 + kBlock <= c.n};
+    const unsigned char* slot = slots + k % kAhead * kSlot<G>;
+    float p[8], gr[8], m[8], v[8];
+    const bool any = b0 < c.n;
+    if (any) {
+      if (b.full) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const int e = q * 128 + lane * 4;
+          const float4 f = *reinterpret_cast<const float4*>(slot + e * 4);
+          p[4 * q] = f.x; p[4 * q + 1] = f.y; p[4 * q + 2] = f.z; p[4 * q + 3] = f.w;
+          load_grad4<G>(reinterpret_cast<const G*>(slot + 1024) + e, gr + 4 * q);
+        }
+      } else {
+        load_pg(b, g, p, gr);
+      }
+      const unsigned char* codes = slot + 1024 + 256 * sizeof(G);
+      const float ms = *reinterpret_cast<const float*>(codes + 512), vs = *reinterpret_cast<const float*>(codes + 516);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        from_e4m3x4(*reinterpret_cast<const uint32_t*>(codes + q * 128 + lane * 4), m + 4 * q);
+        from_e4m3x4(*reinterpret_cast<const uint32_t*>(codes + 256 + q * 128 + lane * 4), v + 4 * q);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        m[i] = __fmul_rn(m[i], ms);
+        v[i] = __fmul_rn(v[i], vs);
+        v[i] = __fmul_rn(v[i], v[i]);
+      }
+    }
+    __syncwarp();                     // the slot is read; its next block may come
+    fetch_rec(k + 2 * kAhead);
+    fetch(k + kAhead);
+    copy_commit();
+    if (any) update<8>(a, b, gs, p, gr, m, v);
   }
 }
 
@@ -309,7 +437,16 @@ cudaError_t launch_range(const hier_avg_adamw* h, const void* const* grads, int 
   for (int t = t0; t < t1; ++t) g.p[t - t0] = grads[t];
   a.chunks = h->table + c0;
   a.first_tensor = t0;
-  k_adamw<BITS, G, NG><<<static_cast<unsigned>(c1 - c0), kThreads, 0, s>>>(g, a);
+  if constexpr (BITS == 32) {
+    k_adamw32<G, NG><<<static_cast<unsigned>(c1 - c0), kThreads, 0, s>>>(g, a);
+  } else {
+    constexpr int smem = kThreads / 32 * kWarpBytes<G>;
+    const cudaError_t e = cudaFuncSetAttribute(k_adamw8<G, NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    const int64_t held = kSms * (227 * 1024 / (smem + 1024) < 4 ? 227 * 1024 / (smem + 1024) : 4);
+    k_adamw8<G, NG><<<static_cast<unsigned>(c1 - c0 < held ? c1 - c0 : held), kThreads, smem, s>>>(
+        g, a, static_cast<int>(c1 - c0));
+  }
   return cudaGetLastError();
 }
 
