@@ -67,15 +67,17 @@ __device__ __forceinline__ float rcp_fast(float x) {
   return r;
 }
 
-// sqrt(x), rounded to nearest: the residual of x * (1 / sqrt(x)) corrects its last bit
+// sqrt(x) of two numbers, rounded to nearest: the residual of x * (1 / sqrt(x)) corrects its last bit
 // (Markstein 1990).  From 2^-102 on all fp32 numbers give __fsqrt_rn's result (compared one by
 // one); below, where the residual underflows, some are off in the last bit, and below the
 // smallest normal number the result is too small (0 stays 0).
-__device__ __forceinline__ float sqrt_near(float x) {
-  float y;
-  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(max_nan(x, 1.17549435e-38f)));
-  const float s = __fmul_rn(x, y);
-  return __fmaf_rn(__fmaf_rn(-s, s, x), 0.5f * y, s);
+__device__ __forceinline__ Pair sqrt_near(Pair x) {
+  float a, b, ya, yb;
+  halves(x, a, b);
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(ya) : "f"(max_nan(a, 1.17549435e-38f)));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(yb) : "f"(max_nan(b, 1.17549435e-38f)));
+  const Pair y = pair(ya, yb), s = mul2(x, y), n = mul2(y, pair(-0.5f, -0.5f));
+  return fma2(fma2(s, s, mul2(x, pair(-1.0f, -1.0f))), n, s);      // (x - s s) y / 2 + s
 }
 
 // 20 random bits for place j: a multiplicative hash with the fractions of the golden
@@ -178,98 +180,107 @@ __device__ __forceinline__ void update(const StepArgs& a, const Block& b, float 
   const bool full = b.full;
   const Chunk& c = b.c;
   const float keep = 1.0f - a.lr * c.decay;
-    float root[8];
-    float m_top = 0.0f, r_top = 0.0f;
+  float root[8];
+  float m_top = 0.0f, r_top = 0.0f;
+  // The states are rounded operation by operation, so that what is stored in 8 bits can be
+  // reproduced exactly: one unit in the 24th place can move a code by 1/8 of its value.  Two
+  // elements an instruction: in 8 bits the arithmetic is as long as the memory takes.
+  auto both = [](float x) { return pair(x, x); };
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      // The states are rounded operation by operation, so that what is stored in 8 bits can be
-      // reproduced exactly: one unit in the 24th place can move a code by 1/8 of its value.
-      const float gi = __fmul_rn(gr[i], gs);
-      m[i] = __fadd_rn(__fmul_rn(a.b1, m[i]), __fmul_rn(a.omb1, gi));
-      v[i] = __fadd_rn(__fmul_rn(a.b2, v[i]), __fmul_rn(__fmul_rn(a.omb2, gi), gi));
-      root[i] = sqrt_near(v[i]);
-      p[i] = p[i] * keep - a.step * (m[i] * rcp_fast(root[i] * a.inv_c2 + a.eps));
-      if constexpr (BITS == 8) {
-        m_top = max_nan(m_top, fabsf(m[i]));
-        r_top = max_nan(r_top, root[i]);
-      }
+  for (int i = 0; i < 8; i += 2) {
+    const Pair g2 = mul2(pair(gr[i], gr[i + 1]), both(gs));
+    const Pair m2 = add2(mul2(both(a.b1), pair(m[i], m[i + 1])), mul2(both(a.omb1), g2));
+    const Pair v2 = add2(mul2(both(a.b2), pair(v[i], v[i + 1])), mul2(mul2(both(a.omb2), g2), g2));
+    const Pair r2 = sqrt_near(v2);
+    float da, db;
+    halves(fma2(r2, both(a.inv_c2), both(a.eps)), da, db);
+    const Pair u = mul2(m2, pair(rcp_fast(da), rcp_fast(db)));
+    halves(fma2(u, both(-a.step), mul2(pair(p[i], p[i + 1]), both(keep))), p[i], p[i + 1]);
+    halves(m2, m[i], m[i + 1]);
+    halves(r2, root[i], root[i + 1]);
+    if constexpr (BITS == 32) {
+      halves(v2, v[i], v[i + 1]);
+    } else {
+      m_top = max_nan(m_top, max_nan(fabsf(m[i]), fabsf(m[i + 1])));
+      r_top = max_nan(r_top, max_nan(root[i], root[i + 1]));
     }
+  }
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int e = b0 + q * 128 + lane * 4;
-      const float* x = p + 4 * q;
-      if (full) {
-        __stcs(reinterpret_cast<float4*>(c.p + e), make_float4(x[0], x[1], x[2], x[3]));
-        if (c.copy) {
-          uint2 w;
-          if (a.copy_type == HA_TYPE_BF16)
-            w = make_uint2(narrow2<__nv_bfloat16>(x[0], x[1]), narrow2<__nv_bfloat16>(x[2], x[3]));
-          else
-            w = make_uint2(narrow2<__half>(x[0], x[1]), narrow2<__half>(x[2], x[3]));
-          __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(c.copy) + e), w);
-        }
-      } else {
+  for (int q = 0; q < 2; ++q) {
+    const int e = b0 + q * 128 + lane * 4;
+    const float* x = p + 4 * q;
+    if (full) {
+      __stcs(reinterpret_cast<float4*>(c.p + e), make_float4(x[0], x[1], x[2], x[3]));
+      if (c.copy) {
+        uint2 w;
+        if (a.copy_type == HA_TYPE_BF16)
+          w = make_uint2(narrow2<__nv_bfloat16>(x[0], x[1]), narrow2<__nv_bfloat16>(x[2], x[3]));
+        else
+          w = make_uint2(narrow2<__half>(x[0], x[1]), narrow2<__half>(x[2], x[3]));
+        __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(c.copy) + e), w);
+      }
+    } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (e + i < c.n) {
-            c.p[e + i] = x[i];
-            if (c.copy) {
-              if (a.copy_type == HA_TYPE_BF16)
-                static_cast<__nv_bfloat16*>(c.copy)[e + i] = __float2bfloat16_rn(x[i]);
-              else
-                static_cast<__half*>(c.copy)[e + i] = __float2half_rn(x[i]);
-            }
+      for (int i = 0; i < 4; ++i)
+        if (e + i < c.n) {
+          c.p[e + i] = x[i];
+          if (c.copy) {
+            if (a.copy_type == HA_TYPE_BF16)
+              static_cast<__nv_bfloat16*>(c.copy)[e + i] = __float2bfloat16_rn(x[i]);
+            else
+              static_cast<__half*>(c.copy)[e + i] = __float2half_rn(x[i]);
           }
-      }
+        }
     }
-    uint32_t m8[2], r8[2];
-    if constexpr (BITS == 8) {
-      m_top = warp_abs_max(m_top);
-      r_top = warp_abs_max(r_top);
-      if (m_top < kTiny) m_top = 0.0f;
-      if (r_top < kTiny) r_top = 0.0f;
-      const float mi = m_top == 0.0f ? 0.0f : __fmul_rn(__frcp_rn(m_top), kTop);
-      const float ri = r_top == 0.0f ? 0.0f : __fmul_rn(__frcp_rn(r_top), kTop);
-      float least = INFINITY;
+  }
+  uint32_t m8[2], r8[2];
+  if constexpr (BITS == 8) {
+    m_top = warp_abs_max(m_top);
+    r_top = warp_abs_max(r_top);
+    if (m_top < kTiny) m_top = 0.0f;
+    if (r_top < kTiny) r_top = 0.0f;
+    const float mi = m_top == 0.0f ? 0.0f : __fmul_rn(__frcp_rn(m_top), kTop);
+    const float ri = r_top == 0.0f ? 0.0f : __fmul_rn(__frcp_rn(r_top), kTop);
+    float least = INFINITY;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        m[i] = __fmul_rn(m[i], mi);
-        root[i] = __fmul_rn(root[i], ri);
-        least = fminf(least, root[i]);
-      }
-      const uint32_t j = static_cast<uint32_t>(s0) + lane * 4;
-      if (__all_sync(~0u, least >= 0.015625f)) {       // nearly always: no value below 2^-6
+    for (int i = 0; i < 8; i += 2) {
+      halves(mul2(pair(m[i], m[i + 1]), both(mi)), m[i], m[i + 1]);
+      halves(mul2(pair(root[i], root[i + 1]), both(ri)), root[i], root[i + 1]);
+      least = fminf(least, fminf(root[i], root[i + 1]));
+    }
+    const uint32_t j = static_cast<uint32_t>(s0) + lane * 4;
+    if (__all_sync(~0u, least >= 0.015625f)) {       // nearly always: no value below 2^-6
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          root[i] = round_random_normal(root[i], random20(j + (i >> 2) * 128 + (i & 3), a.seed));
-      } else {
+      for (int i = 0; i < 8; ++i)
+        root[i] = round_random_normal(root[i], random20(j + (i >> 2) * 128 + (i & 3), a.seed));
+    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          root[i] = round_random(root[i], random20(j + (i >> 2) * 128 + (i & 3), a.seed));
-      }
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        m8[q] = to_e4m3x4(m + 4 * q);
-        r8[q] = to_e4m3x4(root + 4 * q);
-      }
-      if (lane == 0) {
-        a.m_scale[s0 / kBlock] = m_top * (1.0f / kTop);
-        a.v_scale[s0 / kBlock] = r_top * (1.0f / kTop);
-      }
+      for (int i = 0; i < 8; ++i)
+        root[i] = round_random(root[i], random20(j + (i >> 2) * 128 + (i & 3), a.seed));
     }
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      const int64_t s = s0 + q * 128 + lane * 4;
-      if constexpr (BITS == 32) {
-        __stcs(reinterpret_cast<float4*>(static_cast<float*>(a.m) + s),
-               make_float4(m[4 * q], m[4 * q + 1], m[4 * q + 2], m[4 * q + 3]));
-        __stcs(reinterpret_cast<float4*>(static_cast<float*>(a.v) + s),
-               make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
-      } else {
-        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.m) + s), m8[q]);
-        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v) + s), r8[q]);
-      }
+      m8[q] = to_e4m3x4(m + 4 * q);
+      r8[q] = to_e4m3x4(root + 4 * q);
     }
+    if (lane == 0) {
+      a.m_scale[s0 / kBlock] = m_top * (1.0f / kTop);
+      a.v_scale[s0 / kBlock] = r_top * (1.0f / kTop);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int64_t s = s0 + q * 128 + lane * 4;
+    if constexpr (BITS == 32) {
+      __stcs(reinterpret_cast<float4*>(static_cast<float*>(a.m) + s),
+             make_float4(m[4 * q], m[4 * q + 1], m[4 * q + 2], m[4 * q + 3]));
+      __stcs(reinterpret_cast<float4*>(static_cast<float*>(a.v) + s),
+             make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
+    } else {
+      __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.m) + s), m8[q]);
+      __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v) + s), r8[q]);
+    }
+  }
 }
 
 // States of 32 bits: one CTA a chunk.  The stream of 30 bytes an element keeps the memory busy
@@ -394,10 +405,10 @@ __global__ void __launch_bounds__(kThreads, 4) k_adamw8(const __grid_constant__ 
         from_e4m3x4(*reinterpret_cast<const uint32_t*>(codes + 256 + q * 128 + lane * 4), v + 4 * q);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        m[i] = __fmul_rn(m[i], ms);
-        v[i] = __fmul_rn(v[i], vs);
-        v[i] = __fmul_rn(v[i], v[i]);
+      for (int i = 0; i < 8; i += 2) {
+        halves(mul2(pair(m[i], m[i + 1]), pair(ms, ms)), m[i], m[i + 1]);
+        const Pair r2 = mul2(pair(v[i], v[i + 1]), pair(vs, vs));
+        halves(mul2(r2, r2), v[i], v[i + 1]);
       }
     }
     __syncwarp();                     // the slot is read; its next block may come
@@ -441,8 +452,12 @@ cudaError_t launch_range(const hier_avg_adamw* h, const void* const* grads, int 
     k_adamw32<G, NG><<<static_cast<unsigned>(c1 - c0), kThreads, 0, s>>>(g, a);
   } else {
     constexpr int smem = kThreads / 32 * kWarpBytes<G>;
-    const cudaError_t e = cudaFuncSetAttribute(k_adamw8<G, NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaError_t e = cudaFuncSetAttribute(k_adamw8<G, NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(k_adamw8<G, NG>, cudaFuncAttributePreferredSharedMemoryCarveout,
+                               cudaSharedmemCarveoutMaxShared);
     if (e != cudaSuccess) return e;
+    // as many CTAs as the SMs hold at once, since they take the chunks in turn
     const int64_t held = kSms * (227 * 1024 / (smem + 1024) < 4 ? 227 * 1024 / (smem + 1024) : 4);
     k_adamw8<G, NG><<<static_cast<unsigned>(c1 - c0 < held ? c1 - c0 : held), kThreads, smem, s>>>(
         g, a, static_cast<int>(c1 - c0));

@@ -49,4 +49,30 @@ template <> __device__ __forceinline__ uint32_t narrow2<__half>(float a, float b
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// Two floats an instruction, each rounded as by the instruction for one.
+struct Pair { uint64_t w; };
+__device__ __forceinline__ Pair pair(float a, float b) {
+  Pair p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p.w) : "f"(a), "f"(b));
+  return p;
+}
+__device__ __forceinline__ void halves(Pair p, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.w));
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  Pair p;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(p.w) : "l"(a.w), "l"(b.w));
+  return p;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+  Pair p;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(p.w) : "l"(a.w), "l"(b.w));
+  return p;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair p;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(p.w) : "l"(a.w), "l"(b.w), "l"(c.w));
+  return p;
+}
+
 }  // namespace ha
