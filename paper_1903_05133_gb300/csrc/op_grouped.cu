@@ -28,7 +28,8 @@ constexpr int kMaxGroups = 1024;
 constexpr int kEpiWarps = 8;            // two groups of four: a group reads half the columns
 constexpr int kThreads = (kEpiWarps + 2) * 32;          // results, loads, products
 constexpr int kPairCols = 256;          // columns of a tile of two CTAs
-constexpr int kFewCols = 32;            // of a tile of one CTA, where groups have few rows
+constexpr int kMinChunks = 8;           // of each of the CTAs that share a tile
+constexpr int kMaxSplit = 8;            // CTAs that share a tile's summed length
 // fp32 results: the tensor core's running sum is taken into fp32 registers after this many
 // chunks.  Its additions truncate; over a sum of 4096 random products that cost 4.4e-6 of the
 // result's norm, over 16384 1.9e-5, over 512 4.7e-7 (fp32 additions: 6.1e-7, 1.5e-6 and 1.6e-7).
@@ -344,7 +345,7 @@ __device__ __forceinline__ bool finish_tile(const Args& a, const Tile& t, uint32
   const int cb = half * H, ce = min(H, t.cols - cb);      // this warp group's columns
   const int f = cta_m0 + quad * 32 + lane;                // this thread's feature
   const float bias = MODE == kFwd && a.bias && f < a.m ? a.bias[t.g * a.bias_ld + f] : 0.0f;
-  constexpr int STEP = H < 32 ? H : 32;
+  constexpr int STEP = 32;
   auto emit = [&](const float* v, int j) {
     if (MODE == kDw)
       emit_weights(a, v, t.g, cta_m0 + quad * 32, t.c0 + cb + j, t.c0 + cb + ce, stage + warp * kWarpStage);
@@ -357,8 +358,7 @@ __device__ __forceinline__ bool finish_tile(const Args& a, const Tile& t, uint32
   };
   auto read = [&](float* v, int buf, int j) {
     const uint32_t at = tmem + (static_cast<uint32_t>(quad * 32) << 16) + buf * NT + cb + j;
-    if (STEP == 32) tmem_ld32(at, v);
-    else tmem_ld16(at, v);
+    tmem_ld32(at, v);
     tmem_ld_wait();
   };
   if (MODE == kDw && t.bias) {
@@ -408,9 +408,9 @@ __device__ __forceinline__ bool finish_tile(const Args& a, const Tile& t, uint32
     if (segs) release(seg++);
     return true;
   }
-  float acc[H < 32 ? 32 : H];
+  float acc[H];
 #pragma unroll
-  for (int j = 0; j < (H < 32 ? 32 : H); ++j) acc[j] = 0.0f;
+  for (int j = 0; j < H; ++j) acc[j] = 0.0f;
   for (int s = 0; s < segs; ++s) {
     if (!wait(seg)) return false;
 #pragma unroll
@@ -429,33 +429,41 @@ __device__ __forceinline__ bool finish_tile(const Args& a, const Tile& t, uint32
   return true;
 }
 
-// ---- groups of few rows: one CTA a tile of 128 features and up to 32 rows
+// ---- groups of few rows: one CTA a tile of 128 features and up to NT rows
 // The weights' bytes are what counts, so the stages are many and small: a chunk of weights
-// is 16 KB, and 9 of them are in flight.
-struct Few {
-  static constexpr int kA = kM * kK * 2, kB = kFewCols * kK * 2, kStages = 9;
-  static constexpr int kSmem = kStages * (kA + kB) + 2 * kRowsStage + 1024;
+// is 16 KB, and 9 of them (NT = 64: 6) are in flight.  Where there are fewer tiles than SMs, the
+// CTAs of a cluster share a tile: each sums its part of the length, and the first adds the
+// others' sums, in their order, from their shared memory.
+template <int NT>
+struct One {
+  static constexpr int kA = kM * kK * 2, kB = NT * kK * 2, kStages = NT == 32 ? 9 : 6;
+  static constexpr int kPart = kM * NT * 4;               // sums for the cluster's first CTA
+  static constexpr int kOut = 2 * kRowsStage > kPart ? 2 * kRowsStage : kPart;
+  static constexpr int kSmem = kStages * (kA + kB) + kOut + 1024;
 };
 
-template <int MODE, bool FOLD>
+template <int MODE, bool FOLD, int NT>
 __global__ void __launch_bounds__(kThreads, 1)
-    k_grouped_few(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
+    k_grouped_one(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
                   const __grid_constant__ Args a) {
+  using S = One<NT>;
   extern __shared__ unsigned char raw[];
-  __shared__ uint64_t full[Few::kStages], empty[Few::kStages], tfull[2], tempty[2];
+  // theirs (the first CTA's): the other CTAs' sums are there; mine: this CTA's have been read
+  __shared__ uint64_t full[S::kStages], empty[S::kStages], tfull[2], tempty[2], theirs, mine;
   __shared__ uint32_t tmem_at;
   __shared__ int table[2 * (kMaxGroups + 1)];
   const Table tab = {table, table + kMaxGroups + 1};
   unsigned char* As = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
-  unsigned char* Bs = As + Few::kStages * Few::kA;
-  unsigned char* Out = Bs + Few::kStages * Few::kB;
+  unsigned char* Bs = As + S::kStages * S::kA;
+  unsigned char* Out = Bs + S::kStages * S::kB;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = static_cast<int>(cluster_rank()), split = static_cast<int>(cluster_size());
   if (warp == kEpiWarps) {
-    tmem_alloc(&tmem_at, 2 * kFewCols);
+    tmem_alloc(&tmem_at, 2 * NT);
     tmem_relinquish();
   }
   if (tid == 0) {
-    for (int i = 0; i < Few::kStages; ++i) {
+    for (int i = 0; i < S::kStages; ++i) {
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
     }
@@ -463,32 +471,37 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&tfull[i], 1);
       mbar_init(&tempty[i], kEpiWarps);
     }
+    mbar_init(&theirs, (split - 1) * kEpiWarps > 0 ? (split - 1) * kEpiWarps : 1);
+    mbar_init(&mine, kEpiWarps);
     fence_barrier_init();
   }
   tc_fence_before();
-  make_table<MODE, kM, kFewCols>(tab, a);
-  Tiles<MODE, kM, kFewCols, 16> list(tab, a);
+  make_table<MODE, kM, NT>(tab, a);
+  if (split > 1) cluster_arrive();                        // the barriers are set up
+  Tiles<MODE, kM, NT, 16> list(tab, a);
   tc_fence_after();
   const uint32_t tmem = tmem_at;
-  const int tiles = tab.first[a.groups];
+  const int tiles = tab.first[a.groups], i0 = blockIdx.x / split, step = gridDim.x / split;
+  const int all = (a.k + kK - 1) / kK;                     // chunks of a tile, and this CTA's
+  const int c0 = all * rank / split, c1 = all * (rank + 1) / split;
   clear_rows(a, 0, tab.off[0]);
   clear_rows(a, tab.off[a.groups], a.rows);
 
   if (warp == kEpiWarps) {
     // ---- loads
     if (elect_one()) {
-      Ring<Few::kStages> at;
+      Ring<S::kStages> at;
       bool ok = true;
       const uint64_t stream = l2_stream_policy(true), keep = l2_stream_policy(false);
-      for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+      for (int i = i0; i < tiles && ok; i += step) {
         const Tile t = list.at(i);
-        const int nk = (t.k + kK - 1) / kK, boxes = (t.cols + 15) / 16;
-        for (int c = 0; c < nk; ++c, at.next()) {
+        const int boxes = (t.cols + 15) / 16;
+        for (int c = c0; c < c1; ++c, at.next()) {
           const int st = at.st;
           if (!mbar_wait_hot(&empty[st], at.round ^ 1, &g_operator_error)) { ok = false; break; }
           uint64_t* bar = &full[st];
-          mbar_arrive_expect_tx(bar, Few::kA + boxes * 2048);
-          unsigned char* A = As + st * Few::kA;
+          mbar_arrive_expect_tx(bar, S::kA + boxes * 2048);
+          unsigned char* A = As + st * S::kA;
           if (MODE == kFwd) {
             tma_load_3d_hint(A, &ta, bar, c * kK, t.m0, t.g, stream);
           } else {
@@ -496,69 +509,121 @@ __global__ void __launch_bounds__(kThreads, 1)
             tma_load_3d_hint(A + 8192, &ta, bar, t.m0 + 64, c * kK, t.g, stream);
           }
           for (int b = 0; b < boxes; ++b)
-            tma_load_3d_hint(Bs + st * Few::kB + b * 2048, &tb, bar, c * kK, t.r0 + b * 16, 0, keep);
+            tma_load_3d_hint(Bs + st * S::kB + b * 2048, &tb, bar, c * kK, t.r0 + b * 16, 0, keep);
         }
       }
     }
   } else if (warp == kEpiWarps + 1) {
     // ---- matrix products, by one lane
     if (elect_one()) {
-      Ring<Few::kStages> at;
+      Ring<S::kStages> at;
       uint32_t seg = 0;
       bool ok = true, peek = false;
       constexpr int fold = FOLD ? kFold : 1 << 30;
-      for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+      for (int i = i0; i < tiles && ok; i += step) {
         const Tile t = list.at(i);
-        const int nk = (t.k + kK - 1) / kK;
         const uint32_t idesc = idesc_of(a.in_type, kM, (t.cols + 15) / 16 * 16) | (MODE == kFwd ? 0u : 1u << 15);
-        for (int c = 0; c < nk; ++c, at.next()) {
+        int part = 0;                                     // chunks since the last fold
+        for (int c = c0; c < c1; ++c, at.next()) {
           const int buf = seg & 1;
-          ok = (c % fold != 0 || mbar_wait_hot(&tempty[buf], ((seg >> 1) & 1) ^ 1, &g_operator_error)) &&
+          ok = (part != 0 || mbar_wait_hot(&tempty[buf], ((seg >> 1) & 1) ^ 1, &g_operator_error)) &&
                (peek || mbar_wait_hot(&full[at.st], at.round, &g_operator_error));
           if (!ok) break;
           tc_fence_after();
           const int steps = (min(t.k - c * kK, kK) + 15) / 16;
-          const uint32_t as = smem_u32(As + at.st * Few::kA), bs = smem_u32(Bs + at.st * Few::kB);
+          const uint32_t as = smem_u32(As + at.st * S::kA), bs = smem_u32(Bs + at.st * S::kB);
           const uint64_t da = MODE == kFwd ? umma_desc_sw128(as) : umma_desc_sw128_mn(as, 8192);
           const uint64_t db = umma_desc_sw128(bs);
-          constexpr int SA = MODE == kFwd ? 2 : 128;           // 16 values further, in 16 bytes
+          constexpr int SA = MODE == kFwd ? 2 : 128;      // 16 values further, in 16 bytes
           if (steps == 4) {
-            peek = tc_chunk<SA, 2>(tmem + buf * kFewCols, da, db, idesc, c % fold != 0, &empty[at.st],
-                                   &full[at.next_st()], at.next_round());
+            peek = tc_chunk<SA, 2>(tmem + buf * NT, da, db, idesc, part != 0, &empty[at.st], &full[at.next_st()],
+                                   at.next_round());
           } else {
             for (int k = 0; k < steps; ++k)
-              tc_mma_bf16(tmem + buf * kFewCols, da + k * SA, db + k * 2, idesc, (c % fold) || k ? 1u : 0u);
+              tc_mma_bf16(tmem + buf * NT, da + k * SA, db + k * 2, idesc, part || k ? 1u : 0u);
             tc_commit(&empty[at.st]);
             peek = false;
           }
-          if (c % fold == fold - 1 || c == nk - 1) {
+          if (++part == fold || c == c1 - 1) {
             tc_commit(&tfull[buf]);
             ++seg;
+            part = 0;
           }
         }
       }
     }
   } else {
     // ---- results
-    uint32_t seg = 0, turn = 0;
-    bool ok = true;
-    for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+    constexpr int H = NT / 2;                             // columns of a warp group
+    const int half = warp >> 2, quad = warp & 3, feature = quad * 32 + lane;
+    const int segs = FOLD ? (c1 - c0 + kFold - 1) / kFold : (c1 > c0 ? 1 : 0);
+    float* part = reinterpret_cast<float*>(Out) + half * H * kM + feature;   // [column][feature]
+    uint32_t seg = 0, turn = 0, round = 0;
+    if (split > 1) cluster_wait();
+    for (int i = i0; i < tiles; i += step, ++round) {
       const Tile t = list.at(i);
-      ok = finish_tile<MODE, kFewCols, FOLD>(
-          a, t, tmem, t.m0, Out, seg, turn,
-          [&](uint32_t s) {
-            return warp_wait(&tfull[s & 1], (s >> 1) & 1);
-          },
-          [&](uint32_t s) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&tempty[s & 1]);
-          });
+      const int cb = half * H, ce = min(H, t.cols - cb), f = t.m0 + feature;
+      float acc[32];
+#pragma unroll
+      for (int x = 0; x < 32; ++x) acc[x] = 0.0f;
+      bool ok = true;
+      for (int s = 0; s < segs && ok; ++s, ++seg) {
+        ok = warp_wait(&tfull[seg & 1], (seg >> 1) & 1);
+        if (!ok) break;
+        if (ce > 0) {
+          float v[32];
+          const uint32_t at = tmem + (static_cast<uint32_t>(quad * 32) << 16) + (seg & 1) * NT + cb;
+          if (H == 32) tmem_ld32(at, v);
+          else tmem_ld16(at, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int x = 0; x < H; ++x) acc[x] += v[x];
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&tempty[seg & 1]);
+      }
+      if (!ok) break;
+      if (rank != 0) {
+        if (round > 0) ok = warp_wait(&mine, (round - 1) & 1);
+        if (!ok) break;
+#pragma unroll
+        for (int x = 0; x < H; ++x)
+          if (x < ce) part[x * kM] = acc[x];
+        __syncwarp();
+        if (lane == 0) mbar_arrive_release_cluster(cluster_addr(&theirs, 0));
+        continue;
+      }
+      if (split > 1) {
+        if (lane == 0) ok = mbar_wait_cluster(&theirs, round & 1, &g_operator_error);
+        if (!__all_sync(~0u, ok)) break;
+        for (int q = 1; q < split; ++q) {
+          const uint32_t from = cluster_addr(part, q);
+#pragma unroll
+          for (int x = 0; x < H; ++x)
+            if (x < ce) acc[x] += ld_cluster_f32(from + x * kM * 4);
+        }
+        __syncwarp();
+        if (lane == 0)
+          for (int q = 1; q < split; ++q) mbar_arrive_release_cluster(cluster_addr(&mine, q));
+      }
+      const float bias = MODE == kFwd && a.bias && f < a.m ? a.bias[t.g * a.bias_ld + f] : 0.0f;
+      if (ce > 0) {
+        if (FOLD)
+          emit_rows<MODE, float>(a, acc, t.c0 + cb, min(H, ce), t.m0, feature, bias, Out + half * kRowsStage, 1 + half, turn);
+        else
+          emit_rows<MODE, uint16_t>(a, acc, t.c0 + cb, min(H, ce), t.m0, feature, bias, Out + half * kRowsStage, 1 + half, turn);
+      }
     }
+  }
+  if (split > 1 && warp >= kEpiWarps) {
+    __syncwarp();
+    cluster_wait();
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == kEpiWarps) tmem_dealloc(tmem, 2 * kFewCols);
+  if (split > 1) cluster_sync_all();                      // the first CTA reads the others' memory
+  if (warp == kEpiWarps) tmem_dealloc(tmem, 2 * NT);
 }
 
 // ---- everything else: two CTAs of a cluster a tile of 256 features and up to 256 columns
@@ -742,6 +807,8 @@ __global__ void __launch_bounds__(256) k_pack(const uint16_t* src, int64_t rows,
 constexpr int kSms = 152;
 // Groups of at most this many rows on average take the tiles for few rows.
 constexpr int kFewRows = 32;
+// Fewer tiles of pairs than this leave too many SMs idle.
+constexpr int kSmallTiles = 40;
 int64_t round8(int64_t x) { return (x + 7) / 8 * 8; }
 int64_t round256(int64_t x) { return (x + 255) / 256 * 256; }
 
@@ -788,14 +855,54 @@ bool make_map(CUtensorMap* m, const Operand& o, int type, uint32_t b0, uint32_t 
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int MODE, bool FOLD>
-int launch_few(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int64_t most, cudaStream_t s) {
-  if (cudaFuncSetAttribute(k_grouped_few<MODE, FOLD>, cudaFuncAttributeMaxDynamicSharedMemorySize, Few::kSmem) !=
-      cudaSuccess)
-    return HA_ECUDA;
-  k_grouped_few<MODE, FOLD><<<static_cast<unsigned>(std::min<int64_t>(kSms, std::max<int64_t>(most, 1))), kThreads,
-                             Few::kSmem, s>>>(ta, tb, a);
-  return cudaGetLastError() == cudaSuccess ? HA_OK : HA_ECUDA;
+// Clusters of `size` CTAs that the GPU holds at once.
+template <typename K>
+int clusters_held(K kernel, int smem, int size) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(kSms / size * size);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = size;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  return cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess ? n : 0;
+}
+
+// `tiles`: about how many there are; `most`: at most.
+template <int MODE, bool FOLD, int NT>
+int launch_one(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int64_t tiles, int64_t most, cudaStream_t s) {
+  const auto kernel = k_grouped_one<MODE, FOLD, NT>;
+  constexpr int smem = One<NT>::kSmem;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return HA_ECUDA;
+  // CTAs a tile: as many as fill the GPU, with at least kMinChunks chunks each (one row, 4096 ->
+  // 4096: 18.2 us with one CTA a tile).
+  static int held[4] = {0, 0, 0, 0};
+  int split = 1, log = 0;
+  while (split < kMaxSplit && tiles * split * 2 <= kSms && (a.k + kK - 1) / kK >= split * 2 * kMinChunks) {
+    split *= 2;
+    ++log;
+  }
+  if (held[log] == 0) held[log] = split == 1 ? kSms : clusters_held(kernel, smem, split);
+  if (held[log] < 1) return HA_ECUDA;
+  const int64_t clusters = std::min<int64_t>(held[log], std::max<int64_t>(most, 1));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(clusters * split));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = split;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, ta, tb, a) == cudaSuccess ? HA_OK : HA_ECUDA;
 }
 
 template <int MODE, bool FOLD>
@@ -807,22 +914,8 @@ int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap&
   // As many pairs as the GPU holds at once (its clusters of two leave some SMs out): the tiles
   // are dealt out in advance, so a pair that started late would finish late.
   static int held = 0;
-  if (held == 0) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kSms);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = Pair::kSmem;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, k_grouped_pair<MODE, FOLD>, &cfg) != cudaSuccess || n < 1) return HA_ECUDA;
-    held = n;
-  }
+  if (held == 0) held = clusters_held(k_grouped_pair<MODE, FOLD>, Pair::kSmem, 2);
+  if (held < 1) return HA_ECUDA;
   const int64_t pairs = std::min<int64_t>(held, std::max<int64_t>(most, 1));
   k_grouped_pair<MODE, FOLD><<<static_cast<unsigned>(2 * pairs), kThreads, Pair::kSmem, s>>>(ta, tb, ta_head, tb_head, a);
   return cudaGetLastError() == cudaSuccess ? HA_OK : HA_ECUDA;
@@ -846,15 +939,29 @@ int rows_product(Operand x, Operand w, Args a, void* ws, int64_t ws_bytes, cudaS
   if (pack(x, p, s) != cudaSuccess || pack(w, p, s) != cudaSuccess) return HA_ECUDA;
   a.wide_out = (reinterpret_cast<uintptr_t>(a.out) & 15) == 0 && a.out_ld * type_size(a.out_type) % 16 == 0;
   a.wide_h = a.h && (reinterpret_cast<uintptr_t>(a.h) & 15) == 0 && a.h_ld % 8 == 0;
-  const bool few = a.rows <= kFewRows * static_cast<int64_t>(a.groups), fold = a.out_type == HA_TYPE_FP32;
+  const bool fold = a.out_type == HA_TYPE_FP32;
+  const int64_t rows = a.rows, used = std::min<int64_t>(rows, a.groups);      // groups with rows, about
+  const int64_t m1 = (a.m + kM - 1) / kM, m2 = (a.m + 2 * kM - 1) / (2 * kM);
+  // Few rows a group: narrow tiles.  So few rows in all that pairs would leave most SMs idle:
+  // tiles of one CTA, twice as many and four times as narrow (4096 -> 4096, 256 rows of one
+  // group: 24.5 us by pairs).
+  const bool few = rows <= kFewRows * static_cast<int64_t>(a.groups);
+  const bool small = m2 * std::max<int64_t>(used, (rows + kPairCols - 1) / kPairCols) < kSmallTiles;
   CUtensorMap ta, tb;
-  if (!make_map(&ta, w, a.in_type, 64, MODE == kFwd ? 128 : 64) || !make_map(&tb, x, a.in_type, 64, few ? 16 : 64))
+  if (!make_map(&ta, w, a.in_type, 64, MODE == kFwd ? 128 : 64) ||
+      !make_map(&tb, x, a.in_type, 64, few || small ? 16 : 64))
     return HA_ECUDA;
   if (few) {
-    const int64_t most = (a.m + kM - 1) / kM * std::min<int64_t>(a.rows, a.groups + a.rows / kFewCols);
-    return fold ? launch_few<MODE, true>(ta, tb, a, most, s) : launch_few<MODE, false>(ta, tb, a, most, s);
+    const int64_t tiles = m1 * used, most = m1 * std::min<int64_t>(rows, a.groups + rows / 32);
+    return fold ? launch_one<MODE, true, 32>(ta, tb, a, tiles, most, s)
+                : launch_one<MODE, false, 32>(ta, tb, a, tiles, most, s);
   }
-  const int64_t most = (a.m + 2 * kM - 1) / (2 * kM) * std::min<int64_t>(a.rows, a.groups + a.rows / kPairCols);
+  if (small) {
+    const int64_t tiles = m1 * std::max<int64_t>(used, (rows + 63) / 64), most = m1 * std::min<int64_t>(rows, a.groups + rows / 64);
+    return fold ? launch_one<MODE, true, 64>(ta, tb, a, tiles, most, s)
+                : launch_one<MODE, false, 64>(ta, tb, a, tiles, most, s);
+  }
+  const int64_t most = m2 * std::min<int64_t>(rows, a.groups + rows / kPairCols);
   return fold ? launch_pair<MODE, true>(ta, tb, ta, tb, a, most, s)
               : launch_pair<MODE, false>(ta, tb, ta, tb, a, most, s);
 }
