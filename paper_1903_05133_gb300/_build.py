@@ -24,7 +24,7 @@ SOURCES = ["hier_avg_api.cu", "avg_kernels.cu", "step_tc.cu", "step_head.cu", "s
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 COMMON = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-ftz=false",
           "-prec-div=true", "-prec-sqrt=true", f"-I{INCLUDE}", f"-I{CSRC}"]
-EXTRA = {"avg_kernels.cu": ["-fmad=false"]}
+EXTRA = {"avg_kernels.cu": ["-fmad=false"], "op_adamw.cu": ["-fmad=false"]}
 
 
 def _nvcc() -> str:

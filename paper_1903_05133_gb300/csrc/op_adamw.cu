@@ -171,6 +171,15 @@ __device__ __forceinline__ void load_pg(const Block& b, const G* g, float* p, fl
   }
 }
 
+// a + b, each rounded: a product of two pairs and a sum of them would be contracted to one
+// operation (by the assembler, whatever the rounding modifiers and -fmad=false say).
+__device__ __forceinline__ Pair add_products(Pair a, Pair b) {
+  float a0, a1, b0, b1;
+  halves(a, a0, a1);
+  halves(b, b0, b1);
+  return pair(__fadd_rn(a0, b0), __fadd_rn(a1, b1));
+}
+
 // The step of a block and the stores of everything it changes.
 template <int BITS>
 __device__ __forceinline__ void update(const StepArgs& a, const Block& b, float gs, float* p, const float* gr,
@@ -189,8 +198,8 @@ __device__ __forceinline__ void update(const StepArgs& a, const Block& b, float 
 #pragma unroll
   for (int i = 0; i < 8; i += 2) {
     const Pair g2 = mul2(pair(gr[i], gr[i + 1]), both(gs));
-    const Pair m2 = add2(mul2(both(a.b1), pair(m[i], m[i + 1])), mul2(both(a.omb1), g2));
-    const Pair v2 = add2(mul2(both(a.b2), pair(v[i], v[i + 1])), mul2(mul2(both(a.omb2), g2), g2));
+    const Pair m2 = add_products(mul2(both(a.b1), pair(m[i], m[i + 1])), mul2(both(a.omb1), g2));
+    const Pair v2 = add_products(mul2(both(a.b2), pair(v[i], v[i + 1])), mul2(mul2(both(a.omb2), g2), g2));
     const Pair r2 = sqrt_near(v2);
     float da, db;
     halves(fma2(r2, both(a.inv_c2), both(a.eps)), da, db);

@@ -498,6 +498,44 @@ def test_adamw_8(sizes, grad):
                 assert (got[(y == 0)] == 0).all()
 
 
+def codes_of(a, seed=None):
+    """The 8-bit form of blocks of 256 fp32 values in elementary operations, each rounded to fp32."""
+    most = a.abs().amax(1, keepdim=True)
+    most = torch.where(most < 1e-30, 0.0, most)
+    x = torch.where(most > 0, a * (most.reciprocal() * 448.0), 0.0)
+    if seed is not None:
+        j = (torch.arange(a.numel(), device="cuda") + (seed & 0xFFFFFFFF) * 0xBB67AE85) & 0xFFFFFFFF
+        j = (j * 0x9E3779B9) & 0xFFFFFFFF
+        j = ((j ^ (j >> 15)) * 0x6A09E667) & 0xFFFFFFFF
+        r = ((j ^ (j >> 13)) >> 12).int().view(a.shape)
+        low = torch.where(x < 2.0 ** -6, 2.0 ** -6, 0.0)
+        t = (((x + low).view(torch.int32) + r) & ~0xFFFFF).view(torch.float32) - low
+        x = torch.where(x > 0, t.clamp(min=2.0 ** -9), 0.0)
+    return x.clamp(-448.0, 448.0).to(torch.float8_e4m3fn), most[:, 0] * (1.0 / 448.0)
+
+
+def test_adamw_8_to_the_bit():
+    # every code and scale equals that of the formula evaluated operation by operation in fp32: no
+    # operations are contracted, and the square root is the rounded one
+    g = gen(91)
+    n = 256 * 20000
+    p = randn(g, n)
+    o = ops.AdamW([p], bits=8)
+    scale = torch.tensor([0.7], device="cuda")
+    for t in range(1, 4):
+        gr = randn(g, n, dtype=BF, std=1e-3)
+        m = o.m.float().view(-1, 256) * o.m_scale[:, None]
+        r = o.root.float().view(-1, 256) * o.root_scale[:, None]
+        v = r * r
+        x = gr.float().view(-1, 256) * scale
+        m = 0.9 * m + (1 - 0.9) * x
+        v = 0.999 * v + (1 - 0.999) * x * x
+        o.step([gr], lr=1e-3, grad_scale=scale, seed=t * 77)
+        for (code, s), got, got_s in ((codes_of(m), o.m, o.m_scale), (codes_of(v.sqrt(), t * 77), o.root, o.root_scale)):
+            assert torch.equal(got.view(torch.uint8), code.view(-1).view(torch.uint8))
+            assert torch.equal(got_s, s)
+
+
 def test_adamw_8_random_rounding_keeps_the_mean_and_repeats():
     n = 256 * 400
     p = torch.zeros(n, device="cuda")
