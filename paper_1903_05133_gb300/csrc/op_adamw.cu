@@ -461,10 +461,8 @@ cudaError_t launch_range(const hier_avg_adamw* h, const void* const* grads, int 
     k_adamw32<G, NG><<<static_cast<unsigned>(c1 - c0), kThreads, 0, s>>>(g, a);
   } else {
     constexpr int smem = kThreads / 32 * kWarpBytes<G>;
-    cudaError_t e = cudaFuncSetAttribute(k_adamw8<G, NG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e == cudaSuccess)
-      e = cudaFuncSetAttribute(k_adamw8<G, NG>, cudaFuncAttributePreferredSharedMemoryCarveout,
-                               cudaSharedmemCarveoutMaxShared);
+    static bool allowed[kMaxDevices];
+    const cudaError_t e = allow_smem(k_adamw8<G, NG>, smem, allowed);
     if (e != cudaSuccess) return e;
     // as many CTAs as the SMs hold at once, since they take the chunks in turn
     const int64_t held = kSms * (227 * 1024 / (smem + 1024) < 4 ? 227 * 1024 / (smem + 1024) : 4);

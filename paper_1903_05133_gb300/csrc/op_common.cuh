@@ -14,6 +14,23 @@ namespace ha {
 __host__ __device__ constexpr int type_size(int type) { return type == HA_TYPE_FP32 ? 4 : 2; }
 inline bool type_ok(int type) { return type >= HA_TYPE_FP32 && type <= HA_TYPE_FP16; }
 
+// The current device's slot of a table that keeps, for each kernel, what was found out or set
+// once for it (-1: no device).
+constexpr int kMaxDevices = 16;
+inline int device_slot() {
+  int d = -1;
+  return cudaGetDevice(&d) == cudaSuccess && d < kMaxDevices ? d : -1;
+}
+// Allows the kernel `bytes` of dynamic shared memory, once a device.
+template <typename K>
+cudaError_t allow_smem(K kernel, int bytes, bool (&done)[kMaxDevices]) {
+  const int d = device_slot();
+  if (d >= 0 && done[d]) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && d >= 0) done[d] = true;
+  return e;
+}
+
 template <typename T> struct Elem;
 template <> struct Elem<float> {
   static __device__ __forceinline__ float up(float x) { return x; }

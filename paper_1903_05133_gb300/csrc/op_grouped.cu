@@ -878,7 +878,8 @@ template <int MODE, bool FOLD, int NT>
 int launch_one(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int64_t tiles, int64_t most, cudaStream_t s) {
   const auto kernel = k_grouped_one<MODE, FOLD, NT>;
   constexpr int smem = One<NT>::kSmem;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return HA_ECUDA;
+  static bool allowed[kMaxDevices];
+  if (allow_smem(kernel, smem, allowed) != cudaSuccess) return HA_ECUDA;
   // CTAs a tile: as many as fill the GPU, with at least kMinChunks chunks each (one row, 4096 ->
   // 4096: 18.2 us with one CTA a tile).
   static int held[4] = {0, 0, 0, 0};
@@ -908,9 +909,8 @@ int launch_one(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int6
 template <int MODE, bool FOLD>
 int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& ta_head, const CUtensorMap& tb_head,
                 const Args& a, int64_t most, cudaStream_t s) {
-  if (cudaFuncSetAttribute(k_grouped_pair<MODE, FOLD>, cudaFuncAttributeMaxDynamicSharedMemorySize, Pair::kSmem) !=
-      cudaSuccess)
-    return HA_ECUDA;
+  static bool allowed[kMaxDevices];
+  if (allow_smem(k_grouped_pair<MODE, FOLD>, Pair::kSmem, allowed) != cudaSuccess) return HA_ECUDA;
   // As many pairs as the GPU holds at once (its clusters of two leave some SMs out): the tiles
   // are dealt out in advance, so a pair that started late would finish late.
   static int held = 0;

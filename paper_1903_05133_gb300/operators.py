@@ -21,7 +21,7 @@ from ._lib import c_int64, c_void_p, check
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 FORWARD, DX, DW = 0, 1, 2
-_SHAPE, _DTYPE, _CUDA = attrgetter("shape"), attrgetter("dtype"), attrgetter("is_cuda")
+_KIND = attrgetter("dtype", "shape", "is_cuda")
 _ADDRESS, _CONTIGUOUS = torch.Tensor.data_ptr, torch.Tensor.is_contiguous
 BLOCK = 256                     # elements that share a scale of the 8-bit AdamW states
 MAX_TOP = 32
@@ -356,7 +356,7 @@ class AdamW:
             self.h, self._table.data_ptr(), table.value, self.m.data_ptr(), second.data_ptr(),
             self.m_scale.data_ptr() if bits == 8 else None,
             self.root_scale.data_ptr() if bits == 8 else None, s), "adamw_bind")
-        self._shapes = [p.shape for p in params]
+        self._kinds = {d: [(d, p.shape, True) for p in params] for d in TYPES}
 
     def step(self, grads: Sequence[torch.Tensor], lr: float, grad_scale: Optional[torch.Tensor] = None,
              seed: Optional[int] = None, stream=None) -> None:
@@ -365,9 +365,7 @@ class AdamW:
         (the step's number when None); the same seed gives the same step."""
         # each check runs over all tensors at once: a call over hundreds of them is host work
         kind = grads[0].dtype if grads else None
-        if not (list(map(_SHAPE, grads)) == self._shapes and kind in TYPES and
-                set(map(_DTYPE, grads)) == {kind} and all(map(_CONTIGUOUS, grads)) and
-                set(map(_CUDA, grads)) == {True}):
+        if not (kind in TYPES and list(map(_KIND, grads)) == self._kinds[kind] and all(map(_CONTIGUOUS, grads))):
             raise ValueError("grads must be one contiguous CUDA tensor for each of the params, of its "
                              "shape, all of them fp32, bf16 or fp16")
         a = array("Q", map(_ADDRESS, grads))
