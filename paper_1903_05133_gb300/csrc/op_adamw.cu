@@ -24,9 +24,8 @@ namespace ha {
 namespace {
 
 constexpr int kBlock = 256;         // elements that share a scale: one warp, 8 a lane
-constexpr int kChunk = 2048;        // elements of one CTA: a block for each warp
-constexpr int kThreads = 256;
-constexpr int kSms = 152;
+constexpr int kChunk = 1024;        // elements of one CTA: a block for each warp
+constexpr int kThreads = 128;
 constexpr float kTop = 448.0f;      // largest e4m3 value
 constexpr float kTiny = 1e-30f;     // a block whose largest magnitude is below is stored as 0
 
@@ -136,38 +135,37 @@ __device__ __forceinline__ float warp_abs_max(float a) {
   return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(a) & 0x7FFFFFFFu));
 }
 
-// A warp's block of 256 elements, 8 a lane: two groups of four consecutive ones, so that every
-// load and store of a warp is contiguous.
+// A warp's block of 256 elements, 8 a lane.  32-bit states: two groups of four consecutive
+// ones, so that every 16-byte access of a warp is contiguous.  8-bit states: 8 consecutive ones,
+// which takes half the instructions for the narrow arrays.
 struct Block {
   const Chunk& c;
   int b0;              // first element of the block in the chunk
   int64_t s0;          // and in the state arrays
   bool full;           // whole, and aligned for wide accesses
 };
-
-template <typename G>
-__device__ __forceinline__ bool is_wide(const Chunk& c, const G* g) {
-  return ((reinterpret_cast<uintptr_t>(c.p) & 15) | (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(G) - 1)) |
-          (reinterpret_cast<uintptr_t>(c.copy) & 7)) == 0;
+template <int BITS>
+__device__ __forceinline__ int element(int i) {           // of the lane's i-th in the block
+  const int lane = threadIdx.x & 31;
+  return BITS == 32 ? (i >> 2) * 128 + lane * 4 + (i & 3) : lane * 8 + i;
 }
 
-template <typename G>
-__device__ __forceinline__ void load_pg(const Block& b, const G* g, float* p, float* gr) {
-  const int lane = threadIdx.x & 31;
+template <int BITS, typename G>
+__device__ __forceinline__ bool is_wide(const Chunk& c, const G* g) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(c.p), q = reinterpret_cast<uintptr_t>(g),
+                  r = reinterpret_cast<uintptr_t>(c.copy);
+  if (BITS == 32) return ((p & 15) | (q & (4 * sizeof(G) - 1)) | (r & 7)) == 0;
+  return ((p & 31) | (q & 15) | (r & 15)) == 0;
+}
+
+// One by one, where a block is short or not aligned.
+template <int BITS, typename G>
+__device__ __forceinline__ void load_single(const Block& b, const G* g, float* p, float* gr) {
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const int e = b.b0 + q * 128 + lane * 4;
-    if (b.full) {
-      const float4 f = __ldcs(reinterpret_cast<const float4*>(b.c.p + e));
-      p[4 * q] = f.x; p[4 * q + 1] = f.y; p[4 * q + 2] = f.z; p[4 * q + 3] = f.w;
-      load_grad4<G>(g + e, gr + 4 * q);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        p[4 * q + i] = e + i < b.c.n ? b.c.p[e + i] : 0.0f;
-        gr[4 * q + i] = e + i < b.c.n ? Elem<G>::up(g[e + i]) : 0.0f;
-      }
-    }
+  for (int i = 0; i < 8; ++i) {
+    const int e = b.b0 + element<BITS>(i);
+    p[i] = e < b.c.n ? b.c.p[e] : 0.0f;
+    gr[i] = e < b.c.n ? Elem<G>::up(g[e]) : 0.0f;
   }
 }
 
@@ -178,6 +176,12 @@ __device__ __forceinline__ Pair add_products(Pair a, Pair b) {
   halves(a, a0, a1);
   halves(b, b0, b1);
   return pair(__fadd_rn(a0, b0), __fadd_rn(a1, b1));
+}
+
+__device__ __forceinline__ void store_256(float* to, const float* x) {
+  asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "f"(x[0]), "f"(x[1]),
+               "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7])
+               : "memory");
 }
 
 // The step of a block and the stores of everything it changes.
@@ -214,32 +218,38 @@ __device__ __forceinline__ void update(const StepArgs& a, const Block& b, float 
       r_top = max_nan(r_top, max_nan(root[i], root[i + 1]));
     }
   }
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const int e = b0 + q * 128 + lane * 4;
-    const float* x = p + 4 * q;
-    if (full) {
-      __stcs(reinterpret_cast<float4*>(c.p + e), make_float4(x[0], x[1], x[2], x[3]));
-      if (c.copy) {
-        uint2 w;
-        if (a.copy_type == HA_TYPE_BF16)
-          w = make_uint2(narrow2<__nv_bfloat16>(x[0], x[1]), narrow2<__nv_bfloat16>(x[2], x[3]));
-        else
-          w = make_uint2(narrow2<__half>(x[0], x[1]), narrow2<__half>(x[2], x[3]));
-        __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(c.copy) + e), w);
-      }
-    } else {
+  if (full) {
+    uint32_t w[4];
+    if (c.copy) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (e + i < c.n) {
-          c.p[e + i] = x[i];
-          if (c.copy) {
-            if (a.copy_type == HA_TYPE_BF16)
-              static_cast<__nv_bfloat16*>(c.copy)[e + i] = __float2bfloat16_rn(x[i]);
-            else
-              static_cast<__half*>(c.copy)[e + i] = __float2half_rn(x[i]);
-          }
-        }
+        w[i] = a.copy_type == HA_TYPE_BF16 ? narrow2<__nv_bfloat16>(p[2 * i], p[2 * i + 1])
+                                           : narrow2<__half>(p[2 * i], p[2 * i + 1]);
+    }
+    uint16_t* copy = static_cast<uint16_t*>(c.copy);
+    if constexpr (BITS == 32) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int e = b0 + q * 128 + lane * 4;
+        __stcs(reinterpret_cast<float4*>(c.p + e), make_float4(p[4 * q], p[4 * q + 1], p[4 * q + 2], p[4 * q + 3]));
+        if (copy) __stcs(reinterpret_cast<uint2*>(copy + e), make_uint2(w[2 * q], w[2 * q + 1]));
+      }
+    } else {
+      store_256(c.p + b0 + lane * 8, p);
+      if (copy) __stcs(reinterpret_cast<uint4*>(copy + b0 + lane * 8), make_uint4(w[0], w[1], w[2], w[3]));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int e = b0 + element<BITS>(i);
+      if (e >= c.n) continue;
+      c.p[e] = p[i];
+      if (c.copy) {
+        if (a.copy_type == HA_TYPE_BF16)
+          static_cast<__nv_bfloat16*>(c.copy)[e] = __float2bfloat16_rn(p[i]);
+        else
+          static_cast<__half*>(c.copy)[e] = __float2half_rn(p[i]);
+      }
     }
   }
   uint32_t m8[2], r8[2];
@@ -257,15 +267,15 @@ __device__ __forceinline__ void update(const StepArgs& a, const Block& b, float 
       halves(mul2(pair(root[i], root[i + 1]), both(ri)), root[i], root[i + 1]);
       least = fminf(least, fminf(root[i], root[i + 1]));
     }
-    const uint32_t j = static_cast<uint32_t>(s0) + lane * 4;
+    const uint32_t j = static_cast<uint32_t>(s0) + lane * 8;
     if (__all_sync(~0u, least >= 0.015625f)) {       // nearly always: no value below 2^-6
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        root[i] = round_random_normal(root[i], random20(j + (i >> 2) * 128 + (i & 3), a.seed));
+        root[i] = round_random_normal(root[i], random20(j + i, a.seed));
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        root[i] = round_random(root[i], random20(j + (i >> 2) * 128 + (i & 3), a.seed));
+        root[i] = round_random(root[i], random20(j + i, a.seed));
     }
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
@@ -277,34 +287,45 @@ __device__ __forceinline__ void update(const StepArgs& a, const Block& b, float 
       a.v_scale[s0 / kBlock] = r_top * (1.0f / kTop);
     }
   }
+  if constexpr (BITS == 32) {
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const int64_t s = s0 + q * 128 + lane * 4;
-    if constexpr (BITS == 32) {
+    for (int q = 0; q < 2; ++q) {
+      const int64_t s = s0 + q * 128 + lane * 4;
       __stcs(reinterpret_cast<float4*>(static_cast<float*>(a.m) + s),
              make_float4(m[4 * q], m[4 * q + 1], m[4 * q + 2], m[4 * q + 3]));
       __stcs(reinterpret_cast<float4*>(static_cast<float*>(a.v) + s),
              make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
-    } else {
-      __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.m) + s), m8[q]);
-      __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v) + s), r8[q]);
     }
+  } else {
+    const int64_t s = s0 + lane * 8;
+    __stcs(reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.m) + s), make_uint2(m8[0], m8[1]));
+    __stcs(reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.v) + s), make_uint2(r8[0], r8[1]));
   }
 }
 
-// States of 32 bits: one CTA a chunk.  The stream of 30 bytes an element keeps the memory busy
+// One CTA a chunk.  States of 32 bits: the stream of 30 bytes an element keeps the memory busy
 // by itself (71.4 M elements with a 16-bit copy: 304 us, 7.0 TB/s).
 template <typename G, int NG>
-__global__ void __launch_bounds__(kThreads, 5) k_adamw32(const __grid_constant__ Grads<NG> grads,
+__global__ void __launch_bounds__(kThreads, 10) k_adamw32(const __grid_constant__ Grads<NG> grads,
                                                          const __grid_constant__ StepArgs a) {
   const Chunk c = a.chunks[blockIdx.x];
   const G* g = static_cast<const G*>(grads.p[c.tensor - a.first_tensor]) + c.grad;
   const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
   const int lane = threadIdx.x & 31, b0 = (threadIdx.x >> 5) * kBlock;
   if (b0 >= c.n) return;
-  const Block b = {c, b0, c.state + b0, is_wide(c, g) && b0 + kBlock <= c.n};
+  const Block b = {c, b0, c.state + b0, is_wide<32>(c, g) && b0 + kBlock <= c.n};
   float p[8], gr[8], m[8], v[8];
-  load_pg(b, g, p, gr);
+  if (b.full) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int e = b0 + q * 128 + lane * 4;
+      const float4 f = __ldcs(reinterpret_cast<const float4*>(c.p + e));
+      p[4 * q] = f.x; p[4 * q + 1] = f.y; p[4 * q + 2] = f.z; p[4 * q + 3] = f.w;
+      load_grad4<G>(g + e, gr + 4 * q);
+    }
+  } else {
+    load_single<32>(b, g, p, gr);
+  }
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
     const int64_t s = b.s0 + q * 128 + lane * 4;
@@ -316,116 +337,46 @@ __global__ void __launch_bounds__(kThreads, 5) k_adamw32(const __grid_constant__
   update<32>(a, b, gs, p, gr, m, v);
 }
 
-// States of 8 bits: half the bytes and twice the arithmetic, so a warp's loads have to run
-// ahead of its arithmetic.  CTAs stay and take chunks in turn; each warp keeps the loads of its
-// next kAhead blocks under way into shared memory (asynchronous copies hold no registers), and
-// the chunks' descriptions three blocks ahead of those.  (One CTA a chunk, as above: 949 us for
-// 285 M elements with a 16-bit copy, the warps waiting for loads most of the time.)
-constexpr int kAhead = 3;
-constexpr int kRecs = 8;              // descriptions kept: 2 * kAhead and the current one
-template <typename G> constexpr int kSlot = 1024 + 256 * sizeof(G) + 512 + 16;
-template <typename G> constexpr int kWarpBytes = kAhead * kSlot<G> + kRecs * static_cast<int>(sizeof(Chunk));
-static_assert(sizeof(Chunk) == 48, "three copies of 16 bytes");
-
-template <int N>
-__device__ __forceinline__ void copy_async(void* to, const void* from) {
-  const uint32_t d = static_cast<uint32_t>(__cvta_generic_to_shared(to));
-  if constexpr (N == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(from) : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(d), "l"(from), "n"(N) : "memory");
+// States of 8 bits: half the bytes and twice the arithmetic.  Small CTAs in the order of the
+// memory, many of them at once (285 M elements with bf16 gradients and a bf16 copy: 693 us, 6.6
+// TB/s; CTAs of 256 threads 710; CTAs that stay and take every 608th chunk, with loads three
+// blocks ahead in shared memory, 831: they drift apart, and the memory's pages with them).
+__device__ __forceinline__ void load_256(float* x, const float* from) {
+  asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7])
+               : "l"(from));
 }
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
 template <typename G, int NG>
-__global__ void __launch_bounds__(kThreads, 4) k_adamw8(const __grid_constant__ Grads<NG> grads,
-                                                        const __grid_constant__ StepArgs a, int chunks) {
-  extern __shared__ __align__(16) unsigned char dyn[];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b0 = warp * kBlock;
-  unsigned char* slots = dyn + warp * kWarpBytes<G>;
-  Chunk* recs = reinterpret_cast<Chunk*>(slots + kAhead * kSlot<G>);
+__global__ void __launch_bounds__(kThreads, 10) k_adamw8(const __grid_constant__ Grads<NG> grads,
+                                                        const __grid_constant__ StepArgs a) {
+  const Chunk c = a.chunks[blockIdx.x];
+  const G* g = static_cast<const G*>(grads.p[c.tensor - a.first_tensor]) + c.grad;
   const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
-  auto chunk_at = [&](int k) { return static_cast<int64_t>(blockIdx.x) + static_cast<int64_t>(k) * gridDim.x; };
-  auto grad_of = [&](const Chunk& c) { return static_cast<const G*>(grads.p[c.tensor - a.first_tensor]) + c.grad; };
-  auto fetch_rec = [&](int k) {
-    if (chunk_at(k) < chunks && lane < 3)
-      copy_async<16>(reinterpret_cast<unsigned char*>(&recs[k % kRecs]) + lane * 16,
-                     reinterpret_cast<const unsigned char*>(&a.chunks[chunk_at(k)]) + lane * 16);
-  };
-  auto fetch = [&](int k) {
-    if (chunk_at(k) >= chunks) return;
-    const Chunk& c = recs[k % kRecs];
-    if (b0 >= c.n) return;
-    unsigned char* slot = slots + k % kAhead * kSlot<G>;
-    const G* g = grad_of(c);
-    const int64_t s0 = c.state + b0;
-    const bool full = is_wide(c, g) && b0 + kBlock <= c.n;
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int e = q * 128 + lane * 4;
-      if (full) {
-        copy_async<16>(slot + e * 4, c.p + b0 + e);
-        copy_async<4 * sizeof(G)>(slot + 1024 + e * sizeof(G), g + b0 + e);
-      }
-      copy_async<4>(slot + 1024 + 256 * sizeof(G) + e, static_cast<const uint8_t*>(a.m) + s0 + e);
-      copy_async<4>(slot + 1024 + 256 * sizeof(G) + 256 + e, static_cast<const uint8_t*>(a.v) + s0 + e);
-    }
-    if (lane < 2)
-      copy_async<4>(slot + 1024 + 256 * sizeof(G) + 512 + lane * 4, (lane ? a.v_scale : a.m_scale) + s0 / kBlock);
-  };
-  for (int k = 0; k < 2 * kAhead; ++k) fetch_rec(k);
-  copy_commit();
-  copy_wait<0>();
-  __syncwarp();
-  for (int k = 0; k < kAhead; ++k) {
-    fetch(k);
-    copy_commit();
+  const int lane = threadIdx.x & 31, b0 = (threadIdx.x >> 5) * kBlock;
+  if (b0 >= c.n) return;
+  const Block b = {c, b0, c.state + b0, is_wide<8>(c, g) && b0 + kBlock <= c.n};
+  float p[8], gr[8], m[8], v[8];
+  const uint2 mc = __ldcs(reinterpret_cast<const uint2*>(static_cast<uint8_t*>(a.m) + b.s0 + lane * 8));
+  const uint2 rc = __ldcs(reinterpret_cast<const uint2*>(static_cast<uint8_t*>(a.v) + b.s0 + lane * 8));
+  const float ms = a.m_scale[b.s0 / kBlock], vs = a.v_scale[b.s0 / kBlock];
+  if (b.full) {
+    load_256(p, c.p + b0 + lane * 8);
+    load_grad4<G>(g + b0 + lane * 8, gr);
+    load_grad4<G>(g + b0 + lane * 8 + 4, gr + 4);
+  } else {
+    load_single<8>(b, g, p, gr);
   }
-  for (int k = 0; chunk_at(k) < chunks; ++k) {
-    copy_wait<kAhead - 1>();
-    __syncwarp();
-    const Chunk c = recs[k % kRecs];
-    const G* g = grad_of(c);
-    const Block b = {c, b0, c.state + b0, is_wide(c, g) && b0 + kBlock <= c.n};
-    const unsigned char* slot = slots + k % kAhead * kSlot<G>;
-    float p[8], gr[8], m[8], v[8];
-    const bool any = b0 < c.n;
-    if (any) {
-      if (b.full) {
+  from_e4m3x4(mc.x, m);
+  from_e4m3x4(mc.y, m + 4);
+  from_e4m3x4(rc.x, v);
+  from_e4m3x4(rc.y, v + 4);
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const int e = q * 128 + lane * 4;
-          const float4 f = *reinterpret_cast<const float4*>(slot + e * 4);
-          p[4 * q] = f.x; p[4 * q + 1] = f.y; p[4 * q + 2] = f.z; p[4 * q + 3] = f.w;
-          load_grad4<G>(reinterpret_cast<const G*>(slot + 1024) + e, gr + 4 * q);
-        }
-      } else {
-        load_pg(b, g, p, gr);
-      }
-      const unsigned char* codes = slot + 1024 + 256 * sizeof(G);
-      const float ms = *reinterpret_cast<const float*>(codes + 512), vs = *reinterpret_cast<const float*>(codes + 516);
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        from_e4m3x4(*reinterpret_cast<const uint32_t*>(codes + q * 128 + lane * 4), m + 4 * q);
-        from_e4m3x4(*reinterpret_cast<const uint32_t*>(codes + 256 + q * 128 + lane * 4), v + 4 * q);
-      }
-#pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        halves(mul2(pair(m[i], m[i + 1]), pair(ms, ms)), m[i], m[i + 1]);
-        const Pair r2 = mul2(pair(v[i], v[i + 1]), pair(vs, vs));
-        halves(mul2(r2, r2), v[i], v[i + 1]);
-      }
-    }
-    __syncwarp();                     // the slot is read; its next block may come
-    fetch_rec(k + 2 * kAhead);
-    fetch(k + kAhead);
-    copy_commit();
-    if (any) update<8>(a, b, gs, p, gr, m, v);
+  for (int i = 0; i < 8; i += 2) {
+    halves(mul2(pair(m[i], m[i + 1]), pair(ms, ms)), m[i], m[i + 1]);
+    const Pair r2 = mul2(pair(v[i], v[i + 1]), pair(vs, vs));
+    halves(mul2(r2, r2), v[i], v[i + 1]);
   }
+  update<8>(a, b, gs, p, gr, m, v);
 }
 
 }  // namespace
@@ -460,14 +411,7 @@ cudaError_t launch_range(const hier_avg_adamw* h, const void* const* grads, int 
   if constexpr (BITS == 32) {
     k_adamw32<G, NG><<<static_cast<unsigned>(c1 - c0), kThreads, 0, s>>>(g, a);
   } else {
-    constexpr int smem = kThreads / 32 * kWarpBytes<G>;
-    static bool allowed[kMaxDevices];
-    const cudaError_t e = allow_smem(k_adamw8<G, NG>, smem, allowed);
-    if (e != cudaSuccess) return e;
-    // as many CTAs as the SMs hold at once, since they take the chunks in turn
-    const int64_t held = kSms * (227 * 1024 / (smem + 1024) < 4 ? 227 * 1024 / (smem + 1024) : 4);
-    k_adamw8<G, NG><<<static_cast<unsigned>(c1 - c0 < held ? c1 - c0 : held), kThreads, smem, s>>>(
-        g, a, static_cast<int>(c1 - c0));
+    k_adamw8<G, NG><<<static_cast<unsigned>(c1 - c0), kThreads, 0, s>>>(g, a);
   }
   return cudaGetLastError();
 }
