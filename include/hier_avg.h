@@ -14,8 +14,8 @@
  *     must keep them alive while work that uses them is in flight.
  *   - All compute calls are asynchronous on the CUDA stream given to them (or
  *     bound to the handle); a NULL stream is the legacy default stream.  Only
- *     hier_avg_losses, hier_avg_check, hier_avg_round_host and the profile read
- *     synchronise.
+ *     hier_avg_losses, hier_avg_check, hier_avg_operator_check, hier_avg_round_host
+ *     and the profile read synchronise.
  *   - No call changes the calling thread's current CUDA device: a call that runs
  *     work on the handle's device makes it current and restores the caller's.
  *   - Every call returns HA_OK (0) or a negative status; nothing aborts.

@@ -87,7 +87,6 @@ struct Table {
   int* off;         // rows of each group, inside [0, rows]
   int* first;       // first tile of each group
 };
-constexpr int kTableBytes = 2 * (kMaxGroups + 1) * 4;
 
 // The list of tiles, by all threads; ends with a CTA barrier.
 template <int MODE, int M, int NT>
@@ -947,6 +946,7 @@ int rows_product(Operand x, Operand w, Args a, void* ws, int64_t ws_bytes, cudaS
   // group: 24.5 us by pairs).
   const bool few = rows <= kFewRows * static_cast<int64_t>(a.groups);
   const bool small = m2 * std::max<int64_t>(used, (rows + kPairCols - 1) / kPairCols) < kSmallTiles;
+  if (m1 * std::min<int64_t>(rows, a.groups + rows / 32) > 0x7FFFFFFF) return HA_EUNSUPPORTED;    // tiles
   CUtensorMap ta, tb;
   if (!make_map(&ta, w, a.in_type, 64, MODE == kFwd ? 128 : 64) ||
       !make_map(&tb, x, a.in_type, 64, few || small ? 16 : 64))
