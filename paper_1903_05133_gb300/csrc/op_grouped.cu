@@ -27,6 +27,7 @@ constexpr int kK = 64;                  // values summed over in a chunk: one 12
 constexpr int kMaxGroups = 1024;
 constexpr int kEpiWarps = 8;            // two groups of four: a group reads half the columns
 constexpr int kThreads = (kEpiWarps + 2) * 32;          // results, loads, products
+constexpr int kDwThreads = kThreads + 32;               // and the ends of groups
 constexpr int kPairCols = 256;          // columns of a tile of two CTAs
 constexpr int kMinChunks = 8;           // of each of the CTAs that share a tile
 constexpr int kMaxSplit = 8;            // CTAs that share a tile's summed length
@@ -89,10 +90,10 @@ struct Table {
 };
 
 // The list of tiles, by all threads; ends with a CTA barrier.
-template <int MODE, int M, int NT>
+template <int MODE, int M, int NT, int THREADS>
 __device__ __forceinline__ void make_table(const Table& s, const Args& a) {
   const int tid = threadIdx.x, lane = tid & 31;
-  for (int g = tid; g <= a.groups; g += kThreads) s.off[g] = min(max(a.offsets[g], 0), a.rows);
+  for (int g = tid; g <= a.groups; g += THREADS) s.off[g] = min(max(a.offsets[g], 0), a.rows);
   __syncthreads();
   if (tid < 32) {
     const int mt = (a.m + M - 1) / M, nt = (a.n + NT - 1) / NT + (MODE == kDw && a.db ? 1 : 0);
@@ -328,6 +329,16 @@ struct Ring {
       round ^= 1;
     }
   }
+  __device__ __forceinline__ void skip(int n) {
+    const uint32_t to = st + static_cast<uint32_t>(n);
+    st = to % STAGES;
+    round ^= (to / STAGES) & 1;
+  }
+  __device__ __forceinline__ Ring after(int n) const {      // n < STAGES
+    Ring r = {st + n, round};
+    if (r.st >= STAGES) r = {r.st - STAGES, r.round ^ 1};
+    return r;
+  }
   __device__ __forceinline__ uint32_t next_st() const { return st + 1 == STAGES ? 0 : st + 1; }
   __device__ __forceinline__ uint32_t next_round() const { return st + 1 == STAGES ? round ^ 1 : round; }
 };
@@ -475,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_barrier_init();
   }
   tc_fence_before();
-  make_table<MODE, kM, NT>(tab, a);
+  make_table<MODE, kM, NT, kThreads>(tab, a);
   if (split > 1) cluster_arrive();                        // the barriers are set up
   Tiles<MODE, kM, NT, 16> list(tab, a);
   tc_fence_after();
@@ -640,13 +651,13 @@ struct Pair {
 static_assert(2 * kRowsStage == kEpiWarps * kWarpStage, "one buffer serves both kinds of results");
 
 template <int MODE, bool FOLD>
-__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
+__global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __cluster_dims__(2, 1, 1)
     k_grouped_pair(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
-                   const __grid_constant__ CUtensorMap ta_head, const __grid_constant__ CUtensorMap tb_head,
                    const __grid_constant__ Args a) {
   extern __shared__ unsigned char raw[];
-  // full: the first CTA's, on which both CTAs' loads are counted.  tempty: the first CTA's too.
-  __shared__ uint64_t full[Pair::kStages], empty[Pair::kStages], tfull[2], tempty[2];
+  // full: the first CTA's, on which both CTAs' loads and two arrivals are counted.  tempty: the
+  // first CTA's too.  tail: this CTA's load of a chunk in which a group ends.
+  __shared__ uint64_t full[Pair::kStages], empty[Pair::kStages], tfull[2], tempty[2], tail[Pair::kStages];
   __shared__ uint32_t tmem_at;
   __shared__ int table[2 * (kMaxGroups + 1)];
   const Table tab = {table, table + kMaxGroups + 1};
@@ -662,8 +673,9 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
   }
   if (tid == 0) {
     for (int i = 0; i < Pair::kStages; ++i) {
-      mbar_init(&full[i], 1);
+      mbar_init(&full[i], 2);
       mbar_init(&empty[i], 1);
+      mbar_init(&tail[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&tfull[i], 1);
@@ -673,11 +685,11 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
   }
   if (MODE == kDw && a.db) {
     const uint32_t one = a.in_type == HA_TYPE_BF16 ? 0x3F803F80u : 0x3C003C00u;
-    for (int i = tid; i < Pair::kOnes / 4; i += kThreads) reinterpret_cast<uint32_t*>(Ones)[i] = one;
+    for (int i = tid; i < Pair::kOnes / 4; i += kDwThreads) reinterpret_cast<uint32_t*>(Ones)[i] = one;
     fence_proxy_async();
   }
   tc_fence_before();
-  make_table<MODE, 2 * kM, kPairCols>(tab, a);
+  make_table<MODE, 2 * kM, kPairCols, MODE == kDw ? kDwThreads : kThreads>(tab, a);
   Tiles<MODE, 2 * kM, kPairCols, 32> list(tab, a);
   cluster_sync_all();
   tc_fence_after();
@@ -702,25 +714,27 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
         for (int c = 0; c < nk; ++c, at.next()) {
           const int st = at.st, k = c * kK;
           if (!peek && !mbar_wait_hot(&empty[st], at.round ^ 1, &g_operator_error)) { ok = false; break; }
-          const uint32_t bar = full0 + st * 8, armed = rank == 0 ? 2 * bytes : 0;
+          // dW: the rows that fill no chunk, a group's last, are loaded first, and seen first by the
+          // warp that clears what follows them.
+          const bool cut = MODE == kDw && c == 0 && t.k % kK != 0;
+          const uint32_t bar = cut ? smem_u32(&tail[st]) : full0 + st * 8;
+          uint64_t* arm = cut ? &tail[st] : &full[st];
+          const uint32_t armed = cut ? bytes : rank == 0 ? 2 * bytes : 0;
+          if (!cut && rank == 0) mbar_arrive(&full[st]);
           unsigned char* A = As + st * Pair::kA;
           unsigned char* B = Bs + st * Pair::kB;
           uint64_t* next = &empty[at.next_st()];
           const uint32_t parity = at.next_round() ^ 1;
           if (MODE == kFwd) {
-            peek = tma_chunk_pair<false, false>(A, &ta, k, m0, t.g, B, &tb, k, t.r0 + h0, 0, boxes, bar, &full[st], armed,
+            peek = tma_chunk_pair<false, false>(A, &ta, k, m0, t.g, B, &tb, k, t.r0 + h0, 0, boxes, bar, arm, armed,
                                                 next, parity);
           } else if (MODE == kDx) {
-            peek = tma_chunk_pair<true, false>(A, &ta, m0, k, t.g, B, &tb, k, t.r0 + h0, 0, boxes, bar, &full[st], armed,
+            peek = tma_chunk_pair<true, false>(A, &ta, m0, k, t.g, B, &tb, k, t.r0 + h0, 0, boxes, bar, arm, armed,
                                                next, parity);
           } else {
-            // A group's rows that fill no chunk come first, as the first ones of a window that
-            // starts with the group, loaded from a row before it on: zeros, then the rows.
-            const int odd = t.k % kK, row = odd ? t.r0 + odd - kK + k : t.r0 + k;
-            const bool first = c == 0 && odd != 0;
-            peek = tma_chunk_pair<true, true>(A, first ? &ta_head : &ta, m0, first ? odd - kK : row, first ? t.r0 : 0, B,
-                                              first ? &tb_head : &tb, t.c0 + h0, first ? odd - kK : row, first ? t.r0 : 0,
-                                              boxes, bar, &full[st], armed, next, parity);
+            const int row = t.r0 + (cut ? (nk - 1) * kK : t.k % kK != 0 ? k - kK : k);
+            peek = tma_chunk_pair<true, true>(A, &ta, m0, row, 0, B, &tb, t.c0 + h0, row, 0, boxes, bar, arm, armed, next,
+                                              parity);
           }
         }
       }
@@ -738,35 +752,75 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
         const int fold = FOLD || t.bias ? kFold : 1 << 30;
         const uint32_t idesc = idesc_of(a.in_type, 2 * kM, N) | (MODE == kFwd ? 0u : 1u << 15) |
                                (MODE == kDw ? 1u << 16 : 0u);
+        // Chunks in their order, but one that is cut (dW's first) third: clearing takes longer than
+        // the loads are ahead (32 ragged groups of 4096 -> 4096: 527 us with it waited for).
+        const int odd = t.k % kK;
+        const bool cut = MODE == kDw && odd != 0;
+        const Ring<Pair::kStages> at0 = at;
+        auto nth = [&](int q) { return !cut || q > 2 ? q : q + 1 < nk && q < 2 ? q + 1 : 0; };
         int part = 0;                                       // chunks since the last fold
-        for (int c = 0; c < nk; ++c, at.next()) {
-          const int st = at.st, buf = seg & 1;
-          ok = (part != 0 || mbar_wait_hot(&tempty[buf], ((seg >> 1) & 1) ^ 1, &g_operator_error)) &&
-               (peek || mbar_wait_hot(&full[st], at.round, &g_operator_error));
+        for (int q = 0; q < nk; ++q, at.next()) {
+          const int c = nth(q), buf = seg & 1;
+          const Ring<Pair::kStages> me = c == q ? at : at0.after(c);
+          const int st = me.st;
+          ok = part != 0 || mbar_wait_hot(&tempty[buf], ((seg >> 1) & 1) ^ 1, &g_operator_error);
+          if (ok && cut && c == 0)                          // the other CTA has written there
+            ok = mbar_wait_cluster(&full[st], me.round, &g_operator_error);
+          else if (ok && !peek)
+            ok = mbar_wait_hot(&full[st], me.round, &g_operator_error);
           if (!ok) break;
           tc_fence_after();
-          // the values of an incomplete chunk: the last ones (dW) or the first
-          const int odd = t.k % kK;
-          const int steps = odd && c == (MODE == kDw ? 0 : nk - 1) ? (odd + 15) / 16 : 4, skip = MODE == kDw ? 4 - steps : 0;
+          const int steps = odd && c == (MODE == kDw ? 0 : nk - 1) ? (odd + 15) / 16 : 4;
           const uint32_t as = smem_u32(As + st * Pair::kA), bs = smem_u32(t.bias ? Ones : Bs + st * Pair::kB);
           const uint32_t d = tmem + buf * kPairCols;
+          const uint64_t da = MODE == kFwd ? umma_desc_sw128(as) : umma_desc_sw128_mn(as, 8192);
+          const uint64_t db = MODE == kDw ? umma_desc_sw128_mn(bs, 8192) : umma_desc_sw128(bs);
           constexpr int SA = MODE == kFwd ? 2 : 128, SB = MODE == kDw ? 128 : 2;   // 16 values further
-          const uint64_t da = (MODE == kFwd ? umma_desc_sw128(as) : umma_desc_sw128_mn(as, 8192)) + skip * SA;
-          const uint64_t db = (MODE == kDw ? umma_desc_sw128_mn(bs, 8192) : umma_desc_sw128(bs)) + skip * SB;
           if (steps == 4) {
-            peek = tc_chunk_pair<SA, SB>(d, da, db, idesc, part != 0, &empty[st], &full[at.next_st()], at.next_round());
+            // the next chunk's barrier; at a tile's end the next tile's first, if it is taken in order
+            const int cn = q + 1 < nk ? nth(q + 1) : nk;
+            Ring<Pair::kStages> to = at;
+            to.next();
+            if (cn != q + 1 && q + 1 < nk) to = at0.after(cn);
+            peek = tc_chunk_pair<SA, SB>(d, da, db, idesc, part != 0, &empty[st], &full[to.st], to.round);
+            if (MODE == kDw && q + 1 == nk) peek = false;
           } else {
             for (int k = 0; k < steps; ++k) tc_mma_pair(d, da + k * SA, db + k * SB, idesc, part || k ? 1u : 0u);
             tc_commit_pair(&empty[st]);
             peek = false;
           }
-          if (++part == fold || c == nk - 1) {
+          if (++part == fold || q == nk - 1) {
             tc_commit_pair(&tfull[buf]);
             ++seg;
             part = 0;
           }
         }
       }
+    }
+  } else if (MODE == kDw && warp == kEpiWarps + 2) {
+    // ---- the ends of groups, in both CTAs: the rows after a group's last are another group's,
+    // and are cleared up to the products' next step of 16
+    Ring<Pair::kStages> at;
+    uint32_t parity = 0;                                    // of each stage's `tail`
+    for (int i = pair; i < tiles; i += pairs) {
+      const Tile t = list.at(i);
+      const int left = t.k % kK, st = at.st;
+      at.skip((t.k + kK - 1) / kK);
+      if (!left) continue;
+      bool ok = true;
+      if (lane == 0) ok = mbar_wait_hot(&tail[st], parity >> st & 1, &g_operator_error);
+      if (!__all_sync(~0u, ok)) break;
+      parity ^= 1u << st;
+      const int blocks = 2 + (t.bias ? 0 : ((t.cols + 31) / 32 * 16 + 63) / 64);
+      const int n = (left + 15) / 16 * 16 - left;
+      for (int x = lane; x < blocks * n * 8; x += 32) {
+        const int line = x >> 3, b = line / n, row = left + line % n;
+        unsigned char* p = b < 2 ? As + st * Pair::kA + b * 8192 : Bs + st * Pair::kB + (b - 2) * 8192;
+        *reinterpret_cast<uint4*>(p + row * 128 + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_release_cluster(cluster_addr(&full[st], 0));
     }
   } else {
     // ---- results, by both CTAs
@@ -856,10 +910,10 @@ bool make_map(CUtensorMap* m, const Operand& o, int type, uint32_t b0, uint32_t 
 
 // Clusters of `size` CTAs that the GPU holds at once.
 template <typename K>
-int clusters_held(K kernel, int smem, int size) {
+int clusters_held(K kernel, int threads, int smem, int size) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(kSms / size * size);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -887,7 +941,7 @@ int launch_one(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int6
     split *= 2;
     ++log;
   }
-  if (held[log] == 0) held[log] = split == 1 ? kSms : clusters_held(kernel, smem, split);
+  if (held[log] == 0) held[log] = split == 1 ? kSms : clusters_held(kernel, kThreads, smem, split);
   if (held[log] < 1) return HA_ECUDA;
   const int64_t clusters = std::min<int64_t>(held[log], std::max<int64_t>(most, 1));
   cudaLaunchConfig_t cfg = {};
@@ -906,17 +960,17 @@ int launch_one(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int6
 }
 
 template <int MODE, bool FOLD>
-int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& ta_head, const CUtensorMap& tb_head,
-                const Args& a, int64_t most, cudaStream_t s) {
+int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int64_t most, cudaStream_t s) {
   static bool allowed[kMaxDevices];
   if (allow_smem(k_grouped_pair<MODE, FOLD>, Pair::kSmem, allowed) != cudaSuccess) return HA_ECUDA;
   // As many pairs as the GPU holds at once (its clusters of two leave some SMs out): the tiles
   // are dealt out in advance, so a pair that started late would finish late.
+  constexpr int threads = MODE == kDw ? kDwThreads : kThreads;
   static int held = 0;
-  if (held == 0) held = clusters_held(k_grouped_pair<MODE, FOLD>, Pair::kSmem, 2);
+  if (held == 0) held = clusters_held(k_grouped_pair<MODE, FOLD>, threads, Pair::kSmem, 2);
   if (held < 1) return HA_ECUDA;
   const int64_t pairs = std::min<int64_t>(held, std::max<int64_t>(most, 1));
-  k_grouped_pair<MODE, FOLD><<<static_cast<unsigned>(2 * pairs), kThreads, Pair::kSmem, s>>>(ta, tb, ta_head, tb_head, a);
+  k_grouped_pair<MODE, FOLD><<<static_cast<unsigned>(2 * pairs), threads, Pair::kSmem, s>>>(ta, tb, a);
   return cudaGetLastError() == cudaSuccess ? HA_OK : HA_ECUDA;
 }
 
@@ -962,8 +1016,7 @@ int rows_product(Operand x, Operand w, Args a, void* ws, int64_t ws_bytes, cudaS
                 : launch_one<MODE, false, 64>(ta, tb, a, tiles, most, s);
   }
   const int64_t most = m2 * std::min<int64_t>(rows, a.groups + rows / kPairCols);
-  return fold ? launch_pair<MODE, true>(ta, tb, ta, tb, a, most, s)
-              : launch_pair<MODE, false>(ta, tb, ta, tb, a, most, s);
+  return fold ? launch_pair<MODE, true>(ta, tb, a, most, s) : launch_pair<MODE, false>(ta, tb, a, most, s);
 }
 
 }  // namespace
@@ -1088,18 +1141,13 @@ extern "C" int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, co
   const int es = type_size(dw_type);
   a.wide_out = (reinterpret_cast<uintptr_t>(dw_dev) & 15) == 0 && dw_ld * es % 16 == 0 && inner * es % 16 == 0 &&
                (groups == 1 || dw_gs * es % 16 == 0);
-  // Windows of 64 rows, one for each row that may begin a group.  (The last ones reach past the
-  // tensor; only rows of a group are asked for.)
-  auto windows = [](const Operand& o) { return Operand{o.p, o.rows, kK, o.cols, o.ld, o.ld}; };
-  CUtensorMap ta, tb, ta_head, tb_head;
-  if (!make_map(&ta, dy, type, 64, 64) || !make_map(&tb, x, type, 64, 64) ||
-      !make_map(&ta_head, windows(dy), type, 64, 64) || !make_map(&tb_head, windows(x), type, 64, 64))
-    return HA_ECUDA;
+  CUtensorMap ta, tb;
+  if (!make_map(&ta, dy, type, 64, 64) || !make_map(&tb, x, type, 64, 64)) return HA_ECUDA;
   const int64_t most = groups * static_cast<int64_t>((outer + 2 * kM - 1) / (2 * kM)) *
                        ((inner + kPairCols - 1) / kPairCols + (db_dev ? 1 : 0));
   if (most > 0x7FFFFFFF) return HA_EUNSUPPORTED;
-  return dw_type == HA_TYPE_FP32 ? launch_pair<kDw, true>(ta, tb, ta_head, tb_head, a, most, s)
-                                 : launch_pair<kDw, false>(ta, tb, ta_head, tb_head, a, most, s);
+  return dw_type == HA_TYPE_FP32 ? launch_pair<kDw, true>(ta, tb, a, most, s)
+                                 : launch_pair<kDw, false>(ta, tb, a, most, s);
 }
 
 extern "C" int hier_avg_operator_check(void* stream) {
