@@ -256,32 +256,33 @@ __device__ __forceinline__ void emit_rows(const Args& a, const float* v, int row
 // A warp holds 32 features (rows of dW, one a lane) of 32 columns at a time.  Rows of 128
 // bytes are put together in shared memory (16-byte pieces swapped by the row, against bank
 // conflicts), and eight lanes store a row.  (32 groups of 512 rows, 4096 x 4096, 16 bits: lanes
-// storing their own rows 500 us, bulk stores of boxes with 64-byte rows 409 us.)  Where dW's rows
-// are not aligned for that, lanes store their values.
+// storing their own rows 500 us, bulk stores of boxes with 64-byte rows 409, this 376.)  Rows
+// that are not aligned for that leave value by value, side by side.
 constexpr int kWarpStage = 4096;
 __device__ __forceinline__ void emit_weights(const Args& a, const float* v, int g, int f0, int c, int end,
                                              unsigned char* stage) {
   const int lane = threadIdx.x & 31;
-  if (a.wide_out) {
-    const bool wide = a.out_type == HA_TYPE_FP32;
-    const int half = wide ? 0 : (c >> 5) & 1;             // which 32 of a 16-bit row's 64 columns
+  const bool wide = a.out_type == HA_TYPE_FP32;
+  const int half = wide ? 0 : (c >> 5) & 1;               // which 32 of a 16-bit row's 64 columns
 #pragma unroll
-    for (int p = 0; p < 8; ++p) {
-      if (!wide && p >= 4) break;
-      uint4 w;
-      if (wide)
-        w = make_uint4(__float_as_uint(v[4 * p]), __float_as_uint(v[4 * p + 1]), __float_as_uint(v[4 * p + 2]),
-                       __float_as_uint(v[4 * p + 3]));
-      else
-        w = make_uint4(narrow_pair(v[8 * (p & 3)], v[8 * (p & 3) + 1], a.out_type),
-                       narrow_pair(v[8 * (p & 3) + 2], v[8 * (p & 3) + 3], a.out_type),
-                       narrow_pair(v[8 * (p & 3) + 4], v[8 * (p & 3) + 5], a.out_type),
-                       narrow_pair(v[8 * (p & 3) + 6], v[8 * (p & 3) + 7], a.out_type));
-      *reinterpret_cast<uint4*>(stage + lane * 128 + (((half * 4 + p) ^ (lane & 7)) << 4)) = w;
-    }
-    if (!wide && half == 0 && c + 32 < end) return;       // the row's other half comes next
-    __syncwarp();
-    const int es = wide ? 4 : 2, piece = lane & 7, col = c - half * 32 + piece * (16 / es);
+  for (int p = 0; p < 8; ++p) {
+    if (!wide && p >= 4) break;
+    uint4 w;
+    if (wide)
+      w = make_uint4(__float_as_uint(v[4 * p]), __float_as_uint(v[4 * p + 1]), __float_as_uint(v[4 * p + 2]),
+                     __float_as_uint(v[4 * p + 3]));
+    else
+      w = make_uint4(narrow_pair(v[8 * (p & 3)], v[8 * (p & 3) + 1], a.out_type),
+                     narrow_pair(v[8 * (p & 3) + 2], v[8 * (p & 3) + 3], a.out_type),
+                     narrow_pair(v[8 * (p & 3) + 4], v[8 * (p & 3) + 5], a.out_type),
+                     narrow_pair(v[8 * (p & 3) + 6], v[8 * (p & 3) + 7], a.out_type));
+    *reinterpret_cast<uint4*>(stage + lane * 128 + (((half * 4 + p) ^ (lane & 7)) << 4)) = w;
+  }
+  if (!wide && half == 0 && c + 32 < end) return;         // the row's other half comes next
+  __syncwarp();
+  const int c0 = c - half * 32;
+  if (a.wide_out) {
+    const int es = wide ? 4 : 2, piece = lane & 7, col = c0 + piece * (16 / es);
     if (col < end) {
       unsigned char* o = static_cast<unsigned char*>(a.out) +
                          (g * a.out_gs + static_cast<int64_t>(f0 + (lane >> 3)) * a.out_ld + col) * es;
@@ -293,20 +294,24 @@ __device__ __forceinline__ void emit_weights(const Args& a, const float* v, int 
               *reinterpret_cast<const uint4*>(stage + row * 128 + ((piece ^ (row & 7)) << 4));
       }
     }
-    __syncwarp();
-    return;
-  }
-  const int f = f0 + lane;
-  if (f >= a.m) return;
-  const int64_t at = g * a.out_gs + f * a.out_ld + c;
+  } else {
+    const int rows = min(32, a.m - f0);
+    for (int row = 0; row < rows; ++row) {
+      const int64_t at = g * a.out_gs + static_cast<int64_t>(f0 + row) * a.out_ld + c0 + lane;
+      if (wide) {
+        if (c0 + lane < end)
+          static_cast<float*>(a.out)[at] =
+              *reinterpret_cast<const float*>(stage + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4);
+      } else {
 #pragma unroll
-  for (int x = 0; x < 32; ++x)
-    if (c + x < end) {
-      if (a.out_type == HA_TYPE_FP32)
-        static_cast<float*>(a.out)[at + x] = v[x];
-      else
-        static_cast<uint16_t*>(a.out)[at + x] = narrow(v[x], a.out_type);
+        for (int h = 0; h < 2; ++h)
+          if (c0 + h * 32 + lane < end)
+            static_cast<uint16_t*>(a.out)[at + h * 32] = *reinterpret_cast<const uint16_t*>(
+                stage + row * 128 + (((h * 4 + (lane >> 3)) ^ (row & 7)) << 4) + (lane & 7) * 2);
+      }
     }
+  }
+  __syncwarp();
 }
 
 // A warp's wait for sums, by one lane: 32 lanes asking keep the barrier unit from the roles
@@ -333,11 +338,6 @@ struct Ring {
     const uint32_t to = st + static_cast<uint32_t>(n);
     st = to % STAGES;
     round ^= (to / STAGES) & 1;
-  }
-  __device__ __forceinline__ Ring after(int n) const {      // n < STAGES
-    Ring r = {st + n, round};
-    if (r.st >= STAGES) r = {r.st - STAGES, r.round ^ 1};
-    return r;
   }
   __device__ __forceinline__ uint32_t next_st() const { return st + 1 == STAGES ? 0 : st + 1; }
   __device__ __forceinline__ uint32_t next_round() const { return st + 1 == STAGES ? round ^ 1 : round; }
@@ -752,22 +752,12 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
         const int fold = FOLD || t.bias ? kFold : 1 << 30;
         const uint32_t idesc = idesc_of(a.in_type, 2 * kM, N) | (MODE == kFwd ? 0u : 1u << 15) |
                                (MODE == kDw ? 1u << 16 : 0u);
-        // Chunks in their order, but one that is cut (dW's first) third: clearing takes longer than
-        // the loads are ahead (32 ragged groups of 4096 -> 4096: 527 us with it waited for).
         const int odd = t.k % kK;
-        const bool cut = MODE == kDw && odd != 0;
-        const Ring<Pair::kStages> at0 = at;
-        auto nth = [&](int q) { return !cut || q > 2 ? q : q + 1 < nk && q < 2 ? q + 1 : 0; };
         int part = 0;                                       // chunks since the last fold
-        for (int q = 0; q < nk; ++q, at.next()) {
-          const int c = nth(q), buf = seg & 1;
-          const Ring<Pair::kStages> me = c == q ? at : at0.after(c);
-          const int st = me.st;
-          ok = part != 0 || mbar_wait_hot(&tempty[buf], ((seg >> 1) & 1) ^ 1, &g_operator_error);
-          if (ok && cut && c == 0)                          // the other CTA has written there
-            ok = mbar_wait_cluster(&full[st], me.round, &g_operator_error);
-          else if (ok && !peek)
-            ok = mbar_wait_hot(&full[st], me.round, &g_operator_error);
+        for (int c = 0; c < nk; ++c, at.next()) {
+          const int st = at.st, buf = seg & 1;
+          ok = (part != 0 || mbar_wait_hot(&tempty[buf], ((seg >> 1) & 1) ^ 1, &g_operator_error)) &&
+               (peek || mbar_wait_hot(&full[st], at.round, &g_operator_error));
           if (!ok) break;
           tc_fence_after();
           const int steps = odd && c == (MODE == kDw ? 0 : nk - 1) ? (odd + 15) / 16 : 4;
@@ -777,19 +767,13 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
           const uint64_t db = MODE == kDw ? umma_desc_sw128_mn(bs, 8192) : umma_desc_sw128(bs);
           constexpr int SA = MODE == kFwd ? 2 : 128, SB = MODE == kDw ? 128 : 2;   // 16 values further
           if (steps == 4) {
-            // the next chunk's barrier; at a tile's end the next tile's first, if it is taken in order
-            const int cn = q + 1 < nk ? nth(q + 1) : nk;
-            Ring<Pair::kStages> to = at;
-            to.next();
-            if (cn != q + 1 && q + 1 < nk) to = at0.after(cn);
-            peek = tc_chunk_pair<SA, SB>(d, da, db, idesc, part != 0, &empty[st], &full[to.st], to.round);
-            if (MODE == kDw && q + 1 == nk) peek = false;
+            peek = tc_chunk_pair<SA, SB>(d, da, db, idesc, part != 0, &empty[st], &full[at.next_st()], at.next_round());
           } else {
             for (int k = 0; k < steps; ++k) tc_mma_pair(d, da + k * SA, db + k * SB, idesc, part || k ? 1u : 0u);
             tc_commit_pair(&empty[st]);
             peek = false;
           }
-          if (++part == fold || q == nk - 1) {
+          if (++part == fold || c == nk - 1) {
             tc_commit_pair(&tfull[buf]);
             ++seg;
             part = 0;
@@ -811,16 +795,17 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
       if (lane == 0) ok = mbar_wait_hot(&tail[st], parity >> st & 1, &g_operator_error);
       if (!__all_sync(~0u, ok)) break;
       parity ^= 1u << st;
-      const int blocks = 2 + (t.bias ? 0 : ((t.cols + 31) / 32 * 16 + 63) / 64);
-      const int n = (left + 15) / 16 * 16 - left;
-      for (int x = lane; x < blocks * n * 8; x += 32) {
-        const int line = x >> 3, b = line / n, row = left + line % n;
-        unsigned char* p = b < 2 ? As + st * Pair::kA + b * 8192 : Bs + st * Pair::kB + (b - 2) * 8192;
-        *reinterpret_cast<uint4*>(p + row * 128 + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
+      // a lane has one or two of the 16-byte columns of the (at most four) blocks
+      const int columns = 8 * (2 + (t.bias ? 0 : ((t.cols + 31) / 32 * 16 + 63) / 64));
+      for (int x = lane; x < columns; x += 32) {
+        const int b = x >> 3;
+        unsigned char* p = (b < 2 ? As + st * Pair::kA + b * 8192 : Bs + st * Pair::kB + (b - 2) * 8192) + (x & 7) * 16;
+        for (int row = left; row & 15; ++row) *reinterpret_cast<uint4*>(p + row * 128) = make_uint4(0, 0, 0, 0);
       }
-      fence_proxy_async();
+      // Each CTA's tensor core reads its own shared memory, where the fence has ordered the zeros.
+      fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive_release_cluster(cluster_addr(&full[st], 0));
+      if (lane == 0) mbar_arrive_cluster(cluster_addr(&full[st], 0));
     }
   } else {
     // ---- results, by both CTAs
@@ -847,13 +832,32 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
 }
 
 // Rows of 16-bit values to a pitch of whole 16-byte vectors, for operands that a tensor
-// map cannot describe (an odd width, stride or address).
+// map cannot describe (an odd width, stride or address).  A thread makes a vector from loads of
+// the type W, as wide as the rows' alignment allows.
+template <typename W>
 __global__ void __launch_bounds__(256) k_pack(const uint16_t* src, int64_t rows, int64_t per_group,
-                                              int64_t cols, int64_t ld, int64_t gs, uint16_t* dst,
-                                              int64_t pitch) {
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    const uint16_t* s = src + r / per_group * gs + r % per_group * ld;
-    for (int64_t c = threadIdx.x; c < pitch; c += 256) dst[r * pitch + c] = c < cols ? s[c] : 0;
+                                              int cols, int64_t ld, int64_t gs, uint4* dst, int pitch8) {
+  constexpr int N = sizeof(W) / 2;
+  const int64_t all = rows * pitch8;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
+    const int64_t r = i / pitch8;
+    const int c = static_cast<int>(i - r * pitch8) * 8;
+    const uint16_t* s = src + r / per_group * gs + r % per_group * ld + c;
+    uint4 out = make_uint4(0, 0, 0, 0);
+    uint16_t* o = reinterpret_cast<uint16_t*>(&out);
+#pragma unroll
+    for (int e = 0; e < 8; e += N) {
+      if (c + e + N <= cols) {
+        const W w = *reinterpret_cast<const W*>(s + e);
+#pragma unroll
+        for (int x = 0; x < N; ++x) o[e + x] = reinterpret_cast<const uint16_t*>(&w)[x];
+      } else {
+#pragma unroll
+        for (int x = 0; x < N; ++x)
+          if (c + e + x < cols) o[e + x] = s[e + x];
+      }
+    }
+    dst[i] = out;
   }
 }
 
@@ -880,10 +884,14 @@ struct Operand {
 cudaError_t pack(Operand& o, unsigned char*& ws, cudaStream_t s) {
   if (o.fits()) return cudaSuccess;
   const int64_t pitch = round8(o.cols), rows = o.groups * o.rows;
-  uint16_t* dst = reinterpret_cast<uint16_t*>(ws);
+  uint4* dst = reinterpret_cast<uint4*>(ws);
   ws += o.packed_bytes();
-  k_pack<<<static_cast<unsigned>(std::min<int64_t>(rows, 8 * kSms)), 256, 0, s>>>(
-      static_cast<const uint16_t*>(o.p), rows, o.rows, o.cols, o.ld, o.gs, dst, pitch);
+  const uintptr_t low = reinterpret_cast<uintptr_t>(o.p) | static_cast<uintptr_t>(o.ld * 2) |
+                        static_cast<uintptr_t>(o.groups > 1 ? o.gs * 2 : 0);
+  const unsigned grid = static_cast<unsigned>(std::min<int64_t>((rows * pitch / 8 + 255) / 256, 16 * kSms));
+  const auto kernel = (low & 7) == 0 ? k_pack<uint2> : (low & 3) == 0 ? k_pack<uint32_t> : k_pack<uint16_t>;
+  kernel<<<grid, 256, 0, s>>>(static_cast<const uint16_t*>(o.p), rows, o.rows, static_cast<int>(o.cols), o.ld, o.gs, dst,
+                              static_cast<int>(pitch / 8));
   o.p = dst;
   o.ld = pitch;
   o.gs = o.rows * pitch;
