@@ -186,8 +186,15 @@ __device__ __forceinline__ void emit_rows(const Args& a, const float* v, int row
     if (j >= rows) return;                                // the same for the whole warp group
     unsigned char* buf = stage + (turn++ & 1) * 8192;
     uint4 hv[R * S / 128];
-    if (MODE == kDx && a.h) {
-      // the mask's values are asked for before the barrier
+    // the mask's values are asked for before the barrier
+    if (MODE == kDx && a.h && !a.wide_out) {
+      uint32_t* p = &hv[0].x;                             // two rows' a word
+      const uint16_t* h = static_cast<const uint16_t*>(a.h) + static_cast<int64_t>(row0 + j) * a.h_ld + m0 + et;
+      const int n = m0 + et < a.m ? rows - j : 0;
+#pragma unroll
+      for (int x = 0; x < R; x += 2)
+        p[x / 2] = (x < n ? h[x * a.h_ld] : 0u) | (x + 1 < n ? static_cast<uint32_t>(h[(x + 1) * a.h_ld]) << 16 : 0u);
+    } else if (MODE == kDx && a.h) {
 #pragma unroll
       for (int x = 0; x < R * S / 128; ++x) {
         const int i = et + x * 128, r = i / S, e = m0 + i % S * P;
@@ -221,6 +228,21 @@ __device__ __forceinline__ void emit_rows(const Args& a, const float* v, int row
         reinterpret_cast<uint16_t*>(buf)[x * kM + feature] = narrow(f, a.out_type);
     }
     named_barrier_sync(bar, 128);
+    if (!a.wide_out) {
+      // rows that are not aligned for vectors: a thread a feature, so that a row's leave side by
+      // side (2 groups, 4249 rows, 258 -> 1087, bf16: 25 us; a vector's features by one thread, 37)
+      OUT* o = static_cast<OUT*>(a.out) + static_cast<int64_t>(row0 + j) * a.out_ld + m0 + et;
+      const int n = m0 + et < a.m ? rows - j : 0;
+      const uint32_t* p = &hv[0].x;
+#pragma unroll
+      for (int x = 0; x < R; ++x)
+        if (x < n) {
+          OUT w = reinterpret_cast<const OUT*>(buf)[x * kM + et];
+          if (MODE == kDx && a.h && !positive16(p[x / 2] >> (16 * (x & 1)) & 0xFFFFu, a.in_type)) w = 0;
+          o[x * a.out_ld] = w;
+        }
+      continue;
+    }
 #pragma unroll
     for (int x = 0; x < R * S / 128; ++x) {
       const int i = et + x * 128, r = i / S, e = m0 + i % S * P;
@@ -240,7 +262,7 @@ __device__ __forceinline__ void emit_rows(const Args& a, const float* v, int row
         }
       }
       OUT* o = static_cast<OUT*>(a.out) + static_cast<int64_t>(row0 + j + r) * a.out_ld + e;
-      if (a.wide_out && e + P <= a.m) {
+      if (e + P <= a.m) {
         *reinterpret_cast<uint4*>(o) = w;
       } else {
         const OUT* p = reinterpret_cast<const OUT*>(&w);
@@ -832,32 +854,60 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
 }
 
 // Rows of 16-bit values to a pitch of whole 16-byte vectors, for operands that a tensor
-// map cannot describe (an odd width, stride or address).  A thread makes a vector from loads of
-// the type W, as wide as the rows' alignment allows.
+// map cannot describe (an odd width, stride or address).  A thread makes a vector from loads as
+// wide as the rows' alignment allows, and goes on `step` vectors further: that is sg groups, sr
+// rows and sc vectors, so that no place is divided for again.  One launch for both operands.
+struct Pack {
+  const uint16_t* src;
+  uint4* dst;
+  int64_t all, step, ld, gs, per_group, sg, sr;
+  int cols, pitch8, sc, bytes;                            // bytes of a load
+};
+struct Packs {
+  Pack of[2];
+  int blocks;                                             // of the first
+};
 template <typename W>
-__global__ void __launch_bounds__(256) k_pack(const uint16_t* src, int64_t rows, int64_t per_group,
-                                              int cols, int64_t ld, int64_t gs, uint4* dst, int pitch8) {
+__device__ __forceinline__ uint4 pack_vector(const uint16_t* s, int left) {
   constexpr int N = sizeof(W) / 2;
-  const int64_t all = rows * pitch8;
-  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
-    const int64_t r = i / pitch8;
-    const int c = static_cast<int>(i - r * pitch8) * 8;
-    const uint16_t* s = src + r / per_group * gs + r % per_group * ld + c;
-    uint4 out = make_uint4(0, 0, 0, 0);
-    uint16_t* o = reinterpret_cast<uint16_t*>(&out);
+  uint4 out = make_uint4(0, 0, 0, 0);
+  uint16_t* o = reinterpret_cast<uint16_t*>(&out);
 #pragma unroll
-    for (int e = 0; e < 8; e += N) {
-      if (c + e + N <= cols) {
-        const W w = *reinterpret_cast<const W*>(s + e);
+  for (int e = 0; e < 8; e += N) {
+    if (e + N <= left) {
+      const W w = *reinterpret_cast<const W*>(s + e);
 #pragma unroll
-        for (int x = 0; x < N; ++x) o[e + x] = reinterpret_cast<const uint16_t*>(&w)[x];
-      } else {
+      for (int x = 0; x < N; ++x) o[e + x] = reinterpret_cast<const uint16_t*>(&w)[x];
+    } else {
 #pragma unroll
-        for (int x = 0; x < N; ++x)
-          if (c + e + x < cols) o[e + x] = s[e + x];
-      }
+      for (int x = 0; x < N; ++x)
+        if (e + x < left) o[e + x] = s[e + x];
     }
-    dst[i] = out;
+  }
+  return out;
+}
+__global__ void __launch_bounds__(256) k_pack(const __grid_constant__ Packs both) {
+  const int second = static_cast<int>(blockIdx.x) >= both.blocks;
+  const Pack a = both.of[second];
+  int64_t i = (blockIdx.x - (second ? both.blocks : 0)) * 256ll + threadIdx.x, r = i / a.pitch8, g = r / a.per_group;
+  int v = static_cast<int>(i - r * a.pitch8);
+  r -= g * a.per_group;
+  for (; i < a.all; i += a.step) {
+    const uint16_t* s = a.src + g * a.gs + r * a.ld + v * 8;
+    const int left = a.cols - v * 8;
+    a.dst[i] = a.bytes == 8 ? pack_vector<uint2>(s, left)
+               : a.bytes == 4 ? pack_vector<uint32_t>(s, left) : pack_vector<uint16_t>(s, left);
+    v += a.sc;
+    r += a.sr;
+    g += a.sg;
+    if (v >= a.pitch8) {
+      v -= a.pitch8;
+      ++r;
+    }
+    if (r >= a.per_group) {
+      r -= a.per_group;
+      ++g;
+    }
   }
 }
 
@@ -881,20 +931,40 @@ struct Operand {
   int64_t packed_bytes() const { return fits() ? 0 : round256(groups * rows * round8(cols) * 2); }
 };
 
-cudaError_t pack(Operand& o, unsigned char*& ws, cudaStream_t s) {
-  if (o.fits()) return cudaSuccess;
-  const int64_t pitch = round8(o.cols), rows = o.groups * o.rows;
-  uint4* dst = reinterpret_cast<uint4*>(ws);
-  ws += o.packed_bytes();
-  const uintptr_t low = reinterpret_cast<uintptr_t>(o.p) | static_cast<uintptr_t>(o.ld * 2) |
-                        static_cast<uintptr_t>(o.groups > 1 ? o.gs * 2 : 0);
-  const unsigned grid = static_cast<unsigned>(std::min<int64_t>((rows * pitch / 8 + 255) / 256, 16 * kSms));
-  const auto kernel = (low & 7) == 0 ? k_pack<uint2> : (low & 3) == 0 ? k_pack<uint32_t> : k_pack<uint16_t>;
-  kernel<<<grid, 256, 0, s>>>(static_cast<const uint16_t*>(o.p), rows, o.rows, static_cast<int>(o.cols), o.ld, o.gs, dst,
-                              static_cast<int>(pitch / 8));
-  o.p = dst;
-  o.ld = pitch;
-  o.gs = o.rows * pitch;
+// Copies those of two operands that do not fit to ws, which moves on.
+cudaError_t pack(Operand& x, Operand& y, unsigned char*& ws, cudaStream_t s) {
+  Packs p = {};
+  int count = 0;
+  unsigned blocks[2] = {0, 0};
+  for (Operand* o : {&x, &y}) {
+    if (o->fits()) continue;
+    const int64_t pitch = round8(o->cols);
+    Pack& a = p.of[count];
+    a.src = static_cast<const uint16_t*>(o->p);
+    a.dst = reinterpret_cast<uint4*>(ws);
+    a.cols = static_cast<int>(o->cols);
+    a.pitch8 = static_cast<int>(pitch / 8);
+    a.ld = o->ld;
+    a.gs = o->gs;
+    a.per_group = o->rows;
+    a.all = o->groups * o->rows * a.pitch8;
+    blocks[count] = static_cast<unsigned>(std::min<int64_t>((a.all + 255) / 256, 16 * kSms));
+    a.step = blocks[count] * 256ll;
+    a.sc = static_cast<int>(a.step % a.pitch8);
+    a.sr = a.step / a.pitch8 % o->rows;
+    a.sg = a.step / a.pitch8 / o->rows;
+    const uintptr_t low = reinterpret_cast<uintptr_t>(o->p) | static_cast<uintptr_t>(o->ld * 2) |
+                          static_cast<uintptr_t>(o->groups > 1 ? o->gs * 2 : 0);
+    a.bytes = (low & 7) == 0 ? 8 : (low & 3) == 0 ? 4 : 2;
+    ++count;
+    ws += o->packed_bytes();
+    o->p = a.dst;
+    o->ld = pitch;
+    o->gs = o->rows * pitch;
+  }
+  if (count == 0) return cudaSuccess;
+  p.blocks = static_cast<int>(blocks[0]);
+  k_pack<<<blocks[0] + blocks[1], 256, 0, s>>>(p);
   return cudaGetLastError();
 }
 
@@ -997,7 +1067,7 @@ int rows_product(Operand x, Operand w, Args a, void* ws, int64_t ws_bytes, cudaS
   if (x.packed_bytes() + w.packed_bytes() > ws_bytes) return HA_ENOMEM;
   if (ws_bytes > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 15))) return HA_EINVAL;
   unsigned char* p = static_cast<unsigned char*>(ws);
-  if (pack(x, p, s) != cudaSuccess || pack(w, p, s) != cudaSuccess) return HA_ECUDA;
+  if (pack(x, w, p, s) != cudaSuccess) return HA_ECUDA;
   a.wide_out = (reinterpret_cast<uintptr_t>(a.out) & 15) == 0 && a.out_ld * type_size(a.out_type) % 16 == 0;
   a.wide_h = a.h && (reinterpret_cast<uintptr_t>(a.h) & 15) == 0 && a.h_ld % 8 == 0;
   const bool fold = a.out_type == HA_TYPE_FP32;
@@ -1132,7 +1202,7 @@ extern "C" int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, co
   if (workspace_bytes > 0 && (!workspace_dev || (reinterpret_cast<uintptr_t>(workspace_dev) & 15)))
     return HA_EINVAL;
   unsigned char* p = static_cast<unsigned char*>(workspace_dev);
-  if (pack(dy, p, s) != cudaSuccess || pack(x, p, s) != cudaSuccess) return HA_ECUDA;
+  if (pack(dy, x, p, s) != cudaSuccess) return HA_ECUDA;
   Args a = {};
   a.offsets = offsets_dev;
   a.out = dw_dev;
