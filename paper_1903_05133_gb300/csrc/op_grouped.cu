@@ -46,6 +46,7 @@ struct Args {
   int64_t out_ld, out_gs;     // in elements; out_gs: between groups of dW
   int64_t bias_ld, h_ld;      // bias_ld: db's too
   int groups, rows;
+  int split;                  // dW: parts of a group's rows, each a group of its own here
   int m, n, k;                // features; dW: columns; summed length (forward, rows)
   int in_type, out_type;
   int relu;
@@ -93,7 +94,17 @@ struct Table {
 template <int MODE, int M, int NT, int THREADS>
 __device__ __forceinline__ void make_table(const Table& s, const Args& a) {
   const int tid = threadIdx.x, lane = tid & 31;
-  for (int g = tid; g <= a.groups; g += THREADS) s.off[g] = min(max(a.offsets[g], 0), a.rows);
+  for (int g = tid; g <= a.groups; g += THREADS) {
+    const int of = MODE == kDw ? g / a.split : g, part = MODE == kDw ? g - of * a.split : 0;
+    int low = min(max(a.offsets[of], 0), a.rows);
+    if (part > 0) {
+      // the parts are whole chunks of rows, but for the group's last
+      const int n = max(0, min(max(a.offsets[of + 1], 0), a.rows) - low);
+      const int64_t size = ((n + kK - 1) / kK + a.split - 1) / a.split * static_cast<int64_t>(kK);
+      low += static_cast<int>(min(static_cast<int64_t>(n), part * size));
+    }
+    s.off[g] = low;
+  }
   __syncthreads();
   if (tid < 32) {
     const int mt = (a.m + M - 1) / M, nt = (a.n + NT - 1) / NT + (MODE == kDw && a.db ? 1 : 0);
@@ -911,6 +922,51 @@ __global__ void __launch_bounds__(256) k_pack(const __grid_constant__ Packs both
   }
 }
 
+// A split weights' gradient: dW and db are the sums of their parts, in the parts' order.
+struct Join {
+  const float *part, *part_db;      // [groups, split, outer, pitch] and [groups, split, outer]
+  void* out;
+  float* db;
+  int64_t out_ld, out_gs, db_ld;
+  int groups, split, outer, inner, pitch, type;
+};
+__global__ void __launch_bounds__(256) k_join(const Join a) {
+  const int quads = a.pitch / 4;
+  const int64_t all = static_cast<int64_t>(a.groups) * a.outer * quads, step = gridDim.x * 256ll;
+  const int64_t slice = static_cast<int64_t>(a.outer) * a.pitch;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += step) {
+    const int64_t row = i / quads, g = row / a.outer;
+    const int f = static_cast<int>(row - g * a.outer), c = static_cast<int>(i - row * quads) * 4;
+    const float* p = a.part + g * a.split * slice + static_cast<int64_t>(f) * a.pitch + c;
+    float4 sum = *reinterpret_cast<const float4*>(p);
+#pragma unroll 4
+    for (int q = 1; q < a.split; ++q) {
+      const float4 w = *reinterpret_cast<const float4*>(p + q * slice);
+      sum.x += w.x;
+      sum.y += w.y;
+      sum.z += w.z;
+      sum.w += w.w;
+    }
+    const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+    const int64_t o = g * a.out_gs + f * a.out_ld + c;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      if (c + x >= a.inner) break;
+      if (a.type == HA_TYPE_FP32)
+        static_cast<float*>(a.out)[o + x] = v[x];
+      else
+        static_cast<uint16_t*>(a.out)[o + x] = narrow(v[x], a.type);
+    }
+  }
+  if (!a.db) return;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < static_cast<int64_t>(a.groups) * a.outer; i += step) {
+    const int64_t g = i / a.outer, f = i - g * a.outer;
+    float sum = 0.0f;
+    for (int q = 0; q < a.split; ++q) sum += a.part_db[(g * a.split + q) * a.outer + f];
+    a.db[g * a.db_ld + f] = sum;
+  }
+}
+
 constexpr int kSms = 152;
 // Groups of at most this many rows on average take the tiles for few rows.
 constexpr int kFewRows = 32;
@@ -918,6 +974,25 @@ constexpr int kFewRows = 32;
 constexpr int kSmallTiles = 40;
 int64_t round8(int64_t x) { return (x + 7) / 8 * 8; }
 int64_t round256(int64_t x) { return (x + 255) / 256 * 256; }
+
+// Parts of each group's rows in the weights' gradient: where its tiles are fewer than half of the
+// pairs of SMs, as many as give every pair a tile, with at least kMinChunks chunks each on average
+// (one group, 30000 rows, 1024 -> 1000, fp32: 151 us with one part, 55 with 4).
+int dw_split(int groups, int64_t rows, int inner, int outer) {
+  const int64_t tiles = groups * static_cast<int64_t>((outer + 2 * kM - 1) / (2 * kM)) * ((inner + kPairCols - 1) / kPairCols);
+  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kSms / 2 / tiles, rows / groups / (kK * kMinChunks))));
+}
+struct Parts {
+  int split, pitch;
+  int64_t dw, db;                   // bytes
+  Parts(int groups, int64_t rows, int inner, int outer) : split(dw_split(groups, rows, inner, outer)), pitch(0), dw(0), db(0) {
+    if (split == 1) return;
+    pitch = (inner + 3) / 4 * 4;
+    dw = round256(static_cast<int64_t>(groups) * split * outer * pitch * 4);
+    db = round256(static_cast<int64_t>(groups) * split * outer * 4);
+  }
+  int64_t bytes() const { return dw + db; }
+};
 
 // One operand as the tensor maps need it: address, strides and width multiples of 16 bytes (the
 // edge of a map is only sure to cut whole 16-byte pieces).
@@ -1114,6 +1189,7 @@ extern "C" int hier_avg_grouped_product_workspace(int op, const void* a_dev, int
   else if (op != HA_GROUPED_FORWARD && op != HA_GROUPED_DX)
     return HA_EINVAL;
   *bytes = x.packed_bytes() + b.packed_bytes();
+  if (op == HA_GROUPED_DW) *bytes += Parts(groups, rows, inner, outer).bytes();
   return HA_OK;
 }
 
@@ -1198,7 +1274,8 @@ extern "C" int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, co
     const void* p16 = reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(dw_dev) & ~uintptr_t(15));
     dy = x = {p16, 1, 1, 8, 8, 0};
   }
-  if (dy.packed_bytes() + x.packed_bytes() > workspace_bytes) return HA_ENOMEM;
+  const Parts parts(groups, rows, inner, outer);
+  if (dy.packed_bytes() + x.packed_bytes() + parts.bytes() > workspace_bytes) return HA_ENOMEM;
   if (workspace_bytes > 0 && (!workspace_dev || (reinterpret_cast<uintptr_t>(workspace_dev) & 15)))
     return HA_EINVAL;
   unsigned char* p = static_cast<unsigned char*>(workspace_dev);
@@ -1210,7 +1287,8 @@ extern "C" int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, co
   a.bias_ld = db_ld;
   a.out_ld = dw_ld;
   a.out_gs = dw_gs;
-  a.groups = groups;
+  a.groups = groups * parts.split;
+  a.split = parts.split;
   a.rows = static_cast<int>(rows);
   a.m = outer;
   a.n = inner;
@@ -1219,13 +1297,42 @@ extern "C" int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, co
   const int es = type_size(dw_type);
   a.wide_out = (reinterpret_cast<uintptr_t>(dw_dev) & 15) == 0 && dw_ld * es % 16 == 0 && inner * es % 16 == 0 &&
                (groups == 1 || dw_gs * es % 16 == 0);
+  if (parts.split > 1) {
+    a.out = p;
+    a.out_ld = parts.pitch;
+    a.out_gs = static_cast<int64_t>(outer) * parts.pitch;
+    a.out_type = HA_TYPE_FP32;
+    a.wide_out = 1;                 // what is past a row's end is not read
+    if (db_dev) {
+      a.db = reinterpret_cast<float*>(p + parts.dw);
+      a.bias_ld = outer;
+    }
+  }
   CUtensorMap ta, tb;
   if (!make_map(&ta, dy, type, 64, 64) || !make_map(&tb, x, type, 64, 64)) return HA_ECUDA;
-  const int64_t most = groups * static_cast<int64_t>((outer + 2 * kM - 1) / (2 * kM)) *
+  const int64_t most = a.groups * static_cast<int64_t>((outer + 2 * kM - 1) / (2 * kM)) *
                        ((inner + kPairCols - 1) / kPairCols + (db_dev ? 1 : 0));
   if (most > 0x7FFFFFFF) return HA_EUNSUPPORTED;
-  return dw_type == HA_TYPE_FP32 ? launch_pair<kDw, true>(ta, tb, a, most, s)
-                                 : launch_pair<kDw, false>(ta, tb, a, most, s);
+  const int status = a.out_type == HA_TYPE_FP32 ? launch_pair<kDw, true>(ta, tb, a, most, s)
+                                                : launch_pair<kDw, false>(ta, tb, a, most, s);
+  if (status != HA_OK || parts.split == 1) return status;
+  Join j = {};
+  j.part = static_cast<const float*>(a.out);
+  j.part_db = a.db;
+  j.out = dw_dev;
+  j.db = db_dev;
+  j.out_ld = dw_ld;
+  j.out_gs = dw_gs;
+  j.db_ld = db_ld;
+  j.groups = groups;
+  j.split = parts.split;
+  j.outer = outer;
+  j.inner = inner;
+  j.pitch = parts.pitch;
+  j.type = dw_type;
+  const int64_t quads = static_cast<int64_t>(groups) * outer * (parts.pitch / 4);
+  k_join<<<static_cast<unsigned>(std::min<int64_t>((quads + 255) / 256, 8 * kSms)), 256, 0, s>>>(j);
+  return cudaGetLastError() == cudaSuccess ? HA_OK : HA_ECUDA;
 }
 
 extern "C" int hier_avg_operator_check(void* stream) {

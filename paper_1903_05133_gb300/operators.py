@@ -109,15 +109,20 @@ def _out_type(out_dtype, out, dtype):
 
 
 def _workspace(lib, op, a, a_ld, b, b_ld, b_gs, groups, rows, inner, outer):
-    """Device memory for operands that have to be copied first (None where there are none)."""
-    if not ((a_ld | b_ld | inner | outer) & 7 or (b_gs & 7 or b_gs <= 0) and groups > 1 and op != DW or
-            (a.data_ptr() | b.data_ptr()) & 15) or rows == 0:
+    """Device memory for operands that have to be copied first and for sums in parts (None where
+    there are none)."""
+    fits = not ((a_ld | b_ld | inner | outer) & 7 or (b_gs & 7 or b_gs <= 0) and groups > 1 and op != DW or
+                (a.data_ptr() | b.data_ptr()) & 15)
+    # long groups' weights' gradients alone are summed in parts
+    if rows == 0 or fits and (op != DW or rows < 1024 * groups):
         return None, None, 0
     n = c_int64()
     check(lib.hier_avg_grouped_product_workspace(
         op, a.data_ptr(), a_ld, b.data_ptr(), b_ld, b_gs, groups, rows, inner, outer,
         ctypes.byref(n)), "grouped_product_workspace")
-    ws = torch.empty(max(n.value, 16), dtype=torch.uint8, device=a.device)
+    if n.value == 0:
+        return None, None, 0
+    ws = torch.empty(n.value, dtype=torch.uint8, device=a.device)
     return ws, ws.data_ptr(), n.value
 
 

@@ -116,6 +116,33 @@ def test_product_dw(sizes, K, N, dtype, out):
     ops.operator_check()
 
 
+@pytest.mark.parametrize("sizes,K,N", [([3000, 0, 1500, 70, 2001], 72, 130), ([8192], 520, 264), ([1, 9000, 0], 77, 3),
+                                       ([2049], 1, 1), ([1100] * 7, 300, 40)])
+@pytest.mark.parametrize("dtype,out", [(BF, BF), (HF, F)])
+def test_product_dw_long_groups(sizes, K, N, dtype, out):
+    # few tiles over many rows: summed in parts
+    g = gen(K * 17 + N)
+    T, G = sum(sizes), len(sizes)
+    dy, x = randn(g, T, N, dtype=dtype), randn(g, T, K, dtype=dtype)
+    into = torch.full((G, N, K + 3), 7.0, dtype=out, device="cuda")
+    dw, db = ops.grouped_product_dw(dy, x, offsets_of(sizes), bias_grad=True, out=into[:, :, :K])
+    t = 0
+    for i, n in enumerate(sizes):
+        a, b = dy[t:t + n].double(), x[t:t + n].double()
+        assert_within(dw[i], a.T @ b, product_bound(a.T @ b, a.abs().T @ b.abs(), n, out))
+        assert_within(db[i], a.sum(0), (n + 16) * 2.0 ** -24 * a.abs().sum(0) + 1e-300)
+        t += n
+    assert (into[:, :, K:] == 7).all()
+    assert torch.equal(dw, ops.grouped_product_dw(dy, x, offsets_of(sizes), out_dtype=out))
+    # offsets outside the rows, and one that goes back: its group is empty
+    off = torch.tensor([-5, T // 2, T // 4, T + 9], dtype=torch.int32, device="cuda")
+    dw = ops.grouped_product_dw(dy, x, off, out_dtype=F)
+    for i, (b, e) in enumerate(((0, T // 2), (0, 0), (T // 4, T))):
+        a, b = dy[b:e].double(), x[b:e].double()
+        assert_within(dw[i], a.T @ b, product_bound(a.T @ b, a.abs().T @ b.abs(), T, F))
+    ops.operator_check()
+
+
 def test_product_many_groups_and_folds():
     # more groups than a warp's scan takes at once, and sums of several folded segments
     g = gen(3)

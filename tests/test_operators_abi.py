@@ -55,6 +55,17 @@ def test_workspace(lib):
     assert f(0, P, 64, P, 64, 0, 2, 8, 64, 64, None) == EINVAL
 
 
+def test_workspace_of_parts(lib):
+    # few tiles over many rows: the weights' gradient's parts need room
+    n = ctypes.c_int64(-1)
+    assert lib.hier_avg_grouped_product_workspace(2, P, 64, P, 64, 0, 1, 8192, 64, 64, ctypes.byref(n)) == 0
+    assert n.value >= 2 * 64 * 64 * 4
+    dw = [P, 64, P, 64, 1, P, 1, 8192, 64, 64, P, 64, 4096, 1, None, 0, P, n.value - 1, None]
+    assert lib.hier_avg_grouped_product_dw(*dw) == ENOMEM
+    assert lib.hier_avg_grouped_product_workspace(2, P, 64, P, 64, 0, 1000, 1 << 24, 64, 64, ctypes.byref(n)) == 0
+    assert n.value == 0
+
+
 def test_logprobs_refuse(lib):
     fwd = [P, 1, 4, 100, 100, P, 4, None, 0, 1.0, 3, P, P, P, P, P, None]
     for at, v, status in ((0, None, EINVAL), (1, 3, EINVAL), (2, -1, EINVAL), (3, 0, EINVAL), (4, 99, EINVAL), (5, None, EINVAL),
