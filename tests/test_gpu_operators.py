@@ -116,6 +116,28 @@ def test_product_dw(sizes, K, N, dtype, out):
     ops.operator_check()
 
 
+# few tiles and long sums: the CTAs of a cluster share a tile, over more tiles than clusters, columns
+# that do not divide among them, groups of several tiles, and CTAs without a column
+@pytest.mark.parametrize("sizes,K,N", [([5], 4104, 2432), ([1], 8192, 64), ([63, 1], 8200, 300), ([0, 31], 2056, 136),
+                                       ([200], 4096, 520), ([150, 3, 90], 4400, 56), ([2, 3, 1, 0, 9], 2048, 480)])
+@pytest.mark.parametrize("out", [BF, F])
+def test_product_shared_tiles(sizes, K, N, out):
+    g = gen(K * 19 + N)
+    T, G = sum(sizes), len(sizes)
+    x, w = randn(g, T, K, dtype=BF), randn(g, G, N, K, dtype=BF, std=K ** -0.5)
+    off = offsets_of(sizes)
+    ref, mag = ref_rows(x, w, sizes, True)
+    y = ops.grouped_product(x, w, off, out_dtype=out)
+    assert_within(y, ref, product_bound(ref, mag, K, out))
+    wt = w.transpose(1, 2).contiguous()                     # the same sums as a gradient
+    h = randn(g, T, N, dtype=BF)
+    got = ops.grouped_product_dx(x, wt, off, h=h, out_dtype=out)
+    assert_within(got, ref * (h > 0), product_bound(ref, mag, K, out))
+    for _ in range(3):
+        assert torch.equal(y, ops.grouped_product(x, w, off, out_dtype=out))
+    ops.operator_check()
+
+
 @pytest.mark.parametrize("sizes,K,N", [([3000, 0, 1500, 70, 2001], 72, 130), ([8192], 520, 264), ([1, 9000, 0], 77, 3),
                                        ([2049], 1, 1), ([1100] * 7, 300, 40)])
 @pytest.mark.parametrize("dtype,out", [(BF, BF), (HF, F)])
