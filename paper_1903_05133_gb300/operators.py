@@ -108,22 +108,33 @@ def _out_type(out_dtype, out, dtype):
     return d
 
 
+def _copy_bytes(address: int, groups: int, rows: int, cols: int, ld: int, gs: int) -> int:
+    """What the copy of an operand takes, 0 where the kernels can read it in place: as
+    hier_avg_grouped_product_workspace counts it, without the call (3 us of a small product's 20)."""
+    if not (address & 15 or (ld | cols) & 7 or groups > 1 and (gs & 7 or gs <= 0)):
+        return 0
+    return groups * rows * ((cols + 7) & ~7) * 2 + 255 & ~255
+
+
 def _workspace(lib, op, a, a_ld, b, b_ld, b_gs, groups, rows, inner, outer):
     """Device memory for operands that have to be copied first and for sums in parts (None where
     there are none)."""
-    fits = not ((a_ld | b_ld | inner | outer) & 7 or (b_gs & 7 or b_gs <= 0) and groups > 1 and op != DW or
-                (a.data_ptr() | b.data_ptr()) & 15)
-    # long groups' weights' gradients alone are summed in parts
-    if rows == 0 or fits and (op != DW or rows < 1024 * groups):
+    if rows == 0:
         return None, None, 0
-    n = c_int64()
-    check(lib.hier_avg_grouped_product_workspace(
-        op, a.data_ptr(), a_ld, b.data_ptr(), b_ld, b_gs, groups, rows, inner, outer,
-        ctypes.byref(n)), "grouped_product_workspace")
-    if n.value == 0:
+    if op == DW and rows >= 1024 * groups:                  # long groups may be summed in parts
+        n = c_int64()
+        check(lib.hier_avg_grouped_product_workspace(
+            op, a.data_ptr(), a_ld, b.data_ptr(), b_ld, b_gs, groups, rows, inner, outer,
+            ctypes.byref(n)), "grouped_product_workspace")
+        n = n.value
+    else:
+        n = _copy_bytes(a.data_ptr(), 1, rows, inner if op == FORWARD else outer, a_ld, 0) + (
+            _copy_bytes(b.data_ptr(), 1, rows, inner, b_ld, 0) if op == DW else
+            _copy_bytes(b.data_ptr(), groups, outer, inner, b_ld, b_gs))
+    if n == 0:
         return None, None, 0
-    ws = torch.empty(n.value, dtype=torch.uint8, device=a.device)
-    return ws, ws.data_ptr(), n.value
+    ws = torch.empty(n, dtype=torch.uint8, device=a.device)
+    return ws, ws.data_ptr(), n
 
 
 def grouped_product(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,

@@ -66,6 +66,33 @@ def test_workspace_of_parts(lib):
     assert n.value == 0
 
 
+def test_workspace_counted_here(lib):
+    # the Python side counts the copies itself; the library refuses less than it needs
+    import random
+
+    from paper_1903_05133_gb300 import operators as ops
+
+    class Fake:                                             # a tensor as far as its address goes
+        device = "cpu"
+
+        def __init__(self, address):
+            self.data_ptr = lambda: address
+
+    rng = random.Random(5)
+    n = ctypes.c_int64()
+    for _ in range(2000):
+        op, groups, rows = rng.randrange(3), rng.choice((1, 2, 9)), rng.randrange(1, 500)
+        inner, outer = rng.randrange(1, 200), rng.randrange(1, 200)
+        inner, outer = (v * 8 if rng.random() < 0.5 else v for v in (inner, outer))
+        a, b = (Fake(P.value + rng.choice((0, 0, 0, 2, 8, 16))) for _ in range(2))
+        pad = lambda v: v + rng.choice((0, 0, 1, 8))  # noqa: E731
+        a_ld, b_ld = pad(inner if op == 0 else outer), pad(inner)
+        b_gs = 0 if op == 2 else rng.choice((0, outer * b_ld, outer * b_ld + 3, outer * b_ld + 8))
+        assert lib.hier_avg_grouped_product_workspace(op, a.data_ptr(), a_ld, b.data_ptr(), b_ld, b_gs, groups, rows, inner, outer,
+                                                      ctypes.byref(n)) == 0
+        assert ops._workspace(lib, op, a, a_ld, b, b_ld, b_gs, groups, rows, inner, outer)[2] == n.value
+
+
 def test_logprobs_refuse(lib):
     fwd = [P, 1, 4, 100, 100, P, 4, None, 0, 1.0, 3, P, P, P, P, P, None]
     for at, v, status in ((0, None, EINVAL), (1, 3, EINVAL), (2, -1, EINVAL), (3, 0, EINVAL), (4, 99, EINVAL), (5, None, EINVAL),
