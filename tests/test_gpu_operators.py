@@ -440,6 +440,45 @@ def test_logprobs_gradient(T, V, dtype):
     assert ops.token_logprobs_backward(y, t, f.lse, None, d, out=y) is y and torch.equal(y, want)
 
 
+@pytest.mark.parametrize("dtype", [F, BF])
+@pytest.mark.parametrize("T", [3, 1300])
+@pytest.mark.parametrize("V", [1, 33, 64, 65, 300, 512, 513, 1000, 1025, 2048, 2049, 3000])
+def test_logprobs_few_classes(T, V, dtype):
+    # on both sides of each length at which a row is taken by another kernel, few rows and many
+    g = gen(T + V)
+    big = randn(g, T, V + 3, dtype=dtype, std=3.0)
+    z = big[:, 1:V + 1]                                     # rows of unit stride at any alignment
+    t = torch.randint(0, V, (T,), generator=g, device="cuda")
+    t[1] = -1
+    check_logprobs(z, t, 0, temperature=1.7)
+    allowed = torch.rand(T, V, generator=g, device="cuda") < 0.4
+    allowed[0] = False
+    allowed[2, 1:] = False
+    for top, ok in ((1, None), (20, None), (32, allowed), (4, allowed[1])):
+        check_logprobs(z, t, top, allowed=ok)
+    same = torch.ones(T, V, dtype=dtype, device="cuda")     # equal logits: by index
+    check_logprobs(same, t, 5)
+    z = z.clone()
+    z[0, V // 2] = math.nan
+    r = ops.token_logprobs(z, t, top=2)
+    assert r.lse[0].isnan() and r.entropy[0].isnan() and (r.top_index[0] == -1).all() and not r.lse[1:].isnan().any()
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
+@pytest.mark.parametrize("T,V", [(1300, 10), (1300, 500), (1300, 1024), (1300, 1025), (3, 512), (3, 513), (2600, 33)])
+def test_logprobs_gradient_few_classes(T, V, dtype):
+    g = gen(T * 3 + V)
+    z = randn(g, T, V + 1, dtype=dtype, std=3.0)[:, 1:]
+    t = torch.randint(-1, V, (T,), generator=g, device="cuda")
+    check_grad(z, t, temperature=0.9)
+    ok = torch.rand(T, V, generator=g, device="cuda") < 0.5
+    ok[0] = False
+    wide = torch.zeros(T, V + 5, dtype=dtype, device="cuda")
+    check_grad(z, t, allowed=ok, out=wide[:, 3:V + 3])
+    check_grad(z, t, allowed=ok[1], entropy=False)
+    assert (wide[:, :3] == 0).all() and (wide[:, V + 3:] == 0).all()
+
+
 def test_logprobs_gradient_is_differences():
     g = gen(77)
     z = randn(g, 2, 40, std=2.0)
