@@ -887,14 +887,24 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
 }
 
 // Rows of 16-bit values to a pitch of whole 16-byte vectors, for operands that a tensor
-// map cannot describe (an odd width, stride or address).  A thread makes a vector from loads as
-// wide as the rows' alignment allows, and goes on `step` vectors further: that is sg groups, sr
-// rows and sc vectors, so that no place is divided for again.  One launch for both operands.
+// map cannot describe (an odd width, stride or address).  A thread makes a vector at a time, from
+// loads as wide as the rows' alignment allows, and knows how far on its next is, so that no place is
+// divided for again.  One launch for both operands.  Rows of x or dy: the threads go through the
+// vectors.  Weights: 2^`log` neighbouring threads take `per` vectors each of one of the `segs` parts of
+// a row, and pass over groups without rows of x (57 groups of 1718 -> 3496, one row: 218 us with all
+// of them, 22 so).  Small parts keep the threads busy where there are few rows, large ones pass over
+// more at a step.
 struct Pack {
   const uint16_t* src;
   uint4* dst;
-  int64_t all, step, ld, gs, per_group, sg, sr;
-  int cols, pitch8, sc, bytes;                            // bytes of a load
+  const int* offsets;                                     // of the weights' groups, or nullptr: one matrix
+  int64_t all;                                            // its vectors
+  int64_t ld, gs;
+  int groups, per_group, sg, sr;                          // a thread's next row: sg groups, sr rows further
+  int sv;                                                 // and vectors (weights: parts)
+  int segs, per;
+  int cols, pitch8, log, bytes;                           // bytes of a load
+  int rows;                                               // that the offsets may reach
 };
 struct Packs {
   Pack of[2];
@@ -919,22 +929,51 @@ __device__ __forceinline__ uint4 pack_vector(const uint16_t* s, int left) {
   }
   return out;
 }
-__global__ void __launch_bounds__(256) k_pack(const __grid_constant__ Packs both) {
-  const int second = static_cast<int>(blockIdx.x) >= both.blocks;
-  const Pack a = both.of[second];
-  int64_t i = (blockIdx.x - (second ? both.blocks : 0)) * 256ll + threadIdx.x, r = i / a.pitch8, g = r / a.per_group;
-  int v = static_cast<int>(i - r * a.pitch8);
-  r -= g * a.per_group;
-  for (; i < a.all; i += a.step) {
-    const uint16_t* s = a.src + g * a.gs + r * a.ld + v * 8;
-    const int left = a.cols - v * 8;
-    a.dst[i] = a.bytes == 8 ? pack_vector<uint2>(s, left)
-               : a.bytes == 4 ? pack_vector<uint32_t>(s, left) : pack_vector<uint16_t>(s, left);
-    v += a.sc;
+__device__ __forceinline__ uint4 pack_of(const Pack& a, const uint16_t* s, int v) {
+  const int left = a.cols - v * 8;
+  return a.bytes == 8 ? pack_vector<uint2>(s + v * 8, left)
+         : a.bytes == 4 ? pack_vector<uint32_t>(s + v * 8, left) : pack_vector<uint16_t>(s + v * 8, left);
+}
+__device__ __forceinline__ void pack_matrix(const Pack& a, uint32_t block, uint32_t blocks) {
+  const uint32_t first = block * 256 + threadIdx.x;
+  int r = static_cast<int>(first / static_cast<uint32_t>(a.pitch8));
+  int v = static_cast<int>(first - static_cast<uint32_t>(r) * a.pitch8);
+  for (int64_t i = first; i < a.all; i += blocks * 256) {
+    a.dst[i] = pack_of(a, a.src + r * a.ld, v);
     r += a.sr;
-    g += a.sg;
+    v += a.sv;
     if (v >= a.pitch8) {
       v -= a.pitch8;
+      ++r;
+    }
+  }
+}
+__device__ __forceinline__ void pack_weights(const Pack& a, uint32_t block) {
+  const uint32_t first = (block * 256 + threadIdx.x) >> a.log, row = first / static_cast<uint32_t>(a.segs);
+  const int lane = threadIdx.x & ((1 << a.log) - 1);
+  int seg = static_cast<int>(first - row * a.segs), g = static_cast<int>(row / static_cast<uint32_t>(a.per_group));
+  int r = static_cast<int>(row - static_cast<uint32_t>(g) * a.per_group);
+  while (g < a.groups) {
+    if (min(max(a.offsets[g], 0), a.rows) < min(max(a.offsets[g + 1], 0), a.rows)) {
+      const uint16_t* s = a.src + g * a.gs + r * a.ld;
+      uint4* d = a.dst + (static_cast<int64_t>(g) * a.per_group + r) * a.pitch8;
+      const int end = min(a.pitch8, ((seg + 1) * a.per) << a.log);
+      int v = ((seg * a.per) << a.log) + lane;
+#pragma unroll 1
+      do {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int w = v + (x << a.log);
+          if (w < end) d[w] = pack_of(a, s, w);
+        }
+        v += 2 << a.log;
+      } while (v < end);
+    }
+    g += a.sg;
+    r += a.sr;
+    seg += a.sv;
+    if (seg >= a.segs) {
+      seg -= a.segs;
       ++r;
     }
     if (r >= a.per_group) {
@@ -942,6 +981,15 @@ __global__ void __launch_bounds__(256) k_pack(const __grid_constant__ Packs both
       ++g;
     }
   }
+}
+__global__ void __launch_bounds__(256) k_pack(const __grid_constant__ Packs both) {
+  const uint32_t second = blockIdx.x >= static_cast<uint32_t>(both.blocks);
+  const uint32_t block = blockIdx.x - (second ? both.blocks : 0);
+  const Pack& a = both.of[second];
+  if (a.offsets)
+    pack_weights(a, block);
+  else
+    pack_matrix(a, block, second ? gridDim.x - both.blocks : both.blocks);
 }
 
 // A split weights' gradient: dW and db are the sums of their parts, in the parts' order.
@@ -1028,8 +1076,9 @@ struct Operand {
   int64_t packed_bytes() const { return fits() ? 0 : round256(groups * rows * round8(cols) * 2); }
 };
 
-// Copies those of two operands that do not fit to ws, which moves on.
-cudaError_t pack(Operand& x, Operand& y, unsigned char*& ws, cudaStream_t s) {
+// Copies those of two operands that do not fit to ws, which moves on.  Offsets (or nullptr): of the
+// second's groups, up to `rows`.
+cudaError_t pack(Operand& x, Operand& y, const int* offsets, int rows, unsigned char*& ws, cudaStream_t s) {
   Packs p = {};
   int count = 0;
   unsigned blocks[2] = {0, 0};
@@ -1043,13 +1092,28 @@ cudaError_t pack(Operand& x, Operand& y, unsigned char*& ws, cudaStream_t s) {
     a.pitch8 = static_cast<int>(pitch / 8);
     a.ld = o->ld;
     a.gs = o->gs;
-    a.per_group = o->rows;
-    a.all = o->groups * o->rows * a.pitch8;
-    blocks[count] = static_cast<unsigned>(std::min<int64_t>((a.all + 255) / 256, 16 * kSms));
-    a.step = blocks[count] * 256ll;
-    a.sc = static_cast<int>(a.step % a.pitch8);
-    a.sr = a.step / a.pitch8 % o->rows;
-    a.sg = a.step / a.pitch8 / o->rows;
+    a.groups = static_cast<int>(o->groups);
+    a.per_group = static_cast<int>(o->rows);
+    a.offsets = o == &y ? offsets : nullptr;
+    a.rows = rows;
+    const auto grid = [](int64_t threads) { return static_cast<unsigned>(std::min<int64_t>((threads + 255) / 256, 16 * kSms)); };
+    if (a.offsets) {
+      while (a.log < 5 && 2 << a.log < a.pitch8) ++a.log;
+      const int64_t lanes = o->groups * o->rows << a.log;
+      a.per = 2;
+      while (a.per < 16 && lanes * ((a.pitch8 >> a.log) / a.per) > 64 * kSms * 256) a.per *= 2;
+      a.segs = (a.pitch8 + (a.per << a.log) - 1) / (a.per << a.log);
+      blocks[count] = grid(o->groups * o->rows * a.segs << a.log);
+      const int64_t step = static_cast<int64_t>(blocks[count]) * 256 >> a.log, rows_on = step / a.segs;
+      a.sv = static_cast<int>(step % a.segs);
+      a.sr = static_cast<int>(rows_on % o->rows);
+      a.sg = static_cast<int>(rows_on / o->rows);
+    } else {
+      a.all = o->rows * a.pitch8;
+      blocks[count] = grid(a.all);
+      a.sr = static_cast<int>(blocks[count] * 256 / a.pitch8);
+      a.sv = static_cast<int>(blocks[count] * 256 % a.pitch8);
+    }
     const uintptr_t low = reinterpret_cast<uintptr_t>(o->p) | static_cast<uintptr_t>(o->ld * 2) |
                           static_cast<uintptr_t>(o->groups > 1 ? o->gs * 2 : 0);
     a.bytes = (low & 7) == 0 ? 8 : (low & 3) == 0 ? 4 : 2;
@@ -1164,7 +1228,7 @@ int rows_product(Operand x, Operand w, Args a, void* ws, int64_t ws_bytes, cudaS
   if (x.packed_bytes() + w.packed_bytes() > ws_bytes) return HA_ENOMEM;
   if (ws_bytes > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 15))) return HA_EINVAL;
   unsigned char* p = static_cast<unsigned char*>(ws);
-  if (pack(x, w, p, s) != cudaSuccess) return HA_ECUDA;
+  if (pack(x, w, a.offsets, a.rows, p, s) != cudaSuccess) return HA_ECUDA;
   a.wide_out = (reinterpret_cast<uintptr_t>(a.out) & 15) == 0 && a.out_ld * type_size(a.out_type) % 16 == 0;
   a.wide_h = a.h && (reinterpret_cast<uintptr_t>(a.h) & 15) == 0 && a.h_ld % 8 == 0;
   const bool fold = a.out_type == HA_TYPE_FP32;
@@ -1301,7 +1365,7 @@ extern "C" int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, co
   if (workspace_bytes > 0 && (!workspace_dev || (reinterpret_cast<uintptr_t>(workspace_dev) & 15)))
     return HA_EINVAL;
   unsigned char* p = static_cast<unsigned char*>(workspace_dev);
-  if (pack(dy, x, p, s) != cudaSuccess) return HA_ECUDA;
+  if (pack(dy, x, nullptr, 0, p, s) != cudaSuccess) return HA_ECUDA;
   Args a = {};
   a.offsets = offsets_dev;
   a.out = dw_dev;

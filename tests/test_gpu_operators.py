@@ -116,6 +116,28 @@ def test_product_dw(sizes, K, N, dtype, out):
     ops.operator_check()
 
 
+@pytest.mark.parametrize("G,N,K", [(40, 1300, 1101), (30, 7, 205), (9, 130, 9)])
+def test_product_unaligned_weights_of_empty_groups(G, N, K):
+    g = gen(G + N + K)
+    sizes = [0] * G
+    sizes[3], sizes[4], sizes[G - 1] = 2, 1, 5
+    T = sum(sizes)
+    x, w = randn(g, T, K, dtype=BF), randn(g, G, N, K, dtype=BF, std=K ** -0.5)
+    dy = randn(g, T, N, dtype=BF)
+    off = offsets_of(sizes)
+    w[0] = w[5] = math.nan                                  # in groups without rows
+    used = [3, 4, G - 1]
+    ref, mag = ref_rows(x, w[used], [2, 1, 5], True)
+    assert_within(ops.grouped_product(x, w, off), ref, product_bound(ref, mag, K, BF))
+    ref, mag = ref_rows(dy, w[used], [2, 1, 5], False)
+    assert_within(ops.grouped_product_dx(dy, w, off, out_dtype=F), ref, product_bound(ref, mag, N, F))
+    off = off.clone()                                       # outside the rows on both sides
+    off[0], off[G] = -4, T + 100
+    ref, mag = ref_rows(x, w[used], [2, 1, 5], True)
+    assert_within(ops.grouped_product(x, w, off)[2:], ref[2:], product_bound(ref, mag, K, BF)[2:])
+    ops.operator_check()
+
+
 # few tiles and long sums: the CTAs of a cluster share a tile, over more tiles than clusters, columns
 # that do not divide among them, groups of several tiles, and CTAs without a column
 @pytest.mark.parametrize("sizes,K,N", [([5], 4104, 2432), ([1], 8192, 64), ([63, 1], 8200, 300), ([0, 31], 2056, 136),
