@@ -45,9 +45,10 @@ struct Stat {
 template <typename T> constexpr float kNone = -1e30f;
 template <> constexpr float kNone<__nv_bfloat16> = -1.0002555517425873e30f;
 
-// Order of floats (no NaN) as unsigned integers, and back.
+// Order of floats (no NaN) as unsigned integers, and back.  The sum turns a zero's sign, which
+// would order it before the other zero, to plus.
 __device__ __forceinline__ uint32_t ordered(float v) {
-  const uint32_t u = __float_as_uint(v);
+  const uint32_t u = __float_as_uint(v + 0.0f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float from_ordered(uint32_t o) {
