@@ -237,9 +237,10 @@ def _logits(logits, targets, allowed, temperature):
     if not (allowed.is_cuda and allowed.dtype in (torch.bool, torch.uint8) and
             tuple(allowed.shape) in ((V,), (T, V)) and (allowed.stride(-1) == 1 or V == 1)):
         raise ValueError("allowed must be a CUDA bool tensor [classes] or [rows, classes] with unit stride in rows")
-    if allowed.dim() == 1 or (T > 1 and allowed.stride(0) == 0):
+    if allowed.dim() == 1 or T <= 1 or allowed.stride(0) == 0:
         return ld, allowed.data_ptr(), 0
-    return ld, allowed.data_ptr(), _ld(allowed)
+    _need(allowed.stride(0) >= V, "allowed's rows must not overlap")
+    return ld, allowed.data_ptr(), allowed.stride(0)
 
 
 def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, top: int = 0, temperature: float = 1.0,

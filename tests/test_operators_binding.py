@@ -1,0 +1,50 @@
+"""What the operators' binding refuses before it calls the library, on stand-ins for CUDA tensors: no
+address is read here."""
+import pytest
+import torch
+
+from paper_1903_05133_gb300 import operators as ops
+
+BF, HF, F, I32, BOOL = torch.bfloat16, torch.float16, torch.float32, torch.int32, torch.bool
+
+
+class Stand:
+    """A CUDA tensor as far as its type, shape, strides and address go."""
+    is_cuda = True
+
+    def __init__(self, dtype, shape, strides=None, address=1 << 20):
+        self.dtype, self.shape, self.address = dtype, torch.Size(shape), address
+        if strides is None:
+            strides = [1]
+            for n in reversed(shape[1:]):
+                strides.insert(0, strides[0] * n)
+        self.strides = tuple(strides[:len(shape)])
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self, i=None):
+        return self.strides if i is None else self.strides[i]
+
+    def data_ptr(self):
+        return self.address
+
+    def is_contiguous(self):
+        return Stand(self.dtype, self.shape).strides == self.strides or 0 in self.shape
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+
+def test_masks_with_overlapping_rows_are_refused():
+    T, V = 6, 100
+    logits, targets = Stand(BF, (T, V)), Stand(I32, (T,))
+    given = lambda *a, **k: ops._logits(logits, targets, Stand(BOOL, *a, **k), 1.0)[1:]  # noqa: E731
+    for stride in (1, 50, V - 1):                           # a sliding window's 1
+        with pytest.raises(ValueError, match="overlap"):
+            given((T, V), (stride, 1))
+    at = 1 << 20
+    assert given((T, V)) == (at, V) and given((T, V), (V + 3, 1)) == (at, V + 3)
+    assert given((V,)) == (at, 0) and given((T, V), (0, 1)) == (at, 0)
+    one = Stand(BF, (1, V)), Stand(I32, (1,))               # the stride of one row says nothing
+    assert ops._logits(*one, Stand(BOOL, (1, V), (1, 1)), 1.0)[1:] == (at, 0)
