@@ -10,6 +10,7 @@
 // probabilities that keep its mean: with b2 = 0.999 a step moves sqrt(v) by about 0.05 %,
 // which rounding to nearest (steps of 6 to 12 %) would always take back.  The random bits
 // come from the element's place and the caller's seed, so a step is reproducible.
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <memory>
@@ -548,7 +549,7 @@ extern "C" int hier_avg_adamw_step(hier_avg_adamw* h, const void* const* grads_d
                                    const float* grad_scale_dev, uint32_t seed, void* stream) {
   if (!h || !grads_dev || !type_ok(grad_type) || t < 1) return HA_EINVAL;
   if (!std::isfinite(lr) || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) ||
-      !(eps > 0) || !std::isfinite(eps))
+      !(eps >= FLT_MIN) || !std::isfinite(eps))      // below, the reciprocal of eps alone is infinite
     return HA_EINVAL;
   if (h->chunks.empty()) return HA_OK;
   if (!h->table) return HA_ESTATE;

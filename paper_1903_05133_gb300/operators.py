@@ -322,7 +322,8 @@ class AdamW:
         params = list(params)
         _need(len(params) >= 1, "params must not be empty")
         _need(bits in (8, 32), "bits must be 8 or 32")
-        _need(0 <= beta1 < 1 and 0 <= beta2 < 1 and 0 < eps < float("inf"), "betas must be in [0, 1), eps positive")
+        _need(0 <= beta1 < 1 and 0 <= beta2 < 1 and 2.0 ** -126 <= eps < float("inf"),
+              "betas must be in [0, 1), eps at least 2^-126 and finite")
         decays = [float(decay)] * len(params) if isinstance(decay, (int, float)) else [float(d) for d in decay]
         copies = [None] * len(params) if copies is None else list(copies)
         _need(len(decays) == len(params) and len(copies) == len(params), "decay and copies must be one a tensor")

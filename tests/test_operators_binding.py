@@ -48,3 +48,19 @@ def test_masks_with_overlapping_rows_are_refused():
     assert given((V,)) == (at, 0) and given((T, V), (0, 1)) == (at, 0)
     one = Stand(BF, (1, V)), Stand(I32, (1,))               # the stride of one row says nothing
     assert ops._logits(*one, Stand(BOOL, (1, V), (1, 1)), 1.0)[1:] == (at, 0)
+
+
+def test_adamw_eps_without_a_finite_reciprocal_is_refused(lib):
+    import ctypes
+
+    from test_operators_abi import EINVAL, create
+    rc, h = create(lib)
+    assert rc == 0
+    g = (ctypes.c_void_p * 1)(4096)
+    step = lambda eps: lib.hier_avg_adamw_step(h, g, 0, 0.1, 0.9, 0.99, eps, 1, None, 0, None)  # noqa: E731
+    for eps in (2.0 ** -127, 1e-40, 1e-60, 0.0, float("nan")):
+        assert step(eps) == EINVAL, eps
+    assert step(2.0 ** -126) == step(1e-8) == -4            # HA_ESTATE: not bound
+    lib.hier_avg_adamw_destroy(h)
+    with pytest.raises(ValueError, match="eps"):
+        ops.AdamW([Stand(F, (4,))], eps=1e-40)
