@@ -276,12 +276,34 @@ __device__ __forceinline__ int64_t target_of(const void* targets, bool wide, int
   return wide ? static_cast<const int64_t*>(targets)[row] : static_cast<const int*>(targets)[row];
 }
 
+// The sum A of a row whose distances to the largest logit pass fp32's range (logits near its end, a
+// temperature near 0): 0 * inf, which is NaN where S is not.  The row is then summed once more, by
+// one CTA, with the distances cut off where 2^d is 0 (a cut in the loop above would cost every row).
+template <typename T, int THREADS>
+__device__ __noinline__ float sum_again(const T* z, const uint8_t* ok, int classes, float m, float c, float* part) {
+  float A = 0.0f;
+  for (int j = threadIdx.x; j < classes; j += THREADS) {
+    const float v = Elem<T>::up(z[j]);
+    if (!(v > kNone<T>) || (ok && !ok[j])) continue;
+    const float d = fmaxf((v - m) * c, -200.0f);
+    A = fmaf(exp2_fast(d), d, A);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) A += __shfl_xor_sync(~0u, A, o);
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = A;
+  __syncthreads();
+  A = 0.0f;
+  for (int w = 0; w < THREADS / 32; ++w) A += part[w];
+  return A;
+}
+
 // One cluster a row; its CTAs take equal shares of the row's 16-byte vectors.
 template <typename T, bool TOP, bool MASK, int THREADS>
 __global__ void __launch_bounds__(THREADS, (TOP ? 1024 : 1536) / THREADS) k_logprobs(const __grid_constant__ FwdArgs a) {
   constexpr int V = kVec<T>, kWarps = THREADS / 32;
   __shared__ Stat warp_stat[kWarps];
   __shared__ Stat cta_stat, row_stat;
+  __shared__ float again[kWarps];
   extern __shared__ __align__(16) unsigned char dyn[];
   TopState& ts = *reinterpret_cast<TopState*>(dyn);
 
@@ -475,6 +497,7 @@ __global__ void __launch_bounds__(THREADS, (TOP ? 1024 : 1536) / THREADS) k_logp
     __syncthreads();
     s = cta_stat;
   }
+  if (s.A != s.A && s.S == s.S) s.A = sum_again<T, THREADS>(z, ok, classes, s.m, c, again);
 
   const float log_s = log2f(s.S);
   const bool none = !(s.m > kNone<T>) && s.S == s.S;       // NaN stays
@@ -487,18 +510,17 @@ __global__ void __launch_bounds__(THREADS, (TOP ? 1024 : 1536) / THREADS) k_logp
     } else if (t >= 0) {
       float zt = Elem<T>::up(z[t]);
       if (zt <= kNone<T> || (MASK && !ok[t])) zt = -INFINITY;
-      lp = none ? -INFINITY : ((zt - s.m) * c - log_s) * kLn2;
+      lp = none ? -INFINITY : fmaf(zt - s.m, a.inv_t, -log_s * kLn2);
     }
     a.logp[row] = lp;
     a.entropy[row] = none ? 0.0f : (log_s - s.A / s.S) * kLn2;
     a.lse[row] = lse;
   }
   if (TOP && tid < a.top) {
-    const bool bad = !(fabsf(lse) < INFINITY);
-    const bool has = tid < ts.count && !bad;
+    const bool has = tid < ts.count && !none && lse == lse;
     const uint64_t k = has ? ts.keys[tid] : 0;
     a.top_logp[row * a.top + tid] =
-        has ? ((key_value(k) - s.m) * c - log_s) * kLn2 : (lse != lse ? NAN : -INFINITY);
+        has ? fmaf(key_value(k) - s.m, a.inv_t, -log_s * kLn2) : (lse != lse ? NAN : -INFINITY);
     a.top_index[row * a.top + tid] = has ? static_cast<int>(key_index(k)) : -1;
   }
 }
@@ -566,11 +588,21 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_logprobs_row(const __grid_co
       S += __shfl_xor_sync(~0u, S, o);
       A += __shfl_xor_sync(~0u, A, o);
     }
+    if (A != A && S == S) {                               // as sum_again
+      A = 0.0f;
+#pragma unroll
+      for (int u = 0; u < R; ++u) {
+        const float d = fmaxf((v[u] - m) * c, -200.0f);
+        A = fmaf(exp2_fast(d), d, A);
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) A += __shfl_xor_sync(~0u, A, o);
+    }
     const float log_s = log2f(S);
     const bool none = !(m > kNone<T>) && S == S;          // NaN stays
     const float lse = none ? -INFINITY : fmaf(m, a.inv_t, log_s * kLn2);
     if (lane == 0) {
-      a.logp[row] = t >= classes ? NAN : t < 0 ? 0.0f : none ? -INFINITY : ((zt - m) * c - log_s) * kLn2;
+      a.logp[row] = t >= classes ? NAN : t < 0 ? 0.0f : none ? -INFINITY : fmaf(zt - m, a.inv_t, -log_s * kLn2);
       a.entropy[row] = none ? 0.0f : (log_s - A / S) * kLn2;
       a.lse[row] = lse;
     }
@@ -610,9 +642,9 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_logprobs_row(const __grid_co
         }
       }
       if (lane < a.top) {
-        has = has && fabsf(lse) < INFINITY;
+        has = has && !none && lse == lse;
         a.top_logp[row * a.top + lane] =
-            has ? ((from_ordered(mine) - m) * c - log_s) * kLn2 : (lse != lse ? NAN : -INFINITY);
+            has ? fmaf(from_ordered(mine) - m, a.inv_t, -log_s * kLn2) : (lse != lse ? NAN : -INFINITY);
         a.top_index[row * a.top + lane] = has ? static_cast<int>(mine_index) : -1;
       }
     }

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_1903_05133_gb300 import operators as ops
-from test_gpu_operators import BF, F, HF, gen
+from test_gpu_operators import BF, F, HF, close, gen
 
 pytestmark = pytest.mark.gpu
 
@@ -72,3 +72,64 @@ def test_adamw_second_moments_below_the_normal_numbers():
     off = (p.double() - want).abs()[some] / want.abs()[some]
     assert some.sum() > 2000 and off.max() <= 2.0 ** -19, off.max()
     assert p.isfinite().all()
+
+
+def check_far_apart(z, t, top, temperature, allowed=None):
+    # as check_logprobs, with a reference that takes the largest logit away before it divides: next to
+    # a log-sum-exp of 1e20 even 64 bits do not see the others
+    V = z.shape[1]
+    r = ops.token_logprobs(z, t, top=top, temperature=temperature, allowed=allowed)
+    raw = z.double()
+    ok = raw > -1e30
+    if allowed is not None:
+        ok = ok & allowed
+    raw = raw.masked_fill(~ok, -math.inf)
+    m = raw.amax(1, keepdim=True)
+    none = m.isinf()
+    d = ((raw - m) / temperature).masked_fill(~ok, -math.inf)
+    log_s = torch.logsumexp(d, 1, keepdim=True)
+    lp = torch.where(ok, d - log_s, -math.inf)
+    p = lp.exp()
+    ent = -torch.where(p > 0, p * lp, 0.0).sum(1)
+    lse = torch.where(none, -math.inf, m / temperature + log_s)[:, 0]
+    logp = lp.gather(1, t.long()[:, None])[:, 0]
+    s = 2.0 ** -24 * (V / 512 + 64)                         # check_logprobs's bounds
+    size = lambda v: torch.where(v.isinf(), 0.0, v.abs())  # noqa: E731
+    close(r.lse, lse, s + 2.0 ** -22 * size(lse))
+    close(r.logp, logp, s + 2.0 ** -22 * (size(logp) + 1))
+    close(r.entropy, ent, (2 * s + 2.0 ** -22) * (1 + ent))
+    if top:
+        order = torch.sort(raw, dim=1, descending=True, stable=True).indices[:, :top]
+        best = lp.gather(1, order)
+        assert torch.equal(r.top_index[:, :order.shape[1]].long(), torch.where(best.isinf(), -1, order))
+        close(r.top_logp[:, :order.shape[1]], best, s + 2.0 ** -22 * (size(best) + 1))
+    return r
+
+
+@pytest.mark.parametrize("dtype", [F, BF, HF])
+@pytest.mark.parametrize("T,V", [(4, 3), (5, 300), (3, 1800), (1300, 1000), (3, 9000), (400, 3000), (1, 70001)])
+def test_logprobs_tiny_temperatures(T, V, dtype):
+    # the distances to the largest logit, in units of the temperature, pass fp32's range
+    g = gen(T * 5 + V)
+    z = torch.randint(-1, 2, (T, V), generator=g, device="cuda").to(dtype)
+    t = torch.randint(0, V, (T,), generator=g, device="cuda")
+    ok = torch.rand(T, V, generator=g, device="cuda") < 0.5
+    ok[0] = False
+    for temperature in (1e-8, 1e-20, 2e-38):
+        check_far_apart(z, t, 5, temperature)
+        r = check_far_apart(z, t, 5, temperature, allowed=ok)
+        assert r.entropy[0] == 0 and r.lse[0] == -math.inf
+        check_far_apart(z.masked_fill(~ok, -math.inf), t, 0, temperature)
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
+@pytest.mark.parametrize("T,V", [(4, 3), (5, 300), (1300, 1000), (3, 9000), (400, 3000), (1, 70001)])
+def test_logprobs_logits_at_the_ends_of_fp32(T, V, dtype):
+    z = torch.zeros(T, V, device="cuda")
+    z[:, V // 2] = 3e38
+    if T > 1:
+        z[T - 1] = -3e29
+    z = z.to(dtype)
+    t = torch.full((T,), V // 2, device="cuda")
+    r = check_far_apart(z, t, 3, 1.0)
+    assert (r.entropy[:max(T - 1, 1)] == 0).all() and (r.logp[:max(T - 1, 1)] == 0).all()
