@@ -333,6 +333,7 @@ int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, const void* x
  *               gradient; a target >= classes gives NaN
  *   allowed_dev NULL, or one byte a class, not 0 where it is allowed: [rows, classes] with
  *               rows allowed_ld apart, or [classes] for all rows with allowed_ld = 0
+ *   temperature 2^-126 .. 1e27
  *   top         0 .. 32; top_logp_dev, top_index_dev [rows, top]
  * A logit at or below -1e30 counts as not allowed.  A row without an allowed class has
  * lse = logp = -inf and entropy 0; alternatives that do not exist have index -1 and

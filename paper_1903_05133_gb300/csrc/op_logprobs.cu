@@ -8,6 +8,7 @@
 // partial sums of threads and CTAs join by the same rule.  Sums are in units of log 2, since
 // the hardware's exponential is 2^x.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "op_common.cuh"
@@ -885,11 +886,14 @@ cudaError_t backward_type(const BwdArgs& a, cudaStream_t s) {
   return a.allowed ? launch_backward<T, false, true>(a, s) : launch_backward<T, false, false>(a, s);
 }
 
+// Below 2^-126 the temperature's inverse is infinite; above, a class that is raised to kNone would be
+// so close to the others that it had a probability.
+constexpr float kMaxTemperature = 1e27f;
 bool shape_ok(int type, int64_t rows, int64_t classes, int64_t ld, const void* logits,
               const void* targets, int target_bytes, int64_t allowed_ld, float temperature) {
   return type_ok(type) && rows >= 0 && classes >= 1 && classes <= 0x7FFFFFFF && ld >= classes &&
          (target_bytes == 4 || target_bytes == 8) && (allowed_ld == 0 || allowed_ld >= classes) &&
-         temperature > 0 && std::isfinite(temperature) && (rows == 0 || (logits && targets)) &&
+         temperature >= FLT_MIN && temperature <= kMaxTemperature && (rows == 0 || (logits && targets)) &&
          reinterpret_cast<uintptr_t>(logits) % type_size(type) == 0;
 }
 

@@ -231,7 +231,7 @@ def _logits(logits, targets, allowed, temperature):
     if not (targets.is_cuda and targets.dtype in (torch.int32, torch.int64) and
             targets.dim() == 1 and targets.shape[0] == T and targets.is_contiguous()):
         raise ValueError("targets must be a contiguous CUDA int32 or int64 vector, one entry a row")
-    _need(0 < temperature < float("inf"), "temperature must be positive and finite")
+    _need(2.0 ** -126 <= temperature <= 1e27, "temperature must be in [2^-126, 1e27]")
     if allowed is None:
         return ld, None, 0
     if not (allowed.is_cuda and allowed.dtype in (torch.bool, torch.uint8) and

@@ -64,3 +64,20 @@ def test_adamw_eps_without_a_finite_reciprocal_is_refused(lib):
     lib.hier_avg_adamw_destroy(h)
     with pytest.raises(ValueError, match="eps"):
         ops.AdamW([Stand(F, (4,))], eps=1e-40)
+
+
+def test_temperatures_without_a_finite_inverse_or_that_let_masked_classes_in_are_refused(lib):
+    import ctypes
+
+    from test_operators_abi import EINVAL, P
+    fwd = lambda t, rows=0: lib.hier_avg_token_logprobs(P, 1, rows, 100, 100, P, 4, None, 0, t, 3, P, P, P, P, P, None)  # noqa: E731
+    bwd = lambda t: lib.hier_avg_token_logprobs_backward(P, 1, 0, 100, 100, P, 4, None, 0, t, P, P, P, P, P, 100, None)  # noqa: E731
+    logits, targets = Stand(BF, (3, 10)), Stand(I32, (3,))
+    for t in (2.0 ** -127, 1e-45, 1.1e27, 3e38, float("inf"), float("nan"), -1.0, 0.0):
+        t = ctypes.c_float(t).value
+        assert fwd(t) == EINVAL and bwd(t) == EINVAL, t
+        with pytest.raises(ValueError, match="temperature"):
+            ops._logits(logits, targets, None, t)
+    for t in (2.0 ** -126, 1.0, 9.9e26):
+        assert fwd(t) == 0 and bwd(t) == 0, t
+        ops._logits(logits, targets, None, t)
