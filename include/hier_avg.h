@@ -347,7 +347,9 @@ int hier_avg_token_logprobs(const void* logits_dev, int type, int64_t rows, int6
 /* The gradient with respect to the logits, from the forward's lse and entropy and the
  * gradients dlogp_dev and dentropy_dev [rows] (dentropy_dev NULL: zero, and entropy_dev is
  * not read).  dlogits_dev has the logits' type and may be logits_dev itself (with the same
- * ld).  Zero where a class is not allowed. */
+ * ld).  Zero where a class is not allowed, and in a row without an allowed class.  A target
+ * >= classes, or a row whose lse is NaN, gives NaN (where allowed_dev does not say no).  The
+ * probabilities are as exact as lse, which holds its value to 24 bits. */
 int hier_avg_token_logprobs_backward(const void* logits_dev, int type, int64_t rows,
                                      int64_t classes, int64_t ld, const void* targets_dev,
                                      int target_bytes, const uint8_t* allowed_dev,

@@ -706,7 +706,7 @@ __global__ void __launch_bounds__(kBwdThreads) k_logprobs_backward(const __grid_
   const float lse0 = a.lse[row];
   const bool none = lse0 == -INFINITY;           // nothing allowed: no gradient
   const float lse = none ? INFINITY : lse0;      // every p is then 0
-  const float g = t64 < 0 || none ? 0.0f : a.dlogp[row] * a.inv_t;
+  const float g = t64 < 0 || none ? 0.0f : t64 >= a.classes ? NAN : a.dlogp[row] * a.inv_t;
   const float h0 = ENT && !none ? a.dentropy[row] * a.inv_t : 0.0f;
   const float h = h0 * kLn2;                     // d is in units of log 2
   const float k = ENT && !none ? fmaf(h0, a.entropy[row], g) : g;
@@ -776,7 +776,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_logprobs_row_backward(const 
     const float lse0 = a.lse[row];
     const bool none = lse0 == -INFINITY;
     const float lse = none ? INFINITY : lse0;
-    const float g = t64 < 0 || none ? 0.0f : a.dlogp[row] * a.inv_t;
+    const float g = t64 < 0 || none ? 0.0f : t64 >= classes ? NAN : a.dlogp[row] * a.inv_t;
     const float h0 = ENT && !none ? a.dentropy[row] * a.inv_t : 0.0f;
     const float h = h0 * kLn2, k = ENT && !none ? fmaf(h0, a.entropy[row], g) : g;
     for (int j0 = lane; j0 < classes; j0 += 32 * kRowUnroll) {

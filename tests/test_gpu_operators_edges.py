@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_1903_05133_gb300 import operators as ops
-from test_gpu_operators import BF, F, HF, close, gen
+from test_gpu_operators import BF, F, HF, close, gen, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -133,3 +133,26 @@ def test_logprobs_logits_at_the_ends_of_fp32(T, V, dtype):
     t = torch.full((T,), V // 2, device="cuda")
     r = check_far_apart(z, t, 3, 1.0)
     assert (r.entropy[:max(T - 1, 1)] == 0).all() and (r.logp[:max(T - 1, 1)] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
+@pytest.mark.parametrize("T,V", [(3, 10), (1300, 600), (2, 5000)])
+@pytest.mark.parametrize("entropy", [False, True])
+def test_gradient_of_a_target_that_is_no_class(T, V, dtype, entropy):
+    # as its log probability: NaN, and only in its row; a target below 0 has none
+    g = gen(V)
+    z = randn(g, T, V, dtype=dtype, std=2.0)
+    ok = torch.rand(T, V, generator=g, device="cuda") < 0.7
+    ok[:, 0] = True
+    t = torch.randint(0, V, (T,), generator=g, device="cuda")
+    t[0], t[1] = V, -3
+    ones = torch.ones(T, device="cuda")
+    for allowed in (None, ok):
+        f = ops.token_logprobs(z, t, allowed=allowed)
+        assert f.logp[0].isnan() and f.logp[1] == 0
+        d = ops.token_logprobs_backward(z, t, f.lse, f.entropy, ones, ones if entropy else None, allowed=allowed)
+        assert d[1:].isfinite().all()
+        if allowed is None:
+            assert d[0].isnan().all()
+        else:
+            assert d[0][ok[0]].isnan().all() and (d[~ok] == 0).all()
