@@ -286,7 +286,8 @@ int hier_avg_profile_read(hier_avg* h, int kind, double* total_ms, int64_t* laun
  *   hier_avg_grouped_product_dx  dx[t] = W_g^T dy[t], zero where h[t] <= 0 (h_dev != NULL)
  *   hier_avg_grouped_product_dw  dW_g  = sum over the group's t of dy[t] x[t]^T, and with
  *                                db_dev db_g = sum of dy[t]; zero for an empty group
- * Rows of y and dx that belong to no group are set to zero.
+ * Rows of y and dx that belong to no group are set to zero; where offsets go back, a row of y or
+ * dx that lies in two groups is the first one's (dW and db count it in both).
  *   type          HA_TYPE_BF16 or HA_TYPE_FP16, of x, w, dy and h; products are exact and
  *                 summed in fp32
  *   y_type, ...   the inputs' type (rounded once) or HA_TYPE_FP32

@@ -107,6 +107,24 @@ __device__ __forceinline__ void make_table(const Table& s, const Args& a) {
   }
   __syncthreads();
   if (tid < 32) {
+    if (MODE != kDw) {
+      // Offsets that go back would put rows into two groups, whose tiles then write them without
+      // order.  Each start is raised to the largest before it, so that a row is its first group's.
+      int top = 0;
+      for (int g0 = 0; g0 <= a.groups; g0 += 32) {
+        const int g = g0 + lane, x = g <= a.groups ? s.off[g] : 0;
+        int y = x;
+        const int before = __shfl_up_sync(~0u, x, 1);
+        if (__any_sync(~0u, g <= a.groups && x < (lane ? before : top))) {
+          y = max(y, top);
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) y = max(y, __shfl_up_sync(~0u, y, o));
+          if (g <= a.groups) s.off[g] = y;
+        }
+        top = __shfl_sync(~0u, y, min(31, a.groups - g0));
+      }
+      __syncwarp();
+    }
     const int mt = (a.m + M - 1) / M, nt = (a.n + NT - 1) / NT + (MODE == kDw && a.db ? 1 : 0);
     int run = 0;
     for (int g0 = 0; g0 < a.groups; g0 += 32) {

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_1903_05133_gb300 import operators as ops
-from test_gpu_operators import BF, F, HF, close, gen, randn
+from test_gpu_operators import BF, F, HF, assert_within, close, gen, product_bound, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -156,3 +156,39 @@ def test_gradient_of_a_target_that_is_no_class(T, V, dtype, entropy):
             assert d[0].isnan().all()
         else:
             assert d[0][ok[0]].isnan().all() and (d[~ok] == 0).all()
+
+
+@pytest.mark.parametrize("T,K,N,off", [
+    (100, 64, 40, [0, 50, 20]), (100, 72, 136, [0, 30, 10, 200]), (200, 96, 72, [-5, 30, 10, 1000]),
+    (9, 2056, 130, [0, 5, 3, 4, 9, 2]), (700, 512, 520, [100, 400, 50, 350, 600, 20]), (3000, 264, 2568, [7, 2500, 1, 2999, 2000]),
+    (640, 80, 24, [(i * 37) % 641 for i in range(70)]), (5000, 136, 264, [4000 - i if i % 3 else i for i in range(40)])])
+@pytest.mark.parametrize("out", [BF, F])
+def test_offsets_that_go_back_leave_each_row_to_its_first_group(T, K, N, off, out):
+    g = gen(T + K)
+    G = len(off) - 1
+    at = torch.tensor(off, dtype=torch.int32, device="cuda")
+    owner, top = [-1] * T, 0
+    clamped = [min(max(o, 0), T) for o in off]
+    for i in range(G):
+        top = max(top, clamped[i])
+        for r in range(top, clamped[i + 1]):
+            owner[r] = i
+    x, w = randn(g, T, K, dtype=BF), randn(g, G, N, K, dtype=BF, std=K ** -0.5)
+    dy = randn(g, T, N, dtype=BF)
+    h = randn(g, T, K, dtype=BF)
+    first = None
+    for _ in range(3):
+        y = ops.grouped_product(x, w, at, out=torch.full((T, N), 9.0, dtype=out, device="cuda"))
+        dx = ops.grouped_product_dx(dy, w, at, h=h, out=torch.full((T, K), 9.0, dtype=out, device="cuda"))
+        assert first is None or (torch.equal(first[0], y) and torch.equal(first[1], dx))
+        first = y, dx
+    for i in range(-1, G):
+        rows = torch.tensor([r for r in range(T) if owner[r] == i], device="cuda", dtype=torch.int64)
+        if i < 0:
+            assert (y[rows] == 0).all() and (dx[rows] == 0).all()
+        elif len(rows):
+            m = w[i].double()
+            assert_within(y[rows], x[rows].double() @ m.T, product_bound(x[rows].double() @ m.T, x[rows].double().abs() @ m.T.abs(), K, out))
+            ref = dy[rows].double() @ m
+            assert_within(dx[rows], ref * (h[rows] > 0), product_bound(ref, dy[rows].double().abs() @ m.abs(), N, out))
+    ops.operator_check()
