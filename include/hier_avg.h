@@ -295,7 +295,8 @@ int hier_avg_profile_read(hier_avg* h, int kind, double* total_ms, int64_t* laun
  *                 rows.  bias_dev [groups, outer] and db_dev fp32, rows bias_ld / db_ld apart
  *   relu          1: act(v) = max(v, 0), 0: act(v) = v
  *   workspace_dev 16-byte aligned, of the bytes that hier_avg_grouped_product_workspace says
- *                 (0 for operands whose address and strides are multiples of 16 bytes;
+ *                 (0 for operands whose address and strides are multiples of 16 bytes and
+ *                 whose groups and rows do not overlap;
  *                 others are first copied there, and a weights' gradient of few tiles over
  *                 many rows has its parts there before they are added)
  * Errors: HA_EINVAL for sizes, types, strides or pointers out of range, HA_ENOMEM for a

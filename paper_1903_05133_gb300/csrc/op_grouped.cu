@@ -1083,13 +1083,17 @@ struct Parts {
 };
 
 // One operand as the tensor maps need it: address, strides and width multiples of 16 bytes (the
-// edge of a map is only sure to cut whole 16-byte pieces).
+// edge of a map is only sure to cut whole 16-byte pieces), and no two entries in one place (what
+// a map with overlapping dimensions cuts off is not safe from being touched).
 struct Operand {
   const void* p;
   int64_t groups, rows, cols, ld, gs;   // gs: between groups (groups > 1)
+  bool apart() const {                  // groups after one another, or their rows in turn
+    return gs >= (rows - 1) * ld + cols || (gs >= cols && ld >= (groups - 1) * gs + cols);
+  }
   bool fits() const {
     return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0 && cols % 8 == 0 &&
-           (groups == 1 || (gs > 0 && gs % 8 == 0));   // one matrix for all groups is copied
+           (groups == 1 || (gs % 8 == 0 && apart()));   // one matrix for all groups is copied
   }
   int64_t packed_bytes() const { return fits() ? 0 : round256(groups * rows * round8(cols) * 2); }
 };

@@ -111,7 +111,8 @@ def _out_type(out_dtype, out, dtype):
 def _copy_bytes(address: int, groups: int, rows: int, cols: int, ld: int, gs: int) -> int:
     """What the copy of an operand takes, 0 where the kernels can read it in place: as
     hier_avg_grouped_product_workspace counts it, without the call (3 us of a small product's 20)."""
-    if not (address & 15 or (ld | cols) & 7 or groups > 1 and (gs & 7 or gs <= 0)):
+    if not (address & 15 or (ld | cols) & 7 or groups > 1 and (gs & 7 or gs < (rows - 1) * ld + cols and not (
+            gs >= cols and ld >= (groups - 1) * gs + cols))):
         return 0
     return groups * rows * ((cols + 7) & ~7) * 2 + 255 & ~255
 

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_1903_05133_gb300 import operators as ops
-from test_gpu_operators import BF, F, HF, assert_within, close, gen, product_bound, randn
+from test_gpu_operators import BF, F, HF, assert_within, close, gen, offsets_of, product_bound, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -191,4 +191,20 @@ def test_offsets_that_go_back_leave_each_row_to_its_first_group(T, K, N, off, ou
             assert_within(y[rows], x[rows].double() @ m.T, product_bound(x[rows].double() @ m.T, x[rows].double().abs() @ m.T.abs(), K, out))
             ref = dy[rows].double() @ m
             assert_within(dx[rows], ref * (h[rows] > 0), product_bound(ref, dy[rows].double().abs() @ m.abs(), N, out))
+    ops.operator_check()
+
+
+@pytest.mark.parametrize("N,K,step", [(24, 64, 8), (24, 64, 64), (130, 72, 72), (1, 64, 8), (300, 128, 128), (40, 64, 0)])
+def test_weights_whose_groups_overlap(N, K, step):
+    # windows of one buffer, `step` further on for each group, and the groups' rows in turn
+    g = gen(N + step)
+    sizes = [3, 0, 70, 41]
+    T, off = sum(sizes), offsets_of(sizes)
+    flat = randn(g, 3 * step + N * K, dtype=BF)
+    turn = randn(g, N, 4 * K, dtype=BF)
+    x, dy = randn(g, T, K, dtype=BF), randn(g, T, N, dtype=BF)
+    for w in (flat.as_strided((4, N, K), (step, K, 1)), turn.as_strided((4, N, K), (K, 4 * K, 1))):
+        own = w.contiguous()
+        assert torch.equal(ops.grouped_product(x, w, off), ops.grouped_product(x, own, off))
+        assert torch.equal(ops.grouped_product_dx(dy, w, off), ops.grouped_product_dx(dy, own, off))
     ops.operator_check()

@@ -81,3 +81,25 @@ def test_temperatures_without_a_finite_inverse_or_that_let_masked_classes_in_are
     for t in (2.0 ** -126, 1.0, 9.9e26):
         assert fwd(t) == 0 and bwd(t) == 0, t
         ops._logits(logits, targets, None, t)
+
+
+def test_weights_whose_groups_overlap_are_copied_first(lib):
+    # a tensor map of them would have overlapping dimensions
+    import ctypes
+    G, N, K, T = 5, 24, 64, 40
+    n = ctypes.c_int64(-1)
+
+    def bytes_of(ld, gs, N=N, G=G):
+        seen = set()
+        for op, cols in ((ops.FORWARD, K), (ops.DX, N)):
+            a = ctypes.c_void_p(1 << 20)
+            assert lib.hier_avg_grouped_product_workspace(op, a, 64, a, ld, gs, G, T, K, N, ctypes.byref(n)) == 0
+            seen.add(n.value - ops._copy_bytes(1 << 20, 1, T, cols, 64, 0))
+        assert seen == {ops._copy_bytes(1 << 20, G, N, K, ld, gs)}
+        return seen.pop()
+    copy = -(-G * N * K * 2 // 256) * 256
+    assert bytes_of(K, N * K) == 0 and bytes_of(K + 8, N * (K + 8)) == 0
+    assert bytes_of(K, (N - 1) * K + K) == 0 and bytes_of(G * K, K) == 0        # rows of the groups in turn
+    for ld, gs in ((K, 0), (K, 8), (K, K), (K, (N - 1) * K), (G * K - 8, K), (G * K, K - 8)):
+        assert bytes_of(ld, gs) == copy, (ld, gs)
+    assert bytes_of(K, K, N=1) == 0 and bytes_of(K, K - 8, N=1) > 0 and bytes_of(K, 8, G=1) == 0
