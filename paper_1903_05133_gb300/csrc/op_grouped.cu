@@ -31,11 +31,13 @@ constexpr int kDwThreads = kThreads + 32;               // and the ends of group
 constexpr int kPairCols = 256;          // columns of a tile of two CTAs
 constexpr int kMinChunks = 8;           // of each of the CTAs that share a tile
 constexpr int kMaxSplit = 8;            // CTAs that share a tile's summed length
-// fp32 results: the tensor core's running sum is taken into fp32 registers after this many
-// chunks.  Its additions truncate; over a sum of 4096 random products that cost 4.4e-6 of the
-// result's norm, over 16384 1.9e-5, over 512 4.7e-7 (fp32 additions: 6.1e-7, 1.5e-6 and 1.6e-7).
-// A 16-bit result does not see it.
-constexpr int kFold = 8;
+// The tensor core's running sum is taken into fp32 registers after this many chunks: its additions
+// truncate, so its error grows with the length (of random products, in the result's norm: 512
+// values 4.7e-7, 4096 4.4e-6, 16384 1.9e-5; fp32 additions 1.6e-7, 6.1e-7 and 1.5e-6.  Of positive
+// ones about 8e-9 a value: 2^18 of them 2.1e-3).
+constexpr int kFold32 = 8, kFold16 = 64;        // of fp32 and of 16-bit results
+// Results of a pair's tile: 16 bits from one running sum, fp32, or 16 bits from folded sums.
+constexpr int kWhole = 0, kWide = 1, kFolded = 2;
 
 struct Args {
   const int* offsets;
@@ -394,14 +396,19 @@ struct Ring {
   __device__ __forceinline__ uint32_t next_round() const { return st + 1 == STAGES ? round ^ 1 : round; }
 };
 
+template <int RES>
+__device__ __forceinline__ int fold_of(bool bias) {
+  return RES == kWide || bias ? kFold32 : RES == kFolded ? kFold16 : 1 << 30;
+}
+
 // One tile's results: `half` of its NT columns, from the sums in TMEM, segment by segment.
-template <int MODE, int NT, bool FOLD, typename Wait, typename Free>
+template <int MODE, int NT, int RES, typename Wait, typename Free>
 __device__ __forceinline__ bool finish_tile(const Args& a, const Tile& t, uint32_t tmem,
                                             int cta_m0, unsigned char* stage, uint32_t& seg, uint32_t& turn,
                                             Wait wait, Free release) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2, quad = warp & 3;
-  const int nk = (t.k + kK - 1) / kK;
-  const int segs = FOLD || t.bias ? (nk + kFold - 1) / kFold : (nk > 0 ? 1 : 0);
+  const int nk = (t.k + kK - 1) / kK, fold = fold_of<RES>(t.bias);
+  const int segs = (nk + fold - 1) / fold;
   constexpr int H = NT / 2;
   const int cb = half * H, ce = min(H, t.cols - cb);      // this warp group's columns
   const int f = cta_m0 + quad * 32 + lane;                // this thread's feature
@@ -410,7 +417,7 @@ __device__ __forceinline__ bool finish_tile(const Args& a, const Tile& t, uint32
   auto emit = [&](const float* v, int j) {
     if (MODE == kDw)
       emit_weights(a, v, t.g, cta_m0 + quad * 32, t.c0 + cb + j, t.c0 + cb + ce, stage + warp * kWarpStage);
-    else if (FOLD)
+    else if (RES == kWide)
       emit_rows<MODE, float>(a, v, t.c0 + cb + j, min(STEP, ce - j), cta_m0, quad * 32 + lane, bias,
                              stage + half * kRowsStage, 1 + half, turn);
     else
@@ -438,7 +445,7 @@ __device__ __forceinline__ bool finish_tile(const Args& a, const Tile& t, uint32
     if (half == 0 && f < a.m) a.db[t.g * a.bias_ld + f] = sum;
     return true;
   }
-  if (!FOLD) {
+  if (RES == kWhole) {
     if (segs && !wait(seg)) return false;
     if (MODE == kDw && segs) {
       // all of a half's reads are under way before the first is used
@@ -504,7 +511,7 @@ struct One {
   static constexpr int kSmem = kStages * (kA + kB) + kOut + 1024;
 };
 
-template <int MODE, bool FOLD, int NT>
+template <int MODE, bool WIDE, int NT>
 __global__ void __launch_bounds__(kThreads, 1)
     k_grouped_one(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
                   const __grid_constant__ Args a) {
@@ -546,6 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int tiles = tab.first[a.groups], i0 = blockIdx.x / split, step = gridDim.x / split;
   const int all = (a.k + kK - 1) / kK;                     // chunks of a tile, and this CTA's
   const int c0 = all * rank / split, c1 = all * (rank + 1) / split;
+  constexpr int fold = WIDE ? kFold32 : kFold16;
   bool ok = true;                                         // of the results' warps
   uint32_t round = 0;
   clear_rows(a, 0, tab.off[0]);
@@ -583,7 +591,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       Ring<S::kStages> at;
       uint32_t seg = 0;
       bool ok = true, peek = false;
-      constexpr int fold = FOLD ? kFold : 1 << 30;
       for (int i = i0; i < tiles && ok; i += step) {
         const Tile t = list.at(i);
         const uint32_t idesc = idesc_of(a.in_type, kM, (t.cols + 15) / 16 * 16) | (MODE == kFwd ? 0u : 1u << 15);
@@ -620,7 +627,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---- results
     constexpr int H = NT / 2;                             // columns of a warp group
     const int half = warp >> 2, quad = warp & 3, feature = quad * 32 + lane;
-    const int segs = FOLD ? (c1 - c0 + kFold - 1) / kFold : (c1 > c0 ? 1 : 0);
+    const int segs = (c1 - c0 + fold - 1) / fold;
     float* got = reinterpret_cast<float*>(Out);           // [CTA][column][feature]
     float* part = reinterpret_cast<float*>(Out + S::kPart);                 // [column][feature]
     uint32_t seg = 0, turn = 0;
@@ -685,7 +692,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float bias = MODE == kFwd && a.bias && f < a.m ? a.bias[t.g * a.bias_ld + f] : 0.0f;
       const int first = split > 1 ? rank * per : cb, n = split > 1 ? own : min(H, ce);
       if (n > 0) {
-        if (FOLD)
+        if (WIDE)
           emit_rows<MODE, float>(a, acc, t.c0 + first, n, t.m0, feature, bias, Out + half * kRowsStage, 1 + half, turn);
         else
           emit_rows<MODE, uint16_t>(a, acc, t.c0 + first, n, t.m0, feature, bias, Out + half * kRowsStage, 1 + half, turn);
@@ -723,7 +730,7 @@ struct Pair {
 };
 static_assert(2 * kRowsStage == kEpiWarps * kWarpStage, "one buffer serves both kinds of results");
 
-template <int MODE, bool FOLD>
+template <int MODE, int RES>
 __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __cluster_dims__(2, 1, 1)
     k_grouped_pair(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
                    const __grid_constant__ Args a) {
@@ -822,7 +829,7 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
       for (int i = pair; i < tiles && ok; i += pairs) {
         const Tile t = list.at(i);
         const int nk = (t.k + kK - 1) / kK, N = (t.cols + 31) / 32 * 32;
-        const int fold = FOLD || t.bias ? kFold : 1 << 30;
+        const int fold = fold_of<RES>(t.bias);
         const uint32_t idesc = idesc_of(a.in_type, 2 * kM, N) | (MODE == kFwd ? 0u : 1u << 15) |
                                (MODE == kDw ? 1u << 16 : 0u);
         const int odd = t.k % kK;
@@ -886,7 +893,7 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
     bool ok = true;
     for (int i = pair; i < tiles && ok; i += pairs) {
       const Tile t = list.at(i);
-      ok = finish_tile<MODE, kPairCols, FOLD>(
+      ok = finish_tile<MODE, kPairCols, RES>(
           a, t, tmem, t.m0 + rank * kM, Out, seg, turn,
           [&](uint32_t s) {
             return warp_wait(&tfull[s & 1], (s >> 1) & 1);
@@ -1188,9 +1195,9 @@ int clusters_held(K kernel, int threads, int smem, int size) {
 }
 
 // `tiles`: about how many there are; `most`: at most.
-template <int MODE, bool FOLD, int NT>
+template <int MODE, bool WIDE, int NT>
 int launch_one(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int64_t tiles, int64_t most, cudaStream_t s) {
-  const auto kernel = k_grouped_one<MODE, FOLD, NT>;
+  const auto kernel = k_grouped_one<MODE, WIDE, NT>;
   constexpr int smem = One<NT>::kSmem;
   static bool allowed[kMaxDevices];
   if (allow_smem(kernel, smem, allowed) != cudaSuccess) return HA_ECUDA;
@@ -1220,19 +1227,30 @@ int launch_one(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int6
   return cudaLaunchKernelEx(&cfg, kernel, ta, tb, a) == cudaSuccess ? HA_OK : HA_ECUDA;
 }
 
-template <int MODE, bool FOLD>
-int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int64_t most, cudaStream_t s) {
+template <int MODE, int RES>
+int launch_pair_of(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int64_t most, cudaStream_t s) {
   static bool allowed[kMaxDevices];
-  if (allow_smem(k_grouped_pair<MODE, FOLD>, Pair::kSmem, allowed) != cudaSuccess) return HA_ECUDA;
+  if (allow_smem(k_grouped_pair<MODE, RES>, Pair::kSmem, allowed) != cudaSuccess) return HA_ECUDA;
   // As many pairs as the GPU holds at once (its clusters of two leave some SMs out): the tiles
   // are dealt out in advance, so a pair that started late would finish late.
   constexpr int threads = MODE == kDw ? kDwThreads : kThreads;
   static int held = 0;
-  if (held == 0) held = clusters_held(k_grouped_pair<MODE, FOLD>, threads, Pair::kSmem, 2);
+  if (held == 0) held = clusters_held(k_grouped_pair<MODE, RES>, threads, Pair::kSmem, 2);
   if (held < 1) return HA_ECUDA;
   const int64_t pairs = std::min<int64_t>(held, std::max<int64_t>(most, 1));
-  k_grouped_pair<MODE, FOLD><<<static_cast<unsigned>(2 * pairs), threads, Pair::kSmem, s>>>(ta, tb, a);
+  k_grouped_pair<MODE, RES><<<static_cast<unsigned>(2 * pairs), threads, Pair::kSmem, s>>>(ta, tb, a);
   return cudaGetLastError() == cudaSuccess ? HA_OK : HA_ECUDA;
+}
+
+// A sum of this many values at most stays whole in a 16-bit result: what truncating costs is then an
+// eighth of the type's rounding at worst.  (The gradient of weights of 32 groups, 16384
+// rows, 4096 to 4096, bf16: 391 us whole, 425 folded; of 8 groups, 65536 rows, 2048 to 2048: 297 and 301.)
+int64_t whole_sum(int type) { return type == HA_TYPE_BF16 ? 65536 : 8192; }
+template <int MODE>
+int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int64_t length, int64_t most, cudaStream_t s) {
+  if (a.out_type == HA_TYPE_FP32) return launch_pair_of<MODE, kWide>(ta, tb, a, most, s);
+  if (length > whole_sum(a.out_type)) return launch_pair_of<MODE, kFolded>(ta, tb, a, most, s);
+  return launch_pair_of<MODE, kWhole>(ta, tb, a, most, s);
 }
 
 bool half_type(int t) { return t == HA_TYPE_BF16 || t == HA_TYPE_FP16; }
@@ -1253,7 +1271,7 @@ int rows_product(Operand x, Operand w, Args a, void* ws, int64_t ws_bytes, cudaS
   if (pack(x, w, a.offsets, a.rows, p, s) != cudaSuccess) return HA_ECUDA;
   a.wide_out = (reinterpret_cast<uintptr_t>(a.out) & 15) == 0 && a.out_ld * type_size(a.out_type) % 16 == 0;
   a.wide_h = a.h && (reinterpret_cast<uintptr_t>(a.h) & 15) == 0 && a.h_ld % 8 == 0;
-  const bool fold = a.out_type == HA_TYPE_FP32;
+  const bool wide = a.out_type == HA_TYPE_FP32;
   const int64_t rows = a.rows, used = std::min<int64_t>(rows, a.groups);      // groups with rows, about
   const int64_t m1 = (a.m + kM - 1) / kM, m2 = (a.m + 2 * kM - 1) / (2 * kM);
   // Few rows a group: narrow tiles.  So few rows in all that pairs would leave most SMs idle:
@@ -1268,16 +1286,16 @@ int rows_product(Operand x, Operand w, Args a, void* ws, int64_t ws_bytes, cudaS
     return HA_ECUDA;
   if (few) {
     const int64_t tiles = m1 * used, most = m1 * std::min<int64_t>(rows, a.groups + rows / 32);
-    return fold ? launch_one<MODE, true, 32>(ta, tb, a, tiles, most, s)
+    return wide ? launch_one<MODE, true, 32>(ta, tb, a, tiles, most, s)
                 : launch_one<MODE, false, 32>(ta, tb, a, tiles, most, s);
   }
   if (small) {
     const int64_t tiles = m1 * std::max<int64_t>(used, (rows + 63) / 64), most = m1 * std::min<int64_t>(rows, a.groups + rows / 64);
-    return fold ? launch_one<MODE, true, 64>(ta, tb, a, tiles, most, s)
+    return wide ? launch_one<MODE, true, 64>(ta, tb, a, tiles, most, s)
                 : launch_one<MODE, false, 64>(ta, tb, a, tiles, most, s);
   }
   const int64_t most = m2 * std::min<int64_t>(rows, a.groups + rows / kPairCols);
-  return fold ? launch_pair<MODE, true>(ta, tb, a, most, s) : launch_pair<MODE, false>(ta, tb, a, most, s);
+  return launch_pair<MODE>(ta, tb, a, a.k, most, s);
 }
 
 }  // namespace
@@ -1421,8 +1439,8 @@ extern "C" int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, co
   const int64_t most = a.groups * static_cast<int64_t>((outer + 2 * kM - 1) / (2 * kM)) *
                        ((inner + kPairCols - 1) / kPairCols + (db_dev ? 1 : 0));
   if (most > 0x7FFFFFFF) return HA_EUNSUPPORTED;
-  const int status = a.out_type == HA_TYPE_FP32 ? launch_pair<kDw, true>(ta, tb, a, most, s)
-                                                : launch_pair<kDw, false>(ta, tb, a, most, s);
+  // the groups' lengths are not known here: one of them may have all rows
+  const int status = launch_pair<kDw>(ta, tb, a, rows, most, s);
   if (status != HA_OK || parts.split == 1) return status;
   Join j = {};
   j.part = static_cast<const float*>(a.out);

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_1903_05133_gb300 import operators as ops
-from test_gpu_operators import BF, F, HF, assert_within, close, gen, offsets_of, product_bound, randn
+from test_gpu_operators import BF, F, HF, U, assert_within, close, gen, offsets_of, product_bound, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -207,4 +207,44 @@ def test_weights_whose_groups_overlap(N, K, step):
         own = w.contiguous()
         assert torch.equal(ops.grouped_product(x, w, off), ops.grouped_product(x, own, off))
         assert torch.equal(ops.grouped_product_dx(dy, w, off), ops.grouped_product_dx(dy, own, off))
+    ops.operator_check()
+
+
+@pytest.mark.parametrize("dtype", [HF, BF])
+def test_product_dw_long_sums_keep_their_precision(dtype):
+    # 2^20 rows of one group among 40 that are too many tiles to be summed in parts.  Every product is
+    # positive, so that an addition that truncates is off the same way every time.  The bound does not
+    # grow with the length: the result's rounding, and those of sums of a few thousand products.
+    g = gen(40)
+    sizes = [3] * 40
+    sizes[7] = 1 << 20
+    T, N, K = sum(sizes), 40, 24
+    dy = (torch.rand(T, N, generator=g, device="cuda") * 0.2 + 0.1).to(dtype)
+    x = (torch.rand(T, K, generator=g, device="cuda") * 0.2 + 0.1).to(dtype)
+    dw = ops.grouped_product_dw(dy, x, offsets_of(sizes))
+    a, b = dy[21:21 + sizes[7]].double(), x[21:21 + sizes[7]].double()
+    ref = a.T @ b
+    assert ref.max() < 65000
+    assert ((dw[7].double() - ref).abs() <= (U[dtype] + 2.0 ** -14) * ref).all(), ((dw[7].double() - ref).abs() / ref).max()
+    ref = dy[:3].double().T @ x[:3].double()
+    assert ((dw[0].double() - ref).abs() <= (U[dtype] + 2.0 ** -20) * ref).all()
+    ops.operator_check()
+
+
+@pytest.mark.parametrize("T,N", [(3, 136), (300, 136), (1024, 2560)])
+@pytest.mark.parametrize("dx", [False, True])
+def test_product_long_sums_keep_their_precision(T, N, dx):
+    # the same of the rows' products: by clusters, by single CTAs and by pairs, K = 2^18
+    g = gen(T)
+    K = 1 << 18
+    x = torch.rand(T, K, generator=g, device="cuda", dtype=HF) * 0.4 + 0.2
+    w = torch.rand(2, N, K, generator=g, device="cuda", dtype=HF) * 0.4 + 0.2
+    off = offsets_of([T // 3, T - T // 3])
+    if dx:
+        y = ops.grouped_product_dx(x, w.transpose(1, 2).contiguous(), off)
+    else:
+        y = ops.grouped_product(x, w, off)
+    for g0, rows in ((0, slice(0, 1)), (1, slice(T - 2, T))):
+        ref = x[rows].double() @ w[g0].double().T
+        assert ((y[rows].double() - ref).abs() <= (2.0 ** -11 + 2.0 ** -14) * ref).all(), ((y[rows].double() - ref).abs() / ref).max()
     ops.operator_check()
