@@ -27,7 +27,7 @@ constexpr int kK = 64;                  // values summed over in a chunk: one 12
 constexpr int kMaxGroups = 1024;
 constexpr int kEpiWarps = 8;            // two groups of four: a group reads half the columns
 constexpr int kThreads = (kEpiWarps + 2) * 32;          // results, loads, products
-constexpr int kDwThreads = kThreads + 32;               // and the ends of groups
+constexpr int kDwThreads = kThreads + 64;               // and the ends of groups
 constexpr int kPairCols = 256;          // columns of a tile of two CTAs
 constexpr int kMinChunks = 8;           // of each of the CTAs that share a tile
 constexpr int kMaxSplit = 8;            // CTAs that share a tile's summed length
@@ -396,6 +396,10 @@ struct Ring {
   __device__ __forceinline__ uint32_t next_round() const { return st + 1 == STAGES ? round ^ 1 : round; }
 };
 
+// Chunks of a summed length.  In the weights' gradient those of whole steps of 16: what is left is
+// summed from a place of its own.
+template <int MODE>
+__device__ __forceinline__ int chunks_of(int k) { return ((MODE == kDw ? k & ~15 : k) + kK - 1) / kK; }
 template <int RES>
 __device__ __forceinline__ int fold_of(bool bias) {
   return RES == kWide || bias ? kFold32 : RES == kFolded ? kFold16 : 1 << 30;
@@ -407,8 +411,8 @@ __device__ __forceinline__ bool finish_tile(const Args& a, const Tile& t, uint32
                                             int cta_m0, unsigned char* stage, uint32_t& seg, uint32_t& turn,
                                             Wait wait, Free release) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2, quad = warp & 3;
-  const int nk = (t.k + kK - 1) / kK, fold = fold_of<RES>(t.bias);
-  const int segs = (nk + fold - 1) / fold;
+  const int nk = chunks_of<MODE>(t.k), fold = fold_of<RES>(t.bias);
+  const int segs = MODE == kDw && nk == 0 && t.k > 0 ? 1 : (nk + fold - 1) / fold;
   constexpr int H = NT / 2;
   const int cb = half * H, ce = min(H, t.cols - cb);      // this warp group's columns
   const int f = cta_m0 + quad * 32 + lane;                // this thread's feature
@@ -726,18 +730,25 @@ struct Pair {
   static constexpr int kA = kM * kK * 2, kB = kPairCols / 2 * kK * 2, kStages = 5;
   static constexpr int kOut = 2 * kRowsStage;             // = kEpiWarps * kWarpStage
   static constexpr int kOnes = 8192;                      // dW: a column block of ones, for the bias
-  static constexpr int kSmem = kStages * (kA + kB) + kOut + kOnes + 1024;
+  static constexpr int kEnd = 8192;                       // dW: the last rows of a group, two of them
+  static constexpr int kSmem = kStages * (kA + kB) + kOut + kOnes + 2 * kEnd + 1024;
 };
 static_assert(2 * kRowsStage == kEpiWarps * kWarpStage, "one buffer serves both kinds of results");
+
+// Maps with boxes of 16 rows, for the last rows of groups in the weights' gradient.
+template <int MODE> struct Ends {};
+template <> struct Ends<kDw> { CUtensorMap a, b; };
 
 template <int MODE, int RES>
 __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __cluster_dims__(2, 1, 1)
     k_grouped_pair(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
-                   const __grid_constant__ Args a) {
+                   const __grid_constant__ Ends<MODE> ends, const __grid_constant__ Args a) {
   extern __shared__ unsigned char raw[];
-  // full: the first CTA's, on which both CTAs' loads and two arrivals are counted.  tempty: the
-  // first CTA's too.  tail: this CTA's load of a chunk in which a group ends.
-  __shared__ uint64_t full[Pair::kStages], empty[Pair::kStages], tfull[2], tempty[2], tail[Pair::kStages];
+  // full: the first CTA's, on which both CTAs' loads are counted.  tempty: the first CTA's too.  Of a
+  // group's last rows, end_load: they are in this CTA; end_peer: the second CTA's are ready; end_full:
+  // both CTAs' are (these two the first CTA's); end_empty: summed.
+  __shared__ uint64_t full[Pair::kStages], empty[Pair::kStages], tfull[2], tempty[2];
+  __shared__ uint64_t end_load[2], end_peer[2], end_full[2], end_empty[2];
   __shared__ uint32_t tmem_at;
   __shared__ int table[2 * (kMaxGroups + 1)];
   const Table tab = {table, table + kMaxGroups + 1};
@@ -745,6 +756,7 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
   unsigned char* Bs = As + Pair::kStages * Pair::kA;
   unsigned char* Out = Bs + Pair::kStages * Pair::kB;
   unsigned char* Ones = Out + Pair::kOut;
+  unsigned char* End = Ones + Pair::kOnes;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_rank();
   if (warp == kEpiWarps) {
@@ -753,13 +765,16 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
   }
   if (tid == 0) {
     for (int i = 0; i < Pair::kStages; ++i) {
-      mbar_init(&full[i], 2);
+      mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
-      mbar_init(&tail[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&tfull[i], 1);
       mbar_init(&tempty[i], 2 * kEpiWarps);
+      mbar_init(&end_load[i], 1);
+      mbar_init(&end_peer[i], 1);
+      mbar_init(&end_full[i], 1);
+      mbar_init(&end_empty[i], 1);
     }
     fence_barrier_init();
   }
@@ -788,33 +803,26 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
       const uint32_t full0 = cluster_addr(full, 0);
       for (int i = pair; i < tiles && ok; i += pairs) {
         const Tile t = list.at(i);
-        const int nk = (t.k + kK - 1) / kK, hcols = (t.cols + 31) / 32 * 16;   // columns of a CTA
+        const int nk = chunks_of<MODE>(t.k), hcols = (t.cols + 31) / 32 * 16;  // columns of a CTA
         const int m0 = t.m0 + rank * kM, h0 = rank * hcols, boxes = t.bias ? 0 : (hcols + 63) / 64;
         const uint32_t bytes = Pair::kA + boxes * 8192;
         for (int c = 0; c < nk; ++c, at.next()) {
           const int st = at.st, k = c * kK;
           if (!peek && !mbar_wait_hot(&empty[st], at.round ^ 1, &g_operator_error)) { ok = false; break; }
-          // dW: the rows that fill no chunk, a group's last, are loaded first, and seen first by the
-          // warp that clears what follows them.
-          const bool cut = MODE == kDw && c == 0 && t.k % kK != 0;
-          const uint32_t bar = cut ? smem_u32(&tail[st]) : full0 + st * 8;
-          uint64_t* arm = cut ? &tail[st] : &full[st];
-          const uint32_t armed = cut ? bytes : rank == 0 ? 2 * bytes : 0;
-          if (!cut && rank == 0) mbar_arrive(&full[st]);
+          const uint32_t bar = full0 + st * 8, armed = rank == 0 ? 2 * bytes : 0;
           unsigned char* A = As + st * Pair::kA;
           unsigned char* B = Bs + st * Pair::kB;
           uint64_t* next = &empty[at.next_st()];
           const uint32_t parity = at.next_round() ^ 1;
           if (MODE == kFwd) {
-            peek = tma_chunk_pair<false, false>(A, &ta, k, m0, t.g, B, &tb, k, t.r0 + h0, 0, boxes, bar, arm, armed,
+            peek = tma_chunk_pair<false, false>(A, &ta, k, m0, t.g, B, &tb, k, t.r0 + h0, 0, boxes, bar, &full[st], armed,
                                                 next, parity);
           } else if (MODE == kDx) {
-            peek = tma_chunk_pair<true, false>(A, &ta, m0, k, t.g, B, &tb, k, t.r0 + h0, 0, boxes, bar, arm, armed,
+            peek = tma_chunk_pair<true, false>(A, &ta, m0, k, t.g, B, &tb, k, t.r0 + h0, 0, boxes, bar, &full[st], armed,
                                                next, parity);
           } else {
-            const int row = t.r0 + (cut ? (nk - 1) * kK : t.k % kK != 0 ? k - kK : k);
-            peek = tma_chunk_pair<true, true>(A, &ta, m0, row, 0, B, &tb, t.c0 + h0, row, 0, boxes, bar, arm, armed, next,
-                                              parity);
+            peek = tma_chunk_pair<true, true>(A, &ta, m0, t.r0 + k, 0, B, &tb, t.c0 + h0, t.r0 + k, 0, boxes, bar, &full[st],
+                                              armed, next, parity);
           }
         }
       }
@@ -824,15 +832,15 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
     // unit 32 times as long)
     if (rank == 0 && elect_one()) {
       Ring<Pair::kStages> at;
-      uint32_t seg = 0;
+      uint32_t seg = 0, end = 0;
       bool ok = true, peek = false;
       for (int i = pair; i < tiles && ok; i += pairs) {
         const Tile t = list.at(i);
-        const int nk = (t.k + kK - 1) / kK, N = (t.cols + 31) / 32 * 32;
+        const int nk = chunks_of<MODE>(t.k), N = (t.cols + 31) / 32 * 32;
         const int fold = fold_of<RES>(t.bias);
         const uint32_t idesc = idesc_of(a.in_type, 2 * kM, N) | (MODE == kFwd ? 0u : 1u << 15) |
                                (MODE == kDw ? 1u << 16 : 0u);
-        const int odd = t.k % kK;
+        const bool tail = MODE == kDw && t.k % 16 != 0;
         int part = 0;                                       // chunks since the last fold
         for (int c = 0; c < nk; ++c, at.next()) {
           const int st = at.st, buf = seg & 1;
@@ -840,7 +848,7 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
                (peek || mbar_wait_hot(&full[st], at.round, &g_operator_error));
           if (!ok) break;
           tc_fence_after();
-          const int steps = odd && c == (MODE == kDw ? 0 : nk - 1) ? (odd + 15) / 16 : 4;
+          const int left = t.k - c * kK, steps = left >= kK ? 4 : MODE == kDw ? left / 16 : (left + 15) / 16;
           const uint32_t as = smem_u32(As + st * Pair::kA), bs = smem_u32(t.bias ? Ones : Bs + st * Pair::kB);
           const uint32_t d = tmem + buf * kPairCols;
           const uint64_t da = MODE == kFwd ? umma_desc_sw128(as) : umma_desc_sw128_mn(as, 8192);
@@ -854,38 +862,73 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
             peek = false;
           }
           if (++part == fold || c == nk - 1) {
+            if (tail && c == nk - 1) break;                 // the last sum goes on below
             tc_commit_pair(&tfull[buf]);
             ++seg;
             part = 0;
           }
         }
+        if (tail && ok) {
+          if (nk > 0) at.next();                            // which the break has left out
+          const int buf = seg & 1, e = end & 1;
+          ok = (part != 0 || mbar_wait_hot(&tempty[buf], ((seg >> 1) & 1) ^ 1, &g_operator_error)) &&
+               mbar_wait_hot(&end_full[e], (end >> 1) & 1, &g_operator_error);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t as = smem_u32(End + e * Pair::kEnd);
+          const uint64_t db = t.bias ? umma_desc_sw128_mn(smem_u32(Ones), 8192) : umma_desc_sw128_mn(as + 4096, 2048);
+          tc_mma_pair(tmem + buf * kPairCols, umma_desc_sw128_mn(as, 2048), db, idesc, part ? 1u : 0u);
+          tc_commit_pair(&end_empty[e]);
+          tc_commit_pair(&tfull[buf]);
+          ++seg;
+          ++end;
+        }
       }
     }
-  } else if (MODE == kDw && warp == kEpiWarps + 2) {
-    // ---- the ends of groups, in both CTAs: the rows after a group's last are another group's,
-    // and are cleared up to the products' next step of 16
-    Ring<Pair::kStages> at;
-    uint32_t parity = 0;                                    // of each stage's `tail`
-    for (int i = pair; i < tiles; i += pairs) {
-      const Tile t = list.at(i);
-      const int left = t.k % kK, st = at.st;
-      at.skip((t.k + kK - 1) / kK);
-      if (!left) continue;
-      bool ok = true;
-      if (lane == 0) ok = mbar_wait_hot(&tail[st], parity >> st & 1, &g_operator_error);
-      if (!__all_sync(~0u, ok)) break;
-      parity ^= 1u << st;
-      // a lane has one or two of the 16-byte columns of the (at most four) blocks
-      const int columns = 8 * (2 + (t.bias ? 0 : ((t.cols + 31) / 32 * 16 + 63) / 64));
-      for (int x = lane; x < columns; x += 32) {
-        const int b = x >> 3;
-        unsigned char* p = (b < 2 ? As + st * Pair::kA + b * 8192 : Bs + st * Pair::kB + (b - 2) * 8192) + (x & 7) * 16;
-        for (int row = left; row & 15; ++row) *reinterpret_cast<uint4*>(p + row * 128) = make_uint4(0, 0, 0, 0);
+  } else if (MODE == kDw && warp >= kEpiWarps + 2) {
+    // ---- the ends of groups, in both CTAs: the rows that fill no step of 16 are loaded by themselves,
+    // and those after them, which are another group's, cleared.  A warp has every second end, up to two
+    // tiles ahead of the products, so that there is time to tell the first CTA across the cluster.  (In
+    // the ring's own chunks, told to the products' thread by a release and seen by an acquire at cluster
+    // scope: 32 groups, 16384 rows, 4096 to 4096, 434 us, this 385; 64 groups of 47 rows, 2048 to 2048,
+    // 118 and 125, with fp32 results 255 and 226.)
+    if constexpr (MODE == kDw) {
+      uint32_t n = 0;
+      for (int i = pair; i < tiles; i += pairs) {
+        const Tile t = list.at(i);
+        const int left = t.k % 16;
+        if (!left || (n++ & 1) != static_cast<uint32_t>(warp) - (kEpiWarps + 2)) continue;
+        const int e = warp - (kEpiWarps + 2), hcols = (t.cols + 31) / 32 * 16, blocks = 2 + (t.bias ? 0 : (hcols + 63) / 64);
+        const uint32_t parity = ((n - 1) >> 1) & 1;
+        unsigned char* to = End + e * Pair::kEnd;
+        bool ok = true;
+        if (lane == 0) {
+          // the sum of two tiles before this one's end is waited for, each of up to all rows
+          ok = mbar_wait_hot(&end_empty[e], parity ^ 1, &g_operator_error, kWaitLimitCycles + a.rows / kK * 4096ll);
+          if (ok) {
+            const int m0 = t.m0 + rank * kM, c0 = t.c0 + rank * hcols, row = t.r0 + t.k - left;
+            mbar_arrive_expect_tx(&end_load[e], blocks * 2048);
+            for (int b = 0; b < blocks; ++b)
+              tma_load_3d(to + b * 2048, b < 2 ? &ends.a : &ends.b, &end_load[e], b < 2 ? m0 + b * 64 : c0 + (b - 2) * 64, row, 0);
+            ok = mbar_wait_hot(&end_load[e], parity, &g_operator_error);
+          }
+        }
+        if (!__all_sync(~0u, ok)) break;
+        for (int x = lane; x < blocks * 8; x += 32)        // 16-byte columns
+          for (int r = left; r < 16; ++r)
+            *reinterpret_cast<uint4*>(to + (x >> 3) * 2048 + (x & 7) * 16 + r * 128) = make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();                          // before the tensor cores' reads
+        __syncwarp();
+        if (lane == 0) {
+          if (rank != 0) {
+            mbar_arrive_release_cluster(cluster_addr(&end_peer[e], 0));
+          } else {
+            ok = mbar_wait_cluster(&end_peer[e], parity, &g_operator_error);
+            if (ok) mbar_arrive(&end_full[e]);
+          }
+        }
+        if (!__all_sync(~0u, ok)) break;
       }
-      // Each CTA's tensor core reads its own shared memory, where the fence has ordered the zeros.
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(cluster_addr(&full[st], 0));
     }
   } else {
     // ---- results, by both CTAs
@@ -1228,7 +1271,8 @@ int launch_one(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int6
 }
 
 template <int MODE, int RES>
-int launch_pair_of(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int64_t most, cudaStream_t s) {
+int launch_pair_of(const CUtensorMap& ta, const CUtensorMap& tb, const Ends<MODE>& ends, const Args& a, int64_t most,
+                   cudaStream_t s) {
   static bool allowed[kMaxDevices];
   if (allow_smem(k_grouped_pair<MODE, RES>, Pair::kSmem, allowed) != cudaSuccess) return HA_ECUDA;
   // As many pairs as the GPU holds at once (its clusters of two leave some SMs out): the tiles
@@ -1238,7 +1282,7 @@ int launch_pair_of(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, 
   if (held == 0) held = clusters_held(k_grouped_pair<MODE, RES>, threads, Pair::kSmem, 2);
   if (held < 1) return HA_ECUDA;
   const int64_t pairs = std::min<int64_t>(held, std::max<int64_t>(most, 1));
-  k_grouped_pair<MODE, RES><<<static_cast<unsigned>(2 * pairs), threads, Pair::kSmem, s>>>(ta, tb, a);
+  k_grouped_pair<MODE, RES><<<static_cast<unsigned>(2 * pairs), threads, Pair::kSmem, s>>>(ta, tb, ends, a);
   return cudaGetLastError() == cudaSuccess ? HA_OK : HA_ECUDA;
 }
 
@@ -1247,10 +1291,11 @@ int launch_pair_of(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, 
 // rows, 4096 to 4096, bf16: 391 us whole, 425 folded; of 8 groups, 65536 rows, 2048 to 2048: 297 and 301.)
 int64_t whole_sum(int type) { return type == HA_TYPE_BF16 ? 65536 : 8192; }
 template <int MODE>
-int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int64_t length, int64_t most, cudaStream_t s) {
-  if (a.out_type == HA_TYPE_FP32) return launch_pair_of<MODE, kWide>(ta, tb, a, most, s);
-  if (length > whole_sum(a.out_type)) return launch_pair_of<MODE, kFolded>(ta, tb, a, most, s);
-  return launch_pair_of<MODE, kWhole>(ta, tb, a, most, s);
+int launch_pair(const CUtensorMap& ta, const CUtensorMap& tb, const Ends<MODE>& ends, const Args& a, int64_t length,
+                int64_t most, cudaStream_t s) {
+  if (a.out_type == HA_TYPE_FP32) return launch_pair_of<MODE, kWide>(ta, tb, ends, a, most, s);
+  if (length > whole_sum(a.out_type)) return launch_pair_of<MODE, kFolded>(ta, tb, ends, a, most, s);
+  return launch_pair_of<MODE, kWhole>(ta, tb, ends, a, most, s);
 }
 
 bool half_type(int t) { return t == HA_TYPE_BF16 || t == HA_TYPE_FP16; }
@@ -1295,7 +1340,7 @@ int rows_product(Operand x, Operand w, Args a, void* ws, int64_t ws_bytes, cudaS
                 : launch_one<MODE, false, 64>(ta, tb, a, tiles, most, s);
   }
   const int64_t most = m2 * std::min<int64_t>(rows, a.groups + rows / kPairCols);
-  return launch_pair<MODE>(ta, tb, a, a.k, most, s);
+  return launch_pair<MODE>(ta, tb, {}, a, a.k, most, s);
 }
 
 }  // namespace
@@ -1435,12 +1480,15 @@ extern "C" int hier_avg_grouped_product_dw(const void* dy_dev, int64_t dy_ld, co
     }
   }
   CUtensorMap ta, tb;
-  if (!make_map(&ta, dy, type, 64, 64) || !make_map(&tb, x, type, 64, 64)) return HA_ECUDA;
+  Ends<kDw> ends;
+  if (!make_map(&ta, dy, type, 64, 64) || !make_map(&tb, x, type, 64, 64) || !make_map(&ends.a, dy, type, 64, 16) ||
+      !make_map(&ends.b, x, type, 64, 16))
+    return HA_ECUDA;
   const int64_t most = a.groups * static_cast<int64_t>((outer + 2 * kM - 1) / (2 * kM)) *
                        ((inner + kPairCols - 1) / kPairCols + (db_dev ? 1 : 0));
   if (most > 0x7FFFFFFF) return HA_EUNSUPPORTED;
   // the groups' lengths are not known here: one of them may have all rows
-  const int status = launch_pair<kDw>(ta, tb, a, rows, most, s);
+  const int status = launch_pair<kDw>(ta, tb, ends, a, rows, most, s);
   if (status != HA_OK || parts.split == 1) return status;
   Join j = {};
   j.part = static_cast<const float*>(a.out);

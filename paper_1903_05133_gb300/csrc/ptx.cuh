@@ -134,8 +134,9 @@ __device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank) {
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ra) : "r"(smem_u32(p)), "r"(rank));
   return ra;
 }
-// Arrive on a barrier of the cluster.  (With .release.cluster it would be a fence that waits for
-// the thread's loads and stores in flight: nothing that these arrivals order passes through them.)
+// Arrive on a barrier of the cluster, for what is over by then and leaves no memory to be seen: tensor
+// memory loads that have been waited for.  (With .release.cluster it would be a fence that waits for
+// the thread's loads and stores in flight.)
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }

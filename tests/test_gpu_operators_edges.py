@@ -248,3 +248,31 @@ def test_product_long_sums_keep_their_precision(T, N, dx):
         ref = x[rows].double() @ w[g0].double().T
         assert ((y[rows].double() - ref).abs() <= (2.0 ** -11 + 2.0 ** -14) * ref).all(), ((y[rows].double() - ref).abs() / ref).max()
     ops.operator_check()
+
+
+@pytest.mark.parametrize("N,K", [(72, 40), (264, 520)])
+@pytest.mark.parametrize("dtype,out", [(BF, BF), (HF, F)])
+def test_product_dw_every_end_of_a_group(N, K, dtype, out):
+    # all lengths to two chunks and a row, each group between groups of values that may not reach it; the
+    # same to the bit every time
+    g = gen(N + K)
+    sizes = [n for k in range(130) for n in (k, 1 + k % 17)]
+    T = sum(sizes)
+    dy, x = randn(g, T, N, dtype=dtype), randn(g, T, K, dtype=dtype)
+    at = [0]
+    for n in sizes:
+        at.append(at[-1] + n)
+    for i in range(1, len(sizes), 2):
+        dy[at[i]:at[i + 1]], x[at[i]:at[i + 1]] = math.nan, math.inf
+    off = offsets_of(sizes)
+    dw, db = ops.grouped_product_dw(dy, x, off, bias_grad=True, out_dtype=out)
+    for i in range(0, len(sizes), 2):
+        a, b = dy[at[i]:at[i + 1]].double(), x[at[i]:at[i + 1]].double()
+        assert_within(dw[i], a.T @ b, product_bound(a.T @ b, a.abs().T @ b.abs(), sizes[i], out))
+        assert_within(db[i], a.sum(0), (sizes[i] + 16) * 2.0 ** -24 * a.abs().sum(0) + 1e-300)
+    assert dw[1::2].isnan().all() and db[1::2].isnan().all()
+    even = dw[0::2].clone()
+    for _ in range(10):
+        again = ops.grouped_product_dw(dy, x, off, out_dtype=out)
+        assert torch.equal(again[0::2], even)
+    ops.operator_check()
