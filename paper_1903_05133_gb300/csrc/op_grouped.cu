@@ -1246,15 +1246,17 @@ int launch_one(const CUtensorMap& ta, const CUtensorMap& tb, const Args& a, int6
   if (allow_smem(kernel, smem, allowed) != cudaSuccess) return HA_ECUDA;
   // CTAs a tile: as many as fill the GPU, with at least kMinChunks chunks each (one row, 4096 ->
   // 4096: 18.2 us with one CTA a tile).
-  static int held[4] = {0, 0, 0, 0};
+  static int held[kMaxDevices][4];
   int split = 1, log = 0;
   while (split < kMaxSplit && tiles * split * 2 <= kSms && (a.k + kK - 1) / kK >= split * 2 * kMinChunks) {
     split *= 2;
     ++log;
   }
-  if (held[log] == 0) held[log] = split == 1 ? kSms : clusters_held(kernel, kThreads, smem, split);
-  if (held[log] < 1) return HA_ECUDA;
-  const int64_t clusters = std::min<int64_t>(held[log], std::max<int64_t>(most, 1));
+  const int device = device_slot();
+  int once = 0, &found = device >= 0 ? held[device][log] : once;
+  if (found == 0) found = split == 1 ? kSms : clusters_held(kernel, kThreads, smem, split);
+  if (found < 1) return HA_ECUDA;
+  const int64_t clusters = std::min<int64_t>(found, std::max<int64_t>(most, 1));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(clusters * split));
   cfg.blockDim = dim3(kThreads);
@@ -1278,10 +1280,12 @@ int launch_pair_of(const CUtensorMap& ta, const CUtensorMap& tb, const Ends<MODE
   // As many pairs as the GPU holds at once (its clusters of two leave some SMs out): the tiles
   // are dealt out in advance, so a pair that started late would finish late.
   constexpr int threads = MODE == kDw ? kDwThreads : kThreads;
-  static int held = 0;
-  if (held == 0) held = clusters_held(k_grouped_pair<MODE, RES>, threads, Pair::kSmem, 2);
-  if (held < 1) return HA_ECUDA;
-  const int64_t pairs = std::min<int64_t>(held, std::max<int64_t>(most, 1));
+  static int held[kMaxDevices];
+  const int device = device_slot();
+  int once = 0, &found = device >= 0 ? held[device] : once;
+  if (found == 0) found = clusters_held(k_grouped_pair<MODE, RES>, threads, Pair::kSmem, 2);
+  if (found < 1) return HA_ECUDA;
+  const int64_t pairs = std::min<int64_t>(found, std::max<int64_t>(most, 1));
   k_grouped_pair<MODE, RES><<<static_cast<unsigned>(2 * pairs), threads, Pair::kSmem, s>>>(ta, tb, ends, a);
   return cudaGetLastError() == cudaSuccess ? HA_OK : HA_ECUDA;
 }

@@ -44,6 +44,10 @@ class LocalAdamW:
         self.params.copy_(self.layout.pack(layers, self.params.device))
         self.copy.copy_(self.params)
 
+    def _here(self):
+        """The parameters' GPU as the current one."""
+        return torch.cuda.device(self.params.device)
+
     def step(self, X: torch.Tensor, y: torch.Tensor, offsets: torch.Tensor) -> torch.Tensor:
         """One AdamW step of every learner on its rows of X [rows, dims[0]] (bf16) and y [rows]: those from
         offsets[j] to offsets[j + 1].  Returns the log probability of each label before the step."""
@@ -66,13 +70,15 @@ class LocalAdamW:
         return r.logp
 
     def local_average(self) -> None:
-        local_average_buffer(self.params, self.S)
-        self.copy.copy_(self.params)
+        with self._here():
+            local_average_buffer(self.params, self.S)
+            self.copy.copy_(self.params)
 
     def global_average(self) -> None:
         """The last local average of a round and the global one, in one pass."""
-        local_global_average_buffer(self.params, self.S)
-        self.copy.copy_(self.params)
+        with self._here():
+            local_global_average_buffer(self.params, self.S)
+            self.copy.copy_(self.params)
 
     def round(self, batches) -> torch.Tensor:
         """K1 * K2 steps on (X, y, offsets) from the iterator ``batches`` with their averages; the last

@@ -4,7 +4,8 @@ probabilities of given classes with their gradient, and AdamW over many tensors.
 Argument marshalling only, as in hier_avg.py: PyTorch provides the memory and the stream, the
 computation runs in the library's CUDA kernels, and the functions are those of
 include/hier_avg.h without the ``hier_avg_`` prefix.  Results are new tensors unless ``out``
-is given.  A call on ``stream`` makes its results and workspace there.
+is given.  All tensors of a call are on one GPU, where it runs whichever is current.  A call on
+``stream`` makes its results and workspace there.
 """
 from __future__ import annotations
 
@@ -21,20 +22,28 @@ from ._lib import c_int64, c_void_p, check
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 FORWARD, DX, DW = 0, 1, 2
-_KIND = attrgetter("dtype", "shape", "is_cuda")
-_ADDRESS, _CONTIGUOUS = torch.Tensor.data_ptr, torch.Tensor.is_contiguous
+_KIND = attrgetter("dtype", "shape")
+_ADDRESS, _CONTIGUOUS, _DEVICE = torch.Tensor.data_ptr, torch.Tensor.is_contiguous, torch.Tensor.get_device
 BLOCK = 256                     # elements that share a scale of the 8-bit AdamW states
 MAX_TOP = 32
 
 
 _NOWHERE = nullcontext()
 _RAW_STREAM = torch._C._cuda_getCurrentRawStream    # current_stream() makes an object: 5 us
+_CURRENT = torch._C._cuda_getDevice
 
 
-def _on(t, stream):
-    """The stream's handle (the current one of t's device) and a context that allocates on it."""
+def _on(stream, t, *others):
+    """The stream's handle (the current one of t's GPU), and a context in which that GPU is current and
+    allocations are the stream's.  The other tensors (or None) must be on the same GPU."""
+    d = t.get_device()
+    for o in others:
+        if o is not None and o.get_device() != d:
+            raise ValueError("all tensors of a call must be on one GPU")
     if stream is None:
-        return _RAW_STREAM(t.get_device()), _NOWHERE
+        return _RAW_STREAM(d), _NOWHERE if d == _CURRENT() else torch.cuda.device(d)
+    if stream.device_index != d:
+        raise ValueError("stream must be of the tensors' GPU")
     return stream.cuda_stream, torch.cuda.stream(stream)
 
 
@@ -156,14 +165,14 @@ def grouped_product(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
         raise ValueError(f"x must have {K} columns, as w")
     bias_ld = 0 if bias is None else _rows_of("bias", bias, (torch.float32,), G, N)
     d = _out_type(out_dtype, out, kind)
-    s, where = _on(x, stream)
+    s, where = _on(stream, x, w, offsets, bias, out)
     with where:
         y = torch.empty((T, N), dtype=d, device=x.device) if out is None else _given(out, (T, N), d)
         ws, p, n = _workspace(lib, FORWARD, x, ld, w, w_ld, gs, G, T, K, N)
-    check(lib.hier_avg_grouped_product(
-        x.data_ptr(), ld, w.data_ptr(), w_ld, gs, TYPES[kind], offsets.data_ptr(), G, T, K, N,
-        None if bias is None else bias.data_ptr(), bias_ld, relu, y.data_ptr(),
-        N if out is None else _ld(y), TYPES[d], p, n, s), "grouped_product")
+        check(lib.hier_avg_grouped_product(
+            x.data_ptr(), ld, w.data_ptr(), w_ld, gs, TYPES[kind], offsets.data_ptr(), G, T, K, N,
+            None if bias is None else bias.data_ptr(), bias_ld, relu, y.data_ptr(),
+            N if out is None else _ld(y), TYPES[d], p, n, s), "grouped_product")
     return y
 
 
@@ -181,14 +190,14 @@ def grouped_product_dx(dy: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
         raise ValueError(f"dy must have {N} columns, as w has rows")
     h_ld = 0 if h is None else _rows_of("h", h, (kind,), T, K)
     d = _out_type(out_dtype, out, kind)
-    s, where = _on(dy, stream)
+    s, where = _on(stream, dy, w, offsets, h, out)
     with where:
         dx = torch.empty((T, K), dtype=d, device=dy.device) if out is None else _given(out, (T, K), d)
         ws, p, n = _workspace(lib, DX, dy, ld, w, w_ld, gs, G, T, K, N)
-    check(lib.hier_avg_grouped_product_dx(
-        dy.data_ptr(), ld, w.data_ptr(), w_ld, gs, TYPES[kind], offsets.data_ptr(), G, T, K, N,
-        None if h is None else h.data_ptr(), h_ld, dx.data_ptr(), K if out is None else _ld(dx),
-        TYPES[d], p, n, s), "grouped_product_dx")
+        check(lib.hier_avg_grouped_product_dx(
+            dy.data_ptr(), ld, w.data_ptr(), w_ld, gs, TYPES[kind], offsets.data_ptr(), G, T, K, N,
+            None if h is None else h.data_ptr(), h_ld, dx.data_ptr(), K if out is None else _ld(dx),
+            TYPES[d], p, n, s), "grouped_product_dx")
     return dx
 
 
@@ -203,16 +212,16 @@ def grouped_product_dw(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor,
     x_ld = _rows_of("x", x, (kind,), T)
     G, K = _offsets(offsets, None), x.shape[1]
     d = _out_type(out_dtype, out, kind)
-    s, where = _on(dy, stream)
+    s, where = _on(stream, dy, x, offsets, out)
     with where:
         dw = torch.empty((G, N, K), dtype=d, device=dy.device) if out is None else _given(out, (G, N, K), d)
         db = torch.empty((G, N), dtype=torch.float32, device=dy.device) if bias_grad else None
         ws, p, n = _workspace(lib, DW, dy, ld, x, x_ld, 0, G, T, K, N)
-    dw_ld, dw_gs = (K, N * K) if out is None else (_ld(dw), dw.stride(0))
-    check(lib.hier_avg_grouped_product_dw(
-        dy.data_ptr(), ld, x.data_ptr(), x_ld, TYPES[kind], offsets.data_ptr(), G, T, K, N,
-        dw.data_ptr(), dw_ld, dw_gs, TYPES[d], db.data_ptr() if bias_grad else None, N, p, n, s),
-        "grouped_product_dw")
+        dw_ld, dw_gs = (K, N * K) if out is None else (_ld(dw), dw.stride(0))
+        check(lib.hier_avg_grouped_product_dw(
+            dy.data_ptr(), ld, x.data_ptr(), x_ld, TYPES[kind], offsets.data_ptr(), G, T, K, N,
+            dw.data_ptr(), dw_ld, dw_gs, TYPES[d], db.data_ptr() if bias_grad else None, N, p, n, s),
+            "grouped_product_dw")
     return (dw, db) if bias_grad else dw
 
 
@@ -256,7 +265,7 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, top: int = 0, te
     if not 0 <= top <= MAX_TOP:
         raise ValueError(f"top must be in [0, {MAX_TOP}]")
     T, V = logits.shape
-    s, where = _on(logits, stream)
+    s, where = _on(stream, logits, targets, allowed)
     best = index = b = i = None
     with where:
         dev = logits.device
@@ -268,9 +277,9 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, top: int = 0, te
             best = torch.empty((T, top), dtype=torch.float32, device=dev)
             index = torch.empty((T, top), dtype=torch.int32, device=dev)
             b, i = best.data_ptr(), index.data_ptr()
-    check(lib.hier_avg_token_logprobs(
-        logits.data_ptr(), TYPES[logits.dtype], T, V, ld, targets.data_ptr(), targets.element_size(),
-        mask, mask_ld, temperature, top, logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(), b, i, s), "token_logprobs")
+        check(lib.hier_avg_token_logprobs(
+            logits.data_ptr(), TYPES[logits.dtype], T, V, ld, targets.data_ptr(), targets.element_size(), mask, mask_ld,
+            temperature, top, logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(), b, i, s), "token_logprobs")
     return TokenLogprobs(logp, entropy, lse, best, index)
 
 
@@ -289,16 +298,16 @@ def token_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, lse: to
         if v is not None and not (v.is_cuda and v.dtype == torch.float32 and v.dim() == 1 and
                                   v.shape[0] == T and v.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous CUDA fp32 vector, one entry a row")
-    s, where = _on(logits, stream)
+    s, where = _on(stream, logits, targets, allowed, lse, entropy, dlogp, dentropy, out)
     with where:
         d = torch.empty((T, V), dtype=logits.dtype, device=logits.device) if out is None else \
             _given(out, (T, V), logits.dtype)
-    check(lib.hier_avg_token_logprobs_backward(
-        logits.data_ptr(), TYPES[logits.dtype], T, V, ld, targets.data_ptr(),
-        targets.element_size(), mask, mask_ld, temperature, lse.data_ptr(),
-        None if entropy is None else entropy.data_ptr(), dlogp.data_ptr(),
-        None if dentropy is None else dentropy.data_ptr(), d.data_ptr(),
-        V if out is None else _ld(d), s), "token_logprobs_backward")
+        check(lib.hier_avg_token_logprobs_backward(
+            logits.data_ptr(), TYPES[logits.dtype], T, V, ld, targets.data_ptr(),
+            targets.element_size(), mask, mask_ld, temperature, lse.data_ptr(),
+            None if entropy is None else entropy.data_ptr(), dlogp.data_ptr(),
+            None if dentropy is None else dentropy.data_ptr(), d.data_ptr(),
+            V if out is None else _ld(d), s), "token_logprobs_backward")
     return d
 
 
@@ -358,7 +367,7 @@ class AdamW:
         self.params, self.copies, self.bits = params, copies, bits
         self.beta1, self.beta2, self.eps, self.t = beta1, beta2, eps, 0
         e, dev = elements.value, params[0].device
-        s, where = _on(params[0], stream)
+        s, where = _on(stream, *params, *copies)
         with where:
             self._table = torch.empty(max(table.value, 16), dtype=torch.uint8, device=dev)
             self.m_scale = self.root_scale = self.v = self.root = None
@@ -370,12 +379,13 @@ class AdamW:
                 self.root = torch.zeros(e, dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn)
                 self.m_scale = torch.zeros(e // BLOCK, device=dev)
                 self.root_scale = torch.zeros(e // BLOCK, device=dev)
-        second = self.v if bits == 32 else self.root
-        check(lib.hier_avg_adamw_bind(
-            self.h, self._table.data_ptr(), table.value, self.m.data_ptr(), second.data_ptr(),
-            self.m_scale.data_ptr() if bits == 8 else None,
-            self.root_scale.data_ptr() if bits == 8 else None, s), "adamw_bind")
-        self._kinds = {d: [(d, p.shape, True) for p in params] for d in TYPES}
+            second = self.v if bits == 32 else self.root
+            check(lib.hier_avg_adamw_bind(
+                self.h, self._table.data_ptr(), table.value, self.m.data_ptr(), second.data_ptr(),
+                self.m_scale.data_ptr() if bits == 8 else None,
+                self.root_scale.data_ptr() if bits == 8 else None, s), "adamw_bind")
+        self._kinds = {d: [(d, p.shape) for p in params] for d in TYPES}
+        self._devices = [params[0].get_device()] * len(params)
 
     def step(self, grads: Sequence[torch.Tensor], lr: float, grad_scale: Optional[torch.Tensor] = None,
              seed: Optional[int] = None, stream=None) -> None:
@@ -384,18 +394,20 @@ class AdamW:
         (the step's number when None); the same seed gives the same step."""
         # each check runs over all tensors at once: a call over hundreds of them is host work
         kind = grads[0].dtype if grads else None
-        if not (kind in TYPES and list(map(_KIND, grads)) == self._kinds[kind] and all(map(_CONTIGUOUS, grads))):
-            raise ValueError("grads must be one contiguous CUDA tensor for each of the params, of its "
-                             "shape, all of them fp32, bf16 or fp16")
+        if not (kind in TYPES and list(map(_KIND, grads)) == self._kinds[kind] and
+                list(map(_DEVICE, grads)) == self._devices and all(map(_CONTIGUOUS, grads))):
+            raise ValueError("grads must be one contiguous tensor on the params' GPU for each of them, of "
+                             "its shape, all of them fp32, bf16 or fp16")
         a = array("Q", map(_ADDRESS, grads))
         if grad_scale is not None:
             _need(grad_scale.is_cuda and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1,
                   "grad_scale must be one CUDA fp32 value")
-        s = _RAW_STREAM(grads[0].get_device()) if stream is None else stream.cuda_stream
-        check(self._lib.hier_avg_adamw_step(
-            self.h, a.buffer_info()[0], TYPES[kind], lr, self.beta1, self.beta2, self.eps, self.t + 1,
-            grad_scale.data_ptr() if grad_scale is not None else None,
-            (self.t + 1 if seed is None else seed) & 0xFFFFFFFF, s), "adamw_step")
+        s, where = _on(stream, grads[0], grad_scale)
+        with where:
+            check(self._lib.hier_avg_adamw_step(
+                self.h, a.buffer_info()[0], TYPES[kind], lr, self.beta1, self.beta2, self.eps, self.t + 1,
+                grad_scale.data_ptr() if grad_scale is not None else None,
+                (self.t + 1 if seed is None else seed) & 0xFFFFFFFF, s), "adamw_step")
         self.t += 1
 
     def state_dict(self) -> Dict[str, object]:
@@ -440,5 +452,6 @@ def _pieces(p: torch.Tensor, c: Optional[torch.Tensor]):
 
 def operator_check(stream=None) -> None:
     """Synchronise the stream; raise if a bounded wait inside a grouped product ran out."""
-    s = (torch.cuda.current_stream() if stream is None else stream).cuda_stream
-    check(_lib.load().hier_avg_operator_check(s), "operator_check")
+    stream = torch.cuda.current_stream() if stream is None else stream
+    with torch.cuda.device(stream.device):
+        check(_lib.load().hier_avg_operator_check(stream.cuda_stream), "operator_check")

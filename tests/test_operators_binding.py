@@ -12,8 +12,8 @@ class Stand:
     """A CUDA tensor as far as its type, shape, strides and address go."""
     is_cuda = True
 
-    def __init__(self, dtype, shape, strides=None, address=1 << 20):
-        self.dtype, self.shape, self.address = dtype, torch.Size(shape), address
+    def __init__(self, dtype, shape, strides=None, address=1 << 20, gpu=0):
+        self.dtype, self.shape, self.address, self.gpu = dtype, torch.Size(shape), address, gpu
         if strides is None:
             strides = [1]
             for n in reversed(shape[1:]):
@@ -34,6 +34,12 @@ class Stand:
 
     def element_size(self):
         return self.dtype.itemsize
+
+    def numel(self):
+        return self.shape.numel()
+
+    def get_device(self):
+        return self.gpu
 
 
 def test_masks_with_overlapping_rows_are_refused():
@@ -103,3 +109,107 @@ def test_weights_whose_groups_overlap_are_copied_first(lib):
     for ld, gs in ((K, 0), (K, 8), (K, K), (K, (N - 1) * K), (G * K - 8, K), (G * K, K - 8)):
         assert bytes_of(ld, gs) == copy, (ld, gs)
     assert bytes_of(K, K, N=1) == 0 and bytes_of(K, K - 8, N=1) > 0 and bytes_of(K, 8, G=1) == 0
+
+
+class Calls:
+    """A stand-in for the library that notes each call's name, the current GPU and the stream."""
+
+    def __init__(self, gpus):
+        self.gpus, self.made = gpus, []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.made.append((name, self.gpus[0], args[-1]))
+            return 0
+        return call
+
+
+class Guard:
+    def __init__(self, gpus, gpu):
+        self.gpus, self.gpu = gpus, gpu
+
+    def __enter__(self):
+        self.before, self.gpus[0] = self.gpus[0], self.gpu
+
+    def __exit__(self, *_):
+        self.gpus[0] = self.before
+
+
+class Stream:
+    def __init__(self, gpu, handle):
+        self.device_index, self.cuda_stream = gpu, handle
+
+
+@pytest.fixture
+def two_gpus(monkeypatch):
+    """GPU 0 is current; the current stream of GPU d is 100 + d."""
+    gpus = [0]
+    calls = Calls(gpus)
+    monkeypatch.setattr(ops._lib, "load", lambda: calls)
+    monkeypatch.setattr(ops, "_CURRENT", lambda: gpus[0], raising=False)
+    monkeypatch.setattr(ops, "_RAW_STREAM", lambda d: 100 + d)
+    monkeypatch.setattr(ops, "_DEVICE", Stand.get_device, raising=False)
+    monkeypatch.setattr(ops, "_ADDRESS", Stand.data_ptr)
+    monkeypatch.setattr(ops, "_CONTIGUOUS", Stand.is_contiguous)
+    monkeypatch.setattr(torch.cuda, "device", lambda d: Guard(gpus, d))
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: Guard(gpus, s.device_index))
+    return gpus, calls
+
+
+def all_calls():
+    """Each operator's arguments on GPU `gpu(name)`, aligned and with all its tensors given."""
+    T, G, N, K, V = 6, 2, 16, 24, 40
+    at = iter(range(1 << 20, 1 << 30, 1 << 20))
+
+    def tensors(gpu):
+        S = lambda name, dtype, shape: Stand(dtype, shape, address=next(at), gpu=gpu(name))  # noqa: E731
+        off = lambda: S("offsets", I32, (G + 1,))  # noqa: E731
+        opt = ops.AdamW.__new__(ops.AdamW)
+        opt.h, opt._lib, opt.t, opt.bits, opt.beta1, opt.beta2, opt.eps = None, ops._lib.load(), 0, 32, 0.9, 0.99, 1e-8
+        opt._kinds = {F: [(F, torch.Size((4,)))] * 2}
+        opt._devices = [gpu("params")] * 2
+        v = lambda name: S(name, F, (T,))  # noqa: E731
+        return {
+            "grouped_product": lambda **k: ops.grouped_product(
+                S("x", BF, (T, K)), S("w", BF, (G, N, K)), off(), bias=S("bias", F, (G, N)), out=S("out", BF, (T, N)), **k),
+            "grouped_product_dx": lambda **k: ops.grouped_product_dx(
+                S("dy", BF, (T, N)), S("w", BF, (G, N, K)), off(), h=S("h", BF, (T, K)), out=S("out", BF, (T, K)), **k),
+            "grouped_product_dw": lambda **k: ops.grouped_product_dw(
+                S("dy", BF, (T, N)), S("x", BF, (T, K)), off(), out=S("out", BF, (G, N, K)), **k),
+            "token_logprobs_backward": lambda **k: ops.token_logprobs_backward(
+                S("logits", BF, (T, V)), S("targets", I32, (T,)), v("lse"), v("entropy"), v("dlogp"), v("dentropy"),
+                allowed=S("allowed", BOOL, (T, V)), out=S("out", BF, (T, V)), **k),
+            "adamw_step": lambda **k: opt.step([S("grads", F, (4,)), S("grads", F, (4,))], lr=0.1, grad_scale=S("grad_scale", F, (1,)), **k)}
+    return tensors
+
+
+def test_calls_run_on_their_tensors_gpu(two_gpus):
+    gpus, calls = two_gpus
+    for gpu in (0, 1):
+        for name, call in all_calls()(lambda _: gpu).items():
+            calls.made.clear()
+            call()
+            assert calls.made == [("hier_avg_" + name, gpu, 100 + gpu)] and gpus == [0], name
+            calls.made.clear()
+            call(stream=Stream(gpu, 7))
+            assert calls.made == [("hier_avg_" + name, gpu, 7)] and gpus == [0], name
+            calls.made.clear()
+            with pytest.raises(ValueError, match="stream"):
+                call(stream=Stream(1 - gpu, 7))
+            assert not calls.made
+
+
+def test_tensors_of_two_gpus_are_refused(two_gpus):
+    gpus, calls = two_gpus
+    seen = set()
+    named = {"grouped_product": ("x", "w", "offsets", "bias", "out"), "grouped_product_dx": ("dy", "w", "offsets", "h", "out"),
+             "grouped_product_dw": ("dy", "x", "offsets", "out"), "adamw_step": ("grads", "grad_scale", "params"),
+             "token_logprobs_backward": ("logits", "targets", "lse", "entropy", "dlogp", "dentropy", "allowed", "out")}
+    for name, tensors in named.items():
+        for one in tensors:
+            with pytest.raises(ValueError, match="GPU"):
+                all_calls()(lambda n: int(n == one))[name]()
+            seen.add((name, one))
+    assert not calls.made and len(seen) == sum(map(len, named.values()))
+    with pytest.raises(ValueError, match="GPU"):
+        ops.token_logprobs(Stand(BF, (3, 8)), Stand(I32, (3,), gpu=1))
