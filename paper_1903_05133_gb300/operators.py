@@ -83,6 +83,43 @@ def _given(out, shape, dtype):
     return out
 
 
+def _end(t, at):
+    last = 1
+    for n, s in zip(t.shape, t.stride()):
+        last += (n - 1) * s
+    return at + last * t.element_size()
+
+
+def _pitch(t):
+    """Bytes of a row and from row to row (None: there is one row, 0: they differ)."""
+    es = t.element_size()
+    rows = [s for n, s in zip(t.shape[:-1], t.stride()) if n > 1 and s > 0]
+    if not rows:
+        return es * t.shape[-1], None
+    return es * t.shape[-1], 0 if any(s % rows[-1] for s in rows) else es * rows[-1]
+
+
+def _apart(out, *inputs, same=None):
+    """Refuses an out that shares memory with an input, unless it is `same` itself (which then is read
+    before it is written, element by element)."""
+    if out is None or not out.numel():
+        return
+    p = out.data_ptr()
+    end = _end(out, p)
+    for t in inputs:
+        if t is None:
+            continue
+        q = t.data_ptr()
+        if q >= end or _end(t, q) <= p or not t.numel():
+            continue
+        (width, step), (t_width, t_step) = _pitch(out), _pitch(t)
+        if t is same and p == q and t.shape == out.shape and t.dtype == out.dtype and step == t_step:
+            continue
+        # columns of one buffer side by side
+        step = step if t_step is None else t_step if step is None else step if step == t_step else 0
+        _need(bool(step) and width <= (q - p) % step <= step - t_width, "out must not share memory with an input")
+
+
 # ---------------------------------------------------------------------- grouped products
 _HALF = (torch.bfloat16, torch.float16)
 
@@ -165,6 +202,7 @@ def grouped_product(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
         raise ValueError(f"x must have {K} columns, as w")
     bias_ld = 0 if bias is None else _rows_of("bias", bias, (torch.float32,), G, N)
     d = _out_type(out_dtype, out, kind)
+    _apart(out, x, w, offsets, bias)
     s, where = _on(stream, x, w, offsets, bias, out)
     with where:
         y = torch.empty((T, N), dtype=d, device=x.device) if out is None else _given(out, (T, N), d)
@@ -180,7 +218,7 @@ def grouped_product_dx(dy: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
                        h: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                        out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
     """dx[t] = w[g]^T dy[t] for the rows of group g; with h [rows, inner] (the activations that
-    grouped_product read, after a ReLU) zero where h is not positive."""
+    grouped_product read, after a ReLU) zero where h is not positive; ``out`` may be ``h`` itself."""
     lib = _lib.load()
     ld = _rows_of("dy", dy, _HALF)
     kind = dy.dtype
@@ -190,6 +228,7 @@ def grouped_product_dx(dy: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
         raise ValueError(f"dy must have {N} columns, as w has rows")
     h_ld = 0 if h is None else _rows_of("h", h, (kind,), T, K)
     d = _out_type(out_dtype, out, kind)
+    _apart(out, dy, w, offsets, h, same=h)
     s, where = _on(stream, dy, w, offsets, h, out)
     with where:
         dx = torch.empty((T, K), dtype=d, device=dy.device) if out is None else _given(out, (T, K), d)
@@ -212,6 +251,7 @@ def grouped_product_dw(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor,
     x_ld = _rows_of("x", x, (kind,), T)
     G, K = _offsets(offsets, None), x.shape[1]
     d = _out_type(out_dtype, out, kind)
+    _apart(out, dy, x, offsets)
     s, where = _on(stream, dy, x, offsets, out)
     with where:
         dw = torch.empty((G, N, K), dtype=d, device=dy.device) if out is None else _given(out, (G, N, K), d)
@@ -298,6 +338,7 @@ def token_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, lse: to
         if v is not None and not (v.is_cuda and v.dtype == torch.float32 and v.dim() == 1 and
                                   v.shape[0] == T and v.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous CUDA fp32 vector, one entry a row")
+    _apart(out, logits, targets, allowed, lse, entropy, dlogp, dentropy, same=logits)
     s, where = _on(stream, logits, targets, allowed, lse, entropy, dlogp, dentropy, out)
     with where:
         d = torch.empty((T, V), dtype=logits.dtype, device=logits.device) if out is None else \

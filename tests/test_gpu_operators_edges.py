@@ -276,3 +276,13 @@ def test_product_dw_every_end_of_a_group(N, K, dtype, out):
         again = ops.grouped_product_dw(dy, x, off, out_dtype=out)
         assert torch.equal(again[0::2], even)
     ops.operator_check()
+
+
+@pytest.mark.parametrize("sizes,K,N", [([3, 0, 2], 4096, 128), ([300, 1, 513], 512, 264), ([90, 40], 77, 51), ([20, 31], 264, 72)])
+def test_product_dx_into_the_mask_itself(sizes, K, N):
+    g = gen(K + N)
+    T, G = sum(sizes), len(sizes)
+    dy, w, h = randn(g, T, N, dtype=BF), randn(g, G, N, K, dtype=BF), randn(g, T, K + 8, dtype=BF)[:, 8:]
+    off = offsets_of(sizes)
+    want = ops.grouped_product_dx(dy, w, off, h=h)
+    assert ops.grouped_product_dx(dy, w, off, h=h, out=h) is h and torch.equal(h, want)

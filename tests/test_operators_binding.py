@@ -213,3 +213,50 @@ def test_tensors_of_two_gpus_are_refused(two_gpus):
     assert not calls.made and len(seen) == sum(map(len, named.values()))
     with pytest.raises(ValueError, match="GPU"):
         ops.token_logprobs(Stand(BF, (3, 8)), Stand(I32, (3,), gpu=1))
+
+
+def test_results_that_share_memory_with_an_input_are_refused(two_gpus):
+    gpus, calls = two_gpus
+    T, G, N, K, at = 6, 2, 32, 32, 1 << 20
+    far = iter(range(1 << 24, 1 << 30, 1 << 20))
+    S = lambda dtype, shape, address=None, strides=None: Stand(  # noqa: E731
+        dtype, shape, strides, next(far) if address is None else address)
+    off = S(I32, (G + 1,))
+    product = lambda out, x=None, w=None, o=off, b=None: ops.grouped_product(  # noqa: E731
+        x or S(BF, (T, K)), w or S(BF, (G, N, K)), o, bias=b, out=out)
+    x, w, b = S(BF, (T, K), at), S(BF, (G, N, K), at), S(F, (G, N), at)
+    for kw in (dict(x=x), dict(w=w), dict(b=b), dict(o=S(I32, (G + 1,), at))):
+        for place in (0, 2, -(T * N * 2) + 2):
+            with pytest.raises(ValueError, match="share"):
+                product(S(BF, (T, N), at + place), **kw)
+    dy, h = S(BF, (T, N)), S(BF, (T, K), at)
+    with pytest.raises(ValueError, match="share"):
+        ops.grouped_product_dx(dy, S(BF, (G, N, K)), off, h=h, out=S(BF, (T, K), at + 2 * K))
+    with pytest.raises(ValueError, match="share"):
+        ops.grouped_product_dx(dy, S(BF, (G, N, K)), off, h=h, out=S(F, (T, K), at))
+    with pytest.raises(ValueError, match="share"):
+        ops.grouped_product_dx(S(BF, (T, N), at), S(BF, (G, N, K)), off, out=S(BF, (T, K), at))
+    with pytest.raises(ValueError, match="share"):
+        ops.grouped_product_dw(dy, S(BF, (T, K), at + 64), off, out=S(BF, (G, N, K), at))
+    v = S(F, (T,))
+    grad = lambda logits, out, lse=v: ops.token_logprobs_backward(logits, S(I32, (T,)), lse, None, v, out=out)  # noqa: E731
+    for out, lse in ((S(BF, (T, N), at + 2 * N), v), (S(BF, (T, N), at, (2 * N, 1)), v), (S(BF, (T, N)), None)):
+        with pytest.raises(ValueError, match="share"):
+            grad(S(BF, (T, N), at), out, lse or S(F, (T,), out.address))
+    assert not calls.made
+    # what is side by side in one buffer, after one another, or the same where that is allowed
+    side = lambda i, n=32, dtype=BF: S(dtype, (T, n), at + 64 * i, (96, 1))  # noqa: E731
+    product(side(1), x=side(0))
+    product(side(0), x=side(2))
+    product(S(BF, (T, N), at + T * K * 2), x=x)
+    ops.grouped_product_dx(dy, S(BF, (G, N, K)), off, h=h, out=S(BF, (T, K), at))
+    ops.grouped_product_dw(dy, S(BF, (T, K), at, (96, 1)), off, out=S(BF, (G, N, K), at + 64, (N * 96, 96, 1)))
+    grad(S(BF, (T, N), at), S(BF, (T, N), at))
+    grad(side(0), side(1))
+    grad(S(BF, (T, N), at), S(BF, (T, N), at + T * N * 2))
+    with pytest.raises(ValueError, match="share"):          # a mask of one row for all
+        ops.token_logprobs_backward(S(BF, (T, N)), S(I32, (T,)), v, None, v, allowed=Stand(BOOL, (T, N), (0, 1), at),
+                                    out=S(BF, (T, N), at))
+    assert len(calls.made) == 8
+    with pytest.raises(ValueError, match="share"):
+        product(side(1, 33), x=side(2))
