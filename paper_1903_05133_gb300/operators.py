@@ -396,6 +396,9 @@ class AdamW:
                 copy.append(b)
                 size.append(n)
                 weight.append(decays[i])
+        # each element is changed by one thread
+        spans = sorted([(a, a + 4 * n) for a, n in zip(addr, size) if n] + [(b, b + 2 * n) for b, n in zip(copy, size) if b and n])
+        _need(all(a[1] <= b[0] for a, b in zip(spans, spans[1:])), "params and copies must not share memory")
         n = len(tensor)
         arr = lambda kind, v: (kind * max(n, 1))(*v)  # noqa: E731
         check(lib.hier_avg_adamw_create(

@@ -260,3 +260,13 @@ def test_results_that_share_memory_with_an_input_are_refused(two_gpus):
     assert len(calls.made) == 8
     with pytest.raises(ValueError, match="share"):
         product(side(1, 33), x=side(2))
+
+
+def test_adamw_parameters_that_share_memory_are_refused(lib):
+    at = 1 << 20
+    p = lambda n, address: Stand(F, (n,), None, address)  # noqa: E731
+    for params, copies in (([p(8, at), p(8, at)], None), ([p(8, at), p(4, at + 28)], None),
+                           ([p(8, at), p(8, at + 64)], [None, Stand(BF, (8,), None, at + 16)]),
+                           ([p(8, at), p(8, at + 64)], [Stand(BF, (8,), None, at + 128), Stand(BF, (8,), None, at + 140)])):
+        with pytest.raises(ValueError, match="share"):
+            ops.AdamW(params, copies=copies)
