@@ -391,7 +391,9 @@ int hier_avg_adamw_step(hier_avg_adamw* plan, const void* const* grads_dev, int 
                         const float* grad_scale_dev, uint32_t seed, void* stream);
 
 /* Synchronise `stream` and report a bounded wait inside a grouped product that ran out on
- * this device (HA_ETIMEOUT, once; the outputs are then invalid) or an asynchronous error. */
+ * this device (HA_ETIMEOUT, once; the outputs are then invalid) or an asynchronous error.
+ * The device has one word for all streams: another stream's wait that has run out by then
+ * is reported, and cleared, too. */
 int hier_avg_operator_check(void* stream);
 
 const char* hier_avg_strerror(int status);

@@ -18,8 +18,8 @@ import torch
 
 from .configs import MLP512_P16
 from .hier_avg import HierAvg, local_average_buffer, local_global_average_buffer
-from .operators import (AdamW, grouped_product, grouped_product_dw, grouped_product_dx, token_logprobs,
-                        token_logprobs_backward)
+from .operators import (AdamW, grouped_product, grouped_product_dw, grouped_product_dx, operator_check,
+                        token_logprobs, token_logprobs_backward)
 
 
 class LocalAdamW:
@@ -82,7 +82,7 @@ class LocalAdamW:
 
     def round(self, batches) -> torch.Tensor:
         """K1 * K2 steps on (X, y, offsets) from the iterator ``batches`` with their averages; the last
-        step's log probabilities."""
+        step's log probabilities.  Synchronises at its end, and raises if a bounded wait ran out."""
         batches = iter(batches)
         logp = None
         for b in range(self.K2):
@@ -91,6 +91,8 @@ class LocalAdamW:
             if b + 1 < self.K2:
                 self.local_average()
         self.global_average()
+        with self._here():
+            operator_check()
         return logp
 
 

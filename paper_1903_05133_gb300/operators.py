@@ -495,7 +495,8 @@ def _pieces(p: torch.Tensor, c: Optional[torch.Tensor]):
 
 
 def operator_check(stream=None) -> None:
-    """Synchronise the stream; raise if a bounded wait inside a grouped product ran out."""
+    """Synchronise the stream; raise if a bounded wait inside a grouped product ran out.  The GPU keeps
+    one note for all streams: what another one's work has left there is reported, and cleared, too."""
     stream = torch.cuda.current_stream() if stream is None else stream
     with torch.cuda.device(stream.device):
         check(_lib.load().hier_avg_operator_check(stream.cuda_stream), "operator_check")

@@ -68,3 +68,19 @@ def test_rounds_learn_and_agree(bits):
         assert (bits_of == bits_of[0]).all()                # after the global average
     assert -last.mean().item() < 0.5 * first
     assert torch.equal(m.copy, m.params.to(torch.bfloat16)) and m.t == 1 + 6 * W.K1 * W.K2
+
+
+def test_round_reports_a_wait_that_ran_out(monkeypatch):
+    from paper_1903_05133_gb300 import local_adamw
+    from paper_1903_05133_gb300._lib import HierAvgError
+    X, y = learner_data(W, device="cuda")
+    m = LocalAdamW(W.P, W.S, W.K1, W.K2, W.lr, W.dims)
+    m.load(initial_layers(W, device="cuda"))
+    batches = ragged_batches(X, y, W.B, 1)
+    m.round(batches)
+
+    def ran_out():
+        raise HierAvgError(-5, "operator_check")
+    monkeypatch.setattr(local_adamw, "operator_check", ran_out)
+    with pytest.raises(HierAvgError):
+        m.round(batches)
