@@ -375,7 +375,8 @@ int hier_avg_token_logprobs_backward(const void* logits_dev, int type, int64_t r
  *               rounded up or down at random by `seed` and the element's place.  A block with
  *               a NaN or an infinity becomes NaN as a whole.
  * hier_avg_adamw_bind copies the plan to table_dev (16-byte aligned) and keeps the addresses.
- * t counts steps from 1.  Errors: HA_EINVAL (eps must be >= 2^-126, betas in [0, 1)), HA_ENOMEM,
+ * t counts steps from 1.  Errors: HA_EINVAL (eps must be >= 2^-126, betas in [0, 1), a plan's
+ * elements at most 2^37), HA_ENOMEM,
  * HA_ESTATE for a step before bind, HA_ECUDA. */
 typedef struct hier_avg_adamw hier_avg_adamw;
 int hier_avg_adamw_create(int bits, int n_tensors, int64_t n_pieces, const int* tensor,

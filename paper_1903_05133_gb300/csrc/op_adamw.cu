@@ -27,6 +27,7 @@ namespace {
 constexpr int kBlock = 256;         // elements that share a scale: one warp, 8 a lane
 constexpr int kChunk = 1024;        // elements of one CTA: a block for each warp
 constexpr int kThreads = 128;
+constexpr int64_t kMaxElements = int64_t(1) << 37;        // of a plan: twice a GPU's memory of parameters
 constexpr float kTop = 448.0f;      // largest e4m3 value
 constexpr float kTiny = 1e-30f;     // a block whose largest magnitude is below is stored as 0
 
@@ -483,7 +484,8 @@ extern "C" int hier_avg_adamw_create(int bits, int n_tensors, int64_t n_pieces, 
     bool ok = true;
     for (int64_t i = 0; i < n_pieces && ok; ++i) {
       ok = tensor[i] >= last && tensor[i] < n_tensors && n[i] >= 0 && grad_offset[i] >= 0 &&
-           (n[i] == 0 || p_dev[i]) && std::isfinite(decay[i]);
+           (n[i] == 0 || p_dev[i]) && std::isfinite(decay[i]) &&
+           n[i] <= kMaxElements - h->elements;            // before the plan takes the host's memory
       if (!ok) break;
       while (static_cast<int>(h->first_chunk.size()) <= tensor[i])
         h->first_chunk.push_back(static_cast<int64_t>(h->chunks.size()));

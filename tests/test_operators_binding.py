@@ -270,3 +270,10 @@ def test_adamw_parameters_that_share_memory_are_refused(lib):
                            ([p(8, at), p(8, at + 64)], [Stand(BF, (8,), None, at + 128), Stand(BF, (8,), None, at + 140)])):
         with pytest.raises(ValueError, match="share"):
             ops.AdamW(params, copies=copies)
+
+
+def test_adamw_plans_beyond_any_memory_are_refused_at_once(lib):
+    from test_operators_abi import EINVAL, create
+    for n in ((1 << 62,), (1 << 38,), (100, 1 << 37)):
+        rc, h = create(lib, n=n, tensor=(0,) * len(n), decay=(0.0,) * len(n), offset=(0,) * len(n))
+        assert rc == EINVAL and not h.value, n
