@@ -1106,10 +1106,10 @@ __global__ void __launch_bounds__(256) k_join(const Join a) {
 }
 
 constexpr int kSms = 152;
-// Groups of at most this many rows on average take the tiles for few rows.
+// Groups of at most this many rows on average (the offsets are on the device: the host knows no more)
+// take the tiles for few rows.  32 groups, 4096 to 4096, bf16: 32 rows each 165 us, by pairs 173; 40 rows
+// each 222 and 175.
 constexpr int kFewRows = 32;
-// Fewer tiles of pairs than this leave too many SMs idle.
-constexpr int kSmallTiles = 40;
 int64_t round8(int64_t x) { return (x + 7) / 8 * 8; }
 int64_t round256(int64_t x) { return (x + 255) / 256 * 256; }
 
@@ -1323,11 +1323,12 @@ int rows_product(Operand x, Operand w, Args a, void* ws, int64_t ws_bytes, cudaS
   const bool wide = a.out_type == HA_TYPE_FP32;
   const int64_t rows = a.rows, used = std::min<int64_t>(rows, a.groups);      // groups with rows, about
   const int64_t m1 = (a.m + kM - 1) / kM, m2 = (a.m + 2 * kM - 1) / (2 * kM);
-  // Few rows a group: narrow tiles.  So few rows in all that pairs would leave most SMs idle:
-  // tiles of one CTA, twice as many and four times as narrow (4096 -> 4096, 256 rows of one
-  // group: 24.5 us by pairs).
+  // Few rows a group: narrow tiles.  So few rows in all that pairs would leave most SMs idle: tiles of
+  // one CTA, twice as many and four times as narrow, as long as one for each SM is enough (one group,
+  // 512 rows, 4096 to 2304, 144 tiles: 21.2 us, by pairs 25.3; to 2560, 160 tiles: 36.5 and 25.4).
   const bool few = rows <= kFewRows * static_cast<int64_t>(a.groups);
-  const bool small = m2 * std::max<int64_t>(used, (rows + kPairCols - 1) / kPairCols) < kSmallTiles;
+  const int64_t narrow = m1 * used * ((rows + 64 * used - 1) / (64 * used));
+  const bool small = narrow <= kSms;
   if (m1 * std::min<int64_t>(rows, a.groups + rows / 32) > 0x7FFFFFFF) return HA_EUNSUPPORTED;    // tiles
   CUtensorMap ta, tb;
   if (!make_map(&ta, w, a.in_type, 64, MODE == kFwd ? 128 : 64) ||
@@ -1339,9 +1340,9 @@ int rows_product(Operand x, Operand w, Args a, void* ws, int64_t ws_bytes, cudaS
                 : launch_one<MODE, false, 32>(ta, tb, a, tiles, most, s);
   }
   if (small) {
-    const int64_t tiles = m1 * std::max<int64_t>(used, (rows + 63) / 64), most = m1 * std::min<int64_t>(rows, a.groups + rows / 64);
-    return wide ? launch_one<MODE, true, 64>(ta, tb, a, tiles, most, s)
-                : launch_one<MODE, false, 64>(ta, tb, a, tiles, most, s);
+    const int64_t most = m1 * std::min<int64_t>(rows, a.groups + rows / 64);
+    return wide ? launch_one<MODE, true, 64>(ta, tb, a, narrow, most, s)
+                : launch_one<MODE, false, 64>(ta, tb, a, narrow, most, s);
   }
   const int64_t most = m2 * std::min<int64_t>(rows, a.groups + rows / kPairCols);
   return launch_pair<MODE>(ta, tb, {}, a, a.k, most, s);
