@@ -46,14 +46,14 @@ struct Stat {
 template <typename T> constexpr float kNone = -1e30f;
 template <> constexpr float kNone<__nv_bfloat16> = -1.0002555517425873e30f;
 
-// Order of floats (no NaN) as unsigned integers, and back.  The sum turns a zero's sign, which
-// would order it before the other zero, to plus.
+// Order of floats (no NaN) as unsigned integers, and back: 2^31 plus or minus the magnitude's bits, so
+// that zeros of both signs are the same.
 __device__ __forceinline__ uint32_t ordered(float v) {
-  const uint32_t u = __float_as_uint(v + 0.0f);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const uint32_t u = __float_as_uint(v);
+  return u & 0x80000000u ? 0u - u : u | 0x80000000u;
 }
 __device__ __forceinline__ float from_ordered(uint32_t o) {
-  return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+  return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : 0u - o);
 }
 
 // The warp's sums, the same in every lane; c = log2(e) / temperature.
@@ -569,12 +569,15 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_logprobs_row(const __grid_co
     }
     m = from_ordered(__reduce_max_sync(~0u, ordered(m)));
     float S = 0.0f, A = 0.0f;
+    // Distances that pass fp32's range are cut off at once where that is cheaper than a look at the sum:
+    // 262144 rows of 16 49.6 us and 51.5, 65536 of 1000, 5 best, 128 and 139, none 54.6 and 53.9.
+    constexpr bool cut = TOP || R <= 2;
     {
       constexpr int N = R < 4 ? R : 4;                    // sums side by side
       float s4[N], a4[N];
 #pragma unroll
       for (int u = 0; u < R; ++u) {
-        const float d = (v[u] - m) * c, e = exp2_fast(d);
+        const float x = (v[u] - m) * c, d = cut ? max_nan(x, -200.0f) : x, e = exp2_fast(d);
         s4[u % N] = u < N ? e : s4[u % N] + e;
         a4[u % N] = u < N ? e * d : fmaf(e, d, a4[u % N]);
       }
@@ -589,7 +592,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_logprobs_row(const __grid_co
       S += __shfl_xor_sync(~0u, S, o);
       A += __shfl_xor_sync(~0u, A, o);
     }
-    if (A != A && S == S) {                               // as sum_again
+    if (!cut && A != A && S == S) {                       // as sum_again
       A = 0.0f;
 #pragma unroll
       for (int u = 0; u < R; ++u) {
