@@ -327,7 +327,7 @@ __device__ __forceinline__ void update(const StepArgs& a, const Block& b, float 
 }
 
 // One CTA a chunk.  States of 32 bits: the stream of 30 bytes an element keeps the memory busy
-// by itself (71.4 M elements with a 16-bit copy: 304 us, 7.0 TB/s).
+// by itself (71.2 M elements with a 16-bit copy: 307 us, 7.0 TB/s).
 template <typename G, int NG>
 __global__ void __launch_bounds__(kThreads, 10) k_adamw32(const __grid_constant__ Grads<NG> grads,
                                                          const __grid_constant__ StepArgs a) {
@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 10) k_adamw32(const __grid_constant_
 }
 
 // States of 8 bits: half the bytes and twice the arithmetic.  Small CTAs in the order of the
-// memory, many of them at once (285 M elements with bf16 gradients and a bf16 copy: 693 us, 6.6
+// memory, many of them at once (285 M elements with bf16 gradients and a bf16 copy: 688 us, 6.6
 // TB/s; CTAs of 256 threads 710; CTAs that stay and take every 608th chunk, with loads three
 // blocks ahead in shared memory, 831: they drift apart, and the memory's pages with them).
 __device__ __forceinline__ void load_256(float* x, const float* from) {

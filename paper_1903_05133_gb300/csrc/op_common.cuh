@@ -1,6 +1,6 @@
 // Shared by the operator translation units (grouped products, token log
-// probabilities, AdamW): element types, 16-byte vectors of them, and the device
-// error word of their bounded waits.
+// probabilities, AdamW): element types and pairs of them, the table of what is done
+// once a device, and arithmetic on two floats an instruction.
 #pragma once
 #include <cstdint>
 #include <cuda_bf16.h>

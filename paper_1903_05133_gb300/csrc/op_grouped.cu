@@ -261,7 +261,7 @@ __device__ __forceinline__ void emit_rows(const Args& a, const float* v, int row
     named_barrier_sync(bar, 128);
     if (!a.wide_out) {
       // rows that are not aligned for vectors: a thread a feature, so that a row's leave side by
-      // side (2 groups, 4249 rows, 258 -> 1087, bf16: 25 us; a vector's features by one thread, 37)
+      // side (2 groups, 4249 rows, 258 -> 1087, bf16: 21 us; a vector's features by one thread, 37)
       OUT* o = static_cast<OUT*>(a.out) + static_cast<int64_t>(row0 + j) * a.out_ld + m0 + et;
       const int n = m0 + et < a.m ? rows - j : 0;
       const uint32_t* p = &hv[0].x;
@@ -309,7 +309,7 @@ __device__ __forceinline__ void emit_rows(const Args& a, const float* v, int row
 // A warp holds 32 features (rows of dW, one a lane) of 32 columns at a time.  Rows of 128
 // bytes are put together in shared memory (16-byte pieces swapped by the row, against bank
 // conflicts), and eight lanes store a row.  (32 groups of 512 rows, 4096 x 4096, 16 bits: lanes
-// storing their own rows 500 us, bulk stores of boxes with 64-byte rows 409, this 376.)  Rows
+// storing their own rows 500 us, bulk stores of boxes with 64-byte rows 409, this 376 to 380.)  Rows
 // that are not aligned for that leave value by value, side by side.
 constexpr int kWarpStage = 4096;
 __device__ __forceinline__ void emit_weights(const Args& a, const float* v, int g, int f0, int c, int end,
@@ -505,7 +505,7 @@ __device__ __forceinline__ bool finish_tile(const Args& a, const Tile& t, uint32
 // The weights' bytes are what counts, so the stages are many and small: a chunk of weights
 // is 16 KB, and 9 of them (NT = 64: 6) are in flight.  Where there are fewer tiles than SMs, the
 // CTAs of a cluster share a tile: each sums its part of the length and sends each column's sums to
-// the CTA whose column it is, which adds them in the CTAs' order (one row, 4096 -> 4096: 10.6 us; the
+// the CTA whose column it is, which adds them in the CTAs' order (one row, 4096 -> 4096: 10.8 us; the
 // first CTA reading and adding all of them 11.5, one CTA a tile 18.2).
 template <int NT>
 struct One {
@@ -960,7 +960,7 @@ __global__ void __launch_bounds__(MODE == kDw ? kDwThreads : kThreads, 1) __clus
 // divided for again.  One launch for both operands.  Rows of x or dy: the threads go through the
 // vectors.  Weights: 2^`log` neighbouring threads take `per` vectors each of one of the `segs` parts of
 // a row, and pass over groups without rows of x (57 groups of 1718 -> 3496, one row: 218 us with all
-// of them, 22 so).  Small parts keep the threads busy where there are few rows, large ones pass over
+// of them, 21 so).  Small parts keep the threads busy where there are few rows, large ones pass over
 // more at a step.
 struct Pack {
   const uint16_t* src;
@@ -1115,7 +1115,7 @@ int64_t round256(int64_t x) { return (x + 255) / 256 * 256; }
 
 // Parts of each group's rows in the weights' gradient: where its tiles are fewer than half of the
 // pairs of SMs, as many as give every pair a tile, with at least kMinChunks chunks each on average
-// (one group, 30000 rows, 1024 -> 1000, fp32: 151 us with one part, 55 with 4).
+// (one group, 30000 rows, 1024 -> 1000, fp32: 151 us with one part, 53 with 4).
 int dw_split(int groups, int64_t rows, int inner, int outer) {
   const int64_t tiles = groups * static_cast<int64_t>((outer + 2 * kM - 1) / (2 * kM)) * ((inner + kPairCols - 1) / kPairCols);
   return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kSms / 2 / tiles, rows / groups / (kK * kMinChunks))));

@@ -529,7 +529,7 @@ __global__ void __launch_bounds__(THREADS, (TOP ? 1024 : 1536) / THREADS) k_logp
 // ---- rows of few classes: a warp a row, which stays in its lanes' registers
 // The maximum is known before the sums, so nothing is rescaled; the likeliest are taken from the
 // lanes' own one after the other.  Only the latency of a row counts here, and warps hide it for one
-// another (8192 rows of 10, fp32: 3.5 us, 22 with a CTA a row; 8192 of 1000, bf16: 8.5 and 23; 100000 of 16: 19
+// another (8192 rows of 10, fp32: 3.3 us, 22 with a CTA a row; 8192 of 1000, bf16: 8.6 and 23; 100000 of 16: 20
 // and 239).
 constexpr int kRowWarps = 8;
 constexpr int kRowUnroll = 8;          // loads in flight of the gradient
@@ -764,8 +764,8 @@ __global__ void __launch_bounds__(kBwdThreads) k_logprobs_backward(const __grid_
   }
 }
 
-// The same for rows of few classes, a warp a row (8192 rows of 10, fp32: 3.5 us, 13 with a CTA a row;
-// 8192 of 1000, bf16: 10.0 and 15.4; 100000 of 16: 18 and 130).
+// The same for rows of few classes, a warp a row (8192 rows of 10, fp32: 3.1 us, 13 with a CTA a row;
+// 8192 of 1000, bf16: 10.2 and 15.4; 100000 of 16: 17 and 130).
 template <typename T, bool ENT>
 __global__ void __launch_bounds__(kRowWarps * 32) k_logprobs_row_backward(const __grid_constant__ BwdArgs a) {
   const int lane = threadIdx.x & 31, classes = static_cast<int>(a.classes);
@@ -832,8 +832,8 @@ cudaError_t launch_forward(const FwdArgs& a, int parts, cudaStream_t s) {
 }
 
 // Few CTAs take 512 threads each; where they fill the GPU, half the threads have half the
-// cost of a row's end and overlap it with other CTAs' loads (8192 rows of 32768 bf16: 127 us with
-// 512 threads, 108 us with 256).
+// cost of a row's end and overlap it with other CTAs' loads (8192 rows of 32768 bf16: 104 us with
+// 512 threads, 85 us with 256).
 template <typename T, bool TOP, bool MASK>
 cudaError_t forward_rows(const FwdArgs& a, cudaStream_t s) {
   const int parts = cluster_size(a.rows, a.classes * static_cast<int64_t>(sizeof(T)));

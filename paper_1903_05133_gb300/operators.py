@@ -4,8 +4,10 @@ probabilities of given classes with their gradient, and AdamW over many tensors.
 Argument marshalling only, as in hier_avg.py: PyTorch provides the memory and the stream, the
 computation runs in the library's CUDA kernels, and the functions are those of
 include/hier_avg.h without the ``hier_avg_`` prefix.  Results are new tensors unless ``out``
-is given.  All tensors of a call are on one GPU, where it runs whichever is current.  A call on
-``stream`` makes its results and workspace there.
+is given, and outside autograd: a result has no history even where an input requires gradients, whose
+calls are grouped_product_dx, grouped_product_dw and token_logprobs_backward.  All tensors of a
+call are on one GPU, where it runs whichever is current.  A call on ``stream`` makes its results and
+workspace there; its inputs are the caller's to keep until it is done.
 """
 from __future__ import annotations
 
