@@ -391,6 +391,100 @@ int hier_avg_adamw_step(hier_avg_adamw* plan, const void* const* grads_dev, int 
                         double lr, double beta1, double beta2, double eps, int64_t t,
                         const float* grad_scale_dev, uint32_t seed, void* stream);
 
+/* Routing.  For each row of logits_dev [rows, experts] the k largest logits (equal ones by index), rising entries
+ * of a row being their order; a logit at or below -1e30 is masked.
+ *   lse = log sum_i e^{z_i};  weight_j = e^{z_j} / (sum over the chosen of e^z), or e^{z_j - lse} (over_all)
+ * Entries that do not exist have expert -1 and weight 0; a row with NaN or +inf has experts -1, and NaN weights and
+ * lse; a row that is masked as a whole has lse -inf.
+ * The entries (row, j) are then sorted by group, in their order within a group.  An entry's group is its expert, or,
+ * with learners_dev [learners + 1] (rising int32 offsets on the device: learner p has the rows
+ * learners[p] .. learners[p+1]), learner * experts + expert; rows of no learner have no group.
+ *   expert_dev, weight_dev  [rows, k]
+ *   offsets_dev             [groups + 1], as the grouped products read them
+ *   place_dev               [rows, k] the entry's place among the sorted, -1: none
+ *   source_dev              [rows * k] the entry row * k + j at each place, -1 behind the last group
+ *   workspace_dev           16-byte aligned, of hier_avg_sort_workspace's bytes (0 for few rows)
+ * hier_avg_sort_by_group sorts given groups group_dev [rows, per_row] (below 0 or >= groups: none).
+ * hier_avg_route_backward takes dweight_dev [rows, k] to the logits' gradient: zero but for the chosen ones, or with
+ * over_all for every expert (logits_dev and lse_dev are read only then; dlogits_dev may be logits_dev itself with the
+ * same ld).  Rows whose weights are NaN give NaN.
+ * Errors: HA_EINVAL; HA_EUNSUPPORTED for k or per_row > 32, more than 1024 experts or groups, or 2^31 entries;
+ * HA_ENOMEM; HA_ECUDA. */
+int hier_avg_sort_workspace(int64_t rows, int per_row, int groups, int64_t* bytes);
+int hier_avg_route(const void* logits_dev, int type, int64_t rows, int experts, int64_t ld, int k, int over_all,
+                   const int32_t* learners_dev, int learners, int32_t* expert_dev, float* weight_dev, float* lse_dev,
+                   int32_t* offsets_dev, int32_t* place_dev, int32_t* source_dev, void* workspace_dev,
+                   int64_t workspace_bytes, void* stream);
+int hier_avg_sort_by_group(const int32_t* group_dev, int64_t rows, int per_row, int groups, int32_t* offsets_dev,
+                           int32_t* place_dev, int32_t* source_dev, void* workspace_dev, int64_t workspace_bytes,
+                           void* stream);
+int hier_avg_route_backward(const float* dweight_dev, const void* logits_dev, int type, int64_t rows, int experts,
+                            int64_t ld, int k, int over_all, const int32_t* expert_dev, const float* weight_dev,
+                            const float* lse_dev, void* dlogits_dev, int64_t dlogits_ld, void* stream);
+
+/* Rows to their groups and back, by the places of a sort: place_dev [rows, per_row], each place in
+ * [0, rows * per_row) named once, others (-1) nowhere.  offsets_dev [groups + 1]: of it only the last is read,
+ * behind which the sorted rows are set to zero.
+ *   hier_avg_dispatch          xs[place[t, j]] = x[t]
+ *   hier_avg_combine           out[t] = sum over j of weight[t, j] y[place[t, j]], in the order of j in fp32
+ *                              (weight_dev NULL: 1 each, which is the gradient of dispatch)
+ *   hier_avg_combine_backward  dy[place[t, j]] = weight[t, j] dout[t],  dweight[t, j] = <dout[t], y[place[t, j]]>
+ *                              (0 where there is no place)
+ *   type                       any HA_TYPE_*, of x, xs, y and dy; out and dout: the same or HA_TYPE_FP32
+ * Errors: HA_EINVAL, HA_EUNSUPPORTED for 2^31 entries, HA_ECUDA. */
+int hier_avg_dispatch(const void* x_dev, int type, int64_t rows, int width, int64_t x_ld, const int32_t* place_dev,
+                      int per_row, const int32_t* offsets_dev, int groups, void* xs_dev, int64_t xs_ld, void* stream);
+int hier_avg_combine(const void* y_dev, int type, int64_t rows, int width, int64_t y_ld, const int32_t* place_dev,
+                     int per_row, const float* weight_dev, void* out_dev, int64_t out_ld, int out_type, void* stream);
+int hier_avg_combine_backward(const void* dout_dev, int dout_type, int64_t dout_ld, const void* y_dev, int type,
+                              int64_t rows, int width, int64_t y_ld, const int32_t* place_dev, int per_row,
+                              const float* weight_dev, const int32_t* offsets_dev, int groups, void* dy_dev,
+                              int64_t dy_ld, float* dweight_dev, void* stream);
+
+/* The norm of all gradients together, sqrt(sum of their squares), and the factor that clips them: max_norm / norm
+ * where norm > max_norm, else 1 (a NaN among them: norm NaN, factor 1).  Tensor i has n[i] contiguous elements of
+ * types[i] at grads_dev[i].  learners > 1: every tensor's first dimension is the learner's (n[i] is a multiple of
+ * learners), and norm_dev and scale_dev [learners] have one of each.  clip: the gradients are then multiplied by
+ * their factor in place, each rounded once; they must not share memory.  scale_dev may be NULL without clip, and
+ * max_norm is then not read.  Squares are summed so that neither their size nor their number is lost: in fp32 over at most 64
+ * elements and a warp, in 64 bits beyond, and in 64 bits at once where fp32's range does not hold them.
+ * workspace_dev: 8-byte aligned, of hier_avg_grad_norm_workspace's bytes.
+ * Errors: HA_EINVAL (gradients that share memory among them), HA_EUNSUPPORTED for more than 44800 tensors or 2^31
+ * chunks of 32 KB, HA_ENOMEM, HA_ECUDA. */
+int hier_avg_grad_norm_workspace(int tensors, const int* types, const int64_t* n, int learners, int64_t* bytes);
+int hier_avg_grad_norm(int tensors, void* const* grads_dev, const int* types, const int64_t* n, int learners,
+                       double max_norm, int clip, float* norm_dev, float* scale_dev, void* workspace_dev,
+                       int64_t workspace_bytes, void* stream);
+
+/* Verification of drafted tokens.  A sequence has K = drafts drafts and K + 1 rows of logits; row i's probabilities
+ * are p_i = softmax(logits_i / temperature) over the allowed classes, and draft i was drawn from probs_i.
+ *   draft i is accepted while uniform_i * probs_i(draft_i) < p_i(draft_i) (probs_dev NULL: 1 for probs_i(draft_i));
+ *   n, the accepted, is the first that is not, or the first draft below 0 (no draft), or K;
+ *   the next token is argmax_j r_j / noise_j, the lowest index of equal ones: r = max(p_n - probs_n, 0) after a
+ *   rejection (without probs: p_n without the draft; p_n where nothing is left), p_n otherwise.
+ * With uniform numbers in [0, 1) and exponential noise the tokens are drawn as from the target itself; K = 0 draws
+ * one token from p.  Decisions are those of 64-bit arithmetic on the given numbers.
+ *   logits_dev   [sequences, K + 1, classes], sequences logits_seq and rows logits_row apart
+ *   drafts_dev   [sequences, K] int32 or int64 (draft_bytes 4 or 8); a draft >= classes is rejected
+ *   uniform_dev  [sequences, K];  noise_dev [sequences, classes], rows noise_ld apart, positive
+ *   probs_dev    [sequences, K, classes] of any HA_TYPE_*, or NULL
+ *   allowed_dev  NULL, or one byte a class, not 0 where it is allowed (strides 0: the same for all)
+ *   tokens_dev   [sequences, K + 1]: the accepted drafts, the next token, then -1
+ *   logp_dev     [sequences, K + 1]: the tokens' log p, 0 where there is none
+ *   accepted_dev [sequences]
+ * A logit at or below -1e30 counts as not allowed.  A row without an allowed class, or with NaN or +inf among
+ * them, rejects its draft; where it is row n, its token is -1 with log p -inf or NaN.
+ * temperature 2^-126 .. 1e27.  workspace_dev: 16-byte aligned, of hier_avg_verify_workspace's bytes.
+ * Errors: HA_EINVAL, HA_EUNSUPPORTED for 2^28 rows, HA_ENOMEM, HA_ECUDA. */
+int hier_avg_verify_workspace(int64_t sequences, int drafts, int64_t* bytes);
+int hier_avg_verify_drafts(const void* logits_dev, int type, int64_t sequences, int drafts, int64_t classes,
+                           int64_t logits_seq, int64_t logits_row, const void* drafts_dev, int draft_bytes,
+                           const float* uniform_dev, const float* noise_dev, int64_t noise_ld, const void* probs_dev,
+                           int probs_type, int64_t probs_seq, int64_t probs_row, const uint8_t* allowed_dev,
+                           int64_t allowed_seq, int64_t allowed_row, double temperature, int32_t* tokens_dev,
+                           int32_t* accepted_dev, float* logp_dev, void* workspace_dev, int64_t workspace_bytes,
+                           void* stream);
+
 /* Synchronise `stream` and report a bounded wait inside a grouped product that ran out on
  * this device (HA_ETIMEOUT, once; the outputs are then invalid) or an asynchronous error.
  * The device has one word for all streams: another stream's wait that has run out by then

@@ -13,7 +13,9 @@ def __getattr__(name):
         from . import hier_avg
         return getattr(hier_avg, name)
     if name in ("grouped_product", "grouped_product_dx", "grouped_product_dw", "token_logprobs",
-                "token_logprobs_backward", "TokenLogprobs", "AdamW", "operator_check"):
+                "token_logprobs_backward", "TokenLogprobs", "AdamW", "operator_check", "route", "route_backward", "sort_by_group",
+                "Routing", "Sorted", "dispatch", "dispatch_backward", "combine", "combine_backward", "grad_norm",
+                "clip_gradients", "GradNorm", "verify_drafts", "VerifiedDrafts"):
         from . import operators
         return getattr(operators, name)
     raise AttributeError(name)

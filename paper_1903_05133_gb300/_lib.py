@@ -76,6 +76,27 @@ SIGNATURES = {
                                     c_void_p, c_void_p]),
     "hier_avg_adamw_step": (c_int, [c_void_p, c_void_p, c_int, c_double, c_double, c_double,
                                     c_double, c_int64, c_void_p, ctypes.c_uint32, c_void_p]),
+    "hier_avg_sort_workspace": (c_int, [c_int64, c_int, c_int, P_int64]),
+    "hier_avg_route": (c_int, [c_void_p, c_int, c_int64, c_int, c_int64, c_int, c_int, c_void_p, c_int, c_void_p,
+                               c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_void_p]),
+    "hier_avg_sort_by_group": (c_int, [c_void_p, c_int64, c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p,
+                                       c_int64, c_void_p]),
+    "hier_avg_route_backward": (c_int, [c_void_p, c_void_p, c_int, c_int64, c_int, c_int64, c_int, c_int, c_void_p,
+                                        c_void_p, c_void_p, c_void_p, c_int64, c_void_p]),
+    "hier_avg_dispatch": (c_int, [c_void_p, c_int, c_int64, c_int, c_int64, c_void_p, c_int, c_void_p, c_int,
+                                  c_void_p, c_int64, c_void_p]),
+    "hier_avg_combine": (c_int, [c_void_p, c_int, c_int64, c_int, c_int64, c_void_p, c_int, c_void_p, c_void_p,
+                                 c_int64, c_int, c_void_p]),
+    "hier_avg_combine_backward": (c_int, [c_void_p, c_int, c_int64, c_void_p, c_int, c_int64, c_int, c_int64, c_void_p,
+                                          c_int, c_void_p, c_void_p, c_int, c_void_p, c_int64, c_void_p, c_void_p]),
+    "hier_avg_grad_norm_workspace": (c_int, [c_int, c_void_p, c_void_p, c_int, P_int64]),
+    "hier_avg_grad_norm": (c_int, [c_int, c_void_p, c_void_p, c_void_p, c_int, c_double, c_int, c_void_p, c_void_p,
+                                   c_void_p, c_int64, c_void_p]),
+    "hier_avg_verify_workspace": (c_int, [c_int64, c_int, P_int64]),
+    "hier_avg_verify_drafts": (c_int, [c_void_p, c_int, c_int64, c_int, c_int64, c_int64, c_int64, c_void_p, c_int,
+                                       c_void_p, c_void_p, c_int64, c_void_p, c_int, c_int64, c_int64, c_void_p,
+                                       c_int64, c_int64, c_double, c_void_p, c_void_p, c_void_p, c_void_p, c_int64,
+                                       c_void_p]),
     "hier_avg_operator_check": (c_int, [c_void_p]),
     "hier_avg_strerror": (c_char_p, [c_int]),
     "hier_avg_last_error": (c_char_p, [c_void_p]),

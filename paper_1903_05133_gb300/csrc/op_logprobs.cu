@@ -16,45 +16,15 @@
 namespace ha {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kMaxWarps = 16;
 constexpr int kUnroll = 4;            // 16-byte loads in flight a thread
 constexpr int kCap = 2048;            // candidates kept before they are cut to the best
 constexpr int kMaxTop = 32;
 constexpr int kMaxCluster = 8;
 
-__device__ __forceinline__ float exp2_fast(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-
 struct Stat {
   float m, S, A;      // m: largest logit as given (before the temperature)
 };
-
-// Logits at or below this count as not allowed, so a mask written with the lowest finite value
-// of bf16 or fp32 works as one of minus infinity does.  They are raised to it on loading, which
-// keeps every difference finite, and a row whose largest logit it is has no class.  (bf16: the
-// largest value of the type that is not above -1e30.)
-template <typename T> constexpr float kNone = -1e30f;
-template <> constexpr float kNone<__nv_bfloat16> = -1.0002555517425873e30f;
-
-// Order of floats (no NaN) as unsigned integers, and back: 2^31 plus or minus the magnitude's bits, so
-// that zeros of both signs are the same.
-__device__ __forceinline__ uint32_t ordered(float v) {
-  const uint32_t u = __float_as_uint(v);
-  return u & 0x80000000u ? 0u - u : u | 0x80000000u;
-}
-__device__ __forceinline__ float from_ordered(uint32_t o) {
-  return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : 0u - o);
-}
 
 // The warp's sums, the same in every lane; c = log2(e) / temperature.
 __device__ __forceinline__ Stat warp_join(Stat s, float c) {
@@ -170,20 +140,8 @@ __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-template <typename T> constexpr int kVec = 16 / sizeof(T);
 template <typename T> constexpr bool kIsBf16 = false;
 template <> constexpr bool kIsBf16<__nv_bfloat16> = true;
-
-template <typename T>
-__device__ __forceinline__ void unpack(uint4 w, float* v) {
-  if constexpr (sizeof(T) == 4) {
-    v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y);
-    v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
-  } else {
-    widen2<T>(w.x, v[0], v[1]); widen2<T>(w.y, v[2], v[3]);
-    widen2<T>(w.z, v[4], v[5]); widen2<T>(w.w, v[6], v[7]);
-  }
-}
 
 // Raises a vector's entries to kNone where they are below it or not allowed; returns the
 // largest (not a NaN).  16-bit entries stay packed, two to an instruction.

@@ -1,0 +1,323 @@
+// The norm of all gradients together, the factor that clips them, and clipping in place:
+//   norm = sqrt(sum over the tensors of their elements' squares),  scale = max_norm / norm where norm > max_norm, else 1,
+// one of each for a learner where the tensors' first dimension is the learner's.
+//
+// One CTA a chunk of 32 KB, whose squares are summed in fp32 by each thread and its warp and in 64 bits from
+// there on; a second kernel adds the chunks' sums in a fixed order.  Squares that pass fp32's range, or are
+// so small that it loses them, show in a chunk's sum, which is then taken again in 64 bits from the
+// values, still in registers.  Clipping reads the gradients a second time, the last ones first, since those are still in L2.
+#include <algorithm>
+#include <cfloat>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <utility>
+#include <vector>
+
+#include "op_common.cuh"
+
+namespace ha {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kLoads = 8;                 // 16-byte loads of a thread
+constexpr int kChunkBytes = kThreads * kLoads * 16;
+constexpr int kFew = 64, kSome = 384, kMany = 1400;      // tensors of a launch; its arguments are at most 32,764 bytes
+constexpr int kMaxRanges = 32;
+constexpr int kEndThreads = 1024;
+constexpr double kSmallSum = 0x1p-100;    // a chunk's lost squares, 2^14 times 2^-150, are 2^-36 of it
+
+template <int N> struct Table {
+  const void* p[N];
+  int64_t n[N];                           // elements of a learner
+  int first[N + 1];                       // chunks of a learner before each tensor
+  uint8_t type[N];
+  int tensors;
+};
+struct Ranges {
+  int64_t base[kMaxRanges];               // a launch's first sum
+  int chunks[kMaxRanges];                 // and its chunks of each learner
+  int n;
+};
+
+// A chunk: its elements and, from the first 16-byte boundary on, whole vectors.
+template <typename T> struct Span {
+  T* p;
+  int n, head, vecs;
+  __device__ __forceinline__ Span(const void* base, int64_t at, int64_t left) {
+    constexpr int kElements = kChunkBytes / sizeof(T);
+    p = static_cast<T*>(const_cast<void*>(base)) + at;
+    n = static_cast<int>(left < kElements ? left : kElements);
+    const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+    head = min(n, shift ? kVec<T> - shift : 0);
+    vecs = (n - head) / kVec<T>;
+  }
+  // The elements outside the vectors, at most 2 (kVec - 1): one a thread; -1 for the others.
+  __device__ __forceinline__ int single() const {
+    const int tid = threadIdx.x, tail = head + vecs * kVec<T>;
+    if (tid < head) return tid;
+    return tid >= 32 && tail + tid - 32 < n ? tail + tid - 32 : -1;
+  }
+};
+
+template <typename F>
+__device__ __forceinline__ double block_sum(F x, double* part, int threads) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = static_cast<double>(x);
+  __syncthreads();
+  double s = 0.0;
+  for (int w = 0; w < threads / 32; ++w) s += part[w];
+  __syncthreads();
+  return s;
+}
+
+template <typename T>
+__device__ __forceinline__ double sum_of_squares(const Span<T>& c, double* part) {
+  const int tid = threadIdx.x;
+  uint4 w[kLoads];
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) {
+    const int i = u * kThreads + tid;
+    w[u] = i < c.vecs ? __ldg(reinterpret_cast<const uint4*>(c.p + c.head) + i) : make_uint4(0, 0, 0, 0);
+  }
+  const int one = c.single();
+  const float x = one >= 0 ? Elem<T>::up(c.p[one]) : 0.0f;
+  Pair s[2] = {pair(x * x, 0.0f), pair(0.0f, 0.0f)};
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) {
+    float v[kVec<T>];
+    unpack<T>(w[u], v);
+#pragma unroll
+    for (int e = 0; e < kVec<T>; e += 2) {
+      const Pair q = pair(v[e], v[e + 1]);
+      s[e / 2 & 1] = fma2(q, q, s[e / 2 & 1]);
+    }
+  }
+  float a, b;
+  halves(add2(s[0], s[1]), a, b);
+  double sum = block_sum(a + b, part, kThreads);
+  if (sum >= kSmallSum && sum < INFINITY) return sum;
+  uint32_t any = __float_as_uint(x) & 0x7FFFFFFFu;
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) {
+    constexpr uint32_t kSigns = sizeof(T) == 2 ? 0x7FFF7FFFu : 0x7FFFFFFFu;
+    any |= (w[u].x | w[u].y | w[u].z | w[u].w) & kSigns;
+  }
+  if (!__syncthreads_or(any != 0)) return 0.0;
+  double d = static_cast<double>(x) * x;
+#pragma unroll 1
+  for (int u = 0; u < kLoads; ++u) {
+    float v[kVec<T>];
+    uint4 q = w[0];
+#pragma unroll
+    for (int i = 1; i < kLoads; ++i)
+      if (i == u) q = w[i];
+    unpack<T>(q, v);
+#pragma unroll
+    for (int e = 0; e < kVec<T>; ++e) d += static_cast<double>(v[e]) * v[e];
+  }
+  return block_sum(d, part, kThreads);
+}
+
+template <typename T>
+__device__ __forceinline__ void scale_by(const Span<T>& c, float f) {
+  const int tid = threadIdx.x;
+  uint4* at = reinterpret_cast<uint4*>(c.p + c.head);
+  uint4 w[kLoads];
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) {
+    const int i = u * kThreads + tid;
+    if (i < c.vecs) w[u] = at[i];
+  }
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) {
+    const int i = u * kThreads + tid;
+    float v[kVec<T>];
+    unpack<T>(w[u], v);
+#pragma unroll
+    for (int e = 0; e < kVec<T>; ++e) v[e] *= f;
+    if (i < c.vecs) at[i] = pack<T>(v);
+  }
+  const int one = c.single();
+  if (one >= 0) c.p[one] = Elem<T>::down(Elem<T>::up(c.p[one]) * f);
+}
+
+// The chunk `c` of learner `p`: f(span).
+template <int N, typename F>
+__device__ __forceinline__ void with_chunk(const Table<N>& t, int p, int c, F f) {
+  int low = 0, high = t.tensors - 1;      // the last tensor whose first chunk is not behind c
+  while (low < high) {
+    const int mid = (low + high + 1) / 2;
+    if (t.first[mid] <= c) low = mid;
+    else high = mid - 1;
+  }
+  const int64_t size = t.type[low] == HA_TYPE_FP32 ? 4 : 2, skip = static_cast<int64_t>(c - t.first[low]) * (kChunkBytes / size);
+  const int64_t at = p * t.n[low] + skip, left = t.n[low] - skip;
+  if (t.type[low] == HA_TYPE_FP32) f(Span<float>(t.p[low], at, left));
+  else if (t.type[low] == HA_TYPE_BF16) f(Span<__nv_bfloat16>(t.p[low], at, left));
+  else f(Span<__half>(t.p[low], at, left));
+}
+
+template <int N>
+__global__ void __launch_bounds__(kThreads) k_squares(const __grid_constant__ Table<N> t, double* sums) {
+  __shared__ double part[kThreads / 32];
+  const int chunks = t.first[t.tensors], p = blockIdx.x / chunks, c = blockIdx.x % chunks;
+  let_next_start();
+  with_chunk(t, p, c, [&](auto span) {
+    const double s = sum_of_squares(span, part);
+    if (threadIdx.x == 0) sums[blockIdx.x] = s;
+  });
+}
+
+// A CTA a learner.
+__global__ void __launch_bounds__(kEndThreads) k_norm(const double* __restrict__ sums, const __grid_constant__ Ranges r,
+                                                      double max_norm, float* norm, float* scale) {
+  __shared__ double part[kEndThreads / 32];
+  let_next_start();
+  wait_for_previous();
+  const int p = blockIdx.x;
+  double s = 0.0;
+  for (int i = 0; i < r.n; ++i) {
+    const double* from = sums + r.base[i] + static_cast<int64_t>(p) * r.chunks[i];
+#pragma unroll 4
+    for (int c = threadIdx.x; c < r.chunks[i]; c += kEndThreads) s += from[c];
+  }
+  s = sqrt(block_sum(s, part, kEndThreads));
+  if (threadIdx.x == 0) {
+    norm[p] = static_cast<float>(s);
+    if (scale) scale[p] = s > max_norm ? static_cast<float>(max_norm / s) : 1.0f;
+  }
+}
+
+template <int N>
+__global__ void __launch_bounds__(kThreads) k_clip(const __grid_constant__ Table<N> t, const float* scale) {
+  const int chunks = t.first[t.tensors], b = static_cast<int>(gridDim.x - 1 - blockIdx.x), p = b / chunks, c = b % chunks;
+  let_next_start();
+  wait_for_previous();
+  const float f = scale[p];
+  if (f == 1.0f) return;
+  with_chunk(t, p, c, [&](auto span) { scale_by(span, f); });
+}
+
+// Chunks of one learner's part of a tensor.
+int64_t chunks_of(int64_t n, int type) {
+  const int64_t each = kChunkBytes / type_size(type);
+  return (n + each - 1) / each;
+}
+
+struct Call {
+  const void* const* grads;
+  const int* types;
+  const int64_t* n;
+  int learners;
+  double* sums;
+  float* scale;
+  cudaStream_t s;
+};
+
+template <int N>
+cudaError_t launch_range(const Call& a, int t0, int t1, int64_t base, bool clip, int& chunks) {
+  Table<N> t;
+  std::memset(&t, 0, sizeof t);
+  t.tensors = t1 - t0;
+  int64_t at = 0;
+  for (int i = t0; i < t1; ++i) {
+    t.p[i - t0] = a.grads[i];
+    t.n[i - t0] = a.n[i] / a.learners;
+    t.type[i - t0] = static_cast<uint8_t>(a.types[i]);
+    t.first[i - t0] = static_cast<int>(at);
+    at += chunks_of(t.n[i - t0], a.types[i]);
+  }
+  t.first[t.tensors] = static_cast<int>(at);
+  chunks = static_cast<int>(at);
+  if (at == 0) return cudaSuccess;
+  const unsigned grid = static_cast<unsigned>(at * a.learners);
+  if (clip) return launch_early(k_clip<N>, grid, kThreads, 0, a.s, t, static_cast<const float*>(a.scale));
+  k_squares<N><<<grid, kThreads, 0, a.s>>>(t, a.sums + base);
+  return cudaGetLastError();
+}
+cudaError_t launch_all(const Call& a, int tensors, bool clip, Ranges& r) {
+  r.n = 0;
+  int64_t base = 0;
+  const int each = tensors <= kFew ? kFew : tensors <= kSome ? kSome : kMany;
+  for (int t = 0; t < tensors; t += each) {
+    const int end = std::min(t + each, tensors);
+    int chunks = 0;
+    const cudaError_t e = each == kFew    ? launch_range<kFew>(a, t, end, base, clip, chunks)
+                          : each == kSome ? launch_range<kSome>(a, t, end, base, clip, chunks)
+                                          : launch_range<kMany>(a, t, end, base, clip, chunks);
+    if (e != cudaSuccess) return e;
+    r.base[r.n] = base;
+    r.chunks[r.n++] = chunks;
+    base += static_cast<int64_t>(chunks) * a.learners;
+  }
+  return cudaSuccess;
+}
+
+// The sums of a call's chunks; below 0: a status.
+int64_t count_chunks(int tensors, const int* types, const int64_t* n, int learners) {
+  if (tensors < 1 || learners < 1 || !types || !n) return HA_EINVAL;
+  if (tensors > kMaxRanges * kMany) return HA_EUNSUPPORTED;
+  int64_t chunks = 0;
+  for (int i = 0; i < tensors; ++i) {
+    if (!type_ok(types[i]) || n[i] < 0 || n[i] % learners) return HA_EINVAL;
+    chunks += std::min(chunks_of(n[i] / learners, types[i]), int64_t(1) << 31) * learners;
+    if (chunks > 0x7FFFFFFF) return HA_EUNSUPPORTED;
+  }
+  return chunks;
+}
+
+// Do the gradients share memory?  They are usually in the order of their addresses.
+bool overlap(int tensors, const void* const* grads, const int* types, const int64_t* n) {
+  std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+  spans.reserve(tensors);
+  for (int i = 0; i < tensors; ++i)
+    if (n[i]) {
+      const uintptr_t p = reinterpret_cast<uintptr_t>(grads[i]);
+      spans.push_back({p, p + static_cast<uintptr_t>(n[i]) * type_size(types[i])});
+    }
+  if (!std::is_sorted(spans.begin(), spans.end())) std::sort(spans.begin(), spans.end());
+  for (size_t i = 1; i < spans.size(); ++i)
+    if (spans[i].first < spans[i - 1].second) return true;
+  return false;
+}
+
+}  // namespace
+}  // namespace ha
+
+using namespace ha;
+
+extern "C" int hier_avg_grad_norm_workspace(int tensors, const int* types, const int64_t* n, int learners, int64_t* bytes) {
+  if (!bytes) return HA_EINVAL;
+  const int64_t chunks = count_chunks(tensors, types, n, learners);
+  if (chunks < 0) return static_cast<int>(chunks);
+  *bytes = std::max<int64_t>(chunks, 1) * static_cast<int64_t>(sizeof(double));
+  return HA_OK;
+}
+
+extern "C" int hier_avg_grad_norm(int tensors, void* const* grads_dev, const int* types, const int64_t* n, int learners,
+                                  double max_norm, int clip, float* norm_dev, float* scale_dev, void* workspace_dev,
+                                  int64_t workspace_bytes, void* stream) {
+  const int64_t chunks = count_chunks(tensors, types, n, learners);
+  if (chunks < 0) return static_cast<int>(chunks);
+  if (!grads_dev || !norm_dev || (clip && !scale_dev) || (scale_dev && !(max_norm >= 0.0 && std::isfinite(max_norm))))
+    return HA_EINVAL;
+  for (int i = 0; i < tensors; ++i)
+    if (n[i] && (!grads_dev[i] || reinterpret_cast<uintptr_t>(grads_dev[i]) % type_size(types[i]))) return HA_EINVAL;
+  if (!workspace_dev || workspace_bytes < chunks * static_cast<int64_t>(sizeof(double))) return HA_ENOMEM;
+  if (reinterpret_cast<uintptr_t>(workspace_dev) % sizeof(double)) return HA_EINVAL;
+  try {
+    if (clip && overlap(tensors, grads_dev, types, n)) return HA_EINVAL;
+  } catch (const std::bad_alloc&) {
+    return HA_ENOMEM;
+  }
+  const Call a = {grads_dev, types, n, learners, static_cast<double*>(workspace_dev), scale_dev, static_cast<cudaStream_t>(stream)};
+  Ranges r;
+  std::memset(&r, 0, sizeof r);
+  cudaError_t e = launch_all(a, tensors, false, r);
+  if (e == cudaSuccess)
+    e = launch_early(k_norm, static_cast<unsigned>(learners), kEndThreads, 0, a.s, a.sums, r, max_norm, norm_dev, scale_dev);
+  if (e == cudaSuccess && clip) e = launch_all(a, tensors, true, r);
+  return e == cudaSuccess ? HA_OK : HA_ECUDA;
+}

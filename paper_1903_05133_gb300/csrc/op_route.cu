@@ -1,0 +1,566 @@
+// The router of rows to experts, the sort of rows by their group, and the router's gradient.
+//
+// For a row z over E experts: the k largest logits (equal ones by index), lse = log sum_i e^(z_i), and
+//   over the chosen: w_j = e^(z_j) / sum over the chosen of e^z,   over all: w_j = e^(z_j - lse).
+// The entries (row, j) are then sorted by group, in their order within a group: a counting sort.
+// Each warp takes rows that follow one another and counts them by group in shared memory, where a
+// group's count is the next entry's rank; the CTA's warps, then the CTAs add up their counts in order.
+//
+//   over the chosen: dz_j = w_j (dw_j - s) at the chosen, 0 elsewhere;  s = sum over the chosen of w dw
+//   over all:        dz_i = [i chosen] w_i dw_i - p_i s,                p_i = e^(z_i - lse)
+#include <algorithm>
+#include <cmath>
+
+#include "op_common.cuh"
+
+namespace ha {
+namespace {
+
+constexpr int kMaxExperts = 1024, kMaxGroups = 1024, kMaxChosen = 32;
+constexpr int kWarps = 8;                 // of a CTA, where there are several
+constexpr int kOneWarps = 32;             // of a CTA that sorts all by itself, at most
+template <int R> constexpr int kOneRouteWarps = R <= 8 ? kOneWarps : kOneWarps / 2;      // their logits fill the registers
+constexpr int kRankBits = 21;             // an entry in work: its group above, its rank below
+constexpr int kStaged = 2048;             // entries of a CTA that are kept in shared memory meanwhile
+constexpr int64_t kMaxChunk = int64_t(1) << (kRankBits - 1);
+
+struct SortArgs {
+  int* offsets;                           // [groups + 1]
+  int* place;                             // [entries]
+  int* source;                            // [entries]
+  int* counts;                            // [groups, chunks]
+  int* totals;                            // [groups]
+  int64_t entries;
+  int64_t per;                            // entries of a chunk
+  int groups, chunks;
+};
+
+// Exclusive sums of value[0, n) in place and their total behind them.
+__device__ __forceinline__ void block_scan(int* value, int n, int* warp_sum) {
+  const int tid = threadIdx.x, lane = tid & 31, warps = blockDim.x >> 5;
+  const int each = (n + blockDim.x - 1) / blockDim.x, at = tid * each;
+  int sum = 0;
+  for (int i = at; i < min(at + each, n); ++i) sum += value[i];
+  int run = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(~0u, run, o);
+    if (lane >= o) run += x;
+  }
+  if (lane == 31) warp_sum[tid >> 5] = run;
+  __syncthreads();
+  if (tid < 32) {
+    int w = tid < warps ? warp_sum[tid] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(~0u, w, o);
+      if (lane >= o) w += x;
+    }
+    if (tid < warps) warp_sum[tid] = w;
+  }
+  __syncthreads();
+  int before = run - sum + (tid >= 32 ? warp_sum[(tid >> 5) - 1] : 0);
+  for (int i = at; i < min(at + each, n); ++i) {
+    const int v = value[i];
+    value[i] = before;
+    before += v;
+  }
+  if (tid == 0) value[n] = warp_sum[warps - 1];
+  __syncthreads();
+}
+
+// The end of a chunk's first pass: hist [warps, groups] holds each warp's counts, stage the entries with
+// their rank in their warp.  The ranks become those in the chunk, or with ONE the places.
+template <bool ONE>
+__device__ __forceinline__ void end_chunk(const SortArgs& a, int* hist, int* total, const int* stage, int64_t e0, int n) {
+  __shared__ int warp_sum[32];
+  const int warps = blockDim.x >> 5;
+  __syncthreads();
+  for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
+    int run = 0;
+    for (int w = 0; w < warps; ++w) {
+      const int c = hist[w * a.groups + g];
+      hist[w * a.groups + g] = run;
+      run += c;
+    }
+    if (ONE) total[g] = run;
+    else a.counts[static_cast<int64_t>(g) * a.chunks + blockIdx.x] = run;
+  }
+  __syncthreads();
+  if (ONE) {
+    block_scan(total, a.groups, warp_sum);
+    for (int g = threadIdx.x; g <= a.groups; g += blockDim.x) a.offsets[g] = total[g];
+  }
+}
+
+// ---------------------------------------------------------------- the router
+struct RouteArgs {
+  const void* logits;
+  int64_t rows, ld;
+  const int* learners;                    // nullptr: one
+  int n_learners, experts, k;
+  bool all;
+  int* expert;
+  float* weight;
+  float* lse;
+  SortArgs sort;
+};
+
+// A warp takes a row; lane l holds the logits l, l + 32, ...
+template <typename T, int R, bool ONE>
+__global__ void __launch_bounds__(32 * (ONE ? kOneRouteWarps<R> : kWarps)) k_route(const __grid_constant__ RouteArgs a) {
+  extern __shared__ int dyn[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int G = a.sort.groups, k = a.k;
+  int* hist = dyn;                                            // [warps, groups]
+  int* total = hist + warps * G;                              // [groups + 1] (ONE)
+  const int64_t per_rows = a.sort.per / k, r0 = blockIdx.x * per_rows;
+  const int n_rows = static_cast<int>(min(per_rows, a.rows - r0));
+  int* stage = a.sort.per <= kStaged ? total + G + 1 : a.sort.place + r0 * k;
+  let_next_start();
+  for (int i = threadIdx.x; i < warps * G; i += blockDim.x) hist[i] = 0;
+  __syncthreads();
+
+  const int each = (n_rows + warps - 1) / warps, first = min(warp * each, n_rows), last = min(first + each, n_rows);
+  int learner = 0;
+  if (a.learners && first < last) {                           // learners that end at or before the warp's first row
+    int high = a.n_learners;
+    while (learner < high) {
+      const int mid = (learner + high) / 2;
+      if (a.learners[mid + 1] <= r0 + first) learner = mid + 1;
+      else high = mid;
+    }
+  }
+  for (int r = first; r < last; ++r) {
+    const int64_t row = r0 + r;
+    const T* z = static_cast<const T*>(a.logits) + row * a.ld;
+    float v[R];
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+      const int i = u * 32 + lane;
+      v[u] = i < a.experts ? Elem<T>::up(z[i]) : -INFINITY;
+    }
+    bool bad = false;                                         // NaN or infinity among them
+    uint32_t key[R], most = 0;                                // 0: masked
+    int at = 0;
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+      bad = bad || !(v[u] < INFINITY);
+      key[u] = v[u] > kNone<T> ? ordered(v[u]) : 0;
+    }
+    auto look = [&] {                                         // the lane's largest, the first of equal ones
+      most = 0;
+#pragma unroll
+      for (int u = 0; u < R; ++u)
+        if (key[u] > most) {
+          most = key[u];
+          at = u;
+        }
+    };
+    look();
+    bad = __any_sync(~0u, bad);
+    const uint32_t top = __reduce_max_sync(~0u, most);
+    const float m = from_ordered(top);
+    float S = 0.0f;
+#pragma unroll
+    for (int u = 0; u < R; ++u)
+      if (key[u]) S += exp2_fast((v[u] - m) * kLog2e);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(~0u, S, o);
+
+    uint32_t mine = 0;
+    int index = -1;
+    for (int j = 0; j < k; ++j) {
+      const uint32_t best = __reduce_max_sync(~0u, most);
+      if (best == 0 || bad) break;
+      const uint32_t lanes = __ballot_sync(~0u, most == best);
+      int src = __ffs(lanes) - 1;
+      if (lanes & (lanes - 1))                                // equal logits of two lanes
+        src = __reduce_min_sync(~0u, most == best ? static_cast<uint32_t>(at * 32 + lane) : ~0u) & 31;
+      const int i = __shfl_sync(~0u, at, src) * 32 + src;
+      if (lane == j) {
+        mine = best;
+        index = i;
+      }
+      if (lane == src) {
+#pragma unroll
+        for (int u = 0; u < R; ++u)
+          if (u == at) key[u] = 0;
+        look();
+      }
+    }
+    const float e = index >= 0 ? expf(from_ordered(mine) - m) : 0.0f;
+    float sum = S;
+    if (!a.all) {
+      sum = e;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+    }
+    if (lane < k) {
+      a.expert[row * k + lane] = index;
+      a.weight[row * k + lane] = bad ? NAN : index >= 0 ? e / sum : 0.0f;
+    }
+    if (lane == 0) a.lse[row] = bad ? NAN : top == 0 ? -INFINITY : m + logf(S);
+
+    int group = index;
+    if (a.learners) {
+      while (learner < a.n_learners && a.learners[learner + 1] <= row) ++learner;
+      if (learner >= a.n_learners || row < a.learners[learner]) group = -1;
+      else if (index >= 0) group = learner * a.experts + index;
+    }
+    if (lane < k) {
+      int packed = -1;
+      if (group >= 0) {
+        const int rank = hist[warp * G + group];              // a row's experts differ
+        hist[warp * G + group] = rank + 1;
+        packed = group << kRankBits | rank;
+      }
+      stage[r * k + lane] = packed;
+    }
+    __syncwarp();
+  }
+  end_chunk<ONE>(a.sort, hist, total, stage, r0 * k, n_rows * k);
+  const int64_t e0 = r0 * k;
+  for (int i = first * k + lane; i < last * k; i += 32) {
+    int p = stage[i];
+    if (p >= 0) {
+      p += hist[warp * G + (p >> kRankBits)];
+      if (ONE) {
+        p = (p & ((1 << kRankBits) - 1)) + total[p >> kRankBits];
+        a.sort.source[p] = i;
+      }
+    }
+    a.sort.place[e0 + i] = p;
+  }
+  if (ONE)
+    for (int p = total[G] + threadIdx.x; p < n_rows * k; p += blockDim.x) a.sort.source[p] = -1;
+}
+
+// ---------------------------------------------------------------- the sort of given groups
+template <bool ONE>
+__global__ void __launch_bounds__(32 * (ONE ? kOneWarps : kWarps)) k_group(const int* __restrict__ ids, const __grid_constant__ SortArgs a) {
+  extern __shared__ int dyn[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, G = a.groups;
+  int* hist = dyn;
+  int* total = hist + warps * G;
+  const int64_t e0 = blockIdx.x * a.per;
+  const int n = static_cast<int>(min(a.per, a.entries - e0));
+  int* stage = a.per <= kStaged ? total + G + 1 : a.place + e0;
+  let_next_start();
+  for (int i = threadIdx.x; i < warps * G; i += blockDim.x) hist[i] = 0;
+  __syncthreads();
+  const int each = (n + warps - 1) / warps, first = min(warp * each, n), last = min(first + each, n);
+  for (int i0 = first; i0 < last; i0 += 32) {
+    const int i = i0 + lane;
+    int g = i < last ? ids[e0 + i] : -1;
+    if (g >= G) g = -1;
+    const uint32_t same = __match_any_sync(~0u, g);
+    int packed = -1, count = 0;
+    if (g >= 0) {
+      count = hist[warp * G + g];
+      packed = g << kRankBits | (count + __popc(same & ((1u << lane) - 1)));
+    }
+    __syncwarp();
+    if (g >= 0 && lane == __ffs(same) - 1) hist[warp * G + g] = count + __popc(same);
+    if (i < last) stage[i] = packed;
+    __syncwarp();
+  }
+  end_chunk<ONE>(a, hist, total, stage, e0, n);
+  for (int i = first + lane; i < last; i += 32) {
+    int p = stage[i];
+    if (p >= 0) {
+      p += hist[warp * G + (p >> kRankBits)];
+      if (ONE) {
+        p = (p & ((1 << kRankBits) - 1)) + total[p >> kRankBits];
+        a.source[p] = i;
+      }
+    }
+    a.place[e0 + i] = p;
+  }
+  if (ONE)
+    for (int p = total[G] + threadIdx.x; p < n; p += blockDim.x) a.source[p] = -1;
+}
+
+// A warp a group: the chunks' counts become what comes before each chunk.
+__global__ void __launch_bounds__(kWarps * 32) k_chunks(const __grid_constant__ SortArgs a) {
+  const int lane = threadIdx.x & 31, g = blockIdx.x * kWarps + (threadIdx.x >> 5);
+  let_next_start();
+  wait_for_previous();
+  if (g >= a.groups) return;
+  int* c = a.counts + static_cast<int64_t>(g) * a.chunks;
+  int carry = 0;
+  for (int i0 = 0; i0 < a.chunks; i0 += 128) {
+    int v[4], sum = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + lane * 4 + u;
+      v[u] = i < a.chunks ? c[i] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) sum += v[u];
+    int run = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(~0u, run, o);
+      if (lane >= o) run += x;
+    }
+    int before = carry + run - sum;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + lane * 4 + u;
+      if (i < a.chunks) c[i] = before;
+      before += v[u];
+    }
+    carry += __shfl_sync(~0u, run, 31);
+  }
+  if (lane == 0) a.totals[g] = carry;
+}
+
+// Ranks in a chunk become places.
+__global__ void __launch_bounds__(kWarps * 32) k_place(const __grid_constant__ SortArgs a) {
+  __shared__ int base[kMaxGroups + 1];
+  __shared__ int warp_sum[32];
+  wait_for_previous();
+  for (int g = threadIdx.x; g < a.groups; g += blockDim.x) base[g] = a.totals[g];
+  __syncthreads();
+  block_scan(base, a.groups, warp_sum);
+  const int count = base[a.groups];
+  if (blockIdx.x == 0)
+    for (int g = threadIdx.x; g <= a.groups; g += blockDim.x) a.offsets[g] = base[g];
+  __syncthreads();
+  for (int g = threadIdx.x; g < a.groups; g += blockDim.x)
+    base[g] += a.counts[static_cast<int64_t>(g) * a.chunks + blockIdx.x];
+  __syncthreads();
+  const int64_t e0 = blockIdx.x * a.per, e1 = min(e0 + a.per, a.entries);
+  for (int64_t e = e0 + threadIdx.x; e < e1; e += blockDim.x) {
+    int p = a.place[e];
+    if (p >= 0) {
+      p = (p & ((1 << kRankBits) - 1)) + base[p >> kRankBits];
+      a.place[e] = p;
+      a.source[p] = static_cast<int>(e);
+    }
+    if (e >= count) a.source[e] = -1;
+  }
+}
+
+// ---------------------------------------------------------------- the gradient
+struct RouteBwdArgs {
+  const void* logits;
+  const float *dweight, *weight, *lse;
+  const int* expert;
+  void* out;
+  int64_t rows, ld, out_ld;
+  int experts, k;
+  bool all;
+};
+
+// A warp a row.  The chosen ones' lanes write theirs after the row's others.
+template <typename T, bool ALL>
+__global__ void __launch_bounds__(kWarps * 32) k_route_backward(const __grid_constant__ RouteBwdArgs a) {
+  const int lane = threadIdx.x & 31;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kWarps;
+  for (int64_t row = blockIdx.x * static_cast<int64_t>(kWarps) + (threadIdx.x >> 5); row < a.rows; row += step) {
+    const T* z = ALL ? static_cast<const T*>(a.logits) + row * a.ld : nullptr;
+    T* out = static_cast<T*>(a.out) + row * a.out_ld;
+    int i = -1;
+    float w = 0.0f, g = 0.0f;
+    bool bad = false;
+    if (lane < a.k) {
+      i = a.expert[row * a.k + lane];
+      w = a.weight[row * a.k + lane];
+      bad = w != w;
+      if (i < 0 || i >= a.experts) i = -1;
+      else g = w * a.dweight[row * a.k + lane];
+    }
+    bad = __any_sync(~0u, bad);
+    float s = g;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
+    // an expert that is named twice has the sum of both
+    const uint32_t same = __match_any_sync(~0u, i < 0 ? -1 - lane : i);
+    if (__any_sync(~0u, i >= 0 && (same & (same - 1)))) {
+      float g2 = 0.0f, w2 = 0.0f;
+      for (int j = 0; j < a.k; ++j) {
+        const float gj = __shfl_sync(~0u, g, j), wj = __shfl_sync(~0u, w, j);
+        if (same >> j & 1u) {
+          g2 += gj;
+          w2 += wj;
+        }
+      }
+      g = g2;
+      w = w2;
+    }
+    if constexpr (ALL) {
+      const float lse0 = a.lse[row], lse = lse0 == -INFINITY ? INFINITY : lse0;
+      const float zi = i >= 0 ? Elem<T>::up(z[i]) : 0.0f;
+      __syncwarp();                                           // out may be the logits themselves
+      auto p = [&](float x) { return x > kNone<T> ? exp2_fast((x - lse) * kLog2e) : x == x ? 0.0f : x; };
+      for (int j = lane; j < a.experts; j += 32) {
+        const float x = Elem<T>::up(z[j]);
+        out[j] = Elem<T>::down(bad ? NAN : -p(x) * s);
+      }
+      __syncwarp();
+      if (i >= 0) out[i] = Elem<T>::down(bad ? NAN : fmaf(-p(zi), s, g));
+    } else {
+      for (int j = lane; j < a.experts; j += 32) out[j] = Elem<T>::down(bad ? NAN : 0.0f);
+      __syncwarp();
+      if (i >= 0) out[i] = Elem<T>::down(bad ? NAN : fmaf(-w, s, g));
+    }
+  }
+}
+
+// ---------------------------------------------------------------- launches
+// Chunks of a sort: CTAs of 8 warps, four on each of the 152 SMs, more where a chunk's ranks would not fit.
+int64_t chunk_units(int64_t units, int64_t entries_each) {
+  int64_t per = (units + 152 * 4 - 1) / (152 * 4);
+  per = std::max<int64_t>(per, 1);
+  return std::min(per, kMaxChunk / entries_each);
+}
+int64_t workspace_ints(int64_t entries, int unit, int groups) {
+  const int64_t units = entries / unit, per = chunk_units(units, unit);
+  return (static_cast<int64_t>(groups)) * ((units + per - 1) / per) + groups;
+}
+// The entries that one CTA sorts by itself: a second and a third launch take longer than its few rounds.
+constexpr int64_t kOneRows = 256, kOneEntries = 2048;
+
+size_t sort_smem(int warps, int groups, int64_t per) {
+  return sizeof(int) * (static_cast<size_t>(warps) * groups + groups + 1 + (per <= kStaged ? per : 0));
+}
+
+cudaError_t end_sort(const SortArgs& a, cudaStream_t s) {
+  cudaError_t e = launch_early(k_chunks, (a.groups + kWarps - 1) / kWarps, kWarps * 32, 0, s, a);
+  if (e != cudaSuccess) return e;
+  return launch_early(k_place, static_cast<unsigned>(a.chunks), kWarps * 32, 0, s, a);
+}
+
+template <typename T, int R>
+cudaError_t route_rows(RouteArgs a, bool one, cudaStream_t s) {
+  static bool one_ok[kMaxDevices], ok[kMaxDevices];
+  const int warps = one ? static_cast<int>(std::min<int64_t>(a.rows, kOneRouteWarps<R>)) : kWarps;
+  const size_t smem = sort_smem(warps, a.sort.groups, a.sort.per);
+  const auto kernel = one ? k_route<T, R, true> : k_route<T, R, false>;
+  cudaError_t e = allow_smem(kernel, 200 << 10, one ? one_ok : ok);
+  if (e != cudaSuccess) return e;
+  kernel<<<static_cast<unsigned>(a.sort.chunks), warps * 32, smem, s>>>(a);
+  if ((e = cudaGetLastError()) != cudaSuccess || one) return e;
+  return end_sort(a.sort, s);
+}
+
+template <typename T>
+cudaError_t route_type(const RouteArgs& a, bool one, cudaStream_t s) {
+  if (a.experts <= 64) return route_rows<T, 2>(a, one, s);
+  if (a.experts <= 128) return route_rows<T, 4>(a, one, s);
+  if (a.experts <= 256) return route_rows<T, 8>(a, one, s);
+  if (a.experts <= 512) return route_rows<T, 16>(a, one, s);
+  return route_rows<T, 32>(a, one, s);
+}
+
+template <typename T>
+cudaError_t backward_type(const RouteBwdArgs& a, cudaStream_t s) {
+  const int64_t ctas = std::min<int64_t>((a.rows + kWarps - 1) / kWarps, 152 * 8 * 8);
+  const auto kernel = a.all ? k_route_backward<T, true> : k_route_backward<T, false>;
+  kernel<<<static_cast<unsigned>(ctas), kWarps * 32, 0, s>>>(a);
+  return cudaGetLastError();
+}
+
+bool misaligned(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
+
+// Fills in a sort's chunks; false where the workspace is too small.
+bool plan_sort(SortArgs& a, int unit, bool one, void* ws, int64_t bytes) {
+  const int64_t units = a.entries / unit, per = one ? units : chunk_units(units, unit);
+  a.per = per * unit;
+  a.chunks = static_cast<int>((units + per - 1) / per);
+  if (one) return true;
+  const int64_t need = sizeof(int) * (static_cast<int64_t>(a.groups) * a.chunks + a.groups);
+  if (!ws || bytes < need) return false;
+  a.counts = static_cast<int*>(ws);
+  a.totals = a.counts + static_cast<int64_t>(a.groups) * a.chunks;
+  return true;
+}
+bool one_cta(int64_t units, int64_t entries) { return units <= kOneRows && entries <= kOneEntries; }
+
+// offsets[0 .. groups] = 0 where there are no rows
+cudaError_t no_entries(int* offsets, int groups, cudaStream_t s) {
+  return cudaMemsetAsync(offsets, 0, sizeof(int) * (groups + 1), s);
+}
+
+}  // namespace
+}  // namespace ha
+
+using namespace ha;
+
+extern "C" int hier_avg_sort_workspace(int64_t rows, int per_row, int groups, int64_t* bytes) {
+  if (!bytes || rows < 0 || per_row < 1 || groups < 1) return HA_EINVAL;
+  if (groups > kMaxGroups || per_row > kMaxChosen || rows > 0x7FFFFFFF / per_row) return HA_EUNSUPPORTED;
+  *bytes = one_cta(rows, rows * per_row) ? 0 : sizeof(int) * workspace_ints(rows * per_row, per_row, groups);
+  return HA_OK;
+}
+
+extern "C" int hier_avg_route(const void* logits_dev, int type, int64_t rows, int experts, int64_t ld, int k,
+                              int over_all, const int32_t* learners_dev, int learners, int32_t* expert_dev,
+                              float* weight_dev, float* lse_dev, int32_t* offsets_dev, int32_t* place_dev,
+                              int32_t* source_dev, void* workspace_dev, int64_t workspace_bytes, void* stream) {
+  if (!type_ok(type) || rows < 0 || experts < 1 || ld < experts || k < 1 || k > experts || workspace_bytes < 0 ||
+      (learners_dev ? learners < 1 : learners != 0) || misaligned(logits_dev, type_size(type)) ||
+      misaligned(workspace_dev, 4) || !offsets_dev)
+    return HA_EINVAL;
+  if (k > kMaxChosen || experts > kMaxExperts ||
+      static_cast<int64_t>(experts) * std::max(learners, 1) > kMaxGroups || rows > 0x7FFFFFFF / k)
+    return HA_EUNSUPPORTED;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int groups = experts * std::max(learners, 1);
+  if (rows == 0) return no_entries(offsets_dev, groups, s) == cudaSuccess ? HA_OK : HA_ECUDA;
+  if (!logits_dev || !expert_dev || !weight_dev || !lse_dev || !place_dev || !source_dev) return HA_EINVAL;
+  RouteArgs a = {logits_dev, rows, ld, learners_dev, learners, experts, k, over_all != 0, expert_dev, weight_dev, lse_dev,
+                 {offsets_dev, place_dev, source_dev, nullptr, nullptr, rows * k, 0, groups, 0}};
+  const bool one = one_cta(rows, rows * k);
+  if (!plan_sort(a.sort, k, one, workspace_dev, workspace_bytes)) return HA_ENOMEM;
+  const cudaError_t e = type == HA_TYPE_FP32   ? route_type<float>(a, one, s)
+                        : type == HA_TYPE_BF16 ? route_type<__nv_bfloat16>(a, one, s)
+                                               : route_type<__half>(a, one, s);
+  return e == cudaSuccess ? HA_OK : HA_ECUDA;
+}
+
+extern "C" int hier_avg_sort_by_group(const int32_t* group_dev, int64_t rows, int per_row, int groups,
+                                      int32_t* offsets_dev, int32_t* place_dev, int32_t* source_dev,
+                                      void* workspace_dev, int64_t workspace_bytes, void* stream) {
+  if (rows < 0 || per_row < 1 || groups < 1 || workspace_bytes < 0 || misaligned(workspace_dev, 4) || !offsets_dev)
+    return HA_EINVAL;
+  if (groups > kMaxGroups || per_row > kMaxChosen || rows > 0x7FFFFFFF / per_row) return HA_EUNSUPPORTED;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (rows == 0) return no_entries(offsets_dev, groups, s) == cudaSuccess ? HA_OK : HA_ECUDA;
+  if (!group_dev || !place_dev || !source_dev) return HA_EINVAL;
+  SortArgs a = {offsets_dev, place_dev, source_dev, nullptr, nullptr, rows * per_row, 0, groups, 0};
+  const bool one = one_cta(rows, rows * per_row);
+  if (!plan_sort(a, per_row, one, workspace_dev, workspace_bytes)) return HA_ENOMEM;
+  const int warps = one ? static_cast<int>(std::min<int64_t>((a.entries + 31) / 32, kOneWarps)) : kWarps;
+  static bool one_ok[kMaxDevices], ok[kMaxDevices];
+  const auto kernel = one ? k_group<true> : k_group<false>;
+  cudaError_t e = allow_smem(kernel, 200 << 10, one ? one_ok : ok);
+  if (e == cudaSuccess) {
+    kernel<<<static_cast<unsigned>(a.chunks), warps * 32, sort_smem(warps, groups, a.per), s>>>(group_dev, a);
+    e = cudaGetLastError();
+  }
+  if (e == cudaSuccess && !one) e = end_sort(a, s);
+  return e == cudaSuccess ? HA_OK : HA_ECUDA;
+}
+
+extern "C" int hier_avg_route_backward(const float* dweight_dev, const void* logits_dev, int type, int64_t rows,
+                                       int experts, int64_t ld, int k, int over_all, const int32_t* expert_dev,
+                                       const float* weight_dev, const float* lse_dev, void* dlogits_dev,
+                                       int64_t dlogits_ld, void* stream) {
+  if (!type_ok(type) || rows < 0 || experts < 1 || k < 1 || k > experts || dlogits_ld < experts ||
+      misaligned(dlogits_dev, type_size(type)))
+    return HA_EINVAL;
+  if (over_all && (ld < experts || misaligned(logits_dev, type_size(type)))) return HA_EINVAL;
+  if (k > kMaxChosen || experts > kMaxExperts || rows > 0x7FFFFFFF / k) return HA_EUNSUPPORTED;
+  if (rows == 0) return HA_OK;
+  if (!dweight_dev || !expert_dev || !weight_dev || !dlogits_dev || (over_all && (!logits_dev || !lse_dev))) return HA_EINVAL;
+  RouteBwdArgs a = {logits_dev, dweight_dev, weight_dev, lse_dev, expert_dev, dlogits_dev, rows, ld, dlogits_ld,
+                    experts, k, over_all != 0};
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = type == HA_TYPE_FP32   ? backward_type<float>(a, s)
+                        : type == HA_TYPE_BF16 ? backward_type<__nv_bfloat16>(a, s)
+                                               : backward_type<__half>(a, s);
+  return e == cudaSuccess ? HA_OK : HA_ECUDA;
+}

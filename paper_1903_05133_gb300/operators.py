@@ -1,11 +1,12 @@
-"""Operators for models with grouped weights: products by group with their gradients, log
-probabilities of given classes with their gradient, and AdamW over many tensors.
+"""Operators for models with grouped weights: products by group with their gradients, the router that
+makes the groups and the rows' way there and back with theirs, log probabilities of given classes with
+their gradient, drafted tokens verified, the norm of all gradients, and AdamW over many tensors.
 
 Argument marshalling only, as in hier_avg.py: PyTorch provides the memory and the stream, the
 computation runs in the library's CUDA kernels, and the functions are those of
 include/hier_avg.h without the ``hier_avg_`` prefix.  Results are new tensors unless ``out``
 is given, and outside autograd: a result has no history even where an input requires gradients, whose
-calls are grouped_product_dx, grouped_product_dw and token_logprobs_backward.  All tensors of a
+calls are grouped_product_dx, grouped_product_dw and the functions that end in _backward.  All tensors of a
 call are on one GPU, where it runs whichever is current.  A call on ``stream`` makes its results and
 workspace there; its inputs are the caller's to keep until it is done.
 """
@@ -26,6 +27,7 @@ TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 FORWARD, DX, DW = 0, 1, 2
 _KIND = attrgetter("dtype", "shape")
 _ADDRESS, _CONTIGUOUS, _DEVICE = torch.Tensor.data_ptr, torch.Tensor.is_contiguous, torch.Tensor.get_device
+_DTYPE, _NUMEL = attrgetter("dtype"), torch.Tensor.numel
 BLOCK = 256                     # elements that share a scale of the 8-bit AdamW states
 MAX_TOP = 32
 
@@ -352,6 +354,328 @@ def token_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, lse: to
             None if dentropy is None else dentropy.data_ptr(), d.data_ptr(),
             V if out is None else _ld(d), s), "token_logprobs_backward")
     return d
+
+
+# ---------------------------------------------------------------------- routing
+class Routing(NamedTuple):
+    experts: torch.Tensor                     # [rows, k] int32, -1 where there is none
+    weights: torch.Tensor                     # [rows, k]
+    lse: torch.Tensor                         # [rows] log of the sum of the exponentials
+    offsets: torch.Tensor                     # [groups + 1] int32, as the grouped products read them
+    place: torch.Tensor                       # [rows, k] int32, each entry's among the sorted, -1: none
+    source: torch.Tensor                      # [rows * k] int32, the entry at each place, -1 behind the last
+
+
+class Sorted(NamedTuple):
+    offsets: torch.Tensor
+    place: torch.Tensor
+    source: torch.Tensor
+
+
+MAX_CHOSEN, MAX_GROUPS = 32, 1024
+_ONE_ROWS, _ONE_ENTRIES = 256, 2048
+
+
+def _vector(name, t, dtype, shape):
+    if not (t.is_cuda and t.dtype == dtype and tuple(t.shape) == shape and t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor {list(shape)}")
+
+
+def _sort_workspace(lib, rows, k, groups, device):
+    if rows <= _ONE_ROWS and rows * k <= _ONE_ENTRIES:      # one CTA sorts them: none, as the library says
+        return None, None, 0
+    n = c_int64()
+    check(lib.hier_avg_sort_workspace(rows, k, groups, ctypes.byref(n)), "sort_workspace")
+    ws = torch.empty(n.value, dtype=torch.uint8, device=device)
+    return ws, ws.data_ptr(), n.value
+
+
+def _over(over):
+    _need(over in ("chosen", "all"), "over must be 'chosen' or 'all'")
+    return over == "all"
+
+
+def route(logits: torch.Tensor, k: int, over: str = "chosen", learners: Optional[torch.Tensor] = None,
+          stream=None) -> Routing:
+    """The k experts of largest logits for each row (equal logits by index), their weights, and the entries
+    sorted by expert for dispatch, the grouped products and combine.
+
+    logits [rows, experts] fp32, bf16 or fp16, at or below -1e30 where masked; the weights are softmax over the
+    ``chosen`` or over ``all`` experts.  learners [learners + 1] int32 on the device, rising: the rows of
+    each learner, which has experts of its own (group = learner * experts + expert)."""
+    lib = _lib.load()
+    ld = _rows_of("logits", logits, TYPES)
+    T, E = logits.shape
+    _need(1 <= k <= min(E, MAX_CHOSEN), f"k must be in [1, {min(E, MAX_CHOSEN)}]")
+    P = 0 if learners is None else _offsets(learners, None)
+    G = E * max(P, 1)
+    _need(G <= MAX_GROUPS, f"there must be at most {MAX_GROUPS} groups")
+    every = _over(over)
+    s, where = _on(stream, logits, learners)
+    with where:
+        dev = logits.device
+        experts = torch.empty((T, k), dtype=torch.int32, device=dev)
+        weights = torch.empty((T, k), dtype=torch.float32, device=dev)
+        lse = torch.empty(T, dtype=torch.float32, device=dev)
+        offsets = torch.empty(G + 1, dtype=torch.int32, device=dev)
+        place = torch.empty((T, k), dtype=torch.int32, device=dev)
+        source = torch.empty(T * k, dtype=torch.int32, device=dev)
+        ws, p, n = _sort_workspace(lib, T, k, G, dev)
+        check(lib.hier_avg_route(
+            logits.data_ptr(), TYPES[logits.dtype], T, E, ld, k, every, None if learners is None else learners.data_ptr(), P,
+            experts.data_ptr(), weights.data_ptr(), lse.data_ptr(), offsets.data_ptr(), place.data_ptr(),
+            source.data_ptr(), p, n, s), "route")
+    return Routing(experts, weights, lse, offsets, place, source)
+
+
+def route_backward(dweights: torch.Tensor, logits: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor,
+                   lse: Optional[torch.Tensor] = None, over: str = "chosen", out: Optional[torch.Tensor] = None,
+                   stream=None) -> torch.Tensor:
+    """The gradient of sum(dweights * weights) with respect to the logits, in their type, from route's experts and
+    weights (and lse for over="all"); ``out`` may be ``logits`` itself."""
+    lib = _lib.load()
+    ld = _rows_of("logits", logits, TYPES)
+    T, E = logits.shape
+    every = _over(over)
+    _need(experts.dim() == 2, "experts must be [rows, k]")
+    k = experts.shape[1]
+    _need(1 <= k <= min(E, MAX_CHOSEN), f"k must be in [1, {min(E, MAX_CHOSEN)}]")
+    _vector("experts", experts, torch.int32, (T, k))
+    _vector("weights", weights, torch.float32, (T, k))
+    _vector("dweights", dweights, torch.float32, (T, k))
+    _need(lse is not None or not every, "over='all' needs lse")
+    if lse is not None:
+        _vector("lse", lse, torch.float32, (T,))
+    _apart(out, dweights, logits, experts, weights, lse, same=logits)
+    s, where = _on(stream, logits, dweights, experts, weights, lse, out)
+    with where:
+        d = torch.empty((T, E), dtype=logits.dtype, device=logits.device) if out is None else \
+            _given(out, (T, E), logits.dtype)
+        check(lib.hier_avg_route_backward(
+            dweights.data_ptr(), logits.data_ptr(), TYPES[logits.dtype], T, E, ld, k, every, experts.data_ptr(),
+            weights.data_ptr(), None if lse is None else lse.data_ptr(), d.data_ptr(), E if out is None else _ld(d), s),
+            "route_backward")
+    return d
+
+
+def sort_by_group(group: torch.Tensor, groups: int, stream=None) -> Sorted:
+    """The sort of route for given groups [rows, k] int32 (a router of the caller's own, or route's experts
+    after some were dropped); below 0 or from ``groups`` on: none."""
+    lib = _lib.load()
+    _need(group.dim() == 2, "group must be [rows, k]")
+    T, k = group.shape
+    _vector("group", group, torch.int32, (T, k))
+    _need(1 <= k <= MAX_CHOSEN, f"k must be in [1, {MAX_CHOSEN}]")
+    _need(1 <= groups <= MAX_GROUPS, f"groups must be in [1, {MAX_GROUPS}]")
+    s, where = _on(stream, group)
+    with where:
+        dev = group.device
+        offsets = torch.empty(groups + 1, dtype=torch.int32, device=dev)
+        place = torch.empty((T, k), dtype=torch.int32, device=dev)
+        source = torch.empty(T * k, dtype=torch.int32, device=dev)
+        ws, p, n = _sort_workspace(lib, T, k, groups, dev)
+        check(lib.hier_avg_sort_by_group(group.data_ptr(), T, k, groups, offsets.data_ptr(), place.data_ptr(),
+                                         source.data_ptr(), p, n, s), "sort_by_group")
+    return Sorted(offsets, place, source)
+
+
+# ---------------------------------------------------------------------- rows to their groups and back
+def _places(place, entries=None):
+    if not (place.is_cuda and place.dtype == torch.int32 and place.dim() == 2 and place.is_contiguous()):
+        raise ValueError("place must be a contiguous CUDA int32 matrix [rows, k]")
+    T, k = place.shape
+    _need(k >= 1, "place must have columns")
+    _need(entries is None or entries == T * k, "the sorted rows must be as many as place has entries")
+    return T, k
+
+
+def dispatch(x: torch.Tensor, place: torch.Tensor, offsets: torch.Tensor, out: Optional[torch.Tensor] = None,
+             stream=None) -> torch.Tensor:
+    """xs[place[t, j]] = x[t], [rows * k, width]; the rows behind the last group, offsets[-1], are zero.
+
+    x [rows, width] fp32, bf16 or fp16; place [rows, k] and offsets as of route or sort_by_group."""
+    lib = _lib.load()
+    T, k = _places(place)
+    ld = _rows_of("x", x, TYPES, T)
+    G, D = _offsets(offsets, None), x.shape[1]
+    _apart(out, x, place, offsets)
+    s, where = _on(stream, x, place, offsets, out)
+    with where:
+        xs = torch.empty((T * k, D), dtype=x.dtype, device=x.device) if out is None else _given(out, (T * k, D), x.dtype)
+        check(lib.hier_avg_dispatch(x.data_ptr(), TYPES[x.dtype], T, D, ld, place.data_ptr(), k, offsets.data_ptr(), G,
+                                    xs.data_ptr(), D if out is None else _ld(xs), s), "dispatch")
+    return xs
+
+
+def _combine(name, y, place, weights, out, out_dtype, stream):
+    lib = _lib.load()
+    T, k = _places(place)
+    ld = _rows_of(name, y, TYPES, T * k)
+    D = y.shape[1]
+    if weights is not None:
+        _vector("weights", weights, torch.float32, (T, k))
+    d = _out_type(out_dtype, out, y.dtype)
+    _apart(out, y, place, weights)
+    s, where = _on(stream, y, place, weights, out)
+    with where:
+        o = torch.empty((T, D), dtype=d, device=y.device) if out is None else _given(out, (T, D), d)
+        check(lib.hier_avg_combine(y.data_ptr(), TYPES[y.dtype], T, D, ld, place.data_ptr(), k,
+                                   None if weights is None else weights.data_ptr(), o.data_ptr(),
+                                   D if out is None else _ld(o), TYPES[d], s), "combine")
+    return o
+
+
+def dispatch_backward(dxs: torch.Tensor, place: torch.Tensor, out: Optional[torch.Tensor] = None,
+                      out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
+    """dx[t] = sum over j of dxs[place[t, j]], in dxs's type or fp32."""
+    return _combine("dxs", dxs, place, None, out, out_dtype, stream)
+
+
+def combine(y: torch.Tensor, place: torch.Tensor, weights: torch.Tensor, out: Optional[torch.Tensor] = None,
+            out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
+    """out[t] = sum over j of weights[t, j] y[place[t, j]], in y's type or fp32.
+
+    y [rows * k, width] fp32, bf16 or fp16, the sorted rows' results; place and weights [rows, k] as of route."""
+    return _combine("y", y, place, weights, out, out_dtype, stream)
+
+
+def combine_backward(dout: torch.Tensor, y: torch.Tensor, place: torch.Tensor, weights: torch.Tensor, offsets: torch.Tensor,
+                     out: Optional[torch.Tensor] = None, stream=None):
+    """(dy, dweights): dy[place[t, j]] = weights[t, j] dout[t] in y's type, zero behind the last group (``out`` is for
+    dy), and dweights[t, j] = <dout[t], y[place[t, j]]>.  dout is of y's type or fp32."""
+    lib = _lib.load()
+    T, k = _places(place)
+    ld = _rows_of("y", y, TYPES, T * k)
+    D, kind = y.shape[1], y.dtype
+    dout_ld = _rows_of("dout", dout, (kind, torch.float32), T, D)
+    _vector("weights", weights, torch.float32, (T, k))
+    G = _offsets(offsets, None)
+    _apart(out, dout, y, place, weights, offsets)
+    s, where = _on(stream, y, dout, place, weights, offsets, out)
+    with where:
+        dy = torch.empty((T * k, D), dtype=kind, device=y.device) if out is None else _given(out, (T * k, D), kind)
+        dw = torch.empty((T, k), dtype=torch.float32, device=y.device)
+        check(lib.hier_avg_combine_backward(
+            dout.data_ptr(), TYPES[dout.dtype], dout_ld, y.data_ptr(), TYPES[kind], T, D, ld, place.data_ptr(), k,
+            weights.data_ptr(), offsets.data_ptr(), G, dy.data_ptr(), D if out is None else _ld(dy), dw.data_ptr(), s),
+            "combine_backward")
+    return dy, dw
+
+
+# ---------------------------------------------------------------------- drafted tokens
+class VerifiedDrafts(NamedTuple):
+    tokens: torch.Tensor                      # [sequences, drafts + 1] int32: the accepted, the next, then -1
+    accepted: torch.Tensor                    # [sequences] int32
+    logp: torch.Tensor                        # [sequences, drafts + 1] of the tokens, 0 where there is none
+
+
+def _three(name, t, dtypes, shape):
+    """The strides of the first two dimensions of a CUDA tensor of unit stride in the last."""
+    if not (t.is_cuda and t.dtype in dtypes and tuple(t.shape) == shape and (t.stride(-1) == 1 or shape[-1] == 1)):
+        raise ValueError(f"{name} must be a CUDA tensor {list(shape)} of {' or '.join(str(d) for d in dtypes)} with unit stride "
+                         "in its last dimension")
+    return t.stride()[:-1]
+
+
+def verify_drafts(logits: torch.Tensor, drafts: torch.Tensor, uniform: torch.Tensor, noise: torch.Tensor,
+                  draft_probs: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                  allowed: Optional[torch.Tensor] = None, stream=None) -> VerifiedDrafts:
+    """Which drafted tokens the target accepts, and the token that follows them.
+
+    logits [sequences, K + 1, classes] fp32, bf16 or fp16 of the target, after the drafts before each row; drafts
+    [sequences, K] int32 or int64, below 0 where there is none; draft_probs [sequences, K, classes] that they were drawn
+    from (None: they are certain).  Draft i is accepted while uniform[i] * draft_probs[i, draft] < p[i, draft], p =
+    softmax(logits / temperature) over the allowed classes; the next token is the first argmax of r / noise, r = p
+    less draft_probs where positive after a rejection, else p.  uniform [sequences, K] in [0, 1), noise [sequences,
+    classes] positive, exponential for a draw from r, both fp32.  K may be 0: one token is then drawn from p.
+    allowed: a mask [classes] or [sequences, K + 1, classes], which may be expanded."""
+    lib = _lib.load()
+    _need(logits.dim() == 3 and logits.shape[1] >= 1 and logits.shape[2] >= 1, "logits must be [sequences, drafts + 1, classes]")
+    B, R, V = logits.shape
+    K = R - 1
+    z = _three("logits", logits, tuple(TYPES), (B, R, V))
+    if not (drafts.is_cuda and drafts.dtype in (torch.int32, torch.int64) and tuple(drafts.shape) == (B, K) and
+            drafts.is_contiguous()):
+        raise ValueError(f"drafts must be a contiguous CUDA int32 or int64 tensor {[B, K]}")
+    _vector("uniform", uniform, torch.float32, (B, K))
+    noise_ld, = _three("noise", noise, (torch.float32,), (B, V))
+    q = (0, 0) if draft_probs is None else _three("draft_probs", draft_probs, tuple(TYPES), (B, K, V))
+    _need(2.0 ** -126 <= temperature <= 1e27, "temperature must be in [2^-126, 1e27]")
+    ok = (0, 0)
+    if allowed is not None and allowed.dim() == 1:
+        _three("allowed", allowed, (torch.bool, torch.uint8), (V,))
+    elif allowed is not None:
+        ok = _three("allowed", allowed, (torch.bool, torch.uint8), (B, R, V))
+    s, where = _on(stream, logits, drafts, uniform, noise, draft_probs, allowed)
+    with where:
+        dev = logits.device
+        tokens = torch.empty((B, R), dtype=torch.int32, device=dev)
+        accepted = torch.empty(B, dtype=torch.int32, device=dev)
+        logp = torch.empty((B, R), dtype=torch.float32, device=dev)
+        n = 16 * B * R                                      # as hier_avg_verify_workspace says
+        ws = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
+        check(lib.hier_avg_verify_drafts(
+            logits.data_ptr(), TYPES[logits.dtype], B, K, V, *z, drafts.data_ptr(), drafts.element_size(), uniform.data_ptr(),
+            noise.data_ptr(), noise_ld, None if draft_probs is None else draft_probs.data_ptr(),
+            0 if draft_probs is None else TYPES[draft_probs.dtype], *q, None if allowed is None else allowed.data_ptr(), *ok,
+            temperature, tokens.data_ptr(), accepted.data_ptr(), logp.data_ptr(), ws.data_ptr(), n, s), "verify_drafts")
+    return VerifiedDrafts(tokens, accepted, logp)
+
+
+# ---------------------------------------------------------------------- the norm of all gradients
+class GradNorm(NamedTuple):
+    norm: torch.Tensor                        # [1], or [learners]
+    scale: Optional[torch.Tensor]             # max_norm / norm where that is below 1, else 1; as AdamW.step takes it
+
+
+def _norm(grads, max_norm, learners, clip, stream):
+    lib = _lib.load()
+    # each check runs over all tensors at once: a call over hundreds of them is host work
+    n = len(grads)
+    _need(n >= 1, "grads must not be empty")
+    kinds = list(map(_DTYPE, grads))
+    devices = set(map(_DEVICE, grads))
+    if not (set(kinds) <= TYPES.keys() and min(devices) >= 0 and all(map(_CONTIGUOUS, grads))):
+        raise ValueError("grads must be contiguous CUDA tensors of fp32, bf16 or fp16")
+    _need(len(devices) == 1, "all tensors of a call must be on one GPU")
+    P = 1
+    if learners is not None:
+        P = learners
+        _need(P >= 1 and all(g.dim() >= 1 and g.shape[0] == P for g in grads), "the gradients' first dimension must be the learners'")
+    _need(max_norm is None or 0 <= max_norm < float("inf"), "max_norm must be finite and not negative")
+    address = array("Q", map(_ADDRESS, grads))
+    types = array("i", map(TYPES.__getitem__, kinds))
+    sizes = array("q", map(_NUMEL, grads))
+    t, z = types.buffer_info()[0], sizes.buffer_info()[0]
+    s, where = _on(stream, grads[0])
+    with where:
+        dev = grads[0].device
+        norm = torch.empty(P, dtype=torch.float32, device=dev)
+        scale = None if max_norm is None else torch.empty(P, dtype=torch.float32, device=dev)
+        b = c_int64()
+        check(lib.hier_avg_grad_norm_workspace(n, t, z, P, ctypes.byref(b)), "grad_norm_workspace")
+        ws = torch.empty(b.value, dtype=torch.uint8, device=dev)
+        status = lib.hier_avg_grad_norm(n, address.buffer_info()[0], t, z, P, 0.0 if max_norm is None else max_norm, clip,
+                                        norm.data_ptr(), None if scale is None else scale.data_ptr(), ws.data_ptr(), b.value, s)
+        _need(not (clip and status == -1), "gradients that are clipped must not share memory")
+        check(status, "clip_gradients" if clip else "grad_norm")
+    return GradNorm(norm, scale)
+
+
+def grad_norm(grads: Sequence[torch.Tensor], max_norm: Optional[float] = None, learners: Optional[int] = None,
+              stream=None) -> GradNorm:
+    """The norm of all gradients together and, with max_norm, the factor that clips them to it, on the device.
+
+    grads: contiguous fp32, bf16 or fp16 tensors, of types of their own; learners: their first dimension is the learner's,
+    and each has a norm and a factor.  A norm that is NaN has factor 1, an infinite one 0."""
+    return _norm(grads, max_norm, learners, False, stream)
+
+
+def clip_gradients(grads: Sequence[torch.Tensor], max_norm: float, learners: Optional[int] = None, stream=None) -> GradNorm:
+    """grad_norm, and the gradients multiplied by their factor in place (where it is not 1).  They must not
+    share memory.  AdamW.step(grads, lr, grad_scale=grad_norm(grads, max_norm).scale) does the same without this pass."""
+    _need(max_norm is not None, "max_norm must be given")
+    return _norm(grads, max_norm, learners, True, stream)
 
 
 # ---------------------------------------------------------------------- AdamW
