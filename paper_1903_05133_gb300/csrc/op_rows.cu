@@ -8,8 +8,10 @@
 //
 // All are bound by the bytes of the sorted rows.  The work goes by tokens: what belongs to a token is
 // read once, and its entries' rows, which nobody else has, by 16 bytes a thread with as many loads in
-// flight as a token has entries.  Sums are in fp32, in the order of j.
+// flight as a token has entries.  Sums are in fp32, in the order of j.  8192 tokens of 4 entries of 4096 bf16:
+// dispatch 51.3 us, combine 57.5 (336 MB: 6.5 and 5.8 TB/s, the copy's rate is 6.75), its gradient 90.0 (604 MB, 6.7).
 #include <algorithm>
+#include <type_traits>
 
 #include "op_common.cuh"
 
@@ -17,7 +19,9 @@ namespace ha {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kAtOnce = 8;                // entries of a token whose loads are in flight together
+// Parts of a row that a thread has in flight at a time, for 16-byte parts and for single elements.  8192 tokens of 4 entries of
+// 4096 bf16: combine takes 57.6 us with 2 parts (four CTAs an SM; 76 with five, whose registers spill), 60.5 with one.
+constexpr int kWide = 2, kSingle = 8;
 
 struct RowArgs {
   const void* token;                      // x or dout
@@ -30,31 +34,54 @@ struct RowArgs {
   float* dweight;
   int64_t tokens, entries, token_ld, sorted_ld, out_token_ld, out_sorted_ld;
   int k, width;
-  int lanes;                              // threads of an item
-  int slices;                             // items of a token
+  int lanes;                              // threads of a token
 };
 
-// V elements at once, or one where rows are not aligned.
+// V elements of a row as they are held in memory: 16 bytes, or fp32 beside a 16-bit type's eight, or one
+// element where rows are not aligned.  Rows are widened when they are added, so that the loads in flight take
+// no more registers than their bytes.
 template <typename T, int V> struct Part {
-  float v[V];
+  static constexpr int kWords = V == 1 ? 1 : V / kVec<T>;
+  uint4 w[kWords];
+  T one;
   __device__ __forceinline__ void load(const T* p) {
     if constexpr (V == 1) {
-      v[0] = Elem<T>::up(*p);
-    } else if constexpr (V == kVec<T>) {
-      unpack<T>(*reinterpret_cast<const uint4*>(p), v);
-    } else {                              // fp32 beside a 16-bit type's eight
-      unpack<T>(reinterpret_cast<const uint4*>(p)[0], v);
-      unpack<T>(reinterpret_cast<const uint4*>(p)[1], v + 4);
+      one = *p;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
+    }
+  }
+  __device__ __forceinline__ void clear() {
+    if constexpr (V == 1) {
+      one = Elem<T>::down(0.0f);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = make_uint4(0, 0, 0, 0);
     }
   }
   __device__ __forceinline__ void store(T* p) const {
     if constexpr (V == 1) {
-      *p = Elem<T>::down(v[0]);
-    } else if constexpr (V == kVec<T>) {
-      *reinterpret_cast<uint4*>(p) = pack<T>(v);
+      *p = one;
     } else {
-      reinterpret_cast<uint4*>(p)[0] = pack<T>(v);
-      reinterpret_cast<uint4*>(p)[1] = pack<T>(v + 4);
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) reinterpret_cast<uint4*>(p)[i] = w[i];
+    }
+  }
+  __device__ __forceinline__ void up(float* v) const {
+    if constexpr (V == 1) {
+      v[0] = Elem<T>::up(one);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) unpack<T>(w[i], v + i * kVec<T>);
+    }
+  }
+  __device__ __forceinline__ void down(const float* v) {
+    if constexpr (V == 1) {
+      one = Elem<T>::down(v[0]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = pack<T>(v + i * kVec<T>);
     }
   }
 };
@@ -65,162 +92,204 @@ __device__ __forceinline__ int64_t place_of(const RowArgs& a, int64_t entry) {
   return p >= 0 && p < a.entries ? p : -1;
 }
 
-// The item's columns: part i of each row for i in [lane, parts) by steps, of a token's slice.
+// A thread's token and its first part of the rows; the next is a.lanes parts on.
 struct Item {
   int64_t token;
-  int first, step, parts;
+  int first;
 };
-template <int V>
 __device__ __forceinline__ Item item_of(const RowArgs& a) {
-  const int64_t item = blockIdx.x * static_cast<int64_t>(kThreads / a.lanes) + threadIdx.x / a.lanes;
-  const int parts = (a.width + V - 1) / V;
-  return {item / a.slices, static_cast<int>(item % a.slices) * a.lanes + static_cast<int>(threadIdx.x) % a.lanes,
-          a.slices * a.lanes, parts};
-}
-
-// A row's last part may be short: its elements are then taken one by one.
-template <int V, typename F, typename G>
-__device__ __forceinline__ void each_part(const Item& it, int width, F whole, G single) {
-  for (int i = it.first; i < it.parts; i += it.step) {
-    const int c = i * V;
-    if (c + V <= width) whole(c);
-    else
-      for (int e = c; e < width; ++e) single(e);
+  const int64_t at = blockIdx.x * static_cast<int64_t>(kThreads);
+  if (a.tokens * a.lanes <= 0x7FFFFFFF - kThreads) {        // a division of 32 bits
+    const int i = static_cast<int>(at) + static_cast<int>(threadIdx.x);
+    return {i / a.lanes, i % a.lanes};
   }
+  const int64_t i = at + threadIdx.x;
+  return {i / a.lanes, static_cast<int>(i % a.lanes)};
 }
 
-template <typename T, int V>
-__device__ __forceinline__ void dispatch_at(const RowArgs& a, int64_t token, int c) {
-  Part<T, V> x, none;
+// f(first column of the parts, number of them), U parts at a time; a row's last elements, which fill no
+// part, go to g one by one.
+template <int V, int U, typename F, typename G>
+__device__ __forceinline__ void each_part(int first, int lanes, int width, F f, G g) {
+  const int parts = width / V;
+  for (int i = first; i < parts; i += lanes * U) f(i);
+  if constexpr (V > 1)
+    for (int c = parts * V + first; c < width; c += lanes) g(c);
+}
+
+template <typename T, int V, int U>
+__device__ __forceinline__ void dispatch_at(const RowArgs& a, int64_t token, int i, int parts) {
+  Part<T, V> x[U], none;
+  const T* from = static_cast<const T*>(a.token) + token * a.token_ld;
 #pragma unroll
-  for (int e = 0; e < V; ++e) none.v[e] = 0.0f;
-  x.load(static_cast<const T*>(a.token) + token * a.token_ld + c);
-  T* out = static_cast<T*>(a.out_sorted) + c;
+  for (int u = 0; u < U; ++u)
+    if (i + u * a.lanes < parts) x[u].load(from + (i + u * a.lanes) * V);
+  none.clear();
   const int64_t count = *a.count;
   for (int j = 0; j < a.k; ++j) {
     const int64_t e = token * a.k + j, p = place_of(a, e);
-    if (p >= 0) x.store(out + p * a.out_sorted_ld);
-    if (e >= count) none.store(out + e * a.out_sorted_ld);
+    T* out = static_cast<T*>(a.out_sorted);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = (i + u * a.lanes) * V;
+      if (i + u * a.lanes >= parts) break;
+      if (p >= 0) x[u].store(out + p * a.out_sorted_ld + c);
+      if (e >= count) none.store(out + e * a.out_sorted_ld + c);
+    }
   }
 }
-template <typename T, int V>
+template <typename T, int V, int U>
 __global__ void __launch_bounds__(kThreads) k_dispatch(const __grid_constant__ RowArgs a) {
-  const Item it = item_of<V>(a);
+  const Item it = item_of(a);
   if (it.token >= a.tokens) return;
-  each_part<V>(it, a.width, [&](int c) { dispatch_at<T, V>(a, it.token, c); },
-               [&](int c) { dispatch_at<T, 1>(a, it.token, c); });
+  each_part<V, U>(it.first, a.lanes, a.width, [&](int i) { dispatch_at<T, V, U>(a, it.token, i, a.width / V); },
+                  [&](int c) { dispatch_at<T, 1, 1>(a, it.token, c, a.width); });
 }
 
-// out[t] = sum of w y; without weights their sum.
-template <typename T, typename O, int V, bool WEIGHTS>
-__device__ __forceinline__ void combine_at(const RowArgs& a, int64_t token, int c) {
-  const T* rows = static_cast<const T*>(a.sorted) + c;
-  Part<O, V> sum;
+// out[t] = sum of w y; without weights their sum.  AT entries' loads of U parts are in flight together.
+template <typename T, typename O, int V, int U, int AT, bool WEIGHTS>
+__device__ __forceinline__ void combine_at(const RowArgs& a, int64_t token, int i, int parts) {
+  float sum[U][V];
 #pragma unroll
-  for (int e = 0; e < V; ++e) sum.v[e] = 0.0f;
-  for (int j0 = 0; j0 < a.k; j0 += kAtOnce) {
-    Part<T, V> y[kAtOnce];
-    float w[kAtOnce];
-    bool has[kAtOnce];
+  for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
-      const int64_t p = j0 + u < a.k ? place_of(a, token * a.k + j0 + u) : -1;
-      has[u] = p >= 0;
-      if (has[u]) {
-        y[u].load(rows + p * a.sorted_ld);
-        w[u] = WEIGHTS ? a.weight[token * a.k + j0 + u] : 1.0f;
+    for (int e = 0; e < V; ++e) sum[u][e] = 0.0f;
+  for (int j0 = 0; j0 < a.k; j0 += AT) {
+    Part<T, V> y[AT][U];
+    float w[AT];
+#pragma unroll
+    for (int q = 0; q < AT; ++q) {
+      const int64_t p = j0 + q < a.k ? place_of(a, token * a.k + j0 + q) : -1;
+      w[q] = WEIGHTS && p >= 0 ? a.weight[token * a.k + j0 + q] : 0.0f;
+      const T* row = static_cast<const T*>(a.sorted) + p * a.sorted_ld;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (p >= 0 && i + u * a.lanes < parts) y[q][u].load(row + (i + u * a.lanes) * V);
+        else y[q][u].clear();
       }
     }
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u)
-      if (has[u]) {
+    for (int q = 0; q < AT; ++q)
 #pragma unroll
-        for (int e = 0; e < V; ++e) sum.v[e] = WEIGHTS ? fmaf(w[u], y[u].v[e], sum.v[e]) : sum.v[e] + y[u].v[e];
+      for (int u = 0; u < U; ++u) {
+        float v[V];
+        y[q][u].up(v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum[u][e] = WEIGHTS ? fmaf(w[q], v[e], sum[u][e]) : sum[u][e] + v[e];
       }
   }
-  sum.store(static_cast<O*>(a.out_token) + token * a.out_token_ld + c);
+  O* out = static_cast<O*>(a.out_token) + token * a.out_token_ld;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (i + u * a.lanes < parts) {
+      Part<O, V> o;
+      o.down(sum[u]);
+      o.store(out + (i + u * a.lanes) * V);
+    }
 }
-template <typename T, typename O, int V, bool WEIGHTS>
-__global__ void __launch_bounds__(kThreads) k_combine(const __grid_constant__ RowArgs a) {
-  const Item it = item_of<V>(a);
+template <typename T, typename O, int V, int U, int AT, bool WEIGHTS>
+__global__ void __launch_bounds__(kThreads, 4) k_combine(const __grid_constant__ RowArgs a) {
+  const Item it = item_of(a);
   if (it.token >= a.tokens) return;
-  each_part<V>(it, a.width, [&](int c) { combine_at<T, O, V, WEIGHTS>(a, it.token, c); },
-               [&](int c) { combine_at<T, O, 1, WEIGHTS>(a, it.token, c); });
+  each_part<V, U>(it.first, a.lanes, a.width, [&](int i) { combine_at<T, O, V, U, AT, WEIGHTS>(a, it.token, i, a.width / V); },
+                  [&](int c) { combine_at<T, O, 1, 1, AT, WEIGHTS>(a, it.token, c, a.width); });
 }
 
 // A CTA a token (or a warp, a.lanes = 32): the weights' gradients are sums over the whole row.
-template <typename T, typename O, int V>
-__device__ __forceinline__ void combine_backward_at(const RowArgs& a, int64_t token, int j0, int c, const int64_t* p,
+template <typename T, typename O, int V, int U, int AT>
+__device__ __forceinline__ void combine_backward_at(const RowArgs& a, int64_t token, int i, int parts, const int64_t* p,
                                                     const float* w, float* dot) {
-  Part<O, V> d;
-  d.load(static_cast<const O*>(a.token) + token * a.token_ld + c);
-  Part<T, V> y[kAtOnce];
+  Part<O, V> d[U];
+  Part<T, V> y[AT][U];
+  const O* from = static_cast<const O*>(a.token) + token * a.token_ld;
 #pragma unroll
-  for (int u = 0; u < kAtOnce; ++u)
-    if (p[u] >= 0) y[u].load(static_cast<const T*>(a.sorted) + p[u] * a.sorted_ld + c);
+  for (int u = 0; u < U; ++u) {
+    if (i + u * a.lanes < parts) d[u].load(from + (i + u * a.lanes) * V);
+    else d[u].clear();
+  }
 #pragma unroll
-  for (int u = 0; u < kAtOnce; ++u)
-    if (p[u] >= 0) {
-      Part<T, V> dy;
+  for (int q = 0; q < AT; ++q)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (p[q] >= 0 && i + u * a.lanes < parts)
+        y[q][u].load(static_cast<const T*>(a.sorted) + p[q] * a.sorted_ld + (i + u * a.lanes) * V);
+      else
+        y[q][u].clear();
+    }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float dv[V];
+    d[u].up(dv);
+#pragma unroll
+    for (int q = 0; q < AT; ++q) {
+      float v[V];
+      y[q][u].up(v);
+      if (p[q] < 0) continue;                               // dout may be infinite
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        dot[u] = fmaf(d.v[e], y[u].v[e], dot[u]);
-        dy.v[e] = w[u] * d.v[e];
+        dot[q] = fmaf(dv[e], v[e], dot[q]);
+        v[e] = w[q] * dv[e];
       }
-      dy.store(static_cast<T*>(a.out_sorted) + p[u] * a.out_sorted_ld + c);
+      if (i + u * a.lanes < parts) {
+        Part<T, V> dy;
+        dy.down(v);
+        dy.store(static_cast<T*>(a.out_sorted) + p[q] * a.out_sorted_ld + (i + u * a.lanes) * V);
+      }
     }
+  }
 }
-template <typename T, typename O, int V>
+template <typename T, typename O, int V, int U, int AT>
 __global__ void __launch_bounds__(kThreads) k_combine_backward(const __grid_constant__ RowArgs a) {
-  __shared__ float part[kThreads / 32][kAtOnce];
-  const Item it = item_of<V>(a);
+  __shared__ float part[kThreads / 32][AT];
   const bool cta = a.lanes == kThreads;
-  if (it.token >= a.tokens) return;                         // whole warps, or whole CTAs
+  const int64_t token = cta ? blockIdx.x : blockIdx.x * static_cast<int64_t>(kThreads / 32) + threadIdx.x / 32;
+  const int first = threadIdx.x % a.lanes;
+  if (token >= a.tokens) return;                            // whole warps, or whole CTAs
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t count = *a.count;
-  for (int j0 = 0; j0 < a.k; j0 += kAtOnce) {
-    int64_t p[kAtOnce];
-    float w[kAtOnce], dot[kAtOnce];
+  for (int j0 = 0; j0 < a.k; j0 += AT) {
+    int64_t p[AT];
+    float w[AT], dot[AT];
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
-      const int64_t e = it.token * a.k + j0 + u;
-      p[u] = j0 + u < a.k ? place_of(a, e) : -1;
-      w[u] = j0 + u < a.k ? a.weight[e] : 0.0f;
-      dot[u] = 0.0f;
+    for (int q = 0; q < AT; ++q) {
+      const int64_t e = token * a.k + j0 + q;
+      p[q] = j0 + q < a.k ? place_of(a, e) : -1;
+      w[q] = j0 + q < a.k ? a.weight[e] : 0.0f;
+      dot[q] = 0.0f;
     }
-    each_part<V>(it, a.width, [&](int c) { combine_backward_at<T, O, V>(a, it.token, j0, c, p, w, dot); },
-                 [&](int c) { combine_backward_at<T, O, 1>(a, it.token, j0, c, p, w, dot); });
+    each_part<V, U>(first, a.lanes, a.width,
+                    [&](int i) { combine_backward_at<T, O, V, U, AT>(a, token, i, a.width / V, p, w, dot); },
+                    [&](int c) { combine_backward_at<T, O, 1, 1, AT>(a, token, c, a.width, p, w, dot); });
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
+    for (int q = 0; q < AT; ++q) {
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) dot[u] += __shfl_xor_sync(~0u, dot[u], o);
+      for (int o = 16; o > 0; o >>= 1) dot[q] += __shfl_xor_sync(~0u, dot[q], o);
     }
     if (cta) {
       if (lane == 0) {
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) part[warp][u] = dot[u];
+        for (int q = 0; q < AT; ++q) part[warp][q] = dot[q];
       }
       __syncthreads();
-      if (threadIdx.x < kAtOnce && j0 + threadIdx.x < a.k) {
+      if (threadIdx.x < AT && j0 + threadIdx.x < a.k) {
         float s = 0.0f;
         for (int q = 0; q < kThreads / 32; ++q) s += part[q][threadIdx.x];
-        a.dweight[it.token * a.k + j0 + threadIdx.x] = s;
+        a.dweight[token * a.k + j0 + threadIdx.x] = s;
       }
       __syncthreads();
     } else if (lane == 0) {
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u)
-        if (j0 + u < a.k) a.dweight[it.token * a.k + j0 + u] = dot[u];
+      for (int q = 0; q < AT; ++q)
+        if (j0 + q < a.k) a.dweight[token * a.k + j0 + q] = dot[q];
     }
   }
   // the rows that no entry has
-  for (int64_t e = max(count, it.token * a.k); e < (it.token + 1) * a.k; ++e) {
+  for (int64_t e = max(count, token * a.k); e < (token + 1) * a.k; ++e) {
     T* dy = static_cast<T*>(a.out_sorted) + e * a.out_sorted_ld;
-    each_part<V>(it, a.width, [&](int c) {
+    each_part<V, 1>(first, a.lanes, a.width, [&](int i) {
       Part<T, V> none;
-#pragma unroll
-      for (int x = 0; x < V; ++x) none.v[x] = 0.0f;
-      none.store(dy + c);
+      none.clear();
+      none.store(dy + i * V);
     }, [&](int c) { dy[c] = Elem<T>::down(0.0f); });
   }
 }
@@ -230,58 +299,54 @@ __global__ void __launch_bounds__(kThreads) k_combine_backward(const __grid_cons
 bool wide(const void* p, int64_t ld, int type) {
   return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld) * type_size(type)) & 15) == 0;
 }
-int64_t parts_of(int width, int v) { return (width + v - 1) / v; }
-
-// Threads of an item: no more than a row has parts, a power of two.
-int lanes_for(int64_t parts, int least) {
-  int lanes = least;
-  while (lanes < kThreads && lanes < parts) lanes *= 2;
-  return lanes;
-}
-// A part a thread: items of at most a CTA, as many as a row takes.
-cudaError_t plan_flat(RowArgs& a, int v, unsigned& grid) {
-  const int64_t parts = parts_of(a.width, v);
-  a.lanes = lanes_for(parts, 1);
-  a.slices = static_cast<int>((parts + a.lanes - 1) / a.lanes);
-  const int64_t per = kThreads / a.lanes, ctas = (a.tokens * a.slices + per - 1) / per;
+// Threads of a token: U parts each where rows are long.
+cudaError_t plan_flat(RowArgs& a, int v, int u, unsigned& grid) {
+  const int parts = std::max(a.width / v, 1);
+  a.lanes = (parts + u - 1) / u;
+  const int64_t ctas = (a.tokens * a.lanes + kThreads - 1) / kThreads;
   grid = static_cast<unsigned>(ctas);
   return ctas > 0x7FFFFFFF ? cudaErrorInvalidConfiguration : cudaSuccess;
 }
 
+template <typename T, int V, int U>
+cudaError_t launch_dispatch(RowArgs a, cudaStream_t s) {
+  unsigned grid;
+  const cudaError_t e = plan_flat(a, V, U, grid);
+  if (e != cudaSuccess) return e;
+  k_dispatch<T, V, U><<<grid, kThreads, 0, s>>>(a);
+  return cudaGetLastError();
+}
 template <typename T>
-cudaError_t dispatch_type(RowArgs a, bool vec, cudaStream_t s) {
-  unsigned grid;
-  const cudaError_t e = plan_flat(a, vec ? kVec<T> : 1, grid);
-  if (e != cudaSuccess) return e;
-  if (vec) k_dispatch<T, kVec<T>><<<grid, kThreads, 0, s>>>(a);
-  else k_dispatch<T, 1><<<grid, kThreads, 0, s>>>(a);
-  return cudaGetLastError();
+cudaError_t dispatch_type(const RowArgs& a, bool vec, cudaStream_t s) {
+  return vec ? launch_dispatch<T, kVec<T>, 1>(a, s) : launch_dispatch<T, 1, 4>(a, s);
 }
 
-template <typename T, typename O>
-cudaError_t combine_type(RowArgs a, bool vec, cudaStream_t s) {
+template <typename T, typename O, int V, int U, int AT, bool WEIGHTS>
+cudaError_t launch_combine(RowArgs a, cudaStream_t s) {
   unsigned grid;
-  const cudaError_t e = plan_flat(a, vec ? kVec<T> : 1, grid);
+  const cudaError_t e = plan_flat(a, V, U, grid);
   if (e != cudaSuccess) return e;
-  if (a.weight) {
-    if (vec) k_combine<T, O, kVec<T>, true><<<grid, kThreads, 0, s>>>(a);
-    else k_combine<T, O, 1, true><<<grid, kThreads, 0, s>>>(a);
-  } else {
-    if (vec) k_combine<T, O, kVec<T>, false><<<grid, kThreads, 0, s>>>(a);
-    else k_combine<T, O, 1, false><<<grid, kThreads, 0, s>>>(a);
-  }
+  k_combine<T, O, V, U, AT, WEIGHTS><<<grid, kThreads, 0, s>>>(a);
   return cudaGetLastError();
 }
+template <typename T, typename O, bool WEIGHTS>
+cudaError_t combine_type(const RowArgs& a, bool vec, cudaStream_t s) {
+  if (a.k <= 4) return vec ? launch_combine<T, O, kVec<T>, kWide, 4, WEIGHTS>(a, s) : launch_combine<T, O, 1, kSingle, 4, WEIGHTS>(a, s);
+  return vec ? launch_combine<T, O, kVec<T>, 1, 8, WEIGHTS>(a, s) : launch_combine<T, O, 1, kSingle / 2, 8, WEIGHTS>(a, s);
+}
 
-template <typename T, typename O>
-cudaError_t combine_backward_type(RowArgs a, bool vec, cudaStream_t s) {
-  a.lanes = parts_of(a.width, vec ? kVec<T> : 1) <= 128 ? 32 : kThreads;
-  a.slices = 1;
+template <typename T, typename O, int V, int U, int AT>
+cudaError_t launch_combine_backward(RowArgs a, cudaStream_t s) {
+  a.lanes = a.width / V <= 128 ? 32 : kThreads;
   const int64_t per = kThreads / a.lanes, ctas = (a.tokens + per - 1) / per;
   if (ctas > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
-  if (vec) k_combine_backward<T, O, kVec<T>><<<static_cast<unsigned>(ctas), kThreads, 0, s>>>(a);
-  else k_combine_backward<T, O, 1><<<static_cast<unsigned>(ctas), kThreads, 0, s>>>(a);
+  k_combine_backward<T, O, V, U, AT><<<static_cast<unsigned>(ctas), kThreads, 0, s>>>(a);
   return cudaGetLastError();
+}
+template <typename T, typename O>
+cudaError_t combine_backward_type(const RowArgs& a, bool vec, cudaStream_t s) {
+  if (a.k <= 4) return vec ? launch_combine_backward<T, O, kVec<T>, 1, 4>(a, s) : launch_combine_backward<T, O, 1, kSingle, 4>(a, s);
+  return vec ? launch_combine_backward<T, O, kVec<T>, 1, 8>(a, s) : launch_combine_backward<T, O, 1, kSingle / 2, 8>(a, s);
 }
 
 int shape_status(int type, int64_t rows, int width, int k) {
@@ -295,11 +360,14 @@ int status(cudaError_t e) { return e == cudaSuccess ? HA_OK : HA_ECUDA; }
 
 int combine_any(RowArgs a, int type, int out_type, cudaStream_t s) {
   const bool vec = wide(a.sorted, a.sorted_ld, type) && wide(a.out_token, a.out_token_ld, out_type);
-  if (type == HA_TYPE_FP32) return status(combine_type<float, float>(a, vec, s));
-  if (type == HA_TYPE_BF16)
-    return status(out_type == type ? combine_type<__nv_bfloat16, __nv_bfloat16>(a, vec, s)
-                                   : combine_type<__nv_bfloat16, float>(a, vec, s));
-  return status(out_type == type ? combine_type<__half, __half>(a, vec, s) : combine_type<__half, float>(a, vec, s));
+  const auto go = [&](auto weights) {
+    constexpr bool W = decltype(weights)::value;
+    if (type == HA_TYPE_FP32) return combine_type<float, float, W>(a, vec, s);
+    if (type == HA_TYPE_BF16)
+      return out_type == type ? combine_type<__nv_bfloat16, __nv_bfloat16, W>(a, vec, s) : combine_type<__nv_bfloat16, float, W>(a, vec, s);
+    return out_type == type ? combine_type<__half, __half, W>(a, vec, s) : combine_type<__half, float, W>(a, vec, s);
+  };
+  return status(a.weight ? go(std::true_type()) : go(std::false_type()));
 }
 
 }  // namespace
