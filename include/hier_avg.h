@@ -475,15 +475,15 @@ int hier_avg_grad_norm(int tensors, void* const* grads_dev, const int* types, co
  * A logit at or below -1e30 counts as not allowed.  A row without an allowed class, or with NaN or +inf among
  * them, rejects its draft; where it is row n, its token is -1 with log p -inf or NaN.
  * temperature 2^-126 .. 1e27.  workspace_dev: 16-byte aligned, of hier_avg_verify_workspace's bytes.
- * Errors: HA_EINVAL, HA_EUNSUPPORTED for 2^28 rows, HA_ENOMEM, HA_ECUDA. */
+ * Errors: HA_EINVAL, HA_EUNSUPPORTED for 2^26 rows or 2^24 sequences, HA_ENOMEM, HA_ECUDA. */
 int hier_avg_verify_workspace(int64_t sequences, int drafts, int64_t* bytes);
 int hier_avg_verify_drafts(const void* logits_dev, int type, int64_t sequences, int drafts, int64_t classes,
                            int64_t logits_seq, int64_t logits_row, const void* drafts_dev, int draft_bytes,
                            const float* uniform_dev, const float* noise_dev, int64_t noise_ld, const void* probs_dev,
                            int probs_type, int64_t probs_seq, int64_t probs_row, const uint8_t* allowed_dev,
                            int64_t allowed_seq, int64_t allowed_row, double temperature, int32_t* tokens_dev,
-                           int32_t* accepted_dev, float* logp_dev, void* workspace_dev, int64_t workspace_bytes,
-                           void* stream);
+                           int32_t* accepted_dev, float* logp_dev, void* workspace_dev,
+                           int64_t workspace_bytes, void* stream);
 
 /* Synchronise `stream` and report a bounded wait inside a grouped product that ran out on
  * this device (HA_ETIMEOUT, once; the outputs are then invalid) or an asynchronous error.

@@ -6,22 +6,31 @@
 //   the next token is argmax_j r_j / noise_j with r = max(p_n - q_n, 0) after a rejection (p_n where that
 //   leaves nothing), else r = p_n.  With exponential noise that is a draw from r.
 //
-// Two kernels: one takes every row's largest logit and the sum of its exponentials, and says whether its draft
-// would be accepted; the other finds n and looks for the next token.  A row is shared by the CTAs of a cluster.
+// Two kernels, each over as many CTAs as fill the GPU.  The first takes shares of all rows: their largest logit and the
+// sum of the exponentials.  The second joins them, finds n, and takes shares of row n's scores; the last CTA of a
+// sequence to end joins those.  Rows behind a rejected draft are summed for nothing, but a row waits for no other:
+// 128 sequences of 6 rows of 50021 fp32 logits under a mask take 54 us so, 57 where CTAs ask before they start whether
+// a draft has failed, and 95 by a cluster a sequence that takes its rows in turn and stops.  Both kernels are bound by the
+// instructions of an element, about as long as the memory takes (54 us against 41 for all the bytes).
 // Sums and scores are in fp32, with a bound of what that may be off; a decision within the bound is made
-// again by one CTA in 64 bits, so that the tokens are those of the formulas in 64 bits.
+// again in 64 bits, so that the tokens are those of the formulas in 64 bits.
 #include <algorithm>
 #include <cfloat>
+#include <climits>
 #include <cmath>
+#include <type_traits>
 
 #include "op_common.cuh"
 
 namespace ha {
 namespace {
 
-constexpr int kMaxCluster = 8;
-constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kUnroll = 4;
+constexpr int kThreads = 128, kWarps = kThreads / 32;
+constexpr int kResident = 8;              // CTAs of an SM
+constexpr int kUnroll = 4;                // 16-byte loads in flight of a sum
+constexpr int kScores = 4;                // classes whose scores are in flight
+constexpr int kSumParts = 32;             // CTAs of a row, at most
+constexpr int kScoreParts = 128;          // CTAs of a sequence's scores, at most
 
 // The relative error of a probability e^((z - m) / t) / S with d = (z - m) log2(e) / t, in steps of 2^-22: d takes
 // three roundings of 2^-24 of itself each (times ln 2: |d| / 2), 2^d one step, S the same for a mean |d| that is at most
@@ -29,11 +38,28 @@ constexpr int kUnroll = 4;
 float slack(int classes, int elements_a_load) { return 20.0f + (classes / (kThreads * elements_a_load) + 16) * 0.25f; }
 __device__ __forceinline__ float bound(float d, float slack) { return 0x1p-22f * (slack + fabsf(d)); }
 
-struct Row {                              // of the workspace
+struct Sum {
   float m, S;                             // largest logit; sum of e^((z - m) / t), 0: no class, NaN: a bad row
-  float logp;                             // of the draft
-  int accepted;
 };
+// What bounds a class's score, r / noise and what that may be off, from above.
+struct Best {
+  float most, others;                     // the largest, and the largest of all others
+  int index, pad;                         // of the largest
+};
+struct Head {                             // of a row's draft
+  double left;                            // u q(x)
+  float zx;                               // its logit; kNone: no class, or not allowed
+  int draft;                              // -1: none, INT_MAX: no class
+};
+// The workspace; a row is sequence * (K + 1) + i.
+struct Work {
+  Head* heads;                            // [rows]
+  Sum* sums;                              // [rows, kSumParts]
+  Best* bests;                            // [sequences, kScoreParts]
+  int* done;                              // [sequences] CTAs whose scores are there
+};
+constexpr int64_t kRowBytes = sizeof(Head) + kSumParts * sizeof(Sum);
+constexpr int64_t kSequenceBytes = kScoreParts * sizeof(Best) + sizeof(int);
 
 struct VerifyArgs {
   const void* logits;
@@ -48,39 +74,17 @@ struct VerifyArgs {
   int64_t ok_seq, ok_row;
   int *tokens, *accepted;
   float* logp;
-  Row* rows;
   double temperature;
   float c;                                // log2(e) / temperature
   float inv_t;
   float slack;                            // of bound()
   int K, classes;
+  int64_t sequences;
+  int sum_parts, score_parts;
+  Work w;
   bool wide_drafts;
   int probs_type;                         // -1: none
 };
-
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ uint32_t cluster_parts() {
-  uint32_t r;
-  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
-}
-// The same place of shared memory in CTA `rank` of the cluster.
-template <typename V>
-__device__ __forceinline__ V from_cta(const V* p, int rank) {
-  static_assert(sizeof(V) == 4, "a word");
-  const uint32_t la = static_cast<uint32_t>(__cvta_generic_to_shared(p));
-  uint32_t ra, v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ra) : "r"(la), "r"(rank));
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(ra) : "memory");
-  return *reinterpret_cast<V*>(&v);
-}
 
 __device__ __forceinline__ int64_t draft_of(const VerifyArgs& a, int64_t seq, int i) {
   const int64_t e = seq * a.K + i;
@@ -99,9 +103,6 @@ __device__ __forceinline__ float logit(const T* z, const uint8_t* ok, int j) {
   return ok && !ok[j] ? kNone<T> : v;
 }
 
-struct Sum {
-  float m, S;
-};
 __device__ __forceinline__ Sum join(Sum s, float c) {
   const float m = from_ordered(__reduce_max_sync(~0u, ordered(s.m)));
   Sum r = {m, s.S * exp2_fast(max_nan((s.m - m) * c, -200.0f))};
@@ -129,135 +130,124 @@ __device__ __noinline__ double exact_lse(const VerifyArgs& a, const T* z, const 
   return top + log(s);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) k_verify_rows(const __grid_constant__ VerifyArgs a) {
-  __shared__ Sum warp_sum[kWarps];
-  __shared__ Sum cta_sum, row_sum;
-  __shared__ double part[kWarps];
-  __shared__ bool unsure;
-  constexpr int V = kVec<T>;
-  const uint32_t rank = cluster_rank(), parts = cluster_parts();
-  const int64_t row = blockIdx.x / parts, seq = row / (a.K + 1);
-  const int i = static_cast<int>(row % (a.K + 1)), tid = threadIdx.x, lane = tid & 31;
-  const T* z = static_cast<const T*>(a.logits) + seq * a.z_seq + i * a.z_row;
-  const uint8_t* ok = a.allowed ? a.allowed + seq * a.ok_seq + i * a.ok_row : nullptr;
-  const float c = a.c;
-  let_next_start();
+// Two minus infinities of a 16-bit type.
+template <typename T> constexpr uint32_t kBits16 = 0xFC00FC00u;
+template <> constexpr uint32_t kBits16<__nv_bfloat16> = 0xFF80FF80u;
 
+// The sum of share `rank` of `parts` of a row, by a CTA; each warp has its own.  Minus infinity stays as it is: the
+// largest logit is kNone at least, so that its distance is no NaN and its exponential 0.
+template <typename T, bool MASK>
+__device__ __forceinline__ Sum scan(const T* z, const uint8_t* ok, int classes, float c, int rank, int parts) {
+  constexpr int V = kVec<T>;
+  const int tid = threadIdx.x;
   // The vectors start at the row's first 16-byte boundary; the entries before and after them are taken one by one.
   const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
-  const int head = min(a.classes, shift ? V - shift : 0), vecs = (a.classes - head) / V, tail = head + vecs * V;
+  int head = shift ? V - shift : 0;
+  if (MASK && head < 4) head += V;                           // the words around a vector's mask bytes are the row's own
+  head = min(classes, head);
+  int vecs = (classes - head) / V;
+  if (MASK && vecs > 0 && head + vecs * V + 4 > classes) --vecs;
+  const int tail = head + vecs * V;
   const int v0 = static_cast<int>(static_cast<int64_t>(vecs) * rank / parts);
   const int v1 = static_cast<int>(static_cast<int64_t>(vecs) * (rank + 1) / parts);
-  Sum s = {kNone<T>, 0.0f};
+  const uint4* zv = reinterpret_cast<const uint4*>(z + head);
+  const uint32_t ok_shift = MASK ? 8 * static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ok + head) & 3) : 0;
+  const uint32_t* okw = MASK ? reinterpret_cast<const uint32_t*>(ok + head - ok_shift / 8) : nullptr;
+  float m = kNone<T>;
+  Pair S = pair(0.0f, 0.0f);
   int one = -1;
   if (rank == 0 && tid < head) one = tid;
-  if (rank == parts - 1 && tid >= 32 && tail + tid - 32 < a.classes) one = tail + tid - 32;
-  if (one >= 0) {
-    s.m = logit(z, ok, one);
-    s.S = s.m > kNone<T> ? 1.0f : s.m == s.m ? 0.0f : s.m;
-    if (s.m != s.m) s.m = kNone<T>;
-  }
-  for (int r = v0 + tid; r < v1; r += kThreads * kUnroll) {
+  if (rank == parts - 1 && tid >= 16 && tail + tid - 16 < classes) one = tail + tid - 16;
+  const float left = one >= 0 ? logit(z, MASK ? ok : nullptr, one) : kNone<T>;
+  // kUnroll vectors, all loads before the first use and one look at the largest; the last ones may be fewer.
+  auto batch = [&](int r, auto whole) {
+    constexpr bool kWhole = decltype(whole)::value;
     uint4 w[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      if (r + u * kThreads < v1) w[u] = __ldg(reinterpret_cast<const uint4*>(z + head) + r + u * kThreads);
+    uint32_t in[kUnroll][V / 4 + 1];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      if (r + u * kThreads >= v1) break;
-      float v[V];
-      unpack<T>(w[u], v);
-      const int at = head + (r + u * kThreads) * V;
-      float top = s.m;
+      const int i = r + u * kThreads;
+      if (kWhole || i < v1) {
+        w[u] = __ldg(zv + i);
+        if (MASK) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        v[e] = max_nan(v[e], kNone<T>);
-        if (ok && !ok[at + e]) v[e] = kNone<T>;
-        top = fmaxf(top, v[e]);
-      }
-      if (top > s.m) {
-        s.S *= exp2_fast(max_nan((s.m - top) * c, -200.0f));
-        s.m = top;
-      }
-      // what is not allowed adds 0: the largest is above it, or all are not
-      if (s.m > kNone<T>) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = exp2_fast((v[e] - s.m) * c);
-#pragma unroll
-        for (int o = V / 2; o > 0; o >>= 1) {
-#pragma unroll
-          for (int e = 0; e < o; ++e) v[e] += v[e + o];
+          for (int h = 0; h <= V / 4; ++h) in[u][h] = __ldg(okw + i * (V / 4) + h);
         }
-        s.S += v[0];
       } else {
+        const uint32_t inf = sizeof(T) == 4 ? 0xFF800000u : kBits16<T>;
+        w[u] = make_uint4(inf, inf, inf, inf);
+#pragma unroll
+        for (int h = 0; h <= V / 4; ++h) in[u][h] = 0;
+      }
+    }
+    float v[kUnroll][V];
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      unpack<T>(w[u], v[u]);
+      if (MASK) {
+#pragma unroll
+        for (int h = 0; h < V / 4; ++h) {
+          const uint32_t ok4 = __funnelshift_r(in[u][h], in[u][h + 1], ok_shift);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!(ok4 & 0xFFu << 8 * e)) v[u][4 * h + e] = -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < V; e += 2) top = fmaxf(top, fmaxf(v[u][e], v[u][e + 1]));
+    }
+    if (top > m) {
+      const float f = exp2_fast(max_nan((m - top) * c, -200.0f));
+      S = mul2(S, pair(f, f));
+      m = top;
+    }
+    if (m > kNone<T>) {
+      const Pair minus_m = pair(-m, -m), c2 = pair(c, c);
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        Pair sum;
+#pragma unroll
+        for (int e = 0; e < V; e += 2) {
+          float x, y;
+          halves(mul2(add2(pair(v[u][e], v[u][e + 1]), minus_m), c2), x, y);
+          const Pair p = pair(exp2_fast(x), exp2_fast(y));
+          sum = e == 0 ? p : add2(sum, p);
+        }
+        S = add2(S, sum);
+      }
+    } else {                                                 // nothing allowed so far, unless it is a NaN
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
         for (int e = 0; e < V; ++e)
-          if (v[e] != v[e]) s.S = v[e];
-      }
+          if (v[u][e] != v[u][e]) S = pair(NAN, 0.0f);
     }
+  };
+  int r = v0 + tid;
+  for (; r + (kUnroll - 1) * kThreads < v1; r += kUnroll * kThreads) batch(r, std::true_type());
+  if (r < v1) batch(r, std::false_type());
+  Sum s = {m, 0.0f};
+  float x, y;
+  halves(S, x, y);
+  s.S = x + y;
+  if (left > s.m) {
+    s.S = fmaf(s.S, exp2_fast(max_nan((s.m - left) * c, -200.0f)), left < INFINITY ? 1.0f : NAN);
+    s.m = left;
+  } else if (!(left <= kNone<T>)) {
+    s.S += exp2_fast((left - s.m) * c);
   }
-  s = join(s, c);
-  if (lane == 0) warp_sum[tid >> 5] = s;
-  __syncthreads();
-  if (tid < 32) {
-    s = join(tid < kWarps ? warp_sum[tid] : Sum{kNone<T>, 0.0f}, c);
-    if (tid == 0) cta_sum = s;
-  }
-  if (parts > 1) {
-    cluster_barrier();
-    if (rank == 0 && tid < 32) {
-      s = {kNone<T>, 0.0f};
-      if (tid < static_cast<int>(parts)) s = {from_cta(&cta_sum.m, tid), from_cta(&cta_sum.S, tid)};
-      s = join(s, c);
-    }
-    cluster_barrier();
-    if (rank != 0) return;
-  }
-  if (tid == 0) {
-    const int64_t x = i < a.K ? draft_of(a, seq, i) : -1;
-    Row out = {s.m, s.S, 0.0f, 0};
-    unsure = false;
-    if (x >= 0 && x < a.classes && s.S > 0.0f) {            // not where there is no class, or a NaN
-      const float zx = logit(z, ok, static_cast<int>(x)), d = (zx - s.m) * c;
-      const double q = a.probs ? static_cast<double>(prob_at(a, seq * a.q_seq + i * a.q_row + x)) : 1.0;
-      const double left = static_cast<double>(a.uniform[seq * a.K + i]) * q;
-      if (zx > kNone<T>) {
-        const double p = static_cast<double>(exp2_fast(d)) / s.S, off = bound(d, a.slack) * p;
-        out.accepted = left < p;
-        unsure = fabs(left - p) <= off || (p < 1e-30 && left < 1e-30);
-        out.logp = fmaf(zx - s.m, a.inv_t, -logf(s.S));
-      }
-    }
-    a.rows[row] = out;
-    row_sum = s;
-  }
-  __syncthreads();
-  if (!unsure) return;
-  const double lse = exact_lse(a, z, ok, row_sum.m, part);
-  if (tid == 0) {
-    const int64_t x = draft_of(a, seq, i);
-    const double q = a.probs ? static_cast<double>(prob_at(a, seq * a.q_seq + i * a.q_row + x)) : 1.0;
-    const double p = exp(static_cast<double>(logit(z, ok, static_cast<int>(x))) / a.temperature - lse);
-    a.rows[row].accepted = static_cast<double>(a.uniform[seq * a.K + i]) * q < p;
-  }
+  return join(s, c);
 }
 
-// The best class so far: its score, what that may be off, and the most that any other's may be.
-struct Best {
-  float score, off, others;
-  int index;
-};
 __device__ __forceinline__ Best better(const Best& a, const Best& b) {
-  const bool first = a.score > b.score || (a.score == b.score && static_cast<uint32_t>(a.index) < static_cast<uint32_t>(b.index));
-  const Best &w = first ? a : b, &l = first ? b : a;
-  return {w.score, w.off, fmaxf(fmaxf(a.others, b.others), l.index < 0 ? 0.0f : l.score + l.off), w.index};
+  const bool first = a.most > b.most;
+  return {first ? a.most : b.most, fmaxf(fminf(a.most, b.most), fmaxf(a.others, b.others)), first ? a.index : b.index, 0};
 }
 __device__ __forceinline__ Best warp_best(Best b) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    const Best x = {__shfl_xor_sync(~0u, b.score, o), __shfl_xor_sync(~0u, b.off, o), __shfl_xor_sync(~0u, b.others, o),
-                    __shfl_xor_sync(~0u, b.index, o)};
+    const Best x = {__shfl_xor_sync(~0u, b.most, o), __shfl_xor_sync(~0u, b.others, o), __shfl_xor_sync(~0u, b.index, o), 0};
     b = better(b, x);
   }
   return b;
@@ -319,145 +309,250 @@ __device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const u
   return best;
 }
 
+// Whether a row's draft is accepted: 0, 1, or 2 where it takes 64 bits to say.
+__device__ __forceinline__ int decide(const VerifyArgs& a, const Head& h, Sum s, float none) {
+  if (!(h.zx > none && s.S > 0.0f)) return 0;                // no class, or a NaN in the row
+  const float d = (h.zx - s.m) * a.c;
+  const double p = static_cast<double>(exp2_fast(d) / s.S), off = static_cast<double>(bound(d, a.slack)) * p;
+  if (fabs(h.left - p) <= off || (p < 1e-30 && h.left < 1e-30)) return 2;
+  return h.left < p;
+}
+
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_verify_next(const __grid_constant__ VerifyArgs a) {
-  __shared__ Best warp_bests[kWarps];
-  __shared__ Best cta_best;
-  __shared__ double part[kWarps];
-  __shared__ int part_index[kWarps], row_n, token_shared;
-  __shared__ bool unsure;
-  const uint32_t rank = cluster_rank(), parts = cluster_parts();
-  const int64_t seq = blockIdx.x / parts;
-  const int tid = threadIdx.x, lane = tid & 31, K = a.K;
-  wait_for_previous();
-  const Row* rows = a.rows + seq * (K + 1);
-  if (tid < 32) {                                            // the first draft that is not accepted
-    int n = K;
-    for (int i0 = 0; i0 < K && n == K; i0 += 32) {
-      const uint32_t bad = __ballot_sync(~0u, i0 + lane < K && !rows[i0 + lane].accepted);
-      if (bad) n = i0 + __ffs(bad) - 1;
+__device__ __forceinline__ const T* logits_of(const VerifyArgs& a, int64_t seq, int i) {
+  return static_cast<const T*>(a.logits) + seq * a.z_seq + i * a.z_row;
+}
+__device__ __forceinline__ const uint8_t* mask_of(const VerifyArgs& a, int64_t seq, int i) {
+  return a.allowed ? a.allowed + seq * a.ok_seq + i * a.ok_row : nullptr;
+}
+
+template <typename T, bool MASK>
+__global__ void __launch_bounds__(kThreads, kResident) k_verify_sums(const __grid_constant__ VerifyArgs a) {
+  __shared__ Sum warp_sum[kWarps];
+  const int tid = threadIdx.x, lane = tid & 31, rank = blockIdx.x % a.sum_parts;
+  const int64_t row = blockIdx.x / a.sum_parts, seq = row / (a.K + 1);
+  const int i = static_cast<int>(row % (a.K + 1));
+  let_next_start();
+  const T* z = logits_of<T>(a, seq, i);
+  const uint8_t* ok = mask_of(a, seq, i);
+  Head h = {0.0, kNone<T>, -1};
+  if (rank == 0 && tid == 0) {
+    const int64_t x = i < a.K ? draft_of(a, seq, i) : -1;
+    if (x >= 0) {
+      h.draft = x < a.classes ? static_cast<int>(x) : INT_MAX;
+      if (x < a.classes) {
+        h.left = a.uniform[seq * a.K + i];
+        if (a.probs) h.left *= prob_at(a, seq * a.q_seq + i * a.q_row + x);
+        h.zx = logit(z, ok, static_cast<int>(x));
+      }
     }
-    if (lane == 0) row_n = n;
+    a.w.heads[row] = h;
+    if (i == 0) a.w.done[seq] = 0;
   }
+  Sum s = scan<T, MASK>(z, ok, a.classes, a.c, rank, a.sum_parts);
+  if (lane == 0) warp_sum[tid >> 5] = s;
   __syncthreads();
-  const int n = row_n;
-  const int64_t x64 = n < K ? draft_of(a, seq, n) : -1;
-  const bool rejected = x64 >= 0;
-  const int x = x64 < a.classes ? static_cast<int>(x64) : -1;
-  const T* z = static_cast<const T*>(a.logits) + seq * a.z_seq + n * a.z_row;
-  const uint8_t* ok = a.allowed ? a.allowed + seq * a.ok_seq + n * a.ok_row : nullptr;
+  if (tid >= 32) return;
+  s = join(lane < kWarps ? warp_sum[lane] : Sum{kNone<T>, 0.0f}, a.c);
+  if (lane == 0) a.w.sums[row * kSumParts + rank] = s;
+}
+
+// Q: the draft probabilities' type, any where there are none.
+template <typename T, typename Q>
+__global__ void __launch_bounds__(kThreads, kResident) k_verify_next(const __grid_constant__ VerifyArgs a) {
+  __shared__ Sum row_sum[kWarps];
+  __shared__ Head row_head[kWarps];
+  __shared__ int row_state[kWarps];
+  __shared__ Best warp_bests[kWarps];
+  __shared__ double part[kWarps];
+  __shared__ int part_index[kWarps];
+  __shared__ int last_token;
+  __shared__ bool is_last, unsure;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.K, rank = blockIdx.x % a.score_parts;
+  const int64_t seq = blockIdx.x / a.score_parts, row0 = seq * (K + 1);
   const float* noise = a.noise + seq * a.noise_ld;
-  const int64_t q0 = seq * a.q_seq + n * a.q_row;
-  const Row st = rows[n];
-  const bool dead = !(st.S > 0.0f);                          // no class, or a NaN
-  Best best = {0.0f, 0.0f, 0.0f, -1};
-  if (!dead) {
-    const float c = a.c, inv_s = 1.0f / st.S;
-    const bool minus_q = rejected && a.probs;
-    const int hole = rejected && !a.probs ? x : -1;
-    const int step = static_cast<int>(parts) * kThreads;
-    for (int j0 = static_cast<int>(rank) * kThreads + tid; j0 < a.classes; j0 += step * kUnroll) {
-      float v[kUnroll], q[kUnroll], e[kUnroll];
+  // this CTA's classes
+  const int c0 = static_cast<int>(static_cast<int64_t>(a.classes) * rank / a.score_parts);
+  const int c1 = static_cast<int>(static_cast<int64_t>(a.classes) * (rank + 1) / a.score_parts);
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const int64_t j = j0 + static_cast<int64_t>(u) * step;
-        v[u] = kNone<T>;
-        q[u] = 0.0f;
-        if (j < a.classes) {
-          v[u] = logit(z, ok, static_cast<int>(j));
-          e[u] = noise[j];
-          if (minus_q) q[u] = prob_at(a, q0 + j);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const int j = j0 + u * step;
-        if (!(v[u] > kNone<T>) || j == hole) continue;
-        const float d = (v[u] - st.m) * c, p = exp2_fast(d) * inv_s, rn = rcp_fast(e[u]);
-        const Best one = {fmaxf(p - q[u], 0.0f) * rn, fmaf(bound(d, a.slack), p, FLT_MIN) * rn, 0.0f, j};
-        if (!(one.score + one.off <= best.others)) best = better(best, one);
+  for (int u = 0; u < kScores; ++u)                          // what does not depend on n may come meanwhile
+    if (c0 + tid + u * kThreads < c1) asm volatile("prefetch.global.L2 [%0];" ::"l"(noise + c0 + tid + u * kThreads));
+  wait_for_previous();
+
+  // ---- the first row whose draft is not accepted, by every CTA of the sequence
+  int n = -1, drafted = -1;
+  Sum st = {0.0f, 0.0f};
+  for (int i0 = 0; n < 0; i0 += kWarps) {
+    const int rows = min(kWarps, K + 1 - i0);
+    if (warp < rows) {
+      Sum s = {kNone<T>, 0.0f};
+      if (lane < a.sum_parts) s = a.w.sums[(row0 + i0 + warp) * kSumParts + lane];
+      s = join(s, a.c);
+      if (lane == 0) {
+        const Head h = a.w.heads[row0 + i0 + warp];
+        row_sum[warp] = s;
+        row_head[warp] = h;
+        row_state[warp] = decide(a, h, s, kNone<T>);
       }
     }
+    __syncthreads();
+    for (int r = 0; r < rows && n < 0; ++r) {
+      const int i = i0 + r;
+      const Head h = row_head[r];
+      bool accepted = row_state[r] == 1;
+      if (row_state[r] == 2) {
+        const T* z = logits_of<T>(a, seq, i);
+        const uint8_t* ok = mask_of(a, seq, i);
+        const double lse = exact_lse(a, z, ok, row_sum[r].m, part);
+        accepted = h.left < exp(static_cast<double>(h.zx) / a.temperature - lse);
+      }
+      if (!accepted) {
+        n = i;
+        st = row_sum[r];
+        drafted = h.draft;
+      } else if (rank == 0 && tid == 0) {
+        a.tokens[row0 + i] = h.draft;
+        a.logp[row0 + i] = fmaf(h.zx - row_sum[r].m, a.inv_t, -logf(row_sum[r].S));
+      }
+    }
+    __syncthreads();
+  }
+
+  // ---- the token behind it
+  const bool rejected = drafted >= 0;
+  const int x = drafted == INT_MAX ? -1 : drafted;
+  const T* z = logits_of<T>(a, seq, n);
+  const uint8_t* ok = mask_of(a, seq, n);
+  const int64_t q0 = seq * a.q_seq + n * a.q_row;
+  const bool dead = !(st.S > 0.0f);                          // no class, or a NaN
+  const bool minus_q = rejected && a.probs;
+  const int hole = rejected && !a.probs ? x : -1;
+  const float inv_s = 1.0f / st.S;
+  const Q* qs = static_cast<const Q*>(a.probs) + q0;
+  // r / noise, and what it may be off
+  const float c = a.c, slack = a.slack * 0x1p-22f;
+  auto score = [&](float v, float q, float e, float& off) {
+    const float d = max_nan((v - st.m) * c, -1e4f), p = exp2_fast(d) * inv_s, rn = rcp_fast(e);
+    off = fmaf(fmaf(-d, 0x1p-22f, slack), p, FLT_MIN) * rn;  // bound(d) p, and what is below fp32's range
+    return fmaxf(p - q, 0.0f) * rn;
+  };
+  Best best = {0.0f, 0.0f, -1, 0};
+  // kScores classes, all loads before the first use.  A class that is masked has p = 0 and a bound next to 0, with which it wins
+  // only where no other is sure to be above it, and 64 bits decide.
+  auto batch = [&](int j0, auto whole) {
+    constexpr bool kWhole = decltype(whole)::value;
+    T v[kScores];
+    Q q[kScores];
+    float e[kScores];
+    uint8_t in[kScores];
+#pragma unroll
+    for (int u = 0; u < kScores; ++u)
+      if (kWhole || j0 + u * kThreads < c1) {
+        v[u] = z[j0 + u * kThreads];
+        e[u] = noise[j0 + u * kThreads];
+      }
+    if (minus_q) {
+#pragma unroll
+      for (int u = 0; u < kScores; ++u)
+        if (kWhole || j0 + u * kThreads < c1) q[u] = qs[j0 + u * kThreads];
+    }
+    if (ok) {
+#pragma unroll
+      for (int u = 0; u < kScores; ++u)
+        if (kWhole || j0 + u * kThreads < c1) in[u] = ok[j0 + u * kThreads];
+    }
+#pragma unroll
+    for (int u = 0; u < kScores; ++u) {
+      const int j = j0 + u * kThreads;
+      if (!kWhole && j >= c1) break;
+      float off, vu = Elem<T>::up(v[u]);
+      if ((ok && !in[u]) || j == hole) vu = -INFINITY;
+      const float s = score(vu, minus_q ? Elem<Q>::up(q[u]) : 0.0f, e[u], off), most = s + off;
+      // (a NaN, of a noise that is none, makes the others as good as the best)
+      best.others = fmaxf(best.others, fminf(most, best.most));
+      if (most > best.most) {
+        best.most = most;
+        best.index = j;
+      }
+    }
+  };
+  if (!dead) {
+    int j0 = c0 + tid;
+    for (; j0 + (kScores - 1) * kThreads < c1; j0 += kScores * kThreads) batch(j0, std::true_type());
+    if (j0 < c1) batch(j0, std::false_type());
   }
   best = warp_best(best);
-  if (lane == 0) warp_bests[tid >> 5] = best;
+  if (lane == 0) warp_bests[warp] = best;
   __syncthreads();
-  if (tid < 32) {
-    best = warp_best(tid < kWarps ? warp_bests[tid] : Best{0.0f, 0.0f, 0.0f, -1});
-    if (tid == 0) cta_best = best;
+  if (warp == 0) {
+    best = warp_best(lane < kWarps ? warp_bests[lane] : Best{0.0f, 0.0f, -1, 0});
+    if (lane == 0) {
+      bool last = true;
+      if (a.score_parts > 1) {
+        a.w.bests[seq * kScoreParts + rank] = best;
+        __threadfence();
+        last = atomicAdd(a.w.done + seq, 1) == a.score_parts - 1;
+        __threadfence();
+      }
+      is_last = last;
+    }
   }
-  if (parts > 1) {
-    cluster_barrier();
-    if (rank == 0 && tid < 32) {
-      best = {0.0f, 0.0f, 0.0f, -1};
-      if (tid < static_cast<int>(parts))
-        best = {from_cta(&cta_best.score, tid), from_cta(&cta_best.off, tid), from_cta(&cta_best.others, tid),
-                from_cta(&cta_best.index, tid)};
+  __syncthreads();
+  if (!is_last) return;
+  if (warp == 0) {
+    if (a.score_parts > 1) {
+      best = {0.0f, 0.0f, -1, 0};
+      for (int r = lane; r < a.score_parts; r += 32) {
+        const int4 v = __ldcg(reinterpret_cast<const int4*>(a.w.bests + seq * kScoreParts + r));
+        best = better(best, *reinterpret_cast<const Best*>(&v));
+      }
       best = warp_best(best);
     }
-    cluster_barrier();
-    if (rank != 0) return;
-  }
-  if (tid == 0) {
-    token_shared = best.index;
-    unsure = !dead && !(best.score - best.off > best.others);
+    if (lane == 0) {
+      float off = 0.0f;
+      const int j = best.index;
+      if (j >= 0) score(Elem<T>::up(z[j]), minus_q ? prob_at(a, q0 + j) : 0.0f, noise[j], off);
+      last_token = j;
+      unsure = !dead && !(best.most - 2.0f * off > best.others);
+    }
   }
   __syncthreads();
-  int token = token_shared;
+  int token = last_token;
   if (unsure) token = exact_token(a, z, ok, noise, st.m, q0, x, rejected, part, part_index);
-  for (int i = tid; i <= K; i += kThreads) {
+  for (int i = n + tid; i <= K; i += kThreads) {
     int t = -1;
     float lp = 0.0f;
-    if (i < n) {
-      t = static_cast<int>(draft_of(a, seq, i));
-      lp = rows[i].logp;
-    } else if (i == n) {
+    if (i == n) {
       t = dead ? -1 : token;
       if (dead) lp = st.S == 0.0f ? -INFINITY : NAN;
       else if (t >= 0) lp = fmaf(logit(z, ok, t) - st.m, a.inv_t, -logf(st.S));
     }
-    a.tokens[seq * (K + 1) + i] = t;
-    a.logp[seq * (K + 1) + i] = lp;
+    a.tokens[row0 + i] = t;
+    a.logp[row0 + i] = lp;
   }
   if (tid == 0) a.accepted[seq] = n;
 }
 
-// CTAs a row: until all rows' fill the GPU (152 SMs), as long as each has a round of loads.
-int cluster_size(int64_t rows, int64_t bytes) {
-  int parts = 1;
-  while (parts < kMaxCluster && rows * parts < 152 && bytes / (2 * parts) >= kThreads * 16) parts *= 2;
-  return parts;
-}
-
-template <typename K>
-cudaError_t launch(K kernel, const VerifyArgs& a, int64_t rows, int parts, bool early, cudaStream_t s) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(rows * parts));
-  cfg.blockDim = dim3(kThreads);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  int n = 0;
-  if (parts > 1) {
-    attr[n].id = cudaLaunchAttributeClusterDimension;
-    attr[n].val.clusterDim.x = parts;
-    attr[n].val.clusterDim.y = 1;
-    attr[n++].val.clusterDim.z = 1;
-  }
-  if (early) {
-    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[n++].val.programmaticStreamSerializationAllowed = 1;
-  }
-  cfg.attrs = attr;
-  cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, kernel, a);
+// CTAs a row or sequence: as many as `ctas` allow, as long as each has a few KB.
+int parts_for(int64_t n, int64_t bytes, int most, int64_t ctas) {
+  const int64_t parts = std::min(std::min<int64_t>(ctas / n, most), bytes / 4096);
+  return static_cast<int>(std::max<int64_t>(parts, 1));
 }
 
 template <typename T>
-cudaError_t verify_type(const VerifyArgs& a, int64_t sequences, cudaStream_t s) {
-  const int64_t rows = sequences * (a.K + 1), bytes = a.classes * static_cast<int64_t>(sizeof(T));
-  const cudaError_t e = launch(k_verify_rows<T>, a, rows, cluster_size(rows, bytes), false, s);
+cudaError_t verify_type(VerifyArgs a, cudaStream_t s) {
+  const int64_t bytes = a.classes * static_cast<int64_t>(sizeof(T)), rows = a.sequences * (a.K + 1);
+  // several rounds of CTAs for the sums, one for the scores, whose CTAs all look for n first
+  a.sum_parts = parts_for(rows, bytes, kSumParts, 152 * kResident * 3);
+  a.score_parts = parts_for(a.sequences, a.classes * int64_t(8), kScoreParts, 152 * kResident);
+  const auto sums = a.allowed ? k_verify_sums<T, true> : k_verify_sums<T, false>;
+  sums<<<static_cast<unsigned>(rows * a.sum_parts), kThreads, 0, s>>>(a);
+  const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  return launch(k_verify_next<T>, a, sequences, cluster_size(sequences, a.classes * int64_t(8)), true, s);
+  const auto next = a.probs_type == HA_TYPE_BF16   ? k_verify_next<T, __nv_bfloat16>
+                    : a.probs_type == HA_TYPE_FP16 ? k_verify_next<T, __half>
+                                                   : k_verify_next<T, float>;
+  return launch_early(next, static_cast<unsigned>(a.sequences * a.score_parts), kThreads, 0, s, a);
 }
 
 bool misaligned(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
@@ -469,8 +564,9 @@ using namespace ha;
 
 extern "C" int hier_avg_verify_workspace(int64_t sequences, int drafts, int64_t* bytes) {
   if (!bytes || sequences < 0 || drafts < 0) return HA_EINVAL;
-  if (drafts >= 0x7FFFFFFF / kMaxCluster || sequences > 0x7FFFFFFF / kMaxCluster / (drafts + 1)) return HA_EUNSUPPORTED;
-  *bytes = sequences * (drafts + 1) * static_cast<int64_t>(sizeof(Row));
+  if (drafts == 0x7FFFFFFF || sequences > 0x7FFFFFFF / kSumParts / (drafts + int64_t(1)) || sequences > 0x7FFFFFFF / kScoreParts)
+    return HA_EUNSUPPORTED;
+  *bytes = sequences * ((drafts + int64_t(1)) * kRowBytes + kSequenceBytes);
   return HA_OK;
 }
 
@@ -512,18 +608,23 @@ extern "C" int hier_avg_verify_drafts(const void* logits_dev, int type, int64_t 
   a.tokens = tokens_dev;
   a.accepted = accepted_dev;
   a.logp = logp_dev;
-  a.rows = static_cast<Row*>(workspace_dev);
   a.temperature = temperature;
   a.c = static_cast<float>(1.4426950408889634 / temperature);
   a.inv_t = static_cast<float>(1.0 / temperature);
   a.slack = slack(static_cast<int>(classes), 16 / type_size(type));
   a.K = drafts;
+  a.sequences = sequences;
+  const int64_t rows = sequences * (drafts + int64_t(1));
+  a.w.heads = static_cast<Head*>(workspace_dev);
+  a.w.bests = reinterpret_cast<Best*>(a.w.heads + rows);
+  a.w.sums = reinterpret_cast<Sum*>(a.w.bests + sequences * kScoreParts);
+  a.w.done = reinterpret_cast<int*>(a.w.sums + rows * kSumParts);
   a.classes = static_cast<int>(classes);
   a.wide_drafts = draft_bytes == 8;
   a.probs_type = probs_dev ? probs_type : -1;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = type == HA_TYPE_FP32   ? verify_type<float>(a, sequences, s)
-                        : type == HA_TYPE_BF16 ? verify_type<__nv_bfloat16>(a, sequences, s)
-                                               : verify_type<__half>(a, sequences, s);
+  const cudaError_t e = type == HA_TYPE_FP32   ? verify_type<float>(a, s)
+                        : type == HA_TYPE_BF16 ? verify_type<__nv_bfloat16>(a, s)
+                                               : verify_type<__half>(a, s);
   return e == cudaSuccess ? HA_OK : HA_ECUDA;
 }

@@ -612,8 +612,8 @@ def verify_drafts(logits: torch.Tensor, drafts: torch.Tensor, uniform: torch.Ten
         tokens = torch.empty((B, R), dtype=torch.int32, device=dev)
         accepted = torch.empty(B, dtype=torch.int32, device=dev)
         logp = torch.empty((B, R), dtype=torch.float32, device=dev)
-        n = 16 * B * R                                      # as hier_avg_verify_workspace says
-        ws = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
+        n = B * (272 * R + 2052)                            # as hier_avg_verify_workspace says
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
         check(lib.hier_avg_verify_drafts(
             logits.data_ptr(), TYPES[logits.dtype], B, K, V, *z, drafts.data_ptr(), drafts.element_size(), uniform.data_ptr(),
             noise.data_ptr(), noise_ld, None if draft_probs is None else draft_probs.data_ptr(),
