@@ -1,15 +1,19 @@
-"""Compile the CUDA C-ABI library ``libhier_avg.so`` in-tree for sm_103a.
+"""Compile the CUDA C-ABI library ``libhier_avg.so`` in-tree for sm_103a, and the Python
+binding's host module ``_host.so``.
 
 Each translation unit is compiled by nvcc in parallel, then linked with the
 static CUDA runtime into one shared library next to this file.  Arithmetic flags
 are explicit: no fast-math, IEEE division and square root, subnormals kept.
+The host module is compiled by g++ against PyTorch's headers, beside them.
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -18,6 +22,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libhier_avg.so")
+HOST_PATH = os.path.join(HERE, "_host.so")
 
 SOURCES = ["hier_avg_api.cu", "avg_kernels.cu", "step_tc.cu", "step_head.cu", "step_fp32.cu",
            "op_grouped.cu", "op_logprobs.cu", "op_adamw.cu", "op_route.cu", "op_rows.cu", "op_norm.cu",
@@ -42,6 +47,16 @@ def _run(cmd):
     return r.stdout
 
 
+def _host_command(out: str):
+    """g++ on csrc/host.cpp; the libraries are those that ``import torch`` has loaded."""
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    inc, lib = os.path.join(torch, "include"), os.path.join(torch, "lib")
+    return [os.environ.get("CXX") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-o", out,
+            os.path.join(CSRC, "host.cpp"), f"-I{sysconfig.get_paths()['include']}", f"-isystem{inc}",
+            f"-isystem{os.path.join(inc, 'torch', 'csrc', 'api', 'include')}", f"-L{lib}", "-ltorch_python",
+            "-ltorch_cpu", "-lc10"]
+
+
 def build(verbose: bool = False, ptxas_info: bool = False) -> str:
     nvcc = _nvcc()
     os.makedirs(BUILD_DIR, exist_ok=True)
@@ -53,6 +68,7 @@ def build(verbose: bool = False, ptxas_info: bool = False) -> str:
             cmd += ["-Xptxas", "-v"]
         objs.append(obj)
         cmds.append(cmd)
+    cmds.append(_host_command(HOST_PATH + ".tmp"))
     with ThreadPoolExecutor(max_workers=len(cmds)) as ex:
         outs = list(ex.map(_run, cmds))
     if verbose or ptxas_info:
@@ -60,6 +76,7 @@ def build(verbose: bool = False, ptxas_info: bool = False) -> str:
             sys.stdout.write(o)
     tmp = LIB_PATH + ".tmp"
     _run([nvcc, *ARCH, "-shared", "--cudart", "static", "-o", tmp, *objs])
+    os.replace(HOST_PATH + ".tmp", HOST_PATH)
     os.replace(tmp, LIB_PATH)
     return LIB_PATH
 

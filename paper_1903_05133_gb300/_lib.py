@@ -103,6 +103,21 @@ SIGNATURES = {
 }
 
 _lib = None
+_host = None
+
+
+def host():
+    """The module of csrc/host.cpp."""
+    global _host
+    if _host is None:
+        if not os.path.exists(_build.HOST_PATH):
+            raise RuntimeError(f"{_build.HOST_PATH} is missing: it is built with the CUDA library "
+                               "(paper_1903_05133_gb300._build.build()); there is no fallback")
+        import torch  # noqa: F401  (the libraries that it needs)
+
+        from . import _host as module
+        _host = module
+    return _host
 
 
 def load() -> ctypes.CDLL:

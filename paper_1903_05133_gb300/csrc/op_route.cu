@@ -106,11 +106,31 @@ struct RouteArgs {
   SortArgs sort;
 };
 
-// A warp takes a row; lane l holds the logits l, l + 32, ...
-template <typename T, int R, bool ONE>
+template <int L>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t x) {
+  if constexpr (L == 32) {
+    return __reduce_max_sync(~0u, x);
+  } else {
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) x = max(x, __shfl_xor_sync(~0u, x, o));
+    return x;
+  }
+}
+template <int L>
+__device__ __forceinline__ float lanes_sum(float x) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+  return x;
+}
+
+// L lanes take a row, at least as many as it has chosen ones; lane l of them holds the logits l, l + L, ...  The chosen
+// are taken one after the other, the largest of the lanes' largest, which is a chain of latencies: several rows a warp share it.
+template <typename T, int L, int R, bool ONE>
 __global__ void __launch_bounds__(32 * (ONE ? kOneRouteWarps<R> : kWarps)) k_route(const __grid_constant__ RouteArgs a) {
   extern __shared__ int dyn[];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  constexpr int kRows = 32 / L;                               // of a warp at a time
+  constexpr uint32_t kLanes = L == 32 ? ~0u : (1u << L) - 1;
+  const int lane = threadIdx.x & 31, l = lane % L, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   const int G = a.sort.groups, k = a.k;
   int* hist = dyn;                                            // [warps, groups]
   int* total = hist + warps * G;                              // [groups + 1] (ONE)
@@ -121,7 +141,9 @@ __global__ void __launch_bounds__(32 * (ONE ? kOneRouteWarps<R> : kWarps)) k_rou
   for (int i = threadIdx.x; i < warps * G; i += blockDim.x) hist[i] = 0;
   __syncthreads();
 
-  const int each = (n_rows + warps - 1) / warps, first = min(warp * each, n_rows), last = min(first + each, n_rows);
+  // a multiple of kRows for every warp but the last, so that none is idle beside another's rows
+  const int each = ((n_rows + warps - 1) / warps + kRows - 1) / kRows * kRows;
+  const int first = min(warp * each, n_rows), last = min(first + each, n_rows);
   int learner = 0;
   if (a.learners && first < last) {                           // learners that end at or before the warp's first row
     int high = a.n_learners;
@@ -131,15 +153,14 @@ __global__ void __launch_bounds__(32 * (ONE ? kOneRouteWarps<R> : kWarps)) k_rou
       else high = mid;
     }
   }
-  for (int r = first; r < last; ++r) {
-    const int64_t row = r0 + r;
+  for (int r1 = first; r1 < last; r1 += kRows) {
+    const int r = r1 + lane / L;
+    const bool mine = r < last;
+    const int64_t row = r0 + (mine ? r : r1);                 // lanes without a row repeat the first's
     const T* z = static_cast<const T*>(a.logits) + row * a.ld;
     float v[R];
 #pragma unroll
-    for (int u = 0; u < R; ++u) {
-      const int i = u * 32 + lane;
-      v[u] = i < a.experts ? Elem<T>::up(z[i]) : -INFINITY;
-    }
+    for (int u = 0; u < R; ++u) v[u] = u * L + l < a.experts ? Elem<T>::up(z[u * L + l]) : -INFINITY;
     bool bad = false;                                         // NaN or infinity among them
     uint32_t key[R], most = 0;                                // 0: masked
     int at = 0;
@@ -158,65 +179,74 @@ __global__ void __launch_bounds__(32 * (ONE ? kOneRouteWarps<R> : kWarps)) k_rou
         }
     };
     look();
-    bad = __any_sync(~0u, bad);
-    const uint32_t top = __reduce_max_sync(~0u, most);
+    bad = (__ballot_sync(~0u, bad) >> (lane - l) & kLanes) != 0;
+    const uint32_t top = lanes_max<L>(most);
     const float m = from_ordered(top);
     float S = 0.0f;
 #pragma unroll
     for (int u = 0; u < R; ++u)
       if (key[u]) S += exp2_fast((v[u] - m) * kLog2e);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(~0u, S, o);
+    S = lanes_sum<L>(S);
 
-    uint32_t mine = 0;
+    uint32_t mine_key = 0;
     int index = -1;
     for (int j = 0; j < k; ++j) {
-      const uint32_t best = __reduce_max_sync(~0u, most);
-      if (best == 0 || bad) break;
-      const uint32_t lanes = __ballot_sync(~0u, most == best);
+      const uint32_t best = j == 0 ? top : lanes_max<L>(most);
+      if (L == 32 && best == 0) break;
+      const uint32_t lanes = __ballot_sync(~0u, most == best && best != 0) >> (lane - l) & kLanes;
       int src = __ffs(lanes) - 1;
-      if (lanes & (lanes - 1))                                // equal logits of two lanes
-        src = __reduce_min_sync(~0u, most == best ? static_cast<uint32_t>(at * 32 + lane) : ~0u) & 31;
-      const int i = __shfl_sync(~0u, at, src) * 32 + src;
-      if (lane == j) {
-        mine = best;
+      if (__any_sync(~0u, lanes & (lanes - 1))) {             // equal logits of two lanes: the lowest index
+        const uint32_t i = most == best ? static_cast<uint32_t>(at * L + l) : ~0u;
+        src = static_cast<int>(~lanes_max<L>(~i)) % L;
+      }
+      const int i = __shfl_sync(~0u, at, src & (L - 1), L) * L + src;
+      if (best == 0) continue;                                // of this row; others' lanes go on
+      if (l == j) {
+        mine_key = best;
         index = i;
       }
-      if (lane == src) {
+      if (l == src) {
 #pragma unroll
         for (int u = 0; u < R; ++u)
           if (u == at) key[u] = 0;
         look();
       }
     }
-    const float e = index >= 0 ? expf(from_ordered(mine) - m) : 0.0f;
-    float sum = S;
-    if (!a.all) {
-      sum = e;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+    if (bad) index = -1;
+    const float e = index >= 0 ? expf(from_ordered(mine_key) - m) : 0.0f;
+    const float sum = a.all ? S : lanes_sum<L>(e);
+    if (mine && l < k) {
+      a.expert[row * k + l] = index;
+      a.weight[row * k + l] = bad ? NAN : index >= 0 ? e / sum : 0.0f;
     }
-    if (lane < k) {
-      a.expert[row * k + lane] = index;
-      a.weight[row * k + lane] = bad ? NAN : index >= 0 ? e / sum : 0.0f;
-    }
-    if (lane == 0) a.lse[row] = bad ? NAN : top == 0 ? -INFINITY : m + logf(S);
+    if (mine && l == 0) a.lse[row] = bad ? NAN : top == 0 ? -INFINITY : m + logf(S);
 
-    int group = index;
+    int group = mine && l < k ? index : -1;
     if (a.learners) {
-      while (learner < a.n_learners && a.learners[learner + 1] <= row) ++learner;
-      if (learner >= a.n_learners || row < a.learners[learner]) group = -1;
-      else if (index >= 0) group = learner * a.experts + index;
+      int p = learner;
+      while (p < a.n_learners && a.learners[p + 1] <= row) ++p;
+      if (p >= a.n_learners || row < a.learners[p]) group = -1;
+      else if (group >= 0) group += p * a.experts;
+      learner = __shfl_sync(~0u, p, 0);                       // the first row's is not behind the others'
     }
-    if (lane < k) {
-      int packed = -1;
-      if (group >= 0) {
-        const int rank = hist[warp * G + group];              // a row's experts differ
+    int packed = -1;
+    if constexpr (kRows == 1) {
+      if (group >= 0) {                                       // a row's experts differ
+        const int rank = hist[warp * G + group];
         hist[warp * G + group] = rank + 1;
         packed = group << kRankBits | rank;
       }
-      stage[r * k + lane] = packed;
+    } else {
+      const uint32_t same = __match_any_sync(~0u, group);
+      int rank = 0;
+      if (group >= 0) {
+        rank = hist[warp * G + group];
+        packed = group << kRankBits | (rank + __popc(same & ((1u << lane) - 1)));
+      }
+      __syncwarp();
+      if (group >= 0 && lane == __ffs(same) - 1) hist[warp * G + group] = rank + __popc(same);
     }
+    if (mine && l < k) stage[r * k + l] = packed;
     __syncwarp();
   }
   end_chunk<ONE>(a.sort, hist, total, stage, r0 * k, n_rows * k);
@@ -354,35 +384,50 @@ struct RouteBwdArgs {
   bool all;
 };
 
-// A warp a row.  The chosen ones' lanes write theirs after the row's others.
-template <typename T, bool ALL>
+// L lanes a row, at least as many as it has chosen ones, whose lanes write theirs after the row's others.  R of a lane's
+// logits are loaded before the first use.
+template <typename T, int L, bool ALL>
 __global__ void __launch_bounds__(kWarps * 32) k_route_backward(const __grid_constant__ RouteBwdArgs a) {
-  const int lane = threadIdx.x & 31;
-  const int64_t step = static_cast<int64_t>(gridDim.x) * kWarps;
-  for (int64_t row = blockIdx.x * static_cast<int64_t>(kWarps) + (threadIdx.x >> 5); row < a.rows; row += step) {
+  constexpr int R = 8;
+  const int lane = threadIdx.x & 31, l = lane % L;
+  constexpr uint32_t kLanes = L == 32 ? ~0u : (1u << L) - 1;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kWarps * (32 / L);
+  for (int64_t r0 = (blockIdx.x * static_cast<int64_t>(kWarps) + (threadIdx.x >> 5)) * (32 / L); r0 < a.rows; r0 += step) {
+    const bool mine = r0 + lane / L < a.rows;
+    const int64_t row = mine ? r0 + lane / L : r0;           // lanes without a row repeat the first's
     const T* z = ALL ? static_cast<const T*>(a.logits) + row * a.ld : nullptr;
     T* out = static_cast<T*>(a.out) + row * a.out_ld;
     int i = -1;
-    float w = 0.0f, g = 0.0f;
-    bool bad = false;
-    if (lane < a.k) {
-      i = a.expert[row * a.k + lane];
-      w = a.weight[row * a.k + lane];
-      bad = w != w;
-      if (i < 0 || i >= a.experts) i = -1;
-      else g = w * a.dweight[row * a.k + lane];
+    float w = 0.0f, dw = 0.0f, lse = 0.0f;
+    if (l < a.k) {
+      i = a.expert[row * a.k + l];
+      w = a.weight[row * a.k + l];
+      dw = a.dweight[row * a.k + l];
     }
-    bad = __any_sync(~0u, bad);
-    float s = g;
+    T x[R];
+    if constexpr (ALL) {
+      lse = a.lse[row];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
+      for (int u = 0; u < R; ++u)
+        if (u * L + l < a.experts) x[u] = z[u * L + l];
+    }
+    if (i < 0 || i >= a.experts) i = -1;
+    float zi = -INFINITY;
+    if (ALL && i >= 0) zi = Elem<T>::up(z[i]);
+    const bool bad = (__ballot_sync(~0u, w != w) >> (lane - l) & kLanes) != 0;
+    float g = i >= 0 ? w * dw : 0.0f;
+    const float s = lanes_sum<L>(g);
     // an expert that is named twice has the sum of both
-    const uint32_t same = __match_any_sync(~0u, i < 0 ? -1 - lane : i);
-    if (__any_sync(~0u, i >= 0 && (same & (same - 1)))) {
+    int before = 0;
+    for (int j = 0; j < a.k; ++j) {
+      const int other = __shfl_sync(~0u, i, j, L);           // by all lanes
+      before += j < l && other == i;
+    }
+    if (__any_sync(~0u, i >= 0 && before)) {
       float g2 = 0.0f, w2 = 0.0f;
       for (int j = 0; j < a.k; ++j) {
-        const float gj = __shfl_sync(~0u, g, j), wj = __shfl_sync(~0u, w, j);
-        if (same >> j & 1u) {
+        const float gj = __shfl_sync(~0u, g, j, L), wj = __shfl_sync(~0u, w, j, L);
+        if (__shfl_sync(~0u, i, j, L) == i) {
           g2 += gj;
           w2 += wj;
         }
@@ -391,20 +436,25 @@ __global__ void __launch_bounds__(kWarps * 32) k_route_backward(const __grid_con
       w = w2;
     }
     if constexpr (ALL) {
-      const float lse0 = a.lse[row], lse = lse0 == -INFINITY ? INFINITY : lse0;
-      const float zi = i >= 0 ? Elem<T>::up(z[i]) : 0.0f;
-      __syncwarp();                                           // out may be the logits themselves
-      auto p = [&](float x) { return x > kNone<T> ? exp2_fast((x - lse) * kLog2e) : x == x ? 0.0f : x; };
-      for (int j = lane; j < a.experts; j += 32) {
-        const float x = Elem<T>::up(z[j]);
-        out[j] = Elem<T>::down(bad ? NAN : -p(x) * s);
+      if (lse == -INFINITY) lse = INFINITY;                  // nothing allowed: every p is 0
+      auto p = [&](float v) { return v > kNone<T> ? exp2_fast((v - lse) * kLog2e) : v == v ? 0.0f : v; };
+      for (int j0 = 0; j0 < a.experts; j0 += R * L) {
+        if (j0 > 0) {
+#pragma unroll
+          for (int u = 0; u < R; ++u)
+            if (j0 + u * L + l < a.experts) x[u] = z[j0 + u * L + l];
+        }
+#pragma unroll
+        for (int u = 0; u < R; ++u)
+          if (j0 + u * L + l < a.experts && mine) out[j0 + u * L + l] = Elem<T>::down(bad ? NAN : -p(Elem<T>::up(x[u])) * s);
       }
       __syncwarp();
-      if (i >= 0) out[i] = Elem<T>::down(bad ? NAN : fmaf(-p(zi), s, g));
+      if (i >= 0 && mine) out[i] = Elem<T>::down(bad ? NAN : fmaf(-p(zi), s, g));
     } else {
-      for (int j = lane; j < a.experts; j += 32) out[j] = Elem<T>::down(bad ? NAN : 0.0f);
+      if (mine)
+        for (int j = l; j < a.experts; j += L) out[j] = Elem<T>::down(bad ? NAN : 0.0f);
       __syncwarp();
-      if (i >= 0) out[i] = Elem<T>::down(bad ? NAN : fmaf(-w, s, g));
+      if (i >= 0 && mine) out[i] = Elem<T>::down(bad ? NAN : fmaf(-w, s, g));
     }
   }
 }
@@ -433,34 +483,46 @@ cudaError_t end_sort(const SortArgs& a, cudaStream_t s) {
   return launch_early(k_place, static_cast<unsigned>(a.chunks), kWarps * 32, 0, s, a);
 }
 
-template <typename T, int R>
-cudaError_t route_rows(RouteArgs a, bool one, cudaStream_t s) {
-  static bool one_ok[kMaxDevices], ok[kMaxDevices];
-  const int warps = one ? static_cast<int>(std::min<int64_t>(a.rows, kOneRouteWarps<R>)) : kWarps;
+template <typename T, int L, int R, bool ONE>
+cudaError_t route_rows(const RouteArgs& a, cudaStream_t s) {
+  static bool ok[kMaxDevices];
+  const int warps = ONE ? static_cast<int>(std::min<int64_t>(a.rows, kOneRouteWarps<R>)) : kWarps;
   const size_t smem = sort_smem(warps, a.sort.groups, a.sort.per);
-  const auto kernel = one ? k_route<T, R, true> : k_route<T, R, false>;
-  cudaError_t e = allow_smem(kernel, 200 << 10, one ? one_ok : ok);
+  const auto kernel = k_route<T, L, R, ONE>;
+  cudaError_t e = allow_smem(kernel, 200 << 10, ok);
   if (e != cudaSuccess) return e;
   kernel<<<static_cast<unsigned>(a.sort.chunks), warps * 32, smem, s>>>(a);
-  if ((e = cudaGetLastError()) != cudaSuccess || one) return e;
+  if ((e = cudaGetLastError()) != cudaSuccess || ONE) return e;
   return end_sort(a.sort, s);
 }
 
 template <typename T>
 cudaError_t route_type(const RouteArgs& a, bool one, cudaStream_t s) {
-  if (a.experts <= 64) return route_rows<T, 2>(a, one, s);
-  if (a.experts <= 128) return route_rows<T, 4>(a, one, s);
-  if (a.experts <= 256) return route_rows<T, 8>(a, one, s);
-  if (a.experts <= 512) return route_rows<T, 16>(a, one, s);
-  return route_rows<T, 32>(a, one, s);
+  if (one) {                                                  // a warp a row: few rows, whose latency counts
+    if (a.experts <= 64) return route_rows<T, 32, 2, true>(a, s);
+    if (a.experts <= 256) return route_rows<T, 32, 8, true>(a, s);
+    return route_rows<T, 32, 32, true>(a, s);
+  }
+  if (a.k <= 8 && a.experts <= 64) return route_rows<T, 8, 8, false>(a, s);
+  if (a.k <= 8 && a.experts <= 128) return route_rows<T, 8, 16, false>(a, s);
+  if (a.k <= 16 && a.experts <= 256) return route_rows<T, 16, 16, false>(a, s);
+  if (a.experts <= 128) return route_rows<T, 32, 4, false>(a, s);
+  if (a.experts <= 512) return route_rows<T, 32, 16, false>(a, s);
+  return route_rows<T, 32, 32, false>(a, s);
 }
 
-template <typename T>
-cudaError_t backward_type(const RouteBwdArgs& a, cudaStream_t s) {
-  const int64_t ctas = std::min<int64_t>((a.rows + kWarps - 1) / kWarps, 152 * 8 * 8);
-  const auto kernel = a.all ? k_route_backward<T, true> : k_route_backward<T, false>;
+template <typename T, int L>
+cudaError_t backward_rows(const RouteBwdArgs& a, cudaStream_t s) {
+  const int64_t per = kWarps * (32 / L), ctas = std::min<int64_t>((a.rows + per - 1) / per, 152 * 8 * 8);
+  const auto kernel = a.all ? k_route_backward<T, L, true> : k_route_backward<T, L, false>;
   kernel<<<static_cast<unsigned>(ctas), kWarps * 32, 0, s>>>(a);
   return cudaGetLastError();
+}
+template <typename T>
+cudaError_t backward_type(const RouteBwdArgs& a, cudaStream_t s) {
+  if (a.k <= 8 && a.experts <= 128) return backward_rows<T, 8>(a, s);
+  if (a.k <= 16 && a.experts <= 256) return backward_rows<T, 16>(a, s);
+  return backward_rows<T, 32>(a, s);
 }
 
 bool misaligned(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }

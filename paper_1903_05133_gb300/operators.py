@@ -24,10 +24,10 @@ from . import _lib
 from ._lib import c_int64, c_void_p, check
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_F32, _I32, _U8 = 0, 3, 4       # of results made together
 FORWARD, DX, DW = 0, 1, 2
 _KIND = attrgetter("dtype", "shape")
 _ADDRESS, _CONTIGUOUS, _DEVICE = torch.Tensor.data_ptr, torch.Tensor.is_contiguous, torch.Tensor.get_device
-_DTYPE, _NUMEL = attrgetter("dtype"), torch.Tensor.numel
 BLOCK = 256                     # elements that share a scale of the 8-bit AdamW states
 MAX_TOP = 32
 
@@ -49,6 +49,15 @@ def _on(stream, t, *others):
     if stream.device_index != d:
         raise ValueError("stream must be of the tensors' GPU")
     return stream.cuda_stream, torch.cuda.stream(stream)
+
+
+def _empties(like, *specs):
+    """New tensors on like's GPU of (type, size, ...) each, in one call (1.6 us each otherwise)."""
+    return _lib.host().empties(like, *specs)
+
+
+def _empty(like, rows, cols, dtype):
+    return _empties(like, (TYPES[dtype], rows, cols))[0]
 
 
 def _need(ok: bool, message: str) -> None:
@@ -381,13 +390,12 @@ def _vector(name, t, dtype, shape):
         raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor {list(shape)}")
 
 
-def _sort_workspace(lib, rows, k, groups, device):
+def _sort_bytes(lib, rows, k, groups):
     if rows <= _ONE_ROWS and rows * k <= _ONE_ENTRIES:      # one CTA sorts them: none, as the library says
-        return None, None, 0
+        return 0
     n = c_int64()
     check(lib.hier_avg_sort_workspace(rows, k, groups, ctypes.byref(n)), "sort_workspace")
-    ws = torch.empty(n.value, dtype=torch.uint8, device=device)
-    return ws, ws.data_ptr(), n.value
+    return n.value
 
 
 def _over(over):
@@ -413,18 +421,13 @@ def route(logits: torch.Tensor, k: int, over: str = "chosen", learners: Optional
     every = _over(over)
     s, where = _on(stream, logits, learners)
     with where:
-        dev = logits.device
-        experts = torch.empty((T, k), dtype=torch.int32, device=dev)
-        weights = torch.empty((T, k), dtype=torch.float32, device=dev)
-        lse = torch.empty(T, dtype=torch.float32, device=dev)
-        offsets = torch.empty(G + 1, dtype=torch.int32, device=dev)
-        place = torch.empty((T, k), dtype=torch.int32, device=dev)
-        source = torch.empty(T * k, dtype=torch.int32, device=dev)
-        ws, p, n = _sort_workspace(lib, T, k, G, dev)
+        n = _sort_bytes(lib, T, k, G)
+        experts, weights, lse, offsets, place, source, ws = _empties(
+            logits, (_I32, T, k), (_F32, T, k), (_F32, T), (_I32, G + 1), (_I32, T, k), (_I32, T * k), (_U8, n))
         check(lib.hier_avg_route(
             logits.data_ptr(), TYPES[logits.dtype], T, E, ld, k, every, None if learners is None else learners.data_ptr(), P,
             experts.data_ptr(), weights.data_ptr(), lse.data_ptr(), offsets.data_ptr(), place.data_ptr(),
-            source.data_ptr(), p, n, s), "route")
+            source.data_ptr(), ws.data_ptr(), n, s), "route")
     return Routing(experts, weights, lse, offsets, place, source)
 
 
@@ -449,8 +452,7 @@ def route_backward(dweights: torch.Tensor, logits: torch.Tensor, experts: torch.
     _apart(out, dweights, logits, experts, weights, lse, same=logits)
     s, where = _on(stream, logits, dweights, experts, weights, lse, out)
     with where:
-        d = torch.empty((T, E), dtype=logits.dtype, device=logits.device) if out is None else \
-            _given(out, (T, E), logits.dtype)
+        d = _empty(logits, T, E, logits.dtype) if out is None else _given(out, (T, E), logits.dtype)
         check(lib.hier_avg_route_backward(
             dweights.data_ptr(), logits.data_ptr(), TYPES[logits.dtype], T, E, ld, k, every, experts.data_ptr(),
             weights.data_ptr(), None if lse is None else lse.data_ptr(), d.data_ptr(), E if out is None else _ld(d), s),
@@ -469,13 +471,10 @@ def sort_by_group(group: torch.Tensor, groups: int, stream=None) -> Sorted:
     _need(1 <= groups <= MAX_GROUPS, f"groups must be in [1, {MAX_GROUPS}]")
     s, where = _on(stream, group)
     with where:
-        dev = group.device
-        offsets = torch.empty(groups + 1, dtype=torch.int32, device=dev)
-        place = torch.empty((T, k), dtype=torch.int32, device=dev)
-        source = torch.empty(T * k, dtype=torch.int32, device=dev)
-        ws, p, n = _sort_workspace(lib, T, k, groups, dev)
+        n = _sort_bytes(lib, T, k, groups)
+        offsets, place, source, ws = _empties(group, (_I32, groups + 1), (_I32, T, k), (_I32, T * k), (_U8, n))
         check(lib.hier_avg_sort_by_group(group.data_ptr(), T, k, groups, offsets.data_ptr(), place.data_ptr(),
-                                         source.data_ptr(), p, n, s), "sort_by_group")
+                                         source.data_ptr(), ws.data_ptr(), n, s), "sort_by_group")
     return Sorted(offsets, place, source)
 
 
@@ -501,7 +500,7 @@ def dispatch(x: torch.Tensor, place: torch.Tensor, offsets: torch.Tensor, out: O
     _apart(out, x, place, offsets)
     s, where = _on(stream, x, place, offsets, out)
     with where:
-        xs = torch.empty((T * k, D), dtype=x.dtype, device=x.device) if out is None else _given(out, (T * k, D), x.dtype)
+        xs = _empty(x, T * k, D, x.dtype) if out is None else _given(out, (T * k, D), x.dtype)
         check(lib.hier_avg_dispatch(x.data_ptr(), TYPES[x.dtype], T, D, ld, place.data_ptr(), k, offsets.data_ptr(), G,
                                     xs.data_ptr(), D if out is None else _ld(xs), s), "dispatch")
     return xs
@@ -518,7 +517,7 @@ def _combine(name, y, place, weights, out, out_dtype, stream):
     _apart(out, y, place, weights)
     s, where = _on(stream, y, place, weights, out)
     with where:
-        o = torch.empty((T, D), dtype=d, device=y.device) if out is None else _given(out, (T, D), d)
+        o = _empty(y, T, D, d) if out is None else _given(out, (T, D), d)
         check(lib.hier_avg_combine(y.data_ptr(), TYPES[y.dtype], T, D, ld, place.data_ptr(), k,
                                    None if weights is None else weights.data_ptr(), o.data_ptr(),
                                    D if out is None else _ld(o), TYPES[d], s), "combine")
@@ -553,8 +552,10 @@ def combine_backward(dout: torch.Tensor, y: torch.Tensor, place: torch.Tensor, w
     _apart(out, dout, y, place, weights, offsets)
     s, where = _on(stream, y, dout, place, weights, offsets, out)
     with where:
-        dy = torch.empty((T * k, D), dtype=kind, device=y.device) if out is None else _given(out, (T * k, D), kind)
-        dw = torch.empty((T, k), dtype=torch.float32, device=y.device)
+        if out is None:
+            dy, dw = _empties(y, (TYPES[kind], T * k, D), (_F32, T, k))
+        else:
+            dy, dw = _given(out, (T * k, D), kind), _empty(y, T, k, torch.float32)
         check(lib.hier_avg_combine_backward(
             dout.data_ptr(), TYPES[dout.dtype], dout_ld, y.data_ptr(), TYPES[kind], T, D, ld, place.data_ptr(), k,
             weights.data_ptr(), offsets.data_ptr(), G, dy.data_ptr(), D if out is None else _ld(dy), dw.data_ptr(), s),
@@ -608,12 +609,8 @@ def verify_drafts(logits: torch.Tensor, drafts: torch.Tensor, uniform: torch.Ten
         ok = _three("allowed", allowed, (torch.bool, torch.uint8), (B, R, V))
     s, where = _on(stream, logits, drafts, uniform, noise, draft_probs, allowed)
     with where:
-        dev = logits.device
-        tokens = torch.empty((B, R), dtype=torch.int32, device=dev)
-        accepted = torch.empty(B, dtype=torch.int32, device=dev)
-        logp = torch.empty((B, R), dtype=torch.float32, device=dev)
         n = B * (272 * R + 2052)                            # as hier_avg_verify_workspace says
-        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+        tokens, accepted, logp, ws = _empties(logits, (_I32, B, R), (_I32, B), (_F32, B, R), (_U8, n))
         check(lib.hier_avg_verify_drafts(
             logits.data_ptr(), TYPES[logits.dtype], B, K, V, *z, drafts.data_ptr(), drafts.element_size(), uniform.data_ptr(),
             noise.data_ptr(), noise_ld, None if draft_probs is None else draft_probs.data_ptr(),
@@ -630,32 +627,25 @@ class GradNorm(NamedTuple):
 
 def _norm(grads, max_norm, learners, clip, stream):
     lib = _lib.load()
-    # each check runs over all tensors at once: a call over hundreds of them is host work
     n = len(grads)
     _need(n >= 1, "grads must not be empty")
-    kinds = list(map(_DTYPE, grads))
-    devices = set(map(_DEVICE, grads))
-    if not (set(kinds) <= TYPES.keys() and min(devices) >= 0 and all(map(_CONTIGUOUS, grads))):
+    address, types, sizes, d = _lib.host().facts(grads)
+    _need(d != -2, "all tensors of a call must be on one GPU")
+    if d < 0:
         raise ValueError("grads must be contiguous CUDA tensors of fp32, bf16 or fp16")
-    _need(len(devices) == 1, "all tensors of a call must be on one GPU")
     P = 1
     if learners is not None:
         P = learners
         _need(P >= 1 and all(g.dim() >= 1 and g.shape[0] == P for g in grads), "the gradients' first dimension must be the learners'")
     _need(max_norm is None or 0 <= max_norm < float("inf"), "max_norm must be finite and not negative")
-    address = array("Q", map(_ADDRESS, grads))
-    types = array("i", map(TYPES.__getitem__, kinds))
-    sizes = array("q", map(_NUMEL, grads))
-    t, z = types.buffer_info()[0], sizes.buffer_info()[0]
+    b = c_int64()
+    check(lib.hier_avg_grad_norm_workspace(n, types, sizes, P, ctypes.byref(b)), "grad_norm_workspace")
     s, where = _on(stream, grads[0])
     with where:
-        dev = grads[0].device
-        norm = torch.empty(P, dtype=torch.float32, device=dev)
-        scale = None if max_norm is None else torch.empty(P, dtype=torch.float32, device=dev)
-        b = c_int64()
-        check(lib.hier_avg_grad_norm_workspace(n, t, z, P, ctypes.byref(b)), "grad_norm_workspace")
-        ws = torch.empty(b.value, dtype=torch.uint8, device=dev)
-        status = lib.hier_avg_grad_norm(n, address.buffer_info()[0], t, z, P, 0.0 if max_norm is None else max_norm, clip,
+        norm, scale, ws = _empties(grads[0], (_F32, P), (_F32, P), (_U8, b.value))
+        if max_norm is None:
+            scale = None
+        status = lib.hier_avg_grad_norm(n, address, types, sizes, P, 0.0 if max_norm is None else max_norm, clip,
                                         norm.data_ptr(), None if scale is None else scale.data_ptr(), ws.data_ptr(), b.value, s)
         _need(not (clip and status == -1), "gradients that are clipped must not share memory")
         check(status, "clip_gradients" if clip else "grad_norm")
