@@ -16,7 +16,7 @@ constexpr at::ScalarType kTypes[] = {at::kFloat, at::kBFloat16, at::kHalf, at::k
 
 // Results of a call that are small together are parts of one allocation, each from a multiple of 256 bytes on: an
 // allocation takes 0.9 us, a tensor on another's memory 0.3.  (They belong together, and live as long as any of them.)
-constexpr int64_t kShared = 256 << 10, kApart = 256;
+constexpr int64_t kShared = 4 << 20, kApart = 256;
 
 // empties(like, (type, size, ...), ...) -> a tuple of new tensors on like's device.
 PyObject* empties(PyObject*, PyObject* const* args, Py_ssize_t n) {

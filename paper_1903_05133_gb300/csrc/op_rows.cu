@@ -99,7 +99,7 @@ struct Item {
 };
 __device__ __forceinline__ Item item_of(const RowArgs& a) {
   const int64_t at = blockIdx.x * static_cast<int64_t>(kThreads);
-  if (a.tokens * a.lanes <= 0x7FFFFFFF - kThreads) {        // a division of 32 bits
+  if (a.entries * a.lanes <= 0x7FFFFFFF - kThreads) {       // a division of 32 bits
     const int i = static_cast<int>(at) + static_cast<int>(threadIdx.x);
     return {i / a.lanes, i % a.lanes};
   }
@@ -195,24 +195,35 @@ __global__ void __launch_bounds__(kThreads, 4) k_combine(const __grid_constant__
                   [&](int c) { combine_at<T, O, 1, 1, AT, WEIGHTS>(a, it.token, c, a.width); });
 }
 
-// A CTA a token (or a warp, a.lanes = 32): the weights' gradients are sums over the whole row.
+// The sum over a group of lanes, a power of two; a CTA's over each of its warps.
+__device__ __forceinline__ float lanes_sum(float x, int lanes) {
+  if (lanes >= 32) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+  } else {
+    for (int o = lanes / 2; o > 0; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+  }
+  return x;
+}
+
+// A CTA, a warp or some lanes a token, a power of two: the weights' gradients are sums over the whole row.
 template <typename T, typename O, int V, int U, int AT>
-__device__ __forceinline__ void combine_backward_at(const RowArgs& a, int64_t token, int i, int parts, const int64_t* p,
+__device__ __forceinline__ void combine_backward_at(const RowArgs& a, int64_t token, int i, int parts, int lanes, const int64_t* p,
                                                     const float* w, float* dot) {
   Part<O, V> d[U];
   Part<T, V> y[AT][U];
   const O* from = static_cast<const O*>(a.token) + token * a.token_ld;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (i + u * a.lanes < parts) d[u].load(from + (i + u * a.lanes) * V);
+    if (i + u * lanes < parts) d[u].load(from + (i + u * lanes) * V);
     else d[u].clear();
   }
 #pragma unroll
   for (int q = 0; q < AT; ++q)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (p[q] >= 0 && i + u * a.lanes < parts)
-        y[q][u].load(static_cast<const T*>(a.sorted) + p[q] * a.sorted_ld + (i + u * a.lanes) * V);
+      if (p[q] >= 0 && i + u * lanes < parts)
+        y[q][u].load(static_cast<const T*>(a.sorted) + p[q] * a.sorted_ld + (i + u * lanes) * V);
       else
         y[q][u].clear();
     }
@@ -230,22 +241,22 @@ __device__ __forceinline__ void combine_backward_at(const RowArgs& a, int64_t to
         dot[q] = fmaf(dv[e], v[e], dot[q]);
         v[e] = w[q] * dv[e];
       }
-      if (i + u * a.lanes < parts) {
+      if (i + u * lanes < parts) {
         Part<T, V> dy;
         dy.down(v);
-        dy.store(static_cast<T*>(a.out_sorted) + p[q] * a.out_sorted_ld + (i + u * a.lanes) * V);
+        dy.store(static_cast<T*>(a.out_sorted) + p[q] * a.out_sorted_ld + (i + u * lanes) * V);
       }
     }
   }
 }
-template <typename T, typename O, int V, int U, int AT>
+template <typename T, typename O, int V, int U, int AT, bool CTA>
 __global__ void __launch_bounds__(kThreads) k_combine_backward(const __grid_constant__ RowArgs a) {
   __shared__ float part[kThreads / 32][AT];
-  const bool cta = a.lanes == kThreads;
-  const int64_t token = cta ? blockIdx.x : blockIdx.x * static_cast<int64_t>(kThreads / 32) + threadIdx.x / 32;
-  const int first = threadIdx.x % a.lanes;
-  if (token >= a.tokens) return;                            // whole warps, or whole CTAs
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lanes = CTA ? kThreads : a.lanes;
+  const Item it = CTA ? Item{blockIdx.x, static_cast<int>(threadIdx.x)} : item_of(a);
+  const bool mine = CTA || it.token < a.tokens;             // all take part in the sums
+  const int64_t token = mine ? it.token : 0;
+  const int first = it.first, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t count = *a.count;
   for (int j0 = 0; j0 < a.k; j0 += AT) {
     int64_t p[AT];
@@ -253,19 +264,16 @@ __global__ void __launch_bounds__(kThreads) k_combine_backward(const __grid_cons
 #pragma unroll
     for (int q = 0; q < AT; ++q) {
       const int64_t e = token * a.k + j0 + q;
-      p[q] = j0 + q < a.k ? place_of(a, e) : -1;
+      p[q] = mine && j0 + q < a.k ? place_of(a, e) : -1;
       w[q] = j0 + q < a.k ? a.weight[e] : 0.0f;
       dot[q] = 0.0f;
     }
-    each_part<V, U>(first, a.lanes, a.width,
-                    [&](int i) { combine_backward_at<T, O, V, U, AT>(a, token, i, a.width / V, p, w, dot); },
-                    [&](int c) { combine_backward_at<T, O, 1, 1, AT>(a, token, c, a.width, p, w, dot); });
+    if (mine) each_part<V, U>(first, lanes, a.width,
+                    [&](int i) { combine_backward_at<T, O, V, U, AT>(a, token, i, a.width / V, lanes, p, w, dot); },
+                    [&](int c) { combine_backward_at<T, O, 1, 1, AT>(a, token, c, a.width, lanes, p, w, dot); });
 #pragma unroll
-    for (int q = 0; q < AT; ++q) {
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) dot[q] += __shfl_xor_sync(~0u, dot[q], o);
-    }
-    if (cta) {
+    for (int q = 0; q < AT; ++q) dot[q] = lanes_sum(dot[q], lanes);
+    if (CTA) {
       if (lane == 0) {
 #pragma unroll
         for (int q = 0; q < AT; ++q) part[warp][q] = dot[q];
@@ -277,16 +285,16 @@ __global__ void __launch_bounds__(kThreads) k_combine_backward(const __grid_cons
         a.dweight[token * a.k + j0 + threadIdx.x] = s;
       }
       __syncthreads();
-    } else if (lane == 0) {
+    } else if (first == 0 && mine) {
 #pragma unroll
       for (int q = 0; q < AT; ++q)
         if (j0 + q < a.k) a.dweight[token * a.k + j0 + q] = dot[q];
     }
   }
   // the rows that no entry has
-  for (int64_t e = max(count, token * a.k); e < (token + 1) * a.k; ++e) {
+  for (int64_t e = max(count, token * a.k); mine && e < (token + 1) * a.k; ++e) {
     T* dy = static_cast<T*>(a.out_sorted) + e * a.out_sorted_ld;
-    each_part<V, 1>(first, a.lanes, a.width, [&](int i) {
+    each_part<V, 1>(first, lanes, a.width, [&](int i) {
       Part<T, V> none;
       none.clear();
       none.store(dy + i * V);
@@ -294,16 +302,235 @@ __global__ void __launch_bounds__(kThreads) k_combine_backward(const __grid_cons
   }
 }
 
+// ---------------------------------------------------------------- rows that are not aligned
+// 16 bytes from any element on: the two aligned 16 bytes around them, shifted.  The second ones are a neighbour's first, so
+// that they come from L1.  What is read beside the element's own bytes is the rows' too: see Aligned::inside.
+template <typename T> struct Shifted {
+  uint4 a, b;
+  uint32_t shift;                         // bytes
+  __device__ __forceinline__ void load(const T* p) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    shift = static_cast<uint32_t>(at & 15);
+    const uint4* q = reinterpret_cast<const uint4*>(at - shift);
+    a = q[0];
+    b = q[1];
+  }
+  __device__ __forceinline__ void clear() {
+    a = b = make_uint4(0, 0, 0, 0);
+    shift = 0;
+  }
+  __device__ __forceinline__ uint4 get() const {
+    const bool two = shift & 8, one = shift & 4;
+    uint32_t t[6] = {two ? a.z : a.x, two ? a.w : a.y, two ? b.x : a.z, two ? b.y : a.w, two ? b.z : b.x, two ? b.w : b.y};
+#pragma unroll
+    for (int i = 0; i < 5; ++i) t[i] = one ? t[i + 1] : t[i];
+    if constexpr (sizeof(T) == 4) return make_uint4(t[0], t[1], t[2], t[3]);
+    const uint32_t bits = 8 * (shift & 3);
+    return make_uint4(__funnelshift_r(t[0], t[1], bits), __funnelshift_r(t[1], t[2], bits), __funnelshift_r(t[2], t[3], bits),
+                      __funnelshift_r(t[3], t[4], bits));
+  }
+};
+
+// A row that is written: its elements before the first 16-byte boundary, and the parts of V from there on.
+struct Aligned {
+  int head, parts;
+  // Rows that are read beside it begin or end the memory of all rows (`edge`): there the first and the last part, around
+  // which a shifted load reads up to 15 bytes before and 16 behind, are taken element by element.
+  template <int V>
+  __device__ __forceinline__ void inside(bool edge) {
+    if (!edge) return;
+    if (parts > 0) head += V;
+    parts = max(parts - 2, 0);
+  }
+};
+template <typename O, int V>
+__device__ __forceinline__ Aligned aligned(const O* row, int width) {
+  const int off = static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15) / static_cast<int>(sizeof(O));
+  const int head = min(width, off ? kVec<O> - off : 0);
+  return {head, (width - head) / V};
+}
+// f(part, number of parts) for U parts of a row at a time, `lanes` apart; g(column) for the elements outside of them.
+template <int V, int U, typename F, typename G>
+__device__ __forceinline__ void each_aligned(Aligned r, int first, int lanes, int width, F f, G g) {
+  for (int i = first; i < r.parts; i += lanes * U) f(i);
+  for (int c = first; c < r.head; c += lanes) g(c);
+  for (int c = r.head + r.parts * V + first; c < width; c += lanes) g(c);
+}
+
+// By entries, since the rows of a token's entries are aligned each in its own way.
+template <typename T, int U>
+__global__ void __launch_bounds__(kThreads) k_dispatch_shifted(const __grid_constant__ RowArgs a) {
+  constexpr int V = kVec<T>;
+  const Item it = item_of(a);                               // its token is an entry
+  if (it.token >= a.entries) return;
+  const int64_t p = place_of(a, it.token);
+  const T* from = static_cast<const T*>(a.token) + it.token / a.k * a.token_ld;
+  if (p >= 0) {
+    T* out = static_cast<T*>(a.out_sorted) + p * a.out_sorted_ld;
+    Aligned r = aligned<T, V>(out, a.width);
+    r.template inside<V>(it.token < a.k || it.token >= a.entries - a.k);
+    each_aligned<V, U>(r, it.first, a.lanes, a.width, [&](int i) {
+      Shifted<T> x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i + u * a.lanes < r.parts) x[u].load(from + r.head + (i + u * a.lanes) * V);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i + u * a.lanes < r.parts) *reinterpret_cast<uint4*>(out + r.head + (i + u * a.lanes) * V) = x[u].get();
+    }, [&](int c) { out[c] = from[c]; });
+  }
+  if (it.token >= *a.count) {
+    T* out = static_cast<T*>(a.out_sorted) + it.token * a.out_sorted_ld;
+    const Aligned r = aligned<T, V>(out, a.width);
+    each_aligned<V, 1>(r, it.first, a.lanes, a.width,
+                       [&](int i) { *reinterpret_cast<uint4*>(out + r.head + i * V) = make_uint4(0, 0, 0, 0); },
+                       [&](int c) { out[c] = Elem<T>::down(0.0f); });
+  }
+}
+
+template <typename T, typename O, int U, int AT, bool WEIGHTS>
+__global__ void __launch_bounds__(kThreads, 4) k_combine_shifted(const __grid_constant__ RowArgs a) {
+  constexpr int V = kVec<T>;
+  const Item it = item_of(a);
+  if (it.token >= a.tokens) return;
+  O* out = static_cast<O*>(a.out_token) + it.token * a.out_token_ld;
+  Aligned r = aligned<O, V>(out, a.width);
+  bool edge = false;
+  for (int j = 0; j < a.k; ++j) {
+    const int64_t p = place_of(a, it.token * a.k + j);
+    edge = edge || p == 0 || p == a.entries - 1;
+  }
+  r.template inside<V>(edge);
+  each_aligned<V, U>(r, it.first, a.lanes, a.width, [&](int i) {
+    float sum[U][V];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < V; ++e) sum[u][e] = 0.0f;
+    for (int j0 = 0; j0 < a.k; j0 += AT) {
+      Shifted<T> y[AT][U];
+      float w[AT];
+#pragma unroll
+      for (int q = 0; q < AT; ++q) {
+        const int64_t p = j0 + q < a.k ? place_of(a, it.token * a.k + j0 + q) : -1;
+        w[q] = WEIGHTS && p >= 0 ? a.weight[it.token * a.k + j0 + q] : 0.0f;
+        const T* row = static_cast<const T*>(a.sorted) + p * a.sorted_ld + r.head;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (p >= 0 && i + u * a.lanes < r.parts) y[q][u].load(row + (i + u * a.lanes) * V);
+          else y[q][u].clear();
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < AT; ++q)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float v[V];
+          unpack<T>(y[q][u].get(), v);
+#pragma unroll
+          for (int e = 0; e < V; ++e) sum[u][e] = WEIGHTS ? fmaf(w[q], v[e], sum[u][e]) : sum[u][e] + v[e];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i + u * a.lanes < r.parts) {
+        Part<O, V> o;
+        o.down(sum[u]);
+        o.store(out + r.head + (i + u * a.lanes) * V);
+      }
+  }, [&](int c) { combine_at<T, O, 1, 1, AT, WEIGHTS>(a, it.token, c, a.width); });
+}
+
+// Some lanes, a warp or a CTA an entry.
+template <typename T, typename O, int U>
+__global__ void __launch_bounds__(kThreads) k_combine_backward_shifted(const __grid_constant__ RowArgs a) {
+  constexpr int V = kVec<T>, kWords = V / kVec<O>;
+  __shared__ float part[kThreads / 32];
+  const Item it = item_of(a);                               // its token is an entry
+  const bool mine = it.token < a.entries;                   // all take part in the sums
+  const int64_t entry = mine ? it.token : 0, p = mine ? place_of(a, entry) : -1;
+  const O* d = static_cast<const O*>(a.token) + entry / a.k * a.token_ld;
+  float dot = 0.0f;
+  if (p >= 0) {
+    const float w = a.weight[entry];
+    const T* y = static_cast<const T*>(a.sorted) + p * a.sorted_ld;
+    T* dy = static_cast<T*>(a.out_sorted) + p * a.out_sorted_ld;
+    Aligned r = aligned<T, V>(dy, a.width);
+    r.template inside<V>(p == 0 || p == a.entries - 1 || entry < a.k || entry >= a.entries - a.k);
+    each_aligned<V, U>(r, it.first, a.lanes, a.width, [&](int i) {
+      Shifted<T> ys[U];
+      Shifted<O> ds[U][kWords];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = r.head + (i + u * a.lanes) * V;
+        if (i + u * a.lanes < r.parts) {
+          ys[u].load(y + c);
+#pragma unroll
+          for (int x = 0; x < kWords; ++x) ds[u][x].load(d + c + x * kVec<O>);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (i + u * a.lanes >= r.parts) break;
+        float yv[V], dv[V];
+        unpack<T>(ys[u].get(), yv);
+#pragma unroll
+        for (int x = 0; x < kWords; ++x) unpack<O>(ds[u][x].get(), dv + x * kVec<O>);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          dot = fmaf(dv[e], yv[e], dot);
+          dv[e] *= w;
+        }
+        *reinterpret_cast<uint4*>(dy + r.head + (i + u * a.lanes) * V) = pack<T>(dv);
+      }
+    }, [&](int c) {
+      const float dv = Elem<O>::up(d[c]);
+      dot = fmaf(dv, Elem<T>::up(y[c]), dot);
+      dy[c] = Elem<T>::down(w * dv);
+    });
+  }
+  if (mine && entry >= *a.count) {
+    T* dy = static_cast<T*>(a.out_sorted) + entry * a.out_sorted_ld;
+    const Aligned r = aligned<T, V>(dy, a.width);
+    each_aligned<V, 1>(r, it.first, a.lanes, a.width,
+                       [&](int i) { *reinterpret_cast<uint4*>(dy + r.head + i * V) = make_uint4(0, 0, 0, 0); },
+                       [&](int c) { dy[c] = Elem<T>::down(0.0f); });
+  }
+  dot = lanes_sum(dot, a.lanes);
+  if (a.lanes == kThreads) {
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = dot;
+    __syncthreads();
+    dot = 0.0f;
+    for (int q = 0; q < kThreads / 32; ++q) dot += part[q];
+  }
+  if (mine && it.first == 0) a.dweight[entry] = dot;
+}
+
 // ---------------------------------------------------------------- launches
 // A pointer and a stride of rows that allow 16 bytes at a time.
 bool wide(const void* p, int64_t ld, int type) {
   return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld) * type_size(type)) & 15) == 0;
 }
-// Threads of a token: U parts each where rows are long.
-cudaError_t plan_flat(RowArgs& a, int v, int u, unsigned& grid) {
+// Rows of a 16-bit type of at least this many 16 bytes are read by 16 bytes where they are not aligned.  (Of fp32 a warp's
+// single elements are 128 bytes already.)
+// 8192 tokens of 4 entries of 4095 bf16 so and by single elements: dispatch 78 and 148 us, its gradient 76 and 118, combine 84 and
+// 112, its gradient 143 and 209; 16384 of 65: 7.2 and 7.3, 6.6 and 6.1, 8.1 and 6.1, 9.8 and 23.7.
+template <typename T>
+bool shifted(const RowArgs& a, int parts) { return sizeof(T) == 2 && a.width >= parts * kVec<T>; }
+constexpr int kShiftedParts = 16, kShiftedSums = 4;
+// A power of two of lanes for rows of so many parts, a CTA beyond a warp's.
+int lanes_for(int parts) {
+  if (parts > 128) return kThreads;
+  int lanes = 1;
+  while (lanes < 32 && lanes < parts) lanes *= 2;
+  return lanes;
+}
+
+// Threads of a token (or an entry): U parts each where rows are long.
+cudaError_t plan_flat(RowArgs& a, int64_t items, int v, int u, unsigned& grid) {
   const int parts = std::max(a.width / v, 1);
   a.lanes = (parts + u - 1) / u;
-  const int64_t ctas = (a.tokens * a.lanes + kThreads - 1) / kThreads;
+  const int64_t ctas = (items * a.lanes + kThreads - 1) / kThreads;
   grid = static_cast<unsigned>(ctas);
   return ctas > 0x7FFFFFFF ? cudaErrorInvalidConfiguration : cudaSuccess;
 }
@@ -311,40 +538,69 @@ cudaError_t plan_flat(RowArgs& a, int v, int u, unsigned& grid) {
 template <typename T, int V, int U>
 cudaError_t launch_dispatch(RowArgs a, cudaStream_t s) {
   unsigned grid;
-  const cudaError_t e = plan_flat(a, V, U, grid);
+  const cudaError_t e = plan_flat(a, a.tokens, V, U, grid);
   if (e != cudaSuccess) return e;
   k_dispatch<T, V, U><<<grid, kThreads, 0, s>>>(a);
   return cudaGetLastError();
 }
 template <typename T>
 cudaError_t dispatch_type(const RowArgs& a, bool vec, cudaStream_t s) {
-  return vec ? launch_dispatch<T, kVec<T>, 1>(a, s) : launch_dispatch<T, 1, 4>(a, s);
+  if (vec) return launch_dispatch<T, kVec<T>, 1>(a, s);
+  if (!shifted<T>(a, kShiftedParts)) return launch_dispatch<T, 1, 4>(a, s);
+  if constexpr (sizeof(T) == 2) {
+    RowArgs b = a;
+    unsigned grid;
+    const cudaError_t e = plan_flat(b, b.entries, kVec<T>, 4, grid);
+    if (e != cudaSuccess) return e;
+    k_dispatch_shifted<T, 4><<<grid, kThreads, 0, s>>>(b);
+  }
+  return cudaGetLastError();
 }
 
 template <typename T, typename O, int V, int U, int AT, bool WEIGHTS>
 cudaError_t launch_combine(RowArgs a, cudaStream_t s) {
   unsigned grid;
-  const cudaError_t e = plan_flat(a, V, U, grid);
+  const cudaError_t e = plan_flat(a, a.tokens, V, U, grid);
   if (e != cudaSuccess) return e;
   k_combine<T, O, V, U, AT, WEIGHTS><<<grid, kThreads, 0, s>>>(a);
   return cudaGetLastError();
 }
+template <typename T, typename O, int U, int AT, bool WEIGHTS>
+cudaError_t launch_combine_shifted(RowArgs a, cudaStream_t s) {
+  unsigned grid;
+  const cudaError_t e = plan_flat(a, a.tokens, kVec<T>, U, grid);
+  if (e != cudaSuccess) return e;
+  k_combine_shifted<T, O, U, AT, WEIGHTS><<<grid, kThreads, 0, s>>>(a);
+  return cudaGetLastError();
+}
 template <typename T, typename O, bool WEIGHTS>
 cudaError_t combine_type(const RowArgs& a, bool vec, cudaStream_t s) {
+  if constexpr (sizeof(T) == 2)
+    if (!vec && shifted<T>(a, kShiftedParts)) return launch_combine_shifted<T, O, 2, 2, WEIGHTS>(a, s);
   if (a.k <= 4) return vec ? launch_combine<T, O, kVec<T>, kWide, 4, WEIGHTS>(a, s) : launch_combine<T, O, 1, kSingle, 4, WEIGHTS>(a, s);
   return vec ? launch_combine<T, O, kVec<T>, 1, 8, WEIGHTS>(a, s) : launch_combine<T, O, 1, kSingle / 2, 8, WEIGHTS>(a, s);
 }
 
 template <typename T, typename O, int V, int U, int AT>
 cudaError_t launch_combine_backward(RowArgs a, cudaStream_t s) {
-  a.lanes = a.width / V <= 128 ? 32 : kThreads;
-  const int64_t per = kThreads / a.lanes, ctas = (a.tokens + per - 1) / per;
+  a.lanes = lanes_for(std::max(a.width / V, 1));
+  const int64_t ctas = (a.tokens * a.lanes + kThreads - 1) / kThreads;
   if (ctas > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
-  k_combine_backward<T, O, V, U, AT><<<static_cast<unsigned>(ctas), kThreads, 0, s>>>(a);
+  const auto kernel = a.lanes == kThreads ? k_combine_backward<T, O, V, U, AT, true> : k_combine_backward<T, O, V, U, AT, false>;
+  kernel<<<static_cast<unsigned>(ctas), kThreads, 0, s>>>(a);
   return cudaGetLastError();
 }
 template <typename T, typename O>
 cudaError_t combine_backward_type(const RowArgs& a, bool vec, cudaStream_t s) {
+  if constexpr (sizeof(T) == 2)
+    if (!vec && shifted<T>(a, kShiftedSums)) {
+      RowArgs b = a;
+      b.lanes = lanes_for(a.width / kVec<T>);
+      const int64_t ctas = (a.entries * b.lanes + kThreads - 1) / kThreads;
+      if (ctas > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
+      k_combine_backward_shifted<T, O, 1><<<static_cast<unsigned>(ctas), kThreads, 0, s>>>(b);
+      return cudaGetLastError();
+    }
   if (a.k <= 4) return vec ? launch_combine_backward<T, O, kVec<T>, 1, 4>(a, s) : launch_combine_backward<T, O, 1, kSingle, 4>(a, s);
   return vec ? launch_combine_backward<T, O, kVec<T>, 1, 8>(a, s) : launch_combine_backward<T, O, 1, kSingle / 2, 8>(a, s);
 }
