@@ -4,12 +4,14 @@
 //   over the chosen: w_j = e^(z_j) / sum over the chosen of e^z,   over all: w_j = e^(z_j - lse).
 // The entries (row, j) are then sorted by group, in their order within a group: a counting sort.
 // Each warp takes rows that follow one another and counts them by group in shared memory, where a
-// group's count is the next entry's rank; the CTA's warps, then the CTAs add up their counts in order.
+// group's count is the next entry's rank; the CTA's warps, then the CTAs add up their counts in order.  A CTA an SM, so
+// that with few groups the second kernel's CTAs can each add up all CTAs' counts by themselves.
 //
 //   over the chosen: dz_j = w_j (dw_j - s) at the chosen, 0 elsewhere;  s = sum over the chosen of w dw
 //   over all:        dz_i = [i chosen] w_i dw_i - p_i s,                p_i = e^(z_i - lse)
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "op_common.cuh"
 
@@ -17,9 +19,11 @@ namespace ha {
 namespace {
 
 constexpr int kMaxExperts = 1024, kMaxGroups = 1024, kMaxChosen = 32;
-constexpr int kWarps = 8;                 // of a CTA, where there are several
-constexpr int kOneWarps = 32;             // of a CTA that sorts all by itself, at most
-template <int R> constexpr int kOneRouteWarps = R <= 8 ? kOneWarps : kOneWarps / 2;      // their logits fill the registers
+constexpr int kCtas = 152;                // of a sort
+constexpr int kWarps = 32;                // of a CTA
+template <int L, int R> constexpr int kRouteWarps = L == 32 && R > 8 ? kWarps / 2 : kWarps;   // their logits fill the registers
+constexpr int kBackWarps = 8;             // of a CTA of the gradient
+constexpr int kSumGroups = 128;           // groups whose counts each CTA adds up by itself
 constexpr int kRankBits = 21;             // an entry in work: its group above, its rank below
 constexpr int kStaged = 2048;             // entries of a CTA that are kept in shared memory meanwhile
 constexpr int64_t kMaxChunk = int64_t(1) << (kRankBits - 1);
@@ -28,11 +32,12 @@ struct SortArgs {
   int* offsets;                           // [groups + 1]
   int* place;                             // [entries]
   int* source;                            // [entries]
-  int* counts;                            // [groups, chunks]
+  int* counts;                            // of group g in chunk c: [g * g_step + c * c_step]
   int* totals;                            // [groups]
   int64_t entries;
   int64_t per;                            // entries of a chunk
   int groups, chunks;
+  int g_step, c_step;                     // chunk after chunk, or group after group where a kernel of its own adds them up
 };
 
 // Exclusive sums of value[0, n) in place and their total behind them.
@@ -78,13 +83,14 @@ __device__ __forceinline__ void end_chunk(const SortArgs& a, int* hist, int* tot
   __syncthreads();
   for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
     int run = 0;
+#pragma unroll 8
     for (int w = 0; w < warps; ++w) {
       const int c = hist[w * a.groups + g];
       hist[w * a.groups + g] = run;
       run += c;
     }
     if (ONE) total[g] = run;
-    else a.counts[static_cast<int64_t>(g) * a.chunks + blockIdx.x] = run;
+    else a.counts[static_cast<int64_t>(g) * a.g_step + static_cast<int64_t>(blockIdx.x) * a.c_step] = run;
   }
   __syncthreads();
   if (ONE) {
@@ -123,12 +129,45 @@ __device__ __forceinline__ float lanes_sum(float x) {
   return x;
 }
 
+// A logit's key, its order among the row's.  A 16-bit logit's key has its index below, so that no two are equal; equal ones of
+// fp32 have equal keys.  v: the logit, raised to kNone where it is below; +0 makes zeros of both signs the same.
+template <typename T> constexpr bool kUnique = sizeof(T) == 2;
+template <typename T>
+__device__ __forceinline__ uint32_t key_of(float v, int index) {
+  if constexpr (kUnique<T>) {
+    // 16 bits of the type in their order: bf16 is the upper half of an fp32
+    uint32_t u = __float_as_uint(v + 0.0f);
+    if constexpr (!std::is_same<T, __nv_bfloat16>::value) u = static_cast<uint32_t>(__half_as_ushort(__float2half_rn(v + 0.0f))) << 16;
+    const uint32_t flip = (static_cast<uint32_t>(static_cast<int>(u) >> 31) | 0x80000000u) & 0xFFFF0000u;
+    return (u ^ flip) | static_cast<uint32_t>(0xFFFF - index);
+  } else {
+    const uint32_t u = __float_as_uint(v + 0.0f);
+    return u ^ (static_cast<uint32_t>(static_cast<int>(u) >> 31) | 0x80000000u);
+  }
+}
+template <typename T>
+__device__ __forceinline__ float value_of(uint32_t key) {
+  const uint32_t o = kUnique<T> ? key & 0xFFFF0000u : key;
+  uint32_t u = o & 0x80000000u ? o ^ 0x80000000u : ~o;
+  if constexpr (kUnique<T>) u &= 0xFFFF0000u;
+  if constexpr (std::is_same<T, __half>::value) return __half2float(__ushort_as_half(static_cast<unsigned short>(u >> 16)));
+  return __uint_as_float(u);
+}
+// The keys of what is masked are at most this (fp16 has nothing at kNone but minus infinity).
+template <typename T>
+__device__ __forceinline__ uint32_t key_none() {
+  return std::is_same<T, __half>::value ? 0x03FFFFFFu : key_of<T>(kNone<T>, 0) | (kUnique<T> ? 0xFFFFu : 0u);
+}
+
 // L lanes take a row, at least as many as it has chosen ones; lane l of them holds the logits l, l + L, ...  The chosen
-// are taken one after the other, the largest of the lanes' largest, which is a chain of latencies: several rows a warp share it.
+// are found from the largest down: of a lane's keys below the last, less the last, the largest is that of the keys, since
+// differences of unsigned numbers wrap, in one instruction a key.  Several rows a warp share the latencies.
 template <typename T, int L, int R, bool ONE>
-__global__ void __launch_bounds__(32 * (ONE ? kOneRouteWarps<R> : kWarps)) k_route(const __grid_constant__ RouteArgs a) {
+__global__ void __launch_bounds__(32 * kRouteWarps<L, R>) k_route(const __grid_constant__ RouteArgs a) {
   extern __shared__ int dyn[];
   constexpr int kRows = 32 / L;                               // of a warp at a time
+  __shared__ uint32_t slot_key[kUnique<T> ? 1 : kRouteWarps<L, R>][32];
+  __shared__ int slot_index[kUnique<T> ? 1 : kRouteWarps<L, R>][32];
   constexpr uint32_t kLanes = L == 32 ? ~0u : (1u << L) - 1;
   const int lane = threadIdx.x & 31, l = lane % L, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   const int G = a.sort.groups, k = a.k;
@@ -158,68 +197,100 @@ __global__ void __launch_bounds__(32 * (ONE ? kOneRouteWarps<R> : kWarps)) k_rou
     const bool mine = r < last;
     const int64_t row = r0 + (mine ? r : r1);                 // lanes without a row repeat the first's
     const T* z = static_cast<const T*>(a.logits) + row * a.ld;
+    const uint32_t none = key_none<T>();
+    uint32_t key[R], most = 0;
     float v[R];
 #pragma unroll
     for (int u = 0; u < R; ++u) v[u] = u * L + l < a.experts ? Elem<T>::up(z[u * L + l]) : -INFINITY;
-    bool bad = false;                                         // NaN or infinity among them
-    uint32_t key[R], most = 0;                                // 0: masked
-    int at = 0;
 #pragma unroll
     for (int u = 0; u < R; ++u) {
-      bad = bad || !(v[u] < INFINITY);
-      key[u] = v[u] > kNone<T> ? ordered(v[u]) : 0;
+      v[u] = max_nan(v[u], kNone<T>);
+      key[u] = key_of<T>(v[u], u * L + l);
+      most = max(most, key[u]);
     }
-    auto look = [&] {                                         // the lane's largest, the first of equal ones
-      most = 0;
-#pragma unroll
-      for (int u = 0; u < R; ++u)
-        if (key[u] > most) {
-          most = key[u];
-          at = u;
-        }
-    };
-    look();
-    bad = (__ballot_sync(~0u, bad) >> (lane - l) & kLanes) != 0;
     const uint32_t top = lanes_max<L>(most);
-    const float m = from_ordered(top);
-    float S = 0.0f;
+    const float m = value_of<T>(top);
+    Pair S2 = pair(0.0f, 0.0f);
 #pragma unroll
-    for (int u = 0; u < R; ++u)
-      if (key[u]) S += exp2_fast((v[u] - m) * kLog2e);
-    S = lanes_sum<L>(S);
+    for (int u = 0; u < R; u += 2) {
+      float x, y;
+      halves(mul2(add2(pair(v[u], v[u + 1]), pair(-m, -m)), pair(kLog2e, kLog2e)), x, y);
+      S2 = add2(S2, pair(exp2_fast(x), exp2_fast(y)));
+    }
+    float x, y;
+    halves(S2, x, y);
+    const float S = lanes_sum<L>(x + y);                      // NaN where a logit is NaN, or infinite: inf - inf
+    const bool bad = !(S == S);
 
-    uint32_t mine_key = 0;
-    int index = -1;
-    for (int j = 0; j < k; ++j) {
-      const uint32_t best = j == 0 ? top : lanes_max<L>(most);
-      if (L == 32 && best == 0) break;
-      const uint32_t lanes = __ballot_sync(~0u, most == best && best != 0) >> (lane - l) & kLanes;
-      int src = __ffs(lanes) - 1;
-      if (__any_sync(~0u, lanes & (lanes - 1))) {             // equal logits of two lanes: the lowest index
-        const uint32_t i = most == best ? static_cast<uint32_t>(at * L + l) : ~0u;
-        src = static_cast<int>(~lanes_max<L>(~i)) % L;
-      }
-      const int i = __shfl_sync(~0u, at, src & (L - 1), L) * L + src;
-      if (best == 0) continue;                                // of this row; others' lanes go on
-      if (l == j) {
-        mine_key = best;
-        index = i;
-      }
-      if (l == src) {
+    uint32_t slot = l == 0 && top > none ? top : 0, best = max(top, none);     // lane j's is the j-th
+    for (int j = 1; j < k; ++j) {
+      uint32_t t = 0;
 #pragma unroll
-        for (int u = 0; u < R; ++u)
-          if (u == at) key[u] = 0;
-        look();
+      for (int u = 0; u < R; ++u) t = __viaddmax_u32(key[u], 0u - best, t);
+      const uint32_t next = lanes_max<L>(t) + best;
+      best = next < best ? max(next, none) : none;            // (none is below it)
+      if (l == j) slot = best > none ? best : 0;
+    }
+    int index = -1;
+    if constexpr (kUnique<T>) {
+      if (slot) index = 0xFFFF - static_cast<int>(slot & 0xFFFFu);
+    } else {
+      // Which are they?  As many as there are slots, unless logits are equal.
+      uint32_t held = 0;
+      const uint32_t least = max(best, none + 1);
+#pragma unroll
+      for (int u = 0; u < R; ++u) held |= key[u] >= least ? 1u << u : 0;
+      int n = __popc(held);
+#pragma unroll
+      for (int o = L / 2; o > 0; o >>= 1) n += __shfl_xor_sync(~0u, n, o);
+      const int slots = __popc(__ballot_sync(~0u, slot != 0) >> (lane - l) & kLanes);
+      if (__any_sync(~0u, n != slots)) {                      // then one by one, the lowest index first
+        slot = 0;
+        for (int j = 0; j < k; ++j) {
+          uint32_t mine_most = 0;
+          int at = 0;
+#pragma unroll
+          for (int u = 0; u < R; ++u)
+            if (key[u] > mine_most) {
+              mine_most = key[u];
+              at = u;
+            }
+          const uint32_t first = lanes_max<L>(mine_most);
+          const uint32_t i = mine_most == first ? static_cast<uint32_t>(at * L + l) : ~0u;
+          const uint32_t lowest = ~lanes_max<L>(~i);
+          if (first <= none) continue;                        // of this row; others' lanes go on
+          if (l == j) {
+            slot = first;
+            index = static_cast<int>(lowest);
+          }
+          if (static_cast<int>(lowest) % L == l) {
+#pragma unroll
+            for (int u = 0; u < R; ++u)
+              if (u * L + l == static_cast<int>(lowest)) key[u] = 0;
+          }
+        }
+      } else {
+        slot_key[warp][lane] = slot;
+        __syncwarp();
+        while (held) {
+          const int i = (__ffs(held) - 1) * L + l;
+          held &= held - 1;
+          const uint32_t mine_key = key_of<T>(Elem<T>::up(z[i]), i);
+          for (int j = 0; j < k; ++j)
+            if (slot_key[warp][lane - l + j] == mine_key) slot_index[warp][lane - l + j] = i;
+        }
+        __syncwarp();
+        if (slot) index = slot_index[warp][lane];
       }
     }
     if (bad) index = -1;
-    const float e = index >= 0 ? expf(from_ordered(mine_key) - m) : 0.0f;
+    const float e = index >= 0 ? expf(value_of<T>(slot) - m) : 0.0f;
     const float sum = a.all ? S : lanes_sum<L>(e);
     if (mine && l < k) {
       a.expert[row * k + l] = index;
       a.weight[row * k + l] = bad ? NAN : index >= 0 ? e / sum : 0.0f;
     }
-    if (mine && l == 0) a.lse[row] = bad ? NAN : top == 0 ? -INFINITY : m + logf(S);
+    if (mine && l == 0) a.lse[row] = bad ? NAN : top <= none ? -INFINITY : m + logf(S);
 
     int group = mine && l < k ? index : -1;
     if (a.learners) {
@@ -268,7 +339,7 @@ __global__ void __launch_bounds__(32 * (ONE ? kOneRouteWarps<R> : kWarps)) k_rou
 
 // ---------------------------------------------------------------- the sort of given groups
 template <bool ONE>
-__global__ void __launch_bounds__(32 * (ONE ? kOneWarps : kWarps)) k_group(const int* __restrict__ ids, const __grid_constant__ SortArgs a) {
+__global__ void __launch_bounds__(32 * kWarps) k_group(const int* __restrict__ ids, const __grid_constant__ SortArgs a) {
   extern __shared__ int dyn[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, G = a.groups;
   int* hist = dyn;
@@ -312,8 +383,8 @@ __global__ void __launch_bounds__(32 * (ONE ? kOneWarps : kWarps)) k_group(const
 }
 
 // A warp a group: the chunks' counts become what comes before each chunk.
-__global__ void __launch_bounds__(kWarps * 32) k_chunks(const __grid_constant__ SortArgs a) {
-  const int lane = threadIdx.x & 31, g = blockIdx.x * kWarps + (threadIdx.x >> 5);
+__global__ void __launch_bounds__(kBackWarps * 32) k_chunks(const __grid_constant__ SortArgs a) {
+  const int lane = threadIdx.x & 31, g = blockIdx.x * kBackWarps + (threadIdx.x >> 5);
   let_next_start();
   wait_for_previous();
   if (g >= a.groups) return;
@@ -346,24 +417,49 @@ __global__ void __launch_bounds__(kWarps * 32) k_chunks(const __grid_constant__ 
   if (lane == 0) a.totals[g] = carry;
 }
 
-// Ranks in a chunk become places.
+// Ranks in a chunk become places.  SUM: the counts of all chunks are added up here, by as many threads a group as there are.
+template <bool SUM>
 __global__ void __launch_bounds__(kWarps * 32) k_place(const __grid_constant__ SortArgs a) {
-  __shared__ int base[kMaxGroups + 1];
+  __shared__ int base[kMaxGroups + 1], mine[kMaxGroups];
   __shared__ int warp_sum[32];
   wait_for_previous();
-  for (int g = threadIdx.x; g < a.groups; g += blockDim.x) base[g] = a.totals[g];
+  const int chunk = blockIdx.x;
+  const int64_t e0 = chunk * a.per, e1 = min(e0 + a.per, a.entries);
+  int next = e0 + threadIdx.x < e1 ? a.place[e0 + threadIdx.x] : -1;      // on its way meanwhile
+  if (SUM) {
+    int width = 32;                                           // threads of a part, a power of two
+    while (width < a.groups) width *= 2;
+    const int g = threadIdx.x & (width - 1), part = threadIdx.x / width, parts = blockDim.x / width;
+    for (int i = threadIdx.x; i < a.groups; i += blockDim.x) base[i] = mine[i] = 0;
+    __syncthreads();
+    if (g < a.groups) {
+      int all = 0, before = 0;
+#pragma unroll 8
+      for (int c = part; c < a.chunks; c += parts) {
+        const int n = a.counts[c * a.groups + g];
+        all += n;
+        before += c < chunk ? n : 0;
+      }
+      atomicAdd(base + g, all);                               // whole numbers: their order changes nothing
+      atomicAdd(mine + g, before);
+    }
+  } else {
+    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
+      base[g] = a.totals[g];
+      mine[g] = a.counts[static_cast<int64_t>(g) * a.chunks + chunk];
+    }
+  }
   __syncthreads();
   block_scan(base, a.groups, warp_sum);
   const int count = base[a.groups];
-  if (blockIdx.x == 0)
+  if (chunk == 0)
     for (int g = threadIdx.x; g <= a.groups; g += blockDim.x) a.offsets[g] = base[g];
   __syncthreads();
-  for (int g = threadIdx.x; g < a.groups; g += blockDim.x)
-    base[g] += a.counts[static_cast<int64_t>(g) * a.chunks + blockIdx.x];
+  for (int g = threadIdx.x; g < a.groups; g += blockDim.x) base[g] += mine[g];
   __syncthreads();
-  const int64_t e0 = blockIdx.x * a.per, e1 = min(e0 + a.per, a.entries);
   for (int64_t e = e0 + threadIdx.x; e < e1; e += blockDim.x) {
-    int p = a.place[e];
+    int p = next;
+    if (e + blockDim.x < e1) next = a.place[e + blockDim.x];
     if (p >= 0) {
       p = (p & ((1 << kRankBits) - 1)) + base[p >> kRankBits];
       a.place[e] = p;
@@ -387,12 +483,12 @@ struct RouteBwdArgs {
 // L lanes a row, at least as many as it has chosen ones, whose lanes write theirs after the row's others.  R of a lane's
 // logits are loaded before the first use.
 template <typename T, int L, bool ALL>
-__global__ void __launch_bounds__(kWarps * 32) k_route_backward(const __grid_constant__ RouteBwdArgs a) {
+__global__ void __launch_bounds__(kBackWarps * 32) k_route_backward(const __grid_constant__ RouteBwdArgs a) {
   constexpr int R = 8;
   const int lane = threadIdx.x & 31, l = lane % L;
   constexpr uint32_t kLanes = L == 32 ? ~0u : (1u << L) - 1;
-  const int64_t step = static_cast<int64_t>(gridDim.x) * kWarps * (32 / L);
-  for (int64_t r0 = (blockIdx.x * static_cast<int64_t>(kWarps) + (threadIdx.x >> 5)) * (32 / L); r0 < a.rows; r0 += step) {
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kBackWarps * (32 / L);
+  for (int64_t r0 = (blockIdx.x * static_cast<int64_t>(kBackWarps) + (threadIdx.x >> 5)) * (32 / L); r0 < a.rows; r0 += step) {
     const bool mine = r0 + lane / L < a.rows;
     const int64_t row = mine ? r0 + lane / L : r0;           // lanes without a row repeat the first's
     const T* z = ALL ? static_cast<const T*>(a.logits) + row * a.ld : nullptr;
@@ -460,33 +556,37 @@ __global__ void __launch_bounds__(kWarps * 32) k_route_backward(const __grid_con
 }
 
 // ---------------------------------------------------------------- launches
-// Chunks of a sort: CTAs of 8 warps, four on each of the 152 SMs, more where a chunk's ranks would not fit.
+// Units (rows) of a sort's chunk: one for each SM, of a warp's rows at least, more chunks where their ranks would not fit.
 int64_t chunk_units(int64_t units, int64_t entries_each) {
-  int64_t per = (units + 152 * 4 - 1) / (152 * 4);
-  per = std::max<int64_t>(per, 1);
+  const int64_t per = std::max<int64_t>((units + kCtas - 1) / kCtas, 32);
   return std::min(per, kMaxChunk / entries_each);
 }
 int64_t workspace_ints(int64_t entries, int unit, int groups) {
   const int64_t units = entries / unit, per = chunk_units(units, unit);
   return (static_cast<int64_t>(groups)) * ((units + per - 1) / per) + groups;
 }
-// The entries that one CTA sorts by itself: a second and a third launch take longer than its few rounds.
-constexpr int64_t kOneRows = 256, kOneEntries = 2048;
+// The entries that one CTA sorts by itself, a warp a row: 8 rows of 64 experts 4.3 us, 32 rows about as long as two kernels; 128 rows
+// would take 11.1 us, by two kernels 6.1.
+constexpr int64_t kOneRows = 32, kOneEntries = 1024;
 
 size_t sort_smem(int warps, int groups, int64_t per) {
   return sizeof(int) * (static_cast<size_t>(warps) * groups + groups + 1 + (per <= kStaged ? per : 0));
 }
 
+// With few groups the places' kernel adds up the counts, else a third one: 1000 rows of 64 experts 7.5 us so and 8.3 with
+// three kernels, 16384 of 128 experts 15.8 and 16.0, of 200 18.9 and 16.1, of 1024 65 and 53.
 cudaError_t end_sort(const SortArgs& a, cudaStream_t s) {
-  cudaError_t e = launch_early(k_chunks, (a.groups + kWarps - 1) / kWarps, kWarps * 32, 0, s, a);
+  const unsigned chunks = static_cast<unsigned>(a.chunks);
+  if (a.c_step > 1) return launch_early(k_place<true>, chunks, kWarps * 32, 0, s, a);
+  const cudaError_t e = launch_early(k_chunks, (a.groups + kBackWarps - 1) / kBackWarps, kBackWarps * 32, 0, s, a);
   if (e != cudaSuccess) return e;
-  return launch_early(k_place, static_cast<unsigned>(a.chunks), kWarps * 32, 0, s, a);
+  return launch_early(k_place<false>, chunks, kWarps * 32, 0, s, a);
 }
 
 template <typename T, int L, int R, bool ONE>
 cudaError_t route_rows(const RouteArgs& a, cudaStream_t s) {
   static bool ok[kMaxDevices];
-  const int warps = ONE ? static_cast<int>(std::min<int64_t>(a.rows, kOneRouteWarps<R>)) : kWarps;
+  const int warps = ONE ? static_cast<int>(std::min<int64_t>(a.rows, kRouteWarps<L, R>)) : kRouteWarps<L, R>;
   const size_t smem = sort_smem(warps, a.sort.groups, a.sort.per);
   const auto kernel = k_route<T, L, R, ONE>;
   cudaError_t e = allow_smem(kernel, 200 << 10, ok);
@@ -503,8 +603,11 @@ cudaError_t route_type(const RouteArgs& a, bool one, cudaStream_t s) {
     if (a.experts <= 256) return route_rows<T, 32, 8, true>(a, s);
     return route_rows<T, 32, 32, true>(a, s);
   }
+  if (a.k <= 8 && a.experts <= 32) return route_rows<T, 8, 4, false>(a, s);
   if (a.k <= 8 && a.experts <= 64) return route_rows<T, 8, 8, false>(a, s);
   if (a.k <= 8 && a.experts <= 128) return route_rows<T, 8, 16, false>(a, s);
+  if (a.k <= 16 && a.experts <= 32) return route_rows<T, 16, 2, false>(a, s);
+  if (a.k <= 16 && a.experts <= 128) return route_rows<T, 16, 8, false>(a, s);
   if (a.k <= 16 && a.experts <= 256) return route_rows<T, 16, 16, false>(a, s);
   if (a.experts <= 128) return route_rows<T, 32, 4, false>(a, s);
   if (a.experts <= 512) return route_rows<T, 32, 16, false>(a, s);
@@ -513,9 +616,9 @@ cudaError_t route_type(const RouteArgs& a, bool one, cudaStream_t s) {
 
 template <typename T, int L>
 cudaError_t backward_rows(const RouteBwdArgs& a, cudaStream_t s) {
-  const int64_t per = kWarps * (32 / L), ctas = std::min<int64_t>((a.rows + per - 1) / per, 152 * 8 * 8);
+  const int64_t per = kBackWarps * (32 / L), ctas = std::min<int64_t>((a.rows + per - 1) / per, 152 * 8 * 8);
   const auto kernel = a.all ? k_route_backward<T, L, true> : k_route_backward<T, L, false>;
-  kernel<<<static_cast<unsigned>(ctas), kWarps * 32, 0, s>>>(a);
+  kernel<<<static_cast<unsigned>(ctas), kBackWarps * 32, 0, s>>>(a);
   return cudaGetLastError();
 }
 template <typename T>
@@ -537,6 +640,10 @@ bool plan_sort(SortArgs& a, int unit, bool one, void* ws, int64_t bytes) {
   if (!ws || bytes < need) return false;
   a.counts = static_cast<int*>(ws);
   a.totals = a.counts + static_cast<int64_t>(a.groups) * a.chunks;
+  // (one group: the strides are the same)
+  const bool sum = a.groups > 1 && a.groups <= kSumGroups && a.chunks <= 2 * kCtas;
+  a.g_step = sum ? 1 : a.chunks;
+  a.c_step = sum ? a.groups : 1;
   return true;
 }
 bool one_cta(int64_t units, int64_t entries) { return units <= kOneRows && entries <= kOneEntries; }
@@ -595,7 +702,7 @@ extern "C" int hier_avg_sort_by_group(const int32_t* group_dev, int64_t rows, in
   SortArgs a = {offsets_dev, place_dev, source_dev, nullptr, nullptr, rows * per_row, 0, groups, 0};
   const bool one = one_cta(rows, rows * per_row);
   if (!plan_sort(a, per_row, one, workspace_dev, workspace_bytes)) return HA_ENOMEM;
-  const int warps = one ? static_cast<int>(std::min<int64_t>((a.entries + 31) / 32, kOneWarps)) : kWarps;
+  const int warps = one ? static_cast<int>(std::min<int64_t>((a.entries + 31) / 32, kWarps)) : kWarps;
   static bool one_ok[kMaxDevices], ok[kMaxDevices];
   const auto kernel = one ? k_group<true> : k_group<false>;
   cudaError_t e = allow_smem(kernel, 200 << 10, one ? one_ok : ok);

@@ -5,20 +5,20 @@ HierAvg takes plain SGD steps on equal batches.  Here the rows of all learners' 
 one another (``offsets`` says where each learner's begin), a layer of all learners is one grouped
 product, the loss and its gradient are the log probabilities of the labels, and one AdamW step
 updates every learner's tensors in the learner-indexed matrix [P, ld] and writes the bf16 weights
-that the products read.  The averages are the library's.  The moments stay each learner's own.
+that the products read, after each learner's gradients were clipped to a norm where one is given.  The averages are the library's.  The moments stay each learner's own.
 
 ``python -m paper_1903_05133_gb300.local_adamw`` trains 16 learners of 3072-512-10 for a few rounds.
 """
 from __future__ import annotations
 
 import argparse
-from typing import Sequence
+from typing import Optional, Sequence
 
 import torch
 
 from .configs import MLP512_P16
 from .hier_avg import HierAvg, local_average_buffer, local_global_average_buffer
-from .operators import (AdamW, grouped_product, grouped_product_dw, grouped_product_dx, operator_check,
+from .operators import (AdamW, clip_gradients, grouped_product, grouped_product_dw, grouped_product_dx, operator_check,
                         token_logprobs, token_logprobs_backward)
 
 
@@ -27,9 +27,12 @@ class LocalAdamW:
     a round, then the global average."""
 
     def __init__(self, P: int, S: int, K1: int, K2: int, lr: float, dims: Sequence[int], bits: int = 8,
-                 beta1: float = 0.9, beta2: float = 0.999, decay: float = 0.0, device="cuda"):
+                 beta1: float = 0.9, beta2: float = 0.999, decay: float = 0.0, device="cuda",
+                 max_norm: Optional[float] = None):
+        """max_norm: of each learner's gradients, weights and biases together (None: not clipped)."""
         self.layout = HierAvg(P, S, K1, K2, lr, 1, dims, "fp32")       # the rows of [P, ld]
         self.P, self.S, self.K1, self.K2, self.lr, self.dims = P, S, K1, K2, lr, tuple(dims)
+        self.max_norm = max_norm
         self.params = self.layout.new_params(device)
         self.copy = torch.zeros_like(self.params, dtype=torch.bfloat16)
         self.layers = self.layout.unpack(self.params)                  # [(W [P, out, in], b [P, out])]
@@ -64,6 +67,8 @@ class LocalAdamW:
             dw[l], db[l] = grouped_product_dw(dy, h[l], offsets, bias_grad=True)
             if l:
                 dy = grouped_product_dx(dy, self.weights[l], offsets, h=h[l])
+        if self.max_norm is not None:
+            clip_gradients(dw + db, self.max_norm, learners=self.P)
         self.opt_w.step(dw, lr=self.lr)
         self.opt_b.step(db, lr=self.lr)
         self.t += 1
@@ -116,10 +121,11 @@ def main() -> None:
     ap.add_argument("--rounds", type=int, default=4)
     ap.add_argument("--lr", type=float, default=1e-3)
     ap.add_argument("--bits", type=int, default=8, choices=(8, 32))
+    ap.add_argument("--max-norm", type=float, default=None, help="clip each learner's gradients to this norm")
     a = ap.parse_args()
     w = MLP512_P16
     X, y = learner_data(w, device="cuda")
-    m = LocalAdamW(w.P, w.S, w.K1, w.K2, a.lr, w.dims, bits=a.bits)
+    m = LocalAdamW(w.P, w.S, w.K1, w.K2, a.lr, w.dims, bits=a.bits, max_norm=a.max_norm)
     m.load(initial_layers(w, device="cuda"))
     batches = ragged_batches(X, y, w.B, w.seed)
     for n in range(a.rounds):

@@ -382,7 +382,7 @@ class Sorted(NamedTuple):
 
 
 MAX_CHOSEN, MAX_GROUPS = 32, 1024
-_ONE_ROWS, _ONE_ENTRIES = 256, 2048
+_ONE_ROWS, _ONE_ENTRIES = 32, 1024
 
 
 def _vector(name, t, dtype, shape):
@@ -393,6 +393,8 @@ def _vector(name, t, dtype, shape):
 def _sort_bytes(lib, rows, k, groups):
     if rows <= _ONE_ROWS and rows * k <= _ONE_ENTRIES:      # one CTA sorts them: none, as the library says
         return 0
+    if rows * k <= 1 << 27:                                 # at most 153 chunks' counts, without the call
+        return 4 * 154 * groups
     n = c_int64()
     check(lib.hier_avg_sort_workspace(rows, k, groups, ctypes.byref(n)), "sort_workspace")
     return n.value

@@ -154,3 +154,36 @@ def test_captured_and_on_a_stream():
         graph.replay()
         assert torch.equal(r.norm, want.norm) and torch.equal(r.scale, want.scale)
         assert torch.equal(grads[0], start[0] * want.scale)
+
+
+def test_local_adamw_clips_each_learner():
+    # the first moments of a first step are 0.1 of the gradients: with a norm given each learner's are scaled by its factor
+    from paper_1903_05133_gb300.inputs import learner_data, perturbed_layers
+    from paper_1903_05133_gb300.local_adamw import LocalAdamW, ragged_batches
+    from test_gpu_local_adamw import W
+    X, y = learner_data(W, device="cuda")
+    x, t, off = next(ragged_batches(X, y, W.B, 5))
+    models = {}
+    for max_norm in (None, 1e9, 0.5):
+        m = models[max_norm] = LocalAdamW(W.P, W.S, W.K1, W.K2, W.lr, W.dims, bits=32, max_norm=max_norm)
+        m.load(perturbed_layers(W, 0.01, seed=3))
+        m.step(x, t, off)
+
+    def moments(m):
+        # [P] rows of every tensor's first moments, which stand from multiples of 256 on
+        rows = []
+        for opt, tensors in ((m.opt_w, [w for w, _ in m.layers]), (m.opt_b, [b for _, b in m.layers])):
+            at = 0
+            for v in tensors:
+                n = v[0].numel()
+                rows.append(torch.stack([opt.m[at + j * -(-n // 256) * 256:][:n] for j in range(W.P)]))
+                at += W.P * -(-n // 256) * 256
+        return torch.cat(rows, 1).double()
+    free, loose, tight = (moments(models[n]) for n in (None, 1e9, 0.5))
+    assert torch.equal(free, loose)
+    norms = 10 * free.norm(dim=1)
+    assert (norms > 0.5).any()
+    scale = torch.where(norms > 0.5, 0.5 / norms, 1.0)
+    # the weights' gradients are rounded to bf16 once more
+    assert (tight - free * scale[:, None]).norm() <= 2.0 ** -8 * tight.norm()
+    assert ((10 * tight.norm(dim=1) - torch.minimum(norms, torch.full_like(norms, 0.5))).abs() <= 2.0 ** -8 * norms).all()

@@ -26,11 +26,12 @@ def test_sort_workspace(lib):
     refuses(lib.hier_avg_sort_workspace, [1000, 8, 64, b], (
         (0, -1, EINVAL), (1, 0, EINVAL), (2, 0, EINVAL), (3, None, EINVAL), (1, 33, EUNSUPPORTED), (2, 1025, EUNSUPPORTED),
         (0, 1 << 28, EUNSUPPORTED), (0, FAR, EUNSUPPORTED)))
-    # the binding knows without asking where nothing is needed
-    for rows, k in ((0, 1), (1, 32), (256, 8), (257, 1), (64, 32), (65, 32), (2048, 1), (256, 9)):
-        assert lib.hier_avg_sort_workspace(rows, k, 64, b) == 0
-        assert (n.value == 0) == (rows <= ops._ONE_ROWS and rows * k <= ops._ONE_ENTRIES), (rows, k)
-        assert ops._sort_bytes(lib, rows, k, 64) == n.value
+    # the binding knows without asking where nothing is needed, and how much is enough
+    for rows in (0, 1, 31, 32, 33, 64, 256, 2048, 4863, 4864, 4865, 10000, 16384, 99999, 1 << 20, 1 << 22):
+        for k in (1, 2, 8, 31, 32):
+            assert lib.hier_avg_sort_workspace(rows, k, 64, b) == 0
+            assert (n.value == 0) == (rows <= ops._ONE_ROWS and rows * k <= ops._ONE_ENTRIES), (rows, k)
+            assert n.value <= ops._sort_bytes(lib, rows, k, 64) and (n.value or not ops._sort_bytes(lib, rows, k, 64))
     # any number of rows has chunks whose entries' ranks fit
     for rows, k in ((1 << 30, 1), (1 << 26, 31), ((1 << 31) - 1, 1)):
         assert lib.hier_avg_sort_workspace(rows, k, 1024, b) == 0 and n.value < 1 << 26
