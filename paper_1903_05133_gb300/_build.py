@@ -47,14 +47,18 @@ def _run(cmd):
     return r.stdout
 
 
+def _cuda_include() -> str:
+    return os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(_nvcc()))), "include")
+
+
 def _host_command(out: str):
     """g++ on csrc/host.cpp; the libraries are those that ``import torch`` has loaded."""
     torch = importlib.util.find_spec("torch").submodule_search_locations[0]
     inc, lib = os.path.join(torch, "include"), os.path.join(torch, "lib")
     return [os.environ.get("CXX") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-o", out,
             os.path.join(CSRC, "host.cpp"), f"-I{sysconfig.get_paths()['include']}", f"-isystem{inc}",
-            f"-isystem{os.path.join(inc, 'torch', 'csrc', 'api', 'include')}", f"-L{lib}", "-ltorch_python",
-            "-ltorch_cpu", "-lc10"]
+            f"-isystem{os.path.join(inc, 'torch', 'csrc', 'api', 'include')}", f"-L{lib}", f"-isystem{_cuda_include()}",
+            "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
 
 
 def build(verbose: bool = False, ptxas_info: bool = False) -> str:

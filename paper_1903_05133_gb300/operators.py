@@ -6,7 +6,9 @@ Argument marshalling only, as in hier_avg.py: PyTorch provides the memory and th
 computation runs in the library's CUDA kernels, and the functions are those of
 include/hier_avg.h without the ``hier_avg_`` prefix.  Results are new tensors unless ``out``
 is given, and outside autograd: a result has no history even where an input requires gradients, whose
-calls are grouped_product_dx, grouped_product_dw and the functions that end in _backward.  All tensors of a
+calls are grouped_product_dx, grouped_product_dw and the functions that end in _backward.  The usual calls of the
+routing, row, norm and draft operators go through the host module at once; what it does not take (another stream, an
+``out``, anything to refuse) goes through the checks here.  All tensors of a
 call are on one GPU, where it runs whichever is current.  A call on ``stream`` makes its results and
 workspace there; its inputs are the caller's to keep until it is done.
 """
@@ -413,6 +415,11 @@ def route(logits: torch.Tensor, k: int, over: str = "chosen", learners: Optional
     logits [rows, experts] fp32, bf16 or fp16, at or below -1e30 where masked; the weights are softmax over the
     ``chosen`` or over ``all`` experts.  learners [learners + 1] int32 on the device, rising: the rows of
     each learner, which has experts of its own (group = learner * experts + expert)."""
+    every = _over(over)
+    if stream is None:
+        r = _lib.host().route(logits, k, every, learners)
+        if r is not None:
+            return Routing(*r)
     lib = _lib.load()
     ld = _rows_of("logits", logits, TYPES)
     T, E = logits.shape
@@ -420,7 +427,6 @@ def route(logits: torch.Tensor, k: int, over: str = "chosen", learners: Optional
     P = 0 if learners is None else _offsets(learners, None)
     G = E * max(P, 1)
     _need(G <= MAX_GROUPS, f"there must be at most {MAX_GROUPS} groups")
-    every = _over(over)
     s, where = _on(stream, logits, learners)
     with where:
         n = _sort_bytes(lib, T, k, G)
@@ -438,10 +444,14 @@ def route_backward(dweights: torch.Tensor, logits: torch.Tensor, experts: torch.
                    stream=None) -> torch.Tensor:
     """The gradient of sum(dweights * weights) with respect to the logits, in their type, from route's experts and
     weights (and lse for over="all"); ``out`` may be ``logits`` itself."""
+    every = _over(over)
+    if stream is None and out is None:
+        r = _lib.host().route_backward(dweights, logits, experts, weights, lse, every)
+        if r is not None:
+            return r
     lib = _lib.load()
     ld = _rows_of("logits", logits, TYPES)
     T, E = logits.shape
-    every = _over(over)
     _need(experts.dim() == 2, "experts must be [rows, k]")
     k = experts.shape[1]
     _need(1 <= k <= min(E, MAX_CHOSEN), f"k must be in [1, {min(E, MAX_CHOSEN)}]")
@@ -495,6 +505,10 @@ def dispatch(x: torch.Tensor, place: torch.Tensor, offsets: torch.Tensor, out: O
     """xs[place[t, j]] = x[t], [rows * k, width]; the rows behind the last group, offsets[-1], are zero.
 
     x [rows, width] fp32, bf16 or fp16; place [rows, k] and offsets as of route or sort_by_group."""
+    if stream is None and out is None:
+        r = _lib.host().dispatch(x, place, offsets)
+        if r is not None:
+            return r
     lib = _lib.load()
     T, k = _places(place)
     ld = _rows_of("x", x, TYPES, T)
@@ -509,6 +523,10 @@ def dispatch(x: torch.Tensor, place: torch.Tensor, offsets: torch.Tensor, out: O
 
 
 def _combine(name, y, place, weights, out, out_dtype, stream):
+    if stream is None and out is None:
+        r = _lib.host().combine(y, place, weights, out_dtype)
+        if r is not None:
+            return r
     lib = _lib.load()
     T, k = _places(place)
     ld = _rows_of(name, y, TYPES, T * k)
@@ -537,6 +555,7 @@ def combine(y: torch.Tensor, place: torch.Tensor, weights: torch.Tensor, out: Op
     """out[t] = sum over j of weights[t, j] y[place[t, j]], in y's type or fp32.
 
     y [rows * k, width] fp32, bf16 or fp16, the sorted rows' results; place and weights [rows, k] as of route."""
+    _need(weights is not None, "weights must be given")
     return _combine("y", y, place, weights, out, out_dtype, stream)
 
 
@@ -544,6 +563,10 @@ def combine_backward(dout: torch.Tensor, y: torch.Tensor, place: torch.Tensor, w
                      out: Optional[torch.Tensor] = None, stream=None):
     """(dy, dweights): dy[place[t, j]] = weights[t, j] dout[t] in y's type, zero behind the last group (``out`` is for
     dy), and dweights[t, j] = <dout[t], y[place[t, j]]>.  dout is of y's type or fp32."""
+    if stream is None and out is None:
+        r = _lib.host().combine_backward(dout, y, place, weights, offsets)
+        if r is not None:
+            return r
     lib = _lib.load()
     T, k = _places(place)
     ld = _rows_of("y", y, TYPES, T * k)
@@ -592,6 +615,10 @@ def verify_drafts(logits: torch.Tensor, drafts: torch.Tensor, uniform: torch.Ten
     less draft_probs where positive after a rejection, else p.  uniform [sequences, K] in [0, 1), noise [sequences,
     classes] positive, exponential for a draw from r, both fp32.  K may be 0: one token is then drawn from p.
     allowed: a mask [classes] or [sequences, K + 1, classes], which may be expanded."""
+    if stream is None:
+        r = _lib.host().verify(logits, drafts, uniform, noise, draft_probs, temperature, allowed)
+        if r is not None:
+            return VerifiedDrafts(*r)
     lib = _lib.load()
     _need(logits.dim() == 3 and logits.shape[1] >= 1 and logits.shape[2] >= 1, "logits must be [sequences, drafts + 1, classes]")
     B, R, V = logits.shape
@@ -628,6 +655,10 @@ class GradNorm(NamedTuple):
 
 
 def _norm(grads, max_norm, learners, clip, stream):
+    if stream is None:
+        r = _lib.host().norm(grads, max_norm if max_norm is None else float(max_norm), learners, clip)
+        if r is not None:
+            return GradNorm(*r)
     lib = _lib.load()
     n = len(grads)
     _need(n >= 1, "grads must not be empty")

@@ -125,6 +125,7 @@ def test_verify_refuses(lib):
 @pytest.fixture
 def gpus(monkeypatch):
     """GPU 0 is current, the current stream of GPU d is 100 + d; results are stand-ins."""
+    ops._lib.host()
     now = [0]
     calls = Calls(now)
     made = []
@@ -296,3 +297,163 @@ def test_results_made_together(lib):
                 (like,) * 1 + ((0, 1),) * 16):
         with pytest.raises((TypeError, ValueError)):
             empties(*bad)
+
+
+# ---------------------------------------------------------------------- the host module's way and the binding's
+class Noted:
+    """A library whose calls are noted with all their arguments."""
+
+    def __init__(self):
+        self.last = None
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.last = args
+            return 0
+        return call
+
+
+class Like(Stand):
+    """A stand-in for a tensor, contiguous where that is (strides of a single element say nothing)."""
+
+    def __init__(self, t):
+        super().__init__(t.dtype, tuple(t.shape), t.stride(), t.data_ptr())
+        self.is_contiguous = t.is_contiguous
+
+
+def as_stand(t):
+    return Like(t) if isinstance(t, torch.Tensor) else t
+
+
+def both(monkeypatch, name, fast, slow, args, results):
+    """The arguments that reach the C ABI by either way (None: refused), results as their number."""
+    from paper_1903_05133_gb300 import _lib
+    host = _lib.host()
+    host.pretend(True)
+    try:
+        made = getattr(host, fast)(*args)
+    finally:
+        noted = host.pretend(False)
+    def plainly(call, outs):
+        at = {t.data_ptr(): f"result {i}" for i, t in enumerate(outs) if t is not None and t.numel()}
+        return [at.get(a, a) for a in call]
+    first = None
+    if made is not None:
+        first = plainly(noted, made if isinstance(made, tuple) else (made,))
+    library, stands = Noted(), []
+
+    def empties(like, *specs):
+        kinds = (F, BF, HF, I32, torch.uint8)
+        out = tuple(Stand(kinds[q[0]], q[1:], address=(1 << 50) + i * (1 << 40)) for i, q in enumerate(specs))
+        stands.extend(out)
+        return out
+    with monkeypatch.context() as m:
+        m.setattr(ops._lib, "load", lambda: library)
+        m.setattr(ops, "_empties", empties)
+        m.setattr(ops, "_CURRENT", lambda: 0)
+        m.setattr(ops, "_RAW_STREAM", lambda d: 0)
+        try:
+            slow(*[as_stand(a) for a in args])
+            second = plainly(library.last, stands[:results])
+        except (ValueError, AttributeError, TypeError):
+            second = None
+    return first, second, made is not None
+
+
+def same(first, second):
+    """Equal but for the workspace's address, and results without elements."""
+    if len(first) != len(second):
+        return False
+    number = lambda a: 0 if a is None else getattr(a, "value", a)  # noqa: E731
+    for a, b in zip(map(number, first), map(number, second)):
+        far = isinstance(b, int) and b >= 1 << 50
+        if a != b and not far and not (isinstance(a, str) or isinstance(b, str)):
+            return False
+    return True
+
+
+def test_the_host_module_takes_what_the_binding_takes(lib, monkeypatch):
+    """Random calls, most of them with something wrong: what the host module takes reaches the C ABI as the binding
+    would send it, and what the binding refuses it does not take."""
+    import random
+
+    from paper_1903_05133_gb300 import _lib
+    _lib.host()
+    rng = random.Random(11)
+    pick = lambda *v: rng.choice(v)  # noqa: E731
+    wrong = lambda p=0.06: rng.random() < p  # noqa: E731
+
+    def tensor(dtype, *shape):
+        """Contiguous or with gaps, sometimes of another type, size, order or none at all."""
+        if wrong(0.02):
+            return None
+        if wrong():
+            dtype = pick(torch.float64, torch.int64, torch.int16, F, BF, I32)
+        shape = [max(n + pick(-1, 1), 0) if wrong(0.03) else n for n in shape]
+        t = torch.zeros(*shape, dtype=dtype)
+        if len(shape) >= 2 and rng.random() < 0.25:
+            wide = torch.zeros(*shape[:-1], shape[-1] + 5, dtype=dtype)
+            t = wide[..., 2:2 + shape[-1]]
+        if wrong(0.03) and t.dim() >= 2:
+            t = t.transpose(-1, -2)
+        if wrong(0.03) and t.dim() >= 1:
+            t = t[..., ::2]
+        if wrong(0.02):
+            t = t.unsqueeze(0)
+        if wrong(0.03) and t.dim() >= 2:
+            t = t[:1].expand(*t.shape) if t.shape[0] else t
+        return t
+    taken = refused = 0
+    for _ in range(6000):
+        T, k, E, D, G = pick(0, 1, 2, 5, 40, 300), pick(1, 2, 3, 8), pick(1, 3, 8, 64), pick(1, 7, 16), pick(1, 4, 9)
+        B, K, V = pick(0, 1, 3), pick(0, 1, 4), pick(1, 5, 30)
+        kind, over = pick(F, BF, HF), pick(True, False)
+        word = "all" if over else "chosen"
+        out_dtype = pick(None, kind, F, HF, torch.float64)
+        temperature = pick(1.0, 0.5, 1e27, 2.0 ** -126, 0.0, -1.0, 1e28, float("nan"))
+        one, maybe = tensor, lambda *a: None if rng.random() < 0.4 else tensor(*a)  # noqa: E731
+        ok = pick(None, one(torch.bool, V), one(torch.uint8, B, K + 1, V), torch.zeros(B, 1, V, dtype=torch.bool).expand(-1, K + 1, -1),
+                  torch.zeros(V, dtype=torch.bool).expand(B, K + 1, V))
+        name, fast, slow, args, results = pick(
+            lambda: ("route", "route", lambda z, n, o, p: ops.route(z, n, over=word, learners=p),
+                     (one(kind, T, E), pick(k, 0, 33, -1) if wrong() else k, over, maybe(I32, G + 1)), 6),
+            lambda: ("route_backward", "route_backward", lambda dw, z, e, w, s, o: ops.route_backward(dw, z, e, w, lse=s, over=word),
+                     (one(F, T, k), one(kind, T, E), one(I32, T, k), one(F, T, k), maybe(F, T), over), 1),
+            lambda: ("dispatch", "dispatch", ops.dispatch, (one(kind, T, D), one(I32, T, k), one(I32, G + 1)), 1),
+            lambda: ("combine", "combine", lambda y, p, w, d: ops._combine("y", y, p, w, None, d, None),
+                     (one(kind, T * k, D), one(I32, T, k), maybe(F, T, k), out_dtype), 1),
+            lambda: ("combine_backward", "combine_backward", ops.combine_backward,
+                     (one(pick(kind, F), T, D), one(kind, T * k, D), one(I32, T, k), one(F, T, k), one(I32, G + 1)), 2),
+            lambda: ("verify_drafts", "verify", lambda z, x, u, n, q, t, a: ops.verify_drafts(z, x, u, n, draft_probs=q, temperature=t, allowed=a),
+                     (one(kind, B, K + 1, V), one(pick(I32, torch.int64), B, K), one(F, B, K), one(F, B, V),
+                      maybe(pick(F, BF, HF), B, K, V), temperature, ok), 3))()
+        first, second, went = both(monkeypatch, name, fast, slow, args, results)
+        shown = [(tuple(a.shape), a.dtype, a.stride()) if isinstance(a, torch.Tensor) else a for a in args]
+        if went:
+            assert second is not None, (name, shown)
+            assert same(first, second), (name, shown, first, second)
+            taken += 1
+        else:
+            refused += second is None
+    assert taken > 1500 and refused > 1500, (taken, refused)
+
+
+def test_norm_by_the_host_module(lib):
+    from paper_1903_05133_gb300 import _lib
+    host = _lib.host()
+    g = [torch.zeros(4, 3), torch.zeros(4, 2, dtype=BF)]
+    assert host.norm(g, 1.0, None, False) is None            # not on a GPU
+    host.pretend(True)
+    try:
+        norm, scale = host.norm(g, 2.5, 4, True)
+        assert tuple(norm.shape) == tuple(scale.shape) == (4,) and norm.dtype == scale.dtype == F
+        noted = host.pretend(True)
+        assert noted[0] == 2 and noted[4:7] == (4, 2.5, 1) and noted[7] == norm.data_ptr() and noted[8] == scale.data_ptr()
+        assert host.norm(g, None, None, False)[1] is None and host.pretend(True)[8] == 0
+        for bad in (([], 1.0, None, False), (g, -1.0, None, False), (g, float("nan"), None, False), (g, float("inf"), None, False),
+                    (g, 1, None, False), (g, 1.0, 3, False), (g, 1.0, 0, False), (g, 1.0, 2.0, False), (g + [torch.zeros(())], 1.0, 4, False),
+                    (g + [None], 1.0, None, False), (g + [torch.zeros(4, dtype=torch.float64)], 1.0, None, False),
+                    ([torch.zeros(4, 3).T], 1.0, None, False), (iter(g), 1.0, None, False), (g, 1.0, None)):
+            assert host.norm(*bad) is None, bad
+    finally:
+        host.pretend(False)
