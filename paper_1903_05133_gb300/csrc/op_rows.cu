@@ -9,7 +9,7 @@
 // All are bound by the bytes of the sorted rows.  The work goes by tokens: what belongs to a token is
 // read once, and its entries' rows, which nobody else has, by 16 bytes a thread with as many loads in
 // flight as a token has entries.  Sums are in fp32, in the order of j.  8192 tokens of 4 entries of 4096 bf16:
-// dispatch 51.3 us, combine 57.5 (336 MB: 6.5 and 5.8 TB/s, the copy's rate is 6.75), its gradient 90.0 (604 MB, 6.7).
+// dispatch 51.3 us, combine 55.1 (336 MB: 6.5 and 6.1 TB/s, the copy's rate is 6.75), its gradient 90.0 (604 MB, 6.7).
 #include <algorithm>
 #include <type_traits>
 
@@ -50,6 +50,14 @@ template <typename T, int V> struct Part {
     } else {
 #pragma unroll
       for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
+    }
+  }
+  __device__ __forceinline__ void load_once(const T* p) {   // what nobody reads again soon
+    if constexpr (V == 1) {
+      one = *p;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
     }
   }
   __device__ __forceinline__ void clear() {
@@ -164,7 +172,7 @@ __device__ __forceinline__ void combine_at(const RowArgs& a, int64_t token, int 
       const T* row = static_cast<const T*>(a.sorted) + p * a.sorted_ld;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (p >= 0 && i + u * a.lanes < parts) y[q][u].load(row + (i + u * a.lanes) * V);
+        if (p >= 0 && i + u * a.lanes < parts) y[q][u].load_once(row + (i + u * a.lanes) * V);
         else y[q][u].clear();
       }
     }
