@@ -20,7 +20,8 @@ namespace {
 
 constexpr int kThreads = 256;
 // Parts of a row that a thread has in flight at a time, for 16-byte parts and for single elements.  8192 tokens of 4 entries of
-// 4096 bf16: combine takes 57.6 us with 2 parts (four CTAs an SM; 76 with five, whose registers spill), 60.5 with one.
+// 4096 bf16: combine takes 55.1 us with 2 parts (four CTAs an SM; 76 with five, whose registers spill), 57.1 with one and 53.5
+// with four, which fewer tokens do not fill the GPU with.  Rows that are read once do not stay in L2 (58.1 where they do).
 constexpr int kWide = 2, kSingle = 8;
 
 struct RowArgs {
@@ -115,8 +116,7 @@ __device__ __forceinline__ Item item_of(const RowArgs& a) {
   return {i / a.lanes, static_cast<int>(i % a.lanes)};
 }
 
-// f(first column of the parts, number of them), U parts at a time; a row's last elements, which fill no
-// part, go to g one by one.
+// f(part) for U parts of a row at a time, `lanes` apart; a row's last elements, which fill no part, go to g one by one.
 template <int V, int U, typename F, typename G>
 __device__ __forceinline__ void each_part(int first, int lanes, int width, F f, G g) {
   const int parts = width / V;
