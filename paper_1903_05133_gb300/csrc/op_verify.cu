@@ -74,7 +74,7 @@ struct VerifyArgs {
   int64_t ok_seq, ok_row;
   int *tokens, *accepted;
   float* logp;
-  double temperature;
+  double inv_temperature;
   float c;                                // log2(e) / temperature
   float inv_t;
   float slack;                            // of bound()
@@ -114,11 +114,11 @@ __device__ __forceinline__ Sum join(Sum s, float c) {
 // log of the sum of e^(z / t), in 64 bits, by one CTA; every thread has it.
 template <typename T>
 __device__ __noinline__ double exact_lse(const VerifyArgs& a, const T* z, const uint8_t* ok, float m, double* part) {
-  const double top = static_cast<double>(m) / a.temperature;
+  const double top = m * a.inv_temperature;
   double s = 0.0;
   for (int j = threadIdx.x; j < a.classes; j += kThreads) {
     const float v = logit(z, ok, j);
-    if (v > kNone<T>) s += exp(static_cast<double>(v) / a.temperature - top);
+    if (v > kNone<T>) s += exp(fma(static_cast<double>(v), a.inv_temperature, -top));
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
@@ -259,11 +259,21 @@ __device__ __forceinline__ float rcp_fast(float x) {
   return r;
 }
 
-// The next token in 64 bits, by one CTA.
+// A row's scores r / noise, and what they may be off.
+struct Scores {
+  float m, inv_s, c, slack;
+  __device__ __forceinline__ float of(float v, float q, float e, float& off) const {
+    const float d = max_nan((v - m) * c, -1e4f), p = exp2_fast(d) * inv_s, rn = rcp_fast(e);
+    off = fmaf(fmaf(-d, 0x1p-22f, slack), p, FLT_MIN) * rn;  // bound(d) p, and what is below fp32's range
+    return fmaxf(p - q, 0.0f) * rn;
+  }
+};
+
+// The next token in 64 bits, by one CTA.  low: below it no score is the largest (not above 0: nothing is known).
 template <typename T>
-__device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const uint8_t* ok, const float* noise, float m,
-                                        int64_t q0, int x, bool rejected, double* part, int* part_index) {
-  const double lse = exact_lse(a, z, ok, m, part);
+__device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const uint8_t* ok, const float* noise, const Scores& sc,
+                                        float low, int64_t q0, int x, bool rejected, double* part, int* part_index) {
+  const double lse = exact_lse(a, z, ok, sc.m, part);
   int best = -1;
   for (int pass = rejected ? 0 : 1; pass < 2 && best < 0; ++pass) {
     double score = -1.0;
@@ -272,7 +282,12 @@ __device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const u
     for (int j = threadIdx.x; j < a.classes; j += kThreads) {
       const float v = logit(z, ok, j);
       if (!(v > kNone<T>)) continue;
-      double r = exp(static_cast<double>(v) / a.temperature - lse);
+      if (low > 0.0f) {
+        float off;
+        const float s = sc.of(v, pass == 0 && a.probs ? prob_at(a, q0 + j) : 0.0f, noise[j], off);
+        if (s + off < low) continue;
+      }
+      double r = exp(v * a.inv_temperature - lse);
       if (pass == 0) r = a.probs ? fmax(r - static_cast<double>(prob_at(a, q0 + j)), 0.0) : j == x ? 0.0 : r;
       const double s = r / static_cast<double>(noise[j]);
       any = any || r > 0.0;
@@ -368,6 +383,7 @@ __global__ void __launch_bounds__(kThreads, kResident) k_verify_next(const __gri
   __shared__ int part_index[kWarps];
   __shared__ int last_token;
   __shared__ bool is_last, unsure;
+  __shared__ float lowest;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.K, rank = blockIdx.x % a.score_parts;
   const int64_t seq = blockIdx.x / a.score_parts, row0 = seq * (K + 1);
   const float* noise = a.noise + seq * a.noise_ld;
@@ -404,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, kResident) k_verify_next(const __gri
         const T* z = logits_of<T>(a, seq, i);
         const uint8_t* ok = mask_of(a, seq, i);
         const double lse = exact_lse(a, z, ok, row_sum[r].m, part);
-        accepted = h.left < exp(static_cast<double>(h.zx) / a.temperature - lse);
+        accepted = h.left < exp(h.zx * a.inv_temperature - lse);
       }
       if (!accepted) {
         n = i;
@@ -429,13 +445,7 @@ __global__ void __launch_bounds__(kThreads, kResident) k_verify_next(const __gri
   const int hole = rejected && !a.probs ? x : -1;
   const float inv_s = 1.0f / st.S;
   const Q* qs = static_cast<const Q*>(a.probs) + q0;
-  // r / noise, and what it may be off
-  const float c = a.c, slack = a.slack * 0x1p-22f;
-  auto score = [&](float v, float q, float e, float& off) {
-    const float d = max_nan((v - st.m) * c, -1e4f), p = exp2_fast(d) * inv_s, rn = rcp_fast(e);
-    off = fmaf(fmaf(-d, 0x1p-22f, slack), p, FLT_MIN) * rn;  // bound(d) p, and what is below fp32's range
-    return fmaxf(p - q, 0.0f) * rn;
-  };
+  const Scores scores = {st.m, inv_s, a.c, a.slack * 0x1p-22f};
   Best best = {0.0f, 0.0f, -1, 0};
   // kScores classes, all loads before the first use.  A class that is masked has p = 0 and a bound next to 0, with which it wins
   // only where no other is sure to be above it, and 64 bits decide.
@@ -467,7 +477,7 @@ __global__ void __launch_bounds__(kThreads, kResident) k_verify_next(const __gri
       if (!kWhole && j >= c1) break;
       float off, vu = Elem<T>::up(v[u]);
       if ((ok && !in[u]) || j == hole) vu = -INFINITY;
-      const float s = score(vu, minus_q ? Elem<Q>::up(q[u]) : 0.0f, e[u], off), most = s + off;
+      const float s = scores.of(vu, minus_q ? Elem<Q>::up(q[u]) : 0.0f, e[u], off), most = s + off;
       // (a NaN, of a noise that is none, makes the others as good as the best)
       best.others = fmaxf(best.others, fminf(most, best.most));
       if (most > best.most) {
@@ -511,14 +521,15 @@ __global__ void __launch_bounds__(kThreads, kResident) k_verify_next(const __gri
     if (lane == 0) {
       float off = 0.0f;
       const int j = best.index;
-      if (j >= 0) score(Elem<T>::up(z[j]), minus_q ? prob_at(a, q0 + j) : 0.0f, noise[j], off);
+      if (j >= 0) scores.of(Elem<T>::up(z[j]), minus_q ? prob_at(a, q0 + j) : 0.0f, noise[j], off);
       last_token = j;
-      unsure = !dead && !(best.most - 2.0f * off > best.others);
+      lowest = best.most - 2.0f * off;
+      unsure = !dead && !(lowest > best.others);
     }
   }
   __syncthreads();
   int token = last_token;
-  if (unsure) token = exact_token(a, z, ok, noise, st.m, q0, x, rejected, part, part_index);
+  if (unsure) token = exact_token(a, z, ok, noise, scores, lowest, q0, x, rejected, part, part_index);
   for (int i = n + tid; i <= K; i += kThreads) {
     int t = -1;
     float lp = 0.0f;
@@ -608,7 +619,7 @@ extern "C" int hier_avg_verify_drafts(const void* logits_dev, int type, int64_t 
   a.tokens = tokens_dev;
   a.accepted = accepted_dev;
   a.logp = logp_dev;
-  a.temperature = temperature;
+  a.inv_temperature = 1.0 / temperature;
   a.c = static_cast<float>(1.4426950408889634 / temperature);
   a.inv_t = static_cast<float>(1.0 / temperature);
   a.slack = slack(static_cast<int>(classes), 16 / type_size(type));
