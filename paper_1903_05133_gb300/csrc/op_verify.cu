@@ -47,7 +47,7 @@ struct Best {
   int index, pad;                         // of the largest
 };
 struct Head {                             // of a row's draft
-  double left;                            // u q(x)
+  float u, q;                             // accepted while u q < p
   float zx;                               // its logit; kNone: no class, or not allowed
   int draft;                              // -1: none, INT_MAX: no class
 };
@@ -327,10 +327,9 @@ __device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const u
 // Whether a row's draft is accepted: 0, 1, or 2 where it takes 64 bits to say.
 __device__ __forceinline__ int decide(const VerifyArgs& a, const Head& h, Sum s, float none) {
   if (!(h.zx > none && s.S > 0.0f)) return 0;                // no class, or a NaN in the row
-  const float d = (h.zx - s.m) * a.c;
-  const double p = static_cast<double>(exp2_fast(d) / s.S), off = static_cast<double>(bound(d, a.slack)) * p;
-  if (fabs(h.left - p) <= off || (p < 1e-30 && h.left < 1e-30)) return 2;
-  return h.left < p;
+  const float d = (h.zx - s.m) * a.c, p = exp2_fast(d) / s.S, left = h.u * h.q;
+  if (fabsf(left - p) <= fmaf(bound(d, a.slack), p, 0x1p-23f * left) || (p < 1e-30f && left < 1e-30f)) return 2;
+  return left < p;
 }
 
 template <typename T>
@@ -350,14 +349,14 @@ __global__ void __launch_bounds__(kThreads, kResident) k_verify_sums(const __gri
   let_next_start();
   const T* z = logits_of<T>(a, seq, i);
   const uint8_t* ok = mask_of(a, seq, i);
-  Head h = {0.0, kNone<T>, -1};
+  Head h = {0.0f, 0.0f, kNone<T>, -1};
   if (rank == 0 && tid == 0) {
     const int64_t x = i < a.K ? draft_of(a, seq, i) : -1;
     if (x >= 0) {
       h.draft = x < a.classes ? static_cast<int>(x) : INT_MAX;
       if (x < a.classes) {
-        h.left = a.uniform[seq * a.K + i];
-        if (a.probs) h.left *= prob_at(a, seq * a.q_seq + i * a.q_row + x);
+        h.u = a.uniform[seq * a.K + i];
+        h.q = a.probs ? prob_at(a, seq * a.q_seq + i * a.q_row + x) : 1.0f;
         h.zx = logit(z, ok, static_cast<int>(x));
       }
     }
@@ -375,9 +374,10 @@ __global__ void __launch_bounds__(kThreads, kResident) k_verify_sums(const __gri
 // Q: the draft probabilities' type, any where there are none.
 template <typename T, typename Q>
 __global__ void __launch_bounds__(kThreads, kResident) k_verify_next(const __grid_constant__ VerifyArgs a) {
-  __shared__ Sum row_sum[kWarps];
-  __shared__ Head row_head[kWarps];
-  __shared__ int row_state[kWarps];
+  constexpr int kRows = 32;                                  // that are decided together
+  __shared__ Sum row_sum[kRows];
+  __shared__ Head row_head[kRows];
+  __shared__ int row_state[kRows];
   __shared__ Best warp_bests[kWarps];
   __shared__ double part[kWarps];
   __shared__ int part_index[kWarps];
@@ -390,25 +390,24 @@ __global__ void __launch_bounds__(kThreads, kResident) k_verify_next(const __gri
   // this CTA's classes
   const int c0 = static_cast<int>(static_cast<int64_t>(a.classes) * rank / a.score_parts);
   const int c1 = static_cast<int>(static_cast<int64_t>(a.classes) * (rank + 1) / a.score_parts);
-#pragma unroll
-  for (int u = 0; u < kScores; ++u)                          // what does not depend on n may come meanwhile
-    if (c0 + tid + u * kThreads < c1) asm volatile("prefetch.global.L2 [%0];" ::"l"(noise + c0 + tid + u * kThreads));
+  // what does not depend on n may come meanwhile, by lines
+  for (int j = c0 + 32 * tid; j < c1; j += 32 * kThreads) asm volatile("prefetch.global.L2 [%0];" ::"l"(noise + j));
   wait_for_previous();
 
   // ---- the first row whose draft is not accepted, by every CTA of the sequence
   int n = -1, drafted = -1;
   Sum st = {0.0f, 0.0f};
-  for (int i0 = 0; n < 0; i0 += kWarps) {
-    const int rows = min(kWarps, K + 1 - i0);
-    if (warp < rows) {
+  for (int i0 = 0; n < 0; i0 += kRows) {
+    const int rows = min(kRows, K + 1 - i0);
+    for (int r = warp; r < rows; r += kWarps) {
       Sum s = {kNone<T>, 0.0f};
-      if (lane < a.sum_parts) s = a.w.sums[(row0 + i0 + warp) * kSumParts + lane];
+      if (lane < a.sum_parts) s = a.w.sums[(row0 + i0 + r) * kSumParts + lane];
+      const Head h = a.w.heads[row0 + i0 + r];
       s = join(s, a.c);
       if (lane == 0) {
-        const Head h = a.w.heads[row0 + i0 + warp];
-        row_sum[warp] = s;
-        row_head[warp] = h;
-        row_state[warp] = decide(a, h, s, kNone<T>);
+        row_sum[r] = s;
+        row_head[r] = h;
+        row_state[r] = decide(a, h, s, kNone<T>);
       }
     }
     __syncthreads();
@@ -420,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, kResident) k_verify_next(const __gri
         const T* z = logits_of<T>(a, seq, i);
         const uint8_t* ok = mask_of(a, seq, i);
         const double lse = exact_lse(a, z, ok, row_sum[r].m, part);
-        accepted = h.left < exp(h.zx * a.inv_temperature - lse);
+        accepted = static_cast<double>(h.u) * h.q < exp(h.zx * a.inv_temperature - lse);
       }
       if (!accepted) {
         n = i;
