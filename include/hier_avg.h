@@ -391,8 +391,8 @@ int hier_avg_adamw_step(hier_avg_adamw* plan, const void* const* grads_dev, int 
                         double lr, double beta1, double beta2, double eps, int64_t t,
                         const float* grad_scale_dev, uint32_t seed, void* stream);
 
-/* Routing.  For each row of logits_dev [rows, experts] the k largest logits (equal ones by index), rising entries
- * of a row being their order; a logit at or below -1e30 is masked.
+/* Routing.  For each row of logits_dev [rows, experts] the k largest logits, from the largest down and equal ones by
+ * index; a logit at or below -1e30 is masked.
  *   lse = log sum_i e^{z_i};  weight_j = e^{z_j} / (sum over the chosen of e^z), or e^{z_j - lse} (over_all)
  * Entries that do not exist have expert -1 and weight 0; a row with NaN or +inf has experts -1, and NaN weights and
  * lse; a row that is masked as a whole has lse -inf.
@@ -424,7 +424,8 @@ int hier_avg_route_backward(const float* dweight_dev, const void* logits_dev, in
 
 /* Rows to their groups and back, by the places of a sort: place_dev [rows, per_row], each place in
  * [0, rows * per_row) named once, others (-1) nowhere.  offsets_dev [groups + 1]: of it only the last is read,
- * behind which the sorted rows are set to zero.
+ * behind which the sorted rows are set to zero.  (An entry is dropped by sorting again with its group below 0; where
+ * only its place is overwritten, its sorted row is not written and stays in its group.)
  *   hier_avg_dispatch          xs[place[t, j]] = x[t]
  *   hier_avg_combine           out[t] = sum over j of weight[t, j] y[place[t, j]], in the order of j in fp32
  *                              (weight_dev NULL: 1 each, which is the gradient of dispatch)

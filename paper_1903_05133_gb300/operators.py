@@ -504,7 +504,8 @@ def dispatch(x: torch.Tensor, place: torch.Tensor, offsets: torch.Tensor, out: O
              stream=None) -> torch.Tensor:
     """xs[place[t, j]] = x[t], [rows * k, width]; the rows behind the last group, offsets[-1], are zero.
 
-    x [rows, width] fp32, bf16 or fp16; place [rows, k] and offsets as of route or sort_by_group."""
+    x [rows, width] fp32, bf16 or fp16; place [rows, k] and offsets as of route or sort_by_group.  To drop an entry,
+    sort again with its group below 0: a place that is only overwritten leaves a row of its group unwritten."""
     if stream is None and out is None:
         r = _lib.host().dispatch(x, place, offsets)
         if r is not None:

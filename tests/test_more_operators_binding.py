@@ -232,6 +232,7 @@ def test_arguments_are_refused(gpus):
         lambda: ops.dispatch(x, place, off, out=S(BF, (T, D))), lambda: ops.dispatch(x, place, off, out=S(BF, (T * k, D), address=x.address)),
         lambda: ops.dispatch(S(BF, (T, D), (20, 1)), place, off), lambda: ops.dispatch(x, S(I32, (T, 0)), off),
         lambda: ops.combine(x, place, w), lambda: ops.combine(y, place, S(F, (T, 3))), lambda: ops.combine(y, place, S(BF, (T, k))),
+        lambda: ops.combine(y, place, None),
         lambda: ops.combine(y, place, w, out_dtype=HF), lambda: ops.combine(S(F, (T * k, D)), place, w, out_dtype=BF),
         lambda: ops.combine(y, place, w, out=S(F, (T, D), address=y.address)), lambda: ops.dispatch_backward(x, place),
         lambda: ops.dispatch_backward(y, place, out_dtype=HF),
