@@ -417,47 +417,89 @@ __global__ void __launch_bounds__(kBackWarps * 32) k_chunks(const __grid_constan
   if (lane == 0) a.totals[g] = carry;
 }
 
-// Ranks in a chunk become places.  SUM: the counts of all chunks are added up here, by as many threads a group as there are.
+// Ranks in a chunk become places.  SUM, for at most kSumGroups groups: the counts of all chunks are added up here, by as many threads
+// a group as there are, all loads at once, and one warp makes places of them.
 template <bool SUM>
 __global__ void __launch_bounds__(kWarps * 32) k_place(const __grid_constant__ SortArgs a) {
   __shared__ int base[kMaxGroups + 1], mine[kMaxGroups];
   __shared__ int warp_sum[32];
-  wait_for_previous();
-  const int chunk = blockIdx.x;
+  const int chunk = blockIdx.x, tid = threadIdx.x;
   const int64_t e0 = chunk * a.per, e1 = min(e0 + a.per, a.entries);
-  int next = e0 + threadIdx.x < e1 ? a.place[e0 + threadIdx.x] : -1;      // on its way meanwhile
+  int next = -1;
   if (SUM) {
-    int width = 32;                                           // threads of a part, a power of two
-    while (width < a.groups) width *= 2;
-    const int g = threadIdx.x & (width - 1), part = threadIdx.x / width, parts = blockDim.x / width;
-    for (int i = threadIdx.x; i < a.groups; i += blockDim.x) base[i] = mine[i] = 0;
+    for (int i = tid; i < a.groups; i += blockDim.x) base[i] = mine[i] = 0;
     __syncthreads();
+    wait_for_previous();
+    if (e0 + tid < e1) next = a.place[e0 + tid];              // on its way meanwhile
+    int shift = 5;                                            // threads of a part, a power of two
+    while (1 << shift < a.groups) ++shift;
+    const int g = tid & ((1 << shift) - 1), parts = static_cast<int>(blockDim.x) >> shift;
     if (g < a.groups) {
-      int all = 0, before = 0;
-#pragma unroll 8
-      for (int c = part; c < a.chunks; c += parts) {
-        const int n = a.counts[c * a.groups + g];
-        all += n;
-        before += c < chunk ? n : 0;
+      constexpr int kAtOnce = 20;                             // 152 chunks by 8 threads a group
+      for (int c0 = tid >> shift; c0 < a.chunks; c0 += parts * kAtOnce) {
+        int n[kAtOnce], all = 0, before = 0;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int c = c0 + u * parts;
+          n[u] = c < a.chunks ? a.counts[c * a.groups + g] : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          all += n[u];
+          before += c0 + u * parts < chunk ? n[u] : 0;
+        }
+        atomicAdd(base + g, all);                             // whole numbers: their order changes nothing
+        atomicAdd(mine + g, before);
       }
-      atomicAdd(base + g, all);                               // whole numbers: their order changes nothing
-      atomicAdd(mine + g, before);
+    }
+    __syncthreads();
+    if (tid < 32) {
+      constexpr int kEach = kSumGroups / 32;
+      int v[kEach], sum = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        v[i] = tid * kEach + i < a.groups ? base[tid * kEach + i] : 0;
+        sum += v[i];
+      }
+      int run = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(~0u, run, o);
+        if (tid >= o) run += x;
+      }
+      int before = run - sum;
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int at = tid * kEach + i;
+        if (at < a.groups) {
+          base[at] = before + mine[at];
+          if (chunk == 0) a.offsets[at] = before;
+        }
+        before += v[i];
+      }
+      if (tid == 31) {
+        base[a.groups] = run;
+        if (chunk == 0) a.offsets[a.groups] = run;
+      }
     }
   } else {
-    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
+    wait_for_previous();
+    if (e0 + tid < e1) next = a.place[e0 + tid];
+    for (int g = tid; g < a.groups; g += blockDim.x) {
       base[g] = a.totals[g];
       mine[g] = a.counts[static_cast<int64_t>(g) * a.chunks + chunk];
     }
+    __syncthreads();
+    block_scan(base, a.groups, warp_sum);
+    if (chunk == 0)
+      for (int g = tid; g <= a.groups; g += blockDim.x) a.offsets[g] = base[g];
+    __syncthreads();
+    for (int g = tid; g < a.groups; g += blockDim.x) base[g] += mine[g];
   }
   __syncthreads();
-  block_scan(base, a.groups, warp_sum);
   const int count = base[a.groups];
-  if (chunk == 0)
-    for (int g = threadIdx.x; g <= a.groups; g += blockDim.x) a.offsets[g] = base[g];
-  __syncthreads();
-  for (int g = threadIdx.x; g < a.groups; g += blockDim.x) base[g] += mine[g];
-  __syncthreads();
-  for (int64_t e = e0 + threadIdx.x; e < e1; e += blockDim.x) {
+  for (int64_t e = e0 + tid; e < e1; e += blockDim.x) {
     int p = next;
     if (e + blockDim.x < e1) next = a.place[e + blockDim.x];
     if (p >= 0) {
@@ -574,7 +616,7 @@ size_t sort_smem(int warps, int groups, int64_t per) {
 }
 
 // With few groups the places' kernel adds up the counts, else a third one: 1000 rows of 64 experts 7.5 us so and 8.3 with
-// three kernels, 16384 of 128 experts 15.8 and 16.0, of 200 18.9 and 16.1, of 1024 65 and 53.
+// three kernels, 16384 of 128 experts 14.3 and 16.0, of 200 18.9 and 16.1, of 1024 65 and 53.
 cudaError_t end_sort(const SortArgs& a, cudaStream_t s) {
   const unsigned chunks = static_cast<unsigned>(a.chunks);
   if (a.c_step > 1) return launch_early(k_place<true>, chunks, kWarps * 32, 0, s, a);
