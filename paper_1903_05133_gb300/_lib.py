@@ -118,8 +118,7 @@ def host():
         from . import _host as module
         lib = load()
         module.bind(*(ctypes.cast(getattr(lib, "hier_avg_" + name), c_void_p).value for name in (
-            "route", "route_backward", "dispatch", "combine", "combine_backward", "verify_drafts", "grad_norm",
-            "grad_norm_workspace")))
+            "route", "route_backward", "dispatch", "combine", "combine_backward", "verify_drafts", "grad_norm")))
         _host = module
     return _host
 

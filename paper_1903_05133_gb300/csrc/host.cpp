@@ -28,7 +28,7 @@ constexpr at::ScalarType kTypes[] = {at::kFloat, at::kBFloat16, at::kHalf, at::k
 constexpr int kF32 = 0, kI32 = 3, kU8 = 4;
 
 // The C ABI's functions, and for tests: CPU tensors stand for a GPU's, and calls are noted in `noted` instead of made.
-void *g_route, *g_route_backward, *g_dispatch, *g_combine, *g_combine_backward, *g_verify, *g_norm, *g_norm_workspace;
+void *g_route, *g_route_backward, *g_dispatch, *g_combine, *g_combine_backward, *g_verify, *g_norm;
 bool g_pretend = false;
 PyObject* g_noted = nullptr;
 
@@ -454,11 +454,12 @@ PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const double most = scaled ? PyFloat_AS_DOUBLE(args[1]) : 0.0;
   NONE_UNLESS(most >= 0.0 && most <= std::numeric_limits<double>::max());
   const int count = static_cast<int>(f.address.size());
-  I bytes = 16;
-  if (!g_pretend) {
-    const int s = invoke<int, const int*, const I*, int, I*>(g_norm_workspace, count, f.type.data(), f.elements.data(), static_cast<int>(P_), &bytes);
-    NONE_UNLESS(s == 0);
+  I total = 0, pieces = 0;                                              // no less than hier_avg_grad_norm_workspace says
+  for (int i = 0; i < count; ++i) {
+    total += f.elements[i] * (f.type[i] == kF32 ? 4 : 2);
+    pieces += f.elements[i] > 0 ? P_ : 0;
   }
+  const I bytes = 8 * (total / (total < 8192 * pieces ? 2048 : 32768) + pieces + 1);
   const auto r = results(w.device, {{kF32, {P_}}, {kF32, {P_}}, {kU8, {bytes}}});
   const int s = invoke<int, void* const*, const int*, const I*, int, double, int, float*, float*, P, I, P>(
       g_norm, count, f.address.data(), f.type.data(), f.elements.data(), static_cast<int>(P_), most, clip, data<float>(&r[0]),
@@ -474,10 +475,9 @@ PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// bind(addresses of the C ABI's functions): route, route_backward, dispatch, combine, combine_backward, verify_drafts, grad_norm,
-// grad_norm_workspace
+// bind(addresses of the C ABI's functions): route, route_backward, dispatch, combine, combine_backward, verify_drafts, grad_norm
 PyObject* bind(PyObject*, PyObject* args) {
-  void** const to[] = {&g_route, &g_route_backward, &g_dispatch, &g_combine, &g_combine_backward, &g_verify, &g_norm, &g_norm_workspace};
+  void** const to[] = {&g_route, &g_route_backward, &g_dispatch, &g_combine, &g_combine_backward, &g_verify, &g_norm};
   if (!PyTuple_Check(args) || PyTuple_GET_SIZE(args) != static_cast<Py_ssize_t>(std::size(to))) {
     PyErr_SetString(PyExc_TypeError, "bind takes the functions' addresses");
     return nullptr;

@@ -451,6 +451,18 @@ def test_norm_by_the_host_module(lib):
         noted = host.pretend(True)
         assert noted[0] == 2 and noted[4:7] == (4, 2.5, 1) and noted[7] == norm.data_ptr() and noted[8] == scale.data_ptr()
         assert host.norm(g, None, None, False)[1] is None and host.pretend(True)[8] == 0
+        # the workspace is as large as the library says, or larger
+        import random
+        rng, need = random.Random(3), ctypes.c_int64()
+        for _ in range(300):
+            P_, count, most = rng.choice((1, 1, 3, 16)), rng.randint(1, 40), rng.choice((3, 600, 5000, 100000))
+            kinds = [rng.choice((F, BF, HF)) for _ in range(count)]
+            some = [torch.empty(P_, rng.randint(0, most) // P_, dtype=d) for d in kinds]
+            assert host.norm(some, 1.0, P_, False) is not None
+            given = host.pretend(True)[10]
+            sizes, types = (ctypes.c_int64 * count)(*[t.numel() for t in some]), (ctypes.c_int * count)(*[ops.TYPES[d] for d in kinds])
+            assert lib.hier_avg_grad_norm_workspace(count, types, sizes, P_, ctypes.byref(need)) == 0
+            assert need.value <= given <= 4 * need.value + 64 * count * P_
         for bad in (([], 1.0, None, False), (g, -1.0, None, False), (g, float("nan"), None, False), (g, float("inf"), None, False),
                     (g, 1, None, False), (g, 1.0, 3, False), (g, 1.0, 0, False), (g, 1.0, 2.0, False), (g + [torch.zeros(())], 1.0, 4, False),
                     (g + [None], 1.0, None, False), (g + [torch.zeros(4, dtype=torch.float64)], 1.0, None, False),
