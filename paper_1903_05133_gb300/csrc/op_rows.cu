@@ -11,6 +11,7 @@
 // flight as a token has entries.  Sums are in fp32, in the order of j.  8192 tokens of 4 entries of 4096 bf16:
 // dispatch 51.3 us, combine 55.1 (336 MB: 6.5 and 6.1 TB/s, the copy's rate is 6.75), its gradient 90.0 (604 MB, 6.7).
 #include <algorithm>
+#include <climits>
 #include <type_traits>
 
 #include "op_common.cuh"
@@ -451,7 +452,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_combine_shifted(const __grid_co
 
 // Some lanes, a warp or a CTA an entry.
 template <typename T, typename O, int U>
-__global__ void __launch_bounds__(kThreads) k_combine_backward_shifted(const __grid_constant__ RowArgs a) {
+__global__ void __launch_bounds__(kThreads, 5) k_combine_backward_shifted(const __grid_constant__ RowArgs a) {
   constexpr int V = kVec<T>, kWords = V / kVec<O>;
   __shared__ float part[kThreads / 32];
   const Item it = item_of(a);                               // its token is an entry
@@ -522,13 +523,16 @@ bool wide(const void* p, int64_t ld, int type) {
 // Rows of a 16-bit type of at least this many 16 bytes are read by 16 bytes where they are not aligned.  (Of fp32 a warp's
 // single elements are 128 bytes already.)
 // 8192 tokens of 4 entries of 4095 bf16 so and by single elements: dispatch 78 and 148 us, its gradient 76 and 118, combine 84 and
-// 112, its gradient 143 and 209; 16384 of 65: 7.2 and 7.3, 6.6 and 6.1, 8.1 and 6.1, 9.8 and 23.7.
+// 112, its gradient 117 and 209; 16384 of 65: 7.2 and 7.3, 6.6 and 6.1, 8.1 and 6.1, 9.8 and 23.7.
 template <typename T>
 bool shifted(const RowArgs& a, int parts) { return sizeof(T) == 2 && a.width >= parts * kVec<T>; }
 constexpr int kShiftedParts = 16, kShiftedSums = 4;
-// A power of two of lanes for rows of so many parts, a CTA beyond a warp's.
-int lanes_for(int parts) {
-  if (parts > 128) return kThreads;
+// A power of two of lanes for rows of so many parts: a warp at most, and a CTA for long rows where they are few, or longer than
+// `most` parts.  Tokens of 4 entries, bf16, a CTA and a warp each: 8192 of 4096 89.9 and 94.7 us, 3001 of 1112 10.1 and 8.4, 100 of
+// 4096 3.3 and 10.5; odd entries 8192 x 4 of 4095 143 and 117, 3001 x 4 of 1111 32 and 13, 400 x 4 of 4095 8.9 and 8.8, 100 x 4 4.3 and 7.7.
+constexpr int kFewRows = 2000;
+int lanes_for(int64_t rows, int parts, int most) {
+  if (parts > 128 && (rows < kFewRows || parts > most)) return kThreads;
   int lanes = 1;
   while (lanes < 32 && lanes < parts) lanes *= 2;
   return lanes;
@@ -591,7 +595,7 @@ cudaError_t combine_type(const RowArgs& a, bool vec, cudaStream_t s) {
 
 template <typename T, typename O, int V, int U, int AT>
 cudaError_t launch_combine_backward(RowArgs a, cudaStream_t s) {
-  a.lanes = lanes_for(std::max(a.width / V, 1));
+  a.lanes = lanes_for(a.tokens, std::max(a.width / V, 1), 256);
   const int64_t ctas = (a.tokens * a.lanes + kThreads - 1) / kThreads;
   if (ctas > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
   const auto kernel = a.lanes == kThreads ? k_combine_backward<T, O, V, U, AT, true> : k_combine_backward<T, O, V, U, AT, false>;
@@ -603,7 +607,7 @@ cudaError_t combine_backward_type(const RowArgs& a, bool vec, cudaStream_t s) {
   if constexpr (sizeof(T) == 2)
     if (!vec && shifted<T>(a, kShiftedSums)) {
       RowArgs b = a;
-      b.lanes = lanes_for(a.width / kVec<T>);
+      b.lanes = lanes_for(a.entries, a.width / kVec<T>, INT_MAX);
       const int64_t ctas = (a.entries * b.lanes + kThreads - 1) / kThreads;
       if (ctas > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
       k_combine_backward_shifted<T, O, 1><<<static_cast<unsigned>(ctas), kThreads, 0, s>>>(b);
