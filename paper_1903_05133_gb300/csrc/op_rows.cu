@@ -24,6 +24,7 @@ constexpr int kThreads = 256;
 // 4096 bf16: combine takes 55.1 us with 2 parts (four CTAs an SM; 76 with five, whose registers spill), 57.1 with one and 53.5
 // with four, which fewer tokens do not fill the GPU with.  Rows that are read once do not stay in L2 (58.1 where they do).
 constexpr int kWide = 2, kSingle = 8;
+constexpr int kSingleSums = 4;            // of combine's gradient: 3001 tokens of 4 odd entries of 1111 fp32 25 us, 33 with 8
 
 struct RowArgs {
   const void* token;                      // x or dout
@@ -613,8 +614,8 @@ cudaError_t combine_backward_type(const RowArgs& a, bool vec, cudaStream_t s) {
       k_combine_backward_shifted<T, O, 1><<<static_cast<unsigned>(ctas), kThreads, 0, s>>>(b);
       return cudaGetLastError();
     }
-  if (a.k <= 4) return vec ? launch_combine_backward<T, O, kVec<T>, 1, 4>(a, s) : launch_combine_backward<T, O, 1, kSingle, 4>(a, s);
-  return vec ? launch_combine_backward<T, O, kVec<T>, 1, 8>(a, s) : launch_combine_backward<T, O, 1, kSingle / 2, 8>(a, s);
+  if (a.k <= 4) return vec ? launch_combine_backward<T, O, kVec<T>, 1, 4>(a, s) : launch_combine_backward<T, O, 1, kSingleSums, 4>(a, s);
+  return vec ? launch_combine_backward<T, O, kVec<T>, 1, 8>(a, s) : launch_combine_backward<T, O, 1, kSingleSums / 2, 8>(a, s);
 }
 
 int shape_status(int type, int64_t rows, int width, int k) {
