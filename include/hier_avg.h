@@ -464,7 +464,8 @@ int hier_avg_grad_norm(int tensors, void* const* grads_dev, const int* types, co
  *   the next token is argmax_j r_j / noise_j, the lowest index of equal ones: r = max(p_n - probs_n, 0) after a
  *   rejection (without probs: p_n without the draft; p_n where nothing is left), p_n otherwise.
  * With uniform numbers in [0, 1) and exponential noise the tokens are drawn as from the target itself; K = 0 draws
- * one token from p.  Decisions are those of 64-bit arithmetic on the given numbers.
+ * one token from p.  Decisions are those of exact arithmetic on the given numbers, unless the two sides of one are
+ * within 2^-40 of each other.
  *   logits_dev   [sequences, K + 1, classes], sequences logits_seq and rows logits_row apart
  *   drafts_dev   [sequences, K] int32 or int64 (draft_bytes 4 or 8); a draft >= classes is rejected
  *   uniform_dev  [sequences, K];  noise_dev [sequences, classes], rows noise_ld apart, positive

@@ -13,7 +13,7 @@
 // a draft has failed, and 95 by a cluster a sequence that takes its rows in turn and stops.  Both kernels are bound by the
 // instructions of an element, about as long as the memory takes (54 us against 41 for all the bytes).
 // Sums and scores are in fp32, with a bound of what that may be off; a decision within the bound is made
-// again in 64 bits, so that the tokens are those of the formulas in 64 bits.
+// again by one CTA, in 64 bits but for the sum of the exponentials, which pairs of floats hold to 2^-40.
 #include <algorithm>
 #include <cfloat>
 #include <climits>
@@ -61,6 +61,12 @@ struct Work {
 constexpr int64_t kRowBytes = sizeof(Head) + kSumParts * sizeof(Sum);
 constexpr int64_t kSequenceBytes = kScoreParts * sizeof(Best) + sizeof(int);
 
+// A number as the sum of two floats.
+struct Two {
+  float hi, lo;
+};
+__host__ __device__ constexpr Two two(double x) { return {static_cast<float>(x), static_cast<float>(x - static_cast<double>(static_cast<float>(x)))}; }
+
 struct VerifyArgs {
   const void* logits;
   int64_t z_seq, z_row;
@@ -76,6 +82,7 @@ struct VerifyArgs {
   float* logp;
   double inv_temperature;
   float c;                                // log2(e) / temperature
+  Two c2;                                 // the same
   float inv_t;
   float slack;                            // of bound()
   int K, classes;
@@ -111,23 +118,68 @@ __device__ __forceinline__ Sum join(Sum s, float c) {
   return r;
 }
 
-// log of the sum of e^(z / t), in 64 bits, by one CTA; every thread has it.
-template <typename T>
-__device__ __noinline__ double exact_lse(const VerifyArgs& a, const T* z, const uint8_t* ok, float m, double* part) {
-  const double top = m * a.inv_temperature;
-  double s = 0.0;
-  for (int j = threadIdx.x; j < a.classes; j += kThreads) {
-    const float v = logit(z, ok, j);
-    if (v > kNone<T>) s += exp(fma(static_cast<double>(v), a.inv_temperature, -top));
-  }
+// The coefficients of 2^f = sum over n of (f log 2)^n / n!.
+__host__ __device__ constexpr double power_term(int n) {
+  double a = 1.0;
+  for (int i = 1; i <= n; ++i) a = a * 0.69314718055994530942 / i;
+  return a;
+}
+// 2^((v - m) c) to about 2^-40 of it, c = c.hi + c.lo > 0 and v <= m; 0 below 2^-120.  In 64 bits the sum of 128000 takes a CTA 1.1 ms,
+// so 0.23.  The product's integer part n is taken off, f in [-1/2, 1/2] remains; the series' terms from f^8 on are below
+// 2^-27 and need one float, the others are added in two (error-free sums and products, Dekker 1971).
+__device__ __forceinline__ Two power(float v, float m, Two c) {
+  const float d = v - m, p = d * c.hi;
+  const float back = d - v, e = (v - (d - back)) + (-m - back);                // d + e = v - m
+  const float n = rintf(p), g = fmaf(d, c.lo, fmaf(d, c.hi, -p)) + e * c.hi, w = p - n, f = w + g, fl = g - (f - w);
+  float r = static_cast<float>(power_term(12));
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
+  for (int i = 11; i >= 8; --i) r = fmaf(r, f, static_cast<float>(power_term(i)));
+  Two s = {r, 0.0f};
+#pragma unroll
+  for (int i = 7; i >= 0; --i) {
+    const Two a = two(power_term(i));
+    const float h = s.hi * f, l = fmaf(s.lo, f, fmaf(s.hi, fl, fmaf(s.hi, f, -h)));
+    s.hi = a.hi + h;
+    s.lo = (h - (s.hi - a.hi)) + (l + a.lo);
+  }
+  const float scale = __int_as_float((static_cast<int>(n) + 127) << 23);
+  const bool any = p > -120.0f;                              // no branch, so that several are computed side by side
+  return {any ? s.hi * scale : 0.0f, any ? s.lo * scale : 0.0f};
+}
+
+// The sum of e^((z - m) / t) to about 2^-40, by one CTA; every thread has it.
+template <typename T>
+__device__ __noinline__ double exact_sum(const VerifyArgs& a, const T* z, const uint8_t* ok, float m, double* part) {
+  Two s = {0.0f, 0.0f};
+  constexpr int kAtOnce = 4;
+  for (int j0 = threadIdx.x; j0 < a.classes; j0 += kAtOnce * kThreads) {
+    float v[kAtOnce];
+    Two x[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) v[u] = logit(z, ok, min(j0 + u * kThreads, a.classes - 1));
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) x[u] = power(v[u], m, a.c2);
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      if (!(v[u] > kNone<T>) || j0 + u * kThreads >= a.classes) x[u] = {0.0f, 0.0f};
+      const float h = s.hi + x[u].hi, back = h - s.hi;
+      s.lo += ((s.hi - (h - back)) + (x[u].hi - back)) + x[u].lo;
+      s.hi = h;
+    }
+  }
+  double t = static_cast<double>(s.hi) + static_cast<double>(s.lo);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(~0u, t, o);
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = t;
   __syncthreads();
-  s = 0.0;
-  for (int w = 0; w < kWarps; ++w) s += part[w];
-  return top + log(s);
+  t = 0.0;
+  for (int w = 0; w < kWarps; ++w) t += part[w];
+  return t;
+}
+// A class's probability from it, in 64 bits.
+__device__ __forceinline__ double exact_prob(const VerifyArgs& a, float v, float m, double sum) {
+  return exp((static_cast<double>(v) - m) * a.inv_temperature) / sum;
 }
 
 // Two minus infinities of a 16-bit type.
@@ -269,31 +321,41 @@ struct Scores {
   }
 };
 
-// The next token in 64 bits, by one CTA.  low: below it no score is the largest (not above 0: nothing is known).
+// The next token, by one CTA, in 64 bits but for the sum.  low: below it no score is the largest (not above 0: nothing is known).
 template <typename T>
 __device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const uint8_t* ok, const float* noise, const Scores& sc,
                                         float low, int64_t q0, int x, bool rejected, double* part, int* part_index) {
-  const double lse = exact_lse(a, z, ok, sc.m, part);
+  const double sum = exact_sum(a, z, ok, sc.m, part);
   int best = -1;
   for (int pass = rejected ? 0 : 1; pass < 2 && best < 0; ++pass) {
     double score = -1.0;
     bool any = false;
     best = -1;
-    for (int j = threadIdx.x; j < a.classes; j += kThreads) {
-      const float v = logit(z, ok, j);
-      if (!(v > kNone<T>)) continue;
-      if (low > 0.0f) {
-        float off;
-        const float s = sc.of(v, pass == 0 && a.probs ? prob_at(a, q0 + j) : 0.0f, noise[j], off);
-        if (s + off < low) continue;
+    const bool minus_q = pass == 0 && a.probs;
+    constexpr int kAtOnce = 4;
+    for (int j0 = threadIdx.x; j0 < a.classes; j0 += kAtOnce * kThreads) {
+      float v[kAtOnce], e[kAtOnce], q[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int j = min(j0 + u * kThreads, a.classes - 1);
+        v[u] = logit(z, ok, j);
+        e[u] = noise[j];
+        q[u] = minus_q ? prob_at(a, q0 + j) : 0.0f;
       }
-      double r = exp(v * a.inv_temperature - lse);
-      if (pass == 0) r = a.probs ? fmax(r - static_cast<double>(prob_at(a, q0 + j)), 0.0) : j == x ? 0.0 : r;
-      const double s = r / static_cast<double>(noise[j]);
-      any = any || r > 0.0;
-      if (r > 0.0 && s >= 0.0 && s > score) {
-        score = s;
-        best = j;
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int j = j0 + u * kThreads;
+        float off;
+        const float most = sc.of(v[u], q[u], e[u], off) + off;
+        if (j >= a.classes || !(v[u] > kNone<T>) || (low > 0.0f && most < low)) continue;
+        double r = exact_prob(a, v[u], sc.m, sum);
+        if (pass == 0) r = a.probs ? fmax(r - static_cast<double>(q[u]), 0.0) : j == x ? 0.0 : r;
+        const double s = r / static_cast<double>(e[u]);
+        any = any || r > 0.0;
+        if (r > 0.0 && s >= 0.0 && s > score) {
+          score = s;
+          best = j;
+        }
       }
     }
     const int some = __syncthreads_or(any);
@@ -324,7 +386,7 @@ __device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const u
   return best;
 }
 
-// Whether a row's draft is accepted: 0, 1, or 2 where it takes 64 bits to say.
+// Whether a row's draft is accepted: 0, 1, or 2 where it takes more bits to say.
 __device__ __forceinline__ int decide(const VerifyArgs& a, const Head& h, Sum s, float none) {
   if (!(h.zx > none && s.S > 0.0f)) return 0;                // no class, or a NaN in the row
   const float d = (h.zx - s.m) * a.c, p = exp2_fast(d) / s.S, left = h.u * h.q;
@@ -418,8 +480,8 @@ __global__ void __launch_bounds__(kThreads, kResident) k_verify_next(const __gri
       if (row_state[r] == 2) {
         const T* z = logits_of<T>(a, seq, i);
         const uint8_t* ok = mask_of(a, seq, i);
-        const double lse = exact_lse(a, z, ok, row_sum[r].m, part);
-        accepted = static_cast<double>(h.u) * h.q < exp(h.zx * a.inv_temperature - lse);
+        const double sum = exact_sum(a, z, ok, row_sum[r].m, part);
+        accepted = static_cast<double>(h.u) * h.q < exact_prob(a, h.zx, row_sum[r].m, sum);
       }
       if (!accepted) {
         n = i;
@@ -447,7 +509,7 @@ __global__ void __launch_bounds__(kThreads, kResident) k_verify_next(const __gri
   const Scores scores = {st.m, inv_s, a.c, a.slack * 0x1p-22f};
   Best best = {0.0f, 0.0f, -1, 0};
   // kScores classes, all loads before the first use.  A class that is masked has p = 0 and a bound next to 0, with which it wins
-  // only where no other is sure to be above it, and 64 bits decide.
+  // only where no other is sure to be above it, and more bits decide.
   auto batch = [&](int j0, auto whole) {
     constexpr bool kWhole = decltype(whole)::value;
     T v[kScores];
@@ -619,7 +681,8 @@ extern "C" int hier_avg_verify_drafts(const void* logits_dev, int type, int64_t 
   a.accepted = accepted_dev;
   a.logp = logp_dev;
   a.inv_temperature = 1.0 / temperature;
-  a.c = static_cast<float>(1.4426950408889634 / temperature);
+  a.c2 = two(1.4426950408889634 / temperature);
+  a.c = a.c2.hi;
   a.inv_t = static_cast<float>(1.0 / temperature);
   a.slack = slack(static_cast<int>(classes), 16 / type_size(type));
   a.K = drafts;

@@ -170,6 +170,21 @@ def test_equal_scores_and_decisions_next_to_a_border():
     check(torch.full((8, 1, 500), 2.5, device="cuda"), x[:8, :0], u[:8, :0], noise)
 
 
+@pytest.mark.parametrize("dtype", [F, BF])
+@pytest.mark.parametrize("V,temperature", [(20011, 0.7), (3000, 1.0), (20011, 3.0)])
+def test_borders_of_long_rows(V, temperature, dtype):
+    # u is p's fp32 neighbours: the sum of thousands of exponentials has to be known to 2^-26 of it, and mostly far better
+    g = gen(V)
+    z = (torch.randn(48, 2, V, generator=g, device="cuda") * 2).to(dtype)
+    x = z[:, :1].argmax(2).int()
+    p = torch.softmax(z[:, 0].double() / temperature, 1).gather(1, x.long())
+    u = (p.float().view(torch.int32) + torch.randint(-1, 2, (48, 1), generator=g, device="cuda")).int().view(torch.float32)
+    noise = torch.empty(48, V, device="cuda").exponential_(generator=g)
+    check(z, x, u, noise, None, None, temperature)
+    q = torch.full((48, 1, V), 0.75, device="cuda")
+    check(z, x, (p / 0.75).float(), noise, q, None, temperature)
+
+
 def test_nothing_left_after_a_rejection():
     # q is at least p everywhere, and u says no: p is then drawn from
     z = torch.randn(6, 2, 40, generator=gen(2), device="cuda")
