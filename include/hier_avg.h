@@ -447,11 +447,11 @@ int hier_avg_combine_backward(const void* dout_dev, int dout_type, int64_t dout_
  * types[i] at grads_dev[i].  learners > 1: every tensor's first dimension is the learner's (n[i] is a multiple of
  * learners), and norm_dev and scale_dev [learners] have one of each.  clip: the gradients are then multiplied by
  * their factor in place, each rounded once; they must not share memory.  scale_dev may be NULL without clip, and
- * max_norm is then not read.  Squares are summed so that neither their size nor their number is lost: in fp32 over at most 64
- * elements and a warp, in 64 bits beyond, and in 64 bits at once where fp32's range does not hold them.
+ * max_norm is then not read.  Squares are summed so that neither their size nor their number is lost: in fp32 over at
+ * most 32 KB, in 64 bits beyond, and in 64 bits at once where fp32's range does not hold them.
  * workspace_dev: 8-byte aligned, of hier_avg_grad_norm_workspace's bytes.
- * Errors: HA_EINVAL (gradients that share memory among them), HA_EUNSUPPORTED for more than 44800 tensors or 2^31
- * chunks of 32 KB, HA_ENOMEM, HA_ECUDA. */
+ * Errors: HA_EINVAL (gradients that share memory among them), HA_EUNSUPPORTED for more than 44800 tensors, 2^46
+ * elements of one or 2^31 parts of 32 KB (2 KB of small tensors), HA_ENOMEM, HA_ECUDA. */
 int hier_avg_grad_norm_workspace(int tensors, const int* types, const int64_t* n, int learners, int64_t* bytes);
 int hier_avg_grad_norm(int tensors, void* const* grads_dev, const int* types, const int64_t* n, int learners,
                        double max_norm, int clip, float* norm_dev, float* scale_dev, void* workspace_dev,

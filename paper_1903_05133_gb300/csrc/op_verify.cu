@@ -65,7 +65,9 @@ constexpr int64_t kSequenceBytes = kScoreParts * sizeof(Best) + sizeof(int);
 struct Two {
   float hi, lo;
 };
-__host__ __device__ constexpr Two two(double x) { return {static_cast<float>(x), static_cast<float>(x - static_cast<double>(static_cast<float>(x)))}; }
+__host__ __device__ constexpr Two two(double x) {
+  return {static_cast<float>(x), static_cast<float>(x - static_cast<double>(static_cast<float>(x)))};
+}
 
 struct VerifyArgs {
   const void* logits;

@@ -66,6 +66,27 @@ def test_learners(P, shapes):
     check(grads, 1.5 * math.sqrt(n), learners=P)             # the first one's are zero, some are over it
 
 
+def test_single_numbers_and_empty_tensors():
+    one = torch.tensor(-3.0, device="cuda", dtype=HF)
+    none = torch.zeros(0, 4, device="cuda")
+    check([one, none, torch.tensor([4.0], device="cuda")], 2.5)
+    r = ops.clip_gradients([none, none.clone()], 1.0)
+    assert r.norm.item() == 0 and r.scale.item() == 1
+    r = ops.grad_norm([torch.zeros(3, 0, device="cuda")], max_norm=1.0, learners=3)
+    assert r.norm.tolist() == [0] * 3 and r.scale.tolist() == [1] * 3
+
+
+def test_the_binding_and_the_host_module_agree():
+    s = torch.cuda.current_stream()
+    for sizes, P in (([5000] * 3, None), ([64, 130] * 40, 2), ([200000, 3], None)):
+        grads = [torch.randn(P or 1, n, generator=gen(n), device="cuda").to([F, BF][i % 2]) for i, n in enumerate(sizes)]
+        a, b = ops.grad_norm(grads, 1.0, P), ops.grad_norm(grads, 1.0, P, stream=s)
+        assert torch.equal(a.norm, b.norm) and torch.equal(a.scale, b.scale)
+        other = [g.clone() for g in grads]
+        ops.clip_gradients(grads, 1.0, P), ops.clip_gradients(other, 1.0, P, stream=s)
+        assert all(torch.equal(x, y) for x, y in zip(grads, other))
+
+
 def test_one_buffer_of_odd_sizes():
     r = random.Random(4)
     for dtype in (F, BF, HF):

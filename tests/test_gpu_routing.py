@@ -410,3 +410,36 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for r, a, b in got:
         assert all(torch.equal(p, q) for p, q in zip(r, want)) and torch.equal(a, xs) and torch.equal(b, out)
+
+
+def test_the_binding_and_the_host_module_agree():
+    s = torch.cuda.current_stream()
+    for T, E, k, D in ((5, 8, 2, 40), (700, 60, 4, 129), (3000, 256, 8, 256)):
+        z = torch.randn(T, E, generator=gen(T), device="cuda").to(BF)
+        cut = torch.tensor([0, T // 3, T], dtype=torch.int32, device="cuda")
+        learners = cut if 2 * E <= 1024 else None
+        a, b = ops.route(z, k, "all", learners), ops.route(z, k, "all", learners, stream=s)
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+        x = torch.randn(T, D, generator=gen(D), device="cuda").to(BF)
+        xs = ops.dispatch(x, a.place, a.offsets)
+        assert torch.equal(xs, ops.dispatch(x, a.place, a.offsets, stream=s))
+        for d in (None, F):
+            assert torch.equal(ops.combine(xs, a.place, a.weights, out_dtype=d), ops.combine(xs, a.place, a.weights, out_dtype=d, stream=s))
+            assert torch.equal(ops.dispatch_backward(xs, a.place, out_dtype=d), ops.dispatch_backward(xs, a.place, out_dtype=d, stream=s))
+        p, q = ops.combine_backward(x, xs, a.place, a.weights, a.offsets), ops.combine_backward(x, xs, a.place, a.weights, a.offsets, stream=s)
+        assert torch.equal(p[0], q[0]) and torch.equal(p[1], q[1])
+        for over in ("chosen", "all"):
+            assert torch.equal(ops.route_backward(p[1], z, a.experts, a.weights, a.lse, over),
+                               ops.route_backward(p[1], z, a.experts, a.weights, a.lse, over, stream=s))
+
+
+def test_many_equal_logits_of_large_routers():
+    # fp32 logits of which many are equal, at widths of every kernel, with more chosen than different values
+    for T, E, k in ((50, 16, 16), (200, 64, 8), (100, 100, 8), (64, 128, 16), (70, 250, 12), (40, 128, 32), (40, 500, 20), (40, 1000, 32)):
+        g = gen(E)
+        z = torch.randint(0, 3, (T, E), generator=g, device="cuda").float()
+        z[::4] = 1.0
+        z[1::4, E // 2:] = -math.inf
+        z[2::4] = torch.randn(len(z[2::4]), E, generator=g, device="cuda")         # rows without, beside those
+        check_route(z, k, "chosen")
+        check_route(z, k, "all")
