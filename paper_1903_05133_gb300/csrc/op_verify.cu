@@ -6,11 +6,11 @@
 //   the next token is argmax_j r_j / noise_j with r = max(p_n - q_n, 0) after a rejection (p_n where that
 //   leaves nothing), else r = p_n.  With exponential noise that is a draw from r.
 //
-// Two kernels, each over as many CTAs as fill the GPU.  The first takes shares of all rows: their largest logit and the
-// sum of the exponentials.  The second joins them, finds n, and takes shares of row n's scores; the last CTA of a
-// sequence to end joins those.  Rows behind a rejected draft are summed for nothing, but a row waits for no other:
-// 128 sequences of 6 rows of 50021 fp32 logits under a mask take 54 us so, 57 where CTAs ask before they start whether
-// a draft has failed, and 95 by a cluster a sequence that takes its rows in turn and stops.  Both kernels are bound by the
+// Few and short rows are one kernel's, a CTA a sequence.  Else two, each over as many CTAs as fill the GPU.  The first takes
+// shares of all rows: their largest logit and the sum of the exponentials.  The second joins them, finds n, and takes shares of
+// row n's scores; the last CTA of a sequence to end joins those.  Rows behind a rejected draft are summed for nothing, but a row
+// waits for no other: 128 sequences of 6 rows of 50021 fp32 logits under a mask take 54 us so, 57 where CTAs ask before they start
+// whether a draft has failed, and 95 by a cluster a sequence that takes its rows in turn and stops.  Both kernels are bound by the
 // instructions of an element, about as long as the memory takes (54 us against 41 for all the bytes).
 // Sums and scores are in fp32, with a bound of what that may be off; a decision within the bound is made
 // again by one CTA, in 64 bits but for the sum of the exponentials, which pairs of floats hold to 2^-40.
@@ -27,6 +27,14 @@ namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr int kResident = 8;              // CTAs of an SM
+// A CTA of kOneThreads does a sequence by itself, and saves the second launch and its wait, up to so many classes and elements of
+// logits; more where enough sequences fill the SMs.  Above kOneSequences the CTAs of few classes are too wide (2000 sequences, 2
+// rows of 1001: 34 us, against 19.6 in two kernels).  One CTA against two kernels, bf16, in us:
+//   1 sequence, 5 rows of 1001: 5.1, 7.0;  of 8192: 7.7, 8.1;  of 16384: 11.1, 8.3;  8 sequences, 10 rows of 8192: 10.8, 10.3
+//   64 sequences, 5 rows of 1001: 6.4, 8.8;  of 16384: 14.4, 16.9;  fp32, of 32001: 24.8, 21.0;  256, 4 rows of 8192: 10.1, 16.6
+constexpr int kOneThreads = 512, kOneSequences = 512, kFilled = 64;
+constexpr int kOneClasses = 8192, kOneElements = 5 * 8192;             // of fewer than kFilled sequences
+constexpr int kManyClasses = 16384, kManyElements = 8 * 16384;
 constexpr int kUnroll = 4;                // 16-byte loads in flight of a sum
 constexpr int kScores = 4;                // classes whose scores are in flight
 constexpr int kSumParts = 32;             // CTAs of a row, at most
@@ -35,7 +43,7 @@ constexpr int kScoreParts = 128;          // CTAs of a sequence's scores, at mos
 // The relative error of a probability e^((z - m) / t) / S with d = (z - m) log2(e) / t, in steps of 2^-22: d takes
 // three roundings of 2^-24 of itself each (times ln 2: |d| / 2), 2^d one step, S the same for a mean |d| that is at most
 // log2 of the classes, 31, and a quarter step for each addition of a sum's chain.
-float slack(int classes, int elements_a_load) { return 20.0f + (classes / (kThreads * elements_a_load) + 16) * 0.25f; }
+float slack(int classes, int threads, int elements_a_load) { return 20.0f + (classes / (threads * elements_a_load) + 16) * 0.25f; }
 __device__ __forceinline__ float bound(float d, float slack) { return 0x1p-22f * (slack + fabsf(d)); }
 
 struct Sum {
@@ -150,20 +158,20 @@ __device__ __forceinline__ Two power(float v, float m, Two c) {
 }
 
 // The sum of e^((z - m) / t) to about 2^-40, by one CTA; every thread has it.
-template <typename T>
+template <typename T, int THREADS>
 __device__ __noinline__ double exact_sum(const VerifyArgs& a, const T* z, const uint8_t* ok, float m, double* part) {
   Two s = {0.0f, 0.0f};
   constexpr int kAtOnce = 4;
-  for (int j0 = threadIdx.x; j0 < a.classes; j0 += kAtOnce * kThreads) {
+  for (int j0 = threadIdx.x; j0 < a.classes; j0 += kAtOnce * THREADS) {
     float v[kAtOnce];
     Two x[kAtOnce];
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) v[u] = logit(z, ok, min(j0 + u * kThreads, a.classes - 1));
+    for (int u = 0; u < kAtOnce; ++u) v[u] = logit(z, ok, min(j0 + u * THREADS, a.classes - 1));
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) x[u] = power(v[u], m, a.c2);
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
-      if (!(v[u] > kNone<T>) || j0 + u * kThreads >= a.classes) x[u] = {0.0f, 0.0f};
+      if (!(v[u] > kNone<T>) || j0 + u * THREADS >= a.classes) x[u] = {0.0f, 0.0f};
       const float h = s.hi + x[u].hi, back = h - s.hi;
       s.lo += ((s.hi - (h - back)) + (x[u].hi - back)) + x[u].lo;
       s.hi = h;
@@ -176,7 +184,7 @@ __device__ __noinline__ double exact_sum(const VerifyArgs& a, const T* z, const 
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = t;
   __syncthreads();
   t = 0.0;
-  for (int w = 0; w < kWarps; ++w) t += part[w];
+  for (int w = 0; w < THREADS / 32; ++w) t += part[w];
   return t;
 }
 // A class's probability from it, in 64 bits.
@@ -188,12 +196,12 @@ __device__ __forceinline__ double exact_prob(const VerifyArgs& a, float v, float
 template <typename T> constexpr uint32_t kBits16 = 0xFC00FC00u;
 template <> constexpr uint32_t kBits16<__nv_bfloat16> = 0xFF80FF80u;
 
-// The sum of share `rank` of `parts` of a row, by a CTA; each warp has its own.  Minus infinity stays as it is: the
-// largest logit is kNone at least, so that its distance is no NaN and its exponential 0.
-template <typename T, bool MASK>
+// The sum of share `rank` of `parts` of a row, by THREADS threads side by side; each warp has its own.  Minus infinity stays as
+// it is: the largest logit is kNone at least, so that its distance is no NaN and its exponential 0.
+template <typename T, bool MASK, int THREADS>
 __device__ __forceinline__ Sum scan(const T* z, const uint8_t* ok, int classes, float c, int rank, int parts) {
   constexpr int V = kVec<T>;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x % THREADS;
   // The vectors start at the row's first 16-byte boundary; the entries before and after them are taken one by one.
   const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
   int head = shift ? V - shift : 0;
@@ -220,7 +228,7 @@ __device__ __forceinline__ Sum scan(const T* z, const uint8_t* ok, int classes, 
     uint32_t in[kUnroll][V / 4 + 1];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int i = r + u * kThreads;
+      const int i = r + u * THREADS;
       if (kWhole || i < v1) {
         w[u] = __ldg(zv + i);
         if (MASK) {
@@ -279,7 +287,7 @@ __device__ __forceinline__ Sum scan(const T* z, const uint8_t* ok, int classes, 
     }
   };
   int r = v0 + tid;
-  for (; r + (kUnroll - 1) * kThreads < v1; r += kUnroll * kThreads) batch(r, std::true_type());
+  for (; r + (kUnroll - 1) * THREADS < v1; r += kUnroll * THREADS) batch(r, std::true_type());
   if (r < v1) batch(r, std::false_type());
   Sum s = {m, 0.0f};
   float x, y;
@@ -324,10 +332,10 @@ struct Scores {
 };
 
 // The next token, by one CTA, in 64 bits but for the sum.  low: below it no score is the largest (not above 0: nothing is known).
-template <typename T>
+template <typename T, int THREADS>
 __device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const uint8_t* ok, const float* noise, const Scores& sc,
                                         float low, int64_t q0, int x, bool rejected, double* part, int* part_index) {
-  const double sum = exact_sum(a, z, ok, sc.m, part);
+  const double sum = exact_sum<T, THREADS>(a, z, ok, sc.m, part);
   int best = -1;
   for (int pass = rejected ? 0 : 1; pass < 2 && best < 0; ++pass) {
     double score = -1.0;
@@ -335,18 +343,18 @@ __device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const u
     best = -1;
     const bool minus_q = pass == 0 && a.probs;
     constexpr int kAtOnce = 4;
-    for (int j0 = threadIdx.x; j0 < a.classes; j0 += kAtOnce * kThreads) {
+    for (int j0 = threadIdx.x; j0 < a.classes; j0 += kAtOnce * THREADS) {
       float v[kAtOnce], e[kAtOnce], q[kAtOnce];
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
-        const int j = min(j0 + u * kThreads, a.classes - 1);
+        const int j = min(j0 + u * THREADS, a.classes - 1);
         v[u] = logit(z, ok, j);
         e[u] = noise[j];
         q[u] = minus_q ? prob_at(a, q0 + j) : 0.0f;
       }
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
-        const int j = j0 + u * kThreads;
+        const int j = j0 + u * THREADS;
         float off;
         const float most = sc.of(v[u], q[u], e[u], off) + off;
         if (j >= a.classes || !(v[u] > kNone<T>) || (low > 0.0f && most < low)) continue;
@@ -377,7 +385,7 @@ __device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const u
     __syncthreads();
     score = -1.0;
     best = -1;
-    for (int w = 0; w < kWarps; ++w)
+    for (int w = 0; w < THREADS / 32; ++w)
       if (part[w] > score || (part[w] == score && static_cast<uint32_t>(part_index[w]) < static_cast<uint32_t>(best))) {
         score = part[w];
         best = part_index[w];
@@ -404,6 +412,21 @@ __device__ __forceinline__ const uint8_t* mask_of(const VerifyArgs& a, int64_t s
   return a.allowed ? a.allowed + seq * a.ok_seq + i * a.ok_row : nullptr;
 }
 
+// What row i's draft is accepted by.
+template <typename T>
+__device__ __forceinline__ Head head_of(const VerifyArgs& a, int64_t seq, int i, const T* z, const uint8_t* ok) {
+  Head h = {0.0f, 0.0f, kNone<T>, -1};
+  const int64_t x = i < a.K ? draft_of(a, seq, i) : -1;
+  if (x < 0) return h;
+  h.draft = x < a.classes ? static_cast<int>(x) : INT_MAX;
+  if (x < a.classes) {
+    h.u = a.uniform[seq * a.K + i];
+    h.q = a.probs ? prob_at(a, seq * a.q_seq + i * a.q_row + x) : 1.0f;
+    h.zx = logit(z, ok, static_cast<int>(x));
+  }
+  return h;
+}
+
 template <typename T, bool MASK>
 __global__ void __launch_bounds__(kThreads, kResident) k_verify_sums(const __grid_constant__ VerifyArgs a) {
   __shared__ Sum warp_sum[kWarps];
@@ -413,21 +436,11 @@ __global__ void __launch_bounds__(kThreads, kResident) k_verify_sums(const __gri
   let_next_start();
   const T* z = logits_of<T>(a, seq, i);
   const uint8_t* ok = mask_of(a, seq, i);
-  Head h = {0.0f, 0.0f, kNone<T>, -1};
   if (rank == 0 && tid == 0) {
-    const int64_t x = i < a.K ? draft_of(a, seq, i) : -1;
-    if (x >= 0) {
-      h.draft = x < a.classes ? static_cast<int>(x) : INT_MAX;
-      if (x < a.classes) {
-        h.u = a.uniform[seq * a.K + i];
-        h.q = a.probs ? prob_at(a, seq * a.q_seq + i * a.q_row + x) : 1.0f;
-        h.zx = logit(z, ok, static_cast<int>(x));
-      }
-    }
-    a.w.heads[row] = h;
+    a.w.heads[row] = head_of(a, seq, i, z, ok);
     if (i == 0) a.w.done[seq] = 0;
   }
-  Sum s = scan<T, MASK>(z, ok, a.classes, a.c, rank, a.sum_parts);
+  Sum s = scan<T, MASK, kThreads>(z, ok, a.classes, a.c, rank, a.sum_parts);
   if (lane == 0) warp_sum[tid >> 5] = s;
   __syncthreads();
   if (tid >= 32) return;
@@ -435,19 +448,163 @@ __global__ void __launch_bounds__(kThreads, kResident) k_verify_sums(const __gri
   if (lane == 0) a.w.sums[row * kSumParts + rank] = s;
 }
 
-// Q: the draft probabilities' type, any where there are none.
+// Among `rows` rows from i0 on, whose states are known, the first whose draft is not accepted; `first` writes the accepted ones.
+template <typename T, int THREADS>
+__device__ __forceinline__ void first_failed(const VerifyArgs& a, int64_t seq, bool first, int i0, int rows, const Sum* row_sum,
+                                             const Head* row_head, const int* row_state, double* part, int& n, int& drafted,
+                                             Sum& st) {
+  const int64_t row0 = seq * (a.K + 1);
+  for (int r = 0; r < rows && n < 0; ++r) {
+    const int i = i0 + r;
+    const Head h = row_head[r];
+    bool accepted = row_state[r] == 1;
+    if (row_state[r] == 2) {
+      const T* z = logits_of<T>(a, seq, i);
+      const uint8_t* ok = mask_of(a, seq, i);
+      const double sum = exact_sum<T, THREADS>(a, z, ok, row_sum[r].m, part);
+      accepted = static_cast<double>(h.u) * h.q < exact_prob(a, h.zx, row_sum[r].m, sum);
+    }
+    if (!accepted) {
+      n = i;
+      st = row_sum[r];
+      drafted = h.draft;
+    } else if (first && threadIdx.x == 0) {
+      a.tokens[row0 + i] = h.draft;
+      a.logp[row0 + i] = fmaf(h.zx - row_sum[r].m, a.inv_t, -logf(row_sum[r].S));
+    }
+  }
+}
+
+// The token behind row n, by the CTAs of a sequence, each with a share of the classes from c0 to c1; the last to end writes what is
+// left.  Q: the draft probabilities' type, any where there are none.
+template <typename T, typename Q, int THREADS>
+__device__ __forceinline__ void next_token(const VerifyArgs& a, int64_t seq, int rank, int parts, int c0, int c1, int n,
+                                           int drafted, Sum st) {
+  __shared__ Best warp_bests[THREADS / 32];
+  __shared__ double part[THREADS / 32];
+  __shared__ int part_index[THREADS / 32];
+  __shared__ int last_token;
+  __shared__ bool is_last, unsure;
+  __shared__ float lowest;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.K;
+  const int64_t row0 = seq * (K + 1);
+  const float* noise = a.noise + seq * a.noise_ld;
+  const bool rejected = drafted >= 0;
+  const int x = drafted == INT_MAX ? -1 : drafted;
+  const T* z = logits_of<T>(a, seq, n);
+  const uint8_t* ok = mask_of(a, seq, n);
+  const int64_t q0 = seq * a.q_seq + n * a.q_row;
+  const bool dead = !(st.S > 0.0f);                          // no class, or a NaN
+  const bool minus_q = rejected && a.probs;
+  const int hole = rejected && !a.probs ? x : -1;
+  const float inv_s = 1.0f / st.S;
+  const Q* qs = static_cast<const Q*>(a.probs) + q0;
+  const Scores scores = {st.m, inv_s, a.c, a.slack * 0x1p-22f};
+  Best best = {0.0f, 0.0f, -1, 0};
+  // kScores classes, all loads before the first use.  A class that is masked has p = 0 and a bound next to 0, with which it wins
+  // only where no other is sure to be above it, and more bits decide.
+  auto batch = [&](int j0, auto whole) {
+    constexpr bool kWhole = decltype(whole)::value;
+    T v[kScores];
+    Q q[kScores];
+    float e[kScores];
+    uint8_t in[kScores];
+#pragma unroll
+    for (int u = 0; u < kScores; ++u)
+      if (kWhole || j0 + u * THREADS < c1) {
+        v[u] = z[j0 + u * THREADS];
+        e[u] = noise[j0 + u * THREADS];
+      }
+    if (minus_q) {
+#pragma unroll
+      for (int u = 0; u < kScores; ++u)
+        if (kWhole || j0 + u * THREADS < c1) q[u] = qs[j0 + u * THREADS];
+    }
+    if (ok) {
+#pragma unroll
+      for (int u = 0; u < kScores; ++u)
+        if (kWhole || j0 + u * THREADS < c1) in[u] = ok[j0 + u * THREADS];
+    }
+#pragma unroll
+    for (int u = 0; u < kScores; ++u) {
+      const int j = j0 + u * THREADS;
+      if (!kWhole && j >= c1) break;
+      float off, vu = Elem<T>::up(v[u]);
+      if ((ok && !in[u]) || j == hole) vu = -INFINITY;
+      const float s = scores.of(vu, minus_q ? Elem<Q>::up(q[u]) : 0.0f, e[u], off), most = s + off;
+      // (a NaN, of a noise that is none, makes the others as good as the best)
+      best.others = fmaxf(best.others, fminf(most, best.most));
+      if (most > best.most) {
+        best.most = most;
+        best.index = j;
+      }
+    }
+  };
+  if (!dead) {
+    int j0 = c0 + tid;
+    for (; j0 + (kScores - 1) * THREADS < c1; j0 += kScores * THREADS) batch(j0, std::true_type());
+    if (j0 < c1) batch(j0, std::false_type());
+  }
+  best = warp_best(best);
+  if (lane == 0) warp_bests[warp] = best;
+  __syncthreads();
+  if (warp == 0) {
+    best = warp_best(lane < THREADS / 32 ? warp_bests[lane] : Best{0.0f, 0.0f, -1, 0});
+    if (lane == 0) {
+      bool last = true;
+      if (parts > 1) {
+        a.w.bests[seq * kScoreParts + rank] = best;
+        __threadfence();
+        last = atomicAdd(a.w.done + seq, 1) == parts - 1;
+        __threadfence();
+      }
+      is_last = last;
+    }
+  }
+  __syncthreads();
+  if (!is_last) return;
+  if (warp == 0) {
+    if (parts > 1) {
+      best = {0.0f, 0.0f, -1, 0};
+      for (int r = lane; r < parts; r += 32) {
+        const int4 v = __ldcg(reinterpret_cast<const int4*>(a.w.bests + seq * kScoreParts + r));
+        best = better(best, *reinterpret_cast<const Best*>(&v));
+      }
+      best = warp_best(best);
+    }
+    if (lane == 0) {
+      float off = 0.0f;
+      const int j = best.index;
+      if (j >= 0) scores.of(Elem<T>::up(z[j]), minus_q ? prob_at(a, q0 + j) : 0.0f, noise[j], off);
+      last_token = j;
+      lowest = best.most - 2.0f * off;
+      unsure = !dead && !(lowest > best.others);
+    }
+  }
+  __syncthreads();
+  int token = last_token;
+  if (unsure) token = exact_token<T, THREADS>(a, z, ok, noise, scores, lowest, q0, x, rejected, part, part_index);
+  for (int i = n + tid; i <= K; i += THREADS) {
+    int t = -1;
+    float lp = 0.0f;
+    if (i == n) {
+      t = dead ? -1 : token;
+      if (dead) lp = st.S == 0.0f ? -INFINITY : NAN;
+      else if (t >= 0) lp = fmaf(logit(z, ok, t) - st.m, a.inv_t, -logf(st.S));
+    }
+    a.tokens[row0 + i] = t;
+    a.logp[row0 + i] = lp;
+  }
+  if (tid == 0) a.accepted[seq] = n;
+}
+
 template <typename T, typename Q>
 __global__ void __launch_bounds__(kThreads, kResident) k_verify_next(const __grid_constant__ VerifyArgs a) {
   constexpr int kRows = 32;                                  // that are decided together
   __shared__ Sum row_sum[kRows];
   __shared__ Head row_head[kRows];
   __shared__ int row_state[kRows];
-  __shared__ Best warp_bests[kWarps];
   __shared__ double part[kWarps];
-  __shared__ int part_index[kWarps];
-  __shared__ int last_token;
-  __shared__ bool is_last, unsure;
-  __shared__ float lowest;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.K, rank = blockIdx.x % a.score_parts;
   const int64_t seq = blockIdx.x / a.score_parts, row0 = seq * (K + 1);
   const float* noise = a.noise + seq * a.noise_ld;
@@ -475,136 +632,44 @@ __global__ void __launch_bounds__(kThreads, kResident) k_verify_next(const __gri
       }
     }
     __syncthreads();
-    for (int r = 0; r < rows && n < 0; ++r) {
-      const int i = i0 + r;
-      const Head h = row_head[r];
-      bool accepted = row_state[r] == 1;
-      if (row_state[r] == 2) {
-        const T* z = logits_of<T>(a, seq, i);
-        const uint8_t* ok = mask_of(a, seq, i);
-        const double sum = exact_sum(a, z, ok, row_sum[r].m, part);
-        accepted = static_cast<double>(h.u) * h.q < exact_prob(a, h.zx, row_sum[r].m, sum);
-      }
-      if (!accepted) {
-        n = i;
-        st = row_sum[r];
-        drafted = h.draft;
-      } else if (rank == 0 && tid == 0) {
-        a.tokens[row0 + i] = h.draft;
-        a.logp[row0 + i] = fmaf(h.zx - row_sum[r].m, a.inv_t, -logf(row_sum[r].S));
-      }
-    }
+    first_failed<T, kThreads>(a, seq, rank == 0, i0, rows, row_sum, row_head, row_state, part, n, drafted, st);
     __syncthreads();
   }
 
-  // ---- the token behind it
-  const bool rejected = drafted >= 0;
-  const int x = drafted == INT_MAX ? -1 : drafted;
-  const T* z = logits_of<T>(a, seq, n);
-  const uint8_t* ok = mask_of(a, seq, n);
-  const int64_t q0 = seq * a.q_seq + n * a.q_row;
-  const bool dead = !(st.S > 0.0f);                          // no class, or a NaN
-  const bool minus_q = rejected && a.probs;
-  const int hole = rejected && !a.probs ? x : -1;
-  const float inv_s = 1.0f / st.S;
-  const Q* qs = static_cast<const Q*>(a.probs) + q0;
-  const Scores scores = {st.m, inv_s, a.c, a.slack * 0x1p-22f};
-  Best best = {0.0f, 0.0f, -1, 0};
-  // kScores classes, all loads before the first use.  A class that is masked has p = 0 and a bound next to 0, with which it wins
-  // only where no other is sure to be above it, and more bits decide.
-  auto batch = [&](int j0, auto whole) {
-    constexpr bool kWhole = decltype(whole)::value;
-    T v[kScores];
-    Q q[kScores];
-    float e[kScores];
-    uint8_t in[kScores];
-#pragma unroll
-    for (int u = 0; u < kScores; ++u)
-      if (kWhole || j0 + u * kThreads < c1) {
-        v[u] = z[j0 + u * kThreads];
-        e[u] = noise[j0 + u * kThreads];
-      }
-    if (minus_q) {
-#pragma unroll
-      for (int u = 0; u < kScores; ++u)
-        if (kWhole || j0 + u * kThreads < c1) q[u] = qs[j0 + u * kThreads];
-    }
-    if (ok) {
-#pragma unroll
-      for (int u = 0; u < kScores; ++u)
-        if (kWhole || j0 + u * kThreads < c1) in[u] = ok[j0 + u * kThreads];
-    }
-#pragma unroll
-    for (int u = 0; u < kScores; ++u) {
-      const int j = j0 + u * kThreads;
-      if (!kWhole && j >= c1) break;
-      float off, vu = Elem<T>::up(v[u]);
-      if ((ok && !in[u]) || j == hole) vu = -INFINITY;
-      const float s = scores.of(vu, minus_q ? Elem<Q>::up(q[u]) : 0.0f, e[u], off), most = s + off;
-      // (a NaN, of a noise that is none, makes the others as good as the best)
-      best.others = fmaxf(best.others, fminf(most, best.most));
-      if (most > best.most) {
-        best.most = most;
-        best.index = j;
-      }
-    }
-  };
-  if (!dead) {
-    int j0 = c0 + tid;
-    for (; j0 + (kScores - 1) * kThreads < c1; j0 += kScores * kThreads) batch(j0, std::true_type());
-    if (j0 < c1) batch(j0, std::false_type());
+  next_token<T, Q, kThreads>(a, seq, rank, a.score_parts, c0, c1, n, drafted, st);
+}
+
+// Few and short rows: a CTA a sequence does it all, the rows side by side, `per` warps each.
+template <typename T, typename Q, bool MASK>
+__global__ void __launch_bounds__(kOneThreads) k_verify_one(const __grid_constant__ VerifyArgs a, int per) {
+  __shared__ Sum warp_sum[kOneThreads / 32];
+  __shared__ Sum row_sum[kOneThreads / 32];
+  __shared__ Head row_head[kOneThreads / 32];
+  __shared__ int row_state[kOneThreads / 32];
+  __shared__ double part[kOneThreads / 32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.K;
+  const int64_t seq = blockIdx.x, row0 = seq * (K + 1);
+  const int mine = warp / per;
+  if (mine <= K) {
+    const T* z = logits_of<T>(a, seq, mine);
+    const uint8_t* ok = mask_of(a, seq, mine);
+    if (lane == 0 && warp % per == 0) row_head[mine] = head_of(a, seq, mine, z, ok);
+    const Sum s = scan<T, MASK, 32>(z, ok, a.classes, a.c, warp % per, per);
+    if (lane == 0) warp_sum[warp] = s;
   }
-  best = warp_best(best);
-  if (lane == 0) warp_bests[warp] = best;
   __syncthreads();
-  if (warp == 0) {
-    best = warp_best(lane < kWarps ? warp_bests[lane] : Best{0.0f, 0.0f, -1, 0});
+  if (warp <= K) {
+    const Sum s = join(lane < per ? warp_sum[warp * per + lane] : Sum{kNone<T>, 0.0f}, a.c);
     if (lane == 0) {
-      bool last = true;
-      if (a.score_parts > 1) {
-        a.w.bests[seq * kScoreParts + rank] = best;
-        __threadfence();
-        last = atomicAdd(a.w.done + seq, 1) == a.score_parts - 1;
-        __threadfence();
-      }
-      is_last = last;
+      row_sum[warp] = s;
+      row_state[warp] = decide(a, row_head[warp], s, kNone<T>);
     }
   }
   __syncthreads();
-  if (!is_last) return;
-  if (warp == 0) {
-    if (a.score_parts > 1) {
-      best = {0.0f, 0.0f, -1, 0};
-      for (int r = lane; r < a.score_parts; r += 32) {
-        const int4 v = __ldcg(reinterpret_cast<const int4*>(a.w.bests + seq * kScoreParts + r));
-        best = better(best, *reinterpret_cast<const Best*>(&v));
-      }
-      best = warp_best(best);
-    }
-    if (lane == 0) {
-      float off = 0.0f;
-      const int j = best.index;
-      if (j >= 0) scores.of(Elem<T>::up(z[j]), minus_q ? prob_at(a, q0 + j) : 0.0f, noise[j], off);
-      last_token = j;
-      lowest = best.most - 2.0f * off;
-      unsure = !dead && !(lowest > best.others);
-    }
-  }
-  __syncthreads();
-  int token = last_token;
-  if (unsure) token = exact_token(a, z, ok, noise, scores, lowest, q0, x, rejected, part, part_index);
-  for (int i = n + tid; i <= K; i += kThreads) {
-    int t = -1;
-    float lp = 0.0f;
-    if (i == n) {
-      t = dead ? -1 : token;
-      if (dead) lp = st.S == 0.0f ? -INFINITY : NAN;
-      else if (t >= 0) lp = fmaf(logit(z, ok, t) - st.m, a.inv_t, -logf(st.S));
-    }
-    a.tokens[row0 + i] = t;
-    a.logp[row0 + i] = lp;
-  }
-  if (tid == 0) a.accepted[seq] = n;
+  int n = -1, drafted = -1;
+  Sum st = {0.0f, 0.0f};
+  first_failed<T, kOneThreads>(a, seq, true, 0, K + 1, row_sum, row_head, row_state, part, n, drafted, st);
+  next_token<T, Q, kOneThreads>(a, seq, 0, 1, 0, a.classes, n, drafted, st);
 }
 
 // CTAs a row or sequence: as many as `ctas` allow, as long as each has a few KB.
@@ -616,6 +681,23 @@ int parts_for(int64_t n, int64_t bytes, int most, int64_t ctas) {
 template <typename T>
 cudaError_t verify_type(VerifyArgs a, cudaStream_t s) {
   const int64_t bytes = a.classes * static_cast<int64_t>(sizeof(T)), rows = a.sequences * (a.K + 1);
+  const int load = 16 / static_cast<int>(sizeof(T));
+  const bool filled = a.sequences >= kFilled;
+  if (a.K < kOneThreads / 32 && a.sequences <= kOneSequences && a.classes <= (filled ? kManyClasses : kOneClasses) &&
+      (a.K + 1) * a.classes <= (filled ? kManyElements : kOneElements)) {
+    int per = 1;
+    while (2 * per * (a.K + 1) <= kOneThreads / 32) per *= 2;
+    a.slack = slack(a.classes, 32 * per, load);
+    const auto go = [&](auto mask) {
+      constexpr bool M = decltype(mask)::value;
+      return a.probs_type == HA_TYPE_BF16   ? k_verify_one<T, __nv_bfloat16, M>
+             : a.probs_type == HA_TYPE_FP16 ? k_verify_one<T, __half, M>
+                                            : k_verify_one<T, float, M>;
+    };
+    (a.allowed ? go(std::true_type()) : go(std::false_type()))<<<static_cast<unsigned>(a.sequences), kOneThreads, 0, s>>>(a, per);
+    return cudaGetLastError();
+  }
+  a.slack = slack(a.classes, kThreads, load);
   // several rounds of CTAs for the sums, one for the scores, whose CTAs all look for n first
   a.sum_parts = parts_for(rows, bytes, kSumParts, 152 * kResident * 3);
   a.score_parts = parts_for(a.sequences, a.classes * int64_t(8), kScoreParts, 152 * kResident);
@@ -686,7 +768,6 @@ extern "C" int hier_avg_verify_drafts(const void* logits_dev, int type, int64_t 
   a.c2 = two(1.4426950408889634 / temperature);
   a.c = a.c2.hi;
   a.inv_t = static_cast<float>(1.0 / temperature);
-  a.slack = slack(static_cast<int>(classes), 16 / type_size(type));
   a.K = drafts;
   a.sequences = sequences;
   const int64_t rows = sequences * (drafts + int64_t(1));

@@ -298,3 +298,27 @@ def test_captured_and_on_streams():
         graph.replay()
     fresh = check(z, x, u, noise, q, None, 0.9)
     assert all(torch.equal(a, b) for r in got for a, b in zip(r, fresh))
+
+
+@pytest.mark.parametrize("B,K,V", [(3, 15, 1), (5, 15, 2500), (7, 16, 2500), (4, 40, 333), (2, 70, 9), (1, 0, 8192), (1, 0, 8193),
+                                   (2, 4, 8192), (2, 5, 8191), (63, 1, 9000), (64, 1, 9001), (64, 0, 16384), (64, 0, 16385),
+                                   (64, 7, 16384), (65, 8, 16383), (512, 2, 257), (513, 2, 257), (1200, 1, 45)])
+def test_next_to_the_limits_of_one_kernel(B, K, V):
+    # A chain of a thread that shares a row with 31 others has V / 32 / 4 additions at most, 2500 classes: 20 of 2^-24, 5 steps of
+    # 2^-22 (16384 classes, 2 warps of 16-bit vectors: 32 of 2^-24).  The others' 24 take 1 for the power, log2(V) / 2 <= 7
+    # for the arguments, 3 at the end.
+    for dtype, probs, masked in ((BF, F, True), (F, None, False), (HF, BF, False)):
+        if V > 2500 and dtype == F and K > 5:
+            continue
+        check(*make(B, K, V, dtype, probs, masked, 1.0, B + K + V))
+
+
+def test_a_batch_has_its_sequences_tokens():
+    # 520 sequences take two kernels, 70 of them one with 512 threads each
+    z, x, u, noise, q, ok = make(520, 3, 2001, BF, HF, True, 1.0, 77, sure=False)
+    a = ops.verify_drafts(z, x, u, noise, draft_probs=q, allowed=ok)
+    for i in range(0, 520, 70):
+        b = ops.verify_drafts(*(t[i:i + 70] for t in (z, x, u, noise)), draft_probs=q[i:i + 70], allowed=ok[i:i + 70])
+        assert torch.equal(a.tokens[i:i + 70], b.tokens) and torch.equal(a.accepted[i:i + 70], b.accepted)
+        # each within 2^-22 (24 + 13 + |logp|), as above, of the same number
+        assert ((a.logp[i:i + 70] - b.logp).abs() <= 2.0 ** -21 * (37 + b.logp.abs())).all()
