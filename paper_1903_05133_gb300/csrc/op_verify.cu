@@ -134,8 +134,8 @@ __host__ __device__ constexpr double power_term(int n) {
   for (int i = 1; i <= n; ++i) a = a * 0.69314718055994530942 / i;
   return a;
 }
-// 2^((v - m) c) to about 2^-40 of it, c = c.hi + c.lo > 0 and v <= m; 0 below 2^-120.  In 64 bits the sum of 128000 takes a CTA 1.1 ms,
-// so 0.23.  The product's integer part n is taken off, f in [-1/2, 1/2] remains; the series' terms from f^8 on are below
+// 2^((v - m) c) to about 2^-40 of it, c = c.hi + c.lo > 0 and v <= m; 0 below 2^-120.  In 64 bits the sum of 128000 takes a CTA
+// 1.1 ms, so 0.23.  The product's integer part n is taken off, f in [-1/2, 1/2] remains; the series' terms from f^8 on are below
 // 2^-27 and need one float, the others are added in two (error-free sums and products, Dekker 1971).
 __device__ __forceinline__ Two power(float v, float m, Two c) {
   const float d = v - m, p = d * c.hi;
@@ -331,7 +331,40 @@ struct Scores {
   }
 };
 
-// The next token, by one CTA, in 64 bits but for the sum.  low: below it no score is the largest (not above 0: nothing is known).
+// What a row's largest score is at least, 0: nothing is known; by one CTA.  hole: a class without a score.
+template <typename T, int THREADS>
+__device__ __noinline__ float lowest_score(const VerifyArgs& a, const T* z, const uint8_t* ok, const float* noise, const Scores& sc,
+                                           int64_t q0, bool minus_q, int hole, double* part) {
+  float low = 0.0f;
+  constexpr int kAtOnce = 4;
+  for (int j0 = threadIdx.x; j0 < a.classes; j0 += kAtOnce * THREADS) {
+    float v[kAtOnce], e[kAtOnce], q[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int j = min(j0 + u * THREADS, a.classes - 1);
+      v[u] = logit(z, ok, j);
+      e[u] = noise[j];
+      q[u] = minus_q ? prob_at(a, q0 + j) : 0.0f;
+    }
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      float off;
+      const float s = sc.of(v[u], q[u], e[u], off);
+      if (min(j0 + u * THREADS, a.classes - 1) != hole) low = fmaxf(low, s - fabsf(off));
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) low = fmaxf(low, __shfl_xor_sync(~0u, low, o));
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = low;
+  __syncthreads();
+  for (int w = 0; w < THREADS / 32; ++w) low = fmaxf(low, static_cast<float>(part[w]));
+  return low;
+}
+
+// The next token, by one CTA, in 64 bits but for the sum.  low: what the largest score is at least.  Not above 0 where the class
+// that may be the largest is one of a large p next to its q, whose bound is above its score; the others then say more, and 64
+// bits are taken for few classes (2000 sequences of 4097 classes, one token decided so: 50 us; 111 by 64 bits for each class).
 template <typename T, int THREADS>
 __device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const uint8_t* ok, const float* noise, const Scores& sc,
                                         float low, int64_t q0, int x, bool rejected, double* part, int* part_index) {
@@ -342,6 +375,8 @@ __device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const u
     bool any = false;
     best = -1;
     const bool minus_q = pass == 0 && a.probs;
+    const float least = low > 0.0f ? low
+                                   : lowest_score<T, THREADS>(a, z, ok, noise, sc, q0, minus_q, pass == 0 && !a.probs ? x : -1, part);
     constexpr int kAtOnce = 4;
     for (int j0 = threadIdx.x; j0 < a.classes; j0 += kAtOnce * THREADS) {
       float v[kAtOnce], e[kAtOnce], q[kAtOnce];
@@ -357,7 +392,7 @@ __device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const u
         const int j = j0 + u * THREADS;
         float off;
         const float most = sc.of(v[u], q[u], e[u], off) + off;
-        if (j >= a.classes || !(v[u] > kNone<T>) || (low > 0.0f && most < low)) continue;
+        if (j >= a.classes || !(v[u] > kNone<T>) || (least > 0.0f && most < least)) continue;
         double r = exact_prob(a, v[u], sc.m, sum);
         if (pass == 0) r = a.probs ? fmax(r - static_cast<double>(q[u]), 0.0) : j == x ? 0.0 : r;
         const double s = r / static_cast<double>(e[u]);

@@ -322,3 +322,24 @@ def test_a_batch_has_its_sequences_tokens():
         assert torch.equal(a.tokens[i:i + 70], b.tokens) and torch.equal(a.accepted[i:i + 70], b.accepted)
         # each within 2^-22 (24 + 13 + |logp|), as above, of the same number
         assert ((a.logp[i:i + 70] - b.logp).abs() <= 2.0 ** -21 * (37 + b.logp.abs())).all()
+
+
+@pytest.mark.parametrize("B,V", [(40, 1001), (600, 1001), (20, 20011)])
+@pytest.mark.parametrize("dtype", [F, BF])
+def test_a_large_class_that_the_draft_knew(dtype, B, V):
+    # p = q but for its rounding at a class of p = 0.8 and little noise: its score's bound is above all others, its score is not
+    g = gen(B + V)
+    z = torch.randn(B, 2, V, generator=g, device="cuda")
+    at = torch.randint(1, V, (B, 1), generator=g, device="cuda")
+    z[:, 0].scatter_(1, at, math.log(V) + 1.9)
+    z = z.to(dtype)
+    p = torch.softmax(z[:, 0].double(), 1)
+    q = (p * torch.rand(B, V, generator=g, device="cuda").double() * 2).scatter(1, at, p.gather(1, at))
+    q[:, 0] = 1.0
+    x = torch.zeros(B, 1, dtype=torch.int32, device="cuda")
+    noise = torch.empty(B, V, device="cuda").exponential_(generator=g)
+    small = 10.0 ** (-9 + 6 * torch.rand(B, 1, generator=g, device="cuda"))
+    r = check(z, x, torch.full((B, 1), 0.99, device="cuda"), noise.scatter(1, at, small), q.float()[:, None])
+    assert r.accepted.eq(0).all()
+    drawn = r.tokens[:, 0] == at[:, 0]
+    assert drawn.any() and not drawn.all()
