@@ -30,9 +30,10 @@ constexpr int kResident = 8;              // CTAs of an SM
 // A CTA of kOneThreads does a sequence by itself, and saves the second launch and its wait, up to so many classes and elements of
 // logits; more where enough sequences fill the SMs.  Above kOneSequences the CTAs of few classes are too wide (2000 sequences, 2
 // rows of 1001: 34 us, against 19.6 in two kernels).  One CTA against two kernels, bf16, in us:
-//   1 sequence, 5 rows of 1001: 5.1, 7.0;  of 8192: 7.7, 8.1;  of 16384: 11.1, 8.3;  8 sequences, 10 rows of 8192: 10.8, 10.3
-//   64 sequences, 5 rows of 1001: 6.4, 8.8;  of 16384: 14.4, 16.9;  fp32, of 32001: 24.8, 21.0;  256, 4 rows of 8192: 10.1, 16.6
-constexpr int kOneThreads = 512, kOneSequences = 512, kFilled = 64;
+//   1 sequence, 5 rows of 1001: 5.4, 7.2;  of 8192: 8.1, 8.2;  of 16384: 11.1, 8.3;  8 sequences, 10 rows of 8192: 10.8, 10.3
+//   64 sequences, 5 rows of 1001: 6.6, 8.8;  of 16384: 15.0, 16.6;  fp32, of 32001: 24.8, 21.0;  256, 4 rows of 8192: 11.0, 16.4
+// Two CTAs an SM: one takes 13.9 us for the last, three spill, 12.2.
+constexpr int kOneThreads = 512, kOneResident = 2, kOneSequences = 512, kFilled = 64;
 constexpr int kOneClasses = 8192, kOneElements = 5 * 8192;             // of fewer than kFilled sequences
 constexpr int kManyClasses = 16384, kManyElements = 8 * 16384;
 constexpr int kUnroll = 4;                // 16-byte loads in flight of a sum
@@ -98,6 +99,7 @@ struct VerifyArgs {
   int K, classes;
   int64_t sequences;
   int sum_parts, score_parts;
+  int per;                                // warps of a row, where one CTA does the sequence
   Work w;
   bool wide_drafts;
   int probs_type;                         // -1: none
@@ -483,47 +485,93 @@ __global__ void __launch_bounds__(kThreads, kResident) k_verify_sums(const __gri
   if (lane == 0) a.w.sums[row * kSumParts + rank] = s;
 }
 
-// Among `rows` rows from i0 on, whose states are known, the first whose draft is not accepted; `first` writes the accepted ones.
-template <typename T, int THREADS>
-__device__ __forceinline__ void first_failed(const VerifyArgs& a, int64_t seq, bool first, int i0, int rows, const Sum* row_sum,
-                                             const Head* row_head, const int* row_state, double* part, int& n, int& drafted,
-                                             Sum& st) {
-  const int64_t row0 = seq * (a.K + 1);
-  for (int r = 0; r < rows && n < 0; ++r) {
-    const int i = i0 + r;
-    const Head h = row_head[r];
-    bool accepted = row_state[r] == 1;
-    if (row_state[r] == 2) {
-      const T* z = logits_of<T>(a, seq, i);
-      const uint8_t* ok = mask_of(a, seq, i);
-      const double sum = exact_sum<T, THREADS>(a, z, ok, row_sum[r].m, part);
-      accepted = static_cast<double>(h.u) * h.q < exact_prob(a, h.zx, row_sum[r].m, sum);
-    }
-    if (!accepted) {
-      n = i;
-      st = row_sum[r];
-      drafted = h.draft;
-    } else if (first && threadIdx.x == 0) {
-      a.tokens[row0 + i] = h.draft;
-      a.logp[row0 + i] = fmaf(h.zx - row_sum[r].m, a.inv_t, -logf(row_sum[r].S));
-    }
-  }
-}
-
-// The token behind row n, by the CTAs of a sequence, each with a share of the classes from c0 to c1; the last to end writes what is
-// left.  Q: the draft probabilities' type, any where there are none.
-template <typename T, typename Q, int THREADS>
-__device__ __forceinline__ void next_token(const VerifyArgs& a, int64_t seq, int rank, int parts, int c0, int c1, int n,
-                                           int drafted, Sum st) {
+// What follows the sums; ONE: few and short rows, and their sums too, a CTA a sequence, the rows side by side, a.per warps each.
+// Q: the draft probabilities' type, any where there are none.  (One function: cut into several, the scores of 128 sequences of
+// 50021 classes took 27 us, not 22, as the registers do not hold all.)
+template <typename T, typename Q, bool ONE, bool MASK>
+__global__ void __launch_bounds__(ONE ? kOneThreads : kThreads, ONE ? kOneResident : kResident)
+    k_verify_next(const __grid_constant__ VerifyArgs a) {
+  constexpr int THREADS = ONE ? kOneThreads : kThreads, kRows = ONE ? THREADS / 32 : 32;        // rows that are decided together
+  __shared__ Sum row_sum[kRows];
+  __shared__ Head row_head[kRows];
+  __shared__ int row_state[kRows];
   __shared__ Best warp_bests[THREADS / 32];
   __shared__ double part[THREADS / 32];
   __shared__ int part_index[THREADS / 32];
   __shared__ int last_token;
   __shared__ bool is_last, unsure;
   __shared__ float lowest;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.K;
-  const int64_t row0 = seq * (K + 1);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.K, parts = ONE ? 1 : a.score_parts;
+  const int rank = ONE ? 0 : blockIdx.x % parts;
+  const int64_t seq = ONE ? blockIdx.x : blockIdx.x / parts, row0 = seq * (K + 1);
   const float* noise = a.noise + seq * a.noise_ld;
+  // this CTA's classes
+  const int c0 = static_cast<int>(static_cast<int64_t>(a.classes) * rank / parts);
+  const int c1 = static_cast<int>(static_cast<int64_t>(a.classes) * (rank + 1) / parts);
+  if constexpr (ONE) {
+    __shared__ Sum warp_sum[THREADS / 32];
+    const int per = a.per, mine = warp / per;
+    if (mine <= K) {
+      const T* z = logits_of<T>(a, seq, mine);
+      const uint8_t* ok = mask_of(a, seq, mine);
+      if (lane == 0 && warp % per == 0) row_head[mine] = head_of(a, seq, mine, z, ok);
+      const Sum s = scan<T, MASK, 32>(z, ok, a.classes, a.c, warp % per, per);
+      if (lane == 0) warp_sum[warp] = s;
+    }
+    __syncthreads();
+    if (warp <= K) {
+      const Sum s = join(lane < per ? warp_sum[warp * per + lane] : Sum{kNone<T>, 0.0f}, a.c);
+      if (lane == 0) {
+        row_sum[warp] = s;
+        row_state[warp] = decide(a, row_head[warp], s, kNone<T>);
+      }
+    }
+  } else {
+    // what does not depend on n may come meanwhile, by lines
+    for (int j = c0 + 32 * tid; j < c1; j += 32 * THREADS) asm volatile("prefetch.global.L2 [%0];" ::"l"(noise + j));
+    wait_for_previous();
+  }
+
+  // ---- the first row whose draft is not accepted, by every CTA of the sequence
+  int n = -1, drafted = -1;
+  Sum st = {0.0f, 0.0f};
+  for (int i0 = 0; n < 0; i0 += kRows) {
+    const int rows = min(kRows, K + 1 - i0);
+    for (int r = ONE ? rows : warp; r < rows; r += THREADS / 32) {
+      Sum s = {kNone<T>, 0.0f};
+      if (lane < a.sum_parts) s = a.w.sums[(row0 + i0 + r) * kSumParts + lane];
+      const Head h = a.w.heads[row0 + i0 + r];
+      s = join(s, a.c);
+      if (lane == 0) {
+        row_sum[r] = s;
+        row_head[r] = h;
+        row_state[r] = decide(a, h, s, kNone<T>);
+      }
+    }
+    __syncthreads();
+    for (int r = 0; r < rows && n < 0; ++r) {
+      const int i = i0 + r;
+      const Head h = row_head[r];
+      bool accepted = row_state[r] == 1;
+      if (row_state[r] == 2) {
+        const T* z = logits_of<T>(a, seq, i);
+        const uint8_t* ok = mask_of(a, seq, i);
+        const double sum = exact_sum<T, THREADS>(a, z, ok, row_sum[r].m, part);
+        accepted = static_cast<double>(h.u) * h.q < exact_prob(a, h.zx, row_sum[r].m, sum);
+      }
+      if (!accepted) {
+        n = i;
+        st = row_sum[r];
+        drafted = h.draft;
+      } else if (rank == 0 && tid == 0) {
+        a.tokens[row0 + i] = h.draft;
+        a.logp[row0 + i] = fmaf(h.zx - row_sum[r].m, a.inv_t, -logf(row_sum[r].S));
+      }
+    }
+    __syncthreads();
+  }
+
+  // ---- the token behind it
   const bool rejected = drafted >= 0;
   const int x = drafted == INT_MAX ? -1 : drafted;
   const T* z = logits_of<T>(a, seq, n);
@@ -633,80 +681,6 @@ __device__ __forceinline__ void next_token(const VerifyArgs& a, int64_t seq, int
   if (tid == 0) a.accepted[seq] = n;
 }
 
-template <typename T, typename Q>
-__global__ void __launch_bounds__(kThreads, kResident) k_verify_next(const __grid_constant__ VerifyArgs a) {
-  constexpr int kRows = 32;                                  // that are decided together
-  __shared__ Sum row_sum[kRows];
-  __shared__ Head row_head[kRows];
-  __shared__ int row_state[kRows];
-  __shared__ double part[kWarps];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.K, rank = blockIdx.x % a.score_parts;
-  const int64_t seq = blockIdx.x / a.score_parts, row0 = seq * (K + 1);
-  const float* noise = a.noise + seq * a.noise_ld;
-  // this CTA's classes
-  const int c0 = static_cast<int>(static_cast<int64_t>(a.classes) * rank / a.score_parts);
-  const int c1 = static_cast<int>(static_cast<int64_t>(a.classes) * (rank + 1) / a.score_parts);
-  // what does not depend on n may come meanwhile, by lines
-  for (int j = c0 + 32 * tid; j < c1; j += 32 * kThreads) asm volatile("prefetch.global.L2 [%0];" ::"l"(noise + j));
-  wait_for_previous();
-
-  // ---- the first row whose draft is not accepted, by every CTA of the sequence
-  int n = -1, drafted = -1;
-  Sum st = {0.0f, 0.0f};
-  for (int i0 = 0; n < 0; i0 += kRows) {
-    const int rows = min(kRows, K + 1 - i0);
-    for (int r = warp; r < rows; r += kWarps) {
-      Sum s = {kNone<T>, 0.0f};
-      if (lane < a.sum_parts) s = a.w.sums[(row0 + i0 + r) * kSumParts + lane];
-      const Head h = a.w.heads[row0 + i0 + r];
-      s = join(s, a.c);
-      if (lane == 0) {
-        row_sum[r] = s;
-        row_head[r] = h;
-        row_state[r] = decide(a, h, s, kNone<T>);
-      }
-    }
-    __syncthreads();
-    first_failed<T, kThreads>(a, seq, rank == 0, i0, rows, row_sum, row_head, row_state, part, n, drafted, st);
-    __syncthreads();
-  }
-
-  next_token<T, Q, kThreads>(a, seq, rank, a.score_parts, c0, c1, n, drafted, st);
-}
-
-// Few and short rows: a CTA a sequence does it all, the rows side by side, `per` warps each.
-template <typename T, typename Q, bool MASK>
-__global__ void __launch_bounds__(kOneThreads) k_verify_one(const __grid_constant__ VerifyArgs a, int per) {
-  __shared__ Sum warp_sum[kOneThreads / 32];
-  __shared__ Sum row_sum[kOneThreads / 32];
-  __shared__ Head row_head[kOneThreads / 32];
-  __shared__ int row_state[kOneThreads / 32];
-  __shared__ double part[kOneThreads / 32];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.K;
-  const int64_t seq = blockIdx.x, row0 = seq * (K + 1);
-  const int mine = warp / per;
-  if (mine <= K) {
-    const T* z = logits_of<T>(a, seq, mine);
-    const uint8_t* ok = mask_of(a, seq, mine);
-    if (lane == 0 && warp % per == 0) row_head[mine] = head_of(a, seq, mine, z, ok);
-    const Sum s = scan<T, MASK, 32>(z, ok, a.classes, a.c, warp % per, per);
-    if (lane == 0) warp_sum[warp] = s;
-  }
-  __syncthreads();
-  if (warp <= K) {
-    const Sum s = join(lane < per ? warp_sum[warp * per + lane] : Sum{kNone<T>, 0.0f}, a.c);
-    if (lane == 0) {
-      row_sum[warp] = s;
-      row_state[warp] = decide(a, row_head[warp], s, kNone<T>);
-    }
-  }
-  __syncthreads();
-  int n = -1, drafted = -1;
-  Sum st = {0.0f, 0.0f};
-  first_failed<T, kOneThreads>(a, seq, true, 0, K + 1, row_sum, row_head, row_state, part, n, drafted, st);
-  next_token<T, Q, kOneThreads>(a, seq, 0, 1, 0, a.classes, n, drafted, st);
-}
-
 // CTAs a row or sequence: as many as `ctas` allow, as long as each has a few KB.
 int parts_for(int64_t n, int64_t bytes, int most, int64_t ctas) {
   const int64_t parts = std::min(std::min<int64_t>(ctas / n, most), bytes / 4096);
@@ -720,16 +694,16 @@ cudaError_t verify_type(VerifyArgs a, cudaStream_t s) {
   const bool filled = a.sequences >= kFilled;
   if (a.K < kOneThreads / 32 && a.sequences <= kOneSequences && a.classes <= (filled ? kManyClasses : kOneClasses) &&
       (a.K + 1) * a.classes <= (filled ? kManyElements : kOneElements)) {
-    int per = 1;
-    while (2 * per * (a.K + 1) <= kOneThreads / 32) per *= 2;
-    a.slack = slack(a.classes, 32 * per, load);
+    a.per = 1;
+    while (2 * a.per * (a.K + 1) <= kOneThreads / 32) a.per *= 2;
+    a.slack = slack(a.classes, 32 * a.per, load);
     const auto go = [&](auto mask) {
       constexpr bool M = decltype(mask)::value;
-      return a.probs_type == HA_TYPE_BF16   ? k_verify_one<T, __nv_bfloat16, M>
-             : a.probs_type == HA_TYPE_FP16 ? k_verify_one<T, __half, M>
-                                            : k_verify_one<T, float, M>;
+      return a.probs_type == HA_TYPE_BF16   ? k_verify_next<T, __nv_bfloat16, true, M>
+             : a.probs_type == HA_TYPE_FP16 ? k_verify_next<T, __half, true, M>
+                                            : k_verify_next<T, float, true, M>;
     };
-    (a.allowed ? go(std::true_type()) : go(std::false_type()))<<<static_cast<unsigned>(a.sequences), kOneThreads, 0, s>>>(a, per);
+    (a.allowed ? go(std::true_type()) : go(std::false_type()))<<<static_cast<unsigned>(a.sequences), kOneThreads, 0, s>>>(a);
     return cudaGetLastError();
   }
   a.slack = slack(a.classes, kThreads, load);
@@ -740,9 +714,9 @@ cudaError_t verify_type(VerifyArgs a, cudaStream_t s) {
   sums<<<static_cast<unsigned>(rows * a.sum_parts), kThreads, 0, s>>>(a);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const auto next = a.probs_type == HA_TYPE_BF16   ? k_verify_next<T, __nv_bfloat16>
-                    : a.probs_type == HA_TYPE_FP16 ? k_verify_next<T, __half>
-                                                   : k_verify_next<T, float>;
+  const auto next = a.probs_type == HA_TYPE_BF16   ? k_verify_next<T, __nv_bfloat16, false, false>
+                    : a.probs_type == HA_TYPE_FP16 ? k_verify_next<T, __half, false, false>
+                                                   : k_verify_next<T, float, false, false>;
   return launch_early(next, static_cast<unsigned>(a.sequences * a.score_parts), kThreads, 0, s, a);
 }
 
