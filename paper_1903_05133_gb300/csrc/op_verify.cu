@@ -323,6 +323,9 @@ __device__ __forceinline__ float rcp_fast(float x) {
   return r;
 }
 
+// Scores below this are not told apart in fp32: the reciprocal of a noise above 2^126 is 0 here, and the score, at most 2^-126, is lost
+// with its bound; products below 2^-126 lose bits that no bound counts.  Above it, what the bounds say is so.
+constexpr float kLowScore = 0x1p-125f;
 // A row's scores r / noise, and what they may be off.
 struct Scores {
   float m, inv_s, c, slack;
@@ -333,7 +336,7 @@ struct Scores {
   }
 };
 
-// What a row's largest score is at least, 0: nothing is known; by one CTA.  hole: a class without a score.
+// What a row's largest score is at least, if above kLowScore; by one CTA.  hole: a class without a score.
 template <typename T, int THREADS>
 __device__ __noinline__ float lowest_score(const VerifyArgs& a, const T* z, const uint8_t* ok, const float* noise, const Scores& sc,
                                            int64_t q0, bool minus_q, int hole, double* part) {
@@ -364,8 +367,8 @@ __device__ __noinline__ float lowest_score(const VerifyArgs& a, const T* z, cons
   return low;
 }
 
-// The next token, by one CTA, in 64 bits but for the sum.  low: what the largest score is at least.  Not above 0 where the class
-// that may be the largest is one of a large p next to its q, whose bound is above its score; the others then say more, and 64
+// The next token, by one CTA, in 64 bits but for the sum.  low: what the largest score is at least.  Not above kLowScore where the
+// class that may be the largest is one of a large p next to its q, whose bound is above its score; the others then say more, and 64
 // bits are taken for few classes (2000 sequences of 4097 classes, one token decided so: 50 us; 111 by 64 bits for each class).
 template <typename T, int THREADS>
 __device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const uint8_t* ok, const float* noise, const Scores& sc,
@@ -377,8 +380,8 @@ __device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const u
     bool any = false;
     best = -1;
     const bool minus_q = pass == 0 && a.probs;
-    const float least = low > 0.0f ? low
-                                   : lowest_score<T, THREADS>(a, z, ok, noise, sc, q0, minus_q, pass == 0 && !a.probs ? x : -1, part);
+    const float least = low > kLowScore
+                            ? low : lowest_score<T, THREADS>(a, z, ok, noise, sc, q0, minus_q, pass == 0 && !a.probs ? x : -1, part);
     constexpr int kAtOnce = 4;
     for (int j0 = threadIdx.x; j0 < a.classes; j0 += kAtOnce * THREADS) {
       float v[kAtOnce], e[kAtOnce], q[kAtOnce];
@@ -394,7 +397,7 @@ __device__ __noinline__ int exact_token(const VerifyArgs& a, const T* z, const u
         const int j = j0 + u * THREADS;
         float off;
         const float most = sc.of(v[u], q[u], e[u], off) + off;
-        if (j >= a.classes || !(v[u] > kNone<T>) || (least > 0.0f && most < least)) continue;
+        if (j >= a.classes || !(v[u] > kNone<T>) || (least > kLowScore && most < least)) continue;
         double r = exact_prob(a, v[u], sc.m, sum);
         if (pass == 0) r = a.probs ? fmax(r - static_cast<double>(q[u]), 0.0) : j == x ? 0.0 : r;
         const double s = r / static_cast<double>(e[u]);
@@ -661,7 +664,7 @@ __global__ void __launch_bounds__(ONE ? kOneThreads : kThreads, ONE ? kOneReside
       if (j >= 0) scores.of(Elem<T>::up(z[j]), minus_q ? prob_at(a, q0 + j) : 0.0f, noise[j], off);
       last_token = j;
       lowest = best.most - 2.0f * off;
-      unsure = !dead && !(lowest > best.others);
+      unsure = !dead && !(lowest > fmaxf(best.others, kLowScore));
     }
   }
   __syncthreads();

@@ -1,0 +1,54 @@
+"""Where the routing, row, norm and draft operators can go wrong: noise and masks at the ends of their ranges, results
+that are kept, values that must not vanish."""
+import math
+
+import pytest
+import torch
+
+from paper_1903_05133_gb300 import operators as ops
+from test_gpu_operators import BF, F, HF
+from test_gpu_verify_drafts import check, gen, make
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _cuda(lib):
+    assert torch.cuda.is_available(), "GPU tests need CUDA"
+
+
+# Sequences and classes of one kernel, of two, and of two with many CTAs a sequence.
+SIZES = [(6, 2), (6, 300), (600, 50), (3, 40001)]
+
+
+@pytest.mark.parametrize("dtype", [F, BF, HF])
+@pytest.mark.parametrize("B,V", SIZES)
+def test_noise_of_any_size(B, V, dtype):
+    # a class of p = 1 beside one of p = 1e-6, both with noise whose reciprocal is below the normal range of fp32
+    z = torch.full((B, 1, V), -math.inf, device="cuda")
+    z[:, 0, 0], z[:, 0, V - 1] = 0.0, -13.8
+    none = torch.zeros(B, 0, device="cuda")
+    noise = torch.ones(B, V, device="cuda")
+    noise[:, 0], noise[:, V - 1] = 1e38, 8e37
+    r = check(z.to(dtype), none.int(), none, noise)
+    assert (r.tokens == 0).all()
+    # scores over the whole range of positive fp32 numbers, and beyond where they are the largest
+    g = gen(V)
+    for low, high in ((-149, 127), (100, 127), (126, 127.99), (-149, -120)):
+        power = torch.rand(B, V, generator=g, device="cuda", dtype=torch.float64) * (high - low) + low
+        noise = (2.0 ** power).float()
+        for probs, masked in ((F, True), (None, False)):
+            z, x, u, _, q, ok = make(B, 1, V, dtype, probs, masked, 1.0, V, sure=False)
+            check(z * 4, x, u, noise, q, ok)
+            check(z * 4, x, torch.ones_like(u), noise, q, ok)
+
+
+@pytest.mark.parametrize("B,V", SIZES)
+def test_noise_next_to_the_largest_number(B, V):
+    # all scores are subnormal: neighbours are told apart all the same
+    g = gen(V)
+    most = torch.finfo(F).max
+    noise = most * (1 - torch.rand(B, V, generator=g, device="cuda") * 1e-3)
+    none = torch.zeros(B, 0, device="cuda")
+    check(torch.randn(B, 1, V, generator=g, device="cuda") * 1e-3, none.int(), none, noise)
+    check(torch.zeros(B, 1, V, device="cuda"), none.int(), none, torch.full((B, V), most, device="cuda"))
