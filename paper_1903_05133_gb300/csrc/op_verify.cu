@@ -661,7 +661,8 @@ __global__ void __launch_bounds__(ONE ? kOneThreads : kThreads, ONE ? kOneReside
     if (lane == 0) {
       float off = 0.0f;
       const int j = best.index;
-      if (j >= 0) scores.of(Elem<T>::up(z[j]), minus_q ? prob_at(a, q0 + j) : 0.0f, noise[j], off);
+      // as it was scored: a class that is masked, or the draft itself, may have won by its bound
+      if (j >= 0) scores.of(j == hole ? -INFINITY : logit(z, ok, j), minus_q ? prob_at(a, q0 + j) : 0.0f, noise[j], off);
       last_token = j;
       lowest = best.most - 2.0f * off;
       unsure = !dead && !(lowest > fmaxf(best.others, kLowScore));

@@ -52,3 +52,25 @@ def test_noise_next_to_the_largest_number(B, V):
     none = torch.zeros(B, 0, device="cuda")
     check(torch.randn(B, 1, V, generator=g, device="cuda") * 1e-3, none.int(), none, noise)
     check(torch.zeros(B, 1, V, device="cuda"), none.int(), none, torch.full((B, V), most, device="cuda"))
+
+
+@pytest.mark.parametrize("above", [20.0, 60.0, 200.0])
+@pytest.mark.parametrize("dtype", [F, BF, HF])
+@pytest.mark.parametrize("B,V", [(6, 40), (600, 40), (6, 20011)])
+def test_the_only_class_rejected_beside_masked_ones_far_above_it(B, V, dtype, above):
+    # nothing is left of p but the draft itself; the masked logits say nothing, however large they are
+    g = gen(V)
+    z = (torch.randn(B, 2, V, generator=g, device="cuda") + above).to(dtype)
+    z[:, :, 5] = 0.0
+    ok = torch.zeros(V, dtype=torch.bool, device="cuda")
+    ok[5] = True
+    x = torch.full((B, 1), 5, dtype=torch.int32, device="cuda")
+    u = torch.ones(B, 1, device="cuda")                      # not below p = 1
+    noise = torch.empty(B, V, device="cuda").exponential_(generator=g)
+    r = check(z, x, u, noise, None, ok.expand(B, 2, V))
+    assert (r.tokens[:, 0] == 5).all() and (r.logp[:, 0] == 0).all()
+    # and where the draft is the largest but one of two allowed
+    ok[7] = True
+    z[:, :, 7] = -9.0
+    r = check(z, x, u, noise, None, ok.expand(B, 2, V))
+    assert (r.tokens[:, 0] == 7).all()
