@@ -122,6 +122,11 @@ __device__ __forceinline__ float logit(const T* z, const uint8_t* ok, int j) {
   return ok && !ok[j] ? kNone<T> : v;
 }
 
+// Is a row's largest logit so close to a mask's that masked exponentials do not vanish?  (fp32's numbers are 2^76 apart there, so that
+// it takes temperatures above 2^69.)  Its sum is then taken again without them, and 64 bits decide its token.
+template <typename T>
+__device__ __forceinline__ bool near_masked(float m, float c) { return c < 0x1p-68f && (kNone<T> - m) * c > -150.0f; }
+
 __device__ __forceinline__ Sum join(Sum s, float c) {
   const float m = from_ordered(__reduce_max_sync(~0u, ordered(s.m)));
   Sum r = {m, s.S * exp2_fast(max_nan((s.m - m) * c, -200.0f))};
@@ -198,8 +203,8 @@ __device__ __forceinline__ double exact_prob(const VerifyArgs& a, float v, float
 template <typename T> constexpr uint32_t kBits16 = 0xFC00FC00u;
 template <> constexpr uint32_t kBits16<__nv_bfloat16> = 0xFF80FF80u;
 
-// The sum of share `rank` of `parts` of a row, by THREADS threads side by side; each warp has its own.  Minus infinity stays as
-// it is: the largest logit is kNone at least, so that its distance is no NaN and its exponential 0.
+// The sum of share `rank` of `parts` of a row, by THREADS threads side by side; each warp has its own.  Masked logits stay as
+// they are: the largest is kNone at least, so that their distances are no NaN and their exponentials 0 (unless it is near_masked).
 template <typename T, bool MASK, int THREADS>
 __device__ __forceinline__ Sum scan(const T* z, const uint8_t* ok, int classes, float c, int rank, int parts) {
   constexpr int V = kVec<T>;
@@ -355,7 +360,7 @@ __device__ __noinline__ float lowest_score(const VerifyArgs& a, const T* z, cons
     for (int u = 0; u < kAtOnce; ++u) {
       float off;
       const float s = sc.of(v[u], q[u], e[u], off);
-      if (min(j0 + u * THREADS, a.classes - 1) != hole) low = fmaxf(low, s - fabsf(off));
+      if (v[u] > kNone<T> && min(j0 + u * THREADS, a.classes - 1) != hole) low = fmaxf(low, s - fabsf(off));
     }
   }
 #pragma unroll
@@ -556,11 +561,17 @@ __global__ void __launch_bounds__(ONE ? kOneThreads : kThreads, ONE ? kOneReside
       const int i = i0 + r;
       const Head h = row_head[r];
       bool accepted = row_state[r] == 1;
-      if (row_state[r] == 2) {
+      const bool near = row_sum[r].S > 0.0f && near_masked<T>(row_sum[r].m, a.c);
+      if (near || row_state[r] == 2) {
         const T* z = logits_of<T>(a, seq, i);
         const uint8_t* ok = mask_of(a, seq, i);
         const double sum = exact_sum<T, THREADS>(a, z, ok, row_sum[r].m, part);
-        accepted = static_cast<double>(h.u) * h.q < exact_prob(a, h.zx, row_sum[r].m, sum);
+        accepted = h.zx > kNone<T> && static_cast<double>(h.u) * h.q < exact_prob(a, h.zx, row_sum[r].m, sum);
+        if (near) {
+          __syncthreads();
+          if (tid == 0) row_sum[r].S = static_cast<float>(sum);
+          __syncthreads();
+        }
       }
       if (!accepted) {
         n = i;
@@ -626,7 +637,7 @@ __global__ void __launch_bounds__(ONE ? kOneThreads : kThreads, ONE ? kOneReside
       }
     }
   };
-  if (!dead) {
+  if (!dead && !near_masked<T>(st.m, a.c)) {
     int j0 = c0 + tid;
     for (; j0 + (kScores - 1) * THREADS < c1; j0 += kScores * THREADS) batch(j0, std::true_type());
     if (j0 < c1) batch(j0, std::false_type());

@@ -74,3 +74,26 @@ def test_the_only_class_rejected_beside_masked_ones_far_above_it(B, V, dtype, ab
     z[:, :, 7] = -9.0
     r = check(z, x, u, noise, None, ok.expand(B, 2, V))
     assert (r.tokens[:, 0] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
+@pytest.mark.parametrize("B,V", [(8, 3), (8, 333), (600, 70), (4, 40001)])
+def test_logits_next_to_a_masks_at_the_highest_temperature(B, V, dtype):
+    # -1e30 is a mask's even where 1e27 apart is a factor e
+    g = gen(V)
+    z = -9.9e29 - 9.9e27 * torch.rand(B, 3, V, generator=g, device="cuda")
+    z[torch.rand(B, 3, V, generator=g, device="cuda") < 0.7] = -1.0025e30 if dtype == BF else -1e30
+    z[torch.rand(B, 3, V, generator=g, device="cuda") < 0.1] = -math.inf
+    z[:, :, V // 2] = -9.97e29
+    z = z.to(dtype)
+    assert (z.double()[:, :, V // 2] > -1e30).all()
+    x = torch.full((B, 2), V // 2, dtype=torch.int32, device="cuda")
+    noise = torch.empty(B, V, device="cuda").exponential_(generator=g)
+    u = torch.rand(B, 2, generator=g, device="cuda") * 0.01
+    check(z, x, u, noise, None, None, 1e27)
+    check(z, x, torch.ones_like(u), noise, None, None, 1e27)
+    q = torch.full((B, 2, V), 0.5 / V, device="cuda")
+    check(z, x, torch.ones_like(u), noise, q, None, 1e27)
+    ok = torch.rand(V, generator=g, device="cuda") < 0.8
+    ok[V // 2] = True
+    check(z, x, u, noise, None, ok.expand(B, 3, V), 1e27)
