@@ -41,10 +41,17 @@ constexpr int kScores = 4;                // classes whose scores are in flight
 constexpr int kSumParts = 32;             // CTAs of a row, at most
 constexpr int kScoreParts = 128;          // CTAs of a sequence's scores, at most
 
-// The relative error of a probability e^((z - m) / t) / S with d = (z - m) log2(e) / t, in steps of 2^-22: d takes
-// three roundings of 2^-24 of itself each (times ln 2: |d| / 2), 2^d one step, S the same for a mean |d| that is at most
-// log2 of the classes, 31, and a quarter step for each addition of a sum's chain.
-float slack(int classes, int threads, int elements_a_load) { return 20.0f + (classes / (threads * elements_a_load) + 16) * 0.25f; }
+// The relative error of a probability e^((z - m) / t) / S with d = (z - m) log2(e) / t, in steps of 2^-22: the three roundings of d
+// (c, the difference, the product) are 0.52 |d| of them, and bound() takes |d|.  The others, from above:
+//   S: 1 for its terms' powers and 16 for their d, whose mean |d| is at most log2 of the classes, 31; 1.75 for the additions within
+//      a vector and those of a thread's halves and odd element, 1.5 for its rescaling by that; 7.5 for three joins of warps and CTAs, each
+//      a rescaling and 5 additions; of a chain of vectors 0.25 for each addition, and 1.25 for each rescaling by a new largest
+//      logit, of which a batch of kUnroll vectors has one
+//   p, a score, its bound and their comparison: 1 for 2^d, 0.25 for each of ten roundings
+float slack(int64_t classes, int threads, int elements_a_load) {
+  const int64_t vectors = classes / (static_cast<int64_t>(threads) * elements_a_load) + 1;
+  return 32.0f + 0.25f * static_cast<float>(vectors) + 1.25f * static_cast<float>(vectors / kUnroll + 1);
+}
 __device__ __forceinline__ float bound(float d, float slack) { return 0x1p-22f * (slack + fabsf(d)); }
 
 struct Sum {
@@ -721,10 +728,10 @@ cudaError_t verify_type(VerifyArgs a, cudaStream_t s) {
     (a.allowed ? go(std::true_type()) : go(std::false_type()))<<<static_cast<unsigned>(a.sequences), kOneThreads, 0, s>>>(a);
     return cudaGetLastError();
   }
-  a.slack = slack(a.classes, kThreads, load);
   // several rounds of CTAs for the sums, one for the scores, whose CTAs all look for n first
   a.sum_parts = parts_for(rows, bytes, kSumParts, 152 * kResident * 3);
   a.score_parts = parts_for(a.sequences, a.classes * int64_t(8), kScoreParts, 152 * kResident);
+  a.slack = slack(a.classes / a.sum_parts + 1, kThreads, load);
   const auto sums = a.allowed ? k_verify_sums<T, true> : k_verify_sums<T, false>;
   sums<<<static_cast<unsigned>(rows * a.sum_parts), kThreads, 0, s>>>(a);
   const cudaError_t e = cudaGetLastError();

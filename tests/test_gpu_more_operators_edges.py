@@ -97,3 +97,25 @@ def test_logits_next_to_a_masks_at_the_highest_temperature(B, V, dtype):
     ok = torch.rand(V, generator=g, device="cuda") < 0.8
     ok[V // 2] = True
     check(z, x, u, noise, None, ok.expand(B, 3, V), 1e27)
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
+@pytest.mark.parametrize("V,B", [(128000, 1300), (5000, 700), (2001, 500)])
+def test_logits_that_rise_along_the_row(V, B, dtype):
+    # each batch of a thread has a new largest logit, and the sum is rescaled; u is next to p, a step of 2^-26 to 2^-14 away
+    g = gen(V)
+    for step in (1e-5, 3e-4) if dtype == F else (2e-4,):
+        row = (torch.arange(V, device="cuda") * step).to(dtype)
+        z = row.expand(B, 2, V)
+        lp = torch.log_softmax(row.double(), 0)
+        x = V - 1 - torch.randint(0, 50, (B, 1), generator=g, device="cuda")
+        p = torch.exp(lp[x])
+        away = 2.0 ** (-26 + 12 * torch.rand(B, 1, generator=g, device="cuda", dtype=torch.float64))
+        sign = torch.randint(0, 2, (B, 1), generator=g, device="cuda") * 2 - 1
+        u = (p * (1 + sign * away)).float()
+        noise = torch.ones(1, V, device="cuda").expand(B, V)
+        r = ops.verify_drafts(z, x, u, noise)
+        # the two sides are exact numbers but for 2^-45
+        sure = (u.double() - p).abs() > 2.0 ** -40 * p
+        want = u.double() < p
+        assert torch.equal((r.accepted == 1)[:, None][sure], want[sure])
