@@ -472,7 +472,8 @@ int hier_avg_grad_norm(int tensors, void* const* grads_dev, const int* types, co
  *   probs_dev    [sequences, K, classes] of any HA_TYPE_*, or NULL
  *   allowed_dev  NULL, or one byte a class, not 0 where it is allowed (strides 0: the same for all)
  *   tokens_dev   [sequences, K + 1]: the accepted drafts, the next token, then -1
- *   logp_dev     [sequences, K + 1]: the tokens' log p, 0 where there is none
+ *   logp_dev     [sequences, K + 1]: the tokens' log p, 0 where there is none; rounded once, from a sum of fp32
+ *                exponentials that is off by less than 2^-22 (30 + classes / 200) of it
  *   accepted_dev [sequences]
  * A logit at or below -1e30 counts as not allowed.  A row without an allowed class, or with NaN or +inf among
  * them, rejects its draft; where it is row n, its token is -1 with log p -inf or NaN.

@@ -101,7 +101,7 @@ struct VerifyArgs {
   double inv_temperature;
   float c;                                // log2(e) / temperature
   Two c2;                                 // the same
-  float inv_t;
+  Two inv_t2;                             // 1 / temperature
   float slack;                            // of bound()
   int K, classes;
   int64_t sequences;
@@ -169,6 +169,18 @@ __device__ __forceinline__ Two power(float v, float m, Two c) {
   const float scale = __int_as_float((static_cast<int>(n) + 127) << 23);
   const bool any = p > -120.0f;                              // no branch, so that several are computed side by side
   return {any ? s.hi * scale : 0.0f, any ? s.lo * scale : 0.0f};
+}
+
+// (v - m) / t - log S, rounded once, for v <= m and S >= 1: v - m, its product and the difference are held in two floats, and l, the
+// logarithm in fp32, is made exact by what S e^-l differs from 1.
+__device__ __forceinline__ float log_prob(const VerifyArgs& a, float v, float m, float S) {
+  const float l = logf(S);
+  const Two y = power(-l, 0.0f, two(1.4426950408889634));
+  const float rest = fmaf(S, y.hi, -1.0f) + S * y.lo;        // log S = l + log(1 + rest)
+  const float d = v - m, back = d - v, e = (v - (d - back)) + (-m - back);
+  const float h = d * a.inv_t2.hi, s = h - l, from = s - h;
+  const float low = fmaf(d, a.inv_t2.hi, -h) + fmaf(d, a.inv_t2.lo, e * a.inv_t2.hi);
+  return s + ((h - (s - from)) + (-l - from) + (low - rest));
 }
 
 // The sum of e^((z - m) / t) to about 2^-40, by one CTA; every thread has it.
@@ -584,10 +596,11 @@ __global__ void __launch_bounds__(ONE ? kOneThreads : kThreads, ONE ? kOneReside
         n = i;
         st = row_sum[r];
         drafted = h.draft;
-      } else if (rank == 0 && tid == 0) {
-        a.tokens[row0 + i] = h.draft;
-        a.logp[row0 + i] = fmaf(h.zx - row_sum[r].m, a.inv_t, -logf(row_sum[r].S));
       }
+    }
+    if (rank == 0 && tid < (n < 0 ? rows : n - i0)) {        // a thread an accepted draft
+      a.tokens[row0 + i0 + tid] = row_head[tid].draft;
+      a.logp[row0 + i0 + tid] = log_prob(a, row_head[tid].zx, row_sum[tid].m, row_sum[tid].S);
     }
     __syncthreads();
   }
@@ -695,7 +708,7 @@ __global__ void __launch_bounds__(ONE ? kOneThreads : kThreads, ONE ? kOneReside
     if (i == n) {
       t = dead ? -1 : token;
       if (dead) lp = st.S == 0.0f ? -INFINITY : NAN;
-      else if (t >= 0) lp = fmaf(logit(z, ok, t) - st.m, a.inv_t, -logf(st.S));
+      else if (t >= 0) lp = log_prob(a, logit(z, ok, t), st.m, st.S);
     }
     a.tokens[row0 + i] = t;
     a.logp[row0 + i] = lp;
@@ -798,7 +811,7 @@ extern "C" int hier_avg_verify_drafts(const void* logits_dev, int type, int64_t 
   a.inv_temperature = 1.0 / temperature;
   a.c2 = two(1.4426950408889634 / temperature);
   a.c = a.c2.hi;
-  a.inv_t = static_cast<float>(1.0 / temperature);
+  a.inv_t2 = two(1.0 / temperature);
   a.K = drafts;
   a.sequences = sequences;
   const int64_t rows = sequences * (drafts + int64_t(1));

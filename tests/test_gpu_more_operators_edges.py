@@ -119,3 +119,22 @@ def test_logits_that_rise_along_the_row(V, B, dtype):
         sure = (u.double() - p).abs() > 2.0 ** -40 * p
         want = u.double() < p
         assert torch.equal((r.accepted == 1)[:, None][sure], want[sure])
+
+
+@pytest.mark.parametrize("temperature", [1.0, 0.7, 1.3, 0.37])
+@pytest.mark.parametrize("B,V", [(40, 700), (600, 300), (40, 30011)])
+def test_log_probabilities_are_rounded_once(B, V, temperature):
+    # V - 1 equal classes, whose sum is exact, and the draft's below them by a distance at which the sum does not see it
+    g = gen(V)
+    z = torch.full((B, 2, V), 3.25, device="cuda")
+    z[:, 0, 1] = 3.25 - (25 + 200 * torch.rand(B, generator=g, device="cuda")) * temperature
+    x = torch.ones(B, 1, dtype=torch.int32, device="cuda")
+    noise = torch.ones(B, V, device="cuda")
+    r = ops.verify_drafts(z, x, torch.zeros(B, 1, device="cuda"), noise, temperature=temperature)
+    assert (r.accepted == 1).all() and (r.tokens[:, 0] == 1).all() and (r.tokens[:, 1] == 0).all()
+    s = z.double() / temperature
+    lp = s - torch.logsumexp(s, 2, keepdim=True)
+    want = torch.stack([lp[:, 0, 1], lp[:, 1, 0]], 1)
+    # half a step of the result; the draft's own term is below e^-25 of the sum, and what else is lost below 2^-40
+    tol = 2.0 ** -24 * want.abs() + math.exp(-25) + 2.0 ** -36
+    assert ((r.logp.double() - want).abs() <= tol).all()
