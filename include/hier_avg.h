@@ -428,7 +428,8 @@ int hier_avg_route_backward(const float* dweight_dev, const void* logits_dev, in
  * only its place is overwritten, its sorted row is not written and stays in its group.)
  *   hier_avg_dispatch          xs[place[t, j]] = x[t]
  *   hier_avg_combine           out[t] = sum over j of weight[t, j] y[place[t, j]], in the order of j in fp32
- *                              (weight_dev NULL: 1 each, which is the gradient of dispatch)
+ *                              (weight_dev NULL: 1 each, which is the gradient of dispatch); where there is no place,
+ *                              weight[t, j] times 0, which is NaN where the weight is NaN or infinite
  *   hier_avg_combine_backward  dy[place[t, j]] = weight[t, j] dout[t],  dweight[t, j] = <dout[t], y[place[t, j]]>
  *                              (0 where there is no place)
  *   type                       any HA_TYPE_*, of x, xs, y and dy; out and dout: the same or HA_TYPE_FP32

@@ -3,7 +3,7 @@
 //
 //   dispatch           xs[place[t, j]] = x[t]; zero for the rows that no entry has
 //   dispatch_backward  dx[t] = sum over j of dxs[place[t, j]]
-//   combine            out[t] = sum over j of w[t, j] y[place[t, j]]
+//   combine            out[t] = sum over j of w[t, j] y[place[t, j]], 0 for the y of no place
 //   combine_backward   dy[place[t, j]] = w[t, j] dout[t],  dw[t, j] = <dout[t], y[place[t, j]]>
 //
 // All are bound by the bytes of the sorted rows.  The work goes by tokens: what belongs to a token is
@@ -170,7 +170,7 @@ __device__ __forceinline__ void combine_at(const RowArgs& a, int64_t token, int 
 #pragma unroll
     for (int q = 0; q < AT; ++q) {
       const int64_t p = j0 + q < a.k ? place_of(a, token * a.k + j0 + q) : -1;
-      w[q] = WEIGHTS && p >= 0 ? a.weight[token * a.k + j0 + q] : 0.0f;
+      w[q] = WEIGHTS && j0 + q < a.k ? a.weight[token * a.k + j0 + q] : 0.0f;   // of no place too: a router's NaN shows
       const T* row = static_cast<const T*>(a.sorted) + p * a.sorted_ld;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -423,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_combine_shifted(const __grid_co
 #pragma unroll
       for (int q = 0; q < AT; ++q) {
         const int64_t p = j0 + q < a.k ? place_of(a, it.token * a.k + j0 + q) : -1;
-        w[q] = WEIGHTS && p >= 0 ? a.weight[it.token * a.k + j0 + q] : 0.0f;
+        w[q] = WEIGHTS && j0 + q < a.k ? a.weight[it.token * a.k + j0 + q] : 0.0f;
         const T* row = static_cast<const T*>(a.sorted) + p * a.sorted_ld + r.head;
 #pragma unroll
         for (int u = 0; u < U; ++u) {

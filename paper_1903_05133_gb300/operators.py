@@ -555,7 +555,8 @@ def combine(y: torch.Tensor, place: torch.Tensor, weights: torch.Tensor, out: Op
             out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
     """out[t] = sum over j of weights[t, j] y[place[t, j]], in y's type or fp32.
 
-    y [rows * k, width] fp32, bf16 or fp16, the sorted rows' results; place and weights [rows, k] as of route."""
+    y [rows * k, width] fp32, bf16 or fp16, the sorted rows' results; place and weights [rows, k] as of route.  An entry
+    without a place adds its weight times 0: a token whose logits held NaN has NaN weights, and is NaN here."""
     _need(weights is not None, "weights must be given")
     return _combine("y", y, place, weights, out, out_dtype, stream)
 

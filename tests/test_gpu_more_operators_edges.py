@@ -138,3 +138,34 @@ def test_log_probabilities_are_rounded_once(B, V, temperature):
     # half a step of the result; the draft's own term is below e^-25 of the sum, and what else is lost below 2^-40
     tol = 2.0 ** -24 * want.abs() + math.exp(-25) + 2.0 ** -36
     assert ((r.logp.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("width", [256, 255, 40, 7])
+@pytest.mark.parametrize("dtype", [F, BF, HF])
+@pytest.mark.parametrize("k", [3, 6])
+def test_a_router_with_nan_shows_in_what_it_combines(k, dtype, width):
+    # a token whose logits hold NaN or +inf has no expert, and NaN weights: its output is not 0
+    T, E = 50, 16
+    g = gen(k)
+    z = torch.randn(T, E, generator=g, device="cuda")
+    z[3, 2], z[20, 0] = math.nan, math.inf
+    z[7] = -math.inf                                         # no expert is allowed: nothing is added
+    r = ops.route(z, k)
+    assert (r.experts[[3, 20, 7]] == -1).all() and r.weights[[3, 20]].isnan().all() and (r.weights[7] == 0).all()
+    x = torch.randn(T, width, generator=g, device="cuda").to(dtype)
+    y = ops.dispatch(x, r.place, r.offsets)
+    for kind in {dtype, F}:
+        for stream in (None, torch.cuda.current_stream()):
+            out = ops.combine(y, r.place, r.weights, out_dtype=kind, stream=stream)
+            assert out[[3, 20]].isnan().all() and (out[7] == 0).all()
+            rest = torch.ones(T, dtype=torch.bool, device="cuda")
+            rest[[3, 20]] = False
+            assert out[rest].isfinite().all()
+    # an entry that was dropped adds nothing where its weight is finite
+    place = r.place.clone()
+    place[5, 1] = -1
+    w = r.weights[5].double()
+    w[1] = 0
+    got, each = ops.combine(y, place, r.weights, out_dtype=F)[5].double(), y[r.place[5].long()].double()
+    # k products, each sum rounded, by half a step of the sum of their sizes
+    assert ((got - (w[:, None] * each).sum(0)).abs() <= (k + 1) * 2.0 ** -24 * (w[:, None] * each).abs().sum(0)).all()
