@@ -185,9 +185,10 @@ __global__ void __launch_bounds__(kThreads) k_squares(const __grid_constant__ Ta
   });
 }
 
-// Few chunks' sum, by one warp: 64-bit additions are slow, and each CTA that clips does them by itself.
+// Few chunks' sum, by one warp: 64-bit additions are slow, and each CTA that clips does them by itself.  (The sums are no __restrict__
+// const here and below: the kernel may start while the one before it still writes them, and reads them behind its wait.)
 constexpr int kFewChunks = 1024;
-__device__ __forceinline__ double warp_total(const double* __restrict__ sums, int n) {
+__device__ __forceinline__ double warp_total(const double* sums, int n) {
   double s = 0.0;
 #pragma unroll 8
   for (int c = threadIdx.x & 31; c < n; c += 32) s += sums[c];
@@ -200,8 +201,8 @@ __device__ __forceinline__ float scale_of(double norm, double max_norm) {
 }
 
 // A CTA a learner.
-__global__ void __launch_bounds__(kThreads) k_norm(const double* __restrict__ sums, const __grid_constant__ Ranges r,
-                                                      double max_norm, float* norm, float* scale) {
+__global__ void __launch_bounds__(kThreads) k_norm(const double* sums, const __grid_constant__ Ranges r, double max_norm, float* norm,
+                                                   float* scale) {
   __shared__ double part[kThreads / 32];
   let_next_start();
   wait_for_previous();
