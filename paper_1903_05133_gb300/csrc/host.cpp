@@ -15,6 +15,7 @@
 #include <vector>
 
 #include <ATen/ops/empty.h>
+#include <c10/core/Allocator.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
@@ -76,6 +77,19 @@ std::vector<at::Tensor> make(const Specs& specs, Get get, at::Device device) {
 std::vector<at::Tensor> results(at::Device device, std::initializer_list<Spec> specs) {
   return make(specs, [](const Spec& s) { return std::pair<int, at::IntArrayRef>(s.type, s.sizes); }, device);
 }
+
+// A call's workspace.  It is not the results', which would hold it as long as a caller keeps any of them (128 sequences of 5 drafts:
+// 0.5 MB behind 7 KB), unless it is small: memory of its own takes 2 us (clipping 300 tensors by 6.7 KB of sums 20.0 us a call, 16.5 so).
+constexpr int64_t kSmallWork = 8192;
+struct Work {
+  int64_t bytes;
+  c10::DataPtr own;
+  Work(int64_t n, at::Device device) : bytes(n) {
+    if (n > kSmallWork) own = c10::GetAllocator(device.type())->allocate(static_cast<size_t>(n));
+  }
+  int64_t shared() const { return own.get() ? 0 : bytes; }
+  void* in(const at::Tensor& shared) const { return own.get() ? own.get() : shared.data_ptr(); }
+};
 
 // The first n of them as a tuple.
 PyObject* tuple_of(const std::vector<at::Tensor>& t, size_t n) {
@@ -237,11 +251,13 @@ PyObject* route(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const I G = E * std::max<I>(P_, 1);
   NONE_UNLESS(G <= 1024 && T * k <= I(1) << 27);
   const I bytes = T <= 32 && T * k <= 1024 ? 0 : 4 * 154 * G;           // no less than hier_avg_sort_workspace says
-  const auto r = results(w.device, {{kI32, {T, k}}, {kF32, {T, k}}, {kF32, {T}}, {kI32, {G + 1}}, {kI32, {T, k}}, {kI32, {T * k}}, {kU8, {bytes}}});
+  const Work work(bytes, w.device);
+  const auto r = results(w.device, {{kI32, {T, k}}, {kF32, {T, k}}, {kF32, {T}}, {kI32, {G + 1}}, {kI32, {T, k}}, {kI32, {T * k}},
+                                    {kU8, {work.shared()}}});
   const int s = invoke<const void*, int, I, int, I, int, int, const int*, int, int*, float*, float*, int*, int*, int*, P, I, P>(
       g_route, m.p, m.type, T, static_cast<int>(E), m.ld, static_cast<int>(k), PyObject_IsTrue(args[2]) == 1, data<int>(learners),
       static_cast<int>(P_), data<int>(&r[0]), data<float>(&r[1]), data<float>(&r[2]), data<int>(&r[3]), data<int>(&r[4]),
-      data<int>(&r[5]), r[6].data_ptr(), bytes, w.stream);
+      data<int>(&r[5]), work.in(r[6]), bytes, w.stream);
   NONE_UNLESS(s == 0);
   return tuple_of(r, 6);
   END_HANDLE_TH_ERRORS
@@ -369,13 +385,14 @@ PyObject* verify(PyObject*, PyObject* const* args, Py_ssize_t n) {
     NONE_UNLESS(ok->stride(-1) == 1 || V == 1);
   }
   const I bytes = B * (272 * R + 2052);                                 // as hier_avg_verify_workspace says
-  const auto r = results(w.device, {{kI32, {B, R}}, {kI32, {B}}, {kF32, {B, R}}, {kU8, {bytes}}});
+  const Work work(bytes, w.device);
+  const auto r = results(w.device, {{kI32, {B, R}}, {kI32, {B}}, {kF32, {B, R}}, {kU8, {work.shared()}}});
   const int s = invoke<const void*, int, I, int, I, I, I, const void*, int, const float*, const float*, I, const void*, int, I, I,
                        const uint8_t*, I, I, double, int*, int*, float*, P, I, P>(
       g_verify, z->data_ptr(), type_of(*z), B, static_cast<int>(K), V, z->stride(0), z->stride(1), x->data_ptr(),
       x->scalar_type() == at::kInt ? 4 : 8, data<float>(u), data<float>(e), e->stride(0), q ? q->data_ptr() : nullptr,
       q ? type_of(*q) : 0, q ? q->stride(0) : 0, q ? q->stride(1) : 0, data<uint8_t>(ok), ok_seq, ok_row, temperature,
-      data<int>(&r[0]), data<int>(&r[1]), data<float>(&r[2]), r[3].data_ptr(), bytes, w.stream);
+      data<int>(&r[0]), data<int>(&r[1]), data<float>(&r[2]), work.in(r[3]), bytes, w.stream);
   NONE_UNLESS(s == 0);
   return tuple_of(r, 3);
   END_HANDLE_TH_ERRORS
@@ -460,10 +477,11 @@ PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
     pieces += f.elements[i] > 0 ? P_ : 0;
   }
   const I bytes = 8 * (total / (total < 8192 * pieces ? 2048 : 32768) + pieces + 1);
-  const auto r = results(w.device, {{kF32, {P_}}, {kF32, {P_}}, {kU8, {bytes}}});
+  const Work work(bytes, w.device);
+  const auto r = results(w.device, {{kF32, {P_}}, {kF32, {P_}}, {kU8, {work.shared()}}});
   const int s = invoke<int, void* const*, const int*, const I*, int, double, int, float*, float*, P, I, P>(
       g_norm, count, f.address.data(), f.type.data(), f.elements.data(), static_cast<int>(P_), most, clip, data<float>(&r[0]),
-      scaled ? data<float>(&r[1]) : nullptr, r[2].data_ptr(), bytes, w.stream);
+      scaled ? data<float>(&r[1]) : nullptr, work.in(r[2]), bytes, w.stream);
   NONE_UNLESS(s == 0);
   PyObject* out = tuple_of(r, 2);
   if (out && !scaled) {

@@ -8,7 +8,9 @@ include/hier_avg.h without the ``hier_avg_`` prefix.  Results are new tensors un
 is given, and outside autograd: a result has no history even where an input requires gradients, whose
 calls are grouped_product_dx, grouped_product_dw and the functions that end in _backward.  The usual calls of the
 routing, row, norm and draft operators go through the host module at once; what it does not take (another stream, an
-``out``, anything to refuse) goes through the checks here.  All tensors of a
+``out``, anything to refuse) goes through the checks here.  Results of such a call that are below 4 MB together are parts of
+one allocation, which lives as long as any of them (and which torch.save writes as a whole: clone what is to be kept alone).
+All tensors of a
 call are on one GPU, where it runs whichever is current.  A call on ``stream`` makes its results and
 workspace there; its inputs are the caller's to keep until it is done.
 """
@@ -27,6 +29,7 @@ from ._lib import c_int64, c_void_p, check
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _F32, _I32, _U8 = 0, 3, 4       # of results made together
+_SMALL_WORK = 8192              # bytes of a workspace that may share the results' memory
 FORWARD, DX, DW = 0, 1, 2
 _KIND = attrgetter("dtype", "shape")
 _ADDRESS, _CONTIGUOUS, _DEVICE = torch.Tensor.data_ptr, torch.Tensor.is_contiguous, torch.Tensor.get_device
@@ -56,6 +59,13 @@ def _on(stream, t, *others):
 def _empties(like, *specs):
     """New tensors on like's GPU of (type, size, ...) each, in one call (1.6 us each otherwise)."""
     return _lib.host().empties(like, *specs)
+
+
+def _with_workspace(like, n, *specs):
+    """_empties, and n bytes that the results do not hold where they are many (as the host module makes them)."""
+    if n <= _SMALL_WORK:
+        return _empties(like, *specs, (_U8, n))
+    return *_empties(like, *specs), _empties(like, (_U8, n))[0]
 
 
 def _empty(like, rows, cols, dtype):
@@ -430,8 +440,8 @@ def route(logits: torch.Tensor, k: int, over: str = "chosen", learners: Optional
     s, where = _on(stream, logits, learners)
     with where:
         n = _sort_bytes(lib, T, k, G)
-        experts, weights, lse, offsets, place, source, ws = _empties(
-            logits, (_I32, T, k), (_F32, T, k), (_F32, T), (_I32, G + 1), (_I32, T, k), (_I32, T * k), (_U8, n))
+        experts, weights, lse, offsets, place, source, ws = _with_workspace(
+            logits, n, (_I32, T, k), (_F32, T, k), (_F32, T), (_I32, G + 1), (_I32, T, k), (_I32, T * k))
         check(lib.hier_avg_route(
             logits.data_ptr(), TYPES[logits.dtype], T, E, ld, k, every, None if learners is None else learners.data_ptr(), P,
             experts.data_ptr(), weights.data_ptr(), lse.data_ptr(), offsets.data_ptr(), place.data_ptr(),
@@ -484,7 +494,7 @@ def sort_by_group(group: torch.Tensor, groups: int, stream=None) -> Sorted:
     s, where = _on(stream, group)
     with where:
         n = _sort_bytes(lib, T, k, groups)
-        offsets, place, source, ws = _empties(group, (_I32, groups + 1), (_I32, T, k), (_I32, T * k), (_U8, n))
+        offsets, place, source, ws = _with_workspace(group, n, (_I32, groups + 1), (_I32, T, k), (_I32, T * k))
         check(lib.hier_avg_sort_by_group(group.data_ptr(), T, k, groups, offsets.data_ptr(), place.data_ptr(),
                                          source.data_ptr(), ws.data_ptr(), n, s), "sort_by_group")
     return Sorted(offsets, place, source)
@@ -641,7 +651,7 @@ def verify_drafts(logits: torch.Tensor, drafts: torch.Tensor, uniform: torch.Ten
     s, where = _on(stream, logits, drafts, uniform, noise, draft_probs, allowed)
     with where:
         n = B * (272 * R + 2052)                            # as hier_avg_verify_workspace says
-        tokens, accepted, logp, ws = _empties(logits, (_I32, B, R), (_I32, B), (_F32, B, R), (_U8, n))
+        tokens, accepted, logp, ws = _with_workspace(logits, n, (_I32, B, R), (_I32, B), (_F32, B, R))
         check(lib.hier_avg_verify_drafts(
             logits.data_ptr(), TYPES[logits.dtype], B, K, V, *z, drafts.data_ptr(), drafts.element_size(), uniform.data_ptr(),
             noise.data_ptr(), noise_ld, None if draft_probs is None else draft_probs.data_ptr(),
@@ -677,7 +687,7 @@ def _norm(grads, max_norm, learners, clip, stream):
     check(lib.hier_avg_grad_norm_workspace(n, types, sizes, P, ctypes.byref(b)), "grad_norm_workspace")
     s, where = _on(stream, grads[0])
     with where:
-        norm, scale, ws = _empties(grads[0], (_F32, P), (_F32, P), (_U8, b.value))
+        norm, scale, ws = _with_workspace(grads[0], b.value, (_F32, P), (_F32, P))
         if max_norm is None:
             scale = None
         status = lib.hier_avg_grad_norm(n, address, types, sizes, P, 0.0 if max_norm is None else max_norm, clip,

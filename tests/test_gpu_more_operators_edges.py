@@ -169,3 +169,19 @@ def test_a_router_with_nan_shows_in_what_it_combines(k, dtype, width):
     got, each = ops.combine(y, place, r.weights, out_dtype=F)[5].double(), y[r.place[5].long()].double()
     # k products, each sum rounded, by half a step of the sum of their sizes
     assert ((got - (w[:, None] * each).sum(0)).abs() <= (k + 1) * 2.0 ** -24 * (w[:, None] * each).abs().sum(0)).all()
+
+
+def test_kept_results_hold_no_workspace():
+    z, x, u, noise, q, ok = make(200, 5, 1000, BF, F, True, 1.0, 1)
+    for stream in (None, torch.cuda.current_stream()):
+        held = lambda r: max(t.untyped_storage().nbytes() for t in r)  # noqa: E731
+        own = lambda r: sum(-(-t.numel() * t.element_size() // 256) * 256 for t in r)  # noqa: E731
+        r = ops.verify_drafts(z, x, u, noise, draft_probs=q, allowed=ok, stream=stream)
+        assert held(r) <= own(r) + 8192
+        logits = torch.randn(3000, 200, generator=gen(1), device="cuda")
+        r = ops.route(logits, 2, stream=stream)
+        assert held(r) <= own(r) + 8192
+        r = ops.sort_by_group(r.experts, 200, stream=stream)
+        assert held(r) <= own(r) + 8192
+        r = ops.grad_norm([torch.ones(3000, device="cuda") for _ in range(500)], 1.0, stream=stream)
+        assert held(r) <= own(r) + 8192
