@@ -4,7 +4,9 @@ binding's host module ``_host.so``.
 Each translation unit is compiled by nvcc in parallel, then linked with the
 static CUDA runtime into one shared library next to this file.  Arithmetic flags
 are explicit: no fast-math, IEEE division and square root, subnormals kept.
-The host module is compiled by g++ against PyTorch's headers, beside them.
+The host module is compiled by g++ against Python's and PyTorch's headers, beside them.  Where that is not
+possible the library is built all the same: the C ABI needs neither, and _lib.host() raises where the module
+is missing.
 """
 from __future__ import annotations
 
@@ -53,12 +55,23 @@ def _cuda_include() -> str:
 
 def _host_command(out: str):
     """g++ on csrc/host.cpp; the libraries are those that ``import torch`` has loaded."""
-    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
+        raise RuntimeError("PyTorch not found")
+    torch = spec.submodule_search_locations[0]
     inc, lib = os.path.join(torch, "include"), os.path.join(torch, "lib")
     return [os.environ.get("CXX") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-o", out,
             os.path.join(CSRC, "host.cpp"), f"-I{sysconfig.get_paths()['include']}", f"-isystem{inc}",
             f"-isystem{os.path.join(inc, 'torch', 'csrc', 'api', 'include')}", f"-L{lib}", f"-isystem{_cuda_include()}",
             "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+
+
+def _compile_host():
+    """What stands in the way of the host module, or None where it is compiled (to HOST_PATH.tmp)."""
+    try:
+        _run(_host_command(HOST_PATH + ".tmp"))
+    except (RuntimeError, OSError) as e:
+        return e
 
 
 def build(verbose: bool = False, ptxas_info: bool = False) -> str:
@@ -72,16 +85,23 @@ def build(verbose: bool = False, ptxas_info: bool = False) -> str:
             cmd += ["-Xptxas", "-v"]
         objs.append(obj)
         cmds.append(cmd)
-    cmds.append(_host_command(HOST_PATH + ".tmp"))
-    with ThreadPoolExecutor(max_workers=len(cmds)) as ex:
+    with ThreadPoolExecutor(max_workers=len(cmds) + 1) as ex:
+        host = ex.submit(_compile_host)
         outs = list(ex.map(_run, cmds))
     if verbose or ptxas_info:
         for o in outs:
             sys.stdout.write(o)
     tmp = LIB_PATH + ".tmp"
     _run([nvcc, *ARCH, "-shared", "--cudart", "static", "-o", tmp, *objs])
-    os.replace(HOST_PATH + ".tmp", HOST_PATH)
     os.replace(tmp, LIB_PATH)
+    missing = host.result()
+    if missing is None:
+        os.replace(HOST_PATH + ".tmp", HOST_PATH)
+    else:
+        if os.path.exists(HOST_PATH):           # of another build
+            os.remove(HOST_PATH)
+        sys.stderr.write(f"{LIB_PATH} is built, the Python binding's host module is not, which the routing, row, norm and "
+                         f"draft operators of the binding need: {missing}\n")
     return LIB_PATH
 
 

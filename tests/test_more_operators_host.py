@@ -27,3 +27,49 @@ def test_results_hold_no_workspace(noting):
     r = noting.norm([torch.zeros(4, 3000, dtype=BF)] * 500, 1.0, 4, False)
     assert len(r) == 2 and held(r)[0] <= held(r)[1] + 8192 and r[0].dtype == F
     assert noting.pretend(True)[10] > 8192                   # (which is there all the same)
+
+
+def test_the_library_is_built_without_the_host_modules_compiler(monkeypatch, tmp_path, capsys):
+    import os
+
+    from paper_1903_05133_gb300 import _build
+    ran = []
+
+    def run(cmd):
+        """Each command's result is made; the host module's compiler finds no header."""
+        ran.append(cmd)
+        if os.path.join(_build.CSRC, "host.cpp") in cmd:
+            raise RuntimeError("Python.h: No such file or directory")
+        open(cmd[cmd.index("-o") + 1], "w").close()
+        return ""
+
+    def no_compiler(cmd):
+        if os.path.join(_build.CSRC, "host.cpp") in cmd:
+            raise FileNotFoundError("g++")
+        return run(cmd)
+
+    def no_pytorch(out):
+        raise RuntimeError("PyTorch not found")
+    monkeypatch.setattr(_build, "BUILD_DIR", str(tmp_path / "build"))
+    monkeypatch.setattr(_build, "LIB_PATH", str(tmp_path / "libhier_avg.so"))
+    monkeypatch.setattr(_build, "HOST_PATH", str(tmp_path / "_host.so"))
+    for runs, command in ((run, None), (no_compiler, None), (run, no_pytorch)):
+        (tmp_path / "_host.so").write_text("of an older build")
+        monkeypatch.setattr(_build, "_run", runs)
+        if command:
+            monkeypatch.setattr(_build, "_host_command", command)
+        assert _build.build() == str(tmp_path / "libhier_avg.so")
+        assert (tmp_path / "libhier_avg.so").exists() and not (tmp_path / "_host.so").exists()
+        assert "host module" in capsys.readouterr().err
+        (tmp_path / "libhier_avg.so").unlink()
+    monkeypatch.setattr(ops._lib, "_host", None)             # and its absence is an error where it is used
+    with pytest.raises(RuntimeError, match="missing"):
+        ops._lib.host()
+    # what the library itself needs is an error still
+
+    def no_nvcc(cmd):
+        raise RuntimeError("command failed")
+    monkeypatch.setattr(_build, "_run", no_nvcc)
+    with pytest.raises(RuntimeError, match="command failed"):
+        _build.build()
+    assert not (tmp_path / "libhier_avg.so").exists()
