@@ -28,10 +28,11 @@ namespace {
 constexpr at::ScalarType kTypes[] = {at::kFloat, at::kBFloat16, at::kHalf, at::kInt, at::kByte};
 constexpr int kF32 = 0, kI32 = 3, kU8 = 4;
 
-// The C ABI's functions, and for tests: CPU tensors stand for a GPU's, and calls are noted in `noted` instead of made.
+// The C ABI's functions, and for tests, of the thread that asks for it: CPU tensors stand for a GPU's, and their calls are noted
+// in `noted` instead of made.  Calls on a GPU's tensors are made all the same.
 void *g_route, *g_route_backward, *g_dispatch, *g_combine, *g_combine_backward, *g_verify, *g_norm;
-bool g_pretend = false;
-PyObject* g_noted = nullptr;
+thread_local bool g_pretend = false;
+thread_local PyObject* g_noted = nullptr;
 
 // ---------------------------------------------------------------- results
 // Results of a call that are small together are parts of one allocation, each from a multiple of 256 bytes on: an
@@ -152,7 +153,7 @@ int type_of(const at::Tensor& t) {
     if (kTypes[i] == t.scalar_type()) return i;
   return -1;
 }
-bool plain(const at::Tensor& t) { return t.layout() == at::kStrided && (t.is_cuda() || g_pretend); }
+bool plain(const at::Tensor& t) { return t.layout() == at::kStrided && (t.is_cuda() || (g_pretend && t.is_cpu())); }
 
 // What a call's tensors have to share: the current GPU.
 struct Where {
@@ -162,7 +163,7 @@ struct Where {
   explicit Where(const at::Tensor& t) {
     if (!plain(t)) return;
     device = t.device();
-    if (!g_pretend) {
+    if (t.is_cuda()) {
       if (device.index() != c10::cuda::current_device()) return;
       stream = c10::cuda::getCurrentCUDAStream(device.index()).stream();
     }
@@ -214,8 +215,8 @@ PyObject* number(A a) {
   else return PyLong_FromLongLong(static_cast<long long>(a));
 }
 template <typename... A>
-int invoke(void* f, A... a) {
-  if (g_pretend) {
+int invoke(const Where& w, void* f, A... a) {
+  if (w.device.is_cpu()) {
     Py_XDECREF(g_noted);
     g_noted = PyTuple_New(sizeof...(A));
     Py_ssize_t i = 0;
@@ -255,7 +256,7 @@ PyObject* route(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const auto r = results(w.device, {{kI32, {T, k}}, {kF32, {T, k}}, {kF32, {T}}, {kI32, {G + 1}}, {kI32, {T, k}}, {kI32, {T * k}},
                                     {kU8, {work.shared()}}});
   const int s = invoke<const void*, int, I, int, I, int, int, const int*, int, int*, float*, float*, int*, int*, int*, P, I, P>(
-      g_route, m.p, m.type, T, static_cast<int>(E), m.ld, static_cast<int>(k), PyObject_IsTrue(args[2]) == 1, data<int>(learners),
+      w, g_route, m.p, m.type, T, static_cast<int>(E), m.ld, static_cast<int>(k), PyObject_IsTrue(args[2]) == 1, data<int>(learners),
       static_cast<int>(P_), data<int>(&r[0]), data<float>(&r[1]), data<float>(&r[2]), data<int>(&r[3]), data<int>(&r[4]),
       data<int>(&r[5]), work.in(r[6]), bytes, w.stream);
   NONE_UNLESS(s == 0);
@@ -280,7 +281,7 @@ PyObject* route_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
               (!lse || exact(lse, w, at::kFloat, {T})));
   const auto r = results(w.device, {{m.type, {T, E}}});
   const int s = invoke<const float*, const void*, int, I, int, I, int, int, const int*, const float*, const float*, P, I, P>(
-      g_route_backward, data<float>(dw), m.p, m.type, T, static_cast<int>(E), m.ld, static_cast<int>(k), all, data<int>(e),
+      w, g_route_backward, data<float>(dw), m.p, m.type, T, static_cast<int>(E), m.ld, static_cast<int>(k), all, data<int>(e),
       data<float>(wt), data<float>(lse), r[0].data_ptr(), E, w.stream);
   NONE_UNLESS(s == 0);
   return THPVariable_Wrap(r[0]);
@@ -299,7 +300,7 @@ PyObject* dispatch(PyObject*, PyObject* const* args, Py_ssize_t n) {
   NONE_UNLESS(w.ok && matrix(x, w, m) && places(place, w, T, k) && offsets(off, w, G) && m.rows == T && m.cols <= 0x7FFFFFFF);
   const auto r = results(w.device, {{m.type, {T * k, m.cols}}});
   const int s = invoke<const void*, int, I, int, I, const int*, int, const int*, int, P, I, P>(
-      g_dispatch, m.p, m.type, T, static_cast<int>(m.cols), m.ld, data<int>(place), static_cast<int>(k), data<int>(off),
+      w, g_dispatch, m.p, m.type, T, static_cast<int>(m.cols), m.ld, data<int>(place), static_cast<int>(k), data<int>(off),
       static_cast<int>(G), r[0].data_ptr(), m.cols, w.stream);
   NONE_UNLESS(s == 0);
   return THPVariable_Wrap(r[0]);
@@ -326,7 +327,7 @@ PyObject* combine(PyObject*, PyObject* const* args, Py_ssize_t n) {
   }
   const auto r = results(w.device, {{type, {T, m.cols}}});
   const int s = invoke<const void*, int, I, int, I, const int*, int, const float*, P, I, int, P>(
-      g_combine, m.p, m.type, T, static_cast<int>(m.cols), m.ld, data<int>(place), static_cast<int>(k), data<float>(wt),
+      w, g_combine, m.p, m.type, T, static_cast<int>(m.cols), m.ld, data<int>(place), static_cast<int>(k), data<float>(wt),
       r[0].data_ptr(), m.cols, type, w.stream);
   NONE_UNLESS(s == 0);
   return THPVariable_Wrap(r[0]);
@@ -347,7 +348,7 @@ PyObject* combine_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
               exact(wt, w, at::kFloat, {T, k}));
   const auto r = results(w.device, {{m.type, {T * k, m.cols}}, {kF32, {T, k}}});
   const int s = invoke<const void*, int, I, const void*, int, I, int, I, const int*, int, const float*, const int*, int, P, I, float*, P>(
-      g_combine_backward, d.p, d.type, d.ld, m.p, m.type, T, static_cast<int>(m.cols), m.ld, data<int>(place),
+      w, g_combine_backward, d.p, d.type, d.ld, m.p, m.type, T, static_cast<int>(m.cols), m.ld, data<int>(place),
       static_cast<int>(k), data<float>(wt), data<int>(off), static_cast<int>(G), r[0].data_ptr(), m.cols, data<float>(&r[1]),
       w.stream);
   NONE_UNLESS(s == 0);
@@ -389,7 +390,7 @@ PyObject* verify(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const auto r = results(w.device, {{kI32, {B, R}}, {kI32, {B}}, {kF32, {B, R}}, {kU8, {work.shared()}}});
   const int s = invoke<const void*, int, I, int, I, I, I, const void*, int, const float*, const float*, I, const void*, int, I, I,
                        const uint8_t*, I, I, double, int*, int*, float*, P, I, P>(
-      g_verify, z->data_ptr(), type_of(*z), B, static_cast<int>(K), V, z->stride(0), z->stride(1), x->data_ptr(),
+      w, g_verify, z->data_ptr(), type_of(*z), B, static_cast<int>(K), V, z->stride(0), z->stride(1), x->data_ptr(),
       x->scalar_type() == at::kInt ? 4 : 8, data<float>(u), data<float>(e), e->stride(0), q ? q->data_ptr() : nullptr,
       q ? type_of(*q) : 0, q ? q->stride(0) : 0, q ? q->stride(1) : 0, data<uint8_t>(ok), ok_seq, ok_row, temperature,
       data<int>(&r[0]), data<int>(&r[1]), data<float>(&r[2]), work.in(r[3]), bytes, w.stream);
@@ -399,6 +400,7 @@ PyObject* verify(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 // ---------------------------------------------------------------- lists of gradients
+constexpr int64_t kPretended = 1 << 20;  // the device of CPU tensors that stand for a GPU's
 struct Facts {
   std::vector<void*> address;
   std::vector<int> type;
@@ -415,10 +417,10 @@ Facts read(PyObject* seq) {
   for (Py_ssize_t i = 0; i < n; ++i) {
     const at::Tensor* t = tensor(PySequence_Fast_GET_ITEM(seq, i));
     if (!t) f.device = -4;
-    else if (!t->is_cuda() && !g_pretend) f.device = -1;
+    else if (!t->is_cuda() && !(g_pretend && t->is_cpu())) f.device = -1;
     else if (type_of(*t) < 0 || t->layout() != at::kStrided || !t->is_contiguous()) f.device = -3;
-    else if (f.device != -5 && !g_pretend && f.device != t->get_device()) f.device = -2;
-    else f.device = g_pretend ? 0 : t->get_device();
+    else if (const int64_t d = t->is_cuda() ? t->get_device() : kPretended; f.device != -5 && f.device != d) f.device = -2;
+    else f.device = d;
     if (f.device < 0) return f;
     f.address[i] = t->data_ptr();
     f.type[i] = type_of(*t);
@@ -480,7 +482,7 @@ PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const Work work(bytes, w.device);
   const auto r = results(w.device, {{kF32, {P_}}, {kF32, {P_}}, {kU8, {work.shared()}}});
   const int s = invoke<int, void* const*, const int*, const I*, int, double, int, float*, float*, P, I, P>(
-      g_norm, count, f.address.data(), f.type.data(), f.elements.data(), static_cast<int>(P_), most, clip, data<float>(&r[0]),
+      w, g_norm, count, f.address.data(), f.type.data(), f.elements.data(), static_cast<int>(P_), most, clip, data<float>(&r[0]),
       scaled ? data<float>(&r[1]) : nullptr, work.in(r[2]), bytes, w.stream);
   NONE_UNLESS(s == 0);
   PyObject* out = tuple_of(r, 2);

@@ -185,3 +185,17 @@ def test_kept_results_hold_no_workspace():
         assert held(r) <= own(r) + 8192
         r = ops.grad_norm([torch.ones(3000, device="cuda") for _ in range(500)], 1.0, stream=stream)
         assert held(r) <= own(r) + 8192
+
+
+def test_noting_calls_leaves_calls_on_the_gpu_alone():
+    from paper_1903_05133_gb300 import _lib
+    host = _lib.host()
+    z = torch.randn(6, 20, generator=gen(1), device="cuda")
+    want = ops.route(z, 3)
+    host.pretend(True)
+    try:
+        got = ops.route(z, 3)
+        norm = ops.grad_norm([torch.full((4,), 3.0, device="cuda")]).norm
+    finally:
+        noted = host.pretend(False)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and norm.item() == 6.0 and noted is None

@@ -73,3 +73,15 @@ def test_the_library_is_built_without_the_host_modules_compiler(monkeypatch, tmp
     with pytest.raises(RuntimeError, match="command failed"):
         _build.build()
     assert not (tmp_path / "libhier_avg.so").exists()
+
+
+def test_calls_are_noted_for_the_thread_that_asks(noting):
+    import threading
+    z = torch.zeros(3, 4)
+    assert noting.route(z, 2, False, None) is not None
+    other = []
+    t = threading.Thread(target=lambda: other.append((noting.route(z, 2, False, None), noting.pretend(False))))
+    t.start()
+    t.join()
+    assert other == [(None, None)]                           # a CPU tensor is none of a GPU there
+    assert len(noting.pretend(True)) == 18                   # and the call that was noted here is still there
