@@ -6,7 +6,9 @@ Argument marshalling only, as in hier_avg.py: PyTorch provides the memory and th
 computation runs in the library's CUDA kernels, and the functions are those of
 include/hier_avg.h without the ``hier_avg_`` prefix.  Results are new tensors unless ``out``
 is given, and outside autograd: a result has no history even where an input requires gradients, whose
-calls are grouped_product_dx, grouped_product_dw and the functions that end in _backward.  The usual calls of the
+calls are grouped_product_dx, grouped_product_dw and the functions that end in _backward.  Autograd does not see
+what is written into an ``out``, by clip_gradients or by AdamW.step either (no version counter moves): such a tensor must
+not be saved for a backward pass that is still to come.  The usual calls of the
 routing, row, norm and draft operators go through the host module at once; what it does not take (another stream, an
 ``out``, anything to refuse) goes through the checks here.  Results of such a call that are below 4 MB together are parts of
 one allocation, which lives as long as any of them (and which torch.save writes as a whole: clone what is to be kept alone).
@@ -707,8 +709,9 @@ def grad_norm(grads: Sequence[torch.Tensor], max_norm: Optional[float] = None, l
 
 
 def clip_gradients(grads: Sequence[torch.Tensor], max_norm: float, learners: Optional[int] = None, stream=None) -> GradNorm:
-    """grad_norm, and the gradients multiplied by their factor in place (where it is not 1).  They must not
-    share memory.  AdamW.step(grads, lr, grad_scale=grad_norm(grads, max_norm).scale) does the same without this pass."""
+    """grad_norm, and the gradients multiplied by their factor in place (where it is not 1), unseen by
+    autograd.  They must not share memory.
+    AdamW.step(grads, lr, grad_scale=grad_norm(grads, max_norm).scale) does the same without this pass."""
     _need(max_norm is not None, "max_norm must be given")
     return _norm(grads, max_norm, learners, True, stream)
 
