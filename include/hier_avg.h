@@ -433,7 +433,7 @@ int hier_avg_route_backward(const float* dweight_dev, const void* logits_dev, in
  *   hier_avg_combine_backward  dy[place[t, j]] = weight[t, j] dout[t],  dweight[t, j] = <dout[t], y[place[t, j]]>
  *                              (0 where there is no place)
  *   type                       any HA_TYPE_*, of x, xs, y and dy; out and dout: the same or HA_TYPE_FP32
- * Errors: HA_EINVAL, HA_EUNSUPPORTED for 2^31 entries, HA_ECUDA. */
+ * Errors: HA_EINVAL, HA_EUNSUPPORTED for 2^31 entries or rows of more than 2^30 elements, HA_ECUDA. */
 int hier_avg_dispatch(const void* x_dev, int type, int64_t rows, int width, int64_t x_ld, const int32_t* place_dev,
                       int per_row, const int32_t* offsets_dev, int groups, void* xs_dev, int64_t xs_ld, void* stream);
 int hier_avg_combine(const void* y_dev, int type, int64_t rows, int width, int64_t y_ld, const int32_t* place_dev,

@@ -618,9 +618,11 @@ cudaError_t combine_backward_type(const RowArgs& a, bool vec, cudaStream_t s) {
   return vec ? launch_combine_backward<T, O, kVec<T>, 1, 8>(a, s) : launch_combine_backward<T, O, 1, kSingleSums / 2, 8>(a, s);
 }
 
+// A thread's next column, which is up to a row and a share of one on, has to fit 32 bits.
+constexpr int kMaxWidth = 1 << 30;
 int shape_status(int type, int64_t rows, int width, int k) {
   if (!type_ok(type) || rows < 0 || width < 1 || k < 1) return HA_EINVAL;
-  return rows > 0x7FFFFFFF / k ? HA_EUNSUPPORTED : HA_OK;
+  return width > kMaxWidth || rows > 0x7FFFFFFF / k ? HA_EUNSUPPORTED : HA_OK;
 }
 bool rows_ok(const void* p, int64_t ld, int width, int type) {
   return ld >= width && reinterpret_cast<uintptr_t>(p) % type_size(type) == 0;

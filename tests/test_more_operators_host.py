@@ -85,3 +85,20 @@ def test_calls_are_noted_for_the_thread_that_asks(noting):
     t.join()
     assert other == [(None, None)]                           # a CPU tensor is none of a GPU there
     assert len(noting.pretend(True)) == 18                   # and the call that was noted here is still there
+
+
+def test_rows_beyond_2_30_elements_are_refused(lib):
+    # A row's columns are counted in 32 bits: with a thread for four single elements, the column behind a row of 2^31 - 1 is
+    # the first, at most 2^29 - 1, and 2^31 more.
+    from test_operators_abi import EUNSUPPORTED, P
+    for width, status in ((1 << 30, 0), ((1 << 30) + 1, EUNSUPPORTED), ((1 << 31) - 1, EUNSUPPORTED)):
+        for rows in (0, 1) if status else (0,):
+            for kind in (0, 1):
+                assert lib.hier_avg_dispatch(P, kind, rows, width, width, P, 1, P, 1, P, width, None) == status
+                assert lib.hier_avg_combine(P, kind, rows, width, width, P, 1, P, P, width, kind, None) == status
+                assert lib.hier_avg_combine_backward(P, kind, width, P, kind, rows, width, width, P, 1, P, P, 1, P, width, P, None) == status
+    # what is allowed stays in 32 bits: V elements a part, U parts a thread, the last read of a thread without parts left
+    for V, U in ((1, 4), (1, 8), (4, 1), (4, 2), (8, 1), (8, 2), (8, 4)):
+        parts = (1 << 30) // V
+        lanes = -(-parts // U)
+        assert lanes - 1 + lanes * U < 1 << 31 and (lanes - 1 + (U - 1) * lanes) * V < 1 << 31
