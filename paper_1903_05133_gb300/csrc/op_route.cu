@@ -615,8 +615,8 @@ size_t sort_smem(int warps, int groups, int64_t per) {
   return sizeof(int) * (static_cast<size_t>(warps) * groups + groups + 1 + (per <= kStaged ? per : 0));
 }
 
-// With few groups the places' kernel adds up the counts, else a third one: 1000 rows of 64 experts 7.5 us so and 8.3 with
-// three kernels, 16384 of 128 experts 14.3 and 16.0, of 200 18.9 and 16.1, of 1024 65 and 53.
+// With few groups the places' kernel adds up the counts, else a third one.  A route of 8 chosen fp32 so and with three kernels: 1000
+// rows of 64 experts 8.7 and 9.5 us, 16384 of 128 14.4 and 15.4, of 200 19.2 both, of 1024 46.7 and 36.3.
 cudaError_t end_sort(const SortArgs& a, cudaStream_t s) {
   const unsigned chunks = static_cast<unsigned>(a.chunks);
   if (a.c_step > 1) return launch_early(k_place<true>, chunks, kWarps * 32, 0, s, a);

@@ -9,7 +9,7 @@
 // All are bound by the bytes of the sorted rows.  The work goes by tokens: what belongs to a token is
 // read once, and its entries' rows, which nobody else has, by 16 bytes a thread with as many loads in
 // flight as a token has entries.  Sums are in fp32, in the order of j.  8192 tokens of 4 entries of 4096 bf16:
-// dispatch 51.3 us, combine 55.1 (336 MB: 6.5 and 6.1 TB/s, the copy's rate is 6.75), its gradient 90.0 (604 MB, 6.7).
+// dispatch 51.3 us, combine 52.5 (336 MB: 6.5 and 6.4 TB/s, the copy's rate is 6.75), its gradient 89.6 (604 MB, 6.7).
 #include <algorithm>
 #include <climits>
 #include <type_traits>
@@ -22,7 +22,8 @@ namespace {
 constexpr int kThreads = 256;
 // Parts of a row that a thread has in flight at a time, for 16-byte parts and for single elements.  8192 tokens of 4 entries of
 // 4096 bf16: combine takes 55.1 us with 2 parts (four CTAs an SM; 76 with five, whose registers spill), 57.1 with one and 53.5
-// with four, which fewer tokens do not fill the GPU with.  Rows that are read once do not stay in L2 (58.1 where they do).
+// with four, which fewer tokens do not fill the GPU with.  Rows that are read once do not stay in L2 (58.1 where they do).  (52.5 with
+// two since the weights' loads do not wait for the places.)
 constexpr int kWide = 2, kSingle = 8;
 constexpr int kSingleSums = 4;            // of combine's gradient: 3001 tokens of 4 odd entries of 1111 fp32 25 us, 33 with 8
 

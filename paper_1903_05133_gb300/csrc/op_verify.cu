@@ -10,8 +10,8 @@
 // shares of all rows: their largest logit and the sum of the exponentials.  The second joins them, finds n, and takes shares of
 // row n's scores; the last CTA of a sequence to end joins those.  Rows behind a rejected draft are summed for nothing, but a row
 // waits for no other: 128 sequences of 6 rows of 50021 fp32 logits under a mask take 54 us so, 57 where CTAs ask before they start
-// whether a draft has failed, and 95 by a cluster a sequence that takes its rows in turn and stops.  Both kernels are bound by the
-// instructions of an element, about as long as the memory takes (54 us against 41 for all the bytes).
+// whether a draft has failed, and 95 by a cluster a sequence that takes its rows in turn and stops.  Both kernels wait
+// for memory (issue slots 34 and 40 % full, DRAM 67 and 34 %): 53 us against 41 for all the bytes.
 // Sums and scores are in fp32, with a bound of what that may be off; a decision within the bound is made
 // again by one CTA, in 64 bits but for the sum of the exponentials, which pairs of floats hold to 2^-40.
 #include <algorithm>
@@ -32,7 +32,7 @@ constexpr int kResident = 8;              // CTAs of an SM
 // rows of 1001: 34 us, against 19.6 in two kernels).  One CTA against two kernels, bf16, in us:
 //   1 sequence, 5 rows of 1001: 5.4, 7.2;  of 8192: 8.1, 8.2;  of 16384: 11.1, 8.3;  8 sequences, 10 rows of 8192: 10.8, 10.3
 //   64 sequences, 5 rows of 1001: 6.6, 8.8;  of 16384: 15.0, 16.6;  fp32, of 32001: 24.8, 21.0;  256, 4 rows of 8192: 11.0, 16.4
-// Two CTAs an SM: one takes 13.9 us for the last, three spill, 12.2.
+// Two CTAs an SM, 64 registers, of which 36 bytes spill: the last takes 11.4 us; one (nothing spills) 14.0, three (132 to 224 bytes) 12.2.
 constexpr int kOneThreads = 512, kOneResident = 2, kOneSequences = 512, kFilled = 64;
 constexpr int kOneClasses = 8192, kOneElements = 5 * 8192;             // of fewer than kFilled sequences
 constexpr int kManyClasses = 16384, kManyElements = 8 * 16384;
